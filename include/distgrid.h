@@ -35,6 +35,7 @@ extern "C" {
 
 #define DG_F32 0u
 #define DG_F16 1u
+#define DG_BF16 2u                /* layer norm, recurrence and dropout only */
 #define DG_MAX_LEVELS 16
 #define DG_MAX_PARTITIONS 64
 
@@ -510,6 +511,73 @@ int dg_composite_ragged_depth(const float *sigma, const float *delta, const floa
 int dg_composite_ragged_bwd(const float *sigma, const float *rgb, const float *delta, uint32_t n_seg,
                             const uint32_t *first, const uint32_t *seg_ray, const uint32_t *seg_slot, uint32_t k_max,
                             const float *gCk, const float *gTk, float *dsigma, float *drgb, void *stream);
+
+/* ------------------------------------------------------------------------------------
+ * A sequence block along the samples of rays: layer norm, a gated linear recurrence and
+ * dropout, each with its backward pass.  Sec. 4.3 composites a ray's samples by the
+ * recurrence C <- C + T alpha c, T <- T (1 - alpha) with one gate for all channels and
+ * merges segments by carrying (C, T) across; these operators do the same to features with
+ * a gate per channel, so that samples see each other before the networks.
+ * Rows are tokens (samples), dtype DG_F32, DG_F16 or DG_BF16 is that of every `void *`
+ * array; consecutive values of a row lie next to each other, rows ld (>= W) values apart,
+ * so an array may be a range of columns of a wider one; any element-aligned address is
+ * taken.  Everything is computed in fp32 and rounded once, to the nearest even value.
+ * Results do not depend on how the work is spread: the same call gives the same bits.
+ * ---------------------------------------------------------------------------------- */
+
+/* Layer norm of N rows of W values, m the mean of a row, s = 1 / sqrt(mean((x - m)^2) + eps):
+ *   y = (x - m) s gamma + beta.   gamma, beta [W] fp32; NULL: 1 and 0.  y may be x.
+ * Errors: DG_ERR_ARG for W == 0, eps < 0 or not finite, ld < W; DG_ERR_UNSUPPORTED for more than 2^32 rows, W > 2^20. */
+int dg_layer_norm_fwd(const void *x, uint64_t ldx, const float *gamma, const float *beta, uint64_t N, uint32_t W,
+                      float eps, uint32_t dtype, void *y, uint64_t ldy, void *stream);
+/* Its backward pass, from x again (nothing of the forward pass is kept), xh = (x - m) s, g = dy gamma:
+ *   dx = s (g - mean(g) - xh mean(g xh)),  dgamma = sum over rows of dy xh,  dbeta = sum over rows of dy.
+ * dgamma, dbeta [W] fp32, overwritten (0 for N == 0); each of dx, dgamma, dbeta may be NULL; dx may be dy.
+ * ws: dg_layer_norm_bwd_workspace_bytes(N, W) bytes, 16-byte aligned (not needed without dgamma and dbeta). */
+size_t dg_layer_norm_bwd_workspace_bytes(uint64_t N, uint32_t W);
+int dg_layer_norm_bwd(const void *x, uint64_t ldx, const float *gamma, const void *dy, uint64_t lddy, uint64_t N,
+                      uint32_t W, float eps, uint32_t dtype, void *dx, uint64_t lddx, float *dgamma, float *dbeta,
+                      void *ws, size_t ws_bytes, void *stream);
+
+/* Gated linear recurrence of W channels along n_seq sequences of rows, N rows in all:
+ *   a = 1 / (1 + e^-z),  h_t = a_t h_{t-1} + (1 - a_t) u_t,  y_t = h_t,   h before the first token: h0, or 0 if NULL.
+ * z gates, u inputs, y outputs [N, W]; h0, h_last [n_seq, W] fp32, either may be NULL; h_last receives the state after the
+ * last token (h0 for a sequence without one) and may be h0.  One token per sequence (N == n_seq) is the step of a
+ * program that gets its tokens one after the other.
+ * first NULL: every sequence has N / n_seq rows.  Otherwise sequence j has rows [first[j], first[j+1]) (n_seq + 1 ascending
+ * offsets on the device, as dg_march_segments writes them); N is then the number of rows that there is room for: rows that no
+ * sequence has are neither read nor written, rows from N on neither, whatever `first` says.
+ * reverse != 0: every sequence from its last row to its first; h0 is the state behind the last row.
+ * From |z| = 88 on a gate is exactly 0 or 1, and what it shuts out is not looked at, not even infinities or NaN: z >= 88
+ * (+infinity) passes a token over, z <= -88 (-infinity, the lowest value of a type) forgets the past.  z NaN gives NaN.
+ * states: NULL, or dg_recurrence_state_count(N, W) floats for the backward pass (the state at every 16th row).
+ * ws: dg_recurrence_workspace_bytes(N, n_seq, W) bytes (NULL where that is 0), 16-byte aligned.
+ * Errors: DG_ERR_ARG also for N that n_seq does not divide (first NULL); DG_ERR_UNSUPPORTED for N >= 2^32, W > 2^20. */
+size_t dg_recurrence_state_count(uint64_t N, uint32_t W);
+size_t dg_recurrence_workspace_bytes(uint64_t N, uint32_t n_seq, uint32_t W);
+int dg_recurrence_fwd(const void *z, uint64_t ldz, const void *u, uint64_t ldu, uint64_t N, uint32_t n_seq,
+                      const uint32_t *first, uint32_t W, uint32_t reverse, uint32_t dtype, const float *h0, void *y,
+                      uint64_t ldy, float *h_last, float *states, void *ws, size_t ws_bytes, void *stream);
+/* Its backward pass; arguments of the forward pass as they were then, states as it left them.  With the gradient
+ *   G_t = dy_t + a_{t+1} G_{t+1}  of h_t  (dh_last [n_seq, W], or 0 if NULL, added at the last token):
+ *   du = (1 - a) G,  dz = a (1 - a) (h_{t-1} - u_t) G,  dh0 = a_0 G_0 (NULL: not wanted; dh_last for a sequence without a
+ *   token; it may be dh_last).  dz, du [N, W], overwritten; behind a shut gate they are 0. */
+int dg_recurrence_bwd(const void *z, uint64_t ldz, const void *u, uint64_t ldu, uint64_t N, uint32_t n_seq,
+                      const uint32_t *first, uint32_t W, uint32_t reverse, uint32_t dtype, const float *h0,
+                      const float *states, const void *dy, uint64_t lddy, const float *dh_last, void *dz,
+                      uint64_t lddz, void *du, uint64_t lddu, float *dh0, void *ws, size_t ws_bytes, void *stream);
+
+/* Dropout of n values (contiguous): y_i = 0 if value i is dropped, else x_i 65536 / (65536 - below), below = round(65536 p);
+ * residual (NULL: none) is added.  The mask is not stored: value i is dropped iff bits [16 q, 16 q + 16), q = i % 4, of random
+ * word offset + i / 4 are less than `below`; words are those of dg_occ_candidates (splitmix64 output mix of
+ * seed + 0x9E3779B97F4A7C15*(ctr+1)), so a seed of its own, and offsets at least ceil(n / 4) apart, keep masks apart.
+ * The kept share is exactly (65536 - below) / 65536; p == 1 drops everything.  A dropped infinity or NaN leaves 0.
+ * y may be x or residual.  The backward pass draws the same mask: dx_i = 0 or dy_i 65536 / (65536 - below) (the gradient of
+ * the residual is dy itself); dx may be dy.  DG_ERR_ARG for p outside [0, 1]; DG_ERR_UNSUPPORTED for n > 2^40. */
+int dg_dropout_fwd(const void *x, const void *residual, uint64_t n, double p, uint64_t seed, uint64_t offset,
+                   uint32_t dtype, void *y, void *stream);
+int dg_dropout_bwd(const void *dy, uint64_t n, double p, uint64_t seed, uint64_t offset, uint32_t dtype, void *dx,
+                   void *stream);
 
 #ifdef __cplusplus
 }

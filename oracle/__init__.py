@@ -445,3 +445,49 @@ def composite_depth_ragged(sigma, delta, t, first):
     D = np.zeros(first.size - 1, np.float64)
     lib().dgo_composite_depth_ragged(_p(sigma), _p(delta), _p(t), C.c_uint32(first.size - 1), _p(first), _p(D))
     return D
+
+
+# ------------------------------------------------------------------ layer norm, gated recurrence, dropout
+def _f64(a):
+    return None if a is None else _arr(a, np.float64)
+
+
+def layer_norm_fwd(x, gamma, beta, eps):
+    x, gamma, beta = _f64(x), _f64(gamma), _f64(beta)
+    y = np.zeros_like(x)
+    lib().dgo_layer_norm_fwd(_p(x), _p(gamma), _p(beta), C.c_uint64(x.shape[0]), C.c_uint32(x.shape[1]), C.c_double(eps), _p(y))
+    return y
+
+
+def layer_norm_bwd(x, gamma, dy, eps):
+    """(dx, dgamma, dbeta)"""
+    x, gamma, dy = _f64(x), _f64(gamma), _f64(dy)
+    dx, dgamma, dbeta = np.zeros_like(x), np.zeros(x.shape[1]), np.zeros(x.shape[1])
+    lib().dgo_layer_norm_bwd(_p(x), _p(gamma), _p(dy), C.c_uint64(x.shape[0]), C.c_uint32(x.shape[1]), C.c_double(eps), _p(dx), _p(dgamma), _p(dbeta))
+    return dx, dgamma, dbeta
+
+
+def recurrence_fwd(z, u, first, reverse=False, h0=None):
+    """(y, h_last); rows of no sequence are NaN."""
+    z, u, h0, first = _f64(z), _f64(u), _f64(h0), _arr(first, np.uint32)
+    y, h_last = np.full_like(z, np.nan), np.zeros((first.size - 1, z.shape[1]))
+    lib().dgo_recurrence_fwd(_p(z), _p(u), C.c_uint32(first.size - 1), _p(first), C.c_uint32(z.shape[1]), C.c_int(reverse), _p(h0), _p(y), _p(h_last))
+    return y, h_last
+
+
+def recurrence_bwd(z, u, first, dy, reverse=False, h0=None, dh_last=None):
+    """(dz, du, dh0); rows of no sequence are NaN."""
+    z, u, dy, h0, dh_last, first = _f64(z), _f64(u), _f64(dy), _f64(h0), _f64(dh_last), _arr(first, np.uint32)
+    dz, du, dh0 = np.full_like(z, np.nan), np.full_like(z, np.nan), np.zeros((first.size - 1, z.shape[1]))
+    lib().dgo_recurrence_bwd(_p(z), _p(u), C.c_uint32(first.size - 1), _p(first), C.c_uint32(z.shape[1]), C.c_int(reverse), _p(h0), _p(dy), _p(dh_last),
+                             _p(dz), _p(du), _p(dh0))
+    return dz, du, dh0
+
+
+def dropout_mask(seed, offset, n, p):
+    """(keep [n] of bool, factor of the kept values)"""
+    keep = np.zeros(n, np.uint8)
+    f = lib().dgo_dropout_mask
+    f.restype = C.c_double
+    factor = f(C.c_uint64(seed), C.c_uint64(offset), C.c_uint64(n), C.c_double(p), _p(keep))
+    return keep.astype(bool), factor

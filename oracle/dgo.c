@@ -823,3 +823,105 @@ void dgo_composite_depth_ragged(const double *sigma, const double *delta, const 
     for (uint32_t j = 0; j < n_seg; ++j)
         dgo_composite_depth(sigma + first[j], delta + first[j], t + first[j], 1, first[j + 1] - first[j], D + j);
 }
+
+/* ------------------------------------------------------------------ */
+/* Layer norm, gated linear recurrence, dropout                        */
+/* ------------------------------------------------------------------ */
+
+static double row_moments(const double *x, uint32_t W, double eps, double *mean)
+{
+    double m = 0.0, v = 0.0;
+    for (uint32_t c = 0; c < W; ++c) m += x[c];
+    m /= W;
+    for (uint32_t c = 0; c < W; ++c) v += (x[c] - m) * (x[c] - m);
+    *mean = m;
+    return sqrt(v / W + eps);
+}
+
+void dgo_layer_norm_fwd(const double *x, const double *gamma, const double *beta, uint64_t N, uint32_t W, double eps, double *y)
+{
+    for (uint64_t r = 0; r < N; ++r, x += W, y += W) {
+        double m, d = row_moments(x, W, eps, &m);
+        for (uint32_t c = 0; c < W; ++c) y[c] = (x[c] - m) / d * (gamma ? gamma[c] : 1.0) + (beta ? beta[c] : 0.0);
+    }
+}
+
+void dgo_layer_norm_bwd(const double *x, const double *gamma, const double *dy, uint64_t N, uint32_t W, double eps, double *dx,
+                        double *dgamma, double *dbeta)
+{
+    for (uint32_t c = 0; c < W; ++c) dgamma[c] = dbeta[c] = 0.0;
+    for (uint64_t r = 0; r < N; ++r, x += W, dy += W, dx += W) {
+        double m, d = row_moments(x, W, eps, &m);
+        for (uint32_t c = 0; c < W; ++c) {
+            dgamma[c] += dy[c] * (x[c] - m) / d;
+            dbeta[c] += dy[c];
+        }
+        /* d xhat_i / d x_c = (delta_ic - 1/W) / d - (x_i - m) (x_c - m) / (W d^3) */
+        for (uint32_t c = 0; c < W; ++c) {
+            double sum = 0.0;
+            for (uint32_t i = 0; i < W; ++i) {
+                double g = dy[i] * (gamma ? gamma[i] : 1.0);
+                sum += g * (((i == c) - 1.0 / W) / d - (x[i] - m) * (x[c] - m) / (W * d * d * d));
+            }
+            dx[c] = sum;
+        }
+    }
+}
+
+static double opening(double z) { return z >= 88.0 ? 1.0 : z <= -88.0 ? 0.0 : 1.0 / (1.0 + exp(-z)); }
+
+/* the state after a token of gate z and input u */
+static double recur(double z, double u, double h)
+{
+    if (z >= 88.0) return h;
+    if (z <= -88.0) return u;
+    return opening(z) * h + opening(-z) * u;
+}
+
+void dgo_recurrence_fwd(const double *z, const double *u, uint32_t n_seq, const uint32_t *first, uint32_t W, int reverse,
+                        const double *h0, double *y, double *h_last)
+{
+    for (uint32_t j = 0; j < n_seq; ++j)
+        for (uint32_t c = 0; c < W; ++c) {
+            double h = h0 ? h0[(uint64_t)j * W + c] : 0.0;
+            for (uint32_t k = 0; k < first[j + 1] - first[j]; ++k) {
+                uint64_t i = (uint64_t)(reverse ? first[j + 1] - 1 - k : first[j] + k) * W + c;
+                y[i] = h = recur(z[i], u[i], h);
+            }
+            h_last[(uint64_t)j * W + c] = h;
+        }
+}
+
+void dgo_recurrence_bwd(const double *z, const double *u, uint32_t n_seq, const uint32_t *first, uint32_t W, int reverse,
+                        const double *h0, const double *dy, const double *dh_last, double *dz, double *du, double *dh0)
+{
+    for (uint32_t j = 0; j < n_seq; ++j) {
+        uint32_t n = first[j + 1] - first[j];
+        double *h = malloc((n + 1) * sizeof *h);
+        for (uint32_t c = 0; c < W; ++c) {
+            h[0] = h0 ? h0[(uint64_t)j * W + c] : 0.0;
+            for (uint32_t k = 0; k < n; ++k) {
+                uint64_t i = (uint64_t)(reverse ? first[j + 1] - 1 - k : first[j] + k) * W + c;
+                h[k + 1] = recur(z[i], u[i], h[k]);
+            }
+            double g = dh_last ? dh_last[(uint64_t)j * W + c] : 0.0;
+            for (uint32_t k = n; k-- > 0;) {
+                uint64_t i = (uint64_t)(reverse ? first[j + 1] - 1 - k : first[j] + k) * W + c;
+                double a = opening(z[i]), b = opening(-z[i]);
+                g += dy[i];
+                dz[i] = a == 0.0 || b == 0.0 ? 0.0 : g * a * b * (h[k] - u[i]);
+                du[i] = b == 0.0 ? 0.0 : g * b;
+                g = a == 0.0 ? 0.0 : g * a;
+            }
+            dh0[(uint64_t)j * W + c] = g;
+        }
+        free(h);
+    }
+}
+
+double dgo_dropout_mask(uint64_t seed, uint64_t offset, uint64_t n, double p, uint8_t *keep)
+{
+    uint32_t below = (uint32_t)floor(65536.0 * p + 0.5);
+    for (uint64_t i = 0; i < n; ++i) keep[i] = ((dgo_rand64(seed, offset + i / 4) >> (16 * (i % 4))) & 0xffffu) >= below;
+    return below == 65536u ? 0.0 : 65536.0 / (65536u - below);
+}

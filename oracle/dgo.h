@@ -190,6 +190,25 @@ void dgo_composite_bwd_ragged(const double *sigma, const double *rgb, const doub
 void dgo_composite_depth_ragged(const double *sigma, const double *delta, const double *t, uint32_t n_seg,
                                 const uint32_t *first, double *D);
 
+/* ------------------------------------------------------------------------------------------------
+ * Sequence block along the samples of rays: layer norm, gated linear recurrence, dropout.
+ * ---------------------------------------------------------------------------------------------- */
+/* y = (x - mean) / sqrt(mean((x - mean)^2) + eps) * gamma + beta, row by row; gamma, beta may be NULL */
+void dgo_layer_norm_fwd(const double *x, const double *gamma, const double *beta, uint64_t N, uint32_t W, double eps, double *y);
+/* gradients of sum(dy * y); the Jacobian of a row is applied as it stands, W x W */
+void dgo_layer_norm_bwd(const double *x, const double *gamma, const double *dy, uint64_t N, uint32_t W, double eps, double *dx,
+                        double *dgamma, double *dbeta);
+/* h <- a h + (1 - a) u, a = 1 / (1 + e^-z), along rows [first[j], first[j+1]) of sequence j, or from the last to the first
+ * (reverse); |z| >= 88: a is 0 or 1 and what it multiplies by 0 is skipped.  Rows of no sequence are left alone.  h0 may be NULL. */
+void dgo_recurrence_fwd(const double *z, const double *u, uint32_t n_seq, const uint32_t *first, uint32_t W, int reverse,
+                        const double *h0, double *y, double *h_last);
+/* gradients of sum(dy * y) + sum(dh_last * h_last); dh_last may be NULL */
+void dgo_recurrence_bwd(const double *z, const double *u, uint32_t n_seq, const uint32_t *first, uint32_t W, int reverse,
+                        const double *h0, const double *dy, const double *dh_last, double *dz, double *du, double *dh0);
+/* which of n values dropout keeps: 16 bits of dgo_rand64(seed, offset + i / 4), from bit 16 (i % 4) on, are not below
+ * floor(65536 p + 1/2); returns the factor of the kept ones */
+double dgo_dropout_mask(uint64_t seed, uint64_t offset, uint64_t n, double p, uint8_t *keep);
+
 #ifdef __cplusplus
 }
 #endif

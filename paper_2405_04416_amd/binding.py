@@ -14,7 +14,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libdistgrid.so")
 
-DG_F32, DG_F16 = 0, 1
+DG_F32, DG_F16, DG_BF16 = 0, 1, 2
 MAX_LEVELS = 16
 
 
@@ -150,6 +150,19 @@ _SIGNATURES = {
                                                                C.c_void_p, C.c_void_p]),
     "dg_composite_ragged_bwd": (C.c_int, [C.c_void_p] * 3 + [C.c_uint32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint32]
                                 + [C.c_void_p] * 5),
+    "dg_layer_norm_fwd": (C.c_int, [C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p, C.c_uint64, C.c_uint32, C.c_float, C.c_uint32, C.c_void_p, C.c_uint64,
+                                    C.c_void_p]),
+    "dg_layer_norm_bwd_workspace_bytes": (C.c_size_t, [C.c_uint64, C.c_uint32]),
+    "dg_layer_norm_bwd": (C.c_int, [C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p, C.c_uint64, C.c_uint64, C.c_uint32, C.c_float, C.c_uint32, C.c_void_p,
+                                    C.c_uint64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "dg_recurrence_state_count": (C.c_size_t, [C.c_uint64, C.c_uint32]),
+    "dg_recurrence_workspace_bytes": (C.c_size_t, [C.c_uint64, C.c_uint32, C.c_uint32]),
+    "dg_recurrence_fwd": (C.c_int, [C.c_void_p, C.c_uint64] * 2 + [C.c_uint64, C.c_uint32, C.c_void_p] + [C.c_uint32] * 3
+                          + [C.c_void_p, C.c_void_p, C.c_uint64] + [C.c_void_p] * 3 + [C.c_size_t, C.c_void_p]),
+    "dg_recurrence_bwd": (C.c_int, [C.c_void_p, C.c_uint64] * 2 + [C.c_uint64, C.c_uint32, C.c_void_p] + [C.c_uint32] * 3 + [C.c_void_p] * 2
+                          + [C.c_void_p, C.c_uint64, C.c_void_p] + [C.c_void_p, C.c_uint64] * 2 + [C.c_void_p] * 2 + [C.c_size_t, C.c_void_p]),
+    "dg_dropout_fwd": (C.c_int, [C.c_void_p, C.c_void_p, C.c_uint64, C.c_double, C.c_uint64, C.c_uint64, C.c_uint32, C.c_void_p, C.c_void_p]),
+    "dg_dropout_bwd": (C.c_int, [C.c_void_p, C.c_uint64, C.c_double, C.c_uint64, C.c_uint64, C.c_uint32, C.c_void_p, C.c_void_p]),
 }
 
 EXPORTS = tuple(_SIGNATURES)
@@ -647,3 +660,99 @@ def dg_mlp_bwd_rows(*args):
 
 def dg_mlp_bwd_split(*args):
     _mlp_bwd_rows(lib().dg_mlp_bwd_split, *args)
+
+
+# ------------------------------------------------------------------ layer norm, gated recurrence, dropout
+_TYPE_CODES = {torch.float32: DG_F32, torch.float16: DG_F16, torch.bfloat16: DG_BF16}
+
+
+def _type_code(t):
+    code = _TYPE_CODES.get(t.dtype)
+    if code is None:
+        raise DistGridError("expected fp32, fp16 or bf16, got %s" % t.dtype)
+    return code
+
+
+def _rows2d(t, like=None):
+    """(pointer, distance between rows) of a [N, W] tensor whose rows are contiguous; of like's shape and type."""
+    if not t.is_cuda:
+        raise DistGridError("tensor must live on the GPU")
+    if t.dim() != 2:
+        raise DistGridError("expected [rows, width], got %d dimensions" % t.dim())
+    N, W = t.shape
+    ld, step = t.stride()
+    if like is not None and (t.dtype != like.dtype or t.shape != like.shape):
+        raise DistGridError("expected %s %s, got %s %s" % (like.dtype, tuple(like.shape), t.dtype, tuple(t.shape)))
+    if (step != 1 and W > 1) or (ld < W and N > 1):
+        raise DistGridError("the values of a row must lie next to each other, and rows apart")
+    return t.data_ptr(), ld if N > 1 else W
+
+
+def _vector(t, n, dtype=torch.float32):
+    """Pointer to n contiguous values, or None."""
+    if t is None:
+        return None
+    if t.numel() != n:
+        raise DistGridError("expected %d values, got %d" % (n, t.numel()))
+    return _ptr(t, dtype)
+
+
+def _workspace(ws):
+    return (None, 0) if ws is None else (_ptr(ws), ws.numel() * ws.element_size())
+
+
+def dg_layer_norm_fwd(x, gamma, beta, eps, y):
+    """x, y [N, W] fp32, fp16 or bf16; gamma, beta [W] fp32 or None."""
+    code, (px, ldx), (py, ldy), (N, W) = _type_code(x), _rows2d(x), _rows2d(y, x), x.shape
+    _check(lib().dg_layer_norm_fwd(px, ldx, _vector(gamma, W), _vector(beta, W), N, W, eps, code, py, ldy, _stream()))
+
+
+def dg_layer_norm_bwd_workspace_bytes(N, W):
+    return int(lib().dg_layer_norm_bwd_workspace_bytes(N, W))
+
+
+def dg_layer_norm_bwd(x, gamma, dy, eps, dx, dgamma, dbeta, ws=None):
+    """dx, dgamma, dbeta: each may be None."""
+    code, (px, ldx), (pdy, lddy), (N, W) = _type_code(x), _rows2d(x), _rows2d(dy, x), x.shape
+    pdx, lddx = (None, W) if dx is None else _rows2d(dx, x)
+    pws, ws_bytes = _workspace(ws)
+    _check(lib().dg_layer_norm_bwd(px, ldx, _vector(gamma, W), pdy, lddy, N, W, eps, code, pdx, lddx, _vector(dgamma, W), _vector(dbeta, W), pws, ws_bytes,
+                                   _stream()))
+
+
+def dg_recurrence_state_count(N, W):
+    return int(lib().dg_recurrence_state_count(N, W))
+
+
+def dg_recurrence_workspace_bytes(N, n_seq, W):
+    return int(lib().dg_recurrence_workspace_bytes(N, n_seq, W))
+
+
+def dg_recurrence_fwd(z, u, n_seq, first, reverse, h0, y, h_last, states, ws=None):
+    """z, u, y [N, W]; first [n_seq + 1] int32 or None; h0, h_last [n_seq, W] fp32 and states (dg_recurrence_state_count values), each may be None."""
+    code, (pz, ldz), (pu, ldu), (py, ldy), (N, W) = _type_code(z), _rows2d(z), _rows2d(u, z), _rows2d(y, z), z.shape
+    pws, ws_bytes = _workspace(ws)
+    _check(lib().dg_recurrence_fwd(pz, ldz, pu, ldu, N, n_seq, _vector(first, n_seq + 1, torch.int32), W, reverse, code, _vector(h0, n_seq * W), py, ldy,
+                                   _vector(h_last, n_seq * W), None if states is None else _vector(states, dg_recurrence_state_count(N, W)), pws, ws_bytes,
+                                   _stream()))
+
+
+def dg_recurrence_bwd(z, u, n_seq, first, reverse, h0, states, dy, dh_last, dz, du, dh0, ws=None):
+    """states: as the forward pass left them; h0, dh_last, dh0 [n_seq, W] fp32, each may be None."""
+    code, (pz, ldz), (pu, ldu), (pdy, lddy), (N, W) = _type_code(z), _rows2d(z), _rows2d(u, z), _rows2d(dy, z), z.shape
+    (pdz, lddz), (pdu, lddu) = _rows2d(dz, z), _rows2d(du, z)
+    pws, ws_bytes = _workspace(ws)
+    _check(lib().dg_recurrence_bwd(pz, ldz, pu, ldu, N, n_seq, _vector(first, n_seq + 1, torch.int32), W, reverse, code, _vector(h0, n_seq * W),
+                                   _vector(states, dg_recurrence_state_count(N, W)), pdy, lddy, _vector(dh_last, n_seq * W), pdz, lddz, pdu, lddu,
+                                   _vector(dh0, n_seq * W), pws, ws_bytes, _stream()))
+
+
+def dg_dropout_fwd(x, residual, p, seed, offset, y):
+    """x, residual (or None), y: contiguous, of one type and size."""
+    code, n = _type_code(x), x.numel()
+    _check(lib().dg_dropout_fwd(_ptr(x), _vector(residual, n, x.dtype), n, p, seed, offset, code, _vector(y, n, x.dtype), _stream()))
+
+
+def dg_dropout_bwd(dy, p, seed, offset, dx):
+    code, n = _type_code(dy), dy.numel()
+    _check(lib().dg_dropout_bwd(_ptr(dy), n, p, seed, offset, code, _vector(dx, n, dy.dtype), _stream()))

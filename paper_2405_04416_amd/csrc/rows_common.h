@@ -1,0 +1,40 @@
+// Rows of a sequence block (layer norm, recurrence, dropout): element types and loads of several elements.  Internal.
+#pragma once
+#include "dg_internal.h"
+
+namespace dg_rows {
+
+// DG_F32, DG_F16, DG_BF16 in memory; everything is computed in fp32.  A store rounds to the nearest even value, once.
+using f16 = _Float16;
+using bf16 = __bf16;
+
+template <class T, int V>
+struct alignas(sizeof(T) * V) Pack { T v[V]; };
+
+template <class T, int V>
+__device__ __forceinline__ void load(const T *p, float (&out)[V])
+{
+    const Pack<T, V> a = *reinterpret_cast<const Pack<T, V> *>(p);
+#pragma unroll
+    for (int i = 0; i < V; ++i) out[i] = (float)a.v[i];
+}
+
+template <class T, int V>
+__device__ __forceinline__ void store(T *p, const float (&in)[V])
+{
+    Pack<T, V> a;
+#pragma unroll
+    for (int i = 0; i < V; ++i) a.v[i] = (T)in[i];
+    *reinterpret_cast<Pack<T, V> *>(p) = a;
+}
+
+inline size_t item_bytes(uint32_t dtype) { return dtype == DG_F32 ? 4 : 2; }
+inline bool known_type(uint32_t dtype) { return dtype == DG_F32 || dtype == DG_F16 || dtype == DG_BF16; }
+
+// whether rows of `ld` elements from p on can be loaded `bytes` at a time
+inline bool rows_aligned(const void *p, uint64_t ld, uint32_t dtype, size_t bytes)
+{
+    return dg::aligned(p, bytes) && ld * item_bytes(dtype) % bytes == 0;
+}
+
+}  // namespace dg_rows

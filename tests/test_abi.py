@@ -191,3 +191,32 @@ def test_fused_rendering_refuses_split_features():
     kSplit = 2
     assert render(b"views", None, None, kSplit, None, None, 0, 64, 0, 1, None, None, None, None, 1, None, None, None, None) != 0
     assert b"split" in B.lib().dg_last_error()
+
+
+def test_sequence_block_host_side():
+    """What the library refuses before it launches anything, and what it takes with nothing to do (all pointers NULL)."""
+    L = B.lib()
+    assert L.dg_layer_norm_fwd(None, 8, None, None, 0, 8, 1e-5, 0, None, 8, None) == 0
+    assert L.dg_layer_norm_fwd(None, 8, None, None, 4, 8, 1e-5, 0, None, 8, None) == -1           # null pointer
+    assert L.dg_layer_norm_fwd(None, 8, None, None, 0, 0, 1e-5, 0, None, 8, None) == -1           # W
+    assert L.dg_layer_norm_fwd(None, 8, None, None, 0, 8, -1.0, 0, None, 8, None) == -1           # eps
+    assert L.dg_layer_norm_fwd(None, 8, None, None, 0, 8, 1e-5, 3, None, 8, None) == -1           # type
+    assert L.dg_layer_norm_fwd(256, 7, None, None, 4, 8, 1e-5, 0, 256, 8, None) == -1             # rows that overlap
+    assert L.dg_layer_norm_fwd(258, 8, None, None, 4, 8, 1e-5, 0, 256, 8, None) == -1             # misaligned fp32
+    assert L.dg_layer_norm_fwd(None, 8, None, None, 1 << 33, 8, 1e-5, 0, None, 8, None) == -2
+    assert L.dg_layer_norm_bwd(None, 8, None, None, 8, 0, 8, 1e-5, 0, None, 8, None, None, None, 0, None) == 0
+    assert L.dg_layer_norm_bwd(256, 8, None, 256, 8, 4, 8, 1e-5, 0, 256, 8, 256, None, None, 0, None) == -3       # no workspace
+    assert L.dg_layer_norm_bwd_workspace_bytes(0, 8) <= 64 and L.dg_layer_norm_bwd_workspace_bytes(1 << 24, 32) <= 8 << 20
+    rec = lambda N, n_seq, W, p=None, dtype=0, ld=8, first=None: L.dg_recurrence_fwd(p, ld, p, ld, N, n_seq, first, W, 0, dtype, None, p, ld, None, None, None, 0, None)
+    assert rec(0, 0, 8) == 0
+    assert rec(12, 5, 8, 256) == -1 and b"one length" in L.dg_last_error()
+    assert rec(12, 0, 8, 256) == -1
+    assert rec(12, 3, 8) == -1 and rec(12, 3, 0, 256) == -1 and rec(12, 3, 9, 256) == -1 and rec(12, 3, 8, 256, 7) == -1
+    assert rec(1 << 32, 1, 8, 256) == -2
+    assert L.dg_recurrence_bwd(256, 8, 256, 8, 12, 3, None, 8, 0, 0, None, None, 256, 8, None, 256, 8, 256, 8, None, None, 0, None) == -1     # no states
+    assert L.dg_recurrence_state_count(0, 8) == 0 and L.dg_recurrence_state_count(33, 8) == 24
+    assert L.dg_dropout_fwd(None, None, 0, 0.5, 1, 0, 0, None, None) == 0
+    assert L.dg_dropout_fwd(None, None, 4, 0.5, 1, 0, 0, None, None) == -1
+    for p in (-0.1, 1.1, float("nan")):
+        assert L.dg_dropout_fwd(256, None, 0, p, 1, 0, 0, 256, None) == -1
+        assert L.dg_dropout_bwd(256, 0, p, 1, 0, 0, 256, None) == -1

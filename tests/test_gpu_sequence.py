@@ -1,0 +1,570 @@
+"""GPU parity of the sequence block (layer norm, gated linear recurrence, dropout) against the oracle in 64 bits, through the C ABI.
+
+Bounds: U is half a unit in the last place of fp32 relative to the value, T that of the type of an output.  An output may be off by
+T |value| (its one rounding) plus what its fp32 arithmetic may be off by, which each test derives from the magnitudes of the terms that
+were added.
+"""
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from paper_2405_04416_amd import binding as B
+
+from gpu_util import DEV
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+TYPES = {"fp32": torch.float32, "fp16": torch.float16, "bf16": torch.bfloat16}
+T_OF = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+LEAST = {torch.float32: 2.0 ** -140, torch.float16: 2.0 ** -25, torch.bfloat16: 2.0 ** -130}        # half the smallest step near 0
+
+
+def say(*what):
+    print("[case]", *what)
+    sys.stdout.flush()
+
+
+def rounded(a, dtype):
+    """Values of a type, as a host tensor of it and as 64-bit numbers."""
+    t = torch.from_numpy(np.asarray(a, np.float64)).to(dtype)
+    return t, t.double().numpy()
+
+
+def put(t, pad=0, shift=0):
+    """Rows of a device tensor with `pad` values between them, `shift` values into its storage; what lies between is 7."""
+    N, W = t.shape
+    buf = torch.full((shift + N * (W + pad) + 8,), 7.0, dtype=t.dtype, device=DEV)
+    view = buf[shift:shift + N * (W + pad)].view(N, W + pad)[:, :W]
+    view.copy_(t)
+    return view, buf
+
+
+def got(t):
+    return t.double().cpu().numpy()
+
+
+def f32(a):
+    return torch.from_numpy(np.ascontiguousarray(a, np.float32)).to(DEV)
+
+
+def within(what, value, want, bound, dtype):
+    err = np.abs(got(value) - want)
+    limit = bound + T_OF[dtype] * (np.abs(want) + bound) + LEAST[dtype]
+    assert np.all(err <= limit), "%s: off by %.3g where %.3g is allowed" % (what, err.flat[np.argmax(err / limit)], limit.flat[np.argmax(err / limit)])
+
+
+def untouched(buf, view):
+    """The values around and between the rows are still 7."""
+    mark = torch.ones_like(buf, dtype=torch.bool)
+    torch.as_strided(mark, view.shape, view.stride(), view.storage_offset())[...] = False
+    assert bool((buf[mark] == 7.0).all())
+
+
+# ------------------------------------------------------------------ layer norm
+def norm_bounds(x, gamma, beta, dy, eps):
+    """fp32 errors of y, dx, dgamma, dbeta.  A sum of W terms that 8 or more chains add up is off by (W / 8 + 8) U times the sum of
+    magnitudes at most; everything else is a few roundings."""
+    N, W = x.shape
+    k = (W / 8 + 24) * U
+    m, s = x.mean(1, keepdims=True), 1 / np.sqrt(x.var(1, keepdims=True) + eps)
+    size = np.abs(x).max(1, keepdims=True)
+    e_m = k * size                                                   # mean
+    xh = (x - m) * s
+    e_s = k + 2 * e_m * s + (e_m * s) ** 2                           # relative, of s: var is a mean of squares of x - m
+    e_xh = (e_m + 2 * U * size) * s + np.abs(xh) * e_s
+    e_y = e_xh * np.abs(gamma) + 4 * U * (np.abs(xh * gamma) + np.abs(beta))
+    g = dy * gamma
+    mg, mgx = np.abs(g).mean(1, keepdims=True), np.abs(g * xh).mean(1, keepdims=True)
+    e_mgx = k * mgx + (np.abs(g) * e_xh).mean(1, keepdims=True)
+    total = np.abs(g) + mg + np.abs(xh) * mgx
+    e_dx = s * (k * mg + np.abs(xh) * e_mgx + e_xh * mgx + 8 * U * total) + s * total * e_s
+    rows = (N / 4 + 24) * U
+    e_dgamma = (np.abs(dy) * e_xh).sum(0) + rows * np.abs(dy * xh).sum(0)
+    e_dbeta = rows * np.abs(dy).sum(0)
+    return e_y, e_dx, e_dgamma, e_dbeta
+
+
+def check_norm(x64, dtype, eps=1e-5, affine=True, pad=0, shift=0, seed=0):
+    rng = np.random.default_rng(seed)
+    N, W = x64.shape
+    x, x64 = rounded(x64, dtype)
+    dy, dy64 = rounded(rng.standard_normal((N, W)), dtype)
+    gamma, beta = (rng.standard_normal(W).astype(np.float32) for _ in range(2))
+    g64, b64 = (gamma.astype(np.float64), beta.astype(np.float64)) if affine else (np.ones(W), np.zeros(W))
+    xd, _ = put(x, pad, shift)
+    dyd, _ = put(dy, pad, shift)
+    y, ybuf = put(torch.zeros(N, W, dtype=dtype), pad, shift)
+    dx, dxbuf = put(torch.zeros(N, W, dtype=dtype), pad, shift)
+    gd, bd = (f32(gamma), f32(beta)) if affine else (None, None)
+    dgamma, dbeta = (torch.full((W,), 3.0, device=DEV) for _ in range(2))
+    eps32 = float(np.float32(eps))
+    B.dg_layer_norm_fwd(xd, gd, bd, eps, y)
+    ws = torch.empty(max(B.dg_layer_norm_bwd_workspace_bytes(N, W), 16), dtype=torch.uint8, device=DEV)
+    B.dg_layer_norm_bwd(xd, gd, dyd, eps, dx, dgamma, dbeta, ws)
+    torch.cuda.synchronize()
+    e_y, e_dx, e_dgamma, e_dbeta = norm_bounds(x64, g64, b64, dy64, eps32)
+    within("y", y, oracle.layer_norm_fwd(x64, g64, b64, eps32), e_y, dtype)
+    w_dx, w_dgamma, w_dbeta = oracle.layer_norm_bwd(x64, g64, dy64, eps32)
+    within("dx", dx, w_dx, e_dx, dtype)
+    within("dgamma", dgamma, w_dgamma, e_dgamma, torch.float32)
+    within("dbeta", dbeta, w_dbeta, e_dbeta, torch.float32)
+    untouched(ybuf, y)
+    untouched(dxbuf, dx)
+    # the same bits again, and with fewer outputs
+    dx2, dg2 = torch.zeros_like(dx), torch.zeros_like(dgamma)
+    B.dg_layer_norm_bwd(xd, gd, dyd, eps, dx2, None, None)
+    B.dg_layer_norm_bwd(xd, gd, dyd, eps, None, dg2, None, ws)
+    assert torch.equal(dx, dx2) and torch.equal(dgamma, dg2)
+    # in place
+    yy, dd = xd.clone(), dyd.clone()
+    B.dg_layer_norm_fwd(yy, gd, bd, eps, yy)
+    B.dg_layer_norm_bwd(xd.contiguous(), gd, dd, eps, dd, dg2, dbeta, ws)
+    assert torch.equal(yy, y) and torch.equal(dd, dx) and torch.equal(dg2, dgamma)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("N,W", [(1, 1), (7, 1), (5, 2), (65, 3), (67, 8), (515, 32), (33, 37), (9, 64), (40, 72), (5, 129), (3, 250), (3, 1000), (2, 1024),
+                                 (300, 513), (2, 2056), (2, 4096), (1, 4100)])
+def test_norm_sizes(N, W, dtype):
+    say("norm", N, W, dtype)
+    check_norm(np.random.default_rng(N * W).standard_normal((N, W)) * 1.5 + 0.5, TYPES[dtype])
+
+
+@pytest.mark.parametrize("W", [8192, 9001])
+def test_norm_of_very_wide_rows(W):
+    say("norm wide", W)
+    check_norm(np.random.default_rng(W).standard_normal((2, W)), torch.float32)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("W,pad,shift", [(32, 32, 0), (32, 1, 0), (32, 0, 1), (37, 3, 2), (1024, 8, 8), (1024, 3, 1), (2, 2, 4)])
+def test_norm_strides(W, pad, shift, dtype):
+    say("norm strides", W, pad, shift, dtype)
+    check_norm(np.random.default_rng(W).standard_normal((21, W)), TYPES[dtype], pad=pad, shift=shift)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_norm_without_weights(dtype):
+    say("norm plain", dtype)
+    check_norm(np.random.default_rng(0).standard_normal((50, 48)), TYPES[dtype], affine=False)
+
+
+def test_norm_of_flat_and_offset_rows():
+    say("norm flat")
+    x = np.random.default_rng(1).standard_normal((6, 40))
+    x[0] = 0.0
+    x[1] = 3.0                          # variance 0
+    x[2] += 1000.0                      # the mean far from 0: no difference of squares
+    x[3] *= 1e-6                        # variance far below eps
+    x[4] *= 1e6
+    check_norm(x, torch.float32)
+
+
+def test_norm_rows_do_not_mix():
+    """A row that holds NaN or infinity leaves the others alone."""
+    say("norm nan rows")
+    x = np.random.default_rng(2).standard_normal((70, 33))
+    clean, dirty = x.copy(), x.copy()
+    dirty[11, 5], dirty[30, 0] = np.nan, np.inf
+    outs = []
+    for a in (clean, dirty):
+        xd, y, dx = f32(a), torch.zeros(70, 33, device=DEV), torch.zeros(70, 33, device=DEV)
+        B.dg_layer_norm_fwd(xd, None, None, 1e-5, y)
+        B.dg_layer_norm_bwd(xd, None, f32(clean), 1e-5, dx, None, None)
+        outs.append((got(y), got(dx)))
+    rows = np.delete(np.arange(70), [11, 30])
+    for a, b in zip(*outs):
+        np.testing.assert_array_equal(a[rows], b[rows])
+        assert np.all(np.isnan(b[[11, 30]]))
+
+
+def test_norm_of_nothing():
+    say("norm empty")
+    x = torch.zeros(0, 16, device=DEV)
+    dgamma, dbeta = torch.ones(16, device=DEV), torch.ones(16, device=DEV)
+    B.dg_layer_norm_fwd(x, None, None, 1e-5, x)
+    ws = torch.empty(16, dtype=torch.uint8, device=DEV)
+    B.dg_layer_norm_bwd(x, None, x, 1e-5, x, dgamma, dbeta, ws)
+    assert not dgamma.any() and not dbeta.any()
+
+
+def test_norm_gradient_against_differences():
+    """fp32 values, differences of the fp32 forward pass: rounding of y 2 U over the step 2 h, curvature h^2."""
+    say("norm differences")
+    rng = np.random.default_rng(3)
+    N, W, h = 3, 12, 2.0 ** -9
+    x, dy = rng.standard_normal((N, W)), rng.standard_normal((N, W)).astype(np.float32)
+    xd = f32(x)
+    dx = torch.zeros(N, W, device=DEV)
+    B.dg_layer_norm_bwd(xd, None, f32(dy), 0.1, dx, None, None)
+    y = torch.zeros(N, W, device=DEV)
+    for i, j in ((0, 0), (1, 5), (2, 11)):
+        f = []
+        for d in (h, -h):
+            xx = xd.clone()
+            xx[i, j] += d
+            B.dg_layer_norm_fwd(xx, None, None, 0.1, y)
+            f.append(float(np.sum(got(y) * dy)))
+        size = np.abs(dy[i]).sum() * 3.0
+        assert abs((f[0] - f[1]) / (2 * h) - float(dx[i, j])) <= size * (16 * U / h + 20 * h * h)
+
+
+# ------------------------------------------------------------------ recurrence
+def recurrence_bounds(z, u, first, reverse, h0, dy, dh_last):
+    """Bounds of the fp32 errors of (y, h_last, dz, du, dh0): the recurrences of the magnitudes of what each step adds.  Both sides of
+    a gate are off by (|z| + 8) U of themselves; products of gates over a stretch by the sum of that over it, which the same
+    recurrence adds up; twice for the two ways in which a stretch can be joined."""
+    N, W = z.shape
+    n_seq = len(first) - 1
+    zz = np.clip(z, -88, 88)
+    a, c = 1 / (1 + np.exp(-zz)), 1 / (1 + np.exp(zz))
+    a, c = np.where(z <= -88, 0, a), np.where(z >= 88, 0, c)
+    k = 2 * (np.abs(zz) + 8) * U
+    ub = np.where(c == 0, 0, np.abs(u))
+    e_y, e_dz, e_du = np.zeros((N, W)), np.zeros((N, W)), np.zeros((N, W))
+    e_last, e_dh0 = np.zeros((n_seq, W)), np.zeros((n_seq, W))
+    for j in range(n_seq):
+        order = list(range(first[j], first[j + 1]))
+        order = order[::-1] if reverse else order
+        h, e = (np.zeros(W) if h0 is None else np.abs(h0[j])), np.zeros(W)
+        hs, es = [], []
+        for i in order:
+            hs.append(np.where(a[i] == 0, 0, h))
+            es.append(np.where(a[i] == 0, 0, e))
+            e = a[i] * es[-1] + k[i] * (a[i] * hs[-1] + c[i] * ub[i])
+            h = a[i] * hs[-1] + c[i] * ub[i]
+            e_y[i] = e
+        e_last[j] = e
+        g, e = (np.zeros(W) if dh_last is None else np.abs(dh_last[j])), np.zeros(W)
+        for i, hb, eb in zip(order[::-1], hs[::-1], es[::-1]):
+            g = g + np.abs(dy[i])
+            e = e + 4 * U * g
+            span = hb + ub[i]
+            e_dz[i] = a[i] * c[i] * (eb * g + span * e + 4 * k[i] * span * g)
+            e_du[i] = c[i] * (e + 2 * k[i] * g)
+            e = a[i] * e + 2 * k[i] * a[i] * g
+            g = a[i] * g
+        e_dh0[j] = e
+    return e_y, e_last, e_dz, e_du, e_dh0
+
+
+def check_recurrence(z, u, n_seq, first, dtype, reverse=False, carry=False, pad=0, shift=0, finite=True, seed=0):
+    """first None: sequences of one length."""
+    rng = np.random.default_rng(seed + 1)
+    N, W = z.shape
+    offsets = np.arange(n_seq + 1) * (N // max(n_seq, 1)) if first is None else np.asarray(first)
+    z, z64 = rounded(z, dtype)
+    u, u64 = rounded(u, dtype)
+    dy, dy64 = rounded(rng.standard_normal((N, W)), dtype)
+    h0 = rng.standard_normal((n_seq, W)).astype(np.float32) if carry else None
+    dl = rng.standard_normal((n_seq, W)).astype(np.float32) if carry else None
+    (zd, _), (ud, _), (dyd, _) = (put(t, pad, shift) for t in (z, u, dy))
+    sentinel = torch.full((N, W), 5.0, dtype=dtype)
+    (y, ybuf), (dz, dzbuf), (du, dubuf) = (put(sentinel, pad, shift) for _ in range(3))
+    h0d, dld = (None, None) if not carry else (f32(h0), f32(dl))
+    h_last, dh0 = (torch.full((n_seq, W), 5.0, device=DEV) for _ in range(2))
+    fd = None if first is None else torch.from_numpy(np.asarray(first, np.uint32).view(np.int32)).to(DEV)
+    ws = torch.empty(max(B.dg_recurrence_workspace_bytes(N, n_seq, W), 16), dtype=torch.uint8, device=DEV)
+    states = torch.full((B.dg_recurrence_state_count(N, W),), float("nan"), device=DEV)
+    B.dg_recurrence_fwd(zd, ud, n_seq, fd, reverse, h0d, y, h_last, states, ws)
+    ws.fill_(255)
+    B.dg_recurrence_bwd(zd, ud, n_seq, fd, reverse, h0d, states, dyd, dld, dz, du, dh0, ws)
+    torch.cuda.synchronize()
+    w_y, w_last = oracle.recurrence_fwd(z64, u64, offsets, reverse, h0)
+    w_dz, w_du, w_dh0 = oracle.recurrence_bwd(z64, u64, offsets, dy64, reverse, h0, dl)
+    held = np.zeros(N, bool)
+    held[offsets[0]:offsets[-1]] = True
+    for t, buf in ((y, ybuf), (dz, dzbuf), (du, dubuf)):
+        assert np.all(got(t)[~held] == 5.0)
+        untouched(buf, t)
+    if finite:
+        e_y, e_last, e_dz, e_du, e_dh0 = recurrence_bounds(z64, u64, offsets, reverse, h0, dy64, dl)
+        for what, t, want, bound in (("y", y, w_y, e_y), ("dz", dz, w_dz, e_dz), ("du", du, w_du, e_du)):
+            within(what, t[torch.from_numpy(held).to(DEV)], want[held], bound[held], dtype)
+        within("h_last", h_last, w_last, e_last, torch.float32)
+        within("dh0", dh0, w_dh0, e_dh0, torch.float32)
+    # without the states, in place of the old state: the same bits
+    y2, h2 = torch.zeros_like(y), (h0d.clone() if carry else None)
+    B.dg_recurrence_fwd(zd, ud, n_seq, fd, reverse, h2, y2, h2, None, ws)
+    rows = torch.from_numpy(held).to(DEV)
+    same = lambda a, b: bool(((a == b) | (a.isnan() & b.isnan())).all())
+    assert same(y2[rows], y[rows]) and (h2 is None or same(h2, h_last))
+    return (got(y), got(h_last), got(dz), got(du), got(dh0)), (w_y, w_last, w_dz, w_du, w_dh0), held
+
+
+def gates(rng, N, W, spread=2.0):
+    return rng.standard_normal((N, W)) * spread + 1.0
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("n_seq,S,W", [(1, 1, 1), (3, 1, 8), (300, 1, 33), (1, 2, 64), (2, 15, 5), (2, 16, 16), (5, 17, 32), (130, 37, 32), (4, 64, 48),
+                                       (3, 100, 129), (7, 33, 250), (2, 48, 1024)])
+def test_recurrence_sizes(n_seq, S, W, dtype):
+    say("recurrence", n_seq, S, W, dtype)
+    rng = np.random.default_rng(n_seq * S * W)
+    for reverse, carry in ((False, False), (True, True)):
+        check_recurrence(gates(rng, n_seq * S, W), rng.standard_normal((n_seq * S, W)), n_seq, None, TYPES[dtype], reverse, carry)
+
+
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("n_seq,S,W,dtype", [(1, 5000, 8, "fp32"), (1, 4097, 3, "fp16"), (2, 3001, 16, "bf16"), (3, 1024, 64, "fp16"), (1, 20011, 2, "fp32"),
+                                             (1, 2500, 130, "bf16")])
+def test_recurrence_of_long_sequences(n_seq, S, W, dtype, reverse):
+    say("recurrence long", n_seq, S, W, dtype, reverse)
+    rng = np.random.default_rng(S)
+    check_recurrence(gates(rng, n_seq * S, W), rng.standard_normal((n_seq * S, W)), n_seq, None, TYPES[dtype], reverse, True)
+
+
+def test_recurrence_that_remembers_long():
+    """Gates of nearly 1: a state lives over thousands of tokens, and a small share of each input adds up."""
+    say("recurrence memory")
+    rng = np.random.default_rng(8)
+    check_recurrence(8.0 + rng.standard_normal((4000, 6)), 1.0 + rng.standard_normal((4000, 6)), 1, None, torch.float32, False, True)
+
+
+RAGGED = [
+    [0, 0], [0, 1], [0, 3, 3, 4, 9], [0, 0, 0, 40, 40], [0, 16, 32, 48], [0, 15, 16, 17, 33, 65, 65, 200],
+    [3, 10, 25], [0, 5000], [0, 1, 2999, 3000, 3000, 4100],
+]
+
+
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("first", RAGGED, ids=str)
+def test_recurrence_ragged(first, dtype, reverse):
+    say("recurrence ragged", first, dtype, reverse)
+    rng = np.random.default_rng(len(first))
+    for W, room, carry in ((1, 0, True), (32, 5, False), (6, 64, True)):
+        N = first[-1] + room                                        # rows that no sequence has, at the end and before the first
+        if N == 0:
+            continue
+        check_recurrence(gates(rng, N, W), rng.standard_normal((N, W)), len(first) - 1, first, TYPES[dtype], reverse, carry)
+
+
+@pytest.mark.parametrize("reverse", [False, True])
+def test_recurrence_many_ragged(reverse):
+    say("recurrence many ragged", reverse)
+    rng = np.random.default_rng(9)
+    first = np.concatenate([[0], np.cumsum(rng.integers(0, 40, 700))])
+    check_recurrence(gates(rng, first[-1], 24), rng.standard_normal((first[-1], 24)), 700, first, torch.float16, reverse, True)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("W,pad,shift", [(32, 32, 0), (32, 1, 0), (32, 0, 1), (5, 3, 2), (64, 64, 8)])
+def test_recurrence_strides(W, pad, shift, dtype):
+    say("recurrence strides", W, pad, shift, dtype)
+    rng = np.random.default_rng(W)
+    for n_seq, S in ((9, 21), (1, 1500)):
+        check_recurrence(gates(rng, n_seq * S, W), rng.standard_normal((n_seq * S, W)), n_seq, None, TYPES[dtype], False, True, pad, shift)
+
+
+@pytest.mark.parametrize("S", [40, 3000])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_recurrence_shut_gates(S, dtype):
+    """Tokens that are passed over hold NaN and infinities; the past of a reset too; lowest values of the type as gates."""
+    say("recurrence shut", S, dtype)
+    rng = np.random.default_rng(S)
+    W, t = 7, TYPES[dtype]
+    z, u = gates(rng, S, W), rng.standard_normal((S, W))
+    z[rng.random((S, W)) < 0.1] = np.inf
+    z[rng.random((S, W)) < 0.1] = 100.0
+    z[rng.random((S, W)) < 0.05] = -np.inf
+    z[rng.random((S, W)) < 0.05] = torch.finfo(t).min
+    bad = rng.random((S, W)) < 0.5
+    u[(z >= 88) & bad] = np.nan
+    u[(z >= 88) & ~bad] = -np.inf
+    clean = np.where(z >= 88, 0.0, u)
+    have, want, _ = check_recurrence(z, u, 1, None, t, False, True, finite=False)
+    ref, _, _ = check_recurrence(z, clean, 1, None, t, False, True)
+    for h, r in zip(have, ref):
+        np.testing.assert_array_equal(h, r)                         # not looked at: the same bits as with zeros there
+    # a state that is not a number lasts exactly until the next reset
+    u2 = clean.copy()
+    z[S // 3], u2[S // 3] = 0.0, np.nan
+    z[S // 2] = -np.inf
+    z[S // 3 + 1:S // 2] = 1.0
+    have, want, _ = check_recurrence(z, u2, 1, None, t, False, True, finite=False)
+    np.testing.assert_array_equal(np.isnan(have[0]), np.isnan(want[0]))
+    assert np.isnan(have[0][S // 2 - 1]).all() and not np.isnan(have[0][S // 2:]).any()
+    for h, w in zip(have[2:], want[2:]):
+        np.testing.assert_array_equal(np.isnan(h), np.isnan(w))
+
+
+def test_recurrence_state_that_is_infinite_or_nan():
+    """In a long sequence too, and past stretches whose gates' product is below the smallest number."""
+    say("recurrence not finite")
+    S, W = 4000, 3
+    z, u = np.full((S, W), -6.0), np.ones((S, W))
+    u[10, 0], u[10, 1] = np.nan, np.inf
+    have, want, _ = check_recurrence(z, u, 1, None, torch.float32, False, False, finite=False)
+    np.testing.assert_array_equal(np.isnan(have[0]), np.isnan(want[0]))
+    np.testing.assert_array_equal(np.isposinf(have[0]), np.isposinf(want[0]))
+    assert np.isnan(have[0][10:, 0]).all() and np.isposinf(have[0][10:, 1]).all() and np.isfinite(have[0][:, 2]).all()
+
+
+def test_recurrence_offsets_that_are_wrong_stay_inside():
+    """Offsets past the rows, or descending: rows from N on are not touched (the results mean nothing)."""
+    say("recurrence wrong offsets")
+    for W in (4, 64):
+        N = 300
+        for first in ([0, 200, 100000], [50, 20, 10, 290], [400, 500, 600], [0, 0xffffffff, 3]):
+            buf = torch.full((N + 100, W), 7.0, device=DEV)
+            z = u = dy = torch.zeros(N, W, device=DEV)
+            fd = torch.from_numpy(np.array(first, np.uint32).view(np.int32)).to(DEV)
+            ws = torch.empty(max(B.dg_recurrence_workspace_bytes(N, len(first) - 1, W), 16), dtype=torch.uint8, device=DEV)
+            states = torch.zeros(B.dg_recurrence_state_count(N, W), device=DEV)
+            B.dg_recurrence_fwd(z, u, len(first) - 1, fd, False, None, buf[:N], None, states, ws)
+            assert bool((buf[N:] == 7.0).all())
+
+
+def test_recurrence_step_by_step_is_the_whole():
+    """A sequence read one token at a time, the state updated in place."""
+    say("recurrence steps")
+    rng = np.random.default_rng(10)
+    n_seq, S, W = 5, 20, 40
+    z, u = (torch.from_numpy(rng.standard_normal((n_seq, S, W))).float().to(DEV) for _ in range(2))
+    flat = lambda t: t.reshape(n_seq * S, W).contiguous()
+    y, last = torch.zeros(n_seq * S, W, device=DEV), torch.zeros(n_seq, W, device=DEV)
+    ws = torch.empty(max(B.dg_recurrence_workspace_bytes(n_seq * S, n_seq, W), 16), dtype=torch.uint8, device=DEV)
+    B.dg_recurrence_fwd(flat(z), flat(u), n_seq, None, False, None, y, last, None, ws)
+    h, out = torch.zeros(n_seq, W, device=DEV), torch.zeros(n_seq, W, device=DEV)
+    for t in range(S):
+        B.dg_recurrence_fwd(z[:, t], u[:, t], n_seq, None, False, h, out, h, None)
+        np.testing.assert_allclose(got(out), got(y.view(n_seq, S, W)[:, t]), rtol=0, atol=64 * U)      # |h| < 4: 16 U of 4
+    np.testing.assert_allclose(got(h), got(last), rtol=0, atol=64 * U)
+
+
+def test_recurrence_gradient_against_differences():
+    """Differences of the fp32 forward pass: its rounding over the step, curvature times the step squared."""
+    say("recurrence differences")
+    rng = np.random.default_rng(11)
+    S, W, h = 24, 4, 2.0 ** -8
+    z, u, dy = (f32(rng.standard_normal((S, W))) for _ in range(3))
+    states = torch.zeros(B.dg_recurrence_state_count(S, W), device=DEV)
+    ws = torch.empty(max(B.dg_recurrence_workspace_bytes(S, 1, W), 16), dtype=torch.uint8, device=DEV)
+    y, dz, du = torch.zeros(S, W, device=DEV), torch.zeros(S, W, device=DEV), torch.zeros(S, W, device=DEV)
+    B.dg_recurrence_fwd(z, u, 1, None, False, None, y, None, states, ws)
+    B.dg_recurrence_bwd(z, u, 1, None, False, None, states, dy, None, dz, du, None, ws)
+    size = float(dy.abs().sum(0).max()) * 4.0
+    for which, grad in ((z, dz), (u, du)):
+        for i, j in ((0, 0), (7, 1), (15, 2), (16, 3), (23, 0)):
+            f = []
+            for d in (h, -h):
+                which[i, j] += d
+                B.dg_recurrence_fwd(z, u, 1, None, False, None, y, None, None, ws)
+                which[i, j] -= d
+                f.append(float(np.sum(got(y) * got(dy))))
+            assert abs((f[0] - f[1]) / (2 * h) - float(grad[i, j])) <= size * (16 * U / h + h * h)
+
+
+# ------------------------------------------------------------------ dropout
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("n", [1, 3, 4, 7, 8, 9, 1023, 4099, 100000])
+def test_dropout(n, dtype):
+    say("dropout", n, dtype)
+    t = TYPES[dtype]
+    rng = np.random.default_rng(n)
+    (x, x64), (r, r64) = rounded(rng.standard_normal(n), t), rounded(rng.standard_normal(n), t)
+    for p, seed, offset, with_r, shift in ((0.1, 5, 0, True, 0), (0.5, 1 << 63, 12345678901, False, 0), (0.3, 77, 3, True, 1), (0.25, 9, 1, False, 5),
+                                           (0.0, 1, 0, False, 0), (1.0, 1, 0, True, 0)):
+        spot = lambda a: torch.cat([torch.full((shift,), 7.0, dtype=t), a, torch.full((8,), 7.0, dtype=t)]).to(DEV)[shift:shift + n]
+        xd, rd, y, dx = spot(x), spot(r) if with_r else None, spot(torch.zeros_like(x)), spot(torch.zeros_like(x))
+        B.dg_dropout_fwd(xd, rd, p, seed, offset, y)
+        B.dg_dropout_bwd(xd, p, seed, offset, dx)
+        keep, factor = oracle.dropout_mask(seed, offset, n, p)
+        want = np.where(keep, x64 * factor, 0.0)
+        # one rounding of the factor, one of the product, one of the sum
+        within("dx", dx, want, 2 * U * np.abs(want), t)
+        assert np.all(got(dx)[~keep] == 0.0)
+        total = want + (r64 if with_r else 0.0)
+        within("y", y, total, 3 * U * (np.abs(want) + np.abs(r64) * with_r), t)
+        for out in (y, dx):
+            base = torch.as_strided(out, (shift + n + 8,), (1,), 0)
+            assert bool((base[:shift] == 7.0).all()) and bool((base[shift + n:] == 7.0).all())
+        B.dg_dropout_bwd(dx.copy_(xd), p, seed, offset, dx)         # in place
+        again = got(dx)
+        assert np.all(again[~keep] == 0.0) and np.all((again != 0)[keep] == (x64 * factor != 0)[keep])
+
+
+def test_dropout_leaves_nothing_of_a_dropped_infinity():
+    say("dropout inf")
+    n = 4096
+    keep, _ = oracle.dropout_mask(3, 0, n, 0.5)
+    x = np.where(keep, 1.0, np.where(np.arange(n) % 2 == 0, np.inf, np.nan))
+    for t in TYPES.values():
+        y = torch.empty(n, dtype=t, device=DEV)
+        B.dg_dropout_fwd(torch.from_numpy(x).to(t).to(DEV), None, 0.5, 3, 0, y)
+        np.testing.assert_array_equal(got(y), np.where(keep, 2.0, 0.0))
+
+
+# ------------------------------------------------------------------ all
+def test_on_another_stream():
+    say("stream")
+    side = torch.cuda.Stream()
+    rng = np.random.default_rng(12)
+    x = f32(rng.standard_normal((500, 32)))
+    want, have = [torch.empty_like(x) for _ in range(3)], [torch.empty_like(x) for _ in range(3)]
+    states = torch.empty(B.dg_recurrence_state_count(500, 32), device=DEV)
+
+    def calls(out):
+        B.dg_layer_norm_fwd(x, None, None, 1e-5, out[0])
+        B.dg_recurrence_fwd(out[0], x, 5, None, False, None, out[1], None, states)
+        B.dg_dropout_fwd(out[1], x, 0.1, 1, 0, out[2])
+
+    calls(want)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        calls(have)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, have))
+
+
+def test_refusals():
+    say("refusals")
+    z = torch.zeros(12, 8, device=DEV)
+    v, g = torch.zeros(8, device=DEV), torch.zeros(8, device=DEV)
+    states = torch.zeros(B.dg_recurrence_state_count(12, 8), device=DEV)
+    first = torch.tensor([0, 12], dtype=torch.int32, device=DEV)
+    fwd = lambda **k: B.dg_recurrence_fwd(**{**dict(z=z, u=z, n_seq=3, first=None, reverse=False, h0=None, y=z.clone(), h_last=None, states=None, ws=None), **k})
+    bwd = lambda **k: B.dg_recurrence_bwd(**{**dict(z=z, u=z, n_seq=3, first=None, reverse=False, h0=None, states=states, dy=z, dh_last=None, dz=z.clone(),
+                                                    du=z.clone(), dh0=None, ws=None), **k})
+    wrong = [
+        lambda: B.dg_layer_norm_fwd(z, v, g, -1.0, z),                      # eps
+        lambda: B.dg_layer_norm_fwd(z, v, g, float("nan"), z),
+        lambda: B.dg_layer_norm_fwd(z, v[:7], g, 1e-5, z),                  # a short weight
+        lambda: B.dg_layer_norm_fwd(z, v.half(), g, 1e-5, z),
+        lambda: B.dg_layer_norm_fwd(z.double(), v, g, 1e-5, z.double()),
+        lambda: B.dg_layer_norm_fwd(z, v, g, 1e-5, z.half()),
+        lambda: B.dg_layer_norm_fwd(z, v, g, 1e-5, torch.zeros(11, 8, device=DEV)),
+        lambda: B.dg_layer_norm_fwd(z.t(), None, None, 1e-5, z.t()),        # rows that are columns
+        lambda: B.dg_layer_norm_fwd(z[:1].expand(12, 8), None, None, 1e-5, z),
+        lambda: B.dg_layer_norm_fwd(z.cpu(), None, None, 1e-5, z),
+        lambda: B.dg_layer_norm_bwd(z, v, z, 1e-5, z.clone(), v, g, None),  # no workspace
+        lambda: fwd(n_seq=5),                                               # 12 rows are not 5 sequences
+        lambda: fwd(n_seq=0),
+        lambda: fwd(first=first),                                           # 2 offsets, 3 sequences
+        lambda: fwd(first=first.long(), n_seq=1),
+        lambda: fwd(h0=torch.zeros(2, 8, device=DEV)),
+        lambda: fwd(h0=torch.zeros(3, 8, device=DEV, dtype=torch.float16)),
+        lambda: fwd(u=z.half()),
+        lambda: fwd(states=states[1:]),
+        lambda: bwd(states=None),
+        lambda: bwd(dy=z[:11]),
+        lambda: bwd(dh0=torch.zeros(3, 7, device=DEV)),
+        lambda: B.dg_dropout_fwd(z, None, 1.5, 0, 0, z),
+        lambda: B.dg_dropout_fwd(z, None, float("nan"), 0, 0, z),
+        lambda: B.dg_dropout_fwd(z, z.half(), 0.5, 0, 0, z),
+        lambda: B.dg_dropout_fwd(z, None, 0.5, 0, 0, z[:3]),
+        lambda: B.dg_dropout_bwd(z.t(), 0.5, 0, 0, z),
+        lambda: B.dg_dropout_bwd(z.long(), 0.5, 0, 0, z.long()),
+    ]
+    for i, call in enumerate(wrong):
+        with pytest.raises(B.DistGridError):
+            call()
+            say("not refused", i)
+    fwd(), bwd()
+    assert not z.any()
