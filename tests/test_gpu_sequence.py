@@ -293,6 +293,10 @@ def check_recurrence(z, u, n_seq, first, dtype, reverse=False, carry=False, pad=
     rows = torch.from_numpy(held).to(DEV)
     same = lambda a, b: bool(((a == b) | (a.isnan() & b.isnan())).all())
     assert same(y2[rows], y[rows]) and (h2 is None or same(h2, h_last))
+    if carry:
+        g2 = dld.clone()
+        B.dg_recurrence_bwd(zd, ud, n_seq, fd, reverse, h0d, states, dyd, g2, dz, du, g2, ws)
+        assert same(g2, dh0)
     return (got(y), got(h_last), got(dz), got(du), got(dh0)), (w_y, w_last, w_dz, w_du, w_dh0), held
 
 
@@ -509,10 +513,11 @@ def test_on_another_stream():
     x = f32(rng.standard_normal((500, 32)))
     want, have = [torch.empty_like(x) for _ in range(3)], [torch.empty_like(x) for _ in range(3)]
     states = torch.empty(B.dg_recurrence_state_count(500, 32), device=DEV)
+    ws = torch.empty(max(B.dg_recurrence_workspace_bytes(500, 5, 32), 16), dtype=torch.uint8, device=DEV)
 
     def calls(out):
         B.dg_layer_norm_fwd(x, None, None, 1e-5, out[0])
-        B.dg_recurrence_fwd(out[0], x, 5, None, False, None, out[1], None, states)
+        B.dg_recurrence_fwd(out[0], x, 5, None, False, None, out[1], None, states, ws)
         B.dg_dropout_fwd(out[1], x, 0.1, 1, 0, out[2])
 
     calls(want)
