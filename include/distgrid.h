@@ -527,7 +527,8 @@ int dg_composite_ragged_bwd(const float *sigma, const float *rgb, const float *d
 
 /* Layer norm of N rows of W values, m the mean of a row, s = 1 / sqrt(mean((x - m)^2) + eps):
  *   y = (x - m) s gamma + beta.   gamma, beta [W] fp32; NULL: 1 and 0.  y may be x.
- * Errors: DG_ERR_ARG for W == 0, eps < 0 or not finite, ld < W; DG_ERR_UNSUPPORTED for more than 2^32 rows, W > 2^20. */
+ * Errors: DG_ERR_ARG for W == 0, eps < 0 or not finite, ld < W; DG_ERR_UNSUPPORTED for more than 2^32 rows, W > 2^20,
+ * more than 2^39 values. */
 int dg_layer_norm_fwd(const void *x, uint64_t ldx, const float *gamma, const float *beta, uint64_t N, uint32_t W,
                       float eps, uint32_t dtype, void *y, uint64_t ldy, void *stream);
 /* Its backward pass, from x again (nothing of the forward pass is kept), xh = (x - m) s, g = dy gamma:

@@ -2,6 +2,10 @@
 //   xh = (x - m) s,  y = xh gamma + beta;
 //   g = dy gamma,  dx = s (g - mean(g) - xh mean(g xh)),  dgamma = sum over rows of dy xh,  dbeta = sum over rows of dy.
 // The backward pass computes m and s again; nothing is saved.
+//
+// Both passes are bound by memory: a row is read once into registers (K vectors of V values per lane, G lanes per row) and everything
+// is summed there, deviations from the mean after the mean itself.  The backward pass adds up dgamma and dbeta of the rows that a
+// lane sees in its registers; a workgroup's sums go to the workspace and a second launch folds them.  No atomics: the same bits each time.
 #include <cmath>
 #include "rows_common.h"
 
@@ -9,104 +13,302 @@ namespace {
 
 using namespace dg_rows;
 
-constexpr int kBlock = 256, kRowsPerPart = 256;
+constexpr int kBlock = 256;
 
-__device__ __forceinline__ float wave_sum(float v)
+// Sum over G neighbouring lanes, in all of them: exchanges inside groups of 4, 8 and 16 lanes on the way to the vector unit, wider ones
+// through the LDS crossbar.
+template <int kControl>
+__device__ __forceinline__ float exchanged(float v)
 {
-    for (int d = 1; d < dg::kWave; d *= 2) v += __shfl_xor(v, d);
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), kControl, 0xf, 0xf, false));
+}
+
+template <int G>
+__device__ __forceinline__ float group_sum(float v)
+{
+    if (G >= 2) v += exchanged<0xb1>(v);            // lanes 1 0 3 2
+    if (G >= 4) v += exchanged<0x4e>(v);            // lanes 2 3 0 1
+    if (G >= 8) v += exchanged<0x141>(v);           // mirrored in 8 lanes: the other four
+    if (G >= 16) v += exchanged<0x140>(v);          // mirrored in 16 lanes: the other eight
+    if (G >= 32) v += __shfl_xor(v, 16);
+    if (G >= 64) v += __shfl_xor(v, 32);
     return v;
 }
 
-// mean and 1 / standard deviation of a row, by one wavefront
-template <class T>
-__device__ __forceinline__ void moments(const T *x, uint32_t W, float eps, float &m, float &s)
+// The lanes that share a row: G of a wavefront, or all kThreads of the workgroup (G = kThreads).  red: room for one value per
+// wavefront and sum.
+template <int G, int kThreads, int n>
+__device__ __forceinline__ void row_sums(float (&v)[n], float (*red)[n])
 {
-    const uint32_t lane = threadIdx.x % dg::kWave;
-    float sum = 0.0f;
-    for (uint32_t c = lane; c < W; c += dg::kWave) sum += (float)x[c];
-    m = wave_sum(sum) / W;
-    sum = 0.0f;
-    for (uint32_t c = lane; c < W; c += dg::kWave) { const float d = (float)x[c] - m; sum += d * d; }
-    s = 1.0f / sqrtf(wave_sum(sum) / W + eps);
-}
-
-template <class T>
-__global__ void __launch_bounds__(kBlock)
-norm_fwd_kernel(const T *x, uint64_t ldx, const float *gamma, const float *beta, uint64_t N, uint32_t W, float eps, T *y, uint64_t ldy)
-{
-    const uint64_t row = ((uint64_t)blockIdx.x * kBlock + threadIdx.x) / dg::kWave;
-    if (row >= N) return;
-    float m, s;
-    x += row * ldx;
-    moments(x, W, eps, m, s);
-    for (uint32_t c = threadIdx.x % dg::kWave; c < W; c += dg::kWave)
-        y[row * ldy + c] = (T)(((float)x[c] - m) * s * (gamma ? gamma[c] : 1.0f) + (beta ? beta[c] : 0.0f));
-}
-
-template <class T>
-__global__ void __launch_bounds__(kBlock)
-norm_bwd_kernel(const T *x, uint64_t ldx, const float *gamma, const T *dy, uint64_t lddy, uint64_t N, uint32_t W, float eps, T *dx, uint64_t lddx)
-{
-    const uint64_t row = ((uint64_t)blockIdx.x * kBlock + threadIdx.x) / dg::kWave;
-    if (row >= N) return;
-    float m, s, sg = 0.0f, sgx = 0.0f;
-    x += row * ldx;
-    dy += row * lddy;
-    moments(x, W, eps, m, s);
-    for (uint32_t c = threadIdx.x % dg::kWave; c < W; c += dg::kWave) {
-        const float g = (float)dy[c] * (gamma ? gamma[c] : 1.0f);
-        sg += g;
-        sgx += g * ((float)x[c] - m) * s;
-    }
-    sg = wave_sum(sg) / W;
-    sgx = wave_sum(sgx) / W;
-    for (uint32_t c = threadIdx.x % dg::kWave; c < W; c += dg::kWave) {
-        const float g = (float)dy[c] * (gamma ? gamma[c] : 1.0f);
-        dx[row * lddx + c] = (T)(s * (g - sg - ((float)x[c] - m) * s * sgx));
+#pragma unroll
+    for (int i = 0; i < n; ++i) v[i] = group_sum<(G < dg::kWave ? G : dg::kWave)>(v[i]);
+    if (G <= dg::kWave) return;
+    constexpr int kWaves = kThreads / dg::kWave;
+    __syncthreads();                                // the last use of red is over
+    if (threadIdx.x % dg::kWave == 0)
+#pragma unroll
+        for (int i = 0; i < n; ++i) red[threadIdx.x / dg::kWave][i] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+        v[i] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) v[i] += red[w][i];
     }
 }
 
-// one wavefront per part of the rows; part p of the sums at part[p][0 / 1][W].  Before dx is written, which may be dy.
-template <class T>
-__global__ void __launch_bounds__(dg::kWave)
-norm_parts_kernel(const T *x, uint64_t ldx, const T *dy, uint64_t lddy, uint64_t N, uint32_t W, float eps, uint64_t per_part, float *part)
+struct Norm {
+    const void *x, *dy;
+    void *out;                      // y, or dx (NULL: not wanted)
+    const float *gamma, *beta;
+    float *part;                    // backward: [workgroups][2][W], or NULL
+    uint64_t ldx, lddy, ldo, N;
+    uint32_t W;
+    float eps, per_W;               // 1 / W
+};
+
+// V values of vector k of a lane's share of a row; 0 where the row has ended
+template <int V>
+__device__ __forceinline__ bool inside(uint32_t W, uint32_t lane, int k, int G, uint32_t &c)
 {
-    const uint64_t row0 = blockIdx.x * per_part, row1 = row0 + per_part < N ? row0 + per_part : N;
-    part += (uint64_t)blockIdx.x * 2 * W;
-    for (uint32_t c = threadIdx.x; c < 2 * W; c += dg::kWave) part[c] = 0.0f;
-    for (uint64_t row = row0; row < row1; ++row) {
-        float m, s;
-        moments(x + row * ldx, W, eps, m, s);
-        for (uint32_t c = threadIdx.x; c < W; c += dg::kWave) {
-            const float d = (float)dy[row * lddy + c];
-            part[c] += d * ((float)x[row * ldx + c] - m) * s;
-            part[W + c] += d;
+    c = (k * G + lane) * V;
+    return c < W;
+}
+
+template <class T, int V>
+__device__ __forceinline__ void read(const T *row, uint32_t c, bool in, float (&out)[V])
+{
+    if (in) load<T, V>(row + c, out);
+    else
+#pragma unroll
+        for (int v = 0; v < V; ++v) out[v] = 0.0f;
+}
+
+// mean and 1 / standard deviation of a row in registers, which then holds deviations from the mean (0 where the row has ended)
+template <int V, int G, int K, int kThreads>
+__device__ __forceinline__ float centre(float (&x)[K][V], const Norm &a, uint32_t lane, float (*red)[1])
+{
+    float sum[1] = {0.0f};
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum[0] += x[k][v];
+    row_sums<G, kThreads, 1>(sum, red);
+    return sum[0] * a.per_W;
+}
+
+template <class T, int V, int G, int K, int kThreads>
+__global__ void __launch_bounds__(kThreads)
+norm_fwd_kernel(Norm a)
+{
+    __shared__ float red[kThreads / dg::kWave][1];
+    const uint32_t lane = threadIdx.x % G;
+    const uint64_t row = (uint64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G;
+    if (row >= a.N) return;                         // never where the workgroup shares a row: all of it has the same one
+    const T *x = (const T *)a.x + row * a.ldx;
+    float r[K][V];
+    uint32_t c;
+#pragma unroll
+    for (int k = 0; k < K; ++k) { const bool in = inside<V>(a.W, lane, k, G, c); read<T, V>(x, c, in, r[k]); }
+    const float m = centre<V, G, K, kThreads>(r, a, lane, red);
+    float sum[1] = {0.0f};
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        if (inside<V>(a.W, lane, k, G, c))
+#pragma unroll
+            for (int v = 0; v < V; ++v) { r[k][v] -= m; sum[0] += r[k][v] * r[k][v]; }
+    row_sums<G, kThreads, 1>(sum, red);
+    const float s = 1.0f / sqrtf(sum[0] * a.per_W + a.eps);
+    T *y = (T *)a.out + row * a.ldo;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        if (inside<V>(a.W, lane, k, G, c)) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) r[k][v] = r[k][v] * s * (a.gamma ? a.gamma[c + v] : 1.0f) + (a.beta ? a.beta[c + v] : 0.0f);
+            store<T, V>(y + c, r[k]);
+        }
+}
+
+// Workgroups go through the rows side by side: workgroup b takes rows b R, b R + 1, ... of every gridDim.x R, R = kThreads / G at a time.
+template <class T, int V, int G, int K, int kThreads>
+__global__ void __launch_bounds__(kThreads)
+norm_bwd_kernel(Norm a)
+{
+    constexpr int kWaves = kThreads / dg::kWave, R = kThreads / G;
+    __shared__ float red1[kWaves][1], red3[kWaves][3];
+    const uint32_t lane = threadIdx.x % G;
+    float gamma[K][V], sum_g[K][V], sum_b[K][V];
+    uint32_t c;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const bool in = inside<V>(a.W, lane, k, G, c);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            gamma[k][v] = in && a.gamma ? a.gamma[c + v] : 1.0f;
+            sum_g[k][v] = sum_b[k][v] = 0.0f;
+        }
+    }
+    for (uint64_t row0 = (uint64_t)blockIdx.x * R; row0 < a.N; row0 += (uint64_t)gridDim.x * R) {
+        const uint64_t row = row0 + threadIdx.x / G;
+        const bool held = row < a.N;                // lanes without a row go along: sums are over whole groups of lanes
+        const T *px = (const T *)a.x + row * a.ldx, *pdy = (const T *)a.dy + row * a.lddy;
+        float x[K][V], dy[K][V];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const bool in = inside<V>(a.W, lane, k, G, c) && held;
+            read<T, V>(px, c, in, x[k]);
+            read<T, V>(pdy, c, in, dy[k]);
+        }
+        const float m = centre<V, G, K, kThreads>(x, a, lane, red1);
+        float sum[3] = {0.0f, 0.0f, 0.0f};          // of squared deviations, of g, of g times the deviation
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (inside<V>(a.W, lane, k, G, c))
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    x[k][v] -= m;
+                    sum[0] += x[k][v] * x[k][v];
+                    const float g = dy[k][v] * gamma[k][v];
+                    sum[1] += g;
+                    sum[2] += g * x[k][v];
+                }
+        row_sums<G, kThreads, 3>(sum, red3);
+        const float s = 1.0f / sqrtf(sum[0] * a.per_W + a.eps), mean_g = sum[1] * a.per_W, mean_gx = sum[2] * a.per_W * s;
+        T *out = (T *)a.out + row * a.ldo;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            float o[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float xh = x[k][v] * s;
+                o[v] = s * (dy[k][v] * gamma[k][v] - mean_g - xh * mean_gx);
+                if (held) {
+                    sum_g[k][v] += dy[k][v] * xh;
+                    sum_b[k][v] += dy[k][v];
+                }
+            }
+            if (inside<V>(a.W, lane, k, G, c) && held && a.out) store<T, V>(out + c, o);
+        }
+    }
+    if (!a.part) return;
+    // the rows of a wavefront, then those of the workgroup's wavefronts
+    float *part = a.part + (uint64_t)blockIdx.x * 2 * a.W;
+    __shared__ float sums[G < kThreads ? kWaves : 1][2][G < kThreads ? G * V : 1];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const bool in = inside<V>(a.W, lane, k, G, c);
+        if (G >= kThreads) {
+            if (in)
+#pragma unroll
+                for (int v = 0; v < V; ++v) { part[c + v] = sum_g[k][v]; part[a.W + c + v] = sum_b[k][v]; }
+            continue;
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int d = G; d < dg::kWave; d *= 2) {
+                sum_g[k][v] += __shfl_xor(sum_g[k][v], d);
+                sum_b[k][v] += __shfl_xor(sum_b[k][v], d);
+            }
+        __syncthreads();
+        if (threadIdx.x % dg::kWave < G)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                sums[threadIdx.x / dg::kWave][0][lane * V + v] = sum_g[k][v];
+                sums[threadIdx.x / dg::kWave][1][lane * V + v] = sum_b[k][v];
+            }
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < 2 * G * V; i += kThreads) {
+            const uint32_t which = i / (G * V), j = i % (G * V), col = k * G * V + j;
+            float t = 0.0f;
+            for (int w = 0; w < kWaves; ++w) t += sums[w][which][j];
+            if (col < a.W) part[which * a.W + col] = t;
         }
     }
 }
 
-__global__ void __launch_bounds__(kBlock)
+// dgamma and dbeta of the workgroups' sums: 64 columns per workgroup, whose wavefronts share the parts
+constexpr int kFoldWaves = 16;
+
+__global__ void __launch_bounds__(kFoldWaves *dg::kWave)
 norm_fold_kernel(const float *part, uint32_t n_parts, uint32_t W, float *dgamma, float *dbeta)
 {
-    const uint32_t c = blockIdx.x * kBlock + threadIdx.x;
-    if (c >= W) return;
-    float a = 0.0f, b = 0.0f;
-    for (uint32_t p = 0; p < n_parts; ++p) { a += part[(uint64_t)p * 2 * W + c]; b += part[(uint64_t)p * 2 * W + W + c]; }
-    if (dgamma) dgamma[c] = a;
-    if (dbeta) dbeta[c] = b;
+    __shared__ float red[kFoldWaves][dg::kWave];
+    const uint32_t lane = threadIdx.x % dg::kWave, wave = threadIdx.x / dg::kWave, c = blockIdx.x * dg::kWave + lane;
+    float sum = 0.0f;
+    if (c < 2 * W)
+#pragma unroll 8
+        for (uint32_t p = wave; p < n_parts; p += kFoldWaves) sum += part[(uint64_t)p * 2 * W + c];
+    red[wave][lane] = sum;
+    __syncthreads();
+    if (wave != 0 || c >= 2 * W) return;
+    sum = 0.0f;
+    for (int w = 0; w < kFoldWaves; ++w) sum += red[w][lane];
+    if (c < W ? dgamma != nullptr : dbeta != nullptr) (c < W ? dgamma : dbeta - W)[c] = sum;
 }
 
-uint32_t parts_of(uint64_t N)
+// Rows too wide for the registers of a workgroup: read again from the caches for every sum, a workgroup per row.
+constexpr int kWide = 1024;
+
+template <class T>
+__device__ __forceinline__ void wide_moments(const T *x, const Norm &a, float &m, float &s, float (*red)[1])
 {
-    const uint64_t p = (N + kRowsPerPart - 1) / kRowsPerPart;
-    return (uint32_t)(p < 4096 ? p : 4096);
+    float sum[1] = {0.0f};
+    for (uint32_t c = threadIdx.x; c < a.W; c += kWide) sum[0] += (float)x[c];
+    row_sums<kWide, kWide, 1>(sum, red);
+    m = sum[0] * a.per_W;
+    sum[0] = 0.0f;
+    for (uint32_t c = threadIdx.x; c < a.W; c += kWide) { const float d = (float)x[c] - m; sum[0] += d * d; }
+    row_sums<kWide, kWide, 1>(sum, red);
+    s = 1.0f / sqrtf(sum[0] * a.per_W + a.eps);
+}
+
+template <class T>
+__global__ void __launch_bounds__(kWide)
+norm_fwd_wide_kernel(Norm a)
+{
+    __shared__ float red[kWide / dg::kWave][1];
+    const T *x = (const T *)a.x + blockIdx.x * a.ldx;
+    T *y = (T *)a.out + blockIdx.x * a.ldo;
+    float m, s;
+    wide_moments(x, a, m, s, red);
+    for (uint32_t c = threadIdx.x; c < a.W; c += kWide) y[c] = (T)(((float)x[c] - m) * s * (a.gamma ? a.gamma[c] : 1.0f) + (a.beta ? a.beta[c] : 0.0f));
+}
+
+template <class T>
+__global__ void __launch_bounds__(kWide)
+norm_bwd_wide_kernel(Norm a)
+{
+    __shared__ float red[kWide / dg::kWave][1], red2[kWide / dg::kWave][2];
+    float *part = a.part ? a.part + (uint64_t)blockIdx.x * 2 * a.W : nullptr;
+    for (uint32_t c = threadIdx.x; part && c < a.W; c += kWide) part[c] = part[a.W + c] = 0.0f;     // by the lane that adds to them
+    for (uint64_t row = blockIdx.x; row < a.N; row += gridDim.x) {
+        const T *x = (const T *)a.x + row * a.ldx, *dy = (const T *)a.dy + row * a.lddy;
+        T *out = (T *)a.out + row * a.ldo;
+        float m, s, sum[2] = {0.0f, 0.0f};
+        wide_moments(x, a, m, s, red);
+        for (uint32_t c = threadIdx.x; c < a.W; c += kWide) {
+            const float g = (float)dy[c] * (a.gamma ? a.gamma[c] : 1.0f);
+            sum[0] += g;
+            sum[1] += g * ((float)x[c] - m) * s;
+        }
+        row_sums<kWide, kWide, 2>(sum, red2);
+        for (uint32_t c = threadIdx.x; c < a.W; c += kWide) {
+            const float d = (float)dy[c], xh = ((float)x[c] - m) * s;
+            if (part) {
+                part[c] += d * xh;
+                part[a.W + c] += d;
+            }
+            if (a.out) out[c] = (T)(s * (d * (a.gamma ? a.gamma[c] : 1.0f) - sum[0] * a.per_W - xh * sum[1] * a.per_W));
+        }
+    }
 }
 
 int check(const char *who, uint64_t N, uint32_t W, float eps, uint32_t dtype)
 {
     DG_REQUIRE(known_type(dtype), DG_ERR_ARG, "%s: unknown element type %u", who, dtype);
     DG_REQUIRE(W >= 1 && eps >= 0.0f && std::isfinite(eps), DG_ERR_ARG, "%s: W must be positive, eps finite and not negative", who);
-    DG_REQUIRE(N <= 1ull << 32 && W <= 1u << 20, DG_ERR_UNSUPPORTED, "%s: more than 2^32 rows or 2^20 values a row", who);
+    DG_REQUIRE(N <= 1ull << 32 && W <= 1u << 20 && N * W <= 1ull << 39, DG_ERR_UNSUPPORTED, "%s: more than 2^32 rows, 2^20 values a row or 2^39 values", who);
     return DG_OK;
 }
 
@@ -117,23 +319,85 @@ int check_rows(const char *who, const void *p, uint64_t ld, uint32_t W, uint32_t
     return DG_OK;
 }
 
-template <class T>
-void launch_fwd(const void *x, uint64_t ldx, const float *gamma, const float *beta, uint64_t N, uint32_t W, float eps, void *y, uint64_t ldy, hipStream_t st)
+// How a row of n vectors is spread: K of them in each of G lanes.  Up to 64 lanes of a wavefront the combination with the fewest idle
+// places is taken, the one with fewer vectors per lane among equals; then a wavefront with up to 4, a workgroup with up to 8.
+struct Spread { int G, K; };
+
+Spread spread_of(uint32_t n)
 {
-    norm_fwd_kernel<T><<<(uint32_t)((N + 3) / 4), kBlock, 0, st>>>((const T *)x, ldx, gamma, beta, N, W, eps, (T *)y, ldy);
+    Spread best = {0, 0};
+    for (int K = 1; K <= 3; ++K)
+        for (int G = 1; G <= 64; G *= 2)
+            if ((uint32_t)(G * K) >= n) {
+                if (best.G == 0 || G * K < best.G * best.K) best = {G, K};
+                break;
+            }
+    if (best.G) return best;
+    if (n <= 256) return {64, 4};
+    for (int K = 2; K <= 8; K *= 2)
+        if (n <= 256u * K) return {256, K};
+    return {0, 0};
 }
 
-template <class T>
-void launch_bwd(const void *x, uint64_t ldx, const float *gamma, const void *dy, uint64_t lddy, uint64_t N, uint32_t W, float eps, void *dx, uint64_t lddx,
-                float *dgamma, float *dbeta, float *part, hipStream_t st)
+// workgroups of the backward pass: each leaves 2 W sums, so that wide rows have fewer
+uint32_t parts_of(uint64_t N, uint32_t W)
 {
-    const uint32_t n_parts = parts_of(N);
-    if (dgamma || dbeta) {
-        if (n_parts)
-            norm_parts_kernel<T><<<n_parts, dg::kWave, 0, st>>>((const T *)x, ldx, (const T *)dy, lddy, N, W, eps, (N + n_parts - 1) / n_parts, part);
-        norm_fold_kernel<<<(W + kBlock - 1) / kBlock, kBlock, 0, st>>>(part, n_parts, W, dgamma, dbeta);
+    const uint64_t most = W <= 512 ? 2048 : W <= 2048 ? 1024 : 512, rows = W <= 64 ? 64 : W <= 512 ? 16 : 4;
+    const uint64_t p = (N + rows - 1) / rows;
+    return (uint32_t)(p < most ? p : most);
+}
+
+struct Call {
+    Norm a;
+    uint32_t dtype, parts;
+    bool forward;
+    hipStream_t st;
+};
+
+template <class T, int V, int G, int K>
+void launch_spread(const Call &c)
+{
+    if (c.forward) norm_fwd_kernel<T, V, G, K, kBlock><<<(uint32_t)((c.a.N + kBlock / G - 1) / (kBlock / G)), kBlock, 0, c.st>>>(c.a);
+    else norm_bwd_kernel<T, V, G, K, kBlock><<<c.parts, kBlock, 0, c.st>>>(c.a);
+}
+
+template <class T, int V, int G>
+void launch_lanes(const Call &c, int K)
+{
+    if (K == 1) launch_spread<T, V, G, 1>(c);
+    else if (K == 2) launch_spread<T, V, G, 2>(c);
+    else launch_spread<T, V, G, 3>(c);
+}
+
+template <class T, int V>
+void launch_rows(const Call &c)
+{
+    const Spread s = spread_of(c.a.W / V);
+    switch (s.G) {
+    case 1: return launch_lanes<T, V, 1>(c, s.K);
+    case 2: return launch_lanes<T, V, 2>(c, s.K);
+    case 4: return launch_lanes<T, V, 4>(c, s.K);
+    case 8: return launch_lanes<T, V, 8>(c, s.K);
+    case 16: return launch_lanes<T, V, 16>(c, s.K);
+    case 32: return launch_lanes<T, V, 32>(c, s.K);
+    case 64: return s.K == 4 ? launch_spread<T, V, 64, 4>(c) : launch_lanes<T, V, 64>(c, s.K);
+    case 256: return s.K == 2 ? launch_spread<T, V, 256, 2>(c) : s.K == 4 ? launch_spread<T, V, 256, 4>(c) : launch_spread<T, V, 256, 8>(c);
     }
-    if (dx && N) norm_bwd_kernel<T><<<(uint32_t)((N + 3) / 4), kBlock, 0, st>>>((const T *)x, ldx, gamma, (const T *)dy, lddy, N, W, eps, (T *)dx, lddx);
+    if (c.forward) norm_fwd_wide_kernel<T><<<(uint32_t)c.a.N, kWide, 0, c.st>>>(c.a);
+    else norm_bwd_wide_kernel<T><<<c.parts, kWide, 0, c.st>>>(c.a);
+}
+
+// vectors of 16 bytes where every row allows it, single values otherwise
+void launch(const Call &c)
+{
+    const Norm &a = c.a;
+    const uint32_t item = (uint32_t)item_bytes(c.dtype);
+    bool wide = a.W * item % 16 == 0 && rows_aligned(a.x, a.ldx, c.dtype, 16);
+    if (!c.forward) wide = wide && rows_aligned(a.dy, a.lddy, c.dtype, 16);
+    if (a.out) wide = wide && rows_aligned(a.out, a.ldo, c.dtype, 16);
+    if (c.dtype == DG_F32) wide ? launch_rows<float, 4>(c) : launch_rows<float, 1>(c);
+    else if (c.dtype == DG_F16) wide ? launch_rows<f16, 8>(c) : launch_rows<f16, 1>(c);
+    else wide ? launch_rows<bf16, 8>(c) : launch_rows<bf16, 1>(c);
 }
 
 }  // namespace
@@ -147,11 +411,11 @@ extern "C" int dg_layer_norm_fwd(const void *x, uint64_t ldx, const float *gamma
     if (int rc = check_rows(who, x, ldx, W, dtype)) return rc;
     if (int rc = check_rows(who, y, ldy, W, dtype)) return rc;
     DG_REQUIRE(dg::aligned(gamma, 4) && dg::aligned(beta, 4), DG_ERR_ARG, "%s: misaligned pointer", who);
-    (dtype == DG_F32 ? launch_fwd<float> : dtype == DG_F16 ? launch_fwd<f16> : launch_fwd<bf16>)(x, ldx, gamma, beta, N, W, eps, y, ldy, (hipStream_t)stream);
+    launch({{x, nullptr, y, gamma, beta, nullptr, ldx, 0, ldy, N, W, eps, 1.0f / (float)W}, dtype, 0, true, (hipStream_t)stream});
     return dg::launch_status(who);
 }
 
-extern "C" size_t dg_layer_norm_bwd_workspace_bytes(uint64_t N, uint32_t W) { return (size_t)parts_of(N) * 2 * W * sizeof(float); }
+extern "C" size_t dg_layer_norm_bwd_workspace_bytes(uint64_t N, uint32_t W) { return (size_t)parts_of(N, W) * 2 * W * sizeof(float); }
 
 extern "C" int dg_layer_norm_bwd(const void *x, uint64_t ldx, const float *gamma, const void *dy, uint64_t lddy, uint64_t N, uint32_t W, float eps,
                                  uint32_t dtype, void *dx, uint64_t lddx, float *dgamma, float *dbeta, void *ws, size_t ws_bytes, void *stream)
@@ -165,11 +429,15 @@ extern "C" int dg_layer_norm_bwd(const void *x, uint64_t ldx, const float *gamma
             if (int rc = check_rows(who, dx, lddx, W, dtype)) return rc;
     }
     DG_REQUIRE(dg::aligned(gamma, 4) && dg::aligned(dgamma, 4) && dg::aligned(dbeta, 4), DG_ERR_ARG, "%s: misaligned pointer", who);
-    if (!dgamma && !dbeta && (!dx || !N)) return DG_OK;
-    const size_t need = dgamma || dbeta ? dg_layer_norm_bwd_workspace_bytes(N, W) : 0;
+    const bool weights = dgamma || dbeta;
+    if (!weights && (!dx || !N)) return DG_OK;
+    const size_t need = weights ? dg_layer_norm_bwd_workspace_bytes(N, W) : 0;
     DG_REQUIRE(need == 0 || (ws && dg::aligned(ws, 16) && ws_bytes >= need), DG_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", who, need,
                ws ? ws_bytes : 0);
-    (dtype == DG_F32 ? launch_bwd<float> : dtype == DG_F16 ? launch_bwd<f16> : launch_bwd<bf16>)(x, ldx, gamma, dy, lddy, N, W, eps, dx, lddx, dgamma, dbeta,
-                                                                                                 (float *)ws, (hipStream_t)stream);
+    float *part = weights ? (float *)ws : nullptr;
+    const uint32_t parts = parts_of(N, W);
+    if (N) launch({{x, dy, dx, gamma, nullptr, part, ldx, lddy, lddx, N, W, eps, 1.0f / (float)W}, dtype, parts, false, (hipStream_t)stream});
+    if (weights)
+        norm_fold_kernel<<<(2 * W + dg::kWave - 1) / dg::kWave, kFoldWaves * dg::kWave, 0, (hipStream_t)stream>>>(part, parts, W, dgamma, dbeta);
     return dg::launch_status(who);
 }

@@ -120,9 +120,9 @@ def check_norm(x64, dtype, eps=1e-5, affine=True, pad=0, shift=0, seed=0):
     B.dg_layer_norm_bwd(xd, gd, dyd, eps, None, dg2, None, ws)
     assert torch.equal(dx, dx2) and torch.equal(dgamma, dg2)
     # in place
-    yy, dd = xd.clone(), dyd.clone()
+    yy, dd = put(x, pad, shift)[0], put(dy, pad, shift)[0]
     B.dg_layer_norm_fwd(yy, gd, bd, eps, yy)
-    B.dg_layer_norm_bwd(xd.contiguous(), gd, dd, eps, dd, dg2, dbeta, ws)
+    B.dg_layer_norm_bwd(xd, gd, dd, eps, dd, dg2, dbeta, ws)
     assert torch.equal(yy, y) and torch.equal(dd, dx) and torch.equal(dg2, dgamma)
 
 
