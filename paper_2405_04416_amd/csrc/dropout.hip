@@ -9,30 +9,80 @@ namespace {
 using namespace dg_rows;
 
 constexpr int kBlock = 256;
+constexpr uint64_t kStreamedBytes = 64 << 20;
 
-// four elements, one word of the generator, per lane
+struct Drop {
+    const void *x, *r;
+    void *y;
+    uint64_t n, seed, offset;
+    uint32_t below;
+    float scale;
+};
+
+// value k of the four that share a word
+__device__ __forceinline__ float dropped(uint64_t bits, int k, uint32_t below, float scale, float x)
+{
+    const uint32_t field = (uint32_t)(bits >> (k < 2 ? 0 : 32)) >> (16 * (k % 2)) & 0xffffu;
+    return field < below ? 0.0f : x * scale;        // chosen, not multiplied by 0: a dropped infinity or NaN is dropped
+}
+
+// 16 bytes per lane and array; the values behind the last whole vector are done by the first lanes of the last workgroup, one word each.
+// Bound by memory: the generator costs some 14 operations per element, which hide behind the loads.
+template <class T, bool kResidual, bool kStreamed>
+__global__ void __launch_bounds__(kBlock)
+dropout_kernel(Drop a)
+{
+    constexpr int V = 16 / sizeof(T);
+    const T *x = (const T *)a.x, *r = (const T *)a.r;
+    T *y = (T *)a.y;
+    const uint64_t n_vectors = a.n / V, i = (uint64_t)blockIdx.x * kBlock + threadIdx.x;
+    if (i < n_vectors) {
+        Pack<T, V> v = kStreamed ? load_streamed<T, V>(x + i * V) : *reinterpret_cast<const Pack<T, V> *>(x + i * V), b;
+        if (kResidual) b = kStreamed ? load_streamed<T, V>(r + i * V) : *reinterpret_cast<const Pack<T, V> *>(r + i * V);
+#pragma unroll
+        for (int q = 0; q < V / 4; ++q) {
+            const uint64_t bits = dg_sample::mix64(a.seed, a.offset + i * (V / 4) + q);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                float t = dropped(bits, k, a.below, a.scale, (float)v.v[4 * q + k]);
+                if (kResidual) t += (float)b.v[4 * q + k];
+                v.v[4 * q + k] = (T)t;
+            }
+        }
+        if (kStreamed) store_streamed<T, V>(y + i * V, v);
+        else *reinterpret_cast<Pack<T, V> *>(y + i * V) = v;
+    }
+    const uint64_t j = n_vectors * V + threadIdx.x;
+    if (blockIdx.x == gridDim.x - 1 && j < a.n) {
+        const float t = dropped(dg_sample::mix64(a.seed, a.offset + j / 4), j % 4, a.below, a.scale, (float)x[j]);
+        y[j] = (T)(kResidual ? t + (float)r[j] : t);
+    }
+}
+
+// arrays that are not aligned: four values, one word, per lane
 template <class T, bool kResidual>
 __global__ void __launch_bounds__(kBlock)
-dropout_kernel(const T *__restrict__ x, const T *__restrict__ r, uint64_t n, uint32_t below, float scale, uint64_t seed, uint64_t offset, T *y)
+dropout_unaligned_kernel(Drop a)
 {
-    const uint64_t q = (uint64_t)blockIdx.x * kBlock + threadIdx.x;
-    const uint64_t bits = dg_sample::mix64(seed, offset + q);
+    const uint64_t q = (uint64_t)blockIdx.x * kBlock + threadIdx.x, bits = dg_sample::mix64(a.seed, a.offset + q);
+#pragma unroll
     for (int k = 0; k < 4; ++k) {
         const uint64_t i = 4 * q + k;
-        if (i >= n) return;
-        // chosen, not multiplied by 0: a dropped infinity or NaN is dropped
-        float v = ((bits >> (16 * k)) & 0xffffu) < below ? 0.0f : (float)x[i] * scale;
-        if (kResidual) v += (float)r[i];
-        y[i] = (T)v;
+        if (i >= a.n) return;
+        const float t = dropped(bits, k, a.below, a.scale, (float)((const T *)a.x)[i]);
+        ((T *)a.y)[i] = (T)(kResidual ? t + (float)((const T *)a.r)[i] : t);
     }
 }
 
 template <class T>
-void launch(const void *x, const void *r, uint64_t n, uint32_t below, float scale, uint64_t seed, uint64_t offset, void *y, hipStream_t st)
+void launch(const Drop &a, hipStream_t st)
 {
-    const uint32_t grid = (uint32_t)(((n + 3) / 4 + kBlock - 1) / kBlock);
-    if (r) dropout_kernel<T, true><<<grid, kBlock, 0, st>>>((const T *)x, (const T *)r, n, below, scale, seed, offset, (T *)y);
-    else dropout_kernel<T, false><<<grid, kBlock, 0, st>>>((const T *)x, nullptr, n, below, scale, seed, offset, (T *)y);
+    const bool vectors = dg::aligned(a.x, 16) && dg::aligned(a.r, 16) && dg::aligned(a.y, 16);
+    const uint64_t per = (vectors ? 16 / sizeof(T) : 4) * kBlock;
+    auto go = [&](auto kernel) { kernel<<<(uint32_t)((a.n + per - 1) / per), kBlock, 0, st>>>(a); };
+    if (!vectors) return a.r ? go(dropout_unaligned_kernel<T, true>) : go(dropout_unaligned_kernel<T, false>);
+    if (a.n * sizeof(T) >= kStreamedBytes) a.r ? go(dropout_kernel<T, true, true>) : go(dropout_kernel<T, false, true>);
+    else a.r ? go(dropout_kernel<T, true, false>) : go(dropout_kernel<T, false, false>);
 }
 
 int dropout(const char *who, const void *x, const void *r, uint64_t n, double p, uint64_t seed, uint64_t offset, uint32_t dtype, void *y, hipStream_t st)
@@ -45,7 +95,7 @@ int dropout(const char *who, const void *x, const void *r, uint64_t n, double p,
     DG_REQUIRE(n <= 1ull << 40, DG_ERR_UNSUPPORTED, "%s: n too large for one launch", who);
     const uint32_t below = (uint32_t)std::floor(p * 65536.0 + 0.5);
     const float scale = below == 65536u ? 0.0f : (float)(65536.0 / (65536u - below));
-    (dtype == DG_F32 ? launch<float> : dtype == DG_F16 ? launch<f16> : launch<bf16>)(x, r, n, below, scale, seed, offset, y, st);
+    (dtype == DG_F32 ? launch<float> : dtype == DG_F16 ? launch<f16> : launch<bf16>)({x, r, y, n, seed, offset, below, scale}, st);
     return dg::launch_status(who);
 }
 

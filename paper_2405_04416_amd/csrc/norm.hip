@@ -75,18 +75,43 @@ __device__ __forceinline__ bool inside(uint32_t W, uint32_t lane, int k, int G, 
     return c < W;
 }
 
-template <class T, int V>
-__device__ __forceinline__ void read(const T *row, uint32_t c, bool in, float (&out)[V])
+template <class T, int V, int G, int K>
+__device__ __forceinline__ void read(const void *p, uint64_t ld, uint64_t row, const Norm &a, uint32_t lane, Pack<T, V> (&out)[K])
 {
-    if (in) load<T, V>(row + c, out);
-    else
+    uint32_t c;
 #pragma unroll
-        for (int v = 0; v < V; ++v) out[v] = 0.0f;
+    for (int k = 0; k < K; ++k)
+        if (inside<V>(a.W, lane, k, G, c) && row < a.N) out[k] = *reinterpret_cast<const Pack<T, V> *>((const T *)p + row * ld + c);
+        else
+#pragma unroll
+            for (int v = 0; v < V; ++v) out[k].v[v] = (T)0.0f;
 }
 
-// mean and 1 / standard deviation of a row in registers, which then holds deviations from the mean (0 where the row has ended)
+template <class T, int V, int K>
+__device__ __forceinline__ void widen(const Pack<T, V> (&in)[K], float (&out)[K][V])
+{
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int v = 0; v < V; ++v) out[k][v] = (float)in[k].v[v];
+}
+
+// a lane's share of a vector of W values, `none` without one
+template <int V, int G, int K>
+__device__ __forceinline__ void weights(const float *p, float none, const Norm &a, uint32_t lane, float (&out)[K][V])
+{
+    uint32_t c;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const bool in = inside<V>(a.W, lane, k, G, c) && p;
+#pragma unroll
+        for (int v = 0; v < V; ++v) out[k][v] = in ? p[c + v] : none;
+    }
+}
+
+// mean of a row in registers
 template <int V, int G, int K, int kThreads>
-__device__ __forceinline__ float centre(float (&x)[K][V], const Norm &a, uint32_t lane, float (*red)[1])
+__device__ __forceinline__ float mean(const float (&x)[K][V], const Norm &a, float (*red)[1])
 {
     float sum[1] = {0.0f};
 #pragma unroll
@@ -97,39 +122,48 @@ __device__ __forceinline__ float centre(float (&x)[K][V], const Norm &a, uint32_
     return sum[0] * a.per_W;
 }
 
+// Workgroups go through the rows side by side: workgroup b takes rows b R, b R + 1, ... of every gridDim.x R, R = kThreads / G at a
+// time, with gamma and beta in registers; the next row is on its way while one is worked on.
 template <class T, int V, int G, int K, int kThreads>
 __global__ void __launch_bounds__(kThreads)
 norm_fwd_kernel(Norm a)
 {
-    __shared__ float red[kThreads / dg::kWave][1];
+    constexpr int R = kThreads / G;
+    __shared__ float red[kThreads / dg::kWave][1], red2[kThreads / dg::kWave][1];
     const uint32_t lane = threadIdx.x % G;
-    const uint64_t row = (uint64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G;
-    if (row >= a.N) return;                         // never where the workgroup shares a row: all of it has the same one
-    const T *x = (const T *)a.x + row * a.ldx;
-    float r[K][V];
-    uint32_t c;
+    float gamma[K][V], beta[K][V];
+    weights<V, G, K>(a.gamma, 1.0f, a, lane, gamma);
+    weights<V, G, K>(a.beta, 0.0f, a, lane, beta);
+    uint64_t row = (uint64_t)blockIdx.x * R + threadIdx.x / G;
+    Pack<T, V> next[K];
+    read<T, V, G, K>(a.x, a.ldx, row, a, lane, next);
+    for (uint64_t row0 = (uint64_t)blockIdx.x * R; row0 < a.N; row0 += (uint64_t)gridDim.x * R) {
+        float x[K][V];
+        widen<T, V, K>(next, x);
+        const uint64_t now = row;
+        row += (uint64_t)gridDim.x * R;
+        read<T, V, G, K>(a.x, a.ldx, row, a, lane, next);
+        const float m = mean<V, G, K, kThreads>(x, a, red);
+        float sum[1] = {0.0f};
+        uint32_t c;
 #pragma unroll
-    for (int k = 0; k < K; ++k) { const bool in = inside<V>(a.W, lane, k, G, c); read<T, V>(x, c, in, r[k]); }
-    const float m = centre<V, G, K, kThreads>(r, a, lane, red);
-    float sum[1] = {0.0f};
+        for (int k = 0; k < K; ++k)
+            if (inside<V>(a.W, lane, k, G, c))
 #pragma unroll
-    for (int k = 0; k < K; ++k)
-        if (inside<V>(a.W, lane, k, G, c))
+                for (int v = 0; v < V; ++v) { x[k][v] -= m; sum[0] += x[k][v] * x[k][v]; }
+        row_sums<G, kThreads, 1>(sum, red2);
+        const float s = 1.0f / sqrtf(sum[0] * a.per_W + a.eps);
+        T *y = (T *)a.out + now * a.ldo;
 #pragma unroll
-            for (int v = 0; v < V; ++v) { r[k][v] -= m; sum[0] += r[k][v] * r[k][v]; }
-    row_sums<G, kThreads, 1>(sum, red);
-    const float s = 1.0f / sqrtf(sum[0] * a.per_W + a.eps);
-    T *y = (T *)a.out + row * a.ldo;
+        for (int k = 0; k < K; ++k)
+            if (inside<V>(a.W, lane, k, G, c) && now < a.N) {
 #pragma unroll
-    for (int k = 0; k < K; ++k)
-        if (inside<V>(a.W, lane, k, G, c)) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) r[k][v] = r[k][v] * s * (a.gamma ? a.gamma[c + v] : 1.0f) + (a.beta ? a.beta[c + v] : 0.0f);
-            store<T, V>(y + c, r[k]);
-        }
+                for (int v = 0; v < V; ++v) x[k][v] = x[k][v] * s * gamma[k][v] + beta[k][v];
+                store<T, V>(y + c, x[k]);
+            }
+    }
 }
 
-// Workgroups go through the rows side by side: workgroup b takes rows b R, b R + 1, ... of every gridDim.x R, R = kThreads / G at a time.
 template <class T, int V, int G, int K, int kThreads>
 __global__ void __launch_bounds__(kThreads)
 norm_bwd_kernel(Norm a)
@@ -137,29 +171,23 @@ norm_bwd_kernel(Norm a)
     constexpr int kWaves = kThreads / dg::kWave, R = kThreads / G;
     __shared__ float red1[kWaves][1], red3[kWaves][3];
     const uint32_t lane = threadIdx.x % G;
-    float gamma[K][V], sum_g[K][V], sum_b[K][V];
+    float gamma[K][V], sum_g[K][V] = {}, sum_b[K][V] = {};
+    weights<V, G, K>(a.gamma, 1.0f, a, lane, gamma);
     uint32_t c;
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const bool in = inside<V>(a.W, lane, k, G, c);
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            gamma[k][v] = in && a.gamma ? a.gamma[c + v] : 1.0f;
-            sum_g[k][v] = sum_b[k][v] = 0.0f;
-        }
-    }
+    uint64_t row = (uint64_t)blockIdx.x * R + threadIdx.x / G;
+    Pack<T, V> next_x[K], next_dy[K];
+    read<T, V, G, K>(a.x, a.ldx, row, a, lane, next_x);
+    read<T, V, G, K>(a.dy, a.lddy, row, a, lane, next_dy);
     for (uint64_t row0 = (uint64_t)blockIdx.x * R; row0 < a.N; row0 += (uint64_t)gridDim.x * R) {
-        const uint64_t row = row0 + threadIdx.x / G;
         const bool held = row < a.N;                // lanes without a row go along: sums are over whole groups of lanes
-        const T *px = (const T *)a.x + row * a.ldx, *pdy = (const T *)a.dy + row * a.lddy;
+        T *out = (T *)a.out + row * a.ldo;
         float x[K][V], dy[K][V];
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const bool in = inside<V>(a.W, lane, k, G, c) && held;
-            read<T, V>(px, c, in, x[k]);
-            read<T, V>(pdy, c, in, dy[k]);
-        }
-        const float m = centre<V, G, K, kThreads>(x, a, lane, red1);
+        widen<T, V, K>(next_x, x);
+        widen<T, V, K>(next_dy, dy);
+        row += (uint64_t)gridDim.x * R;
+        read<T, V, G, K>(a.x, a.ldx, row, a, lane, next_x);
+        read<T, V, G, K>(a.dy, a.lddy, row, a, lane, next_dy);
+        const float m = mean<V, G, K, kThreads>(x, a, red1);
         float sum[3] = {0.0f, 0.0f, 0.0f};          // of squared deviations, of g, of g times the deviation
 #pragma unroll
         for (int k = 0; k < K; ++k)
@@ -174,7 +202,6 @@ norm_bwd_kernel(Norm a)
                 }
         row_sums<G, kThreads, 3>(sum, red3);
         const float s = 1.0f / sqrtf(sum[0] * a.per_W + a.eps), mean_g = sum[1] * a.per_W, mean_gx = sum[2] * a.per_W * s;
-        T *out = (T *)a.out + row * a.ldo;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             float o[V];
@@ -227,24 +254,29 @@ norm_bwd_kernel(Norm a)
     }
 }
 
-// dgamma and dbeta of the workgroups' sums: 64 columns per workgroup, whose wavefronts share the parts
-constexpr int kFoldWaves = 16;
+// dgamma and dbeta of the workgroups' sums: 16 columns per workgroup, 64 lanes of each share the parts
+constexpr int kFoldColumns = 16, kFoldRuns = 64;
 
-__global__ void __launch_bounds__(kFoldWaves *dg::kWave)
+__global__ void __launch_bounds__(kFoldColumns *kFoldRuns)
 norm_fold_kernel(const float *part, uint32_t n_parts, uint32_t W, float *dgamma, float *dbeta)
 {
-    __shared__ float red[kFoldWaves][dg::kWave];
-    const uint32_t lane = threadIdx.x % dg::kWave, wave = threadIdx.x / dg::kWave, c = blockIdx.x * dg::kWave + lane;
+    __shared__ float red[kFoldRuns][kFoldColumns];
+    const uint32_t lane = threadIdx.x % kFoldColumns, run = threadIdx.x / kFoldColumns, c = blockIdx.x * kFoldColumns + lane;
     float sum = 0.0f;
     if (c < 2 * W)
-#pragma unroll 8
-        for (uint32_t p = wave; p < n_parts; p += kFoldWaves) sum += part[(uint64_t)p * 2 * W + c];
-    red[wave][lane] = sum;
-    __syncthreads();
-    if (wave != 0 || c >= 2 * W) return;
-    sum = 0.0f;
-    for (int w = 0; w < kFoldWaves; ++w) sum += red[w][lane];
-    if (c < W ? dgamma != nullptr : dbeta != nullptr) (c < W ? dgamma : dbeta - W)[c] = sum;
+#pragma unroll 16
+        for (uint32_t p = run; p < n_parts; p += kFoldRuns) sum += part[(uint64_t)p * 2 * W + c];
+    red[run][lane] = sum;
+#pragma unroll
+    for (int d = kFoldRuns / 2; d > 0; d /= 2) {
+        __syncthreads();
+        if ((int)run < d) red[run][lane] += red[run + d][lane];
+    }
+    if (run != 0 || c >= 2 * W) return;
+    sum = red[0][lane];
+    if (c < W) {
+        if (dgamma) dgamma[c] = sum;
+    } else if (dbeta) dbeta[c - W] = sum;
 }
 
 // Rows too wide for the registers of a workgroup: read again from the caches for every sum, a workgroup per row.
@@ -347,6 +379,8 @@ uint32_t parts_of(uint64_t N, uint32_t W)
     return (uint32_t)(p < most ? p : most);
 }
 
+constexpr uint64_t kMostBlocks = 2048;      // of the forward pass: as many as the chip holds at once
+
 struct Call {
     Norm a;
     uint32_t dtype, parts;
@@ -357,7 +391,8 @@ struct Call {
 template <class T, int V, int G, int K>
 void launch_spread(const Call &c)
 {
-    if (c.forward) norm_fwd_kernel<T, V, G, K, kBlock><<<(uint32_t)((c.a.N + kBlock / G - 1) / (kBlock / G)), kBlock, 0, c.st>>>(c.a);
+    const uint64_t all = (c.a.N + kBlock / G - 1) / (kBlock / G);
+    if (c.forward) norm_fwd_kernel<T, V, G, K, kBlock><<<(uint32_t)(all < kMostBlocks ? all : kMostBlocks), kBlock, 0, c.st>>>(c.a);
     else norm_bwd_kernel<T, V, G, K, kBlock><<<c.parts, kBlock, 0, c.st>>>(c.a);
 }
 
@@ -438,6 +473,6 @@ extern "C" int dg_layer_norm_bwd(const void *x, uint64_t ldx, const float *gamma
     const uint32_t parts = parts_of(N, W);
     if (N) launch({{x, dy, dx, gamma, nullptr, part, ldx, lddy, lddx, N, W, eps, 1.0f / (float)W}, dtype, parts, false, (hipStream_t)stream});
     if (weights)
-        norm_fold_kernel<<<(2 * W + dg::kWave - 1) / dg::kWave, kFoldWaves * dg::kWave, 0, (hipStream_t)stream>>>(part, parts, W, dgamma, dbeta);
+        norm_fold_kernel<<<(2 * W + kFoldColumns - 1) / kFoldColumns, kFoldColumns * kFoldRuns, 0, (hipStream_t)stream>>>(part, parts, W, dgamma, dbeta);
     return dg::launch_status(who);
 }

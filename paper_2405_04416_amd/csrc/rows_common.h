@@ -28,6 +28,22 @@ __device__ __forceinline__ void store(T *p, const float (&in)[V])
     *reinterpret_cast<Pack<T, V> *>(p) = a;
 }
 
+// 16 bytes past the caches, which arrays far larger than them pass through without being read again
+template <class T, int V>
+__device__ __forceinline__ Pack<T, V> load_streamed(const T *p)
+{
+    static_assert(sizeof(Pack<T, V>) == 16, "one load");
+    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(Pack<T, V>, __builtin_nontemporal_load(reinterpret_cast<const u4 *>(p)));
+}
+
+template <class T, int V>
+__device__ __forceinline__ void store_streamed(T *p, const Pack<T, V> &a)
+{
+    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+    __builtin_nontemporal_store(__builtin_bit_cast(u4, a), reinterpret_cast<u4 *>(p));
+}
+
 inline size_t item_bytes(uint32_t dtype) { return dtype == DG_F32 ? 4 : 2; }
 inline bool known_type(uint32_t dtype) { return dtype == DG_F32 || dtype == DG_F16 || dtype == DG_BF16; }
 
