@@ -14,6 +14,8 @@ namespace {
 using namespace dg_rows;
 
 constexpr int kBlock = 256;
+// From this size on arrays go past the caches: 2^28 fp16 values forward 194 us against 207 in rows of 32.
+constexpr uint64_t kStreamedBytes = 64 << 20;
 
 // Sum over G neighbouring lanes, in all of them: exchanges inside groups of 4, 8 and 16 lanes on the way to the vector unit, wider ones
 // through the LDS crossbar.
@@ -75,16 +77,29 @@ __device__ __forceinline__ bool inside(uint32_t W, uint32_t lane, int k, int G, 
     return c < W;
 }
 
-template <class T, int V, int G, int K>
+template <class T, int V, int G, int K, bool kStreamed>
 __device__ __forceinline__ void read(const void *p, uint64_t ld, uint64_t row, const Norm &a, uint32_t lane, Pack<T, V> (&out)[K])
 {
     uint32_t c;
 #pragma unroll
     for (int k = 0; k < K; ++k)
-        if (inside<V>(a.W, lane, k, G, c) && row < a.N) out[k] = *reinterpret_cast<const Pack<T, V> *>((const T *)p + row * ld + c);
-        else
+        if (inside<V>(a.W, lane, k, G, c) && row < a.N) {
+            const T *at = (const T *)p + row * ld + c;
+            if constexpr (kStreamed) out[k] = load_streamed<T, V>(at);
+            else out[k] = *reinterpret_cast<const Pack<T, V> *>(at);
+        } else
 #pragma unroll
             for (int v = 0; v < V; ++v) out[k].v[v] = (T)0.0f;
+}
+
+template <class T, int V, bool kStreamed>
+__device__ __forceinline__ void write(T *p, const float (&in)[V])
+{
+    Pack<T, V> a;
+#pragma unroll
+    for (int v = 0; v < V; ++v) a.v[v] = (T)in[v];
+    if constexpr (kStreamed) store_streamed<T, V>(p, a);
+    else *reinterpret_cast<Pack<T, V> *>(p) = a;
 }
 
 template <class T, int V, int K>
@@ -123,12 +138,14 @@ __device__ __forceinline__ float mean(const float (&x)[K][V], const Norm &a, flo
 }
 
 // Workgroups go through the rows side by side: workgroup b takes rows b R, b R + 1, ... of every gridDim.x R, R = kThreads / G at a
-// time, with gamma and beta in registers; the next row is on its way while one is worked on.
-template <class T, int V, int G, int K, int kThreads>
+// time, with gamma and beta in registers.  Where a row takes more than one vector per lane the next row is on its way while one is worked
+// on (2^16 rows of 4096 bf16 values, backward: 316 us against 523); narrower rows have wavefronts enough (2^20 of 256: 290 without, 322).
+template <class T, int V, int G, int K, int kThreads, bool kStreamed>
 __global__ void __launch_bounds__(kThreads)
 norm_fwd_kernel(Norm a)
 {
     constexpr int R = kThreads / G;
+    constexpr bool kAhead = K > 1;
     __shared__ float red[kThreads / dg::kWave][1], red2[kThreads / dg::kWave][1];
     const uint32_t lane = threadIdx.x % G;
     float gamma[K][V], beta[K][V];
@@ -136,13 +153,14 @@ norm_fwd_kernel(Norm a)
     weights<V, G, K>(a.beta, 0.0f, a, lane, beta);
     uint64_t row = (uint64_t)blockIdx.x * R + threadIdx.x / G;
     Pack<T, V> next[K];
-    read<T, V, G, K>(a.x, a.ldx, row, a, lane, next);
+    if (kAhead) read<T, V, G, K, kStreamed>(a.x, a.ldx, row, a, lane, next);
     for (uint64_t row0 = (uint64_t)blockIdx.x * R; row0 < a.N; row0 += (uint64_t)gridDim.x * R) {
         float x[K][V];
+        if (!kAhead) read<T, V, G, K, kStreamed>(a.x, a.ldx, row, a, lane, next);
         widen<T, V, K>(next, x);
         const uint64_t now = row;
         row += (uint64_t)gridDim.x * R;
-        read<T, V, G, K>(a.x, a.ldx, row, a, lane, next);
+        if (kAhead) read<T, V, G, K, kStreamed>(a.x, a.ldx, row, a, lane, next);
         const float m = mean<V, G, K, kThreads>(x, a, red);
         float sum[1] = {0.0f};
         uint32_t c;
@@ -159,16 +177,17 @@ norm_fwd_kernel(Norm a)
             if (inside<V>(a.W, lane, k, G, c) && now < a.N) {
 #pragma unroll
                 for (int v = 0; v < V; ++v) x[k][v] = x[k][v] * s * gamma[k][v] + beta[k][v];
-                store<T, V>(y + c, x[k]);
+                write<T, V, kStreamed>(y + c, x[k]);
             }
     }
 }
 
-template <class T, int V, int G, int K, int kThreads>
+template <class T, int V, int G, int K, int kThreads, bool kStreamed>
 __global__ void __launch_bounds__(kThreads)
 norm_bwd_kernel(Norm a)
 {
     constexpr int kWaves = kThreads / dg::kWave, R = kThreads / G;
+    constexpr bool kAhead = K > 1;
     __shared__ float red1[kWaves][1], red3[kWaves][3];
     const uint32_t lane = threadIdx.x % G;
     float gamma[K][V], sum_g[K][V] = {}, sum_b[K][V] = {};
@@ -176,17 +195,20 @@ norm_bwd_kernel(Norm a)
     uint32_t c;
     uint64_t row = (uint64_t)blockIdx.x * R + threadIdx.x / G;
     Pack<T, V> next_x[K], next_dy[K];
-    read<T, V, G, K>(a.x, a.ldx, row, a, lane, next_x);
-    read<T, V, G, K>(a.dy, a.lddy, row, a, lane, next_dy);
+    auto fetch = [&] {
+        read<T, V, G, K, kStreamed>(a.x, a.ldx, row, a, lane, next_x);
+        read<T, V, G, K, kStreamed>(a.dy, a.lddy, row, a, lane, next_dy);
+    };
+    if (kAhead) fetch();
     for (uint64_t row0 = (uint64_t)blockIdx.x * R; row0 < a.N; row0 += (uint64_t)gridDim.x * R) {
         const bool held = row < a.N;                // lanes without a row go along: sums are over whole groups of lanes
         T *out = (T *)a.out + row * a.ldo;
         float x[K][V], dy[K][V];
+        if (!kAhead) fetch();
         widen<T, V, K>(next_x, x);
         widen<T, V, K>(next_dy, dy);
         row += (uint64_t)gridDim.x * R;
-        read<T, V, G, K>(a.x, a.ldx, row, a, lane, next_x);
-        read<T, V, G, K>(a.dy, a.lddy, row, a, lane, next_dy);
+        if (kAhead) fetch();
         const float m = mean<V, G, K, kThreads>(x, a, red1);
         float sum[3] = {0.0f, 0.0f, 0.0f};          // of squared deviations, of g, of g times the deviation
 #pragma unroll
@@ -214,7 +236,7 @@ norm_bwd_kernel(Norm a)
                     sum_b[k][v] += dy[k][v];
                 }
             }
-            if (inside<V>(a.W, lane, k, G, c) && held && a.out) store<T, V>(out + c, o);
+            if (inside<V>(a.W, lane, k, G, c) && held && a.out) write<T, V, kStreamed>(out + c, o);
         }
     }
     if (!a.part) return;
@@ -351,32 +373,39 @@ int check_rows(const char *who, const void *p, uint64_t ld, uint32_t W, uint32_t
     return DG_OK;
 }
 
-// How a row of n vectors is spread: K of them in each of G lanes.  Up to 64 lanes of a wavefront the combination with the fewest idle
-// places is taken, the one with fewer vectors per lane among equals; then a wavefront with up to 4, a workgroup with up to 8.
+// How a row of n vectors is spread.  Vectors of 16 bytes: up to 64 over as many lanes, rounded up to a power of two; several per lane
+// would leave fewer lanes idle, but a load then takes parts of many lines, which loads past the caches fetch again (48 bf16 values a row,
+// two lanes of three vectors: 1.9 TB/s forward, eight lanes 5.5).  Smaller vectors, where sums across lanes weigh more: up to 4 in a lane
+// with as few idle places as possible (37 fp32 values, 16 lanes of three: 4.0 TB/s, 64 lanes 2.2).  Then a workgroup with up to 8.
 struct Spread { int G, K; };
 
-Spread spread_of(uint32_t n)
+Spread spread_of(uint32_t n, bool small)
 {
     Spread best = {0, 0};
-    for (int K = 1; K <= 3; ++K)
-        for (int G = 1; G <= 64; G *= 2)
-            if ((uint32_t)(G * K) >= n) {
-                if (best.G == 0 || G * K < best.G * best.K) best = {G, K};
-                break;
-            }
+    if (small)
+        for (int K : {4, 3, 1})
+            for (int G = 1; G <= 64; G *= 2)
+                if ((uint32_t)(G * K) >= n) {
+                    if (best.G == 0 || G * K < best.G * best.K) best = {G, K};
+                    break;
+                }
     if (best.G) return best;
-    if (n <= 256) return {64, 4};
+    int G = 1;
+    while (G < 64 && (uint32_t)G < n) G *= 2;
+    for (int K = 1; K <= 4; ++K)
+        if (n <= (uint32_t)(G * K)) return {G, K};
     for (int K = 2; K <= 8; K *= 2)
         if (n <= 256u * K) return {256, K};
     return {0, 0};
 }
 
-// workgroups of the backward pass: each leaves 2 W sums, so that wide rows have fewer
+// Workgroups of the backward pass.  Each leaves 2 W sums, so that wide rows have fewer, and each has some rows to itself, but all compute
+// units have two.  (8192 rows of 4096 bf16 values: 512 workgroups 57.7 us, 1024 66.2.)
 uint32_t parts_of(uint64_t N, uint32_t W)
 {
-    const uint64_t most = W <= 512 ? 2048 : W <= 2048 ? 1024 : 512, rows = W <= 64 ? 64 : W <= 512 ? 16 : 4;
-    const uint64_t p = (N + rows - 1) / rows;
-    return (uint32_t)(p < most ? p : most);
+    const uint64_t most = W <= 512 ? 2048 : W <= 2048 ? 1024 : 512, rows = W <= 64 ? 64 : W <= 2048 ? 16 : 8;
+    const uint64_t least = (N + 3) / 4 < 512 ? (N + 3) / 4 : 512, p = (N + rows - 1) / rows;
+    return (uint32_t)(p > most ? most : p < least ? least : p);
 }
 
 constexpr uint64_t kMostBlocks = 2048;      // of the forward pass: as many as the chip holds at once
@@ -392,22 +421,28 @@ template <class T, int V, int G, int K>
 void launch_spread(const Call &c)
 {
     const uint64_t all = (c.a.N + kBlock / G - 1) / (kBlock / G);
-    if (c.forward) norm_fwd_kernel<T, V, G, K, kBlock><<<(uint32_t)(all < kMostBlocks ? all : kMostBlocks), kBlock, 0, c.st>>>(c.a);
-    else norm_bwd_kernel<T, V, G, K, kBlock><<<c.parts, kBlock, 0, c.st>>>(c.a);
+    const uint32_t grid = c.forward ? (uint32_t)(all < kMostBlocks ? all : kMostBlocks) : c.parts;
+    auto go = [&](auto kernel) { kernel<<<grid, kBlock, 0, c.st>>>(c.a); };
+    if constexpr (V * sizeof(T) == 16)
+        if (c.a.N * c.a.W * sizeof(T) >= kStreamedBytes)
+            return c.forward ? go(norm_fwd_kernel<T, V, G, K, kBlock, true>) : go(norm_bwd_kernel<T, V, G, K, kBlock, true>);
+    c.forward ? go(norm_fwd_kernel<T, V, G, K, kBlock, false>) : go(norm_bwd_kernel<T, V, G, K, kBlock, false>);
 }
 
 template <class T, int V, int G>
 void launch_lanes(const Call &c, int K)
 {
-    if (K == 1) launch_spread<T, V, G, 1>(c);
-    else if (K == 2) launch_spread<T, V, G, 2>(c);
-    else launch_spread<T, V, G, 3>(c);
+    if constexpr (V * sizeof(T) < 16) {
+        if (K == 4) return launch_spread<T, V, G, 4>(c);
+        if (K == 3) return launch_spread<T, V, G, 3>(c);
+    }
+    launch_spread<T, V, G, 1>(c);
 }
 
 template <class T, int V>
 void launch_rows(const Call &c)
 {
-    const Spread s = spread_of(c.a.W / V);
+    const Spread s = spread_of(c.a.W / V, V * sizeof(T) < 16);
     switch (s.G) {
     case 1: return launch_lanes<T, V, 1>(c, s.K);
     case 2: return launch_lanes<T, V, 2>(c, s.K);
@@ -415,24 +450,28 @@ void launch_rows(const Call &c)
     case 8: return launch_lanes<T, V, 8>(c, s.K);
     case 16: return launch_lanes<T, V, 16>(c, s.K);
     case 32: return launch_lanes<T, V, 32>(c, s.K);
-    case 64: return s.K == 4 ? launch_spread<T, V, 64, 4>(c) : launch_lanes<T, V, 64>(c, s.K);
+    case 64:
+        return s.K == 1   ? launch_spread<T, V, 64, 1>(c)
+               : s.K == 2 ? launch_spread<T, V, 64, 2>(c)
+               : s.K == 3 ? launch_spread<T, V, 64, 3>(c)
+                          : launch_spread<T, V, 64, 4>(c);
     case 256: return s.K == 2 ? launch_spread<T, V, 256, 2>(c) : s.K == 4 ? launch_spread<T, V, 256, 4>(c) : launch_spread<T, V, 256, 8>(c);
     }
     if (c.forward) norm_fwd_wide_kernel<T><<<(uint32_t)c.a.N, kWide, 0, c.st>>>(c.a);
     else norm_bwd_wide_kernel<T><<<c.parts, kWide, 0, c.st>>>(c.a);
 }
 
-// vectors of 16 bytes where every row allows it, single values otherwise
+// the widest vectors that every row allows
 void launch(const Call &c)
 {
     const Norm &a = c.a;
-    const uint32_t item = (uint32_t)item_bytes(c.dtype);
-    bool wide = a.W * item % 16 == 0 && rows_aligned(a.x, a.ldx, c.dtype, 16);
-    if (!c.forward) wide = wide && rows_aligned(a.dy, a.lddy, c.dtype, 16);
-    if (a.out) wide = wide && rows_aligned(a.out, a.ldo, c.dtype, 16);
-    if (c.dtype == DG_F32) wide ? launch_rows<float, 4>(c) : launch_rows<float, 1>(c);
-    else if (c.dtype == DG_F16) wide ? launch_rows<f16, 8>(c) : launch_rows<f16, 1>(c);
-    else wide ? launch_rows<bf16, 8>(c) : launch_rows<bf16, 1>(c);
+    auto allowed = [&](uint32_t bytes) {
+        return a.W * item_bytes(c.dtype) % bytes == 0 && rows_aligned(a.x, a.ldx, c.dtype, bytes) && (c.forward || rows_aligned(a.dy, a.lddy, c.dtype, bytes)) &&
+               (!a.out || rows_aligned(a.out, a.ldo, c.dtype, bytes));
+    };
+    if (c.dtype == DG_F32) allowed(16) ? launch_rows<float, 4>(c) : launch_rows<float, 1>(c);
+    else if (c.dtype == DG_F16) allowed(16) ? launch_rows<f16, 8>(c) : allowed(8) ? launch_rows<f16, 4>(c) : launch_rows<f16, 1>(c);
+    else allowed(16) ? launch_rows<bf16, 8>(c) : allowed(8) ? launch_rows<bf16, 4>(c) : launch_rows<bf16, 1>(c);
 }
 
 }  // namespace
