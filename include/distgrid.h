@@ -549,8 +549,8 @@ int dg_layer_norm_bwd(const void *x, uint64_t ldx, const float *gamma, const voi
  * offsets on the device, as dg_march_segments writes them); N is then the number of rows that there is room for: rows that no
  * sequence has are neither read nor written, rows from N on neither, whatever `first` says.
  * reverse != 0: every sequence from its last row to its first; h0 is the state behind the last row.
- * From |z| = 88 on a gate is exactly 0 or 1, and what it shuts out is not looked at, not even infinities or NaN: z >= 88
- * (+infinity) passes a token over, z <= -88 (-infinity, the lowest value of a type) forgets the past.  z NaN gives NaN.
+ * From |z| = 87 on a gate is exactly 0 or 1, and what it shuts out is not looked at, not even infinities or NaN: z >= 87
+ * (+infinity) passes a token over, z <= -87 (-infinity, the lowest value of a type) forgets the past.  z NaN gives NaN.
  * states: NULL, or dg_recurrence_state_count(N, W) floats for the backward pass (the state at every 16th row).
  * ws: dg_recurrence_workspace_bytes(N, n_seq, W) bytes (NULL where that is 0), 16-byte aligned.
  * Errors: DG_ERR_ARG also for N that n_seq does not divide (first NULL); DG_ERR_UNSUPPORTED for N >= 2^32, W > 2^20. */

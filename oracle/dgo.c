@@ -868,13 +868,13 @@ void dgo_layer_norm_bwd(const double *x, const double *gamma, const double *dy, 
     }
 }
 
-static double opening(double z) { return z >= 88.0 ? 1.0 : z <= -88.0 ? 0.0 : 1.0 / (1.0 + exp(-z)); }
+static double opening(double z) { return z >= 87.0 ? 1.0 : z <= -87.0 ? 0.0 : 1.0 / (1.0 + exp(-z)); }
 
 /* the state after a token of gate z and input u */
 static double recur(double z, double u, double h)
 {
-    if (z >= 88.0) return h;
-    if (z <= -88.0) return u;
+    if (z >= 87.0) return h;
+    if (z <= -87.0) return u;
     return opening(z) * h + opening(-z) * u;
 }
 

@@ -199,7 +199,7 @@ void dgo_layer_norm_fwd(const double *x, const double *gamma, const double *beta
 void dgo_layer_norm_bwd(const double *x, const double *gamma, const double *dy, uint64_t N, uint32_t W, double eps, double *dx,
                         double *dgamma, double *dbeta);
 /* h <- a h + (1 - a) u, a = 1 / (1 + e^-z), along rows [first[j], first[j+1]) of sequence j, or from the last to the first
- * (reverse); |z| >= 88: a is 0 or 1 and what it multiplies by 0 is skipped.  Rows of no sequence are left alone.  h0 may be NULL. */
+ * (reverse); |z| >= 87: a is 0 or 1 and what it multiplies by 0 is skipped.  Rows of no sequence are left alone.  h0 may be NULL. */
 void dgo_recurrence_fwd(const double *z, const double *u, uint32_t n_seq, const uint32_t *first, uint32_t W, int reverse,
                         const double *h0, double *y, double *h_last);
 /* gradients of sum(dy * y) + sum(dh_last * h_last); dh_last may be NULL */

@@ -9,7 +9,6 @@ namespace {
 using namespace dg_rows;
 
 constexpr int kBlock = 256;
-constexpr uint64_t kStreamedBytes = 64 << 20;
 
 struct Drop {
     const void *x, *r;

@@ -1,7 +1,7 @@
 // Gated linear recurrence along sequences of rows, channel by channel:
 //   a = 1 / (1 + e^-z),  c = 1 - a = 1 / (1 + e^z),  h_t = a_t h_{t-1} + c_t u_t,  y_t = h_t.
 // Its backward pass: G_t = dy_t + a_{t+1} G_{t+1} from the last token back, du = c G, dz = a c G (h_{t-1} - u_t), dh0 = a_0 G_0.
-// From |z| = 88 on a and c are exactly 0 and 1: what a gate of 0 multiplies is not looked at, be it infinite or NaN.
+// From |z| = 87 on a and c are exactly 0 and 1: what a gate of 0 multiplies is not looked at, be it infinite or NaN.
 //
 // Tokens have a place in the order in which they are gone through: their row, or N - 1 - row back to front.  The forward pass
 // keeps the state before every kKeep-th place in fp32; the backward pass computes the states between them again.
@@ -13,22 +13,47 @@ using namespace dg_rows;
 
 constexpr int kBlock = 256, kKeep = 16;
 constexpr float kLeast = 1.17549435e-38f;       // the smallest normal number
-constexpr float kShut = 88.0f;      // e^-88 is the smallest power that is a normal fp32 number, about
+constexpr float kShut = 87.0f;                  // up to here e^z, e^-z, a and c are normal numbers
+constexpr float kLog2e = 1.44269504f;
 
 struct Gate { float a, c; };
 
-// both sides of the gate to full relative precision: the larger one is s = 1 / (1 + e^-|z|), the smaller one e^-|z| s
+// both sides of an open gate to full relative precision
 __device__ __forceinline__ Gate gate(float z)
 {
-    const float e = __expf(-fabsf(z)), s = __builtin_amdgcn_rcpf(1.0f + e), t = e * s;
-    return z >= 0.0f ? Gate{s, t} : Gate{t, s};
+    const float e = __builtin_amdgcn_exp2f(z * -kLog2e), a = __builtin_amdgcn_rcpf(1.0f + e);
+    return {a, e * a};
 }
 
-// h_t of h_{t-1}
-__device__ __forceinline__ float advance(float z, float u, float h)
+// Whether a wavefront has a shut gate among the tokens that it has loaded.  One operation per two values finds out; the tokens are then
+// gone through without looking at each gate.
+template <class T, int V, int M>
+__device__ __forceinline__ bool any_shut(const Pack<T, V> (&z)[M])
+{
+    float most = 0.0f;
+#pragma unroll
+    for (int k = 0; k < M; ++k)
+#pragma unroll
+        for (int v = 0; v < V; ++v) most = fmaxf(most, fabsf((float)z[k].v[v]));
+    return __any(most >= kShut);
+}
+
+// The gate of a token, its input's share b = c u, and h_t.  kShutting: the gate may be shut.
+struct Step { float a, c, b; };
+
+template <bool kShutting>
+__device__ __forceinline__ Step step_of(float z, float u)
 {
     const Gate g = gate(z);
-    return (z <= -kShut ? 0.0f : g.a * h) + (z >= kShut ? 0.0f : g.c * u);
+    if (!kShutting) return {g.a, g.c, g.c * u};
+    const bool hold = z >= kShut, reset = z <= -kShut;
+    return {reset ? 0.0f : g.a, reset ? 1.0f : hold ? 0.0f : g.c, reset ? u : hold ? 0.0f : g.c * u};
+}
+
+template <bool kShutting>
+__device__ __forceinline__ float advance(const Step &s, float h)
+{
+    return kShutting && s.a == 0.0f ? s.b : fmaf(s.a, h, s.b);
 }
 
 // a stretch of tokens takes the state h to join(A, h, B), A the product of its gates
@@ -148,6 +173,18 @@ __device__ __forceinline__ void in_pieces(uint64_t p, uint64_t end, F f)
     }
 }
 
+template <class T, int V, int M, bool kFull, bool kShutting>
+__device__ __forceinline__ void advance_loaded(const Pack<T, V> (&z)[M], const Pack<T, V> (&u)[M], const Column<T, V> &y, int n, float (&h)[V])
+{
+#pragma unroll
+    for (int k = 0; k < M; ++k)
+        if (kFull || k < n) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) h[v] = advance<kShutting>(step_of<kShutting>((float)z[k].v[v], (float)u[k].v[v]), h[v]);
+            store<T, V>(y.at + k * y.step, h);
+        }
+}
+
 template <class T, int V, int M, bool kFull>
 __device__ __forceinline__ void advance_tokens(const Shape &d, const Fwd &f, uint32_t c, uint64_t p, int n, float (&h)[V])
 {
@@ -155,13 +192,8 @@ __device__ __forceinline__ void advance_tokens(const Shape &d, const Fwd &f, uin
     load_tokens<T, V, M, kFull>(Column<T, V>(d, f.z, f.ldz, c, p), n, z);
     load_tokens<T, V, M, kFull>(Column<T, V>(d, f.u, f.ldu, c, p), n, u);
     const Column<T, V> y(d, f.y, f.ldy, c, p);
-#pragma unroll
-    for (int k = 0; k < M; ++k)
-        if (kFull || k < n) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) h[v] = advance((float)z[k].v[v], (float)u[k].v[v], h[v]);
-            store<T, V>(y.at + k * y.step, h);
-        }
+    if (any_shut<T, V, M>(z)) advance_loaded<T, V, M, kFull, true>(z, u, y, n, h);
+    else advance_loaded<T, V, M, kFull, false>(z, u, y, n, h);
 }
 
 // y of places [p, end) of a sequence from the state before them, and the states that are kept
@@ -176,6 +208,39 @@ __device__ __forceinline__ void advance_places(const Shape &d, const Fwd &f, uin
     });
 }
 
+// Forwards through the tokens for what G is multiplied with, a, c and q = a c (h_{t-1} - u), then backwards with G.
+template <class T, int V, int M, bool kFull, bool kShutting>
+__device__ __forceinline__ void retreat_loaded(const Pack<T, V> (&z)[M], const Pack<T, V> (&u)[M], const Pack<T, V> (&dy)[M], const Column<T, V> &dz,
+                                               const Column<T, V> &du, int n, float (&h)[V], float (&G)[V])
+{
+    float a[M][V], c[M][V], q[M][V];
+#pragma unroll
+    for (int k = 0; k < M; ++k)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float uu = (float)u[k].v[v];
+            const Step s = step_of<kShutting>((float)z[k].v[v], uu);
+            a[k][v] = s.a;
+            c[k][v] = s.c;
+            q[k][v] = kShutting && (s.a == 0.0f || s.c == 0.0f) ? 0.0f : s.a * s.c * (h[v] - uu);
+            h[v] = advance<kShutting>(s, h[v]);
+        }
+#pragma unroll
+    for (int k = M - 1; k >= 0; --k)
+        if (kFull || k < n) {
+            float oz[V], ou[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                G[v] += (float)dy[k].v[v];
+                oz[v] = kShutting && q[k][v] == 0.0f ? 0.0f : q[k][v] * G[v];
+                ou[v] = kShutting && c[k][v] == 0.0f ? 0.0f : c[k][v] * G[v];
+                G[v] = kShutting && a[k][v] == 0.0f ? 0.0f : a[k][v] * G[v];
+            }
+            store<T, V>(dz.at + k * dz.step, oz);
+            store<T, V>(du.at + k * du.step, ou);
+        }
+}
+
 template <class T, int V, int M, bool kFull>
 __device__ __forceinline__ void retreat_tokens(const Shape &d, const Bwd &b, uint32_t c, uint64_t p, int n, float (&h)[V], float (&G)[V])
 {
@@ -183,31 +248,9 @@ __device__ __forceinline__ void retreat_tokens(const Shape &d, const Bwd &b, uin
     load_tokens<T, V, M, kFull>(Column<T, V>(d, b.z, b.ldz, c, p), n, z);
     load_tokens<T, V, M, kFull>(Column<T, V>(d, b.u, b.ldu, c, p), n, u);
     load_tokens<T, V, M, kFull>(Column<T, V>(d, b.dy, b.lddy, c, p), n, dy);
-    float before[M][V];
-#pragma unroll
-    for (int k = 0; k < M; ++k)
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            before[k][v] = h[v];
-            h[v] = advance((float)z[k].v[v], (float)u[k].v[v], h[v]);
-        }
     const Column<T, V> dz(d, b.dz, b.lddz, c, p), du(d, b.du, b.lddu, c, p);
-#pragma unroll
-    for (int k = M - 1; k >= 0; --k)
-        if (kFull || k < n) {
-            float oz[V], ou[V];
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const float zz = (float)z[k].v[v];
-                const Gate g = gate(zz);
-                G[v] += (float)dy[k].v[v];
-                oz[v] = fabsf(zz) >= kShut ? 0.0f : g.a * g.c * (before[k][v] - (float)u[k].v[v]) * G[v];
-                ou[v] = zz >= kShut ? 0.0f : g.c * G[v];
-                G[v] = zz <= -kShut ? 0.0f : g.a * G[v];
-            }
-            store<T, V>(dz.at + k * dz.step, oz);
-            store<T, V>(du.at + k * du.step, ou);
-        }
+    if (any_shut<T, V, M>(z)) retreat_loaded<T, V, M, kFull, true>(z, u, dy, dz, du, n, h, G);
+    else retreat_loaded<T, V, M, kFull, false>(z, u, dy, dz, du, n, h, G);
 }
 
 // dz and du of places [p, end) of the sequence that begins at place `begin`, from the gradient G behind them
@@ -306,22 +349,56 @@ __device__ __forceinline__ void backwards(const Shape &d, uint32_t chunk, F f)
     }
 }
 
+// In both: the product of the gates of these tokens first, which is 0 or underflows only where one of them is shut or times() mends it.
+template <class T, int V, int M, bool kFull, bool kShutting>
+__device__ __forceinline__ void sum_loaded(const Pack<T, V> (&z)[M], const Pack<T, V> (&u)[M], int n, float (&A)[V], float (&h)[V])
+{
+    float product[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) product[v] = 1.0f;
+#pragma unroll
+    for (int k = 0; k < M; ++k)
+        if (kFull || k < n) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const Step s = step_of<kShutting>((float)z[k].v[v], (float)u[k].v[v]);
+                h[v] = advance<kShutting>(s, h[v]);
+                product[v] = kShutting ? times(product[v], s.a) : product[v] * s.a;
+            }
+        }
+#pragma unroll
+    for (int v = 0; v < V; ++v) A[v] = times(A[v], kShutting ? product[v] : fmaxf(product[v], kLeast));
+}
+
 template <class T, int V, int M, bool kFull>
 __device__ __forceinline__ void sum_tokens(const Shape &d, const Fwd &f, uint32_t c, uint64_t p, int n, float (&A)[V], float (&h)[V])
 {
     Pack<T, V> z[M], u[M];
     load_tokens<T, V, M, kFull>(Column<T, V>(d, f.z, f.ldz, c, p), n, z);
     load_tokens<T, V, M, kFull>(Column<T, V>(d, f.u, f.ldu, c, p), n, u);
+    if (any_shut<T, V, M>(z)) sum_loaded<T, V, M, kFull, true>(z, u, n, A, h);
+    else sum_loaded<T, V, M, kFull, false>(z, u, n, A, h);
+}
+
+template <class T, int V, int M, bool kFull, bool kShutting>
+__device__ __forceinline__ void sum_gradients_loaded(const Pack<T, V> (&z)[M], const Pack<T, V> (&dy)[M], int n, float (&A)[V], float (&G)[V])
+{
+    float product[V];
 #pragma unroll
-    for (int k = 0; k < M; ++k)
+    for (int v = 0; v < V; ++v) product[v] = 1.0f;
+#pragma unroll
+    for (int k = M - 1; k >= 0; --k)
         if (kFull || k < n) {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const float zz = (float)z[k].v[v];
-                h[v] = advance(zz, (float)u[k].v[v], h[v]);
-                A[v] = times(A[v], zz <= -kShut ? 0.0f : gate(zz).a);
+                const Step s = step_of<kShutting>((float)z[k].v[v], 0.0f);
+                G[v] += (float)dy[k].v[v];
+                G[v] = kShutting && s.a == 0.0f ? 0.0f : s.a * G[v];
+                product[v] = kShutting ? times(product[v], s.a) : product[v] * s.a;
             }
         }
+#pragma unroll
+    for (int v = 0; v < V; ++v) A[v] = times(A[v], kShutting ? product[v] : fmaxf(product[v], kLeast));
 }
 
 template <class T, int V, int M, bool kFull>
@@ -330,17 +407,8 @@ __device__ __forceinline__ void sum_gradients(const Shape &d, const Bwd &b, uint
     Pack<T, V> z[M], dy[M];
     load_tokens<T, V, M, kFull>(Column<T, V>(d, b.z, b.ldz, c, p), n, z);
     load_tokens<T, V, M, kFull>(Column<T, V>(d, b.dy, b.lddy, c, p), n, dy);
-#pragma unroll
-    for (int k = M - 1; k >= 0; --k)
-        if (kFull || k < n) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const float zz = (float)z[k].v[v], a = zz <= -kShut ? 0.0f : gate(zz).a;
-                G[v] += (float)dy[k].v[v];
-                G[v] = a == 0.0f ? 0.0f : a * G[v];
-                A[v] = times(A[v], a);
-            }
-        }
+    if (any_shut<T, V, M>(z)) sum_gradients_loaded<T, V, M, kFull, true>(z, dy, n, A, G);
+    else sum_gradients_loaded<T, V, M, kFull, false>(z, dy, n, A, G);
 }
 
 // sums[0]: A, sums[1]: B, each [n_chunks, W].  copy: NULL, or room for h0 (backward: dh_last), which the last launch then reads there
@@ -399,38 +467,47 @@ chunk_sums_bwd_kernel(Shape d, Bwd b, float *sums, float *copy)
 }
 
 // What comes before each chunk (backward: behind it), written over its A.  A workgroup has 16 channels and cuts the chunks into
-// 64 runs: each thread joins its run, then the runs before its own, then goes through its run again.
+// 64 runs of at most P, which its threads hold in registers: each joins its run, then the runs before its own, then the chunks of its run.
 constexpr int kJoinChannels = 16, kRuns = 64;
 
+template <int P>
 __global__ void __launch_bounds__(kJoinChannels *kRuns)
 join_chunks_kernel(uint32_t n_chunks, uint32_t W, uint32_t from_the_end, float *sums)
 {
     __shared__ float run_A[kRuns][kJoinChannels], run_B[kRuns][kJoinChannels];
     const uint32_t lane = threadIdx.x % kJoinChannels, run = threadIdx.x / kJoinChannels, c = blockIdx.x * kJoinChannels + lane;
-    const uint32_t per = (n_chunks + kRuns - 1) / kRuns, k0 = run * per < n_chunks ? run * per : n_chunks, k1 = k0 + per < n_chunks ? k0 + per : n_chunks;
+    const uint32_t per = (n_chunks + kRuns - 1) / kRuns, k0 = run * per;
     const uint64_t to_B = (uint64_t)n_chunks * W;
-    auto at = [&](uint32_t k) { return (uint64_t)(from_the_end ? n_chunks - 1 - k : k) * W + c; };
-    float A = 1.0f, B = 0.0f;
-    if (c < W) {
-#pragma unroll 8
-        for (uint32_t k = k0; k < k1; ++k) {
-            const float a = sums[at(k)], b = sums[to_B + at(k)];
-            B = join(a, B, b);
-            A = times(A, a);
-        }
+    auto held = [&](int i) { return (uint32_t)i < per && k0 + i < n_chunks && c < W; };
+    auto at = [&](int i) { return (uint64_t)(from_the_end ? n_chunks - 1 - (k0 + i) : k0 + i) * W + c; };
+    float a[P], b[P], A = 1.0f, B = 0.0f;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        a[i] = held(i) ? sums[at(i)] : 1.0f;
+        b[i] = held(i) ? sums[to_B + at(i)] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        B = join(a[i], B, b[i]);
+        A = times(A, a[i]);
     }
     run_A[run][lane] = A;
     run_B[run][lane] = B;
     __syncthreads();
-    if (c >= W) return;
     float h = 0.0f;
     for (uint32_t r = 0; r < run; ++r) h = join(run_A[r][lane], h, run_B[r][lane]);
-#pragma unroll 8
-    for (uint32_t k = k0; k < k1; ++k) {
-        const float a = sums[at(k)], b = sums[to_B + at(k)];
-        sums[at(k)] = h;
-        h = join(a, h, b);
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        if (held(i)) sums[at(i)] = h;
+        h = join(a[i], h, b[i]);
     }
+}
+
+void join_chunks(uint32_t n_chunks, uint32_t W, uint32_t from_the_end, float *sums, hipStream_t st)
+{
+    const uint32_t grid = (W + kJoinChannels - 1) / kJoinChannels;
+    auto go = [&](auto kernel) { kernel<<<grid, kJoinChannels * kRuns, 0, st>>>(n_chunks, W, from_the_end, sums); };
+    n_chunks <= 8 * kRuns ? go(join_chunks_kernel<8>) : go(join_chunks_kernel<32>);
 }
 
 template <class T, int V>
@@ -490,7 +567,7 @@ int check_rows(const char *who, const void *p, uint64_t ld, const Shape &d, uint
 
 // Few sequences: chunks of places instead, enough of them for kWanted lanes of two channels, each of kKeep places at least.
 constexpr uint64_t kWanted = 1 << 18;
-constexpr uint32_t kMostChunks = 4096;
+constexpr uint32_t kMostChunks = 32 * kRuns;
 
 void cut(Shape &d)
 {
@@ -518,7 +595,7 @@ void launch_fwd(const Shape &d, Fwd f, float *sums, hipStream_t st)
     float *copy = f.h0 && f.h0 == f.h_last ? sums + (size_t)d.n_chunks * d.W * 2 : nullptr;
     chunk_sums_fwd_kernel<T, V><<<grid, kBlock, 0, st>>>(d, f, sums, copy);
     if (copy) f.h0 = copy;
-    join_chunks_kernel<<<(d.W + kJoinChannels - 1) / kJoinChannels, kJoinChannels * kRuns, 0, st>>>(d.n_chunks, d.W, 0, sums);
+    join_chunks(d.n_chunks, d.W, 0, sums, st);
     chunk_fwd_kernel<T, V><<<grid, kBlock, 0, st>>>(d, f, sums);
 }
 
@@ -533,7 +610,7 @@ void launch_bwd(const Shape &d, Bwd b, float *sums, hipStream_t st)
     float *copy = b.dh_last && b.dh_last == b.dh0 ? sums + (size_t)d.n_chunks * d.W * 2 : nullptr;
     chunk_sums_bwd_kernel<T, V><<<grid, kBlock, 0, st>>>(d, b, sums, copy);
     if (copy) b.dh_last = copy;
-    join_chunks_kernel<<<(d.W + kJoinChannels - 1) / kJoinChannels, kJoinChannels * kRuns, 0, st>>>(d.n_chunks, d.W, 1, sums);
+    join_chunks(d.n_chunks, d.W, 1, sums, st);
     chunk_bwd_kernel<T, V><<<grid, kBlock, 0, st>>>(d, b, sums);
 }
 
