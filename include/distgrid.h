@@ -553,7 +553,8 @@ int dg_layer_norm_bwd(const void *x, uint64_t ldx, const float *gamma, const voi
  * (+infinity) passes a token over, z <= -87 (-infinity, the lowest value of a type) forgets the past.  z NaN gives NaN.
  * states: NULL, or dg_recurrence_state_count(N, W) floats for the backward pass (the state at every 16th row).
  * ws: dg_recurrence_workspace_bytes(N, n_seq, W) bytes (NULL where that is 0), 16-byte aligned.
- * Errors: DG_ERR_ARG also for N that n_seq does not divide (first NULL); DG_ERR_UNSUPPORTED for N >= 2^32, W > 2^20. */
+ * Errors: DG_ERR_ARG also for N that n_seq does not divide (first NULL); DG_ERR_UNSUPPORTED for N >= 2^32, W > 2^20,
+ * more than 2^39 values. */
 size_t dg_recurrence_state_count(uint64_t N, uint32_t W);
 size_t dg_recurrence_workspace_bytes(uint64_t N, uint32_t n_seq, uint32_t W);
 int dg_recurrence_fwd(const void *z, uint64_t ldz, const void *u, uint64_t ldu, uint64_t N, uint32_t n_seq,

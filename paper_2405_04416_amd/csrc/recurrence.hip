@@ -5,6 +5,7 @@
 //
 // Tokens have a place in the order in which they are gone through: their row, or N - 1 - row back to front.  The forward pass
 // keeps the state before every kKeep-th place in fp32; the backward pass computes the states between them again.
+#include <type_traits>
 #include "rows_common.h"
 
 namespace {
@@ -25,17 +26,30 @@ __device__ __forceinline__ Gate gate(float z)
     return {a, e * a};
 }
 
-// Whether a wavefront has a shut gate among the tokens that it has loaded.  One operation per two values finds out; the tokens are then
-// gone through without looking at each gate.
+// Whether a wavefront has a shut gate among the tokens that it has loaded; they are then gone through looking at each gate.  By their
+// bits, which without the sign order numbers by magnitude with infinity and NaN on top: two operations for two 16-bit values, and no
+// fp32 copies of the gates that would stay in registers.
+template <class T>
+struct Bits;
+template <>
+struct Bits<float> { using type = uint32_t; static constexpr type kMagnitude = 0x7fffffffu, kShut = 0x42ae0000u; };
+template <>
+struct Bits<f16> { using type = uint16_t; static constexpr type kMagnitude = 0x7fffu, kShut = 0x5570u; };
+template <>
+struct Bits<bf16> { using type = uint16_t; static constexpr type kMagnitude = 0x7fffu, kShut = 0x42aeu; };
+
 template <class T, int V, int M>
 __device__ __forceinline__ bool any_shut(const Pack<T, V> (&z)[M])
 {
-    float most = 0.0f;
+    using B = typename Bits<T>::type;
+    typedef B Vector __attribute__((ext_vector_type(V)));
+    Vector most = 0;
 #pragma unroll
-    for (int k = 0; k < M; ++k)
+    for (int k = 0; k < M; ++k) most = __builtin_elementwise_max(most, __builtin_bit_cast(Vector, z[k]) & (Vector)Bits<T>::kMagnitude);
+    bool shut = false;
 #pragma unroll
-        for (int v = 0; v < V; ++v) most = fmaxf(most, fabsf((float)z[k].v[v]));
-    return __any(most >= kShut);
+    for (int v = 0; v < V; ++v) shut = shut || most[v] >= Bits<T>::kShut;
+    return __any(shut);
 }
 
 // The gate of a token, its input's share b = c u, and h_t.  kShutting: the gate may be shut.
@@ -68,7 +82,7 @@ struct Shape {
     uint32_t n_seq, W, S;           // S: tokens of each sequence, where first is NULL
     const uint32_t *first;
     bool reverse;
-    uint32_t n_chunks, per_chunk;   // places of a chunk, a multiple of kKeep; 0 chunks: sequence by sequence
+    uint32_t n_tiles;               // 0: sequence by sequence
 };
 
 // The sequences in the order of their places: sequence(d, k) is the number of the k-th.
@@ -94,8 +108,8 @@ __device__ __forceinline__ void places(const Shape &d, uint32_t k, uint64_t &beg
 __device__ __forceinline__ uint32_t begun_before(const Shape &d, uint64_t p)
 {
     if (!d.first) {
-        const uint64_t k = (p + d.S - 1) / d.S;
-        return k < d.n_seq ? (uint32_t)k : d.n_seq;
+        const uint32_t k = p ? ((uint32_t)p - 1) / d.S + 1 : 0;         // places lie below 2^32
+        return k < d.n_seq ? k : d.n_seq;
     }
     uint32_t lo = 0, hi = d.n_seq;
     while (lo < hi) {
@@ -108,7 +122,7 @@ __device__ __forceinline__ uint32_t begun_before(const Shape &d, uint64_t p)
     return lo;
 }
 
-// V neighbouring channels of the row of a place, and the way from there to the next place's
+// V neighbouring channels of the row of a place, walked from token to token: an address at a time, not one for each token in registers
 template <class T, int V>
 struct Column {
     T *at;
@@ -121,12 +135,27 @@ struct Column {
 };
 
 template <class T, int V, int M, bool kFull>
-__device__ __forceinline__ void load_tokens(const Column<T, V> &col, int n, Pack<T, V> (&out)[M])
+__device__ __forceinline__ void load_tokens(Column<T, V> col, int n, Pack<T, V> (&out)[M])
 {
 #pragma unroll
     for (int k = 0; k < M; ++k) {
-        const int i = kFull || k < n ? k : n - 1;           // past the last token: that one again
-        out[k] = *reinterpret_cast<const Pack<T, V> *>(col.at + i * col.step);
+        out[k] = *reinterpret_cast<const Pack<T, V> *>(col.at);
+        if (kFull || k + 1 < n) col.at += col.step;         // past the last token: that one again
+    }
+}
+
+// The compiler takes what it knows of these values for unknown from here on: what was computed from them is computed again instead of
+// kept in registers.
+template <class T, int V, int M>
+__device__ __forceinline__ void forget(Pack<T, V> (&a)[M])
+{
+    using Bits = typename std::conditional<sizeof(Pack<T, V>) == 2, uint16_t, uint32_t>::type;
+    static_assert(sizeof(Pack<T, V>) == sizeof(Bits), "one register");
+#pragma unroll
+    for (int k = 0; k < M; ++k) {
+        Bits b = __builtin_bit_cast(Bits, a[k]);
+        asm volatile("" : "+v"(b));
+        a[k] = __builtin_bit_cast(Pack<T, V>, b);
     }
 }
 
@@ -174,14 +203,15 @@ __device__ __forceinline__ void in_pieces(uint64_t p, uint64_t end, F f)
 }
 
 template <class T, int V, int M, bool kFull, bool kShutting>
-__device__ __forceinline__ void advance_loaded(const Pack<T, V> (&z)[M], const Pack<T, V> (&u)[M], const Column<T, V> &y, int n, float (&h)[V])
+__device__ __forceinline__ void advance_loaded(const Pack<T, V> (&z)[M], const Pack<T, V> (&u)[M], Column<T, V> y, int n, float (&h)[V])
 {
 #pragma unroll
     for (int k = 0; k < M; ++k)
         if (kFull || k < n) {
 #pragma unroll
             for (int v = 0; v < V; ++v) h[v] = advance<kShutting>(step_of<kShutting>((float)z[k].v[v], (float)u[k].v[v]), h[v]);
-            store<T, V>(y.at + k * y.step, h);
+            store<T, V>(y.at, h);
+            y.at += y.step;
         }
 }
 
@@ -208,36 +238,42 @@ __device__ __forceinline__ void advance_places(const Shape &d, const Fwd &f, uin
     });
 }
 
-// Forwards through the tokens for what G is multiplied with, a, c and q = a c (h_{t-1} - u), then backwards with G.
-template <class T, int V, int M, bool kFull, bool kShutting>
-__device__ __forceinline__ void retreat_loaded(const Pack<T, V> (&z)[M], const Pack<T, V> (&u)[M], const Pack<T, V> (&dy)[M], const Column<T, V> &dz,
-                                               const Column<T, V> &du, int n, float (&h)[V], float (&G)[V])
+// the states before the tokens, and h behind them
+template <class T, int V, int M, bool kShutting>
+__device__ __forceinline__ void states_before(const Pack<T, V> (&z)[M], const Pack<T, V> (&u)[M], float (&h)[V], float (&before)[M][V])
 {
-    float a[M][V], c[M][V], q[M][V];
 #pragma unroll
     for (int k = 0; k < M; ++k)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const float uu = (float)u[k].v[v];
-            const Step s = step_of<kShutting>((float)z[k].v[v], uu);
-            a[k][v] = s.a;
-            c[k][v] = s.c;
-            q[k][v] = kShutting && (s.a == 0.0f || s.c == 0.0f) ? 0.0f : s.a * s.c * (h[v] - uu);
-            h[v] = advance<kShutting>(s, h[v]);
+            before[k][v] = h[v];
+            h[v] = advance<kShutting>(step_of<kShutting>((float)z[k].v[v], (float)u[k].v[v]), h[v]);
         }
+}
+
+// The gradients of loaded tokens, last first.  The gates are computed again: keeping a, c and a c (h_{t-1} - u) from the way forwards costs
+// 96 registers where this takes 48, and half of the wavefronts.
+template <class T, int V, int M, bool kFull, bool kShutting>
+__device__ __forceinline__ void retreat_loaded(const Pack<T, V> (&z)[M], const Pack<T, V> (&u)[M], const Pack<T, V> (&dy)[M], const float (&before)[M][V],
+                                               Column<T, V> dz, Column<T, V> du, int n, float (&G)[V])
+{
 #pragma unroll
     for (int k = M - 1; k >= 0; --k)
         if (kFull || k < n) {
             float oz[V], ou[V];
 #pragma unroll
             for (int v = 0; v < V; ++v) {
+                const float uu = (float)u[k].v[v];
+                const Step s = step_of<kShutting>((float)z[k].v[v], uu);
                 G[v] += (float)dy[k].v[v];
-                oz[v] = kShutting && q[k][v] == 0.0f ? 0.0f : q[k][v] * G[v];
-                ou[v] = kShutting && c[k][v] == 0.0f ? 0.0f : c[k][v] * G[v];
-                G[v] = kShutting && a[k][v] == 0.0f ? 0.0f : a[k][v] * G[v];
+                ou[v] = kShutting && s.c == 0.0f ? 0.0f : s.c * G[v];
+                G[v] = kShutting && s.a == 0.0f ? 0.0f : s.a * G[v];
+                oz[v] = kShutting && (s.c == 0.0f || s.a == 0.0f) ? 0.0f : s.c * (before[k][v] - uu) * G[v];
             }
-            store<T, V>(dz.at + k * dz.step, oz);
-            store<T, V>(du.at + k * du.step, ou);
+            store<T, V>(dz.at, oz);
+            store<T, V>(du.at, ou);
+            dz.at -= dz.step;
+            du.at -= du.step;
         }
 }
 
@@ -248,9 +284,17 @@ __device__ __forceinline__ void retreat_tokens(const Shape &d, const Bwd &b, uin
     load_tokens<T, V, M, kFull>(Column<T, V>(d, b.z, b.ldz, c, p), n, z);
     load_tokens<T, V, M, kFull>(Column<T, V>(d, b.u, b.ldu, c, p), n, u);
     load_tokens<T, V, M, kFull>(Column<T, V>(d, b.dy, b.lddy, c, p), n, dy);
-    const Column<T, V> dz(d, b.dz, b.lddz, c, p), du(d, b.du, b.lddu, c, p);
-    if (any_shut<T, V, M>(z)) retreat_loaded<T, V, M, kFull, true>(z, u, dy, dz, du, n, h, G);
-    else retreat_loaded<T, V, M, kFull, false>(z, u, dy, dz, du, n, h, G);
+    const Column<T, V> dz(d, b.dz, b.lddz, c, p + n - 1), du(d, b.du, b.lddu, c, p + n - 1);      // the last token first
+    float before[M][V];
+    if (any_shut<T, V, M>(z)) {
+        states_before<T, V, M, true>(z, u, h, before);
+        forget<T, V, M>(z);
+        retreat_loaded<T, V, M, kFull, true>(z, u, dy, before, dz, du, n, G);
+    } else {
+        states_before<T, V, M, false>(z, u, h, before);
+        forget<T, V, M>(z);
+        retreat_loaded<T, V, M, kFull, false>(z, u, dy, before, dz, du, n, G);
+    }
 }
 
 // dz and du of places [p, end) of the sequence that begins at place `begin`, from the gradient G behind them
@@ -311,17 +355,25 @@ sequence_bwd_kernel(Shape d, Bwd b)
     put<V>(b.dh0, (uint64_t)seq * d.W + c, G);
 }
 
-// ------------------------------------------------------------------ long sequences: a lane per chunk of places and V channels
+// ------------------------------------------------------------------ long sequences
 //
-// A chunk takes the state before it to join(A, state, B).  One launch finds A and B of every chunk, one joins them along the
-// chunks into the state before each, one runs the chunks from there.  A sequence that begins inside a chunk makes its A 0.
+// A stretch of tokens takes the state before it to join(A, state, B).  A lane has a window of kKeep places and V channels, whose tokens
+// it keeps in registers: what they need from memory is read once.  A workgroup has a tile, as many windows one behind the other as
+// fit it, for channels that fill the 128 bytes of a line.  It finds A and B of its tile, tells the tiles behind it in a slot of its own,
+// joins what those before it have told until it comes to one whose A is 0 -- a tile that knows the state behind itself tells that as
+// (0, state), and a sequence that begins makes A 0 as well -- and lets its windows run from there, joined in LDS.
+//
+// Tiles are numbered as workgroups start.  A tile waits only for ones with a lower number, which run or have run, and tell A and B
+// before they wait for anything: every wait ends.  A slot is one 64-bit word written at once, so nothing else has to be ordered.
+//
+// A sequence that begins or ends in a window is gone through piece by piece.
 
-// f(k, p, e, begin, end) for the pieces [p, e) of the sequences [begin, end) that lie in a chunk, in order.  A sequence without a place
-// belongs to the chunk where it would begin.
+// f(k, p, e, begin, end) for the pieces [p, e) of the sequences [begin, end) that lie in the window from place p0 on, in order.  A
+// sequence without a place belongs to the window where it would begin.
 template <class F>
-__device__ __forceinline__ void forwards(const Shape &d, uint32_t chunk, F f)
+__device__ __forceinline__ void forwards(const Shape &d, uint64_t p0, F f)
 {
-    const uint64_t p0 = (uint64_t)chunk * d.per_chunk, p1 = p0 + d.per_chunk < d.N ? p0 + d.per_chunk : d.N;
+    const uint64_t p1 = p0 + kKeep < d.N ? p0 + kKeep : d.N;
     uint32_t k = begun_before(d, p0);
     uint64_t begin, end;
     if (k > 0) {
@@ -330,16 +382,16 @@ __device__ __forceinline__ void forwards(const Shape &d, uint32_t chunk, F f)
     }
     for (; k < d.n_seq; ++k) {
         places(d, k, begin, end);
-        if (begin >= p1 && chunk + 1 < d.n_chunks) break;
+        if (begin >= p1 && p1 < d.N) break;
         f(k, begin, end < p1 ? end : p1, begin, end);
     }
 }
 
 template <class F>
-__device__ __forceinline__ void backwards(const Shape &d, uint32_t chunk, F f)
+__device__ __forceinline__ void backwards(const Shape &d, uint64_t p0, F f)
 {
-    const uint64_t p0 = (uint64_t)chunk * d.per_chunk, p1 = p0 + d.per_chunk < d.N ? p0 + d.per_chunk : d.N;
-    uint32_t k = chunk + 1 < d.n_chunks ? begun_before(d, p1) : d.n_seq;
+    const uint64_t p1 = p0 + kKeep < d.N ? p0 + kKeep : d.N;
+    uint32_t k = p1 < d.N ? begun_before(d, p1) : d.n_seq;
     while (k-- > 0) {
         uint64_t begin, end;
         places(d, k, begin, end);
@@ -411,143 +463,374 @@ __device__ __forceinline__ void sum_gradients(const Shape &d, const Bwd &b, uint
     else sum_gradients_loaded<T, V, M, kFull, false>(z, dy, n, A, G);
 }
 
-// sums[0]: A, sums[1]: B, each [n_chunks, W].  copy: NULL, or room for h0 (backward: dh_last), which the last launch then reads there
-// because its own h_last (dh0) lies on it.
+constexpr int kTile = 512;          // lanes of a workgroup
+
+// lanes that have a token's channels side by side: a power of two, at most a line of 128 bytes
 template <class T, int V>
-__global__ void __launch_bounds__(kBlock)
-chunk_sums_fwd_kernel(Shape d, Fwd f, float *sums, float *copy)
+__host__ __device__ __forceinline__ constexpr uint32_t most_across() { return 128 / (sizeof(T) * V) < dg::kWave ? 128 / (sizeof(T) * V) : dg::kWave; }
+
+__host__ __device__ __forceinline__ uint32_t lanes_across(uint32_t W, uint32_t V, uint32_t most)
 {
-    uint32_t chunk, c;
-    if (!lane_place(d, V, d.n_chunks, chunk, c)) return;
+    uint32_t n = 1;
+    while (n < most && n * V < W) n *= 2;
+    return n;
+}
+
+__host__ __device__ __forceinline__ uint32_t groups_of(uint32_t W, uint32_t V, uint32_t across) { return (W + across * V - 1) / (across * V); }
+
+// Pieces of a window in which a sequence begins or ends, four tokens at a time: they run while other lanes of the wavefront hold their
+// windows, so that what they need in registers comes on top.
+constexpr int kFew = 4;
+
+template <class T, int V>
+__device__ __forceinline__ void advance_few(const Shape &d, const Fwd &f, uint32_t c, uint64_t p, uint64_t end, float (&h)[V])
+{
+    if (p < end && p % kKeep == 0) put<V>(f.states, p / kKeep * d.W + c, h);
+#pragma unroll 1
+    for (; p < end; p += kFew) advance_tokens<T, V, kFew, false>(d, f, c, p, end - p < kFew ? (int)(end - p) : kFew, h);
+}
+
+template <class T, int V>
+__device__ __forceinline__ void sum_few(const Shape &d, const Fwd &f, uint32_t c, uint64_t p, uint64_t end, float (&A)[V], float (&h)[V])
+{
+#pragma unroll 1
+    for (; p < end; p += kFew) sum_tokens<T, V, kFew, false>(d, f, c, p, end - p < kFew ? (int)(end - p) : kFew, A, h);
+}
+
+template <class T, int V>
+__device__ __forceinline__ void sum_few_gradients(const Shape &d, const Bwd &b, uint32_t c, uint64_t p, uint64_t end, float (&A)[V], float (&G)[V])
+{
+#pragma unroll 1
+    while (end > p) {
+        const int n = end - p < kFew ? (int)(end - p) : kFew;
+        end -= n;
+        sum_gradients<T, V, kFew, false>(d, b, c, end, n, A, G);
+    }
+}
+
+// every four tokens from the state that was kept, through the tokens in between
+template <class T, int V>
+__device__ __forceinline__ void retreat_few(const Shape &d, const Bwd &b, uint32_t seq, uint32_t c, uint64_t begin, uint64_t p, uint64_t end, float (&G)[V])
+{
+#pragma unroll 1
+    while (end > p) {
+        const int n = end - p < kFew ? (int)(end - p) : kFew;
+        end -= n;
+        float h[V], A[V];
+        if (p == begin) get<V>(b.h0, (uint64_t)seq * d.W + c, h);
+        else get<V>(b.states, p / kKeep * d.W + c, h);
+        Fwd f;
+        f.z = b.z, f.u = b.u, f.ldz = b.ldz, f.ldu = b.ldu;
+#pragma unroll
+        for (int v = 0; v < V; ++v) A[v] = 1.0f;
+        sum_few<T, V>(d, f, c, p, end, A, h);
+        retreat_tokens<T, V, kFew, false>(d, b, c, end, n, h, G);
+    }
+}
+
+struct Lane {
+    uint32_t across, lane, window, windows, c, tile;        // windows of a tile; c: first channel
+    bool active;
+    __device__ __forceinline__ Lane(const Shape &d, uint32_t V, uint32_t most, uint32_t number)
+    {
+        across = lanes_across(d.W, V, most);
+        lane = threadIdx.x & (across - 1);
+        window = threadIdx.x / across;
+        windows = kTile / across;
+        const uint32_t groups = groups_of(d.W, V, across);
+        tile = number / groups;
+        c = (number % groups * across + lane) * V;
+        active = c < d.W;
+    }
+};
+
+// What the tiles share: the number of workgroups that have started, and a slot for each tile and channel: A in the lower half, B in the upper.
+struct Board {
+    uint32_t *started;
+    uint64_t *slots;                // [n_tiles, W]
+};
+
+constexpr uint64_t kEmpty = ~0ull;  // A would be a NaN that no computation gives
+constexpr uint32_t kMostPolls = 1u << 20;      // a second or so; the state is then a NaN
+
+__device__ __forceinline__ uint32_t start(const Board &b)
+{
+    __shared__ uint32_t number;
+    if (threadIdx.x == 0) number = __hip_atomic_fetch_add(b.started, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    return number;
+}
+
+__device__ __forceinline__ uint32_t told_bits(float x) { return x != x ? 0x7fc00000u : __float_as_uint(x); }
+
+template <int V>
+__device__ __forceinline__ void tell(uint64_t *slot, const float (&A)[V], const float (&B)[V])
+{
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        __hip_atomic_store(slot + v, (uint64_t)told_bits(B[v]) << 32 | told_bits(A[v]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// waits for a slot to be written
+template <int V>
+__device__ __forceinline__ void hear(const uint64_t *slot, float (&A)[V], float (&B)[V])
+{
+    uint64_t word[V];
+    for (uint32_t polls = 0; polls < kMostPolls; ++polls) {
+        bool told = true;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            word[v] = __hip_atomic_load(slot + v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            told = told && word[v] != kEmpty;
+        }
+        if (told) break;
+        __builtin_amdgcn_s_sleep(1);
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) A[v] = __uint_as_float((uint32_t)word[v]), B[v] = __uint_as_float((uint32_t)(word[v] >> 32));
+}
+
+// whether the window from place p0 on lies inside a sequence, with more of it on both sides
+__device__ __forceinline__ bool surrounded(const Shape &d, uint64_t p0)
+{
+    if (p0 + kKeep >= d.N) return false;
+    const uint32_t k = begun_before(d, p0);
+    if (k == 0) return false;
+    uint64_t begin, end;
+    places(d, k - 1, begin, end);
+    return begin < p0 && end > p0 + kKeep;
+}
+
+template <int V>
+using Pairs = float[2][kTile * V];
+
+template <int V>
+__device__ __forceinline__ void lay_down(Pairs<V> &all, const Lane &l, uint32_t at, const float (&A)[V], const float (&B)[V])
+{
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        all[0][(at * l.across + l.lane) * V + v] = A[v];
+        all[1][(at * l.across + l.lane) * V + v] = B[v];
+    }
+}
+
+template <int V>
+__device__ __forceinline__ void pick_up(const Pairs<V> &all, const Lane &l, uint32_t at, float (&A)[V], float (&B)[V])
+{
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        A[v] = all[0][(at * l.across + l.lane) * V + v];
+        B[v] = all[1][(at * l.across + l.lane) * V + v];
+    }
+}
+
+// (A, B) of a stretch, then (a, b) of the one behind it: of both
+template <int V>
+__device__ __forceinline__ void append(float (&A)[V], float (&B)[V], const float (&a)[V], const float (&b)[V])
+{
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        B[v] = join(a[v], B[v], b[v]);
+        A[v] = times(A[v], a[v]);
+    }
+}
+
+// From A and B of a lane's window the state before it (backward: the gradient behind it).  All lanes of the workgroup call it.
+// mine: the place of the lane's window among those of the tile in the order in which states pass them; tile: likewise.
+template <int V>
+__device__ __forceinline__ void come_in(const Shape &d, const Board &board, const Lane &l, uint32_t mine, uint32_t tile, const float (&A)[V],
+                                        const float (&B)[V], float (&h)[V])
+{
+    __shared__ Pairs<V> own, heard;
+    __shared__ float in[dg::kWave * V];
+    __shared__ uint32_t done;
+    lay_down<V>(own, l, mine, A, B);
+    if (threadIdx.x == 0) done = 0;
+    __syncthreads();
+    float tA[V], tB[V];
+    if (mine == 0) {
+        pick_up<V>(own, l, 0, tA, tB);
+        for (uint32_t w = 1; w < l.windows; ++w) {
+            float a[V], b[V];
+            pick_up<V>(own, l, w, a, b);
+            append<V>(tA, tB, a, b);
+        }
+        if (tile == 0)
+#pragma unroll
+            for (int v = 0; v < V; ++v) tA[v] = 0.0f;           // nothing comes before it
+        if (l.active) tell<V>(board.slots + (uint64_t)tile * d.W + l.c, tA, tB);
+    }
+    // each window's lanes listen to one tile, the nearest first, until all channels have met an A of 0
+    float sA[V], sB[V];                                         // of the tiles heard so far
+#pragma unroll
+    for (int v = 0; v < V; ++v) sA[v] = 1.0f, sB[v] = 0.0f;
+    for (uint32_t back = 1; tile >= back; back += l.windows) {
+        if (l.active && back + mine <= tile) {
+            float a[V], b[V];
+            hear<V>(board.slots + (uint64_t)(tile - back - mine) * d.W + l.c, a, b);
+            lay_down<V>(heard, l, mine, a, b);
+        }
+        __syncthreads();
+        if (mine == 0) {
+            bool open = false;
+            if (l.active) {
+                const uint32_t n = tile - back + 1 < l.windows ? tile - back + 1 : l.windows;
+                for (uint32_t w = 0; w < n; ++w) {
+                    float a[V], b[V];
+                    pick_up<V>(heard, l, w, a, b);
+                    append<V>(a, b, sA, sB);
+#pragma unroll
+                    for (int v = 0; v < V; ++v) sA[v] = a[v], sB[v] = b[v];
+                }
+#pragma unroll
+                for (int v = 0; v < V; ++v) open = open || sA[v] != 0.0f;
+            }
+            if (!__any(open) && l.lane == 0) done = 1;
+        }
+        __syncthreads();
+        if (done) break;
+    }
+    if (mine == 0) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) in[l.lane * V + v] = sB[v];
+        bool open = false;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            open = open || tA[v] != 0.0f;
+            tB[v] = join(tA[v], sB[v], tB[v]);
+            tA[v] = 0.0f;
+        }
+        if (l.active && open) tell<V>(board.slots + (uint64_t)tile * d.W + l.c, tA, tB);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < V; ++v) h[v] = in[l.lane * V + v];
+    for (uint32_t w = 0; w < mine; ++w) {
+        float a[V], b[V];
+        pick_up<V>(own, l, w, a, b);
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[v] = join(a[v], h[v], b[v]);
+    }
+}
+
+template <class T, int V>
+__global__ void __launch_bounds__(kTile)
+tile_fwd_kernel(Shape d, Fwd f, Board board)
+{
+    const Lane l(d, V, most_across<T, V>(), start(board));
+    const uint64_t p0 = ((uint64_t)l.tile * l.windows + l.window) * kKeep;
+    const bool held = l.active && p0 < d.N, inner = held && surrounded(d, p0);
+    Pack<T, V> z[kKeep], u[kKeep];
     float A[V], h[V];
+    bool shutting = false;
 #pragma unroll
     for (int v = 0; v < V; ++v) A[v] = 1.0f, h[v] = 0.0f;
-    forwards(d, chunk, [&](uint32_t k, uint64_t p, uint64_t e, uint64_t begin, uint64_t) {
-        if (p == begin) {
+    if (inner) {
+        load_tokens<T, V, kKeep, true>(Column<T, V>(d, f.z, f.ldz, l.c, p0), kKeep, z);
+        load_tokens<T, V, kKeep, true>(Column<T, V>(d, f.u, f.ldu, l.c, p0), kKeep, u);
+        shutting = any_shut<T, V, kKeep>(z);
+        if (shutting) sum_loaded<T, V, kKeep, true, true>(z, u, kKeep, A, h);
+        else sum_loaded<T, V, kKeep, true, false>(z, u, kKeep, A, h);
+    } else if (held)
+        forwards(d, p0, [&](uint32_t k, uint64_t p, uint64_t e, uint64_t begin, uint64_t) {
+            if (p == begin) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) A[v] = 0.0f;
-            get<V>(f.h0, (uint64_t)sequence(d, k) * d.W + c, h);
-            put<V>(copy, (uint64_t)sequence(d, k) * d.W + c, h);
-        }
-        in_pieces(p, e, [&](uint64_t q, int n) {
-            if (n == kKeep) sum_tokens<T, V, kKeep, true>(d, f, c, q, n, A, h);
-            else sum_tokens<T, V, kKeep, false>(d, f, c, q, n, A, h);
+                for (int v = 0; v < V; ++v) A[v] = 0.0f;
+                get<V>(f.h0, (uint64_t)sequence(d, k) * d.W + l.c, h);
+            }
+            sum_few<T, V>(d, f, l.c, p, e, A, h);
         });
-    });
-    put<V>(sums, (uint64_t)chunk * d.W + c, A);
-    put<V>(sums, ((uint64_t)d.n_chunks + chunk) * d.W + c, h);
+    float state[V];
+    come_in<V>(d, board, l, l.window, l.tile, A, h, state);
+    if (inner) {
+        put<V>(f.states, p0 / kKeep * d.W + l.c, state);
+        const Column<T, V> y(d, f.y, f.ldy, l.c, p0);
+        forget<T, V, kKeep>(z);
+        if (shutting) advance_loaded<T, V, kKeep, true, true>(z, u, y, kKeep, state);
+        else advance_loaded<T, V, kKeep, true, false>(z, u, y, kKeep, state);
+    } else if (held)
+        forwards(d, p0, [&](uint32_t k, uint64_t p, uint64_t e, uint64_t begin, uint64_t end) {
+            const uint64_t at = (uint64_t)sequence(d, k) * d.W + l.c;
+            if (p == begin) get<V>(f.h0, at, state);
+            advance_few<T, V>(d, f, l.c, p, e, state);
+            if (e == end) put<V>(f.h_last, at, state);
+        });
 }
 
+// from the last tile to the first
 template <class T, int V>
-__global__ void __launch_bounds__(kBlock)
-chunk_sums_bwd_kernel(Shape d, Bwd b, float *sums, float *copy)
+__global__ void __launch_bounds__(kTile)
+tile_bwd_kernel(Shape d, Bwd b, Board board)
 {
-    uint32_t chunk, c;
-    if (!lane_place(d, V, d.n_chunks, chunk, c)) return;
+    Lane l(d, V, most_across<T, V>(), start(board));
+    const uint32_t tile = l.tile;
+    l.tile = d.n_tiles - 1 - tile;
+    const uint64_t p0 = ((uint64_t)l.tile * l.windows + l.window) * kKeep;
+    const bool held = l.active && p0 < d.N, inner = held && surrounded(d, p0);
+    Pack<T, V> z[kKeep], u[kKeep], dy[kKeep];
     float A[V], G[V];
+    bool shutting = false;
 #pragma unroll
     for (int v = 0; v < V; ++v) A[v] = 1.0f, G[v] = 0.0f;
-    backwards(d, chunk, [&](uint32_t k, uint64_t p, uint64_t e, uint64_t, uint64_t end) {
-        if (e == end) {
+    if (inner) {
+        load_tokens<T, V, kKeep, true>(Column<T, V>(d, b.z, b.ldz, l.c, p0), kKeep, z);
+        load_tokens<T, V, kKeep, true>(Column<T, V>(d, b.dy, b.lddy, l.c, p0), kKeep, dy);
+        load_tokens<T, V, kKeep, true>(Column<T, V>(d, b.u, b.ldu, l.c, p0), kKeep, u);
+        shutting = any_shut<T, V, kKeep>(z);
+        if (shutting) sum_gradients_loaded<T, V, kKeep, true, true>(z, dy, kKeep, A, G);
+        else sum_gradients_loaded<T, V, kKeep, true, false>(z, dy, kKeep, A, G);
+    } else if (held)
+        backwards(d, p0, [&](uint32_t k, uint64_t p, uint64_t e, uint64_t, uint64_t end) {
+            if (e == end) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) A[v] = 0.0f;
-            get<V>(b.dh_last, (uint64_t)sequence(d, k) * d.W + c, G);
-            put<V>(copy, (uint64_t)sequence(d, k) * d.W + c, G);
+                for (int v = 0; v < V; ++v) A[v] = 0.0f;
+                get<V>(b.dh_last, (uint64_t)sequence(d, k) * d.W + l.c, G);
+            }
+            sum_few_gradients<T, V>(d, b, l.c, p, e, A, G);
+        });
+    float behind[V];
+    come_in<V>(d, board, l, l.windows - 1 - l.window, tile, A, G, behind);
+    if (inner) {
+        const Column<T, V> dz(d, b.dz, b.lddz, l.c, p0 + kKeep - 1), du(d, b.du, b.lddu, l.c, p0 + kKeep - 1);
+        float state[V], before[kKeep][V];
+        get<V>(b.states, p0 / kKeep * d.W + l.c, state);
+        forget<T, V, kKeep>(z);
+        if (shutting) {
+            states_before<T, V, kKeep, true>(z, u, state, before);
+            forget<T, V, kKeep>(z);
+            retreat_loaded<T, V, kKeep, true, true>(z, u, dy, before, dz, du, kKeep, behind);
+        } else {
+            states_before<T, V, kKeep, false>(z, u, state, before);
+            forget<T, V, kKeep>(z);
+            retreat_loaded<T, V, kKeep, true, false>(z, u, dy, before, dz, du, kKeep, behind);
         }
-        while (e > p) {
-            const uint64_t keep = (e - 1) / kKeep * kKeep, q = keep > p ? keep : p;
-            const int n = (int)(e - q);
-            if (n == kKeep) sum_gradients<T, V, kKeep, true>(d, b, c, q, n, A, G);
-            else sum_gradients<T, V, kKeep, false>(d, b, c, q, n, A, G);
-            e = q;
-        }
-    });
-    put<V>(sums, (uint64_t)chunk * d.W + c, A);
-    put<V>(sums, ((uint64_t)d.n_chunks + chunk) * d.W + c, G);
+    } else if (held)
+        backwards(d, p0, [&](uint32_t k, uint64_t p, uint64_t e, uint64_t begin, uint64_t end) {
+            const uint32_t seq = sequence(d, k);
+            const uint64_t at = (uint64_t)seq * d.W + l.c;
+            if (e == end) get<V>(b.dh_last, at, behind);
+            retreat_few<T, V>(d, b, seq, l.c, begin, p, e, behind);
+            if (p == begin) put<V>(b.dh0, at, behind);
+        });
 }
 
-// What comes before each chunk (backward: behind it), written over its A.  A workgroup has 16 channels and cuts the chunks into
-// 64 runs of at most P, which its threads hold in registers: each joins its run, then the runs before its own, then the chunks of its run.
-constexpr int kJoinChannels = 16, kRuns = 64;
-
-template <int P>
-__global__ void __launch_bounds__(kJoinChannels *kRuns)
-join_chunks_kernel(uint32_t n_chunks, uint32_t W, uint32_t from_the_end, float *sums)
-{
-    __shared__ float run_A[kRuns][kJoinChannels], run_B[kRuns][kJoinChannels];
-    const uint32_t lane = threadIdx.x % kJoinChannels, run = threadIdx.x / kJoinChannels, c = blockIdx.x * kJoinChannels + lane;
-    const uint32_t per = (n_chunks + kRuns - 1) / kRuns, k0 = run * per;
-    const uint64_t to_B = (uint64_t)n_chunks * W;
-    auto held = [&](int i) { return (uint32_t)i < per && k0 + i < n_chunks && c < W; };
-    auto at = [&](int i) { return (uint64_t)(from_the_end ? n_chunks - 1 - (k0 + i) : k0 + i) * W + c; };
-    float a[P], b[P], A = 1.0f, B = 0.0f;
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-        a[i] = held(i) ? sums[at(i)] : 1.0f;
-        b[i] = held(i) ? sums[to_B + at(i)] : 0.0f;
-    }
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-        B = join(a[i], B, b[i]);
-        A = times(A, a[i]);
-    }
-    run_A[run][lane] = A;
-    run_B[run][lane] = B;
-    __syncthreads();
-    float h = 0.0f;
-    for (uint32_t r = 0; r < run; ++r) h = join(run_A[r][lane], h, run_B[r][lane]);
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-        if (held(i)) sums[at(i)] = h;
-        h = join(a[i], h, b[i]);
-    }
-}
-
-void join_chunks(uint32_t n_chunks, uint32_t W, uint32_t from_the_end, float *sums, hipStream_t st)
-{
-    const uint32_t grid = (W + kJoinChannels - 1) / kJoinChannels;
-    auto go = [&](auto kernel) { kernel<<<grid, kJoinChannels * kRuns, 0, st>>>(n_chunks, W, from_the_end, sums); };
-    n_chunks <= 8 * kRuns ? go(join_chunks_kernel<8>) : go(join_chunks_kernel<32>);
-}
-
-template <class T, int V>
+// Empties the board.  from, copy: NULL, or states that the tiles then read in the copy because what they write lies on them.
 __global__ void __launch_bounds__(kBlock)
-chunk_fwd_kernel(Shape d, Fwd f, const float *sums)
+board_kernel(Board board, uint64_t n_slots, const float *from, float *copy, uint64_t n_states)
 {
-    uint32_t chunk, c;
-    if (!lane_place(d, V, d.n_chunks, chunk, c)) return;
-    float h[V];
-    get<V>(sums, (uint64_t)chunk * d.W + c, h);
-    forwards(d, chunk, [&](uint32_t k, uint64_t p, uint64_t e, uint64_t begin, uint64_t end) {
-        const uint64_t at = (uint64_t)sequence(d, k) * d.W + c;
-        if (p == begin) get<V>(f.h0, at, h);
-        advance_places<T, V>(d, f, c, p, e, h);
-        if (e == end) put<V>(f.h_last, at, h);
-    });
-}
-
-template <class T, int V>
-__global__ void __launch_bounds__(kBlock)
-chunk_bwd_kernel(Shape d, Bwd b, const float *sums)
-{
-    uint32_t chunk, c;
-    if (!lane_place(d, V, d.n_chunks, chunk, c)) return;
-    float G[V];
-    get<V>(sums, (uint64_t)chunk * d.W + c, G);
-    backwards(d, chunk, [&](uint32_t k, uint64_t p, uint64_t e, uint64_t begin, uint64_t end) {
-        const uint32_t seq = sequence(d, k);
-        const uint64_t at = (uint64_t)seq * d.W + c;
-        if (e == end) get<V>(b.dh_last, at, G);
-        retreat_places<T, V>(d, b, seq, c, begin, p, e, G);
-        if (p == begin) put<V>(b.dh0, at, G);
-    });
+    const uint64_t i0 = (uint64_t)blockIdx.x * kBlock + threadIdx.x, step = (uint64_t)gridDim.x * kBlock;
+    if (i0 == 0) *board.started = 0;
+    for (uint64_t i = i0; i < n_slots; i += step) board.slots[i] = kEmpty;
+    if (copy)
+        for (uint64_t i = i0; i < n_states; i += step) copy[i] = from[i];
 }
 
 int check(const char *who, Shape &d, uint32_t dtype)
 {
     DG_REQUIRE(known_type(dtype), DG_ERR_ARG, "%s: unknown element type %u", who, dtype);
     DG_REQUIRE(d.W >= 1, DG_ERR_ARG, "%s: rows without a channel", who);
-    DG_REQUIRE(d.N < 1ull << 32 && d.W <= 1u << 20, DG_ERR_UNSUPPORTED, "%s: 2^32 tokens or more, or more than 2^20 channels", who);
+    DG_REQUIRE(d.N < 1ull << 32 && d.W <= 1u << 20 && d.N * d.W <= 1ull << 39, DG_ERR_UNSUPPORTED,
+               "%s: 2^32 tokens or more, more than 2^20 channels or than 2^39 values", who);
     DG_REQUIRE(dg::aligned(d.first, 4), DG_ERR_ARG, "%s: misaligned pointer", who);
     DG_REQUIRE(d.n_seq > 0 || d.N == 0, DG_ERR_ARG, "%s: tokens without a sequence", who);
     DG_REQUIRE(d.first || d.n_seq == 0 || d.N % d.n_seq == 0, DG_ERR_ARG, "%s: %llu tokens are not %u sequences of one length", who, (unsigned long long)d.N,
@@ -565,64 +848,76 @@ int check_rows(const char *who, const void *p, uint64_t ld, const Shape &d, uint
     return DG_OK;
 }
 
-// Few sequences: chunks of places instead, enough of them for kWanted lanes of two channels, each of kKeep places at least.
-constexpr uint64_t kWanted = 1 << 18;
-constexpr uint32_t kMostChunks = 32 * kRuns;
+// Few sequences: tiles instead.  V, most: of the call.
+constexpr uint64_t kWanted = 1 << 16;
 
-void cut(Shape &d)
+void cut(Shape &d, uint32_t V, uint32_t most)
 {
-    d.n_chunks = d.per_chunk = 0;
-    const uint64_t pairs = (d.W + 1) / 2;
-    if (d.n_seq == 0 || d.N / d.n_seq < 4 * kKeep || d.n_seq * pairs >= kWanted / 4) return;
-    uint64_t n = kWanted / pairs;
-    n = n < kMostChunks ? n : kMostChunks;
-    uint64_t per = (d.N + n - 1) / n;
-    per = (per + kKeep - 1) / kKeep * kKeep;
-    d.per_chunk = (uint32_t)per;
-    d.n_chunks = (uint32_t)((d.N + per - 1) / per);
+    d.n_tiles = 0;
+    if (d.n_seq == 0 || d.N / d.n_seq < 4 * kKeep || d.n_seq * ((uint64_t)(d.W + 1) / 2) >= kWanted) return;
+    const uint32_t tile = kTile / lanes_across(d.W, V, most) * kKeep;
+    d.n_tiles = (uint32_t)((d.N + tile - 1) / tile);
 }
 
 uint32_t blocks(uint64_t count, uint32_t W, uint32_t V) { return (uint32_t)((count * (W / V) + kBlock - 1) / kBlock); }
 
-template <class T, int V>
-void launch_fwd(const Shape &d, Fwd f, float *sums, hipStream_t st)
-{
-    if (!d.n_chunks) {
-        sequence_fwd_kernel<T, V><<<blocks(d.n_seq, d.W, V), kBlock, 0, st>>>(d, f);
-        return;
-    }
-    const uint32_t grid = blocks(d.n_chunks, d.W, V);
-    float *copy = f.h0 && f.h0 == f.h_last ? sums + (size_t)d.n_chunks * d.W * 2 : nullptr;
-    chunk_sums_fwd_kernel<T, V><<<grid, kBlock, 0, st>>>(d, f, sums, copy);
-    if (copy) f.h0 = copy;
-    join_chunks(d.n_chunks, d.W, 0, sums, st);
-    chunk_fwd_kernel<T, V><<<grid, kBlock, 0, st>>>(d, f, sums);
-}
+// the board's counter and slots, and room for a copy of the states
+constexpr size_t kSlotsAt = 16;
 
-template <class T, int V>
-void launch_bwd(const Shape &d, Bwd b, float *sums, hipStream_t st)
-{
-    if (!d.n_chunks) {
-        sequence_bwd_kernel<T, V><<<blocks(d.n_seq, d.W, V), kBlock, 0, st>>>(d, b);
-        return;
-    }
-    const uint32_t grid = blocks(d.n_chunks, d.W, V);
-    float *copy = b.dh_last && b.dh_last == b.dh0 ? sums + (size_t)d.n_chunks * d.W * 2 : nullptr;
-    chunk_sums_bwd_kernel<T, V><<<grid, kBlock, 0, st>>>(d, b, sums, copy);
-    if (copy) b.dh_last = copy;
-    join_chunks(d.n_chunks, d.W, 1, sums, st);
-    chunk_bwd_kernel<T, V><<<grid, kBlock, 0, st>>>(d, b, sums);
-}
+size_t workspace_bytes(const Shape &d) { return d.n_tiles ? kSlotsAt + (size_t)d.n_tiles * d.W * sizeof(uint64_t) + (size_t)d.n_seq * d.W * sizeof(float) : 0; }
 
-// sums of the chunks, and room for a copy of the states
-size_t workspace_bytes(const Shape &d) { return d.n_chunks ? ((size_t)d.n_chunks * 2 + d.n_seq) * d.W * sizeof(float) : 0; }
+// whatever the type and the alignment of the call: the smallest tile makes the most of them
+size_t most_workspace_bytes(Shape d)
+{
+    cut(d, 1, dg::kWave);
+    return workspace_bytes(d);
+}
 
 int check_workspace(const char *who, const Shape &d, const void *ws, size_t ws_bytes)
 {
-    const size_t need = workspace_bytes(d);
+    const size_t need = most_workspace_bytes(d);
     DG_REQUIRE(need == 0 || (ws && dg::aligned(ws, 16) && ws_bytes >= need), DG_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", who, need,
                ws ? ws_bytes : 0);
     return DG_OK;
+}
+
+// *in: states (gradients) that the tiles read, out: where they write theirs
+Board board_of(const Shape &d, void *ws, const float **in, const float *out, hipStream_t st)
+{
+    const uint64_t n_slots = (uint64_t)d.n_tiles * d.W;
+    const Board board = {(uint32_t *)ws, (uint64_t *)((char *)ws + kSlotsAt)};
+    float *copy = *in && *in == out ? (float *)(board.slots + n_slots) : nullptr;
+    const uint64_t n = (n_slots + 4 * kBlock - 1) / (4 * kBlock);
+    board_kernel<<<(uint32_t)(n < 2048 ? n : 2048), kBlock, 0, st>>>(board, n_slots, *in, copy, (uint64_t)d.n_seq * d.W);
+    if (copy) *in = copy;
+    return board;
+}
+
+template <class T, int V>
+uint32_t tile_blocks(const Shape &d) { return d.n_tiles * groups_of(d.W, V, lanes_across(d.W, V, most_across<T, V>())); }
+
+template <class T, int V>
+void launch_fwd(Shape d, Fwd f, void *ws, hipStream_t st)
+{
+    cut(d, V, most_across<T, V>());
+    if (!d.n_tiles) {
+        sequence_fwd_kernel<T, V><<<blocks(d.n_seq, d.W, V), kBlock, 0, st>>>(d, f);
+        return;
+    }
+    const Board board = board_of(d, ws, &f.h0, f.h_last, st);
+    tile_fwd_kernel<T, V><<<tile_blocks<T, V>(d), kTile, 0, st>>>(d, f, board);
+}
+
+template <class T, int V>
+void launch_bwd(Shape d, Bwd b, void *ws, hipStream_t st)
+{
+    cut(d, V, most_across<T, V>());
+    if (!d.n_tiles) {
+        sequence_bwd_kernel<T, V><<<blocks(d.n_seq, d.W, V), kBlock, 0, st>>>(d, b);
+        return;
+    }
+    const Board board = board_of(d, ws, &b.dh_last, b.dh0, st);
+    tile_bwd_kernel<T, V><<<tile_blocks<T, V>(d), kTile, 0, st>>>(d, b, board);
 }
 
 }  // namespace
@@ -631,9 +926,8 @@ extern "C" size_t dg_recurrence_state_count(uint64_t N, uint32_t W) { return (si
 
 extern "C" size_t dg_recurrence_workspace_bytes(uint64_t N, uint32_t n_seq, uint32_t W)
 {
-    Shape d = {N, n_seq, W, 0, nullptr, false, 0, 0};
-    cut(d);
-    return workspace_bytes(d);
+    Shape d = {N, n_seq, W, 0, nullptr, false, 0};
+    return most_workspace_bytes(d);
 }
 
 extern "C" int dg_recurrence_fwd(const void *z, uint64_t ldz, const void *u, uint64_t ldu, uint64_t N, uint32_t n_seq, const uint32_t *first, uint32_t W,
@@ -641,20 +935,19 @@ extern "C" int dg_recurrence_fwd(const void *z, uint64_t ldz, const void *u, uin
                                  size_t ws_bytes, void *stream)
 {
     const char *who = "dg_recurrence_fwd";
-    Shape d = {N, n_seq, W, 0, first, reverse != 0, 0, 0};
+    Shape d = {N, n_seq, W, 0, first, reverse != 0, 0};
     if (int rc = check(who, d, dtype)) return rc;
     if (int rc = check_rows(who, z, ldz, d, dtype)) return rc;
     if (int rc = check_rows(who, u, ldu, d, dtype)) return rc;
     if (int rc = check_rows(who, y, ldy, d, dtype)) return rc;
     DG_REQUIRE(dg::aligned(h0, 4) && dg::aligned(h_last, 4) && dg::aligned(states, 4), DG_ERR_ARG, "%s: misaligned pointer", who);
     if (n_seq == 0) return DG_OK;
-    cut(d);
     if (int rc = check_workspace(who, d, ws, ws_bytes)) return rc;
     const Fwd f = {z, u, y, ldz, ldu, ldy, h0, h_last, states};
-    const bool pairs = W % 2 == 0 && rows_aligned(z, ldz, dtype, 4) && rows_aligned(u, ldu, dtype, 4) && rows_aligned(y, ldy, dtype, 4);
+    const bool pairs = dtype != DG_F32 && W % 2 == 0 && rows_aligned(z, ldz, dtype, 4) && rows_aligned(u, ldu, dtype, 4) && rows_aligned(y, ldy, dtype, 4);
     (dtype == DG_F32   ? launch_fwd<float, 1>
      : dtype == DG_F16 ? (pairs ? launch_fwd<f16, 2> : launch_fwd<f16, 1>)
-                       : (pairs ? launch_fwd<bf16, 2> : launch_fwd<bf16, 1>))(d, f, (float *)ws, (hipStream_t)stream);
+                       : (pairs ? launch_fwd<bf16, 2> : launch_fwd<bf16, 1>))(d, f, ws, (hipStream_t)stream);
     return dg::launch_status(who);
 }
 
@@ -663,7 +956,7 @@ extern "C" int dg_recurrence_bwd(const void *z, uint64_t ldz, const void *u, uin
                                  const float *dh_last, void *dz, uint64_t lddz, void *du, uint64_t lddu, float *dh0, void *ws, size_t ws_bytes, void *stream)
 {
     const char *who = "dg_recurrence_bwd";
-    Shape d = {N, n_seq, W, 0, first, reverse != 0, 0, 0};
+    Shape d = {N, n_seq, W, 0, first, reverse != 0, 0};
     if (int rc = check(who, d, dtype)) return rc;
     const struct { const void *p; uint64_t ld; } rows[] = {{z, ldz}, {u, ldu}, {dy, lddy}, {dz, lddz}, {du, lddu}};
     for (const auto &r : rows)
@@ -671,13 +964,12 @@ extern "C" int dg_recurrence_bwd(const void *z, uint64_t ldz, const void *u, uin
     DG_REQUIRE(N == 0 || states, DG_ERR_ARG, "%s: the states that the forward pass kept are missing", who);
     DG_REQUIRE(dg::aligned(h0, 4) && dg::aligned(states, 4) && dg::aligned(dh_last, 4) && dg::aligned(dh0, 4), DG_ERR_ARG, "%s: misaligned pointer", who);
     if (n_seq == 0) return DG_OK;
-    cut(d);
     if (int rc = check_workspace(who, d, ws, ws_bytes)) return rc;
     const Bwd b = {z, u, dy, dz, du, ldz, ldu, lddy, lddz, lddu, h0, states, dh_last, dh0};
-    bool pairs = W % 2 == 0;
+    bool pairs = dtype != DG_F32 && W % 2 == 0;
     for (const auto &r : rows) pairs = pairs && rows_aligned(r.p, r.ld, dtype, 4);
     (dtype == DG_F32   ? launch_bwd<float, 1>
      : dtype == DG_F16 ? (pairs ? launch_bwd<f16, 2> : launch_bwd<f16, 1>)
-                       : (pairs ? launch_bwd<bf16, 2> : launch_bwd<bf16, 1>))(d, b, (float *)ws, (hipStream_t)stream);
+                       : (pairs ? launch_bwd<bf16, 2> : launch_bwd<bf16, 1>))(d, b, ws, (hipStream_t)stream);
     return dg::launch_status(who);
 }
