@@ -360,11 +360,11 @@ sequence_bwd_kernel(Shape d, Bwd b)
 // A stretch of tokens takes the state before it to join(A, state, B).  A lane has a window of kKeep places and V channels, whose tokens
 // it keeps in registers: what they need from memory is read once.  A workgroup has a tile, as many windows one behind the other as
 // fit it, for channels that fill the 128 bytes of a line.  It finds A and B of its tile, tells the tiles behind it in a slot of its own,
-// joins what those before it have told until it comes to one whose A is 0 -- a tile that knows the state behind itself tells that as
-// (0, state), and a sequence that begins makes A 0 as well -- and lets its windows run from there, joined in LDS.
+// joins what those before it have told, and lets its windows run from there, joined in LDS.  A stretch that knows the state behind itself
+// tells it as (0, state); where a sequence begins A is 0 anyway.
 //
-// Tiles are numbered as workgroups start.  A tile waits only for ones with a lower number, which run or have run, and tell A and B
-// before they wait for anything: every wait ends.  A slot is one 64-bit word written at once, so nothing else has to be ordered.
+// Tiles are numbered as workgroups start.  A tile waits only for ones with a lower number, which run or have run, and tell what they do
+// before they wait for a state: every wait ends.  A slot is one 64-bit word written at once, so nothing else has to be ordered.
 //
 // A sequence that begins or ends in a window is gone through piece by piece.
 
@@ -464,6 +464,10 @@ __device__ __forceinline__ void sum_gradients(const Shape &d, const Bwd &b, uint
 }
 
 constexpr int kTile = 512;          // lanes of a workgroup
+constexpr uint32_t kBundle = 16;    // tiles
+constexpr uint32_t kNear = 4;       // bundles that are looked back at
+
+__host__ __device__ __forceinline__ uint32_t bundles_of(uint32_t n_tiles) { return (n_tiles + kBundle - 1) / kBundle; }
 
 // lanes that have a token's channels side by side: a power of two, at most a line of 128 bytes
 template <class T, int V>
@@ -544,10 +548,11 @@ struct Lane {
     }
 };
 
-// What the tiles share: the number of workgroups that have started, and a slot for each tile and channel: A in the lower half, B in the upper.
+// What the tiles share: the number of workgroups that have started, and slots with A in the lower half and B in the upper one, for each
+// channel of each tile and of each kBundle tiles that follow each other.
 struct Board {
     uint32_t *started;
-    uint64_t *slots;                // [n_tiles, W]
+    uint64_t *slots, *bundles;      // [n_tiles, W], [bundles_of(n_tiles), W]
 };
 
 constexpr uint64_t kEmpty = ~0ull;  // A would be a NaN that no computation gives
@@ -571,34 +576,49 @@ __device__ __forceinline__ void tell(uint64_t *slot, const float (&A)[V], const 
         __hip_atomic_store(slot + v, (uint64_t)told_bits(B[v]) << 32 | told_bits(A[v]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// waits for a slot to be written
-template <int V>
-__device__ __forceinline__ void hear(const uint64_t *slot, float (&A)[V], float (&B)[V])
+// waits for n slots, step words apart, to be written
+template <int V, int n>
+__device__ __forceinline__ void hear(const uint64_t *slot, int64_t step, uint32_t count, float (&A)[n][V], float (&B)[n][V])
 {
-    uint64_t word[V];
+    uint64_t word[n][V];
     for (uint32_t polls = 0; polls < kMostPolls; ++polls) {
         bool told = true;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            word[v] = __hip_atomic_load(slot + v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            told = told && word[v] != kEmpty;
-        }
+        for (int i = 0; i < n; ++i)
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                word[i][v] = (uint32_t)i < count ? __hip_atomic_load(slot + i * step + v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
+#pragma unroll
+        for (int i = 0; i < n; ++i)
+#pragma unroll
+            for (int v = 0; v < V; ++v) told = told && word[i][v] != kEmpty;
         if (told) break;
         __builtin_amdgcn_s_sleep(1);
     }
 #pragma unroll
-    for (int v = 0; v < V; ++v) A[v] = __uint_as_float((uint32_t)word[v]), B[v] = __uint_as_float((uint32_t)(word[v] >> 32));
+    for (int i = 0; i < n; ++i)
+#pragma unroll
+        for (int v = 0; v < V; ++v) A[i][v] = __uint_as_float((uint32_t)word[i][v]), B[i][v] = __uint_as_float((uint32_t)(word[i][v] >> 32));
 }
 
-// whether the window from place p0 on lies inside a sequence, with more of it on both sides
-__device__ __forceinline__ bool surrounded(const Shape &d, uint64_t p0)
+// The sequence that a window from place p0 on lies in, and whether it begins or ends with the window.
+struct Inside {
+    bool whole, first, last;        // whole: the window lies in one sequence
+    uint32_t seq;
+};
+
+__device__ __forceinline__ Inside inside(const Shape &d, uint64_t p0)
 {
-    if (p0 + kKeep >= d.N) return false;
-    const uint32_t k = begun_before(d, p0);
-    if (k == 0) return false;
+    Inside in = {};
+    const uint32_t k = d.first ? begun_before(d, p0 + 1) : (uint32_t)p0 / d.S + 1;
+    if (k == 0) return in;
     uint64_t begin, end;
     places(d, k - 1, begin, end);
-    return begin < p0 && end > p0 + kKeep;
+    in.whole = begin <= p0 && end >= p0 + kKeep;
+    in.first = begin == p0;
+    in.last = end == p0 + kKeep;
+    in.seq = sequence(d, k - 1);
+    return in;
 }
 
 template <int V>
@@ -635,18 +655,48 @@ __device__ __forceinline__ void append(float (&A)[V], float (&B)[V], const float
     }
 }
 
+// The state before a bundle: from the nearest of the kNear bundles before it that knows the state behind itself, through the ones in
+// between.  Of lanes that have channels.
+template <int V>
+__device__ __forceinline__ void before_bundle(const Shape &d, const Board &board, uint32_t bundle, uint32_t c, float (&h)[V])
+{
+    const uint32_t n = bundle < kNear ? bundle : kNear;
+#pragma unroll
+    for (int v = 0; v < V; ++v) h[v] = 0.0f;
+    for (uint32_t polls = 0; n && polls < kMostPolls; ++polls) {
+        float A[kNear][V], B[kNear][V];
+        hear<V, kNear>(board.bundles + (uint64_t)(bundle - 1) * d.W + c, -(int64_t)d.W, n, A, B);
+        bool known = true;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            bool met = false;                                   // going forwards to the bundle: start anew at each that knows
+#pragma unroll
+            for (int i = kNear - 1; i >= 0; --i)
+                if ((uint32_t)i < n) {
+                    h[v] = join(A[i][v], met ? h[v] : 0.0f, B[i][v]);
+                    met = met || A[i][v] == 0.0f;
+                }
+            known = known && met;
+        }
+        if (known) return;
+    }
+}
+
 // From A and B of a lane's window the state before it (backward: the gradient behind it).  All lanes of the workgroup call it.
 // mine: the place of the lane's window among those of the tile in the order in which states pass them; tile: likewise.
+//
+// A tile listens to those before it in its bundle; the last of a bundle tells what the whole bundle does, and, when it knows it, the
+// state behind it.  Whoever computes the state behind a bundle computes join(A, the state before it, B): how far back the nearest bundle
+// lies that knows its own depends on timing, the result does not.
 template <int V>
 __device__ __forceinline__ void come_in(const Shape &d, const Board &board, const Lane &l, uint32_t mine, uint32_t tile, const float (&A)[V],
                                         const float (&B)[V], float (&h)[V])
 {
-    __shared__ Pairs<V> own, heard;
-    __shared__ float in[dg::kWave * V];
-    __shared__ uint32_t done;
+    __shared__ Pairs<V> own;
+    __shared__ float heard[2][kBundle][dg::kWave * V], in[dg::kWave * V];
     lay_down<V>(own, l, mine, A, B);
-    if (threadIdx.x == 0) done = 0;
     __syncthreads();
+    const uint32_t bundle = tile / kBundle, place = tile % kBundle;
     float tA[V], tB[V];
     if (mine == 0) {
         pick_up<V>(own, l, 0, tA, tB);
@@ -655,52 +705,49 @@ __device__ __forceinline__ void come_in(const Shape &d, const Board &board, cons
             pick_up<V>(own, l, w, a, b);
             append<V>(tA, tB, a, b);
         }
-        if (tile == 0)
-#pragma unroll
-            for (int v = 0; v < V; ++v) tA[v] = 0.0f;           // nothing comes before it
         if (l.active) tell<V>(board.slots + (uint64_t)tile * d.W + l.c, tA, tB);
     }
-    // each window's lanes listen to one tile, the nearest first, until all channels have met an A of 0
-    float sA[V], sB[V];                                         // of the tiles heard so far
+    if (l.active)
+        for (uint32_t w = mine; w < place; w += l.windows) {
+            float a[1][V], b[1][V];
+            hear<V, 1>(board.slots + (uint64_t)(tile - place + w) * d.W + l.c, 0, 1, a, b);
 #pragma unroll
-    for (int v = 0; v < V; ++v) sA[v] = 1.0f, sB[v] = 0.0f;
-    for (uint32_t back = 1; tile >= back; back += l.windows) {
-        if (l.active && back + mine <= tile) {
-            float a[V], b[V];
-            hear<V>(board.slots + (uint64_t)(tile - back - mine) * d.W + l.c, a, b);
-            lay_down<V>(heard, l, mine, a, b);
+            for (int v = 0; v < V; ++v) heard[0][w][l.lane * V + v] = a[0][v], heard[1][w][l.lane * V + v] = b[0][v];
         }
-        __syncthreads();
-        if (mine == 0) {
-            bool open = false;
-            if (l.active) {
-                const uint32_t n = tile - back + 1 < l.windows ? tile - back + 1 : l.windows;
-                for (uint32_t w = 0; w < n; ++w) {
-                    float a[V], b[V];
-                    pick_up<V>(heard, l, w, a, b);
-                    append<V>(a, b, sA, sB);
+    __syncthreads();
+    if (mine == 0 && l.active) {
+        uint64_t *told = board.bundles + (uint64_t)bundle * d.W + l.c;
+        float bA[V], bB[V];
+        if (place == kBundle - 1) {
 #pragma unroll
-                    for (int v = 0; v < V; ++v) sA[v] = a[v], sB[v] = b[v];
-                }
+            for (int v = 0; v < V; ++v) bA[v] = 1.0f, bB[v] = 0.0f;
+            for (uint32_t w = 0; w < place; ++w) {
+                float a[V], b[V];
 #pragma unroll
-                for (int v = 0; v < V; ++v) open = open || sA[v] != 0.0f;
+                for (int v = 0; v < V; ++v) a[v] = heard[0][w][l.lane * V + v], b[v] = heard[1][w][l.lane * V + v];
+                append<V>(bA, bB, a, b);
             }
-            if (!__any(open) && l.lane == 0) done = 1;
-        }
-        __syncthreads();
-        if (done) break;
-    }
-    if (mine == 0) {
+            append<V>(bA, bB, tA, tB);
+            if (bundle == 0)
 #pragma unroll
-        for (int v = 0; v < V; ++v) in[l.lane * V + v] = sB[v];
-        bool open = false;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            open = open || tA[v] != 0.0f;
-            tB[v] = join(tA[v], sB[v], tB[v]);
-            tA[v] = 0.0f;
+                for (int v = 0; v < V; ++v) bA[v] = 0.0f;       // nothing comes before it
+            tell<V>(told, bA, bB);
         }
-        if (l.active && open) tell<V>(board.slots + (uint64_t)tile * d.W + l.c, tA, tB);
+        float state[V];
+        before_bundle<V>(d, board, bundle, l.c, state);
+        if (place == kBundle - 1) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                bB[v] = join(bA[v], state[v], bB[v]);
+                bA[v] = 0.0f;
+            }
+            if (bundle) tell<V>(told, bA, bB);
+        }
+        for (uint32_t w = 0; w < place; ++w)
+#pragma unroll
+            for (int v = 0; v < V; ++v) state[v] = join(heard[0][w][l.lane * V + v], state[v], heard[1][w][l.lane * V + v]);
+#pragma unroll
+        for (int v = 0; v < V; ++v) in[l.lane * V + v] = state[v];
     }
     __syncthreads();
 #pragma unroll
@@ -713,24 +760,44 @@ __device__ __forceinline__ void come_in(const Shape &d, const Board &board, cons
     }
 }
 
+// Two workgroups share a compute unit, so that one loads while the other listens: 128 registers per lane.  (With as many as the compiler
+// takes, 139 to 200, the gradient of four sequences of 16 384 tokens, 1024 channels, bf16 takes 215 us instead of 170.)
+#define TWO_PER_UNIT __attribute__((amdgpu_waves_per_eu(4)))
+
+// A and B of a window that starts from a state of its own
+template <int V>
+__device__ __forceinline__ void begin_with(float (&A)[V], float (&B)[V], const float *states, uint64_t at)
+{
+    float from[V];
+    get<V>(states, at, from);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        B[v] = join(A[v], from[v], B[v]);
+        A[v] = 0.0f;
+    }
+}
+
 template <class T, int V>
-__global__ void __launch_bounds__(kTile)
+__global__ void __launch_bounds__(kTile) TWO_PER_UNIT
 tile_fwd_kernel(Shape d, Fwd f, Board board)
 {
     const Lane l(d, V, most_across<T, V>(), start(board));
     const uint64_t p0 = ((uint64_t)l.tile * l.windows + l.window) * kKeep;
-    const bool held = l.active && p0 < d.N, inner = held && surrounded(d, p0);
+    const bool held = l.active && p0 < d.N;
+    const Inside in = held ? inside(d, p0) : Inside{};
+    const uint64_t at = (uint64_t)in.seq * d.W + l.c;
     Pack<T, V> z[kKeep], u[kKeep];
     float A[V], h[V];
     bool shutting = false;
 #pragma unroll
     for (int v = 0; v < V; ++v) A[v] = 1.0f, h[v] = 0.0f;
-    if (inner) {
+    if (in.whole) {
         load_tokens<T, V, kKeep, true>(Column<T, V>(d, f.z, f.ldz, l.c, p0), kKeep, z);
         load_tokens<T, V, kKeep, true>(Column<T, V>(d, f.u, f.ldu, l.c, p0), kKeep, u);
         shutting = any_shut<T, V, kKeep>(z);
         if (shutting) sum_loaded<T, V, kKeep, true, true>(z, u, kKeep, A, h);
         else sum_loaded<T, V, kKeep, true, false>(z, u, kKeep, A, h);
+        if (in.first) begin_with<V>(A, h, f.h0, at);
     } else if (held)
         forwards(d, p0, [&](uint32_t k, uint64_t p, uint64_t e, uint64_t begin, uint64_t) {
             if (p == begin) {
@@ -742,12 +809,14 @@ tile_fwd_kernel(Shape d, Fwd f, Board board)
         });
     float state[V];
     come_in<V>(d, board, l, l.window, l.tile, A, h, state);
-    if (inner) {
+    if (in.whole) {
+        if (in.first) get<V>(f.h0, at, state);
         put<V>(f.states, p0 / kKeep * d.W + l.c, state);
         const Column<T, V> y(d, f.y, f.ldy, l.c, p0);
         forget<T, V, kKeep>(z);
         if (shutting) advance_loaded<T, V, kKeep, true, true>(z, u, y, kKeep, state);
         else advance_loaded<T, V, kKeep, true, false>(z, u, y, kKeep, state);
+        if (in.last) put<V>(f.h_last, at, state);
     } else if (held)
         forwards(d, p0, [&](uint32_t k, uint64_t p, uint64_t e, uint64_t begin, uint64_t end) {
             const uint64_t at = (uint64_t)sequence(d, k) * d.W + l.c;
@@ -759,26 +828,29 @@ tile_fwd_kernel(Shape d, Fwd f, Board board)
 
 // from the last tile to the first
 template <class T, int V>
-__global__ void __launch_bounds__(kTile)
+__global__ void __launch_bounds__(kTile) TWO_PER_UNIT
 tile_bwd_kernel(Shape d, Bwd b, Board board)
 {
     Lane l(d, V, most_across<T, V>(), start(board));
     const uint32_t tile = l.tile;
     l.tile = d.n_tiles - 1 - tile;
     const uint64_t p0 = ((uint64_t)l.tile * l.windows + l.window) * kKeep;
-    const bool held = l.active && p0 < d.N, inner = held && surrounded(d, p0);
+    const bool held = l.active && p0 < d.N;
+    const Inside in = held ? inside(d, p0) : Inside{};
+    const uint64_t at = (uint64_t)in.seq * d.W + l.c;
     Pack<T, V> z[kKeep], u[kKeep], dy[kKeep];
     float A[V], G[V];
     bool shutting = false;
 #pragma unroll
     for (int v = 0; v < V; ++v) A[v] = 1.0f, G[v] = 0.0f;
-    if (inner) {
+    if (in.whole) {
         load_tokens<T, V, kKeep, true>(Column<T, V>(d, b.z, b.ldz, l.c, p0), kKeep, z);
         load_tokens<T, V, kKeep, true>(Column<T, V>(d, b.dy, b.lddy, l.c, p0), kKeep, dy);
         load_tokens<T, V, kKeep, true>(Column<T, V>(d, b.u, b.ldu, l.c, p0), kKeep, u);
         shutting = any_shut<T, V, kKeep>(z);
         if (shutting) sum_gradients_loaded<T, V, kKeep, true, true>(z, dy, kKeep, A, G);
         else sum_gradients_loaded<T, V, kKeep, true, false>(z, dy, kKeep, A, G);
+        if (in.last) begin_with<V>(A, G, b.dh_last, at);
     } else if (held)
         backwards(d, p0, [&](uint32_t k, uint64_t p, uint64_t e, uint64_t, uint64_t end) {
             if (e == end) {
@@ -790,10 +862,12 @@ tile_bwd_kernel(Shape d, Bwd b, Board board)
         });
     float behind[V];
     come_in<V>(d, board, l, l.windows - 1 - l.window, tile, A, G, behind);
-    if (inner) {
+    if (in.whole) {
+        if (in.last) get<V>(b.dh_last, at, behind);
         const Column<T, V> dz(d, b.dz, b.lddz, l.c, p0 + kKeep - 1), du(d, b.du, b.lddu, l.c, p0 + kKeep - 1);
         float state[V], before[kKeep][V];
-        get<V>(b.states, p0 / kKeep * d.W + l.c, state);
+        if (in.first) get<V>(b.h0, at, state);
+        else get<V>(b.states, p0 / kKeep * d.W + l.c, state);
         forget<T, V, kKeep>(z);
         if (shutting) {
             states_before<T, V, kKeep, true>(z, u, state, before);
@@ -804,6 +878,7 @@ tile_bwd_kernel(Shape d, Bwd b, Board board)
             forget<T, V, kKeep>(z);
             retreat_loaded<T, V, kKeep, true, false>(z, u, dy, before, dz, du, kKeep, behind);
         }
+        if (in.first) put<V>(b.dh0, at, behind);
     } else if (held)
         backwards(d, p0, [&](uint32_t k, uint64_t p, uint64_t e, uint64_t begin, uint64_t end) {
             const uint32_t seq = sequence(d, k);
@@ -814,15 +889,19 @@ tile_bwd_kernel(Shape d, Bwd b, Board board)
         });
 }
 
-// Empties the board.  from, copy: NULL, or states that the tiles then read in the copy because what they write lies on them.
+// Empties the board, and does the sequences without a token: what comes out is what went in.  copy: NULL, or room for `in`, which the
+// tiles then read there because `out` lies on it.
 __global__ void __launch_bounds__(kBlock)
-board_kernel(Board board, uint64_t n_slots, const float *from, float *copy, uint64_t n_states)
+board_kernel(Shape d, Board board, uint64_t n_slots, const float *in, float *copy, float *out)
 {
-    const uint64_t i0 = (uint64_t)blockIdx.x * kBlock + threadIdx.x, step = (uint64_t)gridDim.x * kBlock;
+    const uint64_t i0 = (uint64_t)blockIdx.x * kBlock + threadIdx.x, step = (uint64_t)gridDim.x * kBlock, n = (uint64_t)d.n_seq * d.W;
     if (i0 == 0) *board.started = 0;
     for (uint64_t i = i0; i < n_slots; i += step) board.slots[i] = kEmpty;
     if (copy)
-        for (uint64_t i = i0; i < n_states; i += step) copy[i] = from[i];
+        for (uint64_t i = i0; i < n; i += step) copy[i] = in[i];
+    if (d.first && out && in != out)
+        for (uint64_t i = i0; i < n; i += step)
+            if (d.first[i / d.W] >= d.first[i / d.W + 1]) out[i] = in ? in[i] : 0.0f;
 }
 
 int check(const char *who, Shape &d, uint32_t dtype)
@@ -848,13 +927,15 @@ int check_rows(const char *who, const void *p, uint64_t ld, const Shape &d, uint
     return DG_OK;
 }
 
-// Few sequences: tiles instead.  V, most: of the call.
-constexpr uint64_t kWanted = 1 << 16;
-
+// Whether tiles serve a call.  Sequence by sequence 16 tokens take some 1.6 us forward however few sequences there are, 16-bit tiles 8 us
+// and then 3 TB/s, so they pay for sequences of more than 80 tokens and a 50 000th of all values.  Sequences / tiles, forward and backward
+// in us: 256 sequences of 512 tokens, 64 channels, fp16 51 / 31 and 85 / 32; 64 of 1024, 256 channels 101 / 57 and 196 / 56; 16 of 4096, 2048
+// channels, bf16 497 / 252 and 831 / 325; 1000 of 200, 32 channels, fp32 21 / 35 and 42 / 46; 512 of 1024, 128 channels, bf16 140 / 170
+// and 230 / 203.  V, most: of the call.
 void cut(Shape &d, uint32_t V, uint32_t most)
 {
     d.n_tiles = 0;
-    if (d.n_seq == 0 || d.N / d.n_seq < 4 * kKeep || d.n_seq * ((uint64_t)(d.W + 1) / 2) >= kWanted) return;
+    if (d.n_seq == 0 || d.N / d.n_seq <= 80 + d.N * d.W / 50000) return;
     const uint32_t tile = kTile / lanes_across(d.W, V, most) * kKeep;
     d.n_tiles = (uint32_t)((d.N + tile - 1) / tile);
 }
@@ -864,7 +945,9 @@ uint32_t blocks(uint64_t count, uint32_t W, uint32_t V) { return (uint32_t)((cou
 // the board's counter and slots, and room for a copy of the states
 constexpr size_t kSlotsAt = 16;
 
-size_t workspace_bytes(const Shape &d) { return d.n_tiles ? kSlotsAt + (size_t)d.n_tiles * d.W * sizeof(uint64_t) + (size_t)d.n_seq * d.W * sizeof(float) : 0; }
+size_t slots_of(const Shape &d) { return (size_t)(d.n_tiles + bundles_of(d.n_tiles)) * d.W; }
+
+size_t workspace_bytes(const Shape &d) { return d.n_tiles ? kSlotsAt + slots_of(d) * sizeof(uint64_t) + (size_t)d.n_seq * d.W * sizeof(float) : 0; }
 
 // whatever the type and the alignment of the call: the smallest tile makes the most of them
 size_t most_workspace_bytes(Shape d)
@@ -882,13 +965,14 @@ int check_workspace(const char *who, const Shape &d, const void *ws, size_t ws_b
 }
 
 // *in: states (gradients) that the tiles read, out: where they write theirs
-Board board_of(const Shape &d, void *ws, const float **in, const float *out, hipStream_t st)
+Board board_of(const Shape &d, void *ws, const float **in, float *out, hipStream_t st)
 {
-    const uint64_t n_slots = (uint64_t)d.n_tiles * d.W;
-    const Board board = {(uint32_t *)ws, (uint64_t *)((char *)ws + kSlotsAt)};
+    const uint64_t n_slots = slots_of(d);
+    Board board = {(uint32_t *)ws, (uint64_t *)((char *)ws + kSlotsAt), nullptr};
+    board.bundles = board.slots + (uint64_t)d.n_tiles * d.W;
     float *copy = *in && *in == out ? (float *)(board.slots + n_slots) : nullptr;
     const uint64_t n = (n_slots + 4 * kBlock - 1) / (4 * kBlock);
-    board_kernel<<<(uint32_t)(n < 2048 ? n : 2048), kBlock, 0, st>>>(board, n_slots, *in, copy, (uint64_t)d.n_seq * d.W);
+    board_kernel<<<(uint32_t)(n < 2048 ? n : 2048), kBlock, 0, st>>>(d, board, n_slots, *in, copy, out);
     if (copy) *in = copy;
     return board;
 }
