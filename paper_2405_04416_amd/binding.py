@@ -666,32 +666,43 @@ def dg_mlp_bwd_split(*args):
 _TYPE_CODES = {torch.float32: DG_F32, torch.float16: DG_F16, torch.bfloat16: DG_BF16}
 
 
-def _type_code(t):
+# These calls may be as short as a launch: one condition finds out that all is well, and only otherwise what is not.
+def _rows(t, dtype, shape):
+    """(pointer, distance between rows) of a tensor of that type and shape [N, W] whose rows are contiguous."""
+    N, W = shape
+    ld, step = t.stride() if t.dim() == 2 else (0, 0)
+    if t.is_cuda and t.dtype is dtype and t.shape == shape and step == 1 and ld >= W:
+        return t.data_ptr(), ld
+    return _unusual_rows(t, dtype, shape)
+
+
+def _unusual_rows(t, dtype, shape):
+    if not t.is_cuda:
+        raise DistGridError("tensor must live on the GPU")
+    if t.dtype != dtype or t.shape != shape:
+        raise DistGridError("expected %s %s, got %s %s" % (dtype, tuple(shape), t.dtype, tuple(t.shape)))
+    N, W = shape
+    ld, step = t.stride()
+    if (step != 1 and W > 1) or (ld < W and N > 1):
+        raise DistGridError("the values of a row must lie next to each other, and rows apart")
+    return t.data_ptr(), ld if N > 1 and ld >= W else W
+
+
+def _code(t, rows=True):
     code = _TYPE_CODES.get(t.dtype)
     if code is None:
         raise DistGridError("expected fp32, fp16 or bf16, got %s" % t.dtype)
-    return code
-
-
-def _rows2d(t, like=None):
-    """(pointer, distance between rows) of a [N, W] tensor whose rows are contiguous; of like's shape and type."""
-    if not t.is_cuda:
-        raise DistGridError("tensor must live on the GPU")
-    if t.dim() != 2:
+    if rows and t.dim() != 2:
         raise DistGridError("expected [rows, width], got %d dimensions" % t.dim())
-    N, W = t.shape
-    ld, step = t.stride()
-    if like is not None and (t.dtype != like.dtype or t.shape != like.shape):
-        raise DistGridError("expected %s %s, got %s %s" % (like.dtype, tuple(like.shape), t.dtype, tuple(t.shape)))
-    if (step != 1 and W > 1) or (ld < W and N > 1):
-        raise DistGridError("the values of a row must lie next to each other, and rows apart")
-    return t.data_ptr(), ld if N > 1 else W
+    return code
 
 
 def _vector(t, n, dtype=torch.float32):
     """Pointer to n contiguous values, or None."""
     if t is None:
         return None
+    if t.is_cuda and t.dtype is dtype and t.numel() == n and t.is_contiguous():
+        return t.data_ptr()
     if t.numel() != n:
         raise DistGridError("expected %d values, got %d" % (n, t.numel()))
     return _ptr(t, dtype)
@@ -703,7 +714,9 @@ def _workspace(ws):
 
 def dg_layer_norm_fwd(x, gamma, beta, eps, y):
     """x, y [N, W] fp32, fp16 or bf16; gamma, beta [W] fp32 or None."""
-    code, (px, ldx), (py, ldy), (N, W) = _type_code(x), _rows2d(x), _rows2d(y, x), x.shape
+    code, dtype, shape = _code(x), x.dtype, x.shape
+    N, W = shape
+    (px, ldx), (py, ldy) = _rows(x, dtype, shape), _rows(y, dtype, shape)
     _check(lib().dg_layer_norm_fwd(px, ldx, _vector(gamma, W), _vector(beta, W), N, W, eps, code, py, ldy, _stream()))
 
 
@@ -713,8 +726,10 @@ def dg_layer_norm_bwd_workspace_bytes(N, W):
 
 def dg_layer_norm_bwd(x, gamma, dy, eps, dx, dgamma, dbeta, ws=None):
     """dx, dgamma, dbeta: each may be None."""
-    code, (px, ldx), (pdy, lddy), (N, W) = _type_code(x), _rows2d(x), _rows2d(dy, x), x.shape
-    pdx, lddx = (None, W) if dx is None else _rows2d(dx, x)
+    code, dtype, shape = _code(x), x.dtype, x.shape
+    N, W = shape
+    (px, ldx), (pdy, lddy) = _rows(x, dtype, shape), _rows(dy, dtype, shape)
+    pdx, lddx = (None, W) if dx is None else _rows(dx, dtype, shape)
     pws, ws_bytes = _workspace(ws)
     _check(lib().dg_layer_norm_bwd(px, ldx, _vector(gamma, W), pdy, lddy, N, W, eps, code, pdx, lddx, _vector(dgamma, W), _vector(dbeta, W), pws, ws_bytes,
                                    _stream()))
@@ -730,7 +745,9 @@ def dg_recurrence_workspace_bytes(N, n_seq, W):
 
 def dg_recurrence_fwd(z, u, n_seq, first, reverse, h0, y, h_last, states, ws=None):
     """z, u, y [N, W]; first [n_seq + 1] int32 or None; h0, h_last [n_seq, W] fp32 and states (dg_recurrence_state_count values), each may be None."""
-    code, (pz, ldz), (pu, ldu), (py, ldy), (N, W) = _type_code(z), _rows2d(z), _rows2d(u, z), _rows2d(y, z), z.shape
+    code, dtype, shape = _code(z), z.dtype, z.shape
+    N, W = shape
+    (pz, ldz), (pu, ldu), (py, ldy) = _rows(z, dtype, shape), _rows(u, dtype, shape), _rows(y, dtype, shape)
     pws, ws_bytes = _workspace(ws)
     _check(lib().dg_recurrence_fwd(pz, ldz, pu, ldu, N, n_seq, _vector(first, n_seq + 1, torch.int32), W, reverse, code, _vector(h0, n_seq * W), py, ldy,
                                    _vector(h_last, n_seq * W), None if states is None else _vector(states, dg_recurrence_state_count(N, W)), pws, ws_bytes,
@@ -739,8 +756,10 @@ def dg_recurrence_fwd(z, u, n_seq, first, reverse, h0, y, h_last, states, ws=Non
 
 def dg_recurrence_bwd(z, u, n_seq, first, reverse, h0, states, dy, dh_last, dz, du, dh0, ws=None):
     """states: as the forward pass left them; h0, dh_last, dh0 [n_seq, W] fp32, each may be None."""
-    code, (pz, ldz), (pu, ldu), (pdy, lddy), (N, W) = _type_code(z), _rows2d(z), _rows2d(u, z), _rows2d(dy, z), z.shape
-    (pdz, lddz), (pdu, lddu) = _rows2d(dz, z), _rows2d(du, z)
+    code, dtype, shape = _code(z), z.dtype, z.shape
+    N, W = shape
+    (pz, ldz), (pu, ldu), (pdy, lddy) = _rows(z, dtype, shape), _rows(u, dtype, shape), _rows(dy, dtype, shape)
+    (pdz, lddz), (pdu, lddu) = _rows(dz, dtype, shape), _rows(du, dtype, shape)
     pws, ws_bytes = _workspace(ws)
     _check(lib().dg_recurrence_bwd(pz, ldz, pu, ldu, N, n_seq, _vector(first, n_seq + 1, torch.int32), W, reverse, code, _vector(h0, n_seq * W),
                                    _vector(states, dg_recurrence_state_count(N, W)), pdy, lddy, _vector(dh_last, n_seq * W), pdz, lddz, pdu, lddu,
@@ -749,10 +768,10 @@ def dg_recurrence_bwd(z, u, n_seq, first, reverse, h0, states, dy, dh_last, dz, 
 
 def dg_dropout_fwd(x, residual, p, seed, offset, y):
     """x, residual (or None), y: contiguous, of one type and size."""
-    code, n = _type_code(x), x.numel()
-    _check(lib().dg_dropout_fwd(_ptr(x), _vector(residual, n, x.dtype), n, p, seed, offset, code, _vector(y, n, x.dtype), _stream()))
+    code, n, dtype = _code(x, rows=False), x.numel(), x.dtype
+    _check(lib().dg_dropout_fwd(_vector(x, n, dtype), _vector(residual, n, dtype), n, p, seed, offset, code, _vector(y, n, dtype), _stream()))
 
 
 def dg_dropout_bwd(dy, p, seed, offset, dx):
-    code, n = _type_code(dy), dy.numel()
-    _check(lib().dg_dropout_bwd(_ptr(dy), n, p, seed, offset, code, _vector(dx, n, dy.dtype), _stream()))
+    code, n, dtype = _code(dy, rows=False), dy.numel(), dy.dtype
+    _check(lib().dg_dropout_bwd(_vector(dy, n, dtype), n, p, seed, offset, code, _vector(dx, n, dtype), _stream()))
