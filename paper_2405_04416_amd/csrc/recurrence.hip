@@ -70,11 +70,11 @@ __device__ __forceinline__ float advance(const Step &s, float h)
     return kShutting && s.a == 0.0f ? s.b : fmaf(s.a, h, s.b);
 }
 
-// a stretch of tokens takes the state h to join(A, h, B), A the product of its gates
-__device__ __forceinline__ float join(float A, float h, float B) { return (A == 0.0f ? 0.0f : A * h) + B; }
+// A stretch of tokens takes the state h to join(A, h, B), A the product of its gates.  The product is 0 only if a gate is, and kLeast where it
+// would be less, so that a state that is infinite or NaN gets through a long stretch as it does token by token; to a finite state that adds
+// less than 2^-126 of itself.
+__device__ __forceinline__ float join(float A, float h, float B) { return A == 0.0f ? B : fmaf(A, h, B); }
 
-// A product of gates: 0 only if one of them is, so that a state that is infinite or NaN gets through a long stretch as it does token
-// by token.  What this adds to a finite state is below 2^-126 of it.
 __device__ __forceinline__ float times(float A, float a) { return a == 0.0f ? 0.0f : fmaxf(A * a, A == 0.0f ? 0.0f : kLeast); }
 
 struct Shape {
@@ -190,7 +190,7 @@ struct Bwd {
     float *dh0;
 };
 
-// Runs f(place, number of tokens, full) over [p, end) in pieces that end where states are kept.
+// Runs f(place, number of tokens) over [p, end) in pieces that end where states are kept.
 template <class F>
 __device__ __forceinline__ void in_pieces(uint64_t p, uint64_t end, F f)
 {
@@ -556,7 +556,7 @@ struct Board {
 };
 
 constexpr uint64_t kEmpty = ~0ull;  // A would be a NaN that no computation gives
-constexpr uint32_t kMostPolls = 1u << 20;      // a second or so; the state is then a NaN
+constexpr uint32_t kMostPolls = 1u << 20;      // of a lane, a second or so: then it takes NaN for what it has not heard
 
 __device__ __forceinline__ uint32_t start(const Board &b)
 {
@@ -576,12 +576,12 @@ __device__ __forceinline__ void tell(uint64_t *slot, const float (&A)[V], const 
         __hip_atomic_store(slot + v, (uint64_t)told_bits(B[v]) << 32 | told_bits(A[v]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// waits for n slots, step words apart, to be written
+// waits for the first `count` of n slots, step words apart, to be written
 template <int V, int n>
-__device__ __forceinline__ void hear(const uint64_t *slot, int64_t step, uint32_t count, float (&A)[n][V], float (&B)[n][V])
+__device__ __forceinline__ void hear(const uint64_t *slot, int64_t step, uint32_t count, uint32_t &polls, float (&A)[n][V], float (&B)[n][V])
 {
     uint64_t word[n][V];
-    for (uint32_t polls = 0; polls < kMostPolls; ++polls) {
+    for (;;) {
         bool told = true;
 #pragma unroll
         for (int i = 0; i < n; ++i)
@@ -592,7 +592,8 @@ __device__ __forceinline__ void hear(const uint64_t *slot, int64_t step, uint32_
         for (int i = 0; i < n; ++i)
 #pragma unroll
             for (int v = 0; v < V; ++v) told = told && word[i][v] != kEmpty;
-        if (told) break;
+        if (told || polls == 0) break;
+        --polls;
         __builtin_amdgcn_s_sleep(1);
     }
 #pragma unroll
@@ -644,28 +645,54 @@ __device__ __forceinline__ void pick_up(const Pairs<V> &all, const Lane &l, uint
     }
 }
 
-// (A, B) of a stretch, then (a, b) of the one behind it: of both
-template <int V>
-__device__ __forceinline__ void append(float (&A)[V], float (&B)[V], const float (&a)[V], const float (&b)[V])
+// h through n stretches one after the other, load(w, a, b) gives A and B of stretch w; A: the product of theirs with it.  As fast as can be
+// first, then with care where that could matter: a state that is not finite stays so on the fast way, even past an A of 0.
+template <int V, class Load>
+__device__ __forceinline__ void pass(uint32_t n, Load load, float (&A)[V], float (&h)[V])
 {
+    float from[V], product[V], least[V];
+    bool finite = true;
+#pragma unroll
+    for (int v = 0; v < V; ++v) from[v] = h[v], product[v] = least[v] = A[v];
+#pragma unroll 4
+    for (uint32_t w = 0; w < n; ++w) {
+        float a[V], b[V];
+        load(w, a, b);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            h[v] = fmaf(a[v], h[v], b[v]);
+            product[v] *= a[v];
+            least[v] = fminf(least[v], a[v]);
+        }
+    }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        B[v] = join(a[v], B[v], b[v]);
-        A[v] = times(A[v], a[v]);
+        A[v] = least[v] == 0.0f ? 0.0f : fmaxf(product[v], kLeast);
+        finite = finite && fabsf(h[v]) <= 3.40282347e38f;
+    }
+    if (finite) return;
+#pragma unroll
+    for (int v = 0; v < V; ++v) h[v] = from[v];
+#pragma unroll 1
+    for (uint32_t w = 0; w < n; ++w) {
+        float a[V], b[V];
+        load(w, a, b);
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[v] = join(a[v], h[v], b[v]);
     }
 }
 
 // The state before a bundle: from the nearest of the kNear bundles before it that knows the state behind itself, through the ones in
 // between.  Of lanes that have channels.
 template <int V>
-__device__ __forceinline__ void before_bundle(const Shape &d, const Board &board, uint32_t bundle, uint32_t c, float (&h)[V])
+__device__ __forceinline__ void before_bundle(const Shape &d, const Board &board, uint32_t bundle, uint32_t c, uint32_t &polls, float (&h)[V])
 {
     const uint32_t n = bundle < kNear ? bundle : kNear;
 #pragma unroll
     for (int v = 0; v < V; ++v) h[v] = 0.0f;
-    for (uint32_t polls = 0; n && polls < kMostPolls; ++polls) {
+    while (n) {
         float A[kNear][V], B[kNear][V];
-        hear<V, kNear>(board.bundles + (uint64_t)(bundle - 1) * d.W + c, -(int64_t)d.W, n, A, B);
+        hear<V, kNear>(board.bundles + (uint64_t)(bundle - 1) * d.W + c, -(int64_t)d.W, n, polls, A, B);
         bool known = true;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -679,7 +706,12 @@ __device__ __forceinline__ void before_bundle(const Shape &d, const Board &board
             known = known && met;
         }
         if (known) return;
+        if (polls == 0) break;
+        --polls;
     }
+    if (n)
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[v] = __uint_as_float(0x7fc00000u);
 }
 
 // From A and B of a lane's window the state before it (backward: the gradient behind it).  All lanes of the workgroup call it.
@@ -694,23 +726,26 @@ __device__ __forceinline__ void come_in(const Shape &d, const Board &board, cons
 {
     __shared__ Pairs<V> own;
     __shared__ float heard[2][kBundle][dg::kWave * V], in[dg::kWave * V];
+    uint32_t polls = kMostPolls;
+    auto window = [&](uint32_t w, float (&a)[V], float (&b)[V]) { pick_up<V>(own, l, w, a, b); };
+    auto neighbour = [&](uint32_t w, float (&a)[V], float (&b)[V]) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) a[v] = heard[0][w][l.lane * V + v], b[v] = heard[1][w][l.lane * V + v];
+    };
     lay_down<V>(own, l, mine, A, B);
     __syncthreads();
     const uint32_t bundle = tile / kBundle, place = tile % kBundle;
-    float tA[V], tB[V];
+    float tA[V] = {}, tB[V] = {};
     if (mine == 0) {
-        pick_up<V>(own, l, 0, tA, tB);
-        for (uint32_t w = 1; w < l.windows; ++w) {
-            float a[V], b[V];
-            pick_up<V>(own, l, w, a, b);
-            append<V>(tA, tB, a, b);
-        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) tA[v] = 1.0f, tB[v] = 0.0f;
+        pass<V>(l.windows, window, tA, tB);
         if (l.active) tell<V>(board.slots + (uint64_t)tile * d.W + l.c, tA, tB);
     }
     if (l.active)
         for (uint32_t w = mine; w < place; w += l.windows) {
             float a[1][V], b[1][V];
-            hear<V, 1>(board.slots + (uint64_t)(tile - place + w) * d.W + l.c, 0, 1, a, b);
+            hear<V, 1>(board.slots + (uint64_t)(tile - place + w) * d.W + l.c, 0, 1, polls, a, b);
 #pragma unroll
             for (int v = 0; v < V; ++v) heard[0][w][l.lane * V + v] = a[0][v], heard[1][w][l.lane * V + v] = b[0][v];
         }
@@ -721,20 +756,16 @@ __device__ __forceinline__ void come_in(const Shape &d, const Board &board, cons
         if (place == kBundle - 1) {
 #pragma unroll
             for (int v = 0; v < V; ++v) bA[v] = 1.0f, bB[v] = 0.0f;
-            for (uint32_t w = 0; w < place; ++w) {
-                float a[V], b[V];
+            pass<V>(place, neighbour, bA, bB);
 #pragma unroll
-                for (int v = 0; v < V; ++v) a[v] = heard[0][w][l.lane * V + v], b[v] = heard[1][w][l.lane * V + v];
-                append<V>(bA, bB, a, b);
+            for (int v = 0; v < V; ++v) {
+                bB[v] = join(tA[v], bB[v], tB[v]);
+                bA[v] = bundle == 0 ? 0.0f : times(bA[v], tA[v]);       // nothing comes before the first
             }
-            append<V>(bA, bB, tA, tB);
-            if (bundle == 0)
-#pragma unroll
-                for (int v = 0; v < V; ++v) bA[v] = 0.0f;       // nothing comes before it
             tell<V>(told, bA, bB);
         }
         float state[V];
-        before_bundle<V>(d, board, bundle, l.c, state);
+        before_bundle<V>(d, board, bundle, l.c, polls, state);
         if (place == kBundle - 1) {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
@@ -743,21 +774,14 @@ __device__ __forceinline__ void come_in(const Shape &d, const Board &board, cons
             }
             if (bundle) tell<V>(told, bA, bB);
         }
-        for (uint32_t w = 0; w < place; ++w)
-#pragma unroll
-            for (int v = 0; v < V; ++v) state[v] = join(heard[0][w][l.lane * V + v], state[v], heard[1][w][l.lane * V + v]);
+        pass<V>(place, neighbour, tA, state);
 #pragma unroll
         for (int v = 0; v < V; ++v) in[l.lane * V + v] = state[v];
     }
     __syncthreads();
 #pragma unroll
     for (int v = 0; v < V; ++v) h[v] = in[l.lane * V + v];
-    for (uint32_t w = 0; w < mine; ++w) {
-        float a[V], b[V];
-        pick_up<V>(own, l, w, a, b);
-#pragma unroll
-        for (int v = 0; v < V; ++v) h[v] = join(a[v], h[v], b[v]);
-    }
+    pass<V>(mine, window, tA, h);
 }
 
 // Two workgroups share a compute unit, so that one loads while the other listens: 128 registers per lane.  (With as many as the compiler
@@ -900,8 +924,10 @@ board_kernel(Shape d, Board board, uint64_t n_slots, const float *in, float *cop
     if (copy)
         for (uint64_t i = i0; i < n; i += step) copy[i] = in[i];
     if (d.first && out && in != out)
-        for (uint64_t i = i0; i < n; i += step)
-            if (d.first[i / d.W] >= d.first[i / d.W + 1]) out[i] = in ? in[i] : 0.0f;
+        for (uint64_t i = i0; i < n; i += step) {
+            const uint64_t end = d.first[i / d.W + 1];
+            if (d.first[i / d.W] >= (end < d.N ? end : d.N)) out[i] = in ? in[i] : 0.0f;
+        }
 }
 
 int check(const char *who, Shape &d, uint32_t dtype)
