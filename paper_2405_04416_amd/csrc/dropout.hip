@@ -26,7 +26,8 @@ __device__ __forceinline__ float dropped(uint64_t bits, int k, uint32_t below, f
 }
 
 // 16 bytes per lane and array; the values behind the last whole vector are done by the first lanes of the last workgroup, one word each.
-// Bound by memory: the generator costs some 14 operations per element, which hide behind the loads.
+// Bound by memory: the generator costs some 14 operations per element, which hide behind the loads.  2^28 fp16 values: with a residual 246 us
+// (6.5 TB/s), without 167 (6.4); through the caches 268 with one.
 template <class T, bool kResidual, bool kStreamed>
 __global__ void __launch_bounds__(kBlock)
 dropout_kernel(Drop a)

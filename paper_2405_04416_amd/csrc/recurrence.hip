@@ -5,6 +5,13 @@
 //
 // Tokens have a place in the order in which they are gone through: their row, or N - 1 - row back to front.  The forward pass
 // keeps the state before every kKeep-th place in fp32; the backward pass computes the states between them again.
+//
+// Bound by memory: 3 values moved per element forward, 5 backward, for some 13 and 40 operations, two in three of them an exp2 and a
+// reciprocal at a quarter of the rate.  Many sequences: a lane runs through a sequence's tokens, 16 of them on their way at a time.  2^17 rays of
+// 64 samples, 32 channels in fp16: forward 306 us (5.3 TB/s), backward 506 (5.3).  Few long ones: tiles that tell each other what they do to a
+// state; each value is still read once.  One sequence of 2^17 tokens, 256 channels in bf16: forward 69 us (2.9 TB/s), backward 103 (3.3); four of
+// 16 384, 1024 channels: 108 (3.7) and 169 (4.0).  What keeps tiles from 6 TB/s: two workgroups per compute unit load, compute, listen and
+// store in turn, and the gates are computed twice.
 #include <type_traits>
 #include "rows_common.h"
 
@@ -953,15 +960,17 @@ int check_rows(const char *who, const void *p, uint64_t ld, const Shape &d, uint
     return DG_OK;
 }
 
-// Whether tiles serve a call.  Sequence by sequence 16 tokens take some 1.6 us forward however few sequences there are, 16-bit tiles 8 us
-// and then 3 TB/s, so they pay for sequences of more than 80 tokens and a 50 000th of all values.  Sequences / tiles, forward and backward
-// in us: 256 sequences of 512 tokens, 64 channels, fp16 51 / 31 and 85 / 32; 64 of 1024, 256 channels 101 / 57 and 196 / 56; 16 of 4096, 2048
-// channels, bf16 497 / 252 and 831 / 325; 1000 of 200, 32 channels, fp32 21 / 35 and 42 / 46; 512 of 1024, 128 channels, bf16 140 / 170
-// and 230 / 203.  V, most: of the call.
+// Whether tiles serve a call.  Sequence by sequence 16 tokens take some 1.6 us forward however few sequences there are; tiles take 8 us
+// and then 3 TB/s with 16-bit values, and longer where many windows hold a sequence's end.  They pay for sequences of more than 120
+// tokens and an 80 000th of all values.  Sequences / tiles in us, forward and backward: 256 sequences of 512 tokens, 64 channels, fp16
+// 51 / 28 and 85 / 32; 64 of 1024, 256 channels 103 / 48 and 196 / 55; 16 of 4096, 2048 channels, bf16 528 / 203 and 832 / 310; 512 of 1024, 128
+// channels 140 / 129 and 230 / 194; 400 of 256, 128 channels 30 / 36 and 56 / 51; 4000 of 400, 64 channels 128 / 193 and 216 / 293; 100 of 400, 32
+// channels, fp32 30 / 12 and 45 / 14; 1000 of 200, 32 channels 21 / 35 and 43 / 46; 1000 of 2000, 64 channels 317 / 339 and 524 / 525;
+// 300 of 1500, 512 channels, fp16 339 / 525 and 602 / 605.  V, most: of the call.
 void cut(Shape &d, uint32_t V, uint32_t most)
 {
     d.n_tiles = 0;
-    if (d.n_seq == 0 || d.N / d.n_seq <= 80 + d.N * d.W / 50000) return;
+    if (d.n_seq == 0 || d.N / d.n_seq <= 120 + d.N * d.W / 80000) return;
     const uint32_t tile = kTile / lanes_across(d.W, V, most) * kKeep;
     d.n_tiles = (uint32_t)((d.N + tile - 1) / tile);
 }
