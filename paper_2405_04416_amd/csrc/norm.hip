@@ -398,14 +398,14 @@ Spread spread_of(uint32_t n, bool small)
     return {0, 0};
 }
 
-// Workgroups of the backward pass.  Each leaves 2 W sums, so that wide rows have fewer, and each has some 8192 values to itself, but all
-// compute units have two.  (8192 rows of 4096 bf16 values: 512 workgroups 57.7 us, 1024 66.2; 2^23 of 32 fp16 values: 2048 304 us, 1024 323;
-// 200 000 of 32: 2048 19.7 us, 1024 15.3.)
+// Workgroups of the backward pass.  Each leaves 2 W sums, so that wide rows have fewer, and each has some 6000 values to itself, but all
+// compute units have two, and as many as each other.  (8192 rows of 4096 bf16 values: 512 workgroups 57.7 us, 1024 66.2; 2^23 of 32 fp16
+// values: 2048 304 us, 1024 323; 200 000 of 32: 2048 19.7 us, 1563 20.2, 1024 15.3, 781 19.3.)
 uint32_t parts_of(uint64_t N, uint32_t W)
 {
-    const uint64_t most = W <= 512 ? 2048 : W <= 2048 ? 1024 : 512, rows = W <= 512 ? 8192 / W : W <= 2048 ? 16 : 8;
-    const uint64_t least = (N + 3) / 4 < 512 ? (N + 3) / 4 : 512, p = (N + rows - 1) / rows;
-    return (uint32_t)(p > most ? most : p < least ? least : p);
+    const uint64_t most = W <= 512 ? 2048 : W <= 2048 ? 1024 : 512, rows = W <= 512 ? 6144 / W : W <= 2048 ? 16 : 8;
+    const uint64_t p = (N + rows - 1) / rows, least = (N + 3) / 4 < 512 ? (N + 3) / 4 : 512;
+    return (uint32_t)(p > most ? most : p < least ? least : p >= 512 ? p / 512 * 512 : p);
 }
 
 constexpr uint64_t kMostBlocks = 2048;      // of the forward pass: as many as the chip holds at once
