@@ -12,7 +12,6 @@
 // state; each value is still read once.  One sequence of 2^17 tokens, 256 channels in bf16: forward 69 us (2.9 TB/s), backward 103 (3.3); four of
 // 16 384, 1024 channels: 108 (3.7) and 169 (4.0).  What keeps tiles from 6 TB/s: two workgroups per compute unit load, compute, listen and
 // store in turn, and the gates are computed twice.
-#include <type_traits>
 #include "rows_common.h"
 
 namespace {
@@ -33,9 +32,31 @@ __device__ __forceinline__ Gate gate(float z)
     return {a, e * a};
 }
 
+// V neighbouring values as they lie in memory, in one register until they are used: arrays of 16-bit values would be taken apart.
+template <class T, int V>
+struct Raw {
+    static_assert(sizeof(T) * V <= 4, "one register");
+    uint32_t bits;
+    __device__ __forceinline__ void load(const T *p)
+    {
+        if constexpr (sizeof(T) * V == 4) bits = *reinterpret_cast<const uint32_t *>(p);
+        else bits = *reinterpret_cast<const uint16_t *>(p);
+    }
+    __device__ __forceinline__ float operator[](int v) const;
+};
+template <>
+__device__ __forceinline__ float Raw<float, 1>::operator[](int) const { return __uint_as_float(bits); }
+template <>
+__device__ __forceinline__ float Raw<f16, 1>::operator[](int) const { return (float)__builtin_bit_cast(f16, (uint16_t)bits); }
+template <>
+__device__ __forceinline__ float Raw<f16, 2>::operator[](int v) const { return (float)__builtin_bit_cast(f16, (uint16_t)(v ? bits >> 16 : bits)); }
+template <>
+__device__ __forceinline__ float Raw<bf16, 1>::operator[](int) const { return __uint_as_float(bits << 16); }
+template <>
+__device__ __forceinline__ float Raw<bf16, 2>::operator[](int v) const { return __uint_as_float(v ? bits & 0xffff0000u : bits << 16); }
+
 // Whether a wavefront has a shut gate among the tokens that it has loaded; they are then gone through looking at each gate.  By their
-// bits, which without the sign order numbers by magnitude with infinity and NaN on top: two operations for two 16-bit values, and no
-// fp32 copies of the gates that would stay in registers.
+// bits, which without the sign order numbers by magnitude with infinity and NaN on top.
 template <class T>
 struct Bits;
 template <>
@@ -46,13 +67,14 @@ template <>
 struct Bits<bf16> { using type = uint16_t; static constexpr type kMagnitude = 0x7fffu, kShut = 0x42aeu; };
 
 template <class T, int V, int M>
-__device__ __forceinline__ bool any_shut(const Pack<T, V> (&z)[M])
+__device__ __forceinline__ bool any_shut(const Raw<T, V> (&z)[M])
 {
     using B = typename Bits<T>::type;
-    typedef B Vector __attribute__((ext_vector_type(V)));
+    constexpr int n = 4 / sizeof(B);
+    typedef B Vector __attribute__((ext_vector_type(n)));
     Vector most = 0;
 #pragma unroll
-    for (int k = 0; k < M; ++k) most = __builtin_elementwise_max(most, __builtin_bit_cast(Vector, z[k]) & (Vector)Bits<T>::kMagnitude);
+    for (int k = 0; k < M; ++k) most = __builtin_elementwise_max(most, __builtin_bit_cast(Vector, z[k].bits) & (Vector)Bits<T>::kMagnitude);
     bool shut = false;
 #pragma unroll
     for (int v = 0; v < V; ++v) shut = shut || most[v] >= Bits<T>::kShut;
@@ -142,28 +164,21 @@ struct Column {
 };
 
 template <class T, int V, int M, bool kFull>
-__device__ __forceinline__ void load_tokens(Column<T, V> col, int n, Pack<T, V> (&out)[M])
+__device__ __forceinline__ void load_tokens(Column<T, V> col, int n, Raw<T, V> (&out)[M])
 {
 #pragma unroll
     for (int k = 0; k < M; ++k) {
-        out[k] = *reinterpret_cast<const Pack<T, V> *>(col.at);
+        out[k].load(col.at);
         if (kFull || k + 1 < n) col.at += col.step;         // past the last token: that one again
     }
 }
 
-// The compiler takes what it knows of these values for unknown from here on: what was computed from them is computed again instead of
-// kept in registers.
+// The compiler takes these values for unknown from here on: what was computed from them is computed again instead of kept in registers.
 template <class T, int V, int M>
-__device__ __forceinline__ void forget(Pack<T, V> (&a)[M])
+__device__ __forceinline__ void forget(Raw<T, V> (&a)[M])
 {
-    using Bits = typename std::conditional<sizeof(Pack<T, V>) == 2, uint16_t, uint32_t>::type;
-    static_assert(sizeof(Pack<T, V>) == sizeof(Bits), "one register");
 #pragma unroll
-    for (int k = 0; k < M; ++k) {
-        Bits b = __builtin_bit_cast(Bits, a[k]);
-        asm volatile("" : "+v"(b));
-        a[k] = __builtin_bit_cast(Pack<T, V>, b);
-    }
+    for (int k = 0; k < M; ++k) asm volatile("" : "+v"(a[k].bits));
 }
 
 template <int V>
@@ -210,13 +225,13 @@ __device__ __forceinline__ void in_pieces(uint64_t p, uint64_t end, F f)
 }
 
 template <class T, int V, int M, bool kFull, bool kShutting>
-__device__ __forceinline__ void advance_loaded(const Pack<T, V> (&z)[M], const Pack<T, V> (&u)[M], Column<T, V> y, int n, float (&h)[V])
+__device__ __forceinline__ void advance_loaded(const Raw<T, V> (&z)[M], const Raw<T, V> (&u)[M], Column<T, V> y, int n, float (&h)[V])
 {
 #pragma unroll
     for (int k = 0; k < M; ++k)
         if (kFull || k < n) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) h[v] = advance<kShutting>(step_of<kShutting>((float)z[k].v[v], (float)u[k].v[v]), h[v]);
+            for (int v = 0; v < V; ++v) h[v] = advance<kShutting>(step_of<kShutting>(z[k][v], u[k][v]), h[v]);
             store<T, V>(y.at, h);
             y.at += y.step;
         }
@@ -225,7 +240,7 @@ __device__ __forceinline__ void advance_loaded(const Pack<T, V> (&z)[M], const P
 template <class T, int V, int M, bool kFull>
 __device__ __forceinline__ void advance_tokens(const Shape &d, const Fwd &f, uint32_t c, uint64_t p, int n, float (&h)[V])
 {
-    Pack<T, V> z[M], u[M];
+    Raw<T, V> z[M], u[M];
     load_tokens<T, V, M, kFull>(Column<T, V>(d, f.z, f.ldz, c, p), n, z);
     load_tokens<T, V, M, kFull>(Column<T, V>(d, f.u, f.ldu, c, p), n, u);
     const Column<T, V> y(d, f.y, f.ldy, c, p);
@@ -245,24 +260,25 @@ __device__ __forceinline__ void advance_places(const Shape &d, const Fwd &f, uin
     });
 }
 
-// the states before the tokens, and h behind them
+// the states before the tokens less their inputs, h_{t-1} - u_t
 template <class T, int V, int M, bool kShutting>
-__device__ __forceinline__ void states_before(const Pack<T, V> (&z)[M], const Pack<T, V> (&u)[M], float (&h)[V], float (&before)[M][V])
+__device__ __forceinline__ void steps_taken(const Raw<T, V> (&z)[M], const Raw<T, V> (&u)[M], float (&h)[V], float (&less)[M][V])
 {
 #pragma unroll
     for (int k = 0; k < M; ++k)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            before[k][v] = h[v];
-            h[v] = advance<kShutting>(step_of<kShutting>((float)z[k].v[v], (float)u[k].v[v]), h[v]);
+            const float uu = u[k][v];
+            less[k][v] = h[v] - uu;
+            h[v] = advance<kShutting>(step_of<kShutting>(z[k][v], uu), h[v]);
         }
 }
 
 // The gradients of loaded tokens, last first.  The gates are computed again: keeping a, c and a c (h_{t-1} - u) from the way forwards costs
 // 96 registers where this takes 48, and half of the wavefronts.
 template <class T, int V, int M, bool kFull, bool kShutting>
-__device__ __forceinline__ void retreat_loaded(const Pack<T, V> (&z)[M], const Pack<T, V> (&u)[M], const Pack<T, V> (&dy)[M], const float (&before)[M][V],
-                                               Column<T, V> dz, Column<T, V> du, int n, float (&G)[V])
+__device__ __forceinline__ void retreat_loaded(const Raw<T, V> (&z)[M], const Raw<T, V> (&dy)[M], const float (&less)[M][V], Column<T, V> dz,
+                                               Column<T, V> du, int n, float (&G)[V])
 {
 #pragma unroll
     for (int k = M - 1; k >= 0; --k)
@@ -270,12 +286,11 @@ __device__ __forceinline__ void retreat_loaded(const Pack<T, V> (&z)[M], const P
             float oz[V], ou[V];
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const float uu = (float)u[k].v[v];
-                const Step s = step_of<kShutting>((float)z[k].v[v], uu);
-                G[v] += (float)dy[k].v[v];
+                const Step s = step_of<kShutting>(z[k][v], 0.0f);
+                G[v] += dy[k][v];
                 ou[v] = kShutting && s.c == 0.0f ? 0.0f : s.c * G[v];
                 G[v] = kShutting && s.a == 0.0f ? 0.0f : s.a * G[v];
-                oz[v] = kShutting && (s.c == 0.0f || s.a == 0.0f) ? 0.0f : s.c * (before[k][v] - uu) * G[v];
+                oz[v] = kShutting && (s.c == 0.0f || s.a == 0.0f) ? 0.0f : s.c * less[k][v] * G[v];
             }
             store<T, V>(dz.at, oz);
             store<T, V>(du.at, ou);
@@ -287,20 +302,20 @@ __device__ __forceinline__ void retreat_loaded(const Pack<T, V> (&z)[M], const P
 template <class T, int V, int M, bool kFull>
 __device__ __forceinline__ void retreat_tokens(const Shape &d, const Bwd &b, uint32_t c, uint64_t p, int n, float (&h)[V], float (&G)[V])
 {
-    Pack<T, V> z[M], u[M], dy[M];
+    Raw<T, V> z[M], u[M], dy[M];
     load_tokens<T, V, M, kFull>(Column<T, V>(d, b.z, b.ldz, c, p), n, z);
     load_tokens<T, V, M, kFull>(Column<T, V>(d, b.u, b.ldu, c, p), n, u);
     load_tokens<T, V, M, kFull>(Column<T, V>(d, b.dy, b.lddy, c, p), n, dy);
     const Column<T, V> dz(d, b.dz, b.lddz, c, p + n - 1), du(d, b.du, b.lddu, c, p + n - 1);      // the last token first
-    float before[M][V];
+    float less[M][V];
     if (any_shut<T, V, M>(z)) {
-        states_before<T, V, M, true>(z, u, h, before);
+        steps_taken<T, V, M, true>(z, u, h, less);
         forget<T, V, M>(z);
-        retreat_loaded<T, V, M, kFull, true>(z, u, dy, before, dz, du, n, G);
+        retreat_loaded<T, V, M, kFull, true>(z, dy, less, dz, du, n, G);
     } else {
-        states_before<T, V, M, false>(z, u, h, before);
+        steps_taken<T, V, M, false>(z, u, h, less);
         forget<T, V, M>(z);
-        retreat_loaded<T, V, M, kFull, false>(z, u, dy, before, dz, du, n, G);
+        retreat_loaded<T, V, M, kFull, false>(z, dy, less, dz, du, n, G);
     }
 }
 
@@ -410,7 +425,7 @@ __device__ __forceinline__ void backwards(const Shape &d, uint64_t p0, F f)
 
 // In both: the product of the gates of these tokens first, which is 0 or underflows only where one of them is shut or times() mends it.
 template <class T, int V, int M, bool kFull, bool kShutting>
-__device__ __forceinline__ void sum_loaded(const Pack<T, V> (&z)[M], const Pack<T, V> (&u)[M], int n, float (&A)[V], float (&h)[V])
+__device__ __forceinline__ void sum_loaded(const Raw<T, V> (&z)[M], const Raw<T, V> (&u)[M], int n, float (&A)[V], float (&h)[V])
 {
     float product[V];
 #pragma unroll
@@ -420,7 +435,7 @@ __device__ __forceinline__ void sum_loaded(const Pack<T, V> (&z)[M], const Pack<
         if (kFull || k < n) {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const Step s = step_of<kShutting>((float)z[k].v[v], (float)u[k].v[v]);
+                const Step s = step_of<kShutting>(z[k][v], u[k][v]);
                 h[v] = advance<kShutting>(s, h[v]);
                 product[v] = kShutting ? times(product[v], s.a) : product[v] * s.a;
             }
@@ -432,7 +447,7 @@ __device__ __forceinline__ void sum_loaded(const Pack<T, V> (&z)[M], const Pack<
 template <class T, int V, int M, bool kFull>
 __device__ __forceinline__ void sum_tokens(const Shape &d, const Fwd &f, uint32_t c, uint64_t p, int n, float (&A)[V], float (&h)[V])
 {
-    Pack<T, V> z[M], u[M];
+    Raw<T, V> z[M], u[M];
     load_tokens<T, V, M, kFull>(Column<T, V>(d, f.z, f.ldz, c, p), n, z);
     load_tokens<T, V, M, kFull>(Column<T, V>(d, f.u, f.ldu, c, p), n, u);
     if (any_shut<T, V, M>(z)) sum_loaded<T, V, M, kFull, true>(z, u, n, A, h);
@@ -440,7 +455,7 @@ __device__ __forceinline__ void sum_tokens(const Shape &d, const Fwd &f, uint32_
 }
 
 template <class T, int V, int M, bool kFull, bool kShutting>
-__device__ __forceinline__ void sum_gradients_loaded(const Pack<T, V> (&z)[M], const Pack<T, V> (&dy)[M], int n, float (&A)[V], float (&G)[V])
+__device__ __forceinline__ void sum_gradients_loaded(const Raw<T, V> (&z)[M], const Raw<T, V> (&dy)[M], int n, float (&A)[V], float (&G)[V])
 {
     float product[V];
 #pragma unroll
@@ -450,8 +465,8 @@ __device__ __forceinline__ void sum_gradients_loaded(const Pack<T, V> (&z)[M], c
         if (kFull || k < n) {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const Step s = step_of<kShutting>((float)z[k].v[v], 0.0f);
-                G[v] += (float)dy[k].v[v];
+                const Step s = step_of<kShutting>(z[k][v], 0.0f);
+                G[v] += dy[k][v];
                 G[v] = kShutting && s.a == 0.0f ? 0.0f : s.a * G[v];
                 product[v] = kShutting ? times(product[v], s.a) : product[v] * s.a;
             }
@@ -463,7 +478,7 @@ __device__ __forceinline__ void sum_gradients_loaded(const Pack<T, V> (&z)[M], c
 template <class T, int V, int M, bool kFull>
 __device__ __forceinline__ void sum_gradients(const Shape &d, const Bwd &b, uint32_t c, uint64_t p, int n, float (&A)[V], float (&G)[V])
 {
-    Pack<T, V> z[M], dy[M];
+    Raw<T, V> z[M], dy[M];
     load_tokens<T, V, M, kFull>(Column<T, V>(d, b.z, b.ldz, c, p), n, z);
     load_tokens<T, V, M, kFull>(Column<T, V>(d, b.dy, b.lddy, c, p), n, dy);
     if (any_shut<T, V, M>(z)) sum_gradients_loaded<T, V, M, kFull, true>(z, dy, n, A, G);
@@ -816,8 +831,8 @@ tile_fwd_kernel(Shape d, Fwd f, Board board)
     const uint64_t p0 = ((uint64_t)l.tile * l.windows + l.window) * kKeep;
     const bool held = l.active && p0 < d.N;
     const Inside in = held ? inside(d, p0) : Inside{};
-    const uint64_t at = (uint64_t)in.seq * d.W + l.c;
-    Pack<T, V> z[kKeep], u[kKeep];
+    auto at = [&] { return (uint64_t)in.seq * d.W + l.c; };
+    Raw<T, V> z[kKeep], u[kKeep];
     float A[V], h[V];
     bool shutting = false;
 #pragma unroll
@@ -828,7 +843,7 @@ tile_fwd_kernel(Shape d, Fwd f, Board board)
         shutting = any_shut<T, V, kKeep>(z);
         if (shutting) sum_loaded<T, V, kKeep, true, true>(z, u, kKeep, A, h);
         else sum_loaded<T, V, kKeep, true, false>(z, u, kKeep, A, h);
-        if (in.first) begin_with<V>(A, h, f.h0, at);
+        if (in.first) begin_with<V>(A, h, f.h0, at());
     } else if (held)
         forwards(d, p0, [&](uint32_t k, uint64_t p, uint64_t e, uint64_t begin, uint64_t) {
             if (p == begin) {
@@ -838,16 +853,17 @@ tile_fwd_kernel(Shape d, Fwd f, Board board)
             }
             sum_few<T, V>(d, f, l.c, p, e, A, h);
         });
+    forget<T, V, kKeep>(z), forget<T, V, kKeep>(u);
     float state[V];
     come_in<V>(d, board, l, l.window, l.tile, A, h, state);
     if (in.whole) {
-        if (in.first) get<V>(f.h0, at, state);
+        if (in.first) get<V>(f.h0, at(), state);
         put<V>(f.states, p0 / kKeep * d.W + l.c, state);
         const Column<T, V> y(d, f.y, f.ldy, l.c, p0);
         forget<T, V, kKeep>(z);
         if (shutting) advance_loaded<T, V, kKeep, true, true>(z, u, y, kKeep, state);
         else advance_loaded<T, V, kKeep, true, false>(z, u, y, kKeep, state);
-        if (in.last) put<V>(f.h_last, at, state);
+        if (in.last) put<V>(f.h_last, at(), state);
     } else if (held)
         forwards(d, p0, [&](uint32_t k, uint64_t p, uint64_t e, uint64_t begin, uint64_t end) {
             const uint64_t at = (uint64_t)sequence(d, k) * d.W + l.c;
@@ -868,8 +884,8 @@ tile_bwd_kernel(Shape d, Bwd b, Board board)
     const uint64_t p0 = ((uint64_t)l.tile * l.windows + l.window) * kKeep;
     const bool held = l.active && p0 < d.N;
     const Inside in = held ? inside(d, p0) : Inside{};
-    const uint64_t at = (uint64_t)in.seq * d.W + l.c;
-    Pack<T, V> z[kKeep], u[kKeep], dy[kKeep];
+    auto at = [&] { return (uint64_t)in.seq * d.W + l.c; };
+    Raw<T, V> z[kKeep], u[kKeep], dy[kKeep];
     float A[V], G[V];
     bool shutting = false;
 #pragma unroll
@@ -881,7 +897,7 @@ tile_bwd_kernel(Shape d, Bwd b, Board board)
         shutting = any_shut<T, V, kKeep>(z);
         if (shutting) sum_gradients_loaded<T, V, kKeep, true, true>(z, dy, kKeep, A, G);
         else sum_gradients_loaded<T, V, kKeep, true, false>(z, dy, kKeep, A, G);
-        if (in.last) begin_with<V>(A, G, b.dh_last, at);
+        if (in.last) begin_with<V>(A, G, b.dh_last, at());
     } else if (held)
         backwards(d, p0, [&](uint32_t k, uint64_t p, uint64_t e, uint64_t, uint64_t end) {
             if (e == end) {
@@ -891,25 +907,26 @@ tile_bwd_kernel(Shape d, Bwd b, Board board)
             }
             sum_few_gradients<T, V>(d, b, l.c, p, e, A, G);
         });
+    forget<T, V, kKeep>(z), forget<T, V, kKeep>(u), forget<T, V, kKeep>(dy);
     float behind[V];
     come_in<V>(d, board, l, l.windows - 1 - l.window, tile, A, G, behind);
     if (in.whole) {
-        if (in.last) get<V>(b.dh_last, at, behind);
+        if (in.last) get<V>(b.dh_last, at(), behind);
         const Column<T, V> dz(d, b.dz, b.lddz, l.c, p0 + kKeep - 1), du(d, b.du, b.lddu, l.c, p0 + kKeep - 1);
-        float state[V], before[kKeep][V];
-        if (in.first) get<V>(b.h0, at, state);
+        float state[V], less[kKeep][V];
+        if (in.first) get<V>(b.h0, at(), state);
         else get<V>(b.states, p0 / kKeep * d.W + l.c, state);
         forget<T, V, kKeep>(z);
         if (shutting) {
-            states_before<T, V, kKeep, true>(z, u, state, before);
+            steps_taken<T, V, kKeep, true>(z, u, state, less);
             forget<T, V, kKeep>(z);
-            retreat_loaded<T, V, kKeep, true, true>(z, u, dy, before, dz, du, kKeep, behind);
+            retreat_loaded<T, V, kKeep, true, true>(z, dy, less, dz, du, kKeep, behind);
         } else {
-            states_before<T, V, kKeep, false>(z, u, state, before);
+            steps_taken<T, V, kKeep, false>(z, u, state, less);
             forget<T, V, kKeep>(z);
-            retreat_loaded<T, V, kKeep, true, false>(z, u, dy, before, dz, du, kKeep, behind);
+            retreat_loaded<T, V, kKeep, true, false>(z, dy, less, dz, du, kKeep, behind);
         }
-        if (in.first) put<V>(b.dh0, at, behind);
+        if (in.first) put<V>(b.dh0, at(), behind);
     } else if (held)
         backwards(d, p0, [&](uint32_t k, uint64_t p, uint64_t e, uint64_t begin, uint64_t end) {
             const uint32_t seq = sequence(d, k);
