@@ -6,12 +6,12 @@
 // Tokens have a place in the order in which they are gone through: their row, or N - 1 - row back to front.  The forward pass
 // keeps the state before every kKeep-th place in fp32; the backward pass computes the states between them again.
 //
-// Bound by memory: 3 values moved per element forward, 5 backward, for some 13 and 40 operations, two in three of them an exp2 and a
-// reciprocal at a quarter of the rate.  Many sequences: a lane runs through a sequence's tokens, 16 of them on their way at a time.  2^17 rays of
-// 64 samples, 32 channels in fp16: forward 306 us (5.3 TB/s), backward 506 (5.3).  Few long ones: tiles that tell each other what they do to a
-// state; each value is still read once.  One sequence of 2^17 tokens, 256 channels in bf16: forward 69 us (2.9 TB/s), backward 103 (3.3); four of
-// 16 384, 1024 channels: 108 (3.7) and 169 (4.0).  What keeps tiles from 6 TB/s: two workgroups per compute unit load, compute, listen and
-// store in turn, and the gates are computed twice.
+// Bound by memory: 3 values moved per element forward, 5 backward, for some 13 and 40 operations, an exp2 and a reciprocal at a quarter of
+// the rate for each time that a gate is computed.  Many sequences: a lane runs through a sequence's tokens, 16 of them on their way at a
+// time.  2^17 rays of 64 samples, 32 channels in fp16: forward 308 us (5.2 TB/s), backward 503 (5.3).  Few long ones: tiles that tell each
+// other what they do to a state; each value is still read once.  One sequence of 2^17 tokens, 256 channels in bf16: forward 66 us (3.1 TB/s),
+// backward 95 (3.5); four of 16 384, 1024 channels: 105 (3.9) and 157 (4.3).  What keeps tiles from 6 TB/s: two workgroups per compute unit
+// load, compute, listen and store in turn, and the gates are computed twice and three times.
 #include "rows_common.h"
 
 namespace {
@@ -806,8 +806,7 @@ __device__ __forceinline__ void come_in(const Shape &d, const Board &board, cons
     pass<V>(mine, window, tA, h);
 }
 
-// Two workgroups share a compute unit, so that one loads while the other listens: 128 registers per lane.  (With as many as the compiler
-// takes, 139 to 200, the gradient of four sequences of 16 384 tokens, 1024 channels, bf16 takes 215 us instead of 170.)
+// 128 registers per lane at most: two workgroups then share a compute unit, and one loads while the other listens.
 #define TWO_PER_UNIT __attribute__((amdgpu_waves_per_eu(4)))
 
 // A and B of a window that starts from a state of its own
@@ -980,9 +979,9 @@ int check_rows(const char *who, const void *p, uint64_t ld, const Shape &d, uint
 // Whether tiles serve a call.  Sequence by sequence 16 tokens take some 1.6 us forward however few sequences there are; tiles take 8 us
 // and then 3 TB/s with 16-bit values, and longer where many windows hold a sequence's end.  They pay for sequences of more than 120
 // tokens and an 80 000th of all values.  Sequences / tiles in us, forward and backward: 256 sequences of 512 tokens, 64 channels, fp16
-// 51 / 28 and 85 / 32; 64 of 1024, 256 channels 103 / 48 and 196 / 55; 16 of 4096, 2048 channels, bf16 528 / 203 and 832 / 310; 512 of 1024, 128
-// channels 140 / 129 and 230 / 194; 400 of 256, 128 channels 30 / 36 and 56 / 51; 4000 of 400, 64 channels 128 / 193 and 216 / 293; 100 of 400, 32
-// channels, fp32 30 / 12 and 45 / 14; 1000 of 200, 32 channels 21 / 35 and 43 / 46; 1000 of 2000, 64 channels 317 / 339 and 524 / 525;
+// 51 / 25 and 85 / 31; 64 of 1024, 256 channels 103 / 41 and 196 / 55; 16 of 4096, 2048 channels, bf16 528 / 203 and 832 / 290; 512 of 1024, 128
+// channels 140 / 126 and 230 / 180; 400 of 256, 128 channels 30 / 36 and 56 / 51; 4000 of 400, 64 channels 128 / 193 and 216 / 293; 100 of 400, 32
+// channels, fp32 30 / 12 and 45 / 14; 1000 of 200, 32 channels 21 / 35 and 43 / 46; 1000 of 2000, 64 channels 317 / 338 and 524 / 521;
 // 300 of 1500, 512 channels, fp16 339 / 525 and 602 / 605.  V, most: of the call.
 void cut(Shape &d, uint32_t V, uint32_t most)
 {
