@@ -573,3 +573,91 @@ def test_refusals():
             say("not refused", i)
     fwd(), bwd()
     assert not z.any()
+
+
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("n_seq,S,W,dtype", [(2, 20011, 33, "fp32"), (1, 40000, 64, "fp16"), (3, 8192, 66, "bf16")])
+def test_recurrence_of_many_tiles(n_seq, S, W, dtype, reverse):
+    """Long enough for several dozen tiles, in bundles, to tell each other their states."""
+    say("recurrence many tiles", n_seq, S, W, dtype, reverse)
+    rng = np.random.default_rng(S + W)
+    check_recurrence(gates(rng, n_seq * S, W), rng.standard_normal((n_seq * S, W)), n_seq, None, TYPES[dtype], reverse, True)
+
+
+LONG_RAGGED = [[16, 0, 32, 160, 0, 0, 1, 15, 600, 512, 0, 1200], [0, 0, 5, 2000, 16, 16, 0], [1, 4095, 0], [1000, 1001, 999, 1000], [0, 3000]]
+
+
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("lengths", LONG_RAGGED, ids=str)
+def test_recurrence_ragged_in_tiles(lengths, dtype, reverse):
+    """Sequences that begin and end with windows and inside them, several in one, empty ones everywhere."""
+    say("recurrence ragged tiles", lengths, dtype, reverse)
+    first = np.concatenate([[0], np.cumsum(lengths)])
+    rng = np.random.default_rng(sum(lengths))
+    for W, room, carry in ((6, 0, True), (64, 37, False), (130, 0, True)):
+        N = first[-1] + room
+        assert B.dg_recurrence_workspace_bytes(N, len(lengths), W) > 0
+        check_recurrence(gates(rng, N, W), rng.standard_normal((N, W)), len(lengths), first, TYPES[dtype], reverse, carry)
+
+
+def test_recurrence_gives_the_same_bits_each_time():
+    """How far a tile has to look back depends on timing; what it computes must not."""
+    say("recurrence bits")
+    torch.manual_seed(0)
+    n_seq, S, W = 4, 8192, 256
+    z, u, dy = (torch.randn(n_seq * S, W, device=DEV, dtype=torch.float32) for _ in range(3))
+    ws = torch.empty(B.dg_recurrence_workspace_bytes(n_seq * S, n_seq, W), dtype=torch.uint8, device=DEV)
+    states = torch.empty(B.dg_recurrence_state_count(n_seq * S, W), device=DEV)
+    runs = []
+    for _ in range(6):
+        y, dz, du, last = torch.empty_like(z), torch.empty_like(z), torch.empty_like(z), torch.empty(n_seq, W, device=DEV)
+        B.dg_recurrence_fwd(z, u, n_seq, None, False, None, y, last, states, ws)
+        B.dg_recurrence_bwd(z, u, n_seq, None, False, None, states, dy, None, dz, du, None, ws)
+        runs.append((y, last, dz, du))
+    for r in runs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(runs[0], r))
+
+
+def test_calls_in_a_graph():
+    """Captured once, replayed on new inputs, with eager work in between: every replay gives what the calls give."""
+    say("graph")
+    torch.manual_seed(1)
+    n_seq, S, W = 3, 700, 48
+    N = n_seq * S
+    x, dy = torch.empty(N, W, device=DEV), torch.empty(N, W, device=DEV)
+    gamma, beta = torch.randn(W, device=DEV), torch.randn(W, device=DEV)
+    ws_scan = torch.empty(B.dg_recurrence_workspace_bytes(N, n_seq, W), dtype=torch.uint8, device=DEV)
+    ws_norm = torch.empty(B.dg_layer_norm_bwd_workspace_bytes(N, W), dtype=torch.uint8, device=DEV)
+    assert ws_scan.numel() > 0
+    states, h = torch.empty(B.dg_recurrence_state_count(N, W), device=DEV), torch.zeros(n_seq, W, device=DEV)
+
+    def calls():
+        z, m, y, dm, dz, du, dx, dg, db = out
+        B.dg_layer_norm_fwd(x, gamma, beta, 1e-5, z)
+        B.dg_recurrence_fwd(z, x, n_seq, None, False, h, m, None, states, ws_scan)
+        B.dg_dropout_fwd(m, x, 0.2, 9, 0, y)
+        B.dg_dropout_bwd(dy, 0.2, 9, 0, dm)
+        B.dg_recurrence_bwd(z, x, n_seq, None, False, h, states, dm, None, dz, du, None, ws_scan)
+        B.dg_layer_norm_bwd(x, gamma, dz, 1e-5, dx, dg, db, ws_norm)
+
+    out = [torch.zeros(N, W, device=DEV) for _ in range(7)] + [torch.zeros(W, device=DEV) for _ in range(2)]
+    x.normal_(), dy.normal_()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        calls()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for i in range(4):
+        x.normal_(), dy.normal_(), h.normal_()
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = [t.clone() for t in out]
+        for t in out:
+            t.fill_(7.0)
+        calls()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, replayed)), i
