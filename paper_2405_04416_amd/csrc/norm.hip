@@ -6,8 +6,8 @@
 // Both passes are bound by memory: a row is read once into registers (K vectors of V values per lane, G lanes per row) and everything
 // is summed there, deviations from the mean after the mean itself.  The backward pass adds up dgamma and dbeta of the rows that a
 // lane sees in its registers; a workgroup's sums go to the workspace and a second launch folds them.  No atomics: the same bits each time.
-// 2^23 rows of 32 fp16 values: forward 194 us (5.5 TB/s), backward 304 (5.3); 2^16 of 4096 bf16 values: 200 (5.4) and 313 (5.1); 2^20 of 37 fp32
-// values, one by one: 77 (4.0) and 113 (4.1).
+// 2^23 rows of 32 fp16 values: forward 194 us (5.5 TB/s), backward 304 (5.3); 2^16 of 4096 bf16 values: 203 (5.3) and 284 (5.7); 2^20 of 37 fp32
+// values, one by one: 75 (4.1) and 108 (4.3).
 #include <cmath>
 #include "rows_common.h"
 
@@ -76,19 +76,24 @@ __device__ __forceinline__ bool inside(uint32_t W, uint32_t lane, int k, int G, 
     return c < W;
 }
 
-template <class T, int V, int G, int K, bool kStreamed>
+// kAhead: without a branch, so that the compiler can count the loads on their way and does not wait for all of them: the last row again
+// where there is no further one, the last vector again where the row has ended (widen clears it).  8192 rows of 4096 bf16 values, backward:
+// 49.0 us, with branches 55.4; 2^16 rows 280 and 312; 2^17 of 2048 fp32 values 668 and 639.
+template <class T, int V, int G, int K, bool kStreamed, bool kAhead>
 __device__ __forceinline__ void read(const void *p, uint64_t ld, uint64_t row, const Norm &a, uint32_t lane, Pack<T, V> (&out)[K])
 {
+    const T *from = (const T *)p + (!kAhead || row < a.N ? row : a.N - 1) * ld;
     uint32_t c;
 #pragma unroll
-    for (int k = 0; k < K; ++k)
-        if (inside<V>(a.W, lane, k, G, c) && row < a.N) {
-            const T *at = (const T *)p + row * ld + c;
-            if constexpr (kStreamed) out[k] = load_streamed<T, V>(at);
-            else out[k] = *reinterpret_cast<const Pack<T, V> *>(at);
-        } else
+    for (int k = 0; k < K; ++k) {
+        const bool here = inside<V>(a.W, lane, k, G, c) && (kAhead || row < a.N);
+        const T *at = from + (here ? c : a.W - V);
+        if (!kAhead && !here) {
 #pragma unroll
             for (int v = 0; v < V; ++v) out[k].v[v] = (T)0.0f;
+        } else if constexpr (kStreamed) out[k] = load_streamed<T, V>(at);
+        else out[k] = *reinterpret_cast<const Pack<T, V> *>(at);
+    }
 }
 
 template <class T, int V, bool kStreamed>
@@ -101,13 +106,16 @@ __device__ __forceinline__ void write(T *p, const float (&in)[V])
     else *reinterpret_cast<Pack<T, V> *>(p) = a;
 }
 
-template <class T, int V, int K>
-__device__ __forceinline__ void widen(const Pack<T, V> (&in)[K], float (&out)[K][V])
+template <class T, int V, int G, int K, bool kAhead>
+__device__ __forceinline__ void widen(const Pack<T, V> (&in)[K], const Norm &a, uint32_t lane, float (&out)[K][V])
 {
+    uint32_t c;
 #pragma unroll
-    for (int k = 0; k < K; ++k)
+    for (int k = 0; k < K; ++k) {
+        const bool here = !kAhead || inside<V>(a.W, lane, k, G, c);
 #pragma unroll
-        for (int v = 0; v < V; ++v) out[k][v] = (float)in[k].v[v];
+        for (int v = 0; v < V; ++v) out[k][v] = here ? (float)in[k].v[v] : 0.0f;
+    }
 }
 
 // a lane's share of a vector of W values, `none` without one
@@ -138,7 +146,7 @@ __device__ __forceinline__ float mean(const float (&x)[K][V], const Norm &a, flo
 
 // Workgroups go through the rows side by side: workgroup b takes rows b R, b R + 1, ... of every gridDim.x R, R = kThreads / G at a
 // time, with gamma and beta in registers.  Where a row takes more than one vector per lane the next row is on its way while one is worked
-// on (2^16 rows of 4096 bf16 values, backward: 316 us against 523); narrower rows have wavefronts enough (2^20 of 256: 290 without, 322).
+// on (2^16 rows of 4096 bf16 values, backward: 284 us, without 523); narrower rows have wavefronts enough (2^20 of 256: 290 without, 322).
 template <class T, int V, int G, int K, int kThreads, bool kStreamed>
 __global__ void __launch_bounds__(kThreads)
 norm_fwd_kernel(Norm a)
@@ -152,14 +160,14 @@ norm_fwd_kernel(Norm a)
     weights<V, G, K>(a.beta, 0.0f, a, lane, beta);
     uint64_t row = (uint64_t)blockIdx.x * R + threadIdx.x / G;
     Pack<T, V> next[K];
-    if (kAhead) read<T, V, G, K, kStreamed>(a.x, a.ldx, row, a, lane, next);
+    if (kAhead) read<T, V, G, K, kStreamed, kAhead>(a.x, a.ldx, row, a, lane, next);
     for (uint64_t row0 = (uint64_t)blockIdx.x * R; row0 < a.N; row0 += (uint64_t)gridDim.x * R) {
         float x[K][V];
-        if (!kAhead) read<T, V, G, K, kStreamed>(a.x, a.ldx, row, a, lane, next);
-        widen<T, V, K>(next, x);
+        if (!kAhead) read<T, V, G, K, kStreamed, kAhead>(a.x, a.ldx, row, a, lane, next);
+        widen<T, V, G, K, kAhead>(next, a, lane, x);
         const uint64_t now = row;
         row += (uint64_t)gridDim.x * R;
-        if (kAhead) read<T, V, G, K, kStreamed>(a.x, a.ldx, row, a, lane, next);
+        if (kAhead) read<T, V, G, K, kStreamed, kAhead>(a.x, a.ldx, row, a, lane, next);
         const float m = mean<V, G, K, kThreads>(x, a, red);
         float sum[1] = {0.0f};
         uint32_t c;
@@ -195,8 +203,8 @@ norm_bwd_kernel(Norm a)
     uint64_t row = (uint64_t)blockIdx.x * R + threadIdx.x / G;
     Pack<T, V> next_x[K], next_dy[K];
     auto fetch = [&] {
-        read<T, V, G, K, kStreamed>(a.x, a.ldx, row, a, lane, next_x);
-        read<T, V, G, K, kStreamed>(a.dy, a.lddy, row, a, lane, next_dy);
+        read<T, V, G, K, kStreamed, kAhead>(a.x, a.ldx, row, a, lane, next_x);
+        read<T, V, G, K, kStreamed, kAhead>(a.dy, a.lddy, row, a, lane, next_dy);
     };
     if (kAhead) fetch();
     for (uint64_t row0 = (uint64_t)blockIdx.x * R; row0 < a.N; row0 += (uint64_t)gridDim.x * R) {
@@ -204,8 +212,8 @@ norm_bwd_kernel(Norm a)
         T *out = (T *)a.out + row * a.ldo;
         float x[K][V], dy[K][V];
         if (!kAhead) fetch();
-        widen<T, V, K>(next_x, x);
-        widen<T, V, K>(next_dy, dy);
+        widen<T, V, G, K, kAhead>(next_x, a, lane, x);
+        widen<T, V, G, K, kAhead>(next_dy, a, lane, dy);
         row += (uint64_t)gridDim.x * R;
         if (kAhead) fetch();
         const float m = mean<V, G, K, kThreads>(x, a, red1);
@@ -399,7 +407,7 @@ Spread spread_of(uint32_t n, bool small)
 }
 
 // Workgroups of the backward pass.  Each leaves 2 W sums, so that wide rows have fewer, and each has some 6000 values to itself, but all
-// compute units have two, and as many as each other.  (8192 rows of 4096 bf16 values: 512 workgroups 57.7 us, 1024 66.2; 2^23 of 32 fp16
+// compute units have two, and as many as each other.  (8192 rows of 4096 bf16 values: 512 workgroups 50 us, 1024 64; 2^23 of 32 fp16
 // values: 2048 304 us, 1024 323; 200 000 of 32: 2048 19.7 us, 1563 20.2, 1024 15.3, 781 19.3.)
 uint32_t parts_of(uint64_t N, uint32_t W)
 {
