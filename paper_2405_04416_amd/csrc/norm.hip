@@ -7,7 +7,7 @@
 // is summed there, deviations from the mean after the mean itself.  The backward pass adds up dgamma and dbeta of the rows that a
 // lane sees in its registers; a workgroup's sums go to the workspace and a second launch folds them.  No atomics: the same bits each time.
 // 2^23 rows of 32 fp16 values: forward 194 us (5.5 TB/s), backward 304 (5.3); 2^16 of 4096 bf16 values: 203 (5.3) and 284 (5.7); 2^20 of 37 fp32
-// values, one by one: 75 (4.1) and 108 (4.3).
+// values, unaligned: 58 (5.3) and 106 (4.4).
 #include <cmath>
 #include "rows_common.h"
 
@@ -68,7 +68,7 @@ struct Norm {
     float eps, per_W;               // 1 / W
 };
 
-// V values of vector k of a lane's share of a row; 0 where the row has ended
+// Vector k of a lane's share of a row, from value c on; false where the row has ended
 template <int V>
 __device__ __forceinline__ bool inside(uint32_t W, uint32_t lane, int k, int G, uint32_t &c)
 {
@@ -76,10 +76,30 @@ __device__ __forceinline__ bool inside(uint32_t W, uint32_t lane, int k, int G, 
     return c < W;
 }
 
-// kAhead: without a branch, so that the compiler can count the loads on their way and does not wait for all of them: the last row again
-// where there is no further one, the last vector again where the row has ended (widen clears it).  8192 rows of 4096 bf16 values, backward:
-// 49.0 us, with branches 55.4; 2^16 rows 280 and 312; 2^17 of 2048 fp32 values 668 and 639.
-template <class T, int V, int G, int K, bool kStreamed, bool kAhead>
+// kLoose: rows that no vector divides.  The row's last vector begins early enough to end with it; the first `skipped` of its values are
+// the last but one's too: both compute them with the same operations, bit by bit, and store them; sums take them once.
+template <int V, bool kLoose>
+__device__ __forceinline__ uint32_t begin_of(uint32_t W, uint32_t c)
+{
+    return kLoose && c + V > W ? W - V : c;
+}
+
+template <int V, bool kLoose>
+__device__ __forceinline__ int skipped(uint32_t W, uint32_t c)
+{
+    return kLoose && c < W ? (int)(c - begin_of<V, kLoose>(W, c)) : 0;
+}
+
+// 16 bytes that lie as their values do
+template <class T>
+struct loose { typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(2))); };
+template <>
+struct loose<float> { typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(4))); };
+
+// kAhead: without a branch, so that the compiler can count the loads on their way and does not wait for all of them: the call's last
+// row again where there is no further one, the last vector again where the row has ended (widen clears it).  8192 rows of 4096 bf16 values, backward: 50.0 us, with
+// branches 55.4; 2^16 rows 284 and 313; 2^17 of 2048 fp32 values 664 and 639.
+template <class T, int V, int G, int K, bool kStreamed, bool kLoose, bool kAhead>
 __device__ __forceinline__ void read(const void *p, uint64_t ld, uint64_t row, const Norm &a, uint32_t lane, Pack<T, V> (&out)[K])
 {
     const T *from = (const T *)p + (!kAhead || row < a.N ? row : a.N - 1) * ld;
@@ -87,22 +107,24 @@ __device__ __forceinline__ void read(const void *p, uint64_t ld, uint64_t row, c
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const bool here = inside<V>(a.W, lane, k, G, c) && (kAhead || row < a.N);
-        const T *at = from + (here ? c : a.W - V);
+        const T *at = from + (here ? begin_of<V, kLoose>(a.W, c) : a.W - V);
         if (!kAhead && !here) {
 #pragma unroll
             for (int v = 0; v < V; ++v) out[k].v[v] = (T)0.0f;
         } else if constexpr (kStreamed) out[k] = load_streamed<T, V>(at);
+        else if constexpr (kLoose) out[k] = __builtin_bit_cast(Pack<T, V>, *reinterpret_cast<const typename loose<T>::u4 *>(at));
         else out[k] = *reinterpret_cast<const Pack<T, V> *>(at);
     }
 }
 
-template <class T, int V, bool kStreamed>
+template <class T, int V, bool kStreamed, bool kLoose>
 __device__ __forceinline__ void write(T *p, const float (&in)[V])
 {
     Pack<T, V> a;
 #pragma unroll
     for (int v = 0; v < V; ++v) a.v[v] = (T)in[v];
     if constexpr (kStreamed) store_streamed<T, V>(p, a);
+    else if constexpr (kLoose) *reinterpret_cast<typename loose<T>::u4 *>(p) = __builtin_bit_cast(typename loose<T>::u4, a);
     else *reinterpret_cast<Pack<T, V> *>(p) = a;
 }
 
@@ -118,28 +140,42 @@ __device__ __forceinline__ void widen(const Pack<T, V> (&in)[K], const Norm &a, 
     }
 }
 
-// a lane's share of a vector of W values, `none` without one
-template <int V, int G, int K>
+// a lane's share of a vector of W values, `none` without one; four at a time, which only lie as fp32 values do
+template <int V, int G, int K, bool kLoose>
 __device__ __forceinline__ void weights(const float *p, float none, const Norm &a, uint32_t lane, float (&out)[K][V])
 {
+    constexpr int n = V % 4 == 0 ? 4 : 1;
     uint32_t c;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const bool in = inside<V>(a.W, lane, k, G, c) && p;
+        const float *at = p + begin_of<V, kLoose>(a.W, c);
 #pragma unroll
-        for (int v = 0; v < V; ++v) out[k][v] = in ? p[c + v] : none;
+        for (int v = 0; v < V; v += n) {
+            Pack<float, n> w;
+#pragma unroll
+            for (float &each : w.v) each = none;
+            if (in) {
+                if constexpr (n == 4) w = __builtin_bit_cast(Pack<float, n>, *reinterpret_cast<const loose<float>::u4 *>(at + v));
+                else w.v[0] = at[v];
+            }
+#pragma unroll
+            for (int i = 0; i < n; ++i) out[k][v + i] = w.v[i];
+        }
     }
 }
 
 // mean of a row in registers
-template <int V, int G, int K, int kThreads>
-__device__ __forceinline__ float mean(const float (&x)[K][V], const Norm &a, float (*red)[1])
+template <int V, int G, int K, int kThreads, bool kLoose>
+__device__ __forceinline__ float mean(const float (&x)[K][V], const Norm &a, uint32_t lane, float (*red)[1])
 {
     float sum[1] = {0.0f};
 #pragma unroll
-    for (int k = 0; k < K; ++k)
+    for (int k = 0; k < K; ++k) {
+        const int from = skipped<V, kLoose>(a.W, (k * G + lane) * V);
 #pragma unroll
-        for (int v = 0; v < V; ++v) sum[0] += x[k][v];
+        for (int v = 0; v < V; ++v) sum[0] += kLoose && v < from ? 0.0f : x[k][v];
+    }
     row_sums<G, kThreads, 1>(sum, red);
     return sum[0] * a.per_W;
 }
@@ -147,7 +183,7 @@ __device__ __forceinline__ float mean(const float (&x)[K][V], const Norm &a, flo
 // Workgroups go through the rows side by side: workgroup b takes rows b R, b R + 1, ... of every gridDim.x R, R = kThreads / G at a
 // time, with gamma and beta in registers.  Where a row takes more than one vector per lane the next row is on its way while one is worked
 // on (2^16 rows of 4096 bf16 values, backward: 284 us, without 523); narrower rows have wavefronts enough (2^20 of 256: 290 without, 322).
-template <class T, int V, int G, int K, int kThreads, bool kStreamed>
+template <class T, int V, int G, int K, int kThreads, bool kStreamed, bool kLoose>
 __global__ void __launch_bounds__(kThreads)
 norm_fwd_kernel(Norm a)
 {
@@ -156,26 +192,28 @@ norm_fwd_kernel(Norm a)
     __shared__ float red[kThreads / dg::kWave][1], red2[kThreads / dg::kWave][1];
     const uint32_t lane = threadIdx.x % G;
     float gamma[K][V], beta[K][V];
-    weights<V, G, K>(a.gamma, 1.0f, a, lane, gamma);
-    weights<V, G, K>(a.beta, 0.0f, a, lane, beta);
+    weights<V, G, K, kLoose>(a.gamma, 1.0f, a, lane, gamma);
+    weights<V, G, K, kLoose>(a.beta, 0.0f, a, lane, beta);
     uint64_t row = (uint64_t)blockIdx.x * R + threadIdx.x / G;
     Pack<T, V> next[K];
-    if (kAhead) read<T, V, G, K, kStreamed, kAhead>(a.x, a.ldx, row, a, lane, next);
+    if (kAhead) read<T, V, G, K, kStreamed, kLoose, kAhead>(a.x, a.ldx, row, a, lane, next);
     for (uint64_t row0 = (uint64_t)blockIdx.x * R; row0 < a.N; row0 += (uint64_t)gridDim.x * R) {
         float x[K][V];
-        if (!kAhead) read<T, V, G, K, kStreamed, kAhead>(a.x, a.ldx, row, a, lane, next);
+        if (!kAhead) read<T, V, G, K, kStreamed, kLoose, kAhead>(a.x, a.ldx, row, a, lane, next);
         widen<T, V, G, K, kAhead>(next, a, lane, x);
         const uint64_t now = row;
         row += (uint64_t)gridDim.x * R;
-        if (kAhead) read<T, V, G, K, kStreamed, kAhead>(a.x, a.ldx, row, a, lane, next);
-        const float m = mean<V, G, K, kThreads>(x, a, red);
+        if (kAhead) read<T, V, G, K, kStreamed, kLoose, kAhead>(a.x, a.ldx, row, a, lane, next);
+        const float m = mean<V, G, K, kThreads, kLoose>(x, a, lane, red);
         float sum[1] = {0.0f};
         uint32_t c;
 #pragma unroll
         for (int k = 0; k < K; ++k)
-            if (inside<V>(a.W, lane, k, G, c))
+            if (inside<V>(a.W, lane, k, G, c)) {
+                const int from = skipped<V, kLoose>(a.W, c);
 #pragma unroll
-                for (int v = 0; v < V; ++v) { x[k][v] -= m; sum[0] += x[k][v] * x[k][v]; }
+                for (int v = 0; v < V; ++v) { x[k][v] -= m; sum[0] += kLoose && v < from ? 0.0f : x[k][v] * x[k][v]; }
+            }
         row_sums<G, kThreads, 1>(sum, red2);
         const float s = 1.0f / sqrtf(sum[0] * a.per_W + a.eps);
         T *y = (T *)a.out + now * a.ldo;
@@ -183,13 +221,13 @@ norm_fwd_kernel(Norm a)
         for (int k = 0; k < K; ++k)
             if (inside<V>(a.W, lane, k, G, c) && now < a.N) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) x[k][v] = x[k][v] * s * gamma[k][v] + beta[k][v];
-                write<T, V, kStreamed>(y + c, x[k]);
+                for (int v = 0; v < V; ++v) x[k][v] = fmaf(x[k][v] * s, gamma[k][v], beta[k][v]);
+                write<T, V, kStreamed, kLoose>(y + begin_of<V, kLoose>(a.W, c), x[k]);
             }
     }
 }
 
-template <class T, int V, int G, int K, int kThreads, bool kStreamed>
+template <class T, int V, int G, int K, int kThreads, bool kStreamed, bool kLoose>
 __global__ void __launch_bounds__(kThreads)
 norm_bwd_kernel(Norm a)
 {
@@ -198,13 +236,13 @@ norm_bwd_kernel(Norm a)
     __shared__ float red1[kWaves][1], red3[kWaves][3];
     const uint32_t lane = threadIdx.x % G;
     float gamma[K][V], sum_g[K][V] = {}, sum_b[K][V] = {};
-    weights<V, G, K>(a.gamma, 1.0f, a, lane, gamma);
+    weights<V, G, K, kLoose>(a.gamma, 1.0f, a, lane, gamma);
     uint32_t c;
     uint64_t row = (uint64_t)blockIdx.x * R + threadIdx.x / G;
     Pack<T, V> next_x[K], next_dy[K];
     auto fetch = [&] {
-        read<T, V, G, K, kStreamed, kAhead>(a.x, a.ldx, row, a, lane, next_x);
-        read<T, V, G, K, kStreamed, kAhead>(a.dy, a.lddy, row, a, lane, next_dy);
+        read<T, V, G, K, kStreamed, kLoose, kAhead>(a.x, a.ldx, row, a, lane, next_x);
+        read<T, V, G, K, kStreamed, kLoose, kAhead>(a.dy, a.lddy, row, a, lane, next_dy);
     };
     if (kAhead) fetch();
     for (uint64_t row0 = (uint64_t)blockIdx.x * R; row0 < a.N; row0 += (uint64_t)gridDim.x * R) {
@@ -216,19 +254,22 @@ norm_bwd_kernel(Norm a)
         widen<T, V, G, K, kAhead>(next_dy, a, lane, dy);
         row += (uint64_t)gridDim.x * R;
         if (kAhead) fetch();
-        const float m = mean<V, G, K, kThreads>(x, a, red1);
+        const float m = mean<V, G, K, kThreads, kLoose>(x, a, lane, red1);
         float sum[3] = {0.0f, 0.0f, 0.0f};          // of squared deviations, of g, of g times the deviation
 #pragma unroll
         for (int k = 0; k < K; ++k)
-            if (inside<V>(a.W, lane, k, G, c))
+            if (inside<V>(a.W, lane, k, G, c)) {
+                const int from = skipped<V, kLoose>(a.W, c);
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
                     x[k][v] -= m;
+                    if (kLoose && v < from) continue;
                     sum[0] += x[k][v] * x[k][v];
                     const float g = dy[k][v] * gamma[k][v];
                     sum[1] += g;
                     sum[2] += g * x[k][v];
                 }
+            }
         row_sums<G, kThreads, 3>(sum, red3);
         const float s = 1.0f / sqrtf(sum[0] * a.per_W + a.eps), mean_g = sum[1] * a.per_W, mean_gx = sum[2] * a.per_W * s;
 #pragma unroll
@@ -237,13 +278,13 @@ norm_bwd_kernel(Norm a)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const float xh = x[k][v] * s;
-                o[v] = s * (dy[k][v] * gamma[k][v] - mean_g - xh * mean_gx);
+                o[v] = s * fmaf(-xh, mean_gx, fmaf(dy[k][v], gamma[k][v], -mean_g));
                 if (held) {
                     sum_g[k][v] += dy[k][v] * xh;
                     sum_b[k][v] += dy[k][v];
                 }
             }
-            if (inside<V>(a.W, lane, k, G, c) && held && a.out) write<T, V, kStreamed>(out + c, o);
+            if (inside<V>(a.W, lane, k, G, c) && held && a.out) write<T, V, kStreamed, kLoose>(out + begin_of<V, kLoose>(a.W, c), o);
         }
     }
     if (!a.part) return;
@@ -254,9 +295,12 @@ norm_bwd_kernel(Norm a)
     for (int k = 0; k < K; ++k) {
         const bool in = inside<V>(a.W, lane, k, G, c);
         if (G >= kThreads) {
-            if (in)
+            if (in) {
+                float *to = part + begin_of<V, kLoose>(a.W, c);
 #pragma unroll
-                for (int v = 0; v < V; ++v) { part[c + v] = sum_g[k][v]; part[a.W + c + v] = sum_b[k][v]; }
+                for (int v = 0; v < V; ++v)
+                    if (!kLoose || v >= skipped<V, kLoose>(a.W, c)) { to[v] = sum_g[k][v]; to[a.W + v] = sum_b[k][v]; }
+            }
             continue;
         }
 #pragma unroll
@@ -275,10 +319,10 @@ norm_bwd_kernel(Norm a)
             }
         __syncthreads();
         for (uint32_t i = threadIdx.x; i < 2 * G * V; i += kThreads) {
-            const uint32_t which = i / (G * V), j = i % (G * V), col = k * G * V + j;
+            const uint32_t which = i / (G * V), j = i % (G * V), begin = k * G * V + j / V * V, col = begin_of<V, kLoose>(a.W, begin) + j % V;
             float t = 0.0f;
             for (int w = 0; w < kWaves; ++w) t += sums[w][which][j];
-            if (col < a.W) part[which * a.W + col] = t;
+            if (begin < a.W && (!kLoose || (int)(j % V) >= skipped<V, kLoose>(a.W, begin))) part[which * a.W + col] = t;
         }
     }
 }
@@ -380,18 +424,18 @@ int check_rows(const char *who, const void *p, uint64_t ld, uint32_t W, uint32_t
     return DG_OK;
 }
 
-// How a row of n vectors is spread.  Vectors of 16 bytes: up to 64 over as many lanes, rounded up to a power of two; several per lane
-// would leave fewer lanes idle, but a load then takes parts of many lines, which loads past the caches fetch again (48 bf16 values a row,
-// two lanes of three vectors: 1.9 TB/s forward, eight lanes 5.5).  Smaller vectors, where sums across lanes weigh more: up to 4 in a lane
-// with as few idle places as possible (37 fp32 values, 16 lanes of three: 4.0 TB/s, 64 lanes 2.2).  Then a workgroup with up to 8.
+// How a row of n vectors is spread: up to 64 over as many lanes, rounded up to a power of two; several per lane would leave fewer lanes
+// idle, but a load then takes parts of many lines, which loads past the caches fetch again (48 bf16 values a row, two lanes of three
+// vectors: 1.9 TB/s forward, eight lanes 5.5).  Then a wavefront with up to 4 each, then a workgroup with up to 8.  Single values: up to 4 in
+// a lane with as few idle places as possible (2^20 rows of 6 fp16 values, two lanes of three: 9.6 us forward, eight lanes 16).
 struct Spread { int G, K; };
 
-Spread spread_of(uint32_t n, bool small)
+Spread spread_of(uint32_t n, bool single)
 {
     Spread best = {0, 0};
-    if (small)
+    if (single)
         for (int K : {4, 3, 1})
-            for (int G = 1; G <= 64; G *= 2)
+            for (int G = 1; G <= 8; G *= 2)
                 if ((uint32_t)(G * K) >= n) {
                     if (best.G == 0 || G * K < best.G * best.K) best = {G, K};
                     break;
@@ -425,61 +469,75 @@ struct Call {
     hipStream_t st;
 };
 
-template <class T, int V, int G, int K>
+template <class T, int V, int G, int K, bool kLoose>
 void launch_spread(const Call &c)
 {
     const uint64_t all = (c.a.N + kBlock / G - 1) / (kBlock / G);
     const uint32_t grid = c.forward ? (uint32_t)(all < kMostBlocks ? all : kMostBlocks) : c.parts;
     auto go = [&](auto kernel) { kernel<<<grid, kBlock, 0, c.st>>>(c.a); };
-    if constexpr (V * sizeof(T) == 16)
+    if constexpr (V * sizeof(T) == 16 && !kLoose)
         if (c.a.N * c.a.W * sizeof(T) >= kStreamedBytes)
-            return c.forward ? go(norm_fwd_kernel<T, V, G, K, kBlock, true>) : go(norm_bwd_kernel<T, V, G, K, kBlock, true>);
-    c.forward ? go(norm_fwd_kernel<T, V, G, K, kBlock, false>) : go(norm_bwd_kernel<T, V, G, K, kBlock, false>);
+            return c.forward ? go(norm_fwd_kernel<T, V, G, K, kBlock, true, false>) : go(norm_bwd_kernel<T, V, G, K, kBlock, true, false>);
+    c.forward ? go(norm_fwd_kernel<T, V, G, K, kBlock, false, kLoose>) : go(norm_bwd_kernel<T, V, G, K, kBlock, false, kLoose>);
 }
 
-template <class T, int V, int G>
+template <class T, int V, int G, bool kLoose>
 void launch_lanes(const Call &c, int K)
 {
-    if constexpr (V * sizeof(T) < 16) {
-        if (K == 4) return launch_spread<T, V, G, 4>(c);
-        if (K == 3) return launch_spread<T, V, G, 3>(c);
+    if constexpr (V == 1) {
+        if (K == 4) return launch_spread<T, V, G, 4, kLoose>(c);
+        if (K == 3) return launch_spread<T, V, G, 3, kLoose>(c);
     }
-    launch_spread<T, V, G, 1>(c);
+    launch_spread<T, V, G, 1, kLoose>(c);
 }
 
-template <class T, int V>
+template <class T, int V, bool kLoose>
 void launch_rows(const Call &c)
 {
-    const Spread s = spread_of(c.a.W / V, V * sizeof(T) < 16);
+    const Spread s = spread_of((c.a.W + V - 1) / V, V == 1);
     switch (s.G) {
-    case 1: return launch_lanes<T, V, 1>(c, s.K);
-    case 2: return launch_lanes<T, V, 2>(c, s.K);
-    case 4: return launch_lanes<T, V, 4>(c, s.K);
-    case 8: return launch_lanes<T, V, 8>(c, s.K);
-    case 16: return launch_lanes<T, V, 16>(c, s.K);
-    case 32: return launch_lanes<T, V, 32>(c, s.K);
-    case 64:
-        return s.K == 1   ? launch_spread<T, V, 64, 1>(c)
-               : s.K == 2 ? launch_spread<T, V, 64, 2>(c)
-               : s.K == 3 ? launch_spread<T, V, 64, 3>(c)
-                          : launch_spread<T, V, 64, 4>(c);
-    case 256: return s.K == 2 ? launch_spread<T, V, 256, 2>(c) : s.K == 4 ? launch_spread<T, V, 256, 4>(c) : launch_spread<T, V, 256, 8>(c);
+    case 1: return launch_lanes<T, V, 1, kLoose>(c, s.K);
+    case 2: return launch_lanes<T, V, 2, kLoose>(c, s.K);
+    case 4: return launch_lanes<T, V, 4, kLoose>(c, s.K);
+    case 8: return launch_lanes<T, V, 8, kLoose>(c, s.K);
     }
+    if constexpr (V > 1)                            // one by one: rows of less than 8 values
+        switch (s.G) {
+        case 16: return launch_spread<T, V, 16, 1, kLoose>(c);
+        case 32: return launch_spread<T, V, 32, 1, kLoose>(c);
+        case 64:
+            return s.K == 1   ? launch_spread<T, V, 64, 1, kLoose>(c)
+                   : s.K == 2 ? launch_spread<T, V, 64, 2, kLoose>(c)
+                   : s.K == 3 ? launch_spread<T, V, 64, 3, kLoose>(c)
+                              : launch_spread<T, V, 64, 4, kLoose>(c);
+        case 256:
+            return s.K == 2 ? launch_spread<T, V, 256, 2, kLoose>(c) : s.K == 4 ? launch_spread<T, V, 256, 4, kLoose>(c) : launch_spread<T, V, 256, 8, kLoose>(c);
+        }
     if (c.forward) norm_fwd_wide_kernel<T><<<(uint32_t)c.a.N, kWide, 0, c.st>>>(c.a);
     else norm_bwd_wide_kernel<T><<<c.parts, kWide, 0, c.st>>>(c.a);
 }
 
-// the widest vectors that every row allows
+// Vectors of 16 bytes, whether they are aligned and divide a row or not; rows of less than one value by value.  Unaligned vectors / single
+// values in us, forward and backward: 2^20 rows of 37 fp32 values 58 / 76 and 106 / 113; 8192 of 4095 44 / 105 and 89 / 283; 2^18 of 999 bf16
+// values 218 / 246 and 324 / 437; 8192 of 4095 33 / 92 and 62 / 243; 2^22 of 33 fp16 values 133 / 187 and 246 / 272; 2^21 of 100, eight bytes at a
+// time, 182 / 210 and 312 / 278.
+template <class T>
 void launch(const Call &c)
 {
+    constexpr int V = 16 / sizeof(T);
     const Norm &a = c.a;
-    auto allowed = [&](uint32_t bytes) {
-        return a.W * item_bytes(c.dtype) % bytes == 0 && rows_aligned(a.x, a.ldx, c.dtype, bytes) && (c.forward || rows_aligned(a.dy, a.lddy, c.dtype, bytes)) &&
-               (!a.out || rows_aligned(a.out, a.ldo, c.dtype, bytes));
-    };
-    if (c.dtype == DG_F32) allowed(16) ? launch_rows<float, 4>(c) : launch_rows<float, 1>(c);
-    else if (c.dtype == DG_F16) allowed(16) ? launch_rows<f16, 8>(c) : allowed(8) ? launch_rows<f16, 4>(c) : launch_rows<f16, 1>(c);
-    else allowed(16) ? launch_rows<bf16, 8>(c) : allowed(8) ? launch_rows<bf16, 4>(c) : launch_rows<bf16, 1>(c);
+    const bool aligned = a.W % V == 0 && rows_aligned(a.x, a.ldx, c.dtype, 16) && (c.forward || rows_aligned(a.dy, a.lddy, c.dtype, 16)) &&
+                         (!a.out || rows_aligned(a.out, a.ldo, c.dtype, 16));
+    if (aligned) launch_rows<T, V, false>(c);
+    else if (a.W >= V) launch_rows<T, V, true>(c);
+    else launch_rows<T, 1, false>(c);
+}
+
+void launch(const Call &c)
+{
+    if (c.dtype == DG_F32) launch<float>(c);
+    else if (c.dtype == DG_F16) launch<f16>(c);
+    else launch<bf16>(c);
 }
 
 }  // namespace
