@@ -601,6 +601,16 @@ def test_recurrence_ragged_in_tiles(lengths, dtype, reverse):
         check_recurrence(gates(rng, N, W), rng.standard_normal((N, W)), len(lengths), first, TYPES[dtype], reverse, carry)
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("N,W,pad,shift", [(200, 3, 0, 0), (90, 6, 1, 0), (70, 7, 0, 1), (70, 9, 0, 0), (31, 15, 2, 1), (50, 17, 0, 3), (33, 63, 1, 1), (20, 65, 0, 0),
+                                           (9, 255, 0, 0), (600, 257, 1, 2), (5, 511, 3, 0), (9, 777, 0, 0), (7, 1023, 0, 1), (6, 1537, 0, 0), (5, 2047, 1, 1),
+                                           (3, 2049, 0, 0), (700, 4095, 0, 0), (3, 8189, 0, 0), (2, 16381, 0, 0)])
+def test_norm_rows_that_no_vector_divides(N, W, pad, shift, dtype):
+    """The last vector of a row overlaps the one before it: values count once, and nothing outside the row is written."""
+    say("norm loose", N, W, pad, shift, dtype)
+    check_norm(np.random.default_rng(N + W).standard_normal((N, W)) * 1.5 + 0.5, TYPES[dtype], pad=pad, shift=shift)
+
+
 def test_recurrence_gives_the_same_bits_each_time():
     """How far a tile has to look back depends on timing; what it computes must not."""
     say("recurrence bits")
