@@ -12,6 +12,7 @@
 // other what they do to a state; each value is still read once.  One sequence of 2^17 tokens, 256 channels in bf16: forward 66 us (3.1 TB/s),
 // backward 95 (3.5); four of 16 384, 1024 channels: 105 (3.9) and 157 (4.3).  What keeps tiles from 6 TB/s: two workgroups per compute unit
 // load, compute, listen and store in turn, and the gates are computed twice and three times.
+#include <type_traits>
 #include "rows_common.h"
 
 namespace {
@@ -25,7 +26,7 @@ constexpr float kLog2e = 1.44269504f;
 
 struct Gate { float a, c; };
 
-// both sides of an open gate to full relative precision
+// Both sides of an open gate.  The argument of exp2 is rounded, so that the smaller one is off by some |z| + 3 half units of its own.
 __device__ __forceinline__ Gate gate(float z)
 {
     const float e = __builtin_amdgcn_exp2f(z * -kLog2e), a = __builtin_amdgcn_rcpf(1.0f + e);
@@ -99,12 +100,70 @@ __device__ __forceinline__ float advance(const Step &s, float h)
     return kShutting && s.a == 0.0f ? s.b : fmaf(s.a, h, s.b);
 }
 
-// A stretch of tokens takes the state h to join(A, h, B), A the product of its gates.  The product is 0 only if a gate is, and kLeast where it
-// would be less, so that a state that is infinite or NaN gets through a long stretch as it does token by token; to a finite state that adds
-// less than 2^-126 of itself.
-__device__ __forceinline__ float join(float A, float h, float B) { return A == 0.0f ? B : fmaf(A, h, B); }
+// the gradient before a token from the one behind it
+template <bool kShutting>
+__device__ __forceinline__ float retreat(const Step &s, float G)
+{
+    return kShutting && s.a == 0.0f ? 0.0f : s.a * G;
+}
 
-__device__ __forceinline__ float times(float A, float a) { return a == 0.0f ? 0.0f : fmaxf(A * a, A == 0.0f ? 0.0f : kLeast); }
+// `a` is rounded: near 1 it and its c do not quite add up to 1, and what a state gains or loses by that adds up over the 1 / c tokens that it
+// lives.  Over kKeep tokens that is 16 half units at most; a longer chain is written with the smaller share alone, as the value of
+// the larger share plus the smaller share of the difference.  2^17 tokens with constant gates of z = 8 / 10 / 12: off by 2.4e-6 / 1.8e-6 / 2.0e-6 of the
+// state, with a h + c u throughout by 5.5e-4 / 2.4e-3 / 5.3e-3.  The difference from a state that is infinite would make it NaN; where the end of
+// some tokens shows that this may have happened they are gone through once more, kCareful, looking at each.  Finite states are the same both ways.
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.40282347e38f; }
+
+template <bool kCareful>
+__device__ __forceinline__ float advance_far(float z, float u, float h)
+{
+    const Gate g = gate(z);
+    const bool more = z > 0.0f;
+    const float next = fmaf(more ? g.c : -g.a, u - h, more ? h : u);
+    if (!kCareful) return next;
+    return fabsf(z) < kShut && finite(next) ? next : advance<true>(step_of<true>(z, u), h);
+}
+
+template <bool kCareful>
+__device__ __forceinline__ float retreat_far(float z, float G)
+{
+    const Gate g = gate(z);
+    const bool more = z > 0.0f;
+    const float next = fmaf(more ? -g.c : g.a, G, more ? G : 0.0f);
+    if (!kCareful) return next;
+    return fabsf(z) < kShut && finite(next) ? next : retreat<true>(step_of<true>(z, 0.0f), G);
+}
+
+// What a stretch of tokens does to the state h before it: A h + B, A the product of its gates and D = 1 - A.  D is summed as what each token
+// takes of h, so that it is precise where it is small.  x = code(A, D) is the smaller one of them, A as it is and D with its sign changed, -0 for a stretch that
+// only holds.  x is +0 only if a gate of the stretch is 0, and A kLeast where it would be less, so that a state that is infinite or NaN gets
+// through a long stretch as it does token by token; to a finite state that adds less than 2^-126 of itself.
+__device__ __forceinline__ float code(float A, float D) { return A <= 0.5f ? A : -D; }
+
+// A of x, rounded
+__device__ __forceinline__ float share(float x) { return (int)__float_as_uint(x) < 0 ? 1.0f + x : x; }
+
+// A h, as precise as x is, and B
+__device__ __forceinline__ float join_finite(float x, float A, float h, float B) { return fmaf(x, h, B) + (A == x ? 0.0f : h); }
+
+__device__ __forceinline__ bool anew(float x) { return __float_as_uint(x) == 0; }
+
+__device__ __forceinline__ float join(float x, float h, float B)
+{
+    if (anew(x)) return B;
+    const float A = share(x), next = join_finite(x, A, h, B);
+    return finite(next) ? next : fmaf(A, h, B);
+}
+
+__device__ __forceinline__ float clamped(float A, bool zero) { return zero ? 0.0f : fmaxf(A, kLeast); }
+
+// A and D with one more token.  Not kShutting: A is yet to be clamped.
+template <bool kShutting>
+__device__ __forceinline__ void extend(const Step &s, float &A, float &D)
+{
+    D = fmaf(s.c, A, D);
+    A = kShutting ? clamped(A * s.a, A == 0.0f || s.a == 0.0f) : A * s.a;
+}
 
 struct Shape {
     uint64_t N;
@@ -224,28 +283,56 @@ __device__ __forceinline__ void in_pieces(uint64_t p, uint64_t end, F f)
     }
 }
 
-template <class T, int V, int M, bool kFull, bool kShutting>
+// kFar: the tokens are some of a longer chain
+template <class T, int V, int M, bool kFull, bool kShutting, bool kFar>
 __device__ __forceinline__ void advance_loaded(const Raw<T, V> (&z)[M], const Raw<T, V> (&u)[M], Column<T, V> y, int n, float (&h)[V])
 {
 #pragma unroll
     for (int k = 0; k < M; ++k)
         if (kFull || k < n) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) h[v] = advance<kShutting>(step_of<kShutting>(z[k][v], u[k][v]), h[v]);
+            for (int v = 0; v < V; ++v)
+                h[v] = kFar ? advance_far<kShutting>(z[k][v], u[k][v], h[v]) : advance<kShutting>(step_of<kShutting>(z[k][v], u[k][v]), h[v]);
             store<T, V>(y.at, h);
             y.at += y.step;
         }
 }
 
-template <class T, int V, int M, bool kFull>
+// f(careful, state) from `state` on: without care first, unless `careful` asks for it at once
+template <int V, class F>
+__device__ __forceinline__ void with_care(bool careful, float (&state)[V], F f)
+{
+    if (!careful) {
+        float to[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) to[v] = state[v];
+        f(std::false_type(), to);
+        bool good = true;
+#pragma unroll
+        for (int v = 0; v < V; ++v) good = good && finite(to[v]);
+        careful = __any(!good);
+        if (!careful)
+#pragma unroll
+            for (int v = 0; v < V; ++v) state[v] = to[v];
+    }
+    if (careful) f(std::true_type(), state);
+}
+
+template <class T, int V, int M, bool kFull, bool kFar>
 __device__ __forceinline__ void advance_tokens(const Shape &d, const Fwd &f, uint32_t c, uint64_t p, int n, float (&h)[V])
 {
     Raw<T, V> z[M], u[M];
     load_tokens<T, V, M, kFull>(Column<T, V>(d, f.z, f.ldz, c, p), n, z);
     load_tokens<T, V, M, kFull>(Column<T, V>(d, f.u, f.ldu, c, p), n, u);
     const Column<T, V> y(d, f.y, f.ldy, c, p);
-    if (any_shut<T, V, M>(z)) advance_loaded<T, V, M, kFull, true>(z, u, y, n, h);
-    else advance_loaded<T, V, M, kFull, false>(z, u, y, n, h);
+    const bool shutting = any_shut<T, V, M>(z);
+    if (kFar)
+        with_care<V>(shutting, h, [&](auto careful, float (&to)[V]) {
+            if (careful) forget<T, V, M>(z), forget<T, V, M>(u);
+            advance_loaded<T, V, M, kFull, careful.value, true>(z, u, y, n, to);
+        });
+    else if (shutting) advance_loaded<T, V, M, kFull, true, false>(z, u, y, n, h);
+    else advance_loaded<T, V, M, kFull, false, false>(z, u, y, n, h);
 }
 
 // y of places [p, end) of a sequence from the state before them, and the states that are kept
@@ -254,9 +341,9 @@ __device__ __forceinline__ void advance_places(const Shape &d, const Fwd &f, uin
 {
     in_pieces(p, end, [&](uint64_t q, int n) {
         if (q % kKeep == 0) put<V>(f.states, q / kKeep * d.W + c, h);
-        if (n == kKeep) advance_tokens<T, V, kKeep, true>(d, f, c, q, n, h);
-        else if (n == 1) advance_tokens<T, V, 1, true>(d, f, c, q, n, h);
-        else advance_tokens<T, V, kKeep, false>(d, f, c, q, n, h);
+        if (n == kKeep) advance_tokens<T, V, kKeep, true, true>(d, f, c, q, n, h);
+        else if (n == 1) advance_tokens<T, V, 1, true, true>(d, f, c, q, n, h);
+        else advance_tokens<T, V, kKeep, false, true>(d, f, c, q, n, h);
     });
 }
 
@@ -276,7 +363,7 @@ __device__ __forceinline__ void steps_taken(const Raw<T, V> (&z)[M], const Raw<T
 
 // The gradients of loaded tokens, last first.  The gates are computed again: keeping a, c and a c (h_{t-1} - u) from the way forwards costs
 // 96 registers where this takes 48, and half of the wavefronts.
-template <class T, int V, int M, bool kFull, bool kShutting>
+template <class T, int V, int M, bool kFull, bool kShutting, bool kFar>
 __device__ __forceinline__ void retreat_loaded(const Raw<T, V> (&z)[M], const Raw<T, V> (&dy)[M], const float (&less)[M][V], Column<T, V> dz,
                                                Column<T, V> du, int n, float (&G)[V])
 {
@@ -289,7 +376,7 @@ __device__ __forceinline__ void retreat_loaded(const Raw<T, V> (&z)[M], const Ra
                 const Step s = step_of<kShutting>(z[k][v], 0.0f);
                 G[v] += dy[k][v];
                 ou[v] = kShutting && s.c == 0.0f ? 0.0f : s.c * G[v];
-                G[v] = kShutting && s.a == 0.0f ? 0.0f : s.a * G[v];
+                G[v] = kFar ? retreat_far<kShutting>(z[k][v], G[v]) : retreat<kShutting>(s, G[v]);
                 oz[v] = kShutting && (s.c == 0.0f || s.a == 0.0f) ? 0.0f : s.c * less[k][v] * G[v];
             }
             store<T, V>(dz.at, oz);
@@ -299,7 +386,7 @@ __device__ __forceinline__ void retreat_loaded(const Raw<T, V> (&z)[M], const Ra
         }
 }
 
-template <class T, int V, int M, bool kFull>
+template <class T, int V, int M, bool kFull, bool kFar>
 __device__ __forceinline__ void retreat_tokens(const Shape &d, const Bwd &b, uint32_t c, uint64_t p, int n, float (&h)[V], float (&G)[V])
 {
     Raw<T, V> z[M], u[M], dy[M];
@@ -308,15 +395,17 @@ __device__ __forceinline__ void retreat_tokens(const Shape &d, const Bwd &b, uin
     load_tokens<T, V, M, kFull>(Column<T, V>(d, b.dy, b.lddy, c, p), n, dy);
     const Column<T, V> dz(d, b.dz, b.lddz, c, p + n - 1), du(d, b.du, b.lddu, c, p + n - 1);      // the last token first
     float less[M][V];
-    if (any_shut<T, V, M>(z)) {
-        steps_taken<T, V, M, true>(z, u, h, less);
-        forget<T, V, M>(z);
-        retreat_loaded<T, V, M, kFull, true>(z, dy, less, dz, du, n, G);
-    } else {
-        steps_taken<T, V, M, false>(z, u, h, less);
-        forget<T, V, M>(z);
-        retreat_loaded<T, V, M, kFull, false>(z, dy, less, dz, du, n, G);
-    }
+    const bool shutting = any_shut<T, V, M>(z);
+    if (shutting) steps_taken<T, V, M, true>(z, u, h, less);
+    else steps_taken<T, V, M, false>(z, u, h, less);
+    forget<T, V, M>(z);
+    if (kFar)
+        with_care<V>(shutting, G, [&](auto careful, float (&to)[V]) {
+            if (careful) forget<T, V, M>(z), forget<T, V, M>(dy);
+            retreat_loaded<T, V, M, kFull, careful.value, true>(z, dy, less, dz, du, n, to);
+        });
+    else if (shutting) retreat_loaded<T, V, M, kFull, true, false>(z, dy, less, dz, du, n, G);
+    else retreat_loaded<T, V, M, kFull, false, false>(z, dy, less, dz, du, n, G);
 }
 
 // dz and du of places [p, end) of the sequence that begins at place `begin`, from the gradient G behind them
@@ -329,9 +418,9 @@ __device__ __forceinline__ void retreat_places(const Shape &d, const Bwd &b, uin
         float h[V];
         if (q == begin) get<V>(b.h0, (uint64_t)seq * d.W + c, h);
         else get<V>(b.states, keep * d.W + c, h);
-        if (n == kKeep) retreat_tokens<T, V, kKeep, true>(d, b, c, q, n, h, G);
-        else if (n == 1) retreat_tokens<T, V, 1, true>(d, b, c, q, n, h, G);
-        else retreat_tokens<T, V, kKeep, false>(d, b, c, q, n, h, G);
+        if (n == kKeep) retreat_tokens<T, V, kKeep, true, true>(d, b, c, q, n, h, G);
+        else if (n == 1) retreat_tokens<T, V, 1, true, true>(d, b, c, q, n, h, G);
+        else retreat_tokens<T, V, kKeep, false, true>(d, b, c, q, n, h, G);
         end = q;
     }
 }
@@ -379,11 +468,11 @@ sequence_bwd_kernel(Shape d, Bwd b)
 
 // ------------------------------------------------------------------ long sequences
 //
-// A stretch of tokens takes the state before it to join(A, state, B).  A lane has a window of kKeep places and V channels, whose tokens
+// A stretch of tokens takes the state before it to join(x, state, B).  A lane has a window of kKeep places and V channels, whose tokens
 // it keeps in registers: what they need from memory is read once.  A workgroup has a tile, as many windows one behind the other as
-// fit it, for channels that fill the 128 bytes of a line.  It finds A and B of its tile, tells the tiles behind it in a slot of its own,
+// fit it, for channels that fill the 128 bytes of a line.  It finds x and B of its tile, tells the tiles behind it in a slot of its own,
 // joins what those before it have told, and lets its windows run from there, joined in LDS.  A stretch that knows the state behind itself
-// tells it as (0, state); where a sequence begins A is 0 anyway.
+// tells it as (+0, state); where a sequence begins x is +0 anyway.
 //
 // Tiles are numbered as workgroups start.  A tile waits only for ones with a lower number, which run or have run, and tell what they do
 // before they wait for a state: every wait ends.  A slot is one 64-bit word written at once, so nothing else has to be ordered.
@@ -423,13 +512,12 @@ __device__ __forceinline__ void backwards(const Shape &d, uint64_t p0, F f)
     }
 }
 
-// In both: the product of the gates of these tokens first, which is 0 or underflows only where one of them is shut or times() mends it.
 template <class T, int V, int M, bool kFull, bool kShutting>
-__device__ __forceinline__ void sum_loaded(const Raw<T, V> (&z)[M], const Raw<T, V> (&u)[M], int n, float (&A)[V], float (&h)[V])
+__device__ __forceinline__ void sum_loaded(const Raw<T, V> (&z)[M], const Raw<T, V> (&u)[M], int n, float (&A)[V], float (&D)[V], float (&h)[V])
 {
-    float product[V];
+    bool zero[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) product[v] = 1.0f;
+    for (int v = 0; v < V; ++v) zero[v] = A[v] == 0.0f;
 #pragma unroll
     for (int k = 0; k < M; ++k)
         if (kFull || k < n) {
@@ -437,52 +525,51 @@ __device__ __forceinline__ void sum_loaded(const Raw<T, V> (&z)[M], const Raw<T,
             for (int v = 0; v < V; ++v) {
                 const Step s = step_of<kShutting>(z[k][v], u[k][v]);
                 h[v] = advance<kShutting>(s, h[v]);
-                product[v] = kShutting ? times(product[v], s.a) : product[v] * s.a;
+                extend<kShutting>(s, A[v], D[v]);
             }
         }
 #pragma unroll
-    for (int v = 0; v < V; ++v) A[v] = times(A[v], kShutting ? product[v] : fmaxf(product[v], kLeast));
+    for (int v = 0; v < V && !kShutting; ++v) A[v] = clamped(A[v], zero[v]);
 }
 
 template <class T, int V, int M, bool kFull>
-__device__ __forceinline__ void sum_tokens(const Shape &d, const Fwd &f, uint32_t c, uint64_t p, int n, float (&A)[V], float (&h)[V])
+__device__ __forceinline__ void sum_tokens(const Shape &d, const Fwd &f, uint32_t c, uint64_t p, int n, float (&A)[V], float (&D)[V], float (&h)[V])
 {
     Raw<T, V> z[M], u[M];
     load_tokens<T, V, M, kFull>(Column<T, V>(d, f.z, f.ldz, c, p), n, z);
     load_tokens<T, V, M, kFull>(Column<T, V>(d, f.u, f.ldu, c, p), n, u);
-    if (any_shut<T, V, M>(z)) sum_loaded<T, V, M, kFull, true>(z, u, n, A, h);
-    else sum_loaded<T, V, M, kFull, false>(z, u, n, A, h);
+    if (any_shut<T, V, M>(z)) sum_loaded<T, V, M, kFull, true>(z, u, n, A, D, h);
+    else sum_loaded<T, V, M, kFull, false>(z, u, n, A, D, h);
 }
 
 template <class T, int V, int M, bool kFull, bool kShutting>
-__device__ __forceinline__ void sum_gradients_loaded(const Raw<T, V> (&z)[M], const Raw<T, V> (&dy)[M], int n, float (&A)[V], float (&G)[V])
+__device__ __forceinline__ void sum_gradients_loaded(const Raw<T, V> (&z)[M], const Raw<T, V> (&dy)[M], int n, float (&A)[V], float (&D)[V], float (&G)[V])
 {
-    float product[V];
+    bool zero[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) product[v] = 1.0f;
+    for (int v = 0; v < V; ++v) zero[v] = A[v] == 0.0f;
 #pragma unroll
     for (int k = M - 1; k >= 0; --k)
         if (kFull || k < n) {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const Step s = step_of<kShutting>(z[k][v], 0.0f);
-                G[v] += dy[k][v];
-                G[v] = kShutting && s.a == 0.0f ? 0.0f : s.a * G[v];
-                product[v] = kShutting ? times(product[v], s.a) : product[v] * s.a;
+                G[v] = retreat<kShutting>(s, G[v] + dy[k][v]);
+                extend<kShutting>(s, A[v], D[v]);
             }
         }
 #pragma unroll
-    for (int v = 0; v < V; ++v) A[v] = times(A[v], kShutting ? product[v] : fmaxf(product[v], kLeast));
+    for (int v = 0; v < V && !kShutting; ++v) A[v] = clamped(A[v], zero[v]);
 }
 
 template <class T, int V, int M, bool kFull>
-__device__ __forceinline__ void sum_gradients(const Shape &d, const Bwd &b, uint32_t c, uint64_t p, int n, float (&A)[V], float (&G)[V])
+__device__ __forceinline__ void sum_gradients(const Shape &d, const Bwd &b, uint32_t c, uint64_t p, int n, float (&A)[V], float (&D)[V], float (&G)[V])
 {
     Raw<T, V> z[M], dy[M];
     load_tokens<T, V, M, kFull>(Column<T, V>(d, b.z, b.ldz, c, p), n, z);
     load_tokens<T, V, M, kFull>(Column<T, V>(d, b.dy, b.lddy, c, p), n, dy);
-    if (any_shut<T, V, M>(z)) sum_gradients_loaded<T, V, M, kFull, true>(z, dy, n, A, G);
-    else sum_gradients_loaded<T, V, M, kFull, false>(z, dy, n, A, G);
+    if (any_shut<T, V, M>(z)) sum_gradients_loaded<T, V, M, kFull, true>(z, dy, n, A, D, G);
+    else sum_gradients_loaded<T, V, M, kFull, false>(z, dy, n, A, D, G);
 }
 
 constexpr int kTile = 512;          // lanes of a workgroup
@@ -513,24 +600,24 @@ __device__ __forceinline__ void advance_few(const Shape &d, const Fwd &f, uint32
 {
     if (p < end && p % kKeep == 0) put<V>(f.states, p / kKeep * d.W + c, h);
 #pragma unroll 1
-    for (; p < end; p += kFew) advance_tokens<T, V, kFew, false>(d, f, c, p, end - p < kFew ? (int)(end - p) : kFew, h);
+    for (; p < end; p += kFew) advance_tokens<T, V, kFew, false, false>(d, f, c, p, end - p < kFew ? (int)(end - p) : kFew, h);
 }
 
 template <class T, int V>
-__device__ __forceinline__ void sum_few(const Shape &d, const Fwd &f, uint32_t c, uint64_t p, uint64_t end, float (&A)[V], float (&h)[V])
+__device__ __forceinline__ void sum_few(const Shape &d, const Fwd &f, uint32_t c, uint64_t p, uint64_t end, float (&A)[V], float (&D)[V], float (&h)[V])
 {
 #pragma unroll 1
-    for (; p < end; p += kFew) sum_tokens<T, V, kFew, false>(d, f, c, p, end - p < kFew ? (int)(end - p) : kFew, A, h);
+    for (; p < end; p += kFew) sum_tokens<T, V, kFew, false>(d, f, c, p, end - p < kFew ? (int)(end - p) : kFew, A, D, h);
 }
 
 template <class T, int V>
-__device__ __forceinline__ void sum_few_gradients(const Shape &d, const Bwd &b, uint32_t c, uint64_t p, uint64_t end, float (&A)[V], float (&G)[V])
+__device__ __forceinline__ void sum_few_gradients(const Shape &d, const Bwd &b, uint32_t c, uint64_t p, uint64_t end, float (&A)[V], float (&D)[V], float (&G)[V])
 {
 #pragma unroll 1
     while (end > p) {
         const int n = end - p < kFew ? (int)(end - p) : kFew;
         end -= n;
-        sum_gradients<T, V, kFew, false>(d, b, c, end, n, A, G);
+        sum_gradients<T, V, kFew, false>(d, b, c, end, n, A, D, G);
     }
 }
 
@@ -542,15 +629,15 @@ __device__ __forceinline__ void retreat_few(const Shape &d, const Bwd &b, uint32
     while (end > p) {
         const int n = end - p < kFew ? (int)(end - p) : kFew;
         end -= n;
-        float h[V], A[V];
+        float h[V], A[V], D[V];
         if (p == begin) get<V>(b.h0, (uint64_t)seq * d.W + c, h);
         else get<V>(b.states, p / kKeep * d.W + c, h);
         Fwd f;
         f.z = b.z, f.u = b.u, f.ldz = b.ldz, f.ldu = b.ldu;
 #pragma unroll
-        for (int v = 0; v < V; ++v) A[v] = 1.0f;
-        sum_few<T, V>(d, f, c, p, end, A, h);
-        retreat_tokens<T, V, kFew, false>(d, b, c, end, n, h, G);
+        for (int v = 0; v < V; ++v) A[v] = 1.0f, D[v] = 0.0f;
+        sum_few<T, V>(d, f, c, p, end, A, D, h);
+        retreat_tokens<T, V, kFew, false, false>(d, b, c, end, n, h, G);
     }
 }
 
@@ -570,14 +657,14 @@ struct Lane {
     }
 };
 
-// What the tiles share: the number of workgroups that have started, and slots with A in the lower half and B in the upper one, for each
+// What the tiles share: the number of workgroups that have started, and slots with x in the lower half and B in the upper one, for each
 // channel of each tile and of each kBundle tiles that follow each other.
 struct Board {
     uint32_t *started;
     uint64_t *slots, *bundles;      // [n_tiles, W], [bundles_of(n_tiles), W]
 };
 
-constexpr uint64_t kEmpty = ~0ull;  // A would be a NaN that no computation gives
+constexpr uint64_t kEmpty = ~0ull;  // x would be a NaN that is not told
 constexpr uint32_t kMostPolls = 1u << 20;      // of a lane, a second or so: then it takes NaN for what it has not heard
 
 __device__ __forceinline__ uint32_t start(const Board &b)
@@ -591,16 +678,16 @@ __device__ __forceinline__ uint32_t start(const Board &b)
 __device__ __forceinline__ uint32_t told_bits(float x) { return x != x ? 0x7fc00000u : __float_as_uint(x); }
 
 template <int V>
-__device__ __forceinline__ void tell(uint64_t *slot, const float (&A)[V], const float (&B)[V])
+__device__ __forceinline__ void tell(uint64_t *slot, const float (&x)[V], const float (&B)[V])
 {
 #pragma unroll
     for (int v = 0; v < V; ++v)
-        __hip_atomic_store(slot + v, (uint64_t)told_bits(B[v]) << 32 | told_bits(A[v]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(slot + v, (uint64_t)told_bits(B[v]) << 32 | told_bits(x[v]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 // waits for the first `count` of n slots, step words apart, to be written
 template <int V, int n>
-__device__ __forceinline__ void hear(const uint64_t *slot, int64_t step, uint32_t count, uint32_t &polls, float (&A)[n][V], float (&B)[n][V])
+__device__ __forceinline__ void hear(const uint64_t *slot, int64_t step, uint32_t count, uint32_t &polls, float (&x)[n][V], float (&B)[n][V])
 {
     uint64_t word[n][V];
     for (;;) {
@@ -621,7 +708,7 @@ __device__ __forceinline__ void hear(const uint64_t *slot, int64_t step, uint32_
 #pragma unroll
     for (int i = 0; i < n; ++i)
 #pragma unroll
-        for (int v = 0; v < V; ++v) A[i][v] = __uint_as_float((uint32_t)word[i][v]), B[i][v] = __uint_as_float((uint32_t)(word[i][v] >> 32));
+        for (int v = 0; v < V; ++v) x[i][v] = __uint_as_float((uint32_t)word[i][v]), B[i][v] = __uint_as_float((uint32_t)(word[i][v] >> 32));
 }
 
 // The sequence that a window from place p0 on lies in, and whether it begins or ends with the window.
@@ -644,64 +731,55 @@ __device__ __forceinline__ Inside inside(const Shape &d, uint64_t p0)
     return in;
 }
 
-template <int V>
-using Pairs = float[2][kTile * V];
-
-template <int V>
-__device__ __forceinline__ void lay_down(Pairs<V> &all, const Lane &l, uint32_t at, const float (&A)[V], const float (&B)[V])
-{
+// x, A and B of the windows of a tile, or the tiles of a bundle, of at most kTile lanes
+template <int V, int n>
+struct Stretches {
+    float x[n][V], A[n][V], B[n][V];
+    __device__ __forceinline__ void put(uint32_t at, const float (&xs)[V], const float (&Bs)[V])
+    {
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        all[0][(at * l.across + l.lane) * V + v] = A[v];
-        all[1][(at * l.across + l.lane) * V + v] = B[v];
+        for (int v = 0; v < V; ++v) x[at][v] = xs[v], A[at][v] = share(xs[v]), B[at][v] = Bs[v];
     }
-}
+};
 
-template <int V>
-__device__ __forceinline__ void pick_up(const Pairs<V> &all, const Lane &l, uint32_t at, float (&A)[V], float (&B)[V])
+// h through n stretches, one every `step` places from `at` on.  As fast as can be first, then with care where that could matter: a state that is not
+// finite stays so on the fast way, even past an A of 0.  kFar: they may be more than kKeep (as few lose no more than the tokens of a window).  kAll: x receives that
+// of all of them.  (D of the whole is right where it is needed: where A is more than 1/2, and with it that of every stretch.)
+template <int V, bool kFar, bool kAll, int n_all>
+__device__ __forceinline__ void pass(uint32_t n, const Stretches<V, n_all> &all, uint32_t at, uint32_t step, float (&h)[V], float (&x)[V])
 {
+    float from[V], A[V], D[V], least[V];
+    bool good = true;
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        A[v] = all[0][(at * l.across + l.lane) * V + v];
-        B[v] = all[1][(at * l.across + l.lane) * V + v];
-    }
-}
-
-// h through n stretches one after the other, load(w, a, b) gives A and B of stretch w; A: the product of theirs with it.  As fast as can be
-// first, then with care where that could matter: a state that is not finite stays so on the fast way, even past an A of 0.
-template <int V, class Load>
-__device__ __forceinline__ void pass(uint32_t n, Load load, float (&A)[V], float (&h)[V])
-{
-    float from[V], product[V], least[V];
-    bool finite = true;
-#pragma unroll
-    for (int v = 0; v < V; ++v) from[v] = h[v], product[v] = least[v] = A[v];
+    for (int v = 0; v < V; ++v) from[v] = h[v], A[v] = least[v] = 1.0f, D[v] = 0.0f;
 #pragma unroll 4
     for (uint32_t w = 0; w < n; ++w) {
-        float a[V], b[V];
-        load(w, a, b);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            h[v] = fmaf(a[v], h[v], b[v]);
-            product[v] *= a[v];
-            least[v] = fminf(least[v], a[v]);
+            const float ax = all.x[at + w * step][v], a = all.A[at + w * step][v], b = all.B[at + w * step][v];
+            h[v] = kFar ? join_finite(ax, a, h[v], b) : fmaf(a, h[v], b);
+            if (kAll) {
+                D[v] = fmaf(-ax, A[v], D[v]);
+                A[v] = kFar ? join_finite(ax, a, A[v], 0.0f) : A[v] * a;
+                least[v] = fminf(least[v], a);
+            }
         }
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        A[v] = least[v] == 0.0f ? 0.0f : fmaxf(product[v], kLeast);
-        finite = finite && fabsf(h[v]) <= 3.40282347e38f;
+        if (kAll) x[v] = code(clamped(A[v], least[v] == 0.0f), D[v]);
+        good = good && finite(h[v]);
     }
-    if (finite) return;
+    if (good) return;
 #pragma unroll
     for (int v = 0; v < V; ++v) h[v] = from[v];
 #pragma unroll 1
-    for (uint32_t w = 0; w < n; ++w) {
-        float a[V], b[V];
-        load(w, a, b);
+    for (uint32_t w = 0; w < n; ++w)
 #pragma unroll
-        for (int v = 0; v < V; ++v) h[v] = join(a[v], h[v], b[v]);
-    }
+        for (int v = 0; v < V; ++v) {
+            const float a = all.A[at + w * step][v], b = all.B[at + w * step][v];
+            h[v] = a == 0.0f ? b : fmaf(a, h[v], b);
+        }
 }
 
 // The state before a bundle: from the nearest of the kNear bundles before it that knows the state behind itself, through the ones in
@@ -713,8 +791,8 @@ __device__ __forceinline__ void before_bundle(const Shape &d, const Board &board
 #pragma unroll
     for (int v = 0; v < V; ++v) h[v] = 0.0f;
     while (n) {
-        float A[kNear][V], B[kNear][V];
-        hear<V, kNear>(board.bundles + (uint64_t)(bundle - 1) * d.W + c, -(int64_t)d.W, n, polls, A, B);
+        float x[kNear][V], B[kNear][V];
+        hear<V, kNear>(board.bundles + (uint64_t)(bundle - 1) * d.W + c, -(int64_t)d.W, n, polls, x, B);
         bool known = true;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -722,8 +800,8 @@ __device__ __forceinline__ void before_bundle(const Shape &d, const Board &board
 #pragma unroll
             for (int i = kNear - 1; i >= 0; --i)
                 if ((uint32_t)i < n) {
-                    h[v] = join(A[i][v], met ? h[v] : 0.0f, B[i][v]);
-                    met = met || A[i][v] == 0.0f;
+                    h[v] = join(x[i][v], met ? h[v] : 0.0f, B[i][v]);
+                    met = met || anew(x[i][v]);
                 }
             known = known && met;
         }
@@ -736,90 +814,90 @@ __device__ __forceinline__ void before_bundle(const Shape &d, const Board &board
         for (int v = 0; v < V; ++v) h[v] = __uint_as_float(0x7fc00000u);
 }
 
-// From A and B of a lane's window the state before it (backward: the gradient behind it).  All lanes of the workgroup call it.
+// From x and B of a lane's window the state before it (backward: the gradient behind it).  All lanes of the workgroup call it.
 // mine: the place of the lane's window among those of the tile in the order in which states pass them; tile: likewise.
 //
 // A tile listens to those before it in its bundle; the last of a bundle tells what the whole bundle does, and, when it knows it, the
-// state behind it.  Whoever computes the state behind a bundle computes join(A, the state before it, B): how far back the nearest bundle
+// state behind it.  Whoever computes the state behind a bundle computes join(x, the state before it, B): how far back the nearest bundle
 // lies that knows its own depends on timing, the result does not.
 template <int V>
-__device__ __forceinline__ void come_in(const Shape &d, const Board &board, const Lane &l, uint32_t mine, uint32_t tile, const float (&A)[V],
+__device__ __forceinline__ void come_in(const Shape &d, const Board &board, const Lane &l, uint32_t mine, uint32_t tile, const float (&x)[V],
                                         const float (&B)[V], float (&h)[V])
 {
-    __shared__ Pairs<V> own;
-    __shared__ float heard[2][kBundle][dg::kWave * V], in[dg::kWave * V];
+    __shared__ Stretches<V, kTile> windows;
+    __shared__ Stretches<V, kBundle * dg::kWave> tiles;
+    __shared__ float in[dg::kWave][V];
     uint32_t polls = kMostPolls;
-    auto window = [&](uint32_t w, float (&a)[V], float (&b)[V]) { pick_up<V>(own, l, w, a, b); };
-    auto neighbour = [&](uint32_t w, float (&a)[V], float (&b)[V]) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) a[v] = heard[0][w][l.lane * V + v], b[v] = heard[1][w][l.lane * V + v];
+    float unused[V];
+    auto through_windows = [&](auto all, uint32_t n, float (&to)[V], float (&of_all)[V]) {
+        if (l.windows > kKeep) pass<V, true, all.value>(n, windows, l.lane, l.across, to, of_all);      // narrow rows
+        else pass<V, false, all.value>(n, windows, l.lane, l.across, to, of_all);
     };
-    lay_down<V>(own, l, mine, A, B);
+    windows.put(mine * l.across + l.lane, x, B);
     __syncthreads();
     const uint32_t bundle = tile / kBundle, place = tile % kBundle;
-    float tA[V] = {}, tB[V] = {};
     if (mine == 0) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) tA[v] = 1.0f, tB[v] = 0.0f;
-        pass<V>(l.windows, window, tA, tB);
-        if (l.active) tell<V>(board.slots + (uint64_t)tile * d.W + l.c, tA, tB);
+        float tx[V], tB[V] = {};
+        through_windows(std::true_type(), l.windows, tB, tx);
+        if (l.active) tell<V>(board.slots + (uint64_t)tile * d.W + l.c, tx, tB);
+        tiles.put(place * dg::kWave + l.lane, tx, tB);
     }
     if (l.active)
         for (uint32_t w = mine; w < place; w += l.windows) {
-            float a[1][V], b[1][V];
-            hear<V, 1>(board.slots + (uint64_t)(tile - place + w) * d.W + l.c, 0, 1, polls, a, b);
-#pragma unroll
-            for (int v = 0; v < V; ++v) heard[0][w][l.lane * V + v] = a[0][v], heard[1][w][l.lane * V + v] = b[0][v];
+            float tx[1][V], tB[1][V];
+            hear<V, 1>(board.slots + (uint64_t)(tile - place + w) * d.W + l.c, 0, 1, polls, tx, tB);
+            tiles.put(w * dg::kWave + l.lane, tx[0], tB[0]);
         }
     __syncthreads();
     if (mine == 0 && l.active) {
         uint64_t *told = board.bundles + (uint64_t)bundle * d.W + l.c;
-        float bA[V], bB[V];
+        float bx[V] = {}, bB[V] = {}, state[V];
         if (place == kBundle - 1) {
+            pass<V, false, true>(kBundle, tiles, l.lane, dg::kWave, bB, bx);
 #pragma unroll
-            for (int v = 0; v < V; ++v) bA[v] = 1.0f, bB[v] = 0.0f;
-            pass<V>(place, neighbour, bA, bB);
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                bB[v] = join(tA[v], bB[v], tB[v]);
-                bA[v] = bundle == 0 ? 0.0f : times(bA[v], tA[v]);       // nothing comes before the first
-            }
-            tell<V>(told, bA, bB);
+            for (int v = 0; v < V; ++v) bx[v] = bundle == 0 ? 0.0f : bx[v];      // nothing comes before the first
+            tell<V>(told, bx, bB);
         }
-        float state[V];
         before_bundle<V>(d, board, bundle, l.c, polls, state);
-        if (place == kBundle - 1) {
+        if (place == kBundle - 1 && bundle) {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                bB[v] = join(bA[v], state[v], bB[v]);
-                bA[v] = 0.0f;
+                bB[v] = join(bx[v], state[v], bB[v]);
+                bx[v] = 0.0f;
             }
-            if (bundle) tell<V>(told, bA, bB);
+            tell<V>(told, bx, bB);
         }
-        pass<V>(place, neighbour, tA, state);
+        pass<V, false, false>(place, tiles, l.lane, dg::kWave, state, unused);
 #pragma unroll
-        for (int v = 0; v < V; ++v) in[l.lane * V + v] = state[v];
+        for (int v = 0; v < V; ++v) in[l.lane][v] = state[v];
     }
     __syncthreads();
 #pragma unroll
-    for (int v = 0; v < V; ++v) h[v] = in[l.lane * V + v];
-    pass<V>(mine, window, tA, h);
+    for (int v = 0; v < V; ++v) h[v] = in[l.lane][v];
+    through_windows(std::false_type(), mine, h, unused);
 }
 
 // 128 registers per lane at most: two workgroups then share a compute unit, and one loads while the other listens.
 #define TWO_PER_UNIT __attribute__((amdgpu_waves_per_eu(4)))
 
-// A and B of a window that starts from a state of its own
+// x and B of a window that starts from a state of its own
 template <int V>
-__device__ __forceinline__ void begin_with(float (&A)[V], float (&B)[V], const float *states, uint64_t at)
+__device__ __forceinline__ void begin_with(float (&x)[V], float (&B)[V], const float *states, uint64_t at)
 {
     float from[V];
     get<V>(states, at, from);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        B[v] = join(A[v], from[v], B[v]);
-        A[v] = 0.0f;
+        B[v] = join(x[v], from[v], B[v]);
+        x[v] = 0.0f;
     }
+}
+
+template <int V>
+__device__ __forceinline__ void code(const float (&A)[V], const float (&D)[V], float (&x)[V])
+{
+#pragma unroll
+    for (int v = 0; v < V; ++v) x[v] = code(A[v], D[v]);
 }
 
 template <class T, int V>
@@ -832,17 +910,16 @@ tile_fwd_kernel(Shape d, Fwd f, Board board)
     const Inside in = held ? inside(d, p0) : Inside{};
     auto at = [&] { return (uint64_t)in.seq * d.W + l.c; };
     Raw<T, V> z[kKeep], u[kKeep];
-    float A[V], h[V];
+    float A[V], D[V], h[V], x[V];
     bool shutting = false;
 #pragma unroll
-    for (int v = 0; v < V; ++v) A[v] = 1.0f, h[v] = 0.0f;
+    for (int v = 0; v < V; ++v) A[v] = 1.0f, D[v] = 0.0f, h[v] = 0.0f;
     if (in.whole) {
         load_tokens<T, V, kKeep, true>(Column<T, V>(d, f.z, f.ldz, l.c, p0), kKeep, z);
         load_tokens<T, V, kKeep, true>(Column<T, V>(d, f.u, f.ldu, l.c, p0), kKeep, u);
         shutting = any_shut<T, V, kKeep>(z);
-        if (shutting) sum_loaded<T, V, kKeep, true, true>(z, u, kKeep, A, h);
-        else sum_loaded<T, V, kKeep, true, false>(z, u, kKeep, A, h);
-        if (in.first) begin_with<V>(A, h, f.h0, at());
+        if (shutting) sum_loaded<T, V, kKeep, true, true>(z, u, kKeep, A, D, h);
+        else sum_loaded<T, V, kKeep, true, false>(z, u, kKeep, A, D, h);
     } else if (held)
         forwards(d, p0, [&](uint32_t k, uint64_t p, uint64_t e, uint64_t begin, uint64_t) {
             if (p == begin) {
@@ -850,18 +927,20 @@ tile_fwd_kernel(Shape d, Fwd f, Board board)
                 for (int v = 0; v < V; ++v) A[v] = 0.0f;
                 get<V>(f.h0, (uint64_t)sequence(d, k) * d.W + l.c, h);
             }
-            sum_few<T, V>(d, f, l.c, p, e, A, h);
+            sum_few<T, V>(d, f, l.c, p, e, A, D, h);
         });
+    code<V>(A, D, x);
+    if (in.whole && in.first) begin_with<V>(x, h, f.h0, at());
     forget<T, V, kKeep>(z), forget<T, V, kKeep>(u);
     float state[V];
-    come_in<V>(d, board, l, l.window, l.tile, A, h, state);
+    come_in<V>(d, board, l, l.window, l.tile, x, h, state);
     if (in.whole) {
         if (in.first) get<V>(f.h0, at(), state);
         put<V>(f.states, p0 / kKeep * d.W + l.c, state);
         const Column<T, V> y(d, f.y, f.ldy, l.c, p0);
         forget<T, V, kKeep>(z);
-        if (shutting) advance_loaded<T, V, kKeep, true, true>(z, u, y, kKeep, state);
-        else advance_loaded<T, V, kKeep, true, false>(z, u, y, kKeep, state);
+        if (shutting) advance_loaded<T, V, kKeep, true, true, false>(z, u, y, kKeep, state);
+        else advance_loaded<T, V, kKeep, true, false, false>(z, u, y, kKeep, state);
         if (in.last) put<V>(f.h_last, at(), state);
     } else if (held)
         forwards(d, p0, [&](uint32_t k, uint64_t p, uint64_t e, uint64_t begin, uint64_t end) {
@@ -885,18 +964,17 @@ tile_bwd_kernel(Shape d, Bwd b, Board board)
     const Inside in = held ? inside(d, p0) : Inside{};
     auto at = [&] { return (uint64_t)in.seq * d.W + l.c; };
     Raw<T, V> z[kKeep], u[kKeep], dy[kKeep];
-    float A[V], G[V];
+    float A[V], D[V], G[V], x[V];
     bool shutting = false;
 #pragma unroll
-    for (int v = 0; v < V; ++v) A[v] = 1.0f, G[v] = 0.0f;
+    for (int v = 0; v < V; ++v) A[v] = 1.0f, D[v] = 0.0f, G[v] = 0.0f;
     if (in.whole) {
         load_tokens<T, V, kKeep, true>(Column<T, V>(d, b.z, b.ldz, l.c, p0), kKeep, z);
         load_tokens<T, V, kKeep, true>(Column<T, V>(d, b.dy, b.lddy, l.c, p0), kKeep, dy);
         load_tokens<T, V, kKeep, true>(Column<T, V>(d, b.u, b.ldu, l.c, p0), kKeep, u);
         shutting = any_shut<T, V, kKeep>(z);
-        if (shutting) sum_gradients_loaded<T, V, kKeep, true, true>(z, dy, kKeep, A, G);
-        else sum_gradients_loaded<T, V, kKeep, true, false>(z, dy, kKeep, A, G);
-        if (in.last) begin_with<V>(A, G, b.dh_last, at());
+        if (shutting) sum_gradients_loaded<T, V, kKeep, true, true>(z, dy, kKeep, A, D, G);
+        else sum_gradients_loaded<T, V, kKeep, true, false>(z, dy, kKeep, A, D, G);
     } else if (held)
         backwards(d, p0, [&](uint32_t k, uint64_t p, uint64_t e, uint64_t, uint64_t end) {
             if (e == end) {
@@ -904,11 +982,13 @@ tile_bwd_kernel(Shape d, Bwd b, Board board)
                 for (int v = 0; v < V; ++v) A[v] = 0.0f;
                 get<V>(b.dh_last, (uint64_t)sequence(d, k) * d.W + l.c, G);
             }
-            sum_few_gradients<T, V>(d, b, l.c, p, e, A, G);
+            sum_few_gradients<T, V>(d, b, l.c, p, e, A, D, G);
         });
+    code<V>(A, D, x);
+    if (in.whole && in.last) begin_with<V>(x, G, b.dh_last, at());
     forget<T, V, kKeep>(z), forget<T, V, kKeep>(u), forget<T, V, kKeep>(dy);
     float behind[V];
-    come_in<V>(d, board, l, l.windows - 1 - l.window, tile, A, G, behind);
+    come_in<V>(d, board, l, l.windows - 1 - l.window, tile, x, G, behind);
     if (in.whole) {
         if (in.last) get<V>(b.dh_last, at(), behind);
         const Column<T, V> dz(d, b.dz, b.lddz, l.c, p0 + kKeep - 1), du(d, b.du, b.lddu, l.c, p0 + kKeep - 1);
@@ -919,11 +999,11 @@ tile_bwd_kernel(Shape d, Bwd b, Board board)
         if (shutting) {
             steps_taken<T, V, kKeep, true>(z, u, state, less);
             forget<T, V, kKeep>(z);
-            retreat_loaded<T, V, kKeep, true, true>(z, dy, less, dz, du, kKeep, behind);
+            retreat_loaded<T, V, kKeep, true, true, false>(z, dy, less, dz, du, kKeep, behind);
         } else {
             steps_taken<T, V, kKeep, false>(z, u, state, less);
             forget<T, V, kKeep>(z);
-            retreat_loaded<T, V, kKeep, true, false>(z, dy, less, dz, du, kKeep, behind);
+            retreat_loaded<T, V, kKeep, true, false, false>(z, dy, less, dz, du, kKeep, behind);
         }
         if (in.first) put<V>(b.dh0, at(), behind);
     } else if (held)

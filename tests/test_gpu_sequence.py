@@ -671,3 +671,127 @@ def test_calls_in_a_graph():
         calls()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, replayed)), i
+
+
+# ------------------------------------------------------------------ gates near 1
+def far_bound(z, n):
+    """What states and gradients of a channel with constant gates may be off by, as a share of the largest one.  Each token's rounding is off by U
+    of a value at most, evenly spread (a variance of U^2 / 3), and lives for the n tokens there are or the 1 / (2 c) that matter in a sum of squares: six
+    standard deviations.  c is off by (|z| + 8) U of itself, which moves a state or a gradient by as much of itself; four of those.  Twice for stretches that are joined."""
+    c = 1 / (1 + np.exp(z))
+    return 2 * U * (6 * np.sqrt(np.minimum(n, 1 / (2 * c)) / 3) + 4 * (np.abs(z) + 8))
+
+
+def check_far(z_of, z, u, dy, h0, dl, offsets, reverse, have, dtype):
+    """have: y, h_last, dz, du, dh0 of sequences with gates z_of (one for each channel, all tokens) against the oracle."""
+    N, W = u.shape
+    w_y, w_last = oracle.recurrence_fwd(z, u, offsets, reverse, h0)
+    w_dz, w_du, w_dh0 = oracle.recurrence_bwd(z, u, offsets, dy, reverse, h0, dl)
+    R = far_bound(z_of, np.diff(offsets).max())
+    c = 1 / (1 + np.exp(z_of))
+    H, G = np.maximum(np.abs(w_y).max(0), np.abs(h0).max(0)), np.maximum(np.abs(w_du).max(0) / c, np.abs(dl).max(0))
+    within("y", have[0], w_y, R * H, dtype)
+    within("h_last", have[1], w_last, R * H, torch.float32)
+    within("dz", have[2], w_dz, 3 * R * c * G * (H + np.abs(u)), dtype)
+    within("du", have[3], w_du, R * c * G, dtype)
+    within("dh0", have[4], w_dh0, R * G, torch.float32)
+
+
+def run_far(z, u, dy, h0, dl, n_seq, reverse, dtype):
+    N, W = u.shape
+    y, dz, du = (torch.empty(N, W, dtype=dtype, device=DEV) for _ in range(3))
+    h_last, dh0 = torch.empty_like(h0), torch.empty_like(h0)
+    ws = torch.empty(max(B.dg_recurrence_workspace_bytes(N, n_seq, W), 16), dtype=torch.uint8, device=DEV)
+    states = torch.empty(B.dg_recurrence_state_count(N, W), device=DEV)
+    B.dg_recurrence_fwd(z, u, n_seq, None, reverse, h0, y, h_last, states, ws)
+    B.dg_recurrence_bwd(z, u, n_seq, None, reverse, h0, states, dy, dl, dz, du, dh0, ws)
+    return y, h_last, dz, du, dh0
+
+
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("n_seq,S,W,dtype,size", [(1, 1 << 16, 9, "fp32", 1.0), (2, 40000, 33, "fp32", 1000.0), (1, 50001, 66, "bf16", 1000.0), (1, 50001, 64, "fp16", 100.0),
+                                                  (1, 70000, 32, "fp32", 1.0), (1, 1 << 17, 3, "fp32", 1.0)])
+def test_recurrence_of_gates_near_one(n_seq, S, W, dtype, size, reverse):
+    """States that live for thousands of tokens, across many bundles of tiles: what comes from outside (`size` times the inputs) is still there
+    at the other end, so that a stretch that is lost, doubled or taken from elsewhere shows, and so does a share that is lost at each token."""
+    say("recurrence near one", n_seq, S, W, dtype, reverse)
+    rng = np.random.default_rng(S + W)
+    t, N = TYPES[dtype], n_seq * S
+    assert B.dg_recurrence_workspace_bytes(N, n_seq, W) > 0             # tiles
+    _, z_of = rounded(np.linspace(8.0, 12.0, W), t)
+    z, z64 = rounded(np.broadcast_to(z_of, (N, W)), t)
+    (u, u64), (dy, dy64) = (rounded(1 + rng.standard_normal((N, W)), t) for _ in range(2))
+    h0, dl = (size * (1 + rng.random((n_seq, W))).astype(np.float32) for _ in range(2))
+    have = run_far(z.to(DEV), u.to(DEV), dy.to(DEV), f32(h0), f32(dl), n_seq, reverse, t)
+    check_far(z_of, z64, u64, dy64, h0, dl, np.arange(n_seq + 1) * S, reverse, have, t)
+
+
+@pytest.mark.parametrize("reverse", [False, True])
+def test_recurrence_of_gates_near_one_sequence_by_sequence(reverse):
+    say("recurrence near one, sequences", reverse)
+    n_seq, S, W = 1300, 1999, 64
+    N = n_seq * S
+    assert B.dg_recurrence_workspace_bytes(N, n_seq, W) == 0            # a lane per sequence
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(5)
+    z_of = np.linspace(8.0, 12.0, W).astype(np.float32)
+    z = f32(z_of).expand(N, W).contiguous()
+    u, dy = (1 + torch.randn(N, W, device=DEV, generator=gen) for _ in range(2))
+    h0, dl = (1 + torch.rand(n_seq, W, device=DEV, generator=gen) for _ in range(2))
+    y, h_last, dz, du, dh0 = run_far(z, u, dy, h0, dl, n_seq, reverse, torch.float32)
+    for j in (0, 1, 649, n_seq - 2):
+        rows, seqs = slice(j * S, (j + 2) * S), slice(j, j + 2)
+        check_far(z_of.astype(np.float64), got(z[rows]), got(u[rows]), got(dy[rows]), got(h0[seqs]), got(dl[seqs]), np.arange(3) * S, reverse,
+                  (y[rows], h_last[seqs], dz[rows], du[rows], dh0[seqs]), torch.float32)
+
+
+def test_recurrence_of_gates_near_one_gives_the_same_bits_each_time():
+    say("recurrence near one, bits")
+    torch.manual_seed(2)
+    n_seq, S, W = 1, 65536, 64
+    z = 8 + 4 * torch.rand(n_seq * S, W, device=DEV)
+    u, dy = torch.randn_like(z), torch.randn_like(z)
+    h0, dl = 1000 * torch.randn(n_seq, W, device=DEV), 1000 * torch.randn(n_seq, W, device=DEV)
+    runs = [run_far(z, u, dy, h0, dl, n_seq, False, torch.float32) for _ in range(6)]
+    for r in runs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(runs[0], r))
+
+
+@pytest.mark.parametrize("S", [40, 4000])
+@pytest.mark.parametrize("gate", [5.0, -5.0, 0.0])
+def test_recurrence_what_is_not_finite_passes_open_gates(gate, S):
+    """An infinite state or gradient stays infinite, and of its sign, whichever share is the larger one."""
+    say("recurrence infinite", gate, S)
+    rng = np.random.default_rng(13)
+    W = 6
+    z, u, dy = np.full((S, W), gate), rng.standard_normal((S, W)), rng.standard_normal((S, W))
+    h0, dl = rng.standard_normal((1, W)), rng.standard_normal((1, W))
+    u[7, 0], u[9, 1], u[11, 2], h0[0, 3] = np.nan, np.inf, -np.inf, -np.inf
+    dy[S - 5, 0], dy[S - 9, 1], dl[0, 4], dy[3, 5] = np.inf, -np.inf, np.inf, np.nan
+    with np.errstate(invalid="ignore"):
+        (z, z64), (u, u64), (dy, dy64) = (rounded(a, torch.float32) for a in (z, u, dy))
+    h0, dl = h0.astype(np.float32), dl.astype(np.float32)
+    have = run_far(z.to(DEV), u.to(DEV), dy.to(DEV), f32(h0), f32(dl), 1, False, torch.float32)
+    want = oracle.recurrence_fwd(z64, u64, [0, S], False, h0) + oracle.recurrence_bwd(z64, u64, [0, S], dy64, False, h0, dl)
+    for what, h, w in zip(("y", "h_last", "dz", "du", "dh0"), have, want):
+        kind = lambda a: np.where(np.isnan(a), 3, np.where(np.isposinf(a), 2, np.where(np.isneginf(a), 1, 0)))
+        np.testing.assert_array_equal(kind(got(h)), kind(w), err_msg=what)
+
+
+@pytest.mark.parametrize("S", [40, 4000])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_recurrence_of_the_largest_values(dtype, S):
+    """Inputs whose difference from the state has no fp32 value: the state has one."""
+    say("recurrence largest", dtype, S)
+    rng = np.random.default_rng(14)
+    W, t = 5, TYPES[dtype]
+    z, z64 = rounded(rng.uniform(-3, 3, (S, W)), t)
+    u, u64 = rounded(np.where(rng.random((S, W)) < 0.5, 3e38, -3e38), t)
+    y, last = torch.empty(S, W, dtype=t, device=DEV), torch.empty(1, W, device=DEV)
+    ws = torch.empty(max(B.dg_recurrence_workspace_bytes(S, 1, W), 16), dtype=torch.uint8, device=DEV)
+    B.dg_recurrence_fwd(z.to(DEV), u.to(DEV), 1, None, False, None, y, last, None, ws)
+    w_y, w_last = oracle.recurrence_fwd(z64, u64, [0, S])
+    # a token is off by (|z| + 8) U of values up to 3e38 and lives for 1 / c <= 22 tokens
+    bound = 22 * 11 * U * 3e38
+    within("y", y, w_y, bound, t)
+    within("h_last", last, w_last, bound, torch.float32)
