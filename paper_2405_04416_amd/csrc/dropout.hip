@@ -74,15 +74,32 @@ dropout_unaligned_kernel(Drop a)
     }
 }
 
+// Values of one launch: 2^31 lanes at most.  A grid of 2^32 lanes and more is cut short without an error.
+constexpr uint64_t kMost = 1ull << 33;
+
 template <class T>
-void launch(const Drop &a, hipStream_t st)
+void launch_one(const Drop &a, bool streamed, hipStream_t st)
 {
     const bool vectors = dg::aligned(a.x, 16) && dg::aligned(a.r, 16) && dg::aligned(a.y, 16);
     const uint64_t per = (vectors ? 16 / sizeof(T) : 4) * kBlock;
     auto go = [&](auto kernel) { kernel<<<(uint32_t)((a.n + per - 1) / per), kBlock, 0, st>>>(a); };
     if (!vectors) return a.r ? go(dropout_unaligned_kernel<T, true>) : go(dropout_unaligned_kernel<T, false>);
-    if (a.n * sizeof(T) >= kStreamedBytes) a.r ? go(dropout_kernel<T, true, true>) : go(dropout_kernel<T, false, true>);
+    if (streamed) a.r ? go(dropout_kernel<T, true, true>) : go(dropout_kernel<T, false, true>);
     else a.r ? go(dropout_kernel<T, true, false>) : go(dropout_kernel<T, false, false>);
+}
+
+template <class T>
+void launch(const Drop &a, hipStream_t st)
+{
+    for (uint64_t at = 0; at < a.n; at += kMost) {
+        Drop part = a;
+        part.x = (const T *)a.x + at;
+        part.r = a.r ? (const T *)a.r + at : nullptr;
+        part.y = (T *)a.y + at;
+        part.n = a.n - at < kMost ? a.n - at : kMost;
+        part.offset += at / 4;
+        launch_one<T>(part, a.n * sizeof(T) >= kStreamedBytes, st);
+    }
 }
 
 int dropout(const char *who, const void *x, const void *r, uint64_t n, double p, uint64_t seed, uint64_t offset, uint32_t dtype, void *y, hipStream_t st)
@@ -92,7 +109,7 @@ int dropout(const char *who, const void *x, const void *r, uint64_t n, double p,
     if (n == 0) return DG_OK;
     const size_t item = item_bytes(dtype);
     DG_REQUIRE(x && y && dg::aligned(x, item) && dg::aligned(y, item) && dg::aligned(r, item), DG_ERR_ARG, "%s: null or misaligned pointer", who);
-    DG_REQUIRE(n <= 1ull << 40, DG_ERR_UNSUPPORTED, "%s: n too large for one launch", who);
+    DG_REQUIRE(n <= 1ull << 40, DG_ERR_UNSUPPORTED, "%s: more than 2^40 values", who);
     const uint32_t below = (uint32_t)std::floor(p * 65536.0 + 0.5);
     const float scale = below == 65536u ? 0.0f : (float)(65536.0 / (65536u - below));
     (dtype == DG_F32 ? launch<float> : dtype == DG_F16 ? launch<f16> : launch<bf16>)({x, r, y, n, seed, offset, below, scale}, st);

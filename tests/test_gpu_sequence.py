@@ -795,3 +795,34 @@ def test_recurrence_of_the_largest_values(dtype, S):
     bound = 22 * 11 * U * 3e38
     within("y", y, w_y, bound, t)
     within("h_last", last, w_last, bound, torch.float32)
+
+
+# ------------------------------------------------------------------ more than one launch
+def needs_memory(gib):
+    free = torch.cuda.mem_get_info()[0] >> 30
+    if free < gib:
+        pytest.skip("%d GiB of GPU memory needed, %d free" % (gib, free))
+
+
+def test_dropout_of_more_values_than_one_launch_takes():
+    """2^34 unaligned values, four to a lane: as many lanes as no launch has."""
+    say("dropout large")
+    needs_memory(40)
+    n, p, seed, offset = (1 << 34) + 4099, 0.25, 21, 5
+    try:
+        buf = torch.ones(1 + n, dtype=torch.float16, device=DEV)
+        y = buf[1:]
+        B.dg_dropout_fwd(y, None, p, seed, offset, y)
+        keep_share, count = 0.75, 0
+        for at in range(0, n, 1 << 30):
+            count += int(torch.count_nonzero(y[at:at + (1 << 30)]))
+        assert abs(count - keep_share * n) <= 6 * np.sqrt(n * keep_share * (1 - keep_share))
+        for at in (0, (1 << 32) - 2048, (1 << 33) - 2048, (1 << 34) - 2048, n - 4099):
+            at = at // 4 * 4
+            part = y[at:at + 4096]
+            keep, factor = oracle.dropout_mask(seed, offset + at // 4, part.numel(), p)
+            np.testing.assert_array_equal(got(part), np.where(keep, np.float16(factor), 0.0))
+        assert float(buf[0]) == 1.0
+    finally:
+        buf = y = part = None
+        torch.cuda.empty_cache()
