@@ -427,21 +427,22 @@ __device__ __forceinline__ void retreat_places(const Shape &d, const Bwd &b, uin
 
 // ------------------------------------------------------------------ a lane per sequence and V channels
 
-__device__ __forceinline__ bool lane_place(const Shape &d, uint32_t V, uint32_t count, uint32_t &k, uint32_t &c)
+// of `count` sequences from place `from` on
+__device__ __forceinline__ bool lane_place(const Shape &d, uint32_t V, uint32_t from, uint32_t count, uint32_t &k, uint32_t &c)
 {
     const uint64_t i = (uint64_t)blockIdx.x * kBlock + threadIdx.x;
     const uint32_t lanes = d.W / V;
-    k = (uint32_t)(i / lanes);
+    k = from + (uint32_t)(i / lanes);
     c = (uint32_t)(i % lanes) * V;
     return i < (uint64_t)count * lanes;
 }
 
 template <class T, int V>
 __global__ void __launch_bounds__(kBlock)
-sequence_fwd_kernel(Shape d, Fwd f)
+sequence_fwd_kernel(Shape d, Fwd f, uint32_t from, uint32_t count)
 {
     uint32_t k, c;
-    if (!lane_place(d, V, d.n_seq, k, c)) return;
+    if (!lane_place(d, V, from, count, k, c)) return;
     uint64_t begin, end;
     places(d, k, begin, end);
     const uint64_t at = (uint64_t)sequence(d, k) * d.W + c;
@@ -453,10 +454,10 @@ sequence_fwd_kernel(Shape d, Fwd f)
 
 template <class T, int V>
 __global__ void __launch_bounds__(kBlock)
-sequence_bwd_kernel(Shape d, Bwd b)
+sequence_bwd_kernel(Shape d, Bwd b, uint32_t from, uint32_t count)
 {
     uint32_t k, c;
-    if (!lane_place(d, V, d.n_seq, k, c)) return;
+    if (!lane_place(d, V, from, count, k, c)) return;
     uint64_t begin, end;
     places(d, k, begin, end);
     const uint32_t seq = sequence(d, k);
@@ -1044,7 +1045,7 @@ int check(const char *who, Shape &d, uint32_t dtype)
     DG_REQUIRE(d.first || d.n_seq == 0 || d.N % d.n_seq == 0, DG_ERR_ARG, "%s: %llu tokens are not %u sequences of one length", who, (unsigned long long)d.N,
                d.n_seq);
     d.S = d.n_seq ? (uint32_t)(d.N / d.n_seq) : 0;
-    DG_REQUIRE((uint64_t)d.n_seq * d.W <= 1ull << 38, DG_ERR_UNSUPPORTED, "%s: too many sequences for one launch", who);
+    DG_REQUIRE((uint64_t)d.n_seq * d.W <= 1ull << 38, DG_ERR_UNSUPPORTED, "%s: more than 2^38 states", who);
     return DG_OK;
 }
 
@@ -1071,7 +1072,26 @@ void cut(Shape &d, uint32_t V, uint32_t most)
     d.n_tiles = (uint32_t)((d.N + tile - 1) / tile);
 }
 
-uint32_t blocks(uint64_t count, uint32_t W, uint32_t V) { return (uint32_t)((count * (W / V) + kBlock - 1) / kBlock); }
+// Lanes of one launch: a grid of 2^32 lanes and more is cut short without an error.
+constexpr uint64_t kMostLanes = 1ull << 31;
+
+// launch(first sequence, sequences, workgroups)
+template <class F>
+void in_sequences(const Shape &d, uint32_t V, F launch)
+{
+    const uint64_t lanes = d.W / V, most = kMostLanes / lanes;
+    for (uint64_t from = 0; from < d.n_seq; from += most) {
+        const uint64_t count = d.n_seq - from < most ? d.n_seq - from : most;
+        launch((uint32_t)from, (uint32_t)count, (uint32_t)((count * lanes + kBlock - 1) / kBlock));
+    }
+}
+
+// launch(workgroups): tiles take their numbers on the device, one launch goes on where the last one has ended
+template <class F>
+void in_tiles(uint64_t n, F launch)
+{
+    for (constexpr uint64_t most = kMostLanes / kTile; n > 0; n -= n < most ? n : most) launch((uint32_t)(n < most ? n : most));
+}
 
 // the board's counter and slots, and room for a copy of the states
 constexpr size_t kSlotsAt = 16;
@@ -1109,18 +1129,18 @@ Board board_of(const Shape &d, void *ws, const float **in, float *out, hipStream
 }
 
 template <class T, int V>
-uint32_t tile_blocks(const Shape &d) { return d.n_tiles * groups_of(d.W, V, lanes_across(d.W, V, most_across<T, V>())); }
+uint64_t tile_blocks(const Shape &d) { return (uint64_t)d.n_tiles * groups_of(d.W, V, lanes_across(d.W, V, most_across<T, V>())); }
 
 template <class T, int V>
 void launch_fwd(Shape d, Fwd f, void *ws, hipStream_t st)
 {
     cut(d, V, most_across<T, V>());
     if (!d.n_tiles) {
-        sequence_fwd_kernel<T, V><<<blocks(d.n_seq, d.W, V), kBlock, 0, st>>>(d, f);
+        in_sequences(d, V, [&](uint32_t from, uint32_t n, uint32_t blocks) { sequence_fwd_kernel<T, V><<<blocks, kBlock, 0, st>>>(d, f, from, n); });
         return;
     }
     const Board board = board_of(d, ws, &f.h0, f.h_last, st);
-    tile_fwd_kernel<T, V><<<tile_blocks<T, V>(d), kTile, 0, st>>>(d, f, board);
+    in_tiles(tile_blocks<T, V>(d), [&](uint32_t blocks) { tile_fwd_kernel<T, V><<<blocks, kTile, 0, st>>>(d, f, board); });
 }
 
 template <class T, int V>
@@ -1128,11 +1148,11 @@ void launch_bwd(Shape d, Bwd b, void *ws, hipStream_t st)
 {
     cut(d, V, most_across<T, V>());
     if (!d.n_tiles) {
-        sequence_bwd_kernel<T, V><<<blocks(d.n_seq, d.W, V), kBlock, 0, st>>>(d, b);
+        in_sequences(d, V, [&](uint32_t from, uint32_t n, uint32_t blocks) { sequence_bwd_kernel<T, V><<<blocks, kBlock, 0, st>>>(d, b, from, n); });
         return;
     }
     const Board board = board_of(d, ws, &b.dh_last, b.dh0, st);
-    tile_bwd_kernel<T, V><<<tile_blocks<T, V>(d), kTile, 0, st>>>(d, b, board);
+    in_tiles(tile_blocks<T, V>(d), [&](uint32_t blocks) { tile_bwd_kernel<T, V><<<blocks, kTile, 0, st>>>(d, b, board); });
 }
 
 }  // namespace

@@ -826,3 +826,30 @@ def test_dropout_of_more_values_than_one_launch_takes():
     finally:
         buf = y = part = None
         torch.cuda.empty_cache()
+
+
+def test_recurrence_of_more_sequences_than_one_launch_takes():
+    """One token each, 33 channels: 2^32 lanes and some, both ways."""
+    say("recurrence large")
+    needs_memory(80)
+    n_seq, W = 130150600, 33
+    assert n_seq * W > 1 << 32
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(3)
+    try:
+        z, u, dy = (torch.randn(n_seq, W, dtype=torch.float16, device=DEV, generator=gen) for _ in range(3))
+        y, dz, du = (torch.empty_like(z) for _ in range(3))
+        states = torch.empty(B.dg_recurrence_state_count(n_seq, W), device=DEV)
+        B.dg_recurrence_fwd(z, u, n_seq, None, False, None, y, None, states)
+        B.dg_recurrence_bwd(z, u, n_seq, None, False, None, states, dy, None, dz, du, None)
+        step = 1 << 22
+        for at in range(0, n_seq, step):
+            zz, uu, gg = (t[at:at + step].double() for t in (z, u, dy))
+            a, c = torch.sigmoid(zz), torch.sigmoid(-zz)
+            # |z| < 7: some ten half units of fp32 for each gate, one rounding to fp16
+            for have, want in ((y, c * uu), (dz, a * c * -uu * gg), (du, c * gg)):
+                off = (have[at:at + step].double() - want).abs()
+                assert bool((off <= (2.0 ** -11 + 64 * U) * want.abs() + 2.0 ** -25).all()), at
+    finally:
+        z = u = dy = y = dz = du = states = zz = uu = gg = a = c = have = want = off = None
+        torch.cuda.empty_cache()
