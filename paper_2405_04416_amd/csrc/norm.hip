@@ -373,11 +373,13 @@ __global__ void __launch_bounds__(kWide)
 norm_fwd_wide_kernel(Norm a)
 {
     __shared__ float red[kWide / dg::kWave][1];
-    const T *x = (const T *)a.x + blockIdx.x * a.ldx;
-    T *y = (T *)a.out + blockIdx.x * a.ldo;
-    float m, s;
-    wide_moments(x, a, m, s, red);
-    for (uint32_t c = threadIdx.x; c < a.W; c += kWide) y[c] = (T)(((float)x[c] - m) * s * (a.gamma ? a.gamma[c] : 1.0f) + (a.beta ? a.beta[c] : 0.0f));
+    for (uint64_t row = blockIdx.x; row < a.N; row += gridDim.x) {
+        const T *x = (const T *)a.x + row * a.ldx;
+        T *y = (T *)a.out + row * a.ldo;
+        float m, s;
+        wide_moments(x, a, m, s, red);
+        for (uint32_t c = threadIdx.x; c < a.W; c += kWide) y[c] = (T)(((float)x[c] - m) * s * (a.gamma ? a.gamma[c] : 1.0f) + (a.beta ? a.beta[c] : 0.0f));
+    }
 }
 
 template <class T>
@@ -462,6 +464,10 @@ uint32_t parts_of(uint64_t N, uint32_t W)
 
 constexpr uint64_t kMostBlocks = 2048;      // of the forward pass: as many as the chip holds at once
 
+// Of the forward pass of rows too wide for registers: far from the 2^32 lanes from which a grid is cut short without an error.  (20 000 rows of 8200 fp32
+// values: a workgroup for each 491 us, 2048 for all 505.)
+constexpr uint64_t kMostWide = 1 << 16;
+
 struct Call {
     Norm a;
     uint32_t dtype, parts;
@@ -513,7 +519,7 @@ void launch_rows(const Call &c)
         case 256:
             return s.K == 2 ? launch_spread<T, V, 256, 2, kLoose>(c) : s.K == 4 ? launch_spread<T, V, 256, 4, kLoose>(c) : launch_spread<T, V, 256, 8, kLoose>(c);
         }
-    if (c.forward) norm_fwd_wide_kernel<T><<<(uint32_t)c.a.N, kWide, 0, c.st>>>(c.a);
+    if (c.forward) norm_fwd_wide_kernel<T><<<(uint32_t)(c.a.N < kMostWide ? c.a.N : kMostWide), kWide, 0, c.st>>>(c.a);
     else norm_bwd_wide_kernel<T><<<c.parts, kWide, 0, c.st>>>(c.a);
 }
 

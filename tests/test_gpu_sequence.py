@@ -853,3 +853,28 @@ def test_recurrence_of_more_sequences_than_one_launch_takes():
     finally:
         z = u = dy = y = dz = du = states = zz = uu = gg = a = c = have = want = off = None
         torch.cuda.empty_cache()
+
+
+def test_norm_of_more_wide_rows_than_one_launch_takes():
+    """A workgroup of 1024 lanes per row, 2^22 rows and some."""
+    say("norm large")
+    needs_memory(150)
+    N, W = (1 << 22) + 3, 8193
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(4)
+    try:
+        x = torch.empty(N, W, device=DEV)
+        some = torch.randn(4099, W, device=DEV, generator=gen)
+        for at in range(0, N, 4099):
+            x[at:at + 4099] = some[:N - at]
+        B.dg_layer_norm_fwd(x, None, None, 1e-5, x)
+        want = torch.empty_like(some)
+        B.dg_layer_norm_fwd(some, None, None, 1e-5, want)
+        for at in range(0, N, 4099):
+            assert torch.equal(x[at:at + 4099], want[:N - at]), at
+        rows = some[:20].double().cpu().numpy()
+        e_y = norm_bounds(rows, np.ones(W), np.zeros(W), np.zeros((20, W)), float(np.float32(1e-5)))[0]
+        within("y", want[:20], oracle.layer_norm_fwd(rows, None, None, float(np.float32(1e-5))), e_y, torch.float32)
+    finally:
+        x = some = want = None
+        torch.cuda.empty_cache()
