@@ -44,6 +44,13 @@ class RayMixer:
     def _rows(self, name, x):
         return self._buffer(name, x.shape, self.dtype)
 
+    def _part_with(self, x):
+        """A result of this block that goes in again is needed until its gradient has been taken: other buffers take its place."""
+        for name in ("y", "dx"):
+            t = self.buffers.get(name)
+            if t is not None and t.untyped_storage().data_ptr() == x.untyped_storage().data_ptr():
+                del self.buffers[name]
+
     def _workspace(self, name, n_bytes):
         return self._buffer(name, torch.Size([n_bytes]), torch.uint8) if n_bytes else None
 
@@ -59,8 +66,10 @@ class RayMixer:
     def forward(self, x, n_seq, first=None, h0=None, h_last=None, training=True):
         """x [N, width] -> y.  n_seq segments of N / n_seq samples each, or of the rows that `first` gives them.  h0, h_last
         [n_seq, width] fp32 or None: states in and out (h_last is written, it may be h0 outside training).  The result is a buffer that the next
-        pass overwrites."""
+        pass overwrites, unless that is a training pass on it."""
         N, W = x.shape
+        if training:
+            self._part_with(x)
         states = self._buffer("states", torch.Size([B.dg_recurrence_state_count(N, W)]), torch.float32) if training else None
         m, y = self._recur(x, n_seq, first, h0, h_last, states), self._rows("y", x)
         p = self.p if training else 0.0

@@ -102,3 +102,20 @@ def test_block_learns(dtype):
     say("block learns", dtype)
     first, last = train_example(rays=512, samples=48, iterations=120, dtype=dtype, report=None)
     assert np.isfinite(last) and last < 0.5 * first
+
+
+def test_block_on_its_own_result():
+    """A result that goes in again is not overwritten before the gradient has used it."""
+    say("block twice")
+    torch.manual_seed(2)
+    n_seq, S, W = 5, 30, 24
+    x, dy = torch.randn(n_seq * S, W, device=DEV), torch.randn(n_seq * S, W, device=DEV)
+    got, want = [], []
+    for out, again in ((got, lambda y: y), (want, lambda y: y.clone())):
+        block = RayMixer(W, torch.float32, p=0.2, seed=3, device=DEV)
+        for _ in range(3):
+            y = again(block.forward(x, n_seq))
+            z = block.forward(y, n_seq)
+            out += [z.clone(), block.backward(dy).clone(), block.grads.clone()]
+            out += [block.forward(again(block.backward(dy)), n_seq).clone(), block.backward(dy).clone(), block.grads.clone()]
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
