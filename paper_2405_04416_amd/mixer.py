@@ -75,7 +75,7 @@ class RayMixer:
         p = self.p if training else 0.0
         B.dg_dropout_fwd(m, x, p, self.seed, self.drawn, y)
         if training:
-            self.saved = (x, n_seq, first, h0, states, self.drawn)
+            self.saved = (x, n_seq, first, h0, states, p, self.drawn)
             self.drawn += -(-x.numel() // 4)
         return y
 
@@ -83,10 +83,10 @@ class RayMixer:
         """Gradient of the last training pass: returns dx, overwrites `grads`.  dh_last, dh0 [n_seq, width] fp32 or None."""
         if self.saved is None:
             raise B.DistGridError("the last pass was not a training pass")
-        x, n_seq, first, h0, states, drawn = self.saved
+        x, n_seq, first, h0, states, p, drawn = self.saved
         N, W = x.shape
         dm, dz, du, dx, part = (self._rows(n, x) for n in ("dm", "dz", "du", "dx", "part"))
-        B.dg_dropout_bwd(dy, self.p, self.seed, drawn, dm)
+        B.dg_dropout_bwd(dy, p, self.seed, drawn, dm)
         B.dg_recurrence_bwd(self.buffers["z"], self.buffers["u"], n_seq, first, self.reverse, h0, states, dm, dh_last, dz, du, dh0,
                             self._workspace("ws_scan", B.dg_recurrence_workspace_bytes(N, n_seq, W)))
         ws = self._workspace("ws_norm", B.dg_layer_norm_bwd_workspace_bytes(N, W))

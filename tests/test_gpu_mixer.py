@@ -119,3 +119,18 @@ def test_block_on_its_own_result():
             out += [z.clone(), block.backward(dy).clone(), block.grads.clone()]
             out += [block.forward(again(block.backward(dy)), n_seq).clone(), block.backward(dy).clone(), block.grads.clone()]
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_block_gradient_is_of_the_pass_that_was():
+    """A schedule may change p before the gradient is taken."""
+    say("block p")
+    torch.manual_seed(3)
+    n_seq, S, W = 4, 20, 16
+    x, dy = torch.randn(n_seq * S, W, device=DEV), torch.randn(n_seq * S, W, device=DEV)
+    out = []
+    for later in (0.3, 0.9):
+        block = RayMixer(W, torch.float32, p=0.3, device=DEV)
+        block.forward(x, n_seq)
+        block.p = later
+        out.append((block.backward(dy).clone(), block.grads.clone()))
+    assert all(torch.equal(a, b) for a, b in zip(*out))
