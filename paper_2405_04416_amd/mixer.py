@@ -19,6 +19,12 @@ from . import binding as B
 EPS = 1e-5
 
 
+def _overlap(a, b):
+    """Whether two contiguous tensors share memory."""
+    begin, end = (lambda t: t.data_ptr()), (lambda t: t.data_ptr() + t.numel() * t.element_size())
+    return begin(a) < end(b) and begin(b) < end(a)
+
+
 class RayMixer:
     def __init__(self, width, dtype=torch.float16, p=0.1, reverse=False, seed=0, device="cuda:0"):
         """width: features per sample; p: share that dropout takes during training; reverse: back to front; seed: of dropout, not
@@ -69,6 +75,8 @@ class RayMixer:
         pass overwrites, unless that is a training pass on it."""
         N, W = x.shape
         if training:
+            if h0 is not None and h_last is not None and _overlap(h0, h_last):
+                raise B.DistGridError("the gradient needs h0: h_last must not lie in its memory")
             self._part_with(x)
         states = self._buffer("states", torch.Size([B.dg_recurrence_state_count(N, W)]), torch.float32) if training else None
         m, y = self._recur(x, n_seq, first, h0, h_last, states), self._rows("y", x)

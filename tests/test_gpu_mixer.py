@@ -6,6 +6,7 @@ import pytest
 import torch
 
 import oracle
+from paper_2405_04416_amd.binding import DistGridError
 from paper_2405_04416_amd.mixer import EPS, RayMixer, train_example
 
 from gpu_util import DEV
@@ -134,3 +135,19 @@ def test_block_gradient_is_of_the_pass_that_was():
         block.p = later
         out.append((block.backward(dy).clone(), block.grads.clone()))
     assert all(torch.equal(a, b) for a, b in zip(*out))
+
+
+def test_block_refuses_states_in_place_in_training():
+    """The gradient needs the state that went in."""
+    say("block h0")
+    n_seq, S, W = 4, 20, 16
+    x, h = torch.randn(n_seq * S, W, device=DEV), torch.randn(n_seq, W, device=DEV)
+    block = RayMixer(W, torch.float32, device=DEV)
+    for last in (h, h.view(-1), h.view(n_seq, W)):
+        with pytest.raises(DistGridError):
+            block.forward(x, n_seq, h0=h, h_last=last)
+    block.forward(x, n_seq, h0=h, h_last=h, training=False)
+    block.forward(x, n_seq, h0=h, h_last=torch.empty_like(h))
+    both = torch.zeros(2, n_seq, W, device=DEV)
+    block.forward(x, n_seq, h0=both[0], h_last=both[1])
+    assert both[1].any() and not both[0].any()
