@@ -72,7 +72,7 @@ class RayMixer:
     def forward(self, x, n_seq, first=None, h0=None, h_last=None, training=True):
         """x [N, width] -> y.  n_seq segments of N / n_seq samples each, or of the rows that `first` gives them.  h0, h_last
         [n_seq, width] fp32 or None: states in and out (h_last is written, it may be h0 outside training).  The result is a buffer that the next
-        pass overwrites, unless that is a training pass on it."""
+        pass overwrites, unless that is a training pass on it.  backward reads x, first and h0 again: they have to stay as they are until then."""
         N, W = x.shape
         if training:
             if h0 is not None and h_last is not None and _overlap(h0, h_last):
