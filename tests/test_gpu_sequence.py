@@ -878,3 +878,95 @@ def test_norm_of_more_wide_rows_than_one_launch_takes():
     finally:
         x = some = want = None
         torch.cuda.empty_cache()
+
+
+# ------------------------------------------------------------------ large arrays, against torch in 64 bits
+def within_there(what, value, want, bound):
+    off, limit = (value.double() - want).abs(), bound + T_OF[value.dtype] * (want.abs() + bound) + LEAST[value.dtype]
+    assert bool((off <= limit).all()), "%s: off by up to %.3g times what is allowed" % (what, float((off / limit).max()))
+
+
+def norm_there(N, W, dtype, seed):
+    """Forward and backward pass of N rows against the definition; bounds as in norm_bounds, sums over rows in chains of N / 512 rows at most and some
+    hundred folds."""
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(seed)
+    normal = lambda *shape: torch.randn(*shape, device=DEV, generator=gen)
+    eps = float(np.float32(1e-5))
+    x, dy = (normal(N, W) * 1.5 + 0.5).to(dtype), normal(N, W).to(dtype)
+    gamma, beta = normal(W), normal(W)
+    y, dx, dgamma, dbeta = torch.empty_like(x), torch.empty_like(x), torch.empty(W, device=DEV), torch.empty(W, device=DEV)
+    ws = torch.empty(B.dg_layer_norm_bwd_workspace_bytes(N, W), dtype=torch.uint8, device=DEV)
+    B.dg_layer_norm_fwd(x, gamma, beta, 1e-5, y)
+    B.dg_layer_norm_bwd(x, gamma, dy, 1e-5, dx, dgamma, dbeta, ws)
+    k, rows = (W / 8 + 24) * U, (N / 512 + 100) * U
+    g64, b64 = gamma.double(), beta.double()
+    sums = torch.zeros(4, W, device=DEV, dtype=torch.float64)
+    for at in range(0, N, 1 << 18):
+        some = slice(at, at + (1 << 18))
+        xx, dd = x[some].double(), dy[some].double()
+        mean = lambda t: t.mean(1, keepdim=True)
+        m = mean(xx)
+        s = 1 / torch.sqrt(mean((xx - m) ** 2) + eps)
+        xh, g, size = (xx - m) * s, dd * g64, xx.abs().amax(1, keepdim=True)
+        e_m = k * size
+        e_s = k + 2 * e_m * s + (e_m * s) ** 2
+        e_xh = (e_m + 2 * U * size) * s + xh.abs() * e_s
+        within_there("y", y[some], xh * g64 + b64, e_xh * g64.abs() + 4 * U * ((xh * g64).abs() + b64.abs()))
+        mg, mgx = mean(g.abs()), mean((g * xh).abs())
+        e_mgx = k * mgx + mean(g.abs() * e_xh)
+        total = g.abs() + mg + xh.abs() * mgx
+        within_there("dx", dx[some], s * (g - mean(g) - xh * mean(g * xh)),
+                     s * (k * mg + xh.abs() * e_mgx + e_xh * mgx + 8 * U * total) + s * total * e_s)
+        sums += torch.stack([(dd * xh).sum(0), dd.sum(0), (dd.abs() * e_xh).sum(0) + rows * (dd * xh).abs().sum(0), rows * dd.abs().sum(0)])
+    within_there("dgamma", dgamma, sums[0], sums[2])
+    within_there("dbeta", dbeta, sums[1], sums[3])
+
+
+@pytest.mark.parametrize("N,W,dtype", [(5003, 4096, "bf16"), (9001, 1024, "fp32"), (20001, 777, "bf16"), (100003, 37, "fp32"), (70001, 6, "fp16"), (2500, 8191, "fp32")])
+def test_norm_of_more_rows_than_workgroups(N, W, dtype):
+    """Workgroups that go through several rows, the next one on its way."""
+    say("norm rows", N, W, dtype)
+    norm_there(N, W, TYPES[dtype], 5)
+
+
+@pytest.mark.parametrize("N,W,dtype", [(24593, 1024, "fp32"), (12301, 4096, "bf16"), (1572881, 32, "fp16"), (3081, 16384, "fp16"), (393301, 64, "fp32")])
+def test_norm_past_the_caches(N, W, dtype):
+    say("norm streamed", N, W, dtype)
+    assert N * W * (4 if dtype == "fp32" else 2) > 96 << 20
+    norm_there(N, W, TYPES[dtype], 6)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_norm_of_rows_too_wide_for_registers(dtype):
+    """Workgroups with several rows, in every type."""
+    say("norm too wide", dtype)
+    norm_there(45, 16391, TYPES[dtype], 7)
+
+
+@pytest.mark.parametrize("dtype,n,with_residual", [("fp16", (48 << 20) + 5, True), ("bf16", 50 << 20, False), ("fp32", (24 << 20) + 3, True), ("fp32", (25 << 20) + 2, False)])
+def test_dropout_past_the_caches(dtype, n, with_residual):
+    say("dropout streamed", dtype, n, with_residual)
+    t, p, seed, offset = TYPES[dtype], 0.1, 31, 77
+    assert n * (4 if dtype == "fp32" else 2) >= 96 << 20
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(8)
+    x, r = (torch.randn(n, device=DEV, generator=gen).to(t) for _ in range(2))
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    B.dg_dropout_fwd(x, r if with_residual else None, p, seed, offset, y)
+    B.dg_dropout_bwd(x, p, seed, offset, dx)
+    keep, factor = oracle.dropout_mask(seed, offset, n, p)
+    want = torch.where(torch.from_numpy(keep).to(DEV), x.double() * factor, 0.0)
+    within_there("dx", dx, want, 2 * U * want.abs())
+    total = want + r.double() if with_residual else want
+    within_there("y", y, total, 3 * U * (want.abs() + r.double().abs() * with_residual))
+
+
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_recurrence_of_a_long_sequence_among_short_ones(dtype, reverse):
+    say("recurrence long among short", dtype, reverse)
+    rng = np.random.default_rng(15)
+    lengths = [10] * 150 + [3001] + [0, 1, 10] * 50
+    first = np.concatenate([[0], np.cumsum(lengths)])
+    check_recurrence(gates(rng, first[-1], 12), rng.standard_normal((first[-1], 12)), len(lengths), first, TYPES[dtype], reverse, True)
