@@ -12,14 +12,6 @@ template <class T, int V>
 struct alignas(sizeof(T) * V) Pack { T v[V]; };
 
 template <class T, int V>
-__device__ __forceinline__ void load(const T *p, float (&out)[V])
-{
-    const Pack<T, V> a = *reinterpret_cast<const Pack<T, V> *>(p);
-#pragma unroll
-    for (int i = 0; i < V; ++i) out[i] = (float)a.v[i];
-}
-
-template <class T, int V>
 __device__ __forceinline__ void store(T *p, const float (&in)[V])
 {
     Pack<T, V> a;
