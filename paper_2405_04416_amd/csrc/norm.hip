@@ -428,21 +428,11 @@ int check_rows(const char *who, const void *p, uint64_t ld, uint32_t W, uint32_t
 
 // How a row of n vectors is spread: up to 64 over as many lanes, rounded up to a power of two; several per lane would leave fewer lanes
 // idle, but a load then takes parts of many lines, which loads past the caches fetch again (48 bf16 values a row, two lanes of three
-// vectors: 1.9 TB/s forward, eight lanes 5.5).  Then a wavefront with up to 4 each, then a workgroup with up to 8.  Single values: up to 4 in
-// a lane with as few idle places as possible (2^20 rows of 6 fp16 values, two lanes of three: 9.6 us forward, eight lanes 16).
+// vectors: 1.9 TB/s forward, eight lanes 5.5).  Then a wavefront with up to 4 each, then a workgroup with up to 8.
 struct Spread { int G, K; };
 
-Spread spread_of(uint32_t n, bool single)
+Spread spread_of(uint32_t n)
 {
-    Spread best = {0, 0};
-    if (single)
-        for (int K : {4, 3, 1})
-            for (int G = 1; G <= 8; G *= 2)
-                if ((uint32_t)(G * K) >= n) {
-                    if (best.G == 0 || G * K < best.G * best.K) best = {G, K};
-                    break;
-                }
-    if (best.G) return best;
     int G = 1;
     while (G < 64 && (uint32_t)G < n) G *= 2;
     for (int K = 1; K <= 4; ++K)
@@ -487,40 +477,43 @@ void launch_spread(const Call &c)
     c.forward ? go(norm_fwd_kernel<T, V, G, K, kBlock, false, kLoose>) : go(norm_bwd_kernel<T, V, G, K, kBlock, false, kLoose>);
 }
 
-template <class T, int V, int G, bool kLoose>
-void launch_lanes(const Call &c, int K)
-{
-    if constexpr (V == 1) {
-        if (K == 4) return launch_spread<T, V, G, 4, kLoose>(c);
-        if (K == 3) return launch_spread<T, V, G, 3, kLoose>(c);
-    }
-    launch_spread<T, V, G, 1, kLoose>(c);
-}
-
 template <class T, int V, bool kLoose>
 void launch_rows(const Call &c)
 {
-    const Spread s = spread_of((c.a.W + V - 1) / V, V == 1);
+    const Spread s = spread_of((c.a.W + V - 1) / V);
     switch (s.G) {
-    case 1: return launch_lanes<T, V, 1, kLoose>(c, s.K);
-    case 2: return launch_lanes<T, V, 2, kLoose>(c, s.K);
-    case 4: return launch_lanes<T, V, 4, kLoose>(c, s.K);
-    case 8: return launch_lanes<T, V, 8, kLoose>(c, s.K);
+    case 1: return launch_spread<T, V, 1, 1, kLoose>(c);
+    case 2: return launch_spread<T, V, 2, 1, kLoose>(c);
+    case 4: return launch_spread<T, V, 4, 1, kLoose>(c);
+    case 8: return launch_spread<T, V, 8, 1, kLoose>(c);
+    case 16: return launch_spread<T, V, 16, 1, kLoose>(c);
+    case 32: return launch_spread<T, V, 32, 1, kLoose>(c);
+    case 64:
+        return s.K == 1   ? launch_spread<T, V, 64, 1, kLoose>(c)
+               : s.K == 2 ? launch_spread<T, V, 64, 2, kLoose>(c)
+               : s.K == 3 ? launch_spread<T, V, 64, 3, kLoose>(c)
+                          : launch_spread<T, V, 64, 4, kLoose>(c);
+    case 256:
+        return s.K == 2 ? launch_spread<T, V, 256, 2, kLoose>(c) : s.K == 4 ? launch_spread<T, V, 256, 4, kLoose>(c) : launch_spread<T, V, 256, 8, kLoose>(c);
     }
-    if constexpr (V > 1)                            // one by one: rows of less than 8 values
-        switch (s.G) {
-        case 16: return launch_spread<T, V, 16, 1, kLoose>(c);
-        case 32: return launch_spread<T, V, 32, 1, kLoose>(c);
-        case 64:
-            return s.K == 1   ? launch_spread<T, V, 64, 1, kLoose>(c)
-                   : s.K == 2 ? launch_spread<T, V, 64, 2, kLoose>(c)
-                   : s.K == 3 ? launch_spread<T, V, 64, 3, kLoose>(c)
-                              : launch_spread<T, V, 64, 4, kLoose>(c);
-        case 256:
-            return s.K == 2 ? launch_spread<T, V, 256, 2, kLoose>(c) : s.K == 4 ? launch_spread<T, V, 256, 4, kLoose>(c) : launch_spread<T, V, 256, 8, kLoose>(c);
-        }
     if (c.forward) norm_fwd_wide_kernel<T><<<(uint32_t)(c.a.N < kMostWide ? c.a.N : kMostWide), kWide, 0, c.st>>>(c.a);
     else norm_bwd_wide_kernel<T><<<c.parts, kWide, 0, c.st>>>(c.a);
+}
+
+// Rows of less than 16 bytes, value by value: up to 4 in a lane with as few idle places as possible (2^20 rows of 6 fp16 values, two lanes of three:
+// 9.6 us forward, eight lanes 16).
+template <class T>
+void launch_narrow(const Call &c)
+{
+    const uint32_t W = c.a.W;
+    if (W == 1) return launch_spread<T, 1, 1, 1, false>(c);
+    if (W == 2) return launch_spread<T, 1, 2, 1, false>(c);
+    if (W == 3) return launch_spread<T, 1, 1, 3, false>(c);
+    if constexpr (sizeof(T) == 2) {
+        if (W == 4) return launch_spread<T, 1, 1, 4, false>(c);
+        if (W <= 6) return launch_spread<T, 1, 2, 3, false>(c);
+        launch_spread<T, 1, 2, 4, false>(c);
+    }
 }
 
 // Vectors of 16 bytes, whether they are aligned and divide a row or not; rows of less than one value by value.  Unaligned vectors / single
@@ -536,7 +529,7 @@ void launch(const Call &c)
                          (!a.out || rows_aligned(a.out, a.ldo, c.dtype, 16));
     if (aligned) launch_rows<T, V, false>(c);
     else if (a.W >= V) launch_rows<T, V, true>(c);
-    else launch_rows<T, 1, false>(c);
+    else launch_narrow<T>(c);
 }
 
 void launch(const Call &c)

@@ -970,3 +970,11 @@ def test_recurrence_of_a_long_sequence_among_short_ones(dtype, reverse):
     lengths = [10] * 150 + [3001] + [0, 1, 10] * 50
     first = np.concatenate([[0], np.cumsum(lengths)])
     check_recurrence(gates(rng, first[-1], 12), rng.standard_normal((first[-1], 12)), len(lengths), first, TYPES[dtype], reverse, True)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("W", list(range(1, 10)))
+def test_norm_of_narrow_rows(W, dtype):
+    """Every spread of rows around the width of a vector."""
+    say("norm narrow", W, dtype)
+    norm_there(1237, W, TYPES[dtype], W)
