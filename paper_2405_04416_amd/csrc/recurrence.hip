@@ -622,6 +622,24 @@ __device__ __forceinline__ void sum_few_gradients(const Shape &d, const Bwd &b, 
     }
 }
 
+// h through places [p, end)
+template <class T, int V>
+__device__ __forceinline__ void go_few(const Shape &d, const Bwd &b, uint32_t c, uint64_t p, uint64_t end, float (&h)[V])
+{
+#pragma unroll 1
+    for (; p < end; p += kFew) {
+        const int n = end - p < kFew ? (int)(end - p) : kFew;
+        Raw<T, V> z[kFew], u[kFew];
+        load_tokens<T, V, kFew, false>(Column<T, V>(d, b.z, b.ldz, c, p), n, z);
+        load_tokens<T, V, kFew, false>(Column<T, V>(d, b.u, b.ldu, c, p), n, u);
+#pragma unroll
+        for (int k = 0; k < kFew; ++k)
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (k < n) h[v] = advance<true>(step_of<true>(z[k][v], u[k][v]), h[v]);
+    }
+}
+
 // every four tokens from the state that was kept, through the tokens in between
 template <class T, int V>
 __device__ __forceinline__ void retreat_few(const Shape &d, const Bwd &b, uint32_t seq, uint32_t c, uint64_t begin, uint64_t p, uint64_t end, float (&G)[V])
@@ -630,14 +648,10 @@ __device__ __forceinline__ void retreat_few(const Shape &d, const Bwd &b, uint32
     while (end > p) {
         const int n = end - p < kFew ? (int)(end - p) : kFew;
         end -= n;
-        float h[V], A[V], D[V];
+        float h[V];
         if (p == begin) get<V>(b.h0, (uint64_t)seq * d.W + c, h);
         else get<V>(b.states, p / kKeep * d.W + c, h);
-        Fwd f;
-        f.z = b.z, f.u = b.u, f.ldz = b.ldz, f.ldu = b.ldu;
-#pragma unroll
-        for (int v = 0; v < V; ++v) A[v] = 1.0f, D[v] = 0.0f;
-        sum_few<T, V>(d, f, c, p, end, A, D, h);
+        go_few<T, V>(d, b, c, p, end, h);
         retreat_tokens<T, V, kFew, false, false>(d, b, c, end, n, h, G);
     }
 }
