@@ -5,11 +5,13 @@ import numpy as np
 import pytest
 import torch
 
+import dg_inputs as di
 import oracle
+from paper_2405_04416_amd import binding as B
 from paper_2405_04416_amd.binding import DistGridError
 from paper_2405_04416_amd.mixer import EPS, RayMixer, train_example
 
-from gpu_util import DEV
+from gpu_util import DEV, dev, host, rel_err
 
 pytestmark = pytest.mark.gpu
 
@@ -151,3 +153,51 @@ def test_block_refuses_states_in_place_in_training():
     both = torch.zeros(2, n_seq, W, device=DEV)
     block.forward(x, n_seq, h0=both[0], h_last=both[1])
     assert both[1].any() and not both[0].any()
+
+
+def test_block_between_the_encode_and_the_networks():
+    """Features of a hash grid, the samples of a segment one after the other, through the block to the field networks and back to the table: every
+    hand-over against the oracle on what the stage before it gave.  A stage rounds to fp16 some eight times, 2^-11 of values up to twice its
+    result's: 0.01 of it."""
+    say("block in the field")
+    rng = np.random.default_rng(6)
+    n_seg, S, scale = 41, 32, 64.0
+    N = n_seg * S
+    u = di.make_unit_coords(N, seed=7)
+    growth = B.dg_growth_factor(16, 512, 16)
+    grid, ref_grid = B.dg_grid_desc_init(16, 2, 14, 16, growth, [1.0, 1.0, 1.0]), oracle.grid_init(16, 2, 14, 16, growth, [1.0, 1.0, 1.0])
+    table = di.make_table(ref_grid.n_entries, 2, 1.0, seed=8)
+    order = B.dg_order_desc_init(grid, N)
+    ordered, pieces = torch.zeros(N, 4, device=DEV), torch.zeros(B.dg_order_pieces_words(order, N), dtype=torch.int32, device=DEV)
+    B.dg_order_samples(order, dev(u), N, ordered, pieces, torch.zeros(B.dg_order_workspace_bytes(order) // 4, dtype=torch.int32, device=DEV))
+    feat = torch.empty(N, 32, dtype=torch.float16, device=DEV)
+    B.dg_hashgrid_encode_fwd_ordered(grid, dev(table), ordered, N, feat)
+    assert rel_err(host(feat).astype(np.float64), oracle.encode_fwd(ref_grid, table, u)) <= 2.0 ** -10
+    block = RayMixer(32, torch.float16, p=0.0, device=DEV)
+    params = (rng.standard_normal((4, 32)) * 0.2 + 1.0).astype(np.float32)
+    block.params.copy_(dev(params).reshape(-1))
+    y = block.forward(feat, n_seg)
+    x64, offsets = host(feat).astype(np.float64), np.arange(n_seg + 1) * S
+    z, v = oracle.layer_norm_fwd(x64, params[0], params[1], EPS), oracle.layer_norm_fwd(x64, params[2], params[3], EPS)
+    assert rel_err(host(y).astype(np.float64), x64 + oracle.recurrence_fwd(z, v, offsets)[0]) <= 0.01
+    mlp, ref_mlp = B.dg_mlp_desc(32, 64, 16, 16, 64, 2, 1), oracle.mlp_desc(32, 64, 16, 16, 64, 2, 1)
+    weights, dirs = (rng.standard_normal(9408) * 0.2).astype(np.float16), rng.standard_normal((n_seg, 16)).astype(np.float16)
+    dsigma, drgb = rng.standard_normal(N).astype(np.float32) * 0.01, rng.standard_normal((N, 3)).astype(np.float32) * 0.01
+    sigma, rgb, dfeat = torch.zeros(N, device=DEV), torch.zeros(N, 3, device=DEV), torch.zeros(N, 32, device=DEV)
+    dW, largest = torch.zeros(9408, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.dg_mlp_fwd_rows(mlp, dev(weights), y, dev(dirs), None, S, N, sigma, rgb)
+    B.dg_mlp_bwd_rows(mlp, dev(weights), y, dev(dirs), None, S, N, dev(dsigma), dev(drgb), 256.0, 16, dfeat, largest, dW,
+                      torch.zeros(B.dg_mlp_bwd_app_workspace_bytes(mlp, N, S) // 4 + 64, device=DEV))
+    y64 = host(y).astype(np.float64)
+    w_sigma, w_rgb = oracle.mlp_fwd(ref_mlp, weights, y64, dirs, S)
+    assert rel_err(host(sigma), w_sigma) <= 0.01 and rel_err(host(rgb), w_rgb) <= 0.01
+    assert rel_err(host(dfeat), oracle.mlp_bwd(ref_mlp, weights, y64, dirs, S, dsigma, drgb, 256.0)[0]) <= 0.01
+    dy = (dfeat * scale).half()                                     # the networks give their gradient in fp32
+    dx = block.backward(dy)
+    dy64 = host(dy).astype(np.float64)
+    dz, dv, _ = oracle.recurrence_bwd(z, v, offsets, dy64)
+    w_dx = dy64 + oracle.layer_norm_bwd(x64, params[0], dz, EPS)[0] + oracle.layer_norm_bwd(x64, params[2], dv, EPS)[0]
+    assert rel_err(host(dx).astype(np.float64), w_dx) <= 0.01
+    dtable, ws = torch.zeros(ref_grid.n_entries, 2, device=DEV), torch.zeros(B.dg_hashgrid_encode_bwd_workspace_bytes(grid, N) // 4 + 64, device=DEV)
+    B.dg_hashgrid_encode_bwd(grid, dev(u), (dx.float() / scale).view(N, 16, 2).transpose(0, 1).contiguous(), N, dtable, ws)     # and it is read in planes
+    assert rel_err(host(dtable), oracle.encode_bwd(ref_grid, u, host(dx).astype(np.float64) / scale)) <= 0.01
