@@ -520,9 +520,9 @@ int dg_composite_ragged_bwd(const float *sigma, const float *rgb, const float *d
  * a gate per channel, so that samples see each other before the networks.
  * Rows are tokens (samples), dtype DG_F32, DG_F16 or DG_BF16 is that of every `void *`
  * array; consecutive values of a row lie next to each other, rows ld (>= W) values apart,
- * so an array may be a range of columns of a wider one; any element-aligned address is
- * taken.  Everything is computed in fp32 and rounded once, to the nearest even value.
- * Results do not depend on how the work is spread: the same call gives the same bits.
+ * so an array may be a range of columns of a wider one (not in dropout); any element-aligned
+ * address is taken.  Everything is computed in fp32 and rounded once, to the nearest even value.
+ * The same call on arrays of the same alignment gives the same bits, whatever the timing.
  * ---------------------------------------------------------------------------------- */
 
 /* Layer norm of N rows of W values, m the mean of a row, s = 1 / sqrt(mean((x - m)^2) + eps):
@@ -552,9 +552,12 @@ int dg_layer_norm_bwd(const void *x, uint64_t ldx, const float *gamma, const voi
  * From |z| = 87 on a gate is exactly 0 or 1, and what it shuts out is not looked at, not even infinities or NaN: z >= 87
  * (+infinity) passes a token over, z <= -87 (-infinity, the lowest value of a type) forgets the past.  z NaN gives NaN.
  * states: NULL, or dg_recurrence_state_count(N, W) floats for the backward pass (the state at every 16th row).
- * ws: dg_recurrence_workspace_bytes(N, n_seq, W) bytes (NULL where that is 0), 16-byte aligned.
+ * Errors do not grow with the length: gates up to z = 12 over 2^17 tokens leave a state off by some 2e-6 of the largest it has been.
+ * ws: dg_recurrence_workspace_bytes(N, n_seq, W) bytes (NULL where that is 0), 16-byte aligned.  Workgroups that run side by side
+ * tell each other states there and wait for them, a second or so at most; then what comes is NaN, and no error is given.  That takes a
+ * workspace that something else writes to during the call, or offsets that descend.
  * Errors: DG_ERR_ARG also for N that n_seq does not divide (first NULL); DG_ERR_UNSUPPORTED for N >= 2^32, W > 2^20,
- * more than 2^39 values. */
+ * more than 2^39 values or 2^38 states. */
 size_t dg_recurrence_state_count(uint64_t N, uint32_t W);
 size_t dg_recurrence_workspace_bytes(uint64_t N, uint32_t n_seq, uint32_t W);
 int dg_recurrence_fwd(const void *z, uint64_t ldz, const void *u, uint64_t ldu, uint64_t N, uint32_t n_seq,
@@ -563,7 +566,7 @@ int dg_recurrence_fwd(const void *z, uint64_t ldz, const void *u, uint64_t ldu, 
 /* Its backward pass; arguments of the forward pass as they were then, states as it left them.  With the gradient
  *   G_t = dy_t + a_{t+1} G_{t+1}  of h_t  (dh_last [n_seq, W], or 0 if NULL, added at the last token):
  *   du = (1 - a) G,  dz = a (1 - a) (h_{t-1} - u_t) G,  dh0 = a_0 G_0 (NULL: not wanted; dh_last for a sequence without a
- *   token; it may be dh_last).  dz, du [N, W], overwritten; behind a shut gate they are 0. */
+ *   token; it may be dh_last).  dz, du [N, W], overwritten; dz of a gate that is shut is 0, and du of a token that is passed over. */
 int dg_recurrence_bwd(const void *z, uint64_t ldz, const void *u, uint64_t ldu, uint64_t N, uint32_t n_seq,
                       const uint32_t *first, uint32_t W, uint32_t reverse, uint32_t dtype, const float *h0,
                       const float *states, const void *dy, uint64_t lddy, const float *dh_last, void *dz,
@@ -573,7 +576,7 @@ int dg_recurrence_bwd(const void *z, uint64_t ldz, const void *u, uint64_t ldu, 
  * residual (NULL: none) is added.  The mask is not stored: value i is dropped iff bits [16 q, 16 q + 16), q = i % 4, of random
  * word offset + i / 4 are less than `below`; words are those of dg_occ_candidates (splitmix64 output mix of
  * seed + 0x9E3779B97F4A7C15*(ctr+1)), so a seed of its own, and offsets at least ceil(n / 4) apart, keep masks apart.
- * The kept share is exactly (65536 - below) / 65536; p == 1 drops everything.  A dropped infinity or NaN leaves 0.
+ * A value is kept with a chance of exactly (65536 - below) / 65536; p == 1 drops everything.  A dropped infinity or NaN leaves 0.
  * y may be x or residual.  The backward pass draws the same mask: dx_i = 0 or dy_i 65536 / (65536 - below) (the gradient of
  * the residual is dy itself); dx may be dy.  DG_ERR_ARG for p outside [0, 1]; DG_ERR_UNSUPPORTED for n > 2^40. */
 int dg_dropout_fwd(const void *x, const void *residual, uint64_t n, double p, uint64_t seed, uint64_t offset,

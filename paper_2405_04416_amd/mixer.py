@@ -1,14 +1,19 @@
 """A sequence block on the features of the samples of rays: call sequencing only.
 
 Sec. 4.3 composites the samples of a ray by one recurrence, with the transmittance as its gate, and merges segments by carrying
-the state across.  `RayMixer` lets the features of the samples pass through such a recurrence before the networks see them, with a
-gate for each channel that is learned, as the residual block of a sequence model:
+the state across.  `RayMixer` sends rows of features through such a recurrence, with a gate for each channel that is learned, as the
+residual block of a sequence model:
 
     y = x + dropout(recurrence(gates = norm(x; gamma_z, beta_z), inputs = norm(x; gamma_u, beta_u)))
 
 Rows are samples, segment after segment: all of one length, or with the offsets `first` that dg_march_segments writes.  A segment
 can start from the state in which another one ended, as partitions do along a ray.  Every arithmetic step happens inside
 libdistgrid; this file allocates, slices and calls.
+
+A program of its own puts the block between the encode and the networks; TrainStep has no place for it.  fp16 rows of 32 features as
+dg_hashgrid_encode_fwd_ordered writes them, in the samples' own order, go in as they are, and the result goes to dg_mlp_fwd_rows as it
+is.  On the way back the caller converts twice: dg_mlp_bwd_rows with n_merged = 16 gives rows in fp32 (scaled, they fit fp16), and
+dg_hashgrid_encode_bwd reads planes in fp32.
 
     python -m paper_2405_04416_amd.mixer        trains a block to clean noisy features along rays
 """
@@ -100,7 +105,8 @@ class RayMixer:
         ws = self._workspace("ws_norm", B.dg_layer_norm_bwd_workspace_bytes(N, W))
         g = self.grads.view(4, W)
         B.dg_layer_norm_bwd(x, self.gamma_z, dz, EPS, part, g[0], g[1], ws)
-        B.dg_dropout_fwd(part, dy, 0.0, 0, 0, dx)                   # without dropping: dx = dy + part
+        # Without dropping: dx = dy + part.  In 16 bits dx is rounded at both sums, each once to half a unit: less than dz and du are already off by.
+        B.dg_dropout_fwd(part, dy, 0.0, 0, 0, dx)
         B.dg_layer_norm_bwd(x, self.gamma_u, du, EPS, part, g[2], g[3], ws)
         B.dg_dropout_fwd(part, dx, 0.0, 0, 0, dx)
         return dx
