@@ -452,8 +452,9 @@ sequence_fwd_kernel(Shape d, Fwd f, uint32_t from, uint32_t count)
     put<V>(f.h_last, at, h);
 }
 
+// Two wavefronts per SIMD: the registers of a third one keep more tokens on their way.  2^17 rays of 64 samples, 32 channels in fp16: 505 us, with three 527.
 template <class T, int V>
-__global__ void __launch_bounds__(kBlock)
+__global__ void __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(2, 2)))
 sequence_bwd_kernel(Shape d, Bwd b, uint32_t from, uint32_t count)
 {
     uint32_t k, c;
