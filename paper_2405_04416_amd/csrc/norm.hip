@@ -442,8 +442,9 @@ Spread spread_of(uint32_t n)
     return {0, 0};
 }
 
-// Workgroups of the backward pass.  Each leaves 2 W sums, so that wide rows have fewer, and each has some 6000 values to itself, but all
-// compute units have two, and as many as each other.  (8192 rows of 4096 bf16 values: 512 workgroups 50 us, 1024 64; 2^23 of 32 fp16
+// Workgroups of the backward pass.  Each leaves 2 W sums, so that wide rows have fewer, and each has some 6000 values to itself, but there are two
+// for each compute unit, and as many for all (they run side by side unless a lane has eight vectors, whose registers leave room for one: 8192 rows of 8192 fp32 values
+// 156 us, 5.2 TB/s; of 16 384 bf16 values 223, 3.6).  (8192 rows of 4096 bf16 values: 512 workgroups 50 us, 1024 64; 2^23 of 32 fp16
 // values: 2048 304 us, 1024 323; 200 000 of 32: 2048 19.7 us, 1563 20.2, 1024 15.3, 781 19.3.)
 uint32_t parts_of(uint64_t N, uint32_t W)
 {
@@ -452,7 +453,8 @@ uint32_t parts_of(uint64_t N, uint32_t W)
     return (uint32_t)(p > most ? most : p < least ? least : p >= 512 ? p / 512 * 512 : p);
 }
 
-constexpr uint64_t kMostBlocks = 2048;      // of the forward pass: as many as the chip holds at once
+// of the forward pass: as many as the chip holds at once where a lane has one vector; with more of them it holds two to five eighths
+constexpr uint64_t kMostBlocks = 2048;
 
 // Of the forward pass of rows too wide for registers: far from the 2^32 lanes from which a grid is cut short without an error.  (20 000 rows of 8200 fp32
 // values: a workgroup for each 491 us, 2048 for all 505.)
@@ -516,7 +518,7 @@ void launch_narrow(const Call &c)
     }
 }
 
-// Vectors of 16 bytes, whether they are aligned and divide a row or not; rows of less than one value by value.  Unaligned vectors / single
+// Vectors of 16 bytes, whether they are aligned and divide a row or not; rows of less than 16 bytes value by value.  Unaligned vectors / single
 // values in us, forward and backward: 2^20 rows of 37 fp32 values 58 / 76 and 106 / 113; 8192 of 4095 44 / 105 and 89 / 283; 2^18 of 999 bf16
 // values 218 / 246 and 324 / 437; 8192 of 4095 33 / 92 and 62 / 243; 2^22 of 33 fp16 values 133 / 187 and 246 / 272; 2^21 of 100, eight bytes at a
 // time, 182 / 210 and 312 / 278.

@@ -6,12 +6,16 @@
 // Tokens have a place in the order in which they are gone through: their row, or N - 1 - row back to front.  The forward pass
 // keeps the state before every kKeep-th place in fp32; the backward pass computes the states between them again.
 //
-// Bound by memory: 3 values moved per element forward, 5 backward, for some 13 and 40 operations, an exp2 and a reciprocal at a quarter of
+// Bound by memory: 3 values moved per element forward, 5 backward, for some 16 and 43 operations, an exp2 and a reciprocal at a quarter of
 // the rate for each time that a gate is computed.  Many sequences: a lane runs through a sequence's tokens, 16 of them on their way at a
-// time.  2^17 rays of 64 samples, 32 channels in fp16: forward 308 us (5.2 TB/s), backward 503 (5.3).  Few long ones: tiles that tell each
-// other what they do to a state; each value is still read once.  One sequence of 2^17 tokens, 256 channels in bf16: forward 66 us (3.1 TB/s),
-// backward 95 (3.5); four of 16 384, 1024 channels: 105 (3.9) and 157 (4.3).  What keeps tiles from 6 TB/s: two workgroups per compute unit
+// time.  2^17 rays of 64 samples, 32 channels in fp16: forward 313 us (5.1 TB/s), backward 507 (5.3).  Few long ones: tiles that tell each
+// other what they do to a state; each value is still read once.  One sequence of 2^17 tokens, 256 channels in bf16: forward 69 us (2.9 TB/s);
+// four of 16 384, 1024 channels: 115 (3.5) and 167 (4.0).  What keeps tiles from 6 TB/s: two workgroups per compute unit
 // load, compute, listen and store in turn, and the gates are computed twice and three times.
+//
+// 16-bit values go in pairs where width and alignment allow it, else one by one: 2^16 sequences of 64 tokens in bf16, 38 / 37 channels: 215 / 231 us and
+// 374 / 398; four of 16 384, 1000 / 999 channels, in tiles: 128 / 147 and 201 / 230.  Rows of less than a line: 2^17 rays of 64 samples in fp16, 16 channels:
+// 172 us (4.7 TB/s) and 270 (5.0), 8 channels 123 (3.3) and 185 (3.6).
 #include <type_traits>
 #include "rows_common.h"
 
@@ -681,7 +685,8 @@ struct Board {
 };
 
 constexpr uint64_t kEmpty = ~0ull;  // x would be a NaN that is not told
-constexpr uint32_t kMostPolls = 1u << 20;      // of a lane, a second or so: then it takes NaN for what it has not heard
+// Of a lane, a second or so: then it takes NaN for what it has not heard.  A workspace that something else writes to would otherwise never let it go.
+constexpr uint32_t kMostPolls = 1u << 20;
 
 __device__ __forceinline__ uint32_t start(const Board &b)
 {
@@ -1075,10 +1080,11 @@ int check_rows(const char *who, const void *p, uint64_t ld, const Shape &d, uint
 // Whether tiles serve a call.  Sequence by sequence 16 tokens take some 1.6 us forward however few sequences there are; tiles take 8 us
 // and then 3 TB/s with 16-bit values, and longer where many windows hold a sequence's end.  They pay for sequences of more than 120
 // tokens and an 80 000th of all values.  Sequences / tiles in us, forward and backward: 256 sequences of 512 tokens, 64 channels, fp16
-// 51 / 25 and 85 / 31; 64 of 1024, 256 channels 103 / 41 and 196 / 55; 16 of 4096, 2048 channels, bf16 528 / 203 and 832 / 290; 512 of 1024, 128
-// channels 140 / 126 and 230 / 180; 400 of 256, 128 channels 30 / 36 and 56 / 51; 4000 of 400, 64 channels 128 / 193 and 216 / 293; 100 of 400, 32
-// channels, fp32 30 / 12 and 45 / 14; 1000 of 200, 32 channels 21 / 35 and 43 / 46; 1000 of 2000, 64 channels 317 / 338 and 524 / 521;
-// 300 of 1500, 512 channels, fp16 339 / 525 and 602 / 605.  V, most: of the call.
+// 57 / 26 and 93 / 33; 64 of 1024, 256 channels 110 / 42 and 181 / 52; 16 of 4096, 2048 channels, bf16 505 / 186 and 828 / 293; 512 of 1024, 128
+// channels 143 / 133 and 225 / 182; 400 of 256, 128 channels 31 / 36 and 49 / 47; 4000 of 400, 64 channels 126 / 199 and 217 / 274; 100 of 400, 32
+// channels, fp32 31 / 12 and 47 / 14; 1000 of 200, 32 channels 28 / 31 and 44 / 40; 1000 of 2000, 64 channels 278 / 245 and 442 / 335;
+// 300 of 1500, 512 channels, fp16 336 / 448 and 593 / 610.  The rule sees the mean length alone, which is all that the host knows: one long sequence among many
+// short ones goes by itself (20 000 of 10 tokens and one of 131 072, 64 channels: 14 ms and 24).  V, most: of the call.
 void cut(Shape &d, uint32_t V, uint32_t most)
 {
     d.n_tiles = 0;
