@@ -220,3 +220,15 @@ def test_sequence_block_host_side():
     for p in (-0.1, 1.1, float("nan")):
         assert L.dg_dropout_fwd(256, None, 0, p, 1, 0, 0, 256, None) == -1
         assert L.dg_dropout_bwd(256, 0, p, 1, 0, 0, 256, None) == -1
+
+
+def test_sequence_block_limits():
+    """Sizes beyond the stated limits are refused before anything is launched."""
+    L = B.lib()
+    assert L.dg_dropout_fwd(256, None, (1 << 40) + 1, 0.5, 1, 0, 0, 256, None) == -2 and b"2^40" in L.dg_last_error()
+    assert L.dg_dropout_bwd(256, (1 << 40) + 1, 0.5, 1, 0, 0, 256, None) == -2
+    rec = lambda N, n_seq, W: L.dg_recurrence_fwd(256, W, 256, W, N, n_seq, None, W, 0, 0, None, 256, W, None, None, None, 0, None)
+    assert rec(0, (1 << 32) - 1, 65) == -2 and b"2^38" in L.dg_last_error()
+    assert rec(1 << 31, 1 << 31, 257) == -2 and rec(1 << 31, 1 << 20, (1 << 20) + 1) == -2
+    assert L.dg_layer_norm_fwd(256, 1 << 20, None, None, (1 << 19) + 1, 1 << 20, 1e-5, 0, 256, 1 << 20, None) == -2
+    assert L.dg_layer_norm_fwd(256, (1 << 20) + 1, None, None, 1, (1 << 20) + 1, 1e-5, 0, 256, (1 << 20) + 1, None) == -2
