@@ -719,7 +719,7 @@ def test_recurrence_of_gates_near_one(n_seq, S, W, dtype, size, reverse):
     t, N = TYPES[dtype], n_seq * S
     assert B.dg_recurrence_workspace_bytes(N, n_seq, W) > 0             # tiles
     _, z_of = rounded(np.linspace(8.0, 12.0, W), t)
-    z, z64 = rounded(np.broadcast_to(z_of, (N, W)), t)
+    z, z64 = rounded(np.tile(z_of, (N, 1)), t)
     (u, u64), (dy, dy64) = (rounded(1 + rng.standard_normal((N, W)), t) for _ in range(2))
     h0, dl = (size * (1 + rng.random((n_seq, W))).astype(np.float32) for _ in range(2))
     have = run_far(z.to(DEV), u.to(DEV), dy.to(DEV), f32(h0), f32(dl), n_seq, reverse, t)
