@@ -584,6 +584,51 @@ int dg_dropout_fwd(const void *x, const void *residual, uint64_t n, double p, ui
 int dg_dropout_bwd(const void *dy, uint64_t n, double p, uint64_t seed, uint64_t offset, uint32_t dtype, void *dx,
                    void *stream);
 
+/* ------------------------------------------------------------------------------------
+ * A block with an associative memory: root-mean-square norm with the residual's addition,
+ * rows in 8-bit floating point and their matrix product, and the gated delta rule.
+ * Rows, types, alignment and equal bits as in the sequence block above.
+ * ---------------------------------------------------------------------------------- */
+
+/* Root-mean-square norm of N rows of W values after the residual's addition:
+ *   t = x + r, rounded to dtype;   y = t s gamma,  s = 1 / sqrt(mean(t^2) + eps).
+ * residual NULL: t = x, and total has to be NULL.  total (t) may be NULL, and may be x or residual; y may be x or residual, but not where
+ * total is.  gamma [W] fp32; NULL: 1.  Other overlaps of outputs with each other or with inputs are not allowed.
+ * Errors: as dg_layer_norm_fwd. */
+int dg_rms_norm_fwd(const void *x, uint64_t ldx, const void *residual, uint64_t ldr, const float *gamma, uint64_t N,
+                    uint32_t W, float eps, uint32_t dtype, void *total, uint64_t ldt, void *y, uint64_t ldy,
+                    void *stream);
+/* Its backward pass, from t (nothing else of the forward pass is kept), th = t s, g = dy gamma:
+ *   dx = dtotal + s (g - th mean(g th)), the gradient of x and of the residual alike;  dgamma = sum over rows of dy th.
+ * dtotal: gradient that reaches t past the norm, or NULL.  dgamma [W] fp32, overwritten (0 for N == 0); each of dx, dgamma may be
+ * NULL; dx may be dy or dtotal.  ws: dg_rms_norm_bwd_workspace_bytes(N, W) bytes, 16-byte aligned (not needed without dgamma). */
+size_t dg_rms_norm_bwd_workspace_bytes(uint64_t N, uint32_t W);
+int dg_rms_norm_bwd(const void *total, uint64_t ldt, const float *gamma, const void *dy, uint64_t lddy,
+                    const void *dtotal, uint64_t lddt, uint64_t N, uint32_t W, float eps, uint32_t dtype, void *dx,
+                    uint64_t lddx, float *dgamma, void *ws, size_t ws_bytes, void *stream);
+
+/* Rows in 8 bits: value c of row i stands for q[i, c] 2^(scales[i, c / 128] - 127), q in e4m3 (bias 7, largest 448, no
+ * infinity).  A block of 128 columns has the smallest scale >= 2^-127 for which none of its finite values is beyond 448 times it; infinities and NaN
+ * become NaN.  Values are rounded once, from fp32, to the nearest even one.  q: 16-byte aligned, ldq (in values) a multiple of 16;
+ * scales [N, ceil(W / 128)] bytes, rows lds apart; what lies between rows stays as it is.  q, scales and total must not overlap, nor q and scales inputs.
+ * dg_rms_norm_e4m3_fwd: what dg_rms_norm_fwd gives, in 8 bits.  dg_e4m3_rows: the rows themselves (weights). */
+int dg_rms_norm_e4m3_fwd(const void *x, uint64_t ldx, const void *residual, uint64_t ldr, const float *gamma,
+                         uint64_t N, uint32_t W, float eps, uint32_t dtype, void *total, uint64_t ldt, void *q,
+                         uint64_t ldq, uint8_t *scales, uint64_t lds, void *stream);
+int dg_e4m3_rows(const void *x, uint64_t ldx, uint64_t N, uint32_t W, uint32_t dtype, void *q, uint64_t ldq,
+                 uint8_t *scales, uint64_t lds, void *stream);
+/* Product of rows in 8 bits: y[m, n] = sum over k of a[m, k] b[n, k], what they stand for; a [M, K], b [N, K] (a projection's
+ * weights, a row for each output), scales [M or N, ceil(K / 128)].  y [M, N] of type dtype, DG_F16 or DG_BF16: the matrix instruction
+ * aligns a sum's terms to the largest, so that sums are off by some 1e-5 of it, which fp32 would show.  Columns from K on and rows that
+ * are not there are not read.  y must not overlap an input.
+ * ws: dg_e4m3_product_workspace_bytes(M, N, K) bytes (NULL where that is 0), 16-byte aligned.
+ * Errors: DG_ERR_ARG for K == 0, sides that are not 16-byte aligned or whose ld is no multiple of 16, another dtype;
+ * DG_ERR_UNSUPPORTED for more than 2^24 rows or columns, or 2^40 results. */
+size_t dg_e4m3_product_workspace_bytes(uint64_t M, uint64_t N, uint32_t K);
+int dg_e4m3_product(const void *a, uint64_t lda, const uint8_t *a_scales, uint64_t ldsa, const void *b, uint64_t ldb,
+                    const uint8_t *b_scales, uint64_t ldsb, uint64_t M, uint64_t N, uint32_t K, uint32_t dtype,
+                    void *y, uint64_t ldy, void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

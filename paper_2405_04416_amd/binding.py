@@ -163,6 +163,17 @@ _SIGNATURES = {
                           + [C.c_void_p, C.c_uint64, C.c_void_p] + [C.c_void_p, C.c_uint64] * 2 + [C.c_void_p] * 2 + [C.c_size_t, C.c_void_p]),
     "dg_dropout_fwd": (C.c_int, [C.c_void_p, C.c_void_p, C.c_uint64, C.c_double, C.c_uint64, C.c_uint64, C.c_uint32, C.c_void_p, C.c_void_p]),
     "dg_dropout_bwd": (C.c_int, [C.c_void_p, C.c_uint64, C.c_double, C.c_uint64, C.c_uint64, C.c_uint32, C.c_void_p, C.c_void_p]),
+    "dg_rms_norm_fwd": (C.c_int, [C.c_void_p, C.c_uint64] * 2 + [C.c_void_p, C.c_uint64, C.c_uint32, C.c_float, C.c_uint32] + [C.c_void_p, C.c_uint64] * 2
+                        + [C.c_void_p]),
+    "dg_rms_norm_bwd_workspace_bytes": (C.c_size_t, [C.c_uint64, C.c_uint32]),
+    "dg_rms_norm_bwd": (C.c_int, [C.c_void_p, C.c_uint64, C.c_void_p] + [C.c_void_p, C.c_uint64] * 2 + [C.c_uint64, C.c_uint32, C.c_float, C.c_uint32]
+                        + [C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "dg_rms_norm_e4m3_fwd": (C.c_int, [C.c_void_p, C.c_uint64] * 2 + [C.c_void_p, C.c_uint64, C.c_uint32, C.c_float, C.c_uint32] + [C.c_void_p, C.c_uint64] * 3
+                             + [C.c_void_p]),
+    "dg_e4m3_rows": (C.c_int, [C.c_void_p, C.c_uint64, C.c_uint64, C.c_uint32, C.c_uint32] + [C.c_void_p, C.c_uint64] * 2 + [C.c_void_p]),
+    "dg_e4m3_product_workspace_bytes": (C.c_size_t, [C.c_uint64, C.c_uint64, C.c_uint32]),
+    "dg_e4m3_product": (C.c_int, [C.c_void_p, C.c_uint64] * 4 + [C.c_uint64, C.c_uint64, C.c_uint32, C.c_uint32, C.c_void_p, C.c_uint64, C.c_void_p, C.c_size_t,
+                                  C.c_void_p]),
 }
 
 EXPORTS = tuple(_SIGNATURES)
@@ -775,3 +786,65 @@ def dg_dropout_fwd(x, residual, p, seed, offset, y):
 def dg_dropout_bwd(dy, p, seed, offset, dx):
     code, n, dtype = _code(dy, rows=False), dy.numel(), dy.dtype
     _check(lib().dg_dropout_bwd(_vector(dy, n, dtype), n, p, seed, offset, code, _vector(dx, n, dtype), _stream()))
+
+
+# ------------------------------------------------------------------ root-mean-square norm, rows in 8 bits and their product
+def _optional_rows(t, dtype, shape):
+    return (None, shape[1]) if t is None else _rows(t, dtype, shape)
+
+
+def _rows8(q, scales, shape):
+    """(pointer, distance, pointer, distance) of rows in 8 bits: values float8_e4m3fn [N, W], scales float8_e8m0fnu [N, ceil(W / 128)]."""
+    pq, ldq = _rows(q, torch.float8_e4m3fn, shape)
+    ps, lds = _rows(scales, torch.float8_e8m0fnu, (shape[0], -(-shape[1] // 128)))
+    return pq, ldq if shape[0] > 1 else -(-ldq // 16) * 16, ps, lds
+
+
+def dg_rms_norm_fwd(x, residual, gamma, eps, total, y):
+    """x, residual, total, y [N, W] fp32, fp16 or bf16; residual, gamma ([W] fp32) and total may be None."""
+    code, dtype, shape = _code(x), x.dtype, x.shape
+    N, W = shape
+    (px, ldx), (pr, ldr), (pt, ldt), (py, ldy) = _rows(x, dtype, shape), _optional_rows(residual, dtype, shape), _optional_rows(total, dtype, shape), _rows(y, dtype, shape)
+    _check(lib().dg_rms_norm_fwd(px, ldx, pr, ldr, _vector(gamma, W), N, W, eps, code, pt, ldt, py, ldy, _stream()))
+
+
+def dg_rms_norm_bwd_workspace_bytes(N, W):
+    return int(lib().dg_rms_norm_bwd_workspace_bytes(N, W))
+
+
+def dg_rms_norm_bwd(total, gamma, dy, dtotal, eps, dx, dgamma, ws=None):
+    """total: what was normed; dtotal, dx, dgamma: each may be None."""
+    code, dtype, shape = _code(total), total.dtype, total.shape
+    N, W = shape
+    (pt, ldt), (pdy, lddy), (pdt, lddt), (pdx, lddx) = _rows(total, dtype, shape), _rows(dy, dtype, shape), _optional_rows(dtotal, dtype, shape), _optional_rows(dx, dtype, shape)
+    pws, ws_bytes = _workspace(ws)
+    _check(lib().dg_rms_norm_bwd(pt, ldt, _vector(gamma, W), pdy, lddy, pdt, lddt, N, W, eps, code, pdx, lddx, _vector(dgamma, W), pws, ws_bytes, _stream()))
+
+
+def dg_rms_norm_e4m3_fwd(x, residual, gamma, eps, total, q, scales):
+    """As dg_rms_norm_fwd, the result as values q [N, W] float8_e4m3fn, rows a multiple of 16 apart, and scales [N, ceil(W / 128)] float8_e8m0fnu."""
+    code, dtype, shape = _code(x), x.dtype, x.shape
+    N, W = shape
+    (px, ldx), (pr, ldr), (pt, ldt) = _rows(x, dtype, shape), _optional_rows(residual, dtype, shape), _optional_rows(total, dtype, shape)
+    _check(lib().dg_rms_norm_e4m3_fwd(px, ldx, pr, ldr, _vector(gamma, W), N, W, eps, code, pt, ldt, *_rows8(q, scales, shape), _stream()))
+
+
+def dg_e4m3_rows(x, q, scales):
+    """x [N, W] fp32, fp16 or bf16 in 8 bits."""
+    code, shape = _code(x), x.shape
+    px, ldx = _rows(x, x.dtype, shape)
+    _check(lib().dg_e4m3_rows(px, ldx, *shape, code, *_rows8(q, scales, shape), _stream()))
+
+
+def dg_e4m3_product_workspace_bytes(M, N, K):
+    return int(lib().dg_e4m3_product_workspace_bytes(M, N, K))
+
+
+def dg_e4m3_product(a, a_scales, b, b_scales, y, ws=None):
+    """a [M, K], b [N, K] in 8 bits, with their scales; y [M, N] fp16 or bf16."""
+    if a.dim() != 2 or b.dim() != 2 or a.shape[1] != b.shape[1]:
+        raise DistGridError("expected [M, K] and [N, K], got %s and %s" % (tuple(a.shape), tuple(b.shape)))
+    (M, K), N = a.shape, b.shape[0]
+    py, ldy = _rows(y, y.dtype, (M, N))
+    pws, ws_bytes = _workspace(ws)
+    _check(lib().dg_e4m3_product(*_rows8(a, a_scales, (M, K)), *_rows8(b, b_scales, (N, K)), M, N, K, _code(y), py, ldy, pws, ws_bytes, _stream()))
