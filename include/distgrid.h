@@ -629,6 +629,37 @@ int dg_e4m3_product(const void *a, uint64_t lda, const uint8_t *a_scales, uint64
                     const uint8_t *b_scales, uint64_t ldsb, uint64_t M, uint64_t N, uint32_t K, uint32_t dtype,
                     void *y, uint64_t ldy, void *ws, size_t ws_bytes, void *stream);
 
+/* Gated delta rule: H heads, each with a memory S [Dk, Dv], along n_seq sequences of rows, N rows in all.  For a token
+ *   S <- e^g S;   S <- S + beta k (v - S^T k)^T;   o = scale S^T q,      S before the first token: s0, or 0 if NULL.
+ * q, k [N, Hk Dk], v, o [N, H Dv], heads next to each other in a row; H is a multiple of Hk, head h takes key head h / (H / Hk).
+ * g (logarithm of the decay, <= 0; -infinity, and anything below -104, forgets all) and beta (rate) [N, H] fp32, rows ldg and ldbeta apart.
+ * s0, s_last [n_seq, H, Dk, Dv] fp32, either may be NULL; s_last receives the memories after the last tokens (s0 for a sequence without
+ * one) and may be s0, unless a backward pass is to follow.  Keys of length one (dg_rms_norm_fwd over rows of Dk with gamma = Dk^-1/2) and rates up to 1 keep memories bounded.
+ * first, reverse: as for dg_recurrence_fwd.  One token per sequence (N == n_seq), or a few, is the step of a program that gets its tokens one after the other.
+ * saved: NULL, or dg_delta_rule_saved_bytes(N, n_seq, H, Dk, Dv) bytes for the backward pass, 16-byte aligned (what tokens write, and the memories before every
+ * 64th).  ws: dg_delta_rule_workspace_bytes(N, n_seq, Hk, H, Dk, Dv) bytes, 16-byte aligned, that both passes take; no call needs what another left there.
+ * Everything is as exact as in fp32, and the same call gives the same bits.  Tokens are taken 32 or 64 at a time: an infinity or NaN in a token's row may show in
+ * the results of up to 63 tokens before it.  o must not overlap an input.
+ * Errors: DG_ERR_ARG for heads or sizes of 0, H that Hk does not divide, N that n_seq does not divide (first NULL), a scale that is not finite;
+ * DG_ERR_UNSUPPORTED for Dk or Dv above 128, N >= 2^32, n_seq >= 2^31, H > 2^16, N H > 2^36, n_seq H > 2^32. */
+size_t dg_delta_rule_saved_bytes(uint64_t N, uint32_t n_seq, uint32_t H, uint32_t Dk, uint32_t Dv);
+size_t dg_delta_rule_workspace_bytes(uint64_t N, uint32_t n_seq, uint32_t Hk, uint32_t H, uint32_t Dk, uint32_t Dv);
+int dg_delta_rule_fwd(const void *q, uint64_t ldq, const void *k, uint64_t ldk, const void *v, uint64_t ldv,
+                      const float *g, uint64_t ldg, const float *beta, uint64_t ldbeta, uint64_t N, uint32_t n_seq,
+                      const uint32_t *first, uint32_t Hk, uint32_t H, uint32_t Dk, uint32_t Dv, uint32_t reverse,
+                      float scale, uint32_t dtype, const float *s0, void *o, uint64_t ldo, float *s_last, void *saved,
+                      size_t saved_bytes, void *ws, size_t ws_bytes, void *stream);
+/* Its backward pass; arguments of the forward pass as they were then, saved as it left it, do_ the gradient of o, ds_last that of s_last (0 if NULL).
+ * dq, dk [N, Hk Dk], dv [N, H Dv], dg, dbeta [N, H] and ds0 [n_seq, H, Dk, Dv] (NULL: not wanted; it may be ds_last) are overwritten; rows that no
+ * sequence has are left as they are.  Gradients of a key head are summed over the heads that share it.  They must not overlap inputs. */
+int dg_delta_rule_bwd(const void *q, uint64_t ldq, const void *k, uint64_t ldk, const void *v, uint64_t ldv,
+                      const float *g, uint64_t ldg, const float *beta, uint64_t ldbeta, uint64_t N, uint32_t n_seq,
+                      const uint32_t *first, uint32_t Hk, uint32_t H, uint32_t Dk, uint32_t Dv, uint32_t reverse,
+                      float scale, uint32_t dtype, const void *saved, size_t saved_bytes, const void *do_,
+                      uint64_t lddo, const float *ds_last, void *dq, uint64_t lddq, void *dk, uint64_t lddk, void *dv,
+                      uint64_t lddv, float *dg, uint64_t lddg, float *dbeta, uint64_t lddbeta, float *ds0, void *ws,
+                      size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -174,6 +174,12 @@ _SIGNATURES = {
     "dg_e4m3_product_workspace_bytes": (C.c_size_t, [C.c_uint64, C.c_uint64, C.c_uint32]),
     "dg_e4m3_product": (C.c_int, [C.c_void_p, C.c_uint64] * 4 + [C.c_uint64, C.c_uint64, C.c_uint32, C.c_uint32, C.c_void_p, C.c_uint64, C.c_void_p, C.c_size_t,
                                   C.c_void_p]),
+    "dg_delta_rule_saved_bytes": (C.c_size_t, [C.c_uint64] + [C.c_uint32] * 4),
+    "dg_delta_rule_workspace_bytes": (C.c_size_t, [C.c_uint64] + [C.c_uint32] * 5),
+    "dg_delta_rule_fwd": (C.c_int, [C.c_void_p, C.c_uint64] * 5 + [C.c_uint64, C.c_uint32, C.c_void_p] + [C.c_uint32] * 5 + [C.c_float, C.c_uint32, C.c_void_p, C.c_void_p,
+                                    C.c_uint64, C.c_void_p] + [C.c_void_p, C.c_size_t] * 2 + [C.c_void_p]),
+    "dg_delta_rule_bwd": (C.c_int, [C.c_void_p, C.c_uint64] * 5 + [C.c_uint64, C.c_uint32, C.c_void_p] + [C.c_uint32] * 5 + [C.c_float, C.c_uint32, C.c_void_p, C.c_size_t,
+                                    C.c_void_p, C.c_uint64, C.c_void_p] + [C.c_void_p, C.c_uint64] * 5 + [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
 }
 
 EXPORTS = tuple(_SIGNATURES)
@@ -848,3 +854,39 @@ def dg_e4m3_product(a, a_scales, b, b_scales, y, ws=None):
     py, ldy = _rows(y, y.dtype, (M, N))
     pws, ws_bytes = _workspace(ws)
     _check(lib().dg_e4m3_product(*_rows8(a, a_scales, (M, K)), *_rows8(b, b_scales, (N, K)), M, N, K, _code(y), py, ldy, pws, ws_bytes, _stream()))
+
+
+# ------------------------------------------------------------------ gated delta rule
+def dg_delta_rule_saved_bytes(N, n_seq, H, Dk, Dv):
+    return int(lib().dg_delta_rule_saved_bytes(N, n_seq, H, Dk, Dv))
+
+
+def dg_delta_rule_workspace_bytes(N, n_seq, Hk, H, Dk, Dv):
+    return int(lib().dg_delta_rule_workspace_bytes(N, n_seq, Hk, H, Dk, Dv))
+
+
+def _delta_rule(q, k, v, g, beta, Hk, n_seq, first, reverse, scale):
+    """The arguments that both passes begin with, and N, H, Dk, Dv, shapes of q and v, type."""
+    code, dtype, N, H = _code(v), v.dtype, v.shape[0], g.shape[1] if g.dim() == 2 else 0
+    if H < 1 or Hk < 1 or q.dim() != 2 or q.shape[1] % Hk or v.shape[1] % H:
+        raise DistGridError("expected q, k [N, Hk Dk], v [N, H Dv], g, beta [N, H]; got %s, %s, %s" % (tuple(q.shape), tuple(v.shape), tuple(g.shape)))
+    Dk, Dv, sq, sv, sg = q.shape[1] // Hk, v.shape[1] // H, (N, q.shape[1]), v.shape, (N, H)
+    args = (*_rows(q, dtype, sq), *_rows(k, dtype, sq), *_rows(v, dtype, sv), *_rows(g, torch.float32, sg), *_rows(beta, torch.float32, sg), N, n_seq,
+            _vector(first, n_seq + 1, torch.int32), Hk, H, Dk, Dv, reverse, scale, code)
+    return args, N, H, Dk, Dv, sq, sv, dtype
+
+
+def dg_delta_rule_fwd(q, k, v, g, beta, Hk, n_seq, first, reverse, scale, s0, o, s_last, saved=None, ws=None):
+    """q, k [N, Hk Dk], v, o [N, H Dv] fp32, fp16 or bf16; g, beta [N, H] fp32; first [n_seq + 1] int32 or None; s0, s_last [n_seq, H, Dk, Dv] fp32 and saved
+    (dg_delta_rule_saved_bytes), each may be None."""
+    args, N, H, Dk, Dv, _, sv, dtype = _delta_rule(q, k, v, g, beta, Hk, n_seq, first, reverse, scale)
+    m = n_seq * H * Dk * Dv
+    _check(lib().dg_delta_rule_fwd(*args, _vector(s0, m), *_rows(o, dtype, sv), _vector(s_last, m), *_workspace(saved), *_workspace(ws), _stream()))
+
+
+def dg_delta_rule_bwd(q, k, v, g, beta, Hk, n_seq, first, reverse, scale, saved, do, ds_last, dq, dk, dv, dg, dbeta, ds0, ws=None):
+    """saved: as the forward pass left it; ds_last, ds0 [n_seq, H, Dk, Dv] fp32, each may be None."""
+    args, N, H, Dk, Dv, sq, sv, dtype = _delta_rule(q, k, v, g, beta, Hk, n_seq, first, reverse, scale)
+    m, f32 = n_seq * H * Dk * Dv, torch.float32
+    _check(lib().dg_delta_rule_bwd(*args, *_workspace(saved), *_rows(do, dtype, sv), _vector(ds_last, m), *_rows(dq, dtype, sq), *_rows(dk, dtype, sq), *_rows(dv, dtype, sv),
+                                   *_rows(dg, f32, (N, H)), *_rows(dbeta, f32, (N, H)), _vector(ds0, m), *_workspace(ws), _stream()))

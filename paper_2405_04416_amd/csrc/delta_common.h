@@ -1,0 +1,176 @@
+// The gated delta rule: what its kernels share.  Internal.
+//
+// Per head, with a memory S [Dk, Dv]:  S <- e^g S;  S <- S + beta k (v - S^T k)^T;  o = scale S^T q.
+// Over a chunk of tokens, S the memory before it, G the sums of g from its start on, D[i, j] = e^(G[i] - G[j]):
+//   A[i, j] = beta[i] D[i, j] k[i] k[j]  (j < i),   T = (1 + A)^-1,   P[i, j] = scale D[i, j] q[i] k[j]  (j <= i),
+//   U = T beta (V - e^G K S)  (what the tokens write),   O = scale e^G Q S + P U,   S' = e^G[last] S + K^T (e^(G[last] - G) U).
+//
+// Products are taken on the matrix units in bf16, of values that are cut into pieces of 8 bits: one for a bf16 value, two for fp16, three for
+// fp32, which lose nothing; of the products of pieces those below 2^-24 are left out.  So everything is as exact as in fp32, at several times
+// the rate of the fp32 matrix instruction (139 TFLOP/s measured; three bf16 products 445).
+#pragma once
+#include "rows_common.h"
+
+namespace dg_delta {
+
+using dg_rows::bf16;
+using dg_rows::f16;
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kMark = 64;               // tokens between memories that the forward pass leaves for the backward pass
+constexpr int kMaxD = 128;
+// e^-104 is 0 in fp32: below that a gate is shut.  Logarithms are cut off here so that their differences stay numbers.
+constexpr float kShut = -200.0f;
+
+struct Delta {
+    const void *q, *k, *v;
+    const float *g, *beta;
+    uint64_t ldq, ldk, ldv, ldg, ldb;
+    const float *s0, *ds_last;
+    void *o;
+    const void *dout;
+    uint64_t ldo, lddo;
+    float *s_last, *ds0;
+    float *marks, *dmarks;              // [slots][H][Dk][Dv]: memories before each 64 tokens, gradients of those after
+    float *u, *dr;                      // [N][H][Dv]
+    void *dq, *dk, *dv;
+    uint64_t lddq, lddk, lddv;
+    float *dg, *dbeta;
+    uint64_t lddg, lddb;
+    const uint32_t *first;
+    const uint32_t *slot_seq;
+    uint64_t N;
+    uint32_t n_seq, Hk, H, Dk, Dv, reverse, slots;
+    float scale;
+    uint32_t vec_q, vec_k, vec_v, vec_o;        // whether 8 values of a head's row can be loaded at once
+};
+
+template <class T>
+struct Pieces { static constexpr int n = sizeof(T) == 4 ? 3 : 2; };
+template <>
+struct Pieces<bf16> { static constexpr int n = 1; };
+
+// ------------------------------------------------------------------------------ sequences
+struct Span {
+    uint64_t begin;
+    uint32_t len, reverse;
+    __device__ __forceinline__ uint64_t row(uint32_t i) const { return reverse ? begin + len - 1 - i : begin + i; }
+};
+
+// no row from N on, whatever the offsets say
+__device__ __forceinline__ Span span_of(const Delta &d, uint32_t seq)
+{
+    if (!d.first) {
+        const uint64_t len = d.N / d.n_seq;
+        return {seq * len, (uint32_t)len, d.reverse};
+    }
+    const uint64_t b = d.first[seq], e = d.first[seq + 1], begin = b < d.N ? b : d.N, end = e < d.N ? e : d.N;
+    return {begin, end > begin ? (uint32_t)(end - begin) : 0u, d.reverse};
+}
+
+// Where the memories of a sequence are left: every sequence begins one slot after floor(begin / 64) more than the one before, which leaves room for all
+// of them, whatever the lengths.
+__device__ __forceinline__ uint32_t first_slot(const Span &s, uint32_t seq) { return (uint32_t)(s.begin / kMark) + seq; }
+
+// ------------------------------------------------------------------------------ pieces
+__device__ __forceinline__ float top(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
+
+// the upper halves of two words, a's below b's
+__device__ __forceinline__ uint32_t upper(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302); }
+
+// x = sum of n pieces, each the leading 8 bits of what the ones before leave
+template <int n, int count>
+__device__ __forceinline__ void split(const float (&x)[count], uint32_t (&out)[n][count / 2])
+{
+#pragma unroll
+    for (int i = 0; i < count; i += 2) {
+        float a = x[i], b = x[i + 1];
+#pragma unroll
+        for (int p = 0; p < n; ++p) {
+            out[p][i / 2] = upper(a, b);
+            if (p + 1 < n) {
+                a -= top(a);
+                b -= top(b);
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ bf16x8 operand(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
+
+template <int n>
+__device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&out)[n])
+{
+    uint32_t w[n][4];
+    split<n, 8>(x, w);
+#pragma unroll
+    for (int p = 0; p < n; ++p) out[p] = operand((u32x4){w[p][0], w[p][1], w[p][2], w[p][3]});
+}
+
+// Two 16-row results of the matrix unit, one above the other, as the right operand of a product that sums over their rows: lane (column c, group q) has rows
+// 4 q to 4 q + 3 of each, and takes them for its eight places.  Left operands come with their columns in that order (`place`).
+template <int n>
+__device__ __forceinline__ void split_rows(const f32x4 &a, const f32x4 &b, bf16x8 (&out)[n])
+{
+    const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    split8<n>(x, out);
+}
+
+// place of column c among the columns of a left operand; runs of four stay together
+__device__ __forceinline__ uint32_t place(uint32_t c) { return (c & ~31u) | (c >> 2 & 3) << 3 | (c >> 4 & 1) << 2 | (c & 3); }
+
+__device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+// Sum of the products of pieces whose orders add up to less than three
+template <int na, int nb>
+__device__ __forceinline__ f32x4 multiply(const bf16x8 (&a)[na], const bf16x8 (&b)[nb], f32x4 c)
+{
+#pragma unroll
+    for (int i = 0; i < na; ++i)
+#pragma unroll
+        for (int j = 0; j < nb; ++j)
+            if (i + j < 3) c = mfma(a[i], b[j], c);
+    return c;
+}
+
+// ------------------------------------------------------------------------------ memory
+// eight values of a row of D from column c on, 0 from D on (and without a row)
+template <class T>
+__device__ __forceinline__ void load8(const T *row, uint32_t c, uint32_t D, bool vec, float (&out)[8])
+{
+    if (row && vec && c + 8 <= D) {
+#pragma unroll
+        for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+            constexpr int n = 16 / sizeof(T);
+            const dg_rows::Pack<T, n> p = *reinterpret_cast<const dg_rows::Pack<T, n> *>(row + c + h * n);
+#pragma unroll
+            for (int i = 0; i < n; ++i) out[h * n + i] = (float)p.v[i];
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) out[i] = row && c + i < D ? (float)row[c + i] : 0.0f;
+}
+
+__device__ __forceinline__ void wave_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+inline bool wide_rows(const void *p, uint64_t ld, uint32_t D, uint32_t dtype)
+{
+    return dg_rows::rows_aligned(p, ld, dtype, 16) && D * dg_rows::item_bytes(dtype) % 16 == 0;
+}
+
+// kernels of the other files, by the rows' type
+void launch_forward(const Delta &d, uint32_t dtype, hipStream_t st);
+void launch_tokens(const Delta &d, uint32_t dtype, hipStream_t st);
+void launch_backward(const Delta &d, uint32_t dtype, hipStream_t st);
+void launch_gradients(const Delta &d, uint32_t dtype, hipStream_t st);
+
+}  // namespace dg_delta
