@@ -13,8 +13,17 @@ uint64_t slots_of(uint64_t N, uint32_t n_seq) { return N / kMark + n_seq; }
 
 size_t marks_bytes(uint64_t N, uint32_t n_seq, uint32_t H, uint32_t Dk, uint32_t Dv) { return (size_t)slots_of(N, n_seq) * H * Dk * Dv * sizeof(float); }
 size_t rows_bytes(uint64_t N, uint32_t H, uint32_t Dv) { return (size_t)(N * H * Dv * sizeof(float) + 15) / 16 * 16; }
-size_t slot_bytes(uint64_t N, uint32_t n_seq) { return (size_t)(slots_of(N, n_seq) * 4 + 15) / 16 * 16; }
 size_t padded(size_t n) { return (n + 15) / 16 * 16; }
+size_t slot_bytes(uint64_t N, uint32_t n_seq) { return padded(slots_of(N, n_seq) * 4); }
+
+// The workspace: T and P of the chunks and whose the chunks are, for either pass; then what the backward pass hands on.
+size_t forward_bytes(uint64_t N, uint32_t n_seq, uint32_t H) { return weight_bytes(N, n_seq, H) + chunk_bytes(N, n_seq); }
+
+void use_workspace(Delta &d, void *ws)
+{
+    d.weights = (Weights *)ws;
+    d.chunk_seq = (const uint32_t *)((char *)ws + weight_bytes(d.N, d.n_seq, d.H));
+}
 
 int check_sizes(const char *who, uint64_t N, uint32_t n_seq, const uint32_t *first, uint32_t Hk, uint32_t H, uint32_t Dk, uint32_t Dv, uint32_t dtype)
 {
@@ -44,9 +53,11 @@ extern "C" size_t dg_delta_rule_saved_bytes(uint64_t N, uint32_t n_seq, uint32_t
     return padded(marks_bytes(N, n_seq, H, Dk, Dv)) + rows_bytes(N, H, Dv);
 }
 
+extern "C" size_t dg_delta_rule_fwd_workspace_bytes(uint64_t N, uint32_t n_seq, uint32_t H) { return forward_bytes(N, n_seq, H); }
+
 extern "C" size_t dg_delta_rule_workspace_bytes(uint64_t N, uint32_t n_seq, uint32_t Hk, uint32_t H, uint32_t Dk, uint32_t Dv)
 {
-    return padded(marks_bytes(N, n_seq, H, Dk, Dv)) + rows_bytes(N, H, Dv) + slot_bytes(N, n_seq);
+    return forward_bytes(N, n_seq, H) + padded(marks_bytes(N, n_seq, H, Dk, Dv)) + rows_bytes(N, H, Dv) + slot_bytes(N, n_seq);
 }
 
 extern "C" int dg_delta_rule_fwd(const void *q, uint64_t ldq, const void *k, uint64_t ldk, const void *v, uint64_t ldv, const float *g, uint64_t ldg,
@@ -74,7 +85,13 @@ extern "C" int dg_delta_rule_fwd(const void *q, uint64_t ldq, const void *k, uin
     if (saved) d.marks = (float *)saved, d.u = (float *)((char *)saved + padded(marks_bytes(N, n_seq, H, Dk, Dv)));
     d.vec_q = wide_rows(q, ldq, Dk, dtype), d.vec_k = wide_rows(k, ldk, Dk, dtype), d.vec_v = wide_rows(v, ldv, Dv, dtype);
     if (!saved && N <= kFewTokens * n_seq) launch_tokens(d, dtype, (hipStream_t)stream);
-    else launch_forward(d, dtype, (hipStream_t)stream);
+    else {
+        const size_t bytes = forward_bytes(N, n_seq, H);
+        DG_REQUIRE(ws && dg::aligned(ws, 16) && ws_bytes >= bytes, DG_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", who, bytes, ws ? ws_bytes : 0);
+        use_workspace(d, ws);
+        if (N) launch_weights(d, dtype, false, (hipStream_t)stream);
+        launch_forward(d, dtype, (hipStream_t)stream);
+    }
     return dg::launch_status(who);
 }
 
@@ -105,8 +122,11 @@ extern "C" int dg_delta_rule_bwd(const void *q, uint64_t ldq, const void *k, uin
     d.dout = do_, d.lddo = lddo, d.dq = dq, d.dk = dk, d.dv = dv, d.lddq = lddq, d.lddk = lddk, d.lddv = lddv, d.dg = dg, d.dbeta = dbeta, d.lddg = lddg, d.lddb = lddbeta;
     d.first = first, d.N = N, d.n_seq = n_seq, d.Hk = Hk, d.H = H, d.Dk = Dk, d.Dv = Dv, d.reverse = reverse, d.scale = scale, d.slots = (uint32_t)slots_of(N, n_seq);
     d.marks = (float *)const_cast<void *>(saved), d.u = (float *)((char *)const_cast<void *>(saved) + marks);
-    d.dmarks = (float *)ws, d.dr = (float *)((char *)ws + marks), d.slot_seq = (const uint32_t *)((char *)ws + marks + rows_bytes(N, H, Dv));
+    use_workspace(d, ws);
+    char *const rest = (char *)ws + forward_bytes(N, n_seq, H);
+    d.dmarks = (float *)rest, d.dr = (float *)(rest + marks), d.slot_seq = (const uint32_t *)(rest + marks + rows_bytes(N, H, Dv));
     d.vec_q = wide_rows(q, ldq, Dk, dtype), d.vec_k = wide_rows(k, ldk, Dk, dtype), d.vec_v = wide_rows(v, ldv, Dv, dtype), d.vec_o = wide_rows(do_, lddo, Dv, dtype);
+    if (N) launch_weights(d, dtype, true, (hipStream_t)stream);
     launch_backward(d, dtype, (hipStream_t)stream);
     if (N) launch_gradients(d, dtype, (hipStream_t)stream);
     return dg::launch_status(who);

@@ -1,8 +1,9 @@
-// The gated delta rule in chunks of 32 tokens: what a workgroup's producing wavefront lays out in LDS for the others, of which each has 16 columns of the
-// memory in its registers, all along the sequence.  Internal.
+// The gated delta rule in chunks of 32 tokens, along the sequences.  Internal.
 //
-// With all rows of 16 columns in one wavefront a chunk needs no exchange between wavefronts: results of the matrix unit are the right operands of the next
-// product (split_rows).  Left operands depend on q, k, g and beta alone; one more wavefront makes them, a chunk ahead.
+// A wavefront has all rows of 16 columns of the memory in its registers, so that a chunk needs no exchange between wavefronts: results of the matrix unit
+// are the right operands of the next product (split_rows).  Left operands are the same for all columns and lie in LDS.  Those that depend on q, k, g and beta
+// alone (T and P) are made by a launch of its own (delta_weights.hip), for all chunks at once, in the workspace, as they are to lie in LDS, and come by loads that write there;
+// K and Q come through registers, which cut them into pieces and turn them.
 #pragma once
 #include "delta_common.h"
 
@@ -10,28 +11,31 @@ namespace dg_delta {
 
 constexpr int kChunk = 32;
 constexpr int kPitch = kChunk + 8;      // of rows of 32 values: 16 lanes that read 16 bytes each of neighbouring rows meet all banks once
-constexpr int kMostWaves = 4;           // with columns, in a workgroup
+constexpr int kPage = 1024;             // what a wavefront fetches at once
 
-// Left operands of a chunk; columns in the order of `place`
+// The matrix unit's result holds rows 4 q to 4 q + 3 of 16 with lane (column, q); two such results are the right operand of a sum over 32 rows, where lane
+// (column, q) has places 8 q to 8 q + 7.  So that sums go over tokens, or columns of keys, in their own order, row r of result h (of two) is number 8 (r / 4) + 4 h + r % 4.
+// Rows of left operands lie by result: number i at `line(i)`.
+__host__ __device__ constexpr uint32_t line(uint32_t i) { return (i & ~31u) | (i >> 2 & 1) << 4 | (i >> 3 & 3) << 2 | (i & 3); }
+
 template <class T, int KS, bool kBackward>
-struct Operands {
+struct alignas(16) Keys {
     static constexpr int n = Pieces<T>::n, DK = 32 * KS;
     uint16_t K[n][kChunk][DK + 8];
     uint16_t KT[n][DK][kPitch];
     uint16_t Q[n][kBackward ? DK : kChunk][kBackward ? kPitch : DK + 8];       // backward: Q^T
-    uint16_t inverse[3][kChunk][kPitch], P[3][kChunk][kPitch];                 // T; backward: T^T, P^T
+};
+
+struct alignas(kPage) Weights {
+    uint16_t inverse[3][kChunk][kPitch], P[3][kChunk][kPitch];                 // T and P; backward: T^T and P^T
     float beta[kChunk], read[kChunk], query[kChunk], until[kChunk];            // beta, beta e^G, scale e^G, e^(G[last] - G)
     float whole;                                                               // e^G[last]
 };
 
-// The producing wavefront's own
-template <class T, int KS, bool kBackward>
-struct Scratch {
-    double G[kChunk];
-    float beta[kChunk];
-    float A[2][16][20], inverse[2][16][20];         // A^T and T of the diagonal blocks
-    uint16_t Q[kBackward ? Pieces<T>::n : 1][kBackward ? kChunk : 1][kBackward ? 32 * KS + 8 : 8];
-};
+// In the workspace: a chunk's slot has those of its heads.  A sequence's first slot is floor(begin / 32) + its number, which leaves room for all.
+inline uint64_t chunk_slots(uint64_t N, uint32_t n_seq) { return N / kChunk + n_seq; }
+
+__device__ __forceinline__ uint64_t first_chunk(const Span &s, uint32_t seq) { return s.begin / kChunk + seq; }
 
 __device__ __forceinline__ bf16x8 left(const uint16_t *row) { return operand(*reinterpret_cast<const u32x4 *>(row)); }
 
@@ -49,298 +53,193 @@ __device__ __forceinline__ void load8_aligned(const T *row, uint32_t c, uint32_t
     }
 }
 
+// eight values of a row of D from column c on, 0 from D on and without a row
+template <class T>
+__device__ __forceinline__ void eight(const T *row, uint32_t c, uint32_t D, bool in, bool vec, float (&out)[8])
+{
+    if (vec) {
+        dg_rows::Pack<T, 8> p;
+        load8_aligned<T>(row, c, D, in, p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) out[i] = (float)p.v[i];
+    } else
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const bool here = in && c + i < D;
+            const T v = row[here ? c + i : 0];
+            out[i] = here ? (float)v : 0.0f;
+        }
+}
+
+// ------------------------------------------------------------------------------ along a sequence
+constexpr int kMostWaves = 4;           // in a workgroup
+
 template <class T, int KS, bool kBackward>
-struct Producer {
-    using Ops = Operands<T, KS, kBackward>;
-    using Own = Scratch<T, KS, kBackward>;
-    static constexpr int n = Ops::n, kItems = 2 * KS;
-
-    const Delta &d;
-    const Span &span;
-    const uint32_t head, hk, lane;
-    dg_rows::Pack<T, 8> k[kItems], q[kItems];
-    float g, beta;
-
-    __device__ __forceinline__ Producer(const Delta &d, const Span &span, uint32_t head, uint32_t lane)
-        : d(d), span(span), head(head), hk(head / (d.H / d.Hk)), lane(lane) {}
-
-    // item `it` of a lane: eight columns of a token of the chunk
-    __device__ __forceinline__ uint32_t token(int it) const { return it * (16 / KS) + lane / (4 * KS); }
-    __device__ __forceinline__ uint32_t column() const { return lane % (4 * KS) * 8; }
-
-    // rows of chunk c, on their way into registers if vectors divide them; otherwise produce() loads them, value by value
-    __device__ __forceinline__ void fetch(uint32_t c)
-    {
-        if (d.vec_q && d.vec_k) {
-            const T *at_k = (const T *)d.k + hk * d.Dk, *at_q = (const T *)d.q + hk * d.Dk;
-#pragma unroll
-            for (int it = 0; it < kItems; ++it) {
-                const uint32_t t = c * kChunk + token(it);
-                const bool in = t < span.len;
-                const uint64_t row = span.row(in ? t : c * kChunk);
-                load8_aligned<T>(at_k + row * d.ldk, column(), d.Dk, in, k[it]);
-                load8_aligned<T>(at_q + row * d.ldq, column(), d.Dk, in, q[it]);
-            }
-        }
-        const uint32_t t = c * kChunk + lane % 32;
-        const uint64_t row = t < span.len ? span.row(t) : 0;
-        g = t < span.len ? fmaxf(d.g[row * d.ldg + head], kShut) : 0.0f;
-        beta = t < span.len ? d.beta[row * d.ldb + head] : 0.0f;
-    }
-
-    // eight values of a token: as they lie in its row, and each into its column's row
-    template <int pitch>
-    __device__ __forceinline__ static void put(const dg_rows::Pack<T, 8> &x, uint32_t t, uint32_t col, uint16_t (*rows)[kChunk][pitch], uint16_t (*columns)[32 * KS][kPitch])
-    {
-        float v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)x.v[i];
-        uint32_t w[n][4];
-        split<n, 8>(v, w);
-#pragma unroll
-        for (int p = 0; p < n; ++p) {
-            if (rows) {
-                *reinterpret_cast<u32x2 *>(&rows[p][t][place(col)]) = (u32x2){w[p][0], w[p][1]};
-                *reinterpret_cast<u32x2 *>(&rows[p][t][place(col + 4)]) = (u32x2){w[p][2], w[p][3]};
-            }
-            if (columns)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) columns[p][col + i][place(t)] = (uint16_t)(w[p][i / 2] >> (i % 2 * 16));
-        }
-    }
-
-    // four values side by side, in pieces
-    __device__ __forceinline__ static void put4(const float (&v)[4], uint16_t (*rows)[kChunk][kPitch], uint32_t row, uint32_t col)
-    {
-        uint32_t w[3][2];
-        split<3, 4>(v, w);
-#pragma unroll
-        for (int p = 0; p < 3; ++p) *reinterpret_cast<u32x2 *>(&rows[p][row][place(col)]) = (u32x2){w[p][0], w[p][1]};
-    }
-
-    // what never changes: the blocks of T and P behind the diagonal
-    __device__ __forceinline__ static void clear(Ops &o, uint32_t lane)
-    {
-        const float none[4] = {};
-        const uint32_t r = lane % 16, c = lane / 16 * 4;
-        put4(none, o.inverse, kBackward ? 16 + r : r, kBackward ? c : 16 + c);
-        put4(none, o.P, kBackward ? 16 + r : r, kBackward ? c : 16 + c);
-    }
-
-    // the product of two 16-row blocks of K or Q
-    template <int pa, int pb>
-    __device__ __forceinline__ f32x4 rows_product(const uint16_t (*a)[kChunk][pa], uint32_t ra, const uint16_t (*b)[kChunk][pb], uint32_t rb) const
-    {
-        f32x4 acc = {};
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            bf16x8 x[n], y[n];
-#pragma unroll
-            for (int p = 0; p < n; ++p) {
-                x[p] = left(&a[p][ra + lane % 16][s * 32 + lane / 16 * 8]);
-                y[p] = left(&b[p][rb + lane % 16][s * 32 + lane / 16 * 8]);
-            }
-            acc = multiply<n, n>(x, y, acc);
-        }
-        return acc;
-    }
-
-    __device__ __forceinline__ void produce(Ops &o, Own &own, uint32_t c, uint32_t next, uint32_t chunks)
-    {
-        constexpr int kRowPitch = 32 * KS + 8;
-        auto q_rows = [&] {
-            if constexpr (kBackward) return own.Q;
-            else return o.Q;
-        }();
-        auto put_both = [&](const dg_rows::Pack<T, 8> &k8, const dg_rows::Pack<T, 8> &q8, uint32_t t) {
-            put<kRowPitch>(k8, t, column(), o.K, o.KT);
-            if constexpr (kBackward) put<kRowPitch>(q8, t, column(), own.Q, o.Q);
-            else put<kRowPitch>(q8, t, column(), o.Q, nullptr);
-        };
-        if (d.vec_q && d.vec_k) {
-#pragma unroll
-            for (int it = 0; it < kItems; ++it) put_both(k[it], q[it], token(it));
-        } else
-#pragma unroll 1
-            for (int it = 0; it < kItems; ++it) {
-                const uint32_t t = c * kChunk + token(it);
-                dg_rows::Pack<T, 8> k8, q8;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const bool in = t < span.len && column() + i < d.Dk;
-                    const uint64_t row = span.row(in ? t : c * kChunk);
-                    const uint32_t at = hk * d.Dk + (in ? column() + i : 0);
-                    k8.v[i] = in ? ((const T *)d.k)[row * d.ldk + at] : (T)0.0f;
-                    q8.v[i] = in ? ((const T *)d.q)[row * d.ldq + at] : (T)0.0f;
-                }
-                put_both(k8, q8, token(it));
-            }
-        double G = (double)g;
-#pragma unroll
-        for (int s = 1; s < kChunk; s *= 2) {
-            const double before = __shfl_up(G, s, kChunk);
-            if (lane % kChunk >= (uint32_t)s) G += before;
-        }
-        const double last = __shfl(G, kChunk - 1, kChunk);
-        if (lane < kChunk) {
-            const float since = expf((float)G);
-            own.G[lane] = G;
-            own.beta[lane] = o.beta[lane] = beta;
-            o.read[lane] = beta * since;
-            o.query[lane] = d.scale * since;
-            o.until[lane] = expf((float)(last - G));
-            if (lane == 0) o.whole = expf((float)last);
-        }
-        if (next < chunks) fetch(next);
-        wave_fence();
-        const uint32_t c16 = lane % 16, r4 = lane / 16 * 4;
-        // P
-#pragma unroll
-        for (int b = 0; b < 3; ++b) {           // blocks (row of tokens i, row of tokens j): (0, 0), (1, 0), (1, 1)
-            const uint32_t bi = b ? 16 : 0, bj = b == 2 ? 16 : 0;
-            f32x4 acc;
-            if constexpr (kBackward) acc = rows_product<kRowPitch, kRowPitch>(q_rows, bi, o.K, bj);      // rows i, columns j
-            else acc = rows_product<kRowPitch, kRowPitch>(o.K, bj, q_rows, bi);                          // rows j, columns i
-            float v[4];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const uint32_t i = bi + (kBackward ? r4 + x : c16), j = bj + (kBackward ? c16 : r4 + x);
-                v[x] = i >= j ? d.scale * acc[x] * expf((float)(own.G[i] - own.G[j])) : 0.0f;
-            }
-            if (kBackward) put4(v, o.P, bj + c16, bi + r4);
-            else put4(v, o.P, bi + c16, bj + r4);
-        }
-        // A: the diagonal blocks to LDS, the other stays as an operand
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const f32x4 acc = rows_product<kRowPitch, kRowPitch>(o.K, b * 16, o.K, b * 16);
-            f32x4 v;
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {       // A[r4 + x, c16]
-                const uint32_t i = b * 16 + r4 + x, j = b * 16 + c16;
-                v[x] = i > j ? own.beta[i] * acc[x] * expf((float)(own.G[i] - own.G[j])) : 0.0f;
-            }
-            *reinterpret_cast<f32x4 *>(&own.A[b][c16][r4]) = v;
-        }
-        f32x4 a21;
-        {
-            // forward: rows i, columns j; backward: rows j, columns i
-            const f32x4 acc = kBackward ? rows_product<kRowPitch, kRowPitch>(o.K, 0, o.K, 16) : rows_product<kRowPitch, kRowPitch>(o.K, 16, o.K, 0);
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const uint32_t i = 16 + (kBackward ? c16 : r4 + x), j = kBackward ? r4 + x : c16;
-                a21[x] = own.beta[i] * acc[x] * expf((float)(own.G[i] - own.G[j]));
-            }
-        }
-        wave_fence();
-        // T (1 + A) = 1 by rows: lane (block, row r), t[j] = [j = r] - sum over m > j of t[m] A[m, j]
-        const uint32_t block = lane / 16 % 2;
-        float t[16];
-#pragma unroll
-        for (int j = 15; j >= 0; --j) {
-            float sum = 0.0f;
-#pragma unroll
-            for (int m4 = j / 4 * 4; m4 < 16; m4 += 4) {
-                const f32x4 a = *reinterpret_cast<const f32x4 *>(&own.A[block][j][m4]);
-#pragma unroll
-                for (int x = 0; x < 4; ++x)
-                    if (m4 + x > j) sum = fmaf(t[m4 + x], a[x], sum);
-            }
-            t[j] = (j == (int)c16 ? 1.0f : 0.0f) - sum;
-        }
-        if (lane < 32)
-#pragma unroll
-            for (int j = 0; j < 16; j += 4) {
-                *reinterpret_cast<f32x4 *>(&own.inverse[block][c16][j]) = (f32x4){t[j], t[j + 1], t[j + 2], t[j + 3]};
-                if (!kBackward) {
-                    const float v[4] = {t[j], t[j + 1], t[j + 2], t[j + 3]};
-                    put4(v, o.inverse, block * 16 + c16, block * 16 + j);
-                }
-            }
-        wave_fence();
-        if (kBackward && lane < 32)             // rows of T^T
-#pragma unroll
-            for (int j = 0; j < 16; j += 4) {
-                const float v[4] = {own.inverse[block][j][c16], own.inverse[block][j + 1][c16], own.inverse[block][j + 2][c16], own.inverse[block][j + 3][c16]};
-                put4(v, o.inverse, block * 16 + c16, block * 16 + j);
-            }
-        // the block below the diagonal, -T22 A21 T11, in fp32: forward as its transpose (A21^T T22^T, then T11^T times that), so that a lane has four
-        // values of a row of T in either case
-        const f32x4 t22 = *reinterpret_cast<const f32x4 *>(&own.inverse[1][c16][r4]);
-        f32x4 w = {}, x = {};
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const float t11 = own.inverse[0][r4 + s][c16];
-            w = __builtin_amdgcn_mfma_f32_16x16x4f32(a21[s], kBackward ? t11 : t22[s], w, 0, 0, 0);
-        }
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const float t11 = own.inverse[0][r4 + s][c16];
-            x = __builtin_amdgcn_mfma_f32_16x16x4f32(kBackward ? t22[s] : t11, w[s], x, 0, 0, 0);
-        }
-        const float v[4] = {-x[0], -x[1], -x[2], -x[3]};
-        // forward: lane i, rows j; backward: lane j, rows i
-        if (kBackward) put4(v, o.inverse, c16, 16 + r4);
-        else put4(v, o.inverse, 16 + c16, r4);
-    }
+struct Operands {
+    Weights weight;
+    Keys<T, KS, kBackward> key;
 };
 
-// Buffers: two if they fit, so that operands are made while others are used
+// Buffers: two if they fit, so that a chunk's operands come while the one before is worked on
 template <class T, int KS, bool kBackward>
 struct Room {
-    static constexpr int kBuffers = 2 * sizeof(Operands<T, KS, kBackward>) + sizeof(Scratch<T, KS, kBackward>) <= 160 * 1024 ? 2 : 1;
+    static constexpr int kBuffers = 2 * sizeof(Operands<T, KS, kBackward>) <= 160 * 1024 ? 2 : 1;
     Operands<T, KS, kBackward> ops[kBuffers];
-    Scratch<T, KS, kBackward> own;
 };
 
-// The roles of a workgroup along a sequence's chunks.  use(operands, i): the i-th chunk that is taken.
-template <class T, int KS, bool kBackward, class Use>
-__device__ __forceinline__ void along(const Delta &d, const Span &span, uint32_t head, bool producer, Room<T, KS, kBackward> &room, uint32_t chunks, Use use)
+// eight values of a token: as they lie in its row, and each into its column's row
+template <int n, int KS>
+__device__ __forceinline__ void put(const float (&v)[8], uint32_t t, uint32_t col, uint16_t (*rows)[kChunk][32 * KS + 8], uint16_t (*columns)[32 * KS][kPitch])
 {
-    constexpr int kBuffers = Room<T, KS, kBackward>::kBuffers;
-    if (chunks == 0) return;
-    if (producer) {
-        Producer<T, KS, kBackward> p(d, span, head, threadIdx.x % 64);
-        auto chunk = [&](uint32_t i) { return kBackward ? chunks - 1 - i : i; };        // past the end: one that there is not
-        p.fetch(chunk(0));
-        auto produce = [&](uint32_t i) {
-            // the next chunk's rows are fetched on the way
-            p.produce(room.ops[i % kBuffers], room.own, chunk(i), chunk(i + 1), chunks);
-        };
-        if (kBuffers == 2) produce(0);
-        __syncthreads();
-        for (uint32_t i = 0; i < chunks; ++i) {
-            if (kBuffers == 2) {
-                if (i + 1 < chunks) produce(i + 1);
-                __syncthreads();
-            } else {
-                produce(i);
-                __syncthreads();
-                __syncthreads();
-            }
-        }
-    } else {
-        __syncthreads();
-        for (uint32_t i = 0; i < chunks; ++i) {
-            if (kBuffers == 1) __syncthreads();
-            use(room.ops[i % kBuffers], i);
-            __syncthreads();
-        }
+    uint32_t w[n][4];
+    split<n, 8>(v, w);
+#pragma unroll
+    for (int p = 0; p < n; ++p) {
+        if (rows) *reinterpret_cast<u32x4 *>(&rows[p][line(t)][col]) = (u32x4){w[p][0], w[p][1], w[p][2], w[p][3]};
+        if (columns)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) columns[p][line(col + i)][t] = (uint16_t)(w[p][i / 2] >> (i % 2 * 16));
     }
 }
 
-// columns that a workgroup's wavefronts take, and how many workgroups a head has
-struct Columns { uint32_t waves, groups; };
+// K and Q of a chunk on their way to LDS: a workgroup has at least KS wavefronts, so that two vectors of each are enough for a lane
+template <class T, int KS, bool kBackward>
+struct Rows {
+    static constexpr int n = Pieces<T>::n;
+    const T *q, *k;
+    uint64_t ldq, ldk;
+    uint32_t Dk, wave, waves, lane;
+    bool vec;
+    Span span;
+    dg_rows::Pack<T, 8> qs[2], ks[2];
+
+    __device__ __forceinline__ uint32_t token(int i) const { return (i * waves + wave) * (16 / KS) + lane / (4 * KS); }
+    __device__ __forceinline__ uint32_t column() const { return lane % (4 * KS) * 8; }
+
+    __device__ __forceinline__ void fetch(uint32_t c)
+    {
+        if (!vec) return;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t t = c * kChunk + token(i);
+            const bool in = token(i) < kChunk && t < span.len;
+            const uint64_t row = span.row(in ? t : c * kChunk);
+            load8_aligned<T>(k + row * ldk, column(), Dk, in, ks[i]);
+            load8_aligned<T>(q + row * ldq, column(), Dk, in, qs[i]);
+        }
+    }
+
+    __device__ __forceinline__ void store(uint32_t c, Keys<T, KS, kBackward> &to)
+    {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t t = token(i);
+            if (t >= kChunk) continue;
+            float x[8], y[8];
+            if (vec) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    x[j] = (float)ks[i].v[j];
+                    y[j] = (float)qs[i].v[j];
+                }
+            } else {
+                const bool in = c * kChunk + t < span.len;
+                const uint64_t row = span.row(in ? c * kChunk + t : c * kChunk);
+                eight<T>(k + row * ldk, column(), Dk, in, false, x);
+                eight<T>(q + row * ldq, column(), Dk, in, false, y);
+            }
+            put<n, KS>(x, t, column(), to.K, to.KT);
+            if constexpr (kBackward) put<n, KS>(y, t, column(), nullptr, to.Q);
+            else put<n, KS>(y, t, column(), to.Q, nullptr);
+        }
+    }
+};
+
+// use(operands, chunk) for a sequence's chunks in turn, backward from the last one on
+template <class T, int KS, bool kBackward, class Use>
+__device__ __forceinline__ void along(const Delta &d, const Span &span, uint32_t seq, uint32_t head, Room<T, KS, kBackward> &room, uint32_t wave, uint32_t waves, Use use)
+{
+    constexpr int kBuffers = Room<T, KS, kBackward>::kBuffers;
+    const uint32_t chunks = (span.len + kChunk - 1) / kChunk, hk = head / (d.H / d.Hk);
+    if (chunks == 0) return;
+    const uint64_t slot0 = first_chunk(span, seq);
+    auto chunk = [&](uint32_t i) { return kBackward ? chunks - 1 - i : i; };
+    Rows<T, KS, kBackward> rows = {(const T *)d.q + hk * d.Dk, (const T *)d.k + hk * d.Dk, d.ldq, d.ldk, d.Dk, wave, waves, threadIdx.x % 64, d.vec_q && d.vec_k, span, {}, {}};
+    auto weights = [&](uint32_t i) {
+        const uint8_t *from = (const uint8_t *)(d.weights + (slot0 + chunk(i)) * d.H + head) + threadIdx.x % 64 * 16;
+        uint8_t *to = (uint8_t *)&room.ops[i % kBuffers].weight;
+        for (uint32_t at = wave * kPage; at < sizeof(Weights); at += waves * kPage)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)(from + at), (__attribute__((address_space(3))) uint32_t *)(to + at), 16, 0, 0);
+    };
+    rows.fetch(chunk(0));
+    weights(0);
+    rows.store(chunk(0), room.ops[0].key);
+    for (uint32_t i = 0; i < chunks; ++i) {
+        __builtin_amdgcn_s_waitcnt(0x0f70);         // all loads, those that write to LDS among them
+        __syncthreads();
+        const bool more = i + 1 < chunks;
+        if (more) {
+            rows.fetch(chunk(i + 1));
+            if (kBuffers == 2) weights(i + 1);
+        }
+        use(room.ops[i % kBuffers], chunk(i));
+        if (kBuffers == 1) {
+            __syncthreads();
+            if (more) weights(i + 1);
+        }
+        if (more) rows.store(chunk(i + 1), room.ops[(i + 1) % kBuffers].key);
+    }
+}
+
+// How many wavefronts of a workgroup have columns, how many there are (those that fetch K and Q alone among them), and how many workgroups a head has
+struct Columns { uint32_t with, waves, groups; };
 
 inline Columns columns_of(const Delta &d)
 {
-    const uint32_t all = (d.Dv + 15) / 16;
+    const uint32_t all = (d.Dv + 15) / 16, least = d.Dk <= 32 ? 1 : d.Dk <= 64 ? 2 : 4;
     const uint64_t units = (uint64_t)d.n_seq * d.H;
-    uint32_t waves = all < (uint32_t)kMostWaves ? all : kMostWaves;
-    while (waves > 1 && units * ((all + waves - 1) / waves) < 256) waves = (waves + 1) / 2;        // few heads: as many workgroups as there are compute units
-    return {waves, (all + waves - 1) / waves};
+    uint32_t with = all < (uint32_t)kMostWaves ? all : kMostWaves;
+    while (with > 1 && units * ((all + with - 1) / with) < 256) with = (with + 1) / 2;        // few heads: as many workgroups as there are compute units
+    return {with, with < least ? least : with, (all + with - 1) / with};
 }
 
 constexpr uint64_t kMostGroups = 1 << 22;      // of a launch: its lanes have to stay below 2^32
+
+// Memories in registers: result t of 2 KS has rows 32 (t / 2) + 8 q + 4 (t % 2) on with lane (column, q)
+template <int KS>
+__device__ __forceinline__ void load_memory(const float *from, uint32_t Dk, uint32_t Dv, bool in, uint32_t r8, f32x4 (&S)[2 * KS])
+{
+#pragma unroll
+    for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const uint32_t r = t / 2 * 32 + r8 + t % 2 * 4 + x;
+            S[t][x] = from && in && r < Dk ? from[(uint64_t)r * Dv] : 0.0f;
+        }
+}
+
+template <int KS>
+__device__ __forceinline__ void store_memory(float *to, uint32_t Dk, uint32_t Dv, bool in, uint32_t r8, const f32x4 (&S)[2 * KS])
+{
+#pragma unroll
+    for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const uint32_t r = t / 2 * 32 + r8 + t % 2 * 4 + x;
+            if (in && r < Dk) to[(uint64_t)r * Dv] = S[t][x];
+        }
+}
+
+// A lane's eight tokens of a chunk in one column of rows [N, ld], 0 where there is no token
+template <class T>
+__device__ __forceinline__ void load_column(const T *p, uint64_t ld, const Span &span, uint32_t t0, bool in, T (&out)[8])
+{
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+        const bool here = in && t0 + x < span.len;
+        const T value = p[span.row(here ? t0 + x : 0) * ld];
+        out[x] = here ? value : (T)0.0f;
+    }
+}
 
 }  // namespace dg_delta

@@ -26,6 +26,8 @@ constexpr int kMaxD = 128;
 // e^-104 is 0 in fp32: below that a gate is shut.  Logarithms are cut off here so that their differences stay numbers.
 constexpr float kShut = -200.0f;
 
+struct Weights;
+
 struct Delta {
     const void *q, *k, *v;
     const float *g, *beta;
@@ -42,7 +44,8 @@ struct Delta {
     float *dg, *dbeta;
     uint64_t lddg, lddb;
     const uint32_t *first;
-    const uint32_t *slot_seq;
+    const uint32_t *slot_seq, *chunk_seq;       // whose the slots of 64 and of 32 tokens are
+    Weights *weights;                           // [chunk slots][H]
     uint64_t N;
     uint32_t n_seq, Hk, H, Dk, Dv, reverse, slots;
     float scale;
@@ -111,17 +114,13 @@ __device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&out)[n])
     for (int p = 0; p < n; ++p) out[p] = operand((u32x4){w[p][0], w[p][1], w[p][2], w[p][3]});
 }
 
-// Two 16-row results of the matrix unit, one above the other, as the right operand of a product that sums over their rows: lane (column c, group q) has rows
-// 4 q to 4 q + 3 of each, and takes them for its eight places.  Left operands come with their columns in that order (`place`).
+// Two 16-row results of the matrix unit as the right operand of a product that sums over their rows
 template <int n>
 __device__ __forceinline__ void split_rows(const f32x4 &a, const f32x4 &b, bf16x8 (&out)[n])
 {
     const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
     split8<n>(x, out);
 }
-
-// place of column c among the columns of a left operand; runs of four stay together
-__device__ __forceinline__ uint32_t place(uint32_t c) { return (c & ~31u) | (c >> 2 & 3) << 3 | (c >> 4 & 1) << 2 | (c & 3); }
 
 __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
@@ -168,6 +167,10 @@ inline bool wide_rows(const void *p, uint64_t ld, uint32_t D, uint32_t dtype)
 }
 
 // kernels of the other files, by the rows' type
+// bytes of `weights` and of `chunk_seq`
+size_t weight_bytes(uint64_t N, uint32_t n_seq, uint32_t H);
+size_t chunk_bytes(uint64_t N, uint32_t n_seq);
+void launch_weights(const Delta &d, uint32_t dtype, bool backward, hipStream_t st);
 void launch_forward(const Delta &d, uint32_t dtype, hipStream_t st);
 void launch_tokens(const Delta &d, uint32_t dtype, hipStream_t st);
 void launch_backward(const Delta &d, uint32_t dtype, hipStream_t st);

@@ -6,53 +6,30 @@ namespace {
 using namespace dg_delta;
 
 template <class T, int KS>
-__global__ void __launch_bounds__((kMostWaves + 1) * 64)
-delta_fwd_kernel(Delta d, uint32_t waves, uint32_t groups, uint64_t from)
+__global__ void __launch_bounds__(kMostWaves * 64)
+delta_fwd_kernel(Delta d, uint32_t with, uint32_t groups, uint64_t from)
 {
     __shared__ alignas(16) Room<T, KS, false> room;
     constexpr int n = Pieces<T>::n, kTiles = 2 * KS;
-    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c16 = lane % 16, r4 = lane / 16 * 4;
-    const bool producer = wave == waves;
-    if (producer)
-        for (auto &ops : room.ops) Producer<T, KS, false>::clear(ops, lane);
+    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = blockDim.x / 64, c16 = lane % 16, r8 = lane / 16 * 8;
     const uint64_t unit = from + blockIdx.x;
-    const uint32_t head = (uint32_t)(unit / groups % d.H), seq = (uint32_t)(unit / groups / d.H), col = ((uint32_t)(unit % groups) * waves + wave) * 16 + c16;
+    const uint32_t head = (uint32_t)(unit / groups % d.H), seq = (uint32_t)(unit / groups / d.H), col = ((uint32_t)(unit % groups) * with + wave) * 16 + c16;
     const Span span = span_of(d, seq);
-    const uint32_t chunks = (span.len + kChunk - 1) / kChunk;
-    const bool in = !producer && col < d.Dv;
+    const bool in = wave < with && col < d.Dv;
     const uint64_t memory = ((uint64_t)seq * d.H + head) * d.Dk * d.Dv + col;
     f32x4 S[kTiles];
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            const uint32_t r = t * 16 + r4 + x;
-            S[t][x] = d.s0 && in && r < d.Dk ? d.s0[memory + (uint64_t)r * d.Dv] : 0.0f;
-        }
-    T v[8];
-    auto fetch = [&](uint32_t c) {
-#pragma unroll
-        for (int x = 0; x < 8; ++x) {
-            const uint32_t t = c * kChunk + x / 4 * 16 + r4 + x % 4;
-            const bool here = in && t < span.len;
-            const T value = ((const T *)d.v)[span.row(here ? t : 0) * d.ldv + head * d.Dv + (here ? col : 0)];
-            v[x] = here ? value : (T)0.0f;
-        }
-    };
-    if (!producer && chunks) fetch(0);
-    along<T, KS, false>(d, span, head, producer, room, chunks, [&](const Operands<T, KS, false> &o, uint32_t c) {
-        if (d.marks && c % (kMark / kChunk) == 0) {
-            float *to = d.marks + ((uint64_t)(first_slot(span, seq) + c / (kMark / kChunk)) * d.H + head) * d.Dk * d.Dv + col;
-#pragma unroll
-            for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-                for (int x = 0; x < 4; ++x)
-                    if (in && t * 16 + r4 + x < d.Dk) to[(uint64_t)(t * 16 + r4 + x) * d.Dv] = S[t][x];
-        }
+    load_memory<KS>(d.s0 ? d.s0 + memory : nullptr, d.Dk, d.Dv, in, r8, S);
+    const T *values = (const T *)d.v + head * d.Dv + (in ? col : 0);
+    T next[8];
+    if (span.len) load_column<T>(values, d.ldv, span, r8, in, next);
+    along<T, KS, false>(d, span, seq, head, room, wave, waves, [&](const Operands<T, KS, false> &o, uint32_t c) {
+        if (wave >= with) return;
+        if (d.marks && c % (kMark / kChunk) == 0)
+            store_memory<KS>(d.marks + ((uint64_t)(first_slot(span, seq) + c / (kMark / kChunk)) * d.H + head) * d.Dk * d.Dv + col, d.Dk, d.Dv, in, r8, S);
         float value[8];
 #pragma unroll
-        for (int x = 0; x < 8; ++x) value[x] = (float)v[x];
-        fetch(c + 1);
+        for (int x = 0; x < 8; ++x) value[x] = (float)next[x];
+        load_column<T>(values, d.ldv, span, (c + 1) * kChunk + r8, in, next);
         f32x4 ks[2] = {}, qs[2] = {};
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
@@ -62,18 +39,18 @@ delta_fwd_kernel(Delta d, uint32_t waves, uint32_t groups, uint64_t from)
             for (int h = 0; h < 2; ++h) {
                 bf16x8 a[n];
 #pragma unroll
-                for (int p = 0; p < n; ++p) a[p] = left(&o.K[p][h * 16 + c16][s * 32 + r4 * 2]);
+                for (int p = 0; p < n; ++p) a[p] = left(&o.key.K[p][h * 16 + c16][s * 32 + r8]);
                 ks[h] = multiply<n, 3>(a, sp, ks[h]);
 #pragma unroll
-                for (int p = 0; p < n; ++p) a[p] = left(&o.Q[p][h * 16 + c16][s * 32 + r4 * 2]);
+                for (int p = 0; p < n; ++p) a[p] = left(&o.key.Q[p][h * 16 + c16][s * 32 + r8]);
                 qs[h] = multiply<n, 3>(a, sp, qs[h]);
             }
         }
         f32x4 r[2], u[2], until[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const f32x4 beta = *reinterpret_cast<const f32x4 *>(&o.beta[h * 16 + r4]), read = *reinterpret_cast<const f32x4 *>(&o.read[h * 16 + r4]);
-            until[h] = *reinterpret_cast<const f32x4 *>(&o.until[h * 16 + r4]);
+            const f32x4 beta = *reinterpret_cast<const f32x4 *>(&o.weight.beta[r8 + h * 4]), read = *reinterpret_cast<const f32x4 *>(&o.weight.read[r8 + h * 4]);
+            until[h] = *reinterpret_cast<const f32x4 *>(&o.weight.until[r8 + h * 4]);
 #pragma unroll
             for (int x = 0; x < 4; ++x) r[h][x] = beta[x] * value[h * 4 + x] - read[x] * ks[h][x];
         }
@@ -83,20 +60,20 @@ delta_fwd_kernel(Delta d, uint32_t waves, uint32_t groups, uint64_t from)
         for (int h = 0; h < 2; ++h) {
             bf16x8 a[3];
 #pragma unroll
-            for (int p = 0; p < 3; ++p) a[p] = left(&o.inverse[p][h * 16 + c16][r4 * 2]);
+            for (int p = 0; p < 3; ++p) a[p] = left(&o.weight.inverse[p][h * 16 + c16][r8]);
             u[h] = multiply<3, 3>(a, right, (f32x4){});
         }
         split_rows<3>(u[0], u[1], right);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const f32x4 query = *reinterpret_cast<const f32x4 *>(&o.query[h * 16 + r4]);
+            const f32x4 query = *reinterpret_cast<const f32x4 *>(&o.weight.query[r8 + h * 4]);
             bf16x8 a[3];
 #pragma unroll
-            for (int p = 0; p < 3; ++p) a[p] = left(&o.P[p][h * 16 + c16][r4 * 2]);
+            for (int p = 0; p < 3; ++p) a[p] = left(&o.weight.P[p][h * 16 + c16][r8]);
             const f32x4 out = multiply<3, 3>(a, right, query * qs[h]);
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-                const uint32_t t = c * kChunk + h * 16 + r4 + x;
+                const uint32_t t = c * kChunk + r8 + h * 4 + x;
                 if (!in || t >= span.len) continue;
                 const uint64_t row = span.row(t);
                 ((T *)d.o)[row * d.ldo + head * d.Dv + col] = (T)out[x];
@@ -104,21 +81,16 @@ delta_fwd_kernel(Delta d, uint32_t waves, uint32_t groups, uint64_t from)
             }
         }
         split_rows<3>(u[0] * until[0], u[1] * until[1], right);
-        const float whole = o.whole;
+        const float whole = o.weight.whole;
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
             bf16x8 a[n];
 #pragma unroll
-            for (int p = 0; p < n; ++p) a[p] = left(&o.KT[p][t * 16 + c16][r4 * 2]);
+            for (int p = 0; p < n; ++p) a[p] = left(&o.key.KT[p][t * 16 + c16][r8]);
             S[t] = multiply<n, 3>(a, right, S[t] * whole);
         }
     });
-    if (d.s_last && in)
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-            for (int x = 0; x < 4; ++x)
-                if (t * 16 + r4 + x < d.Dk) d.s_last[memory + (uint64_t)(t * 16 + r4 + x) * d.Dv] = S[t][x];
+    if (d.s_last) store_memory<KS>(d.s_last + memory, d.Dk, d.Dv, in, r8, S);
 }
 
 template <class T>
@@ -127,10 +99,10 @@ void launch_type(const Delta &d, hipStream_t st)
     const Columns c = columns_of(d);
     const uint64_t units = (uint64_t)d.n_seq * d.H * c.groups;
     for (uint64_t from = 0; from < units; from += kMostGroups) {
-        const uint32_t grid = (uint32_t)(units - from < kMostGroups ? units - from : kMostGroups), threads = (c.waves + 1) * 64;
-        if (d.Dk <= 32) delta_fwd_kernel<T, 1><<<grid, threads, 0, st>>>(d, c.waves, c.groups, from);
-        else if (d.Dk <= 64) delta_fwd_kernel<T, 2><<<grid, threads, 0, st>>>(d, c.waves, c.groups, from);
-        else delta_fwd_kernel<T, 4><<<grid, threads, 0, st>>>(d, c.waves, c.groups, from);
+        const uint32_t grid = (uint32_t)(units - from < kMostGroups ? units - from : kMostGroups), threads = c.waves * 64;
+        if (d.Dk <= 32) delta_fwd_kernel<T, 1><<<grid, threads, 0, st>>>(d, c.with, c.groups, from);
+        else if (d.Dk <= 64) delta_fwd_kernel<T, 2><<<grid, threads, 0, st>>>(d, c.with, c.groups, from);
+        else delta_fwd_kernel<T, 4><<<grid, threads, 0, st>>>(d, c.with, c.groups, from);
     }
 }
 

@@ -24,23 +24,9 @@ struct Shared {
     float beta[kTokens], dG[kTokens], end[4];
 };
 
-// eight values of a row of D from column c on, 0 from D on and without a row
-template <class T>
-__device__ __forceinline__ void eight(const T *row, uint32_t c, uint32_t D, bool in, bool vec, float (&out)[8])
-{
-    if (vec) {
-        dg_rows::Pack<T, 8> p;
-        load8_aligned<T>(row, c, D, in, p);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) out[i] = (float)p.v[i];
-    } else
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const bool here = in && c + i < D;
-            const T v = row[here ? c + i : 0];
-            out[i] = here ? (float)v : 0.0f;
-        }
-}
+// A lane has rows 4 q to 4 q + 3 of two results of 16, which become places 8 q to 8 q + 7 of the next sum over tokens: where token t stands among the columns
+// of its left operands.
+__device__ __forceinline__ uint32_t place(uint32_t t) { return (t & ~31u) | (t >> 2 & 3) << 3 | (t >> 4 & 1) << 2 | (t & 3); }
 
 // sum over the four lanes that have a token
 __device__ __forceinline__ float of_token(float v)
