@@ -9,6 +9,9 @@ using namespace dg_delta;
 // Up to so many tokens a sequence, on average, they are taken one by one.
 constexpr uint64_t kFewTokens = 4;
 
+// Whether a lane takes a column or row of the memory along a sequence, instead of wavefronts chunks of it
+bool takes_small(uint32_t n_seq, uint32_t H, uint32_t Dk, uint32_t Dv) { return Dk <= 32 && Dv <= 32 && (uint64_t)n_seq * H >= 1; }
+
 uint64_t slots_of(uint64_t N, uint32_t n_seq) { return N / kMark + n_seq; }
 
 size_t marks_bytes(uint64_t N, uint32_t n_seq, uint32_t H, uint32_t Dk, uint32_t Dv) { return (size_t)slots_of(N, n_seq) * H * Dk * Dv * sizeof(float); }
@@ -42,7 +45,8 @@ int check_rows(const char *who, const char *name, const void *p, uint64_t ld, ui
 {
     if (N == 0) return DG_OK;
     DG_REQUIRE(p && dg::aligned(p, item), DG_ERR_ARG, "%s: %s: null or misaligned pointer", who, name);
-    DG_REQUIRE(ld >= W && ld <= 1ull << 32, DG_ERR_ARG, "%s: %s: rows of %llu values lie %llu apart", who, name, (unsigned long long)W, (unsigned long long)ld);
+    DG_REQUIRE(ld < 1ull << 24, DG_ERR_UNSUPPORTED, "%s: %s: rows 2^24 values or more apart", who, name);
+    DG_REQUIRE(ld >= W, DG_ERR_ARG, "%s: %s: rows of %llu values lie %llu apart", who, name, (unsigned long long)W, (unsigned long long)ld);
     return DG_OK;
 }
 
@@ -82,9 +86,10 @@ extern "C" int dg_delta_rule_fwd(const void *q, uint64_t ldq, const void *k, uin
     Delta d = {};
     d.q = q, d.k = k, d.v = v, d.g = g, d.beta = beta, d.ldq = ldq, d.ldk = ldk, d.ldv = ldv, d.ldg = ldg, d.ldb = ldbeta, d.s0 = s0, d.o = o, d.ldo = ldo, d.s_last = s_last;
     d.first = first, d.N = N, d.n_seq = n_seq, d.Hk = Hk, d.H = H, d.Dk = Dk, d.Dv = Dv, d.reverse = reverse, d.scale = scale;
-    if (saved) d.marks = (float *)saved, d.u = (float *)((char *)saved + padded(marks_bytes(N, n_seq, H, Dk, Dv)));
+    if (saved) d.marks = (float *)saved, d.y = (float *)((char *)saved + padded(marks_bytes(N, n_seq, H, Dk, Dv)));
     d.vec_q = wide_rows(q, ldq, Dk, dtype), d.vec_k = wide_rows(k, ldk, Dk, dtype), d.vec_v = wide_rows(v, ldv, Dv, dtype);
-    if (!saved && N <= kFewTokens * n_seq) launch_tokens(d, dtype, (hipStream_t)stream);
+    if (takes_small(n_seq, H, Dk, Dv)) launch_small(d, dtype, false, (hipStream_t)stream);
+    else if (!saved && N <= kFewTokens * n_seq) launch_tokens(d, dtype, (hipStream_t)stream);
     else {
         const size_t bytes = forward_bytes(N, n_seq, H);
         DG_REQUIRE(ws && dg::aligned(ws, 16) && ws_bytes >= bytes, DG_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", who, bytes, ws ? ws_bytes : 0);
@@ -121,13 +126,18 @@ extern "C" int dg_delta_rule_bwd(const void *q, uint64_t ldq, const void *k, uin
     d.q = q, d.k = k, d.v = v, d.g = g, d.beta = beta, d.ldq = ldq, d.ldk = ldk, d.ldv = ldv, d.ldg = ldg, d.ldb = ldbeta, d.ds_last = ds_last, d.ds0 = ds0;
     d.dout = do_, d.lddo = lddo, d.dq = dq, d.dk = dk, d.dv = dv, d.lddq = lddq, d.lddk = lddk, d.lddv = lddv, d.dg = dg, d.dbeta = dbeta, d.lddg = lddg, d.lddb = lddbeta;
     d.first = first, d.N = N, d.n_seq = n_seq, d.Hk = Hk, d.H = H, d.Dk = Dk, d.Dv = Dv, d.reverse = reverse, d.scale = scale, d.slots = (uint32_t)slots_of(N, n_seq);
-    d.marks = (float *)const_cast<void *>(saved), d.u = (float *)((char *)const_cast<void *>(saved) + marks);
+    d.marks = (float *)const_cast<void *>(saved), d.y = (float *)((char *)const_cast<void *>(saved) + marks);
     use_workspace(d, ws);
     char *const rest = (char *)ws + forward_bytes(N, n_seq, H);
     d.dmarks = (float *)rest, d.dr = (float *)(rest + marks), d.slot_seq = (const uint32_t *)(rest + marks + rows_bytes(N, H, Dv));
     d.vec_q = wide_rows(q, ldq, Dk, dtype), d.vec_k = wide_rows(k, ldk, Dk, dtype), d.vec_v = wide_rows(v, ldv, Dv, dtype), d.vec_o = wide_rows(do_, lddo, Dv, dtype);
-    if (N) launch_weights(d, dtype, true, (hipStream_t)stream);
-    launch_backward(d, dtype, (hipStream_t)stream);
-    if (N) launch_gradients(d, dtype, (hipStream_t)stream);
+    d.vec_dv = wide_rows(dv, lddv, Dv, dtype), d.vec_dqk = wide_rows(dq, lddq, Dk, dtype) && wide_rows(dk, lddk, Dk, dtype);
+    if (N) launch_slots(d, (hipStream_t)stream);
+    if (takes_small(n_seq, H, Dk, Dv)) launch_small(d, dtype, true, (hipStream_t)stream);
+    else {
+        if (N) launch_weights(d, dtype, true, (hipStream_t)stream);
+        launch_backward(d, dtype, (hipStream_t)stream);
+        if (N) launch_gradients(d, dtype, (hipStream_t)stream);
+    }
     return dg::launch_status(who);
 }

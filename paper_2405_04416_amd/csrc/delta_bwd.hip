@@ -21,77 +21,78 @@ delta_bwd_kernel(Delta d, uint32_t with, uint32_t groups, uint64_t from)
     const uint64_t memory = ((uint64_t)seq * d.H + head) * d.Dk * d.Dv + col;
     f32x4 S[kTiles];
     load_memory<KS>(d.ds_last ? d.ds_last + memory : nullptr, d.Dk, d.Dv, in, r8, S);
-    const T *gradients = (const T *)d.dout + head * d.Dv + (in ? col : 0);
-    const uint32_t last = span.len ? (span.len - 1) / kChunk : 0;
+    const T *gradients = (const T *)d.dout + head * d.Dv;
+    const uint32_t at = in ? col : 0, last = span.len ? (span.len - 1) / kChunk : 0;
     T next[8];
-    if (span.len) load_column<T>(gradients, d.lddo, span, last * kChunk + r8, in, next);
+    float gradient[8];                  // of the chunk before: stored when the next one's loads are on their way
+    auto store = [&](uint32_t t0) { store_column<float>(d.dr + head * d.Dv, (uint64_t)d.H * d.Dv, at, span, t0, r8, in, gradient); };
+    load_column<T>(gradients, d.lddo, at, span, last * kChunk, r8, next);
     along<T, KS, true>(d, span, seq, head, room, wave, waves, [&](const Operands<T, KS, true> &o, uint32_t c) {
         if (wave >= with) return;
+        const uint32_t t0 = c * kChunk;
         if (c == last || c % (kMark / kChunk) == kMark / kChunk - 1)
             store_memory<KS>(d.dmarks + ((uint64_t)(first_slot(span, seq) + c / (kMark / kChunk)) * d.H + head) * d.Dk * d.Dv + col, d.Dk, d.Dv, in, r8, S);
-        float dout[8], queried[8];
+        if (c != last) store(t0 + kChunk);
+        float dout[8];
 #pragma unroll
-        for (int x = 0; x < 8; ++x) {
-            dout[x] = (float)next[x];
-            queried[x] = dout[x] * o.weight.query[r8 + x];
+        for (int x = 0; x < 8; ++x) dout[x] = held(next[x], span, t0 + r8 + x, in);
+        load_column<T>(gradients, d.lddo, at, span, c ? t0 - kChunk : 0, r8, next);
+
+        bf16x8 keys[KS][2][n], inverse[2][3], pull[2][3];
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) lefts(o.key.K, h * 16 + c16, s * 32 + r8, keys[s][h]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            lefts(o.weight.P, h * 16 + c16, r8, pull[h]);
+            lefts(o.weight.inverse, h * 16 + c16, r8, inverse[h]);
         }
-        load_column<T>(gradients, d.lddo, span, (c ? c - 1 : 0) * kChunk + r8, in, next);
+        __builtin_amdgcn_sched_barrier(0);
         f32x4 ks[2] = {};
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             bf16x8 sp[3];
             split_rows<3>(S[2 * s], S[2 * s + 1], sp);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                bf16x8 a[n];
-#pragma unroll
-                for (int p = 0; p < n; ++p) a[p] = left(&o.key.K[p][h * 16 + c16][s * 32 + r8]);
-                ks[h] = multiply<n, 3>(a, sp, ks[h]);
-            }
+            for (int h = 0; h < 2; ++h) ks[h] = multiply<n, 3>(keys[s][h], sp, ks[h]);
         }
-        bf16x8 exact[n], right[3];
+        bf16x8 turned[kTiles][n], queries[kTiles][n];
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+            lefts(o.key.KT, t * 16 + c16, r8, turned[t]);
+            lefts(o.key.Q, t * 16 + c16, r8, queries[t]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        bf16x8 exact[n], right[3], right_q[3];
         split8<n>(dout, exact);
-        f32x4 du[2], dr[2];
+        f32x4 du[2], dr[2], back[2];
+        float queried[8];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const f32x4 until = *reinterpret_cast<const f32x4 *>(&o.weight.until[r8 + h * 4]);
-            bf16x8 a[3];
+            const f32x4 until = *reinterpret_cast<const f32x4 *>(&o.weight.until[r8 + h * 4]), query = *reinterpret_cast<const f32x4 *>(&o.weight.query[r8 + h * 4]);
+            du[h] = multiply<3, n>(pull[h], exact, until * ks[h]);
 #pragma unroll
-            for (int p = 0; p < 3; ++p) a[p] = left(&o.weight.P[p][h * 16 + c16][r8]);
-            du[h] = multiply<3, n>(a, exact, until * ks[h]);
+            for (int x = 0; x < 4; ++x) queried[h * 4 + x] = dout[h * 4 + x] * query[x];
         }
         split_rows<3>(du[0], du[1], right);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            bf16x8 a[3];
+            dr[h] = multiply<3, 3>(inverse[h], right, (f32x4){});
+            back[h] = -dr[h] * *reinterpret_cast<const f32x4 *>(&o.weight.read[r8 + h * 4]);
 #pragma unroll
-            for (int p = 0; p < 3; ++p) a[p] = left(&o.weight.inverse[p][h * 16 + c16][r8]);
-            dr[h] = multiply<3, 3>(a, right, (f32x4){});
+            for (int x = 0; x < 4; ++x) gradient[h * 4 + x] = dr[h][x];
         }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const uint32_t t = c * kChunk + r8 + h * 4 + x;
-                if (in && t < span.len) d.dr[(span.row(t) * d.H + head) * d.Dv + col] = dr[h][x];
-            }
-            dr[h] *= -*reinterpret_cast<const f32x4 *>(&o.weight.read[r8 + h * 4]);
-        }
-        bf16x8 right_q[3];
         split8<3>(queried, right_q);
-        split_rows<3>(dr[0], dr[1], right);
+        split_rows<3>(back[0], back[1], right);
         const float whole = o.weight.whole;
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
-            bf16x8 a[n];
-#pragma unroll
-            for (int p = 0; p < n; ++p) a[p] = left(&o.key.Q[p][t * 16 + c16][r8]);
-            S[t] = multiply<n, 3>(a, right_q, S[t] * whole);
-#pragma unroll
-            for (int p = 0; p < n; ++p) a[p] = left(&o.key.KT[p][t * 16 + c16][r8]);
-            S[t] = multiply<n, 3>(a, right, S[t]);
+            S[t] = multiply<n, 3>(queries[t], right_q, S[t] * whole);
+            S[t] = multiply<n, 3>(turned[t], right, S[t]);
         }
     });
+    if (span.len && wave < with) store(0);
     if (d.ds0) store_memory<KS>(d.ds0 + memory, d.Dk, d.Dv, in, r8, S);
 }
 
@@ -100,8 +101,8 @@ void launch_type(const Delta &d, hipStream_t st)
 {
     const Columns c = columns_of(d);
     const uint64_t units = (uint64_t)d.n_seq * d.H * c.groups;
-    for (uint64_t from = 0; from < units; from += kMostGroups) {
-        const uint32_t grid = (uint32_t)(units - from < kMostGroups ? units - from : kMostGroups), threads = c.waves * 64;
+    for (uint64_t from = 0; from < units; from += kMostLaunched) {
+        const uint32_t grid = (uint32_t)(units - from < kMostLaunched ? units - from : kMostLaunched), threads = c.waves * 64;
         if (d.Dk <= 32) delta_bwd_kernel<T, 1><<<grid, threads, 0, st>>>(d, c.with, c.groups, from);
         else if (d.Dk <= 64) delta_bwd_kernel<T, 2><<<grid, threads, 0, st>>>(d, c.with, c.groups, from);
         else delta_bwd_kernel<T, 4><<<grid, threads, 0, st>>>(d, c.with, c.groups, from);

@@ -28,7 +28,7 @@ struct alignas(16) Keys {
 
 struct alignas(kPage) Weights {
     uint16_t inverse[3][kChunk][kPitch], P[3][kChunk][kPitch];                 // T and P; backward: T^T and P^T
-    float beta[kChunk], read[kChunk], query[kChunk], until[kChunk];            // beta, beta e^G, scale e^G, e^(G[last] - G)
+    float beta[kChunk], read[kChunk], query[kChunk], until[kChunk];            // beta, e^G (backward: beta e^G), scale e^G, e^(G[last] - G)
     float whole;                                                               // e^G[last]
 };
 
@@ -116,16 +116,25 @@ struct Rows {
     __device__ __forceinline__ uint32_t token(int i) const { return (i * waves + wave) * (16 / KS) + lane / (4 * KS); }
     __device__ __forceinline__ uint32_t column() const { return lane % (4 * KS) * 8; }
 
+    // a vector where there is one, otherwise another, which store() clears
     __device__ __forceinline__ void fetch(uint32_t c)
     {
         if (!vec) return;
+        constexpr int m = 16 / sizeof(T);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const uint32_t t = c * kChunk + token(i);
-            const bool in = token(i) < kChunk && t < span.len;
-            const uint64_t row = span.row(in ? t : c * kChunk);
-            load8_aligned<T>(k + row * ldk, column(), Dk, in, ks[i]);
-            load8_aligned<T>(q + row * ldq, column(), Dk, in, qs[i]);
+            const uint64_t row = span.row(token(i) < kChunk && t < span.len ? t : c * kChunk);
+#pragma unroll
+            for (int h = 0; h < 8 / m; ++h) {
+                const uint32_t col = column() + h * m < Dk ? column() + h * m : 0;
+                const dg_rows::Pack<T, m> x = *reinterpret_cast<const dg_rows::Pack<T, m> *>(k + row * ldk + col), y = *reinterpret_cast<const dg_rows::Pack<T, m> *>(q + row * ldq + col);
+#pragma unroll
+                for (int j = 0; j < m; ++j) {
+                    ks[i].v[h * m + j] = x.v[j];
+                    qs[i].v[h * m + j] = y.v[j];
+                }
+            }
         }
     }
 
@@ -136,14 +145,15 @@ struct Rows {
             const uint32_t t = token(i);
             if (t >= kChunk) continue;
             float x[8], y[8];
+            const bool in = c * kChunk + t < span.len;
             if (vec) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    x[j] = (float)ks[i].v[j];
-                    y[j] = (float)qs[i].v[j];
+                    const bool here = in && column() + j < Dk;
+                    x[j] = here ? (float)ks[i].v[j] : 0.0f;
+                    y[j] = here ? (float)qs[i].v[j] : 0.0f;
                 }
             } else {
-                const bool in = c * kChunk + t < span.len;
                 const uint64_t row = span.row(in ? c * kChunk + t : c * kChunk);
                 eight<T>(k + row * ldk, column(), Dk, in, false, x);
                 eight<T>(q + row * ldq, column(), Dk, in, false, y);
@@ -203,8 +213,6 @@ inline Columns columns_of(const Delta &d)
     return {with, with < least ? least : with, (all + with - 1) / with};
 }
 
-constexpr uint64_t kMostGroups = 1 << 22;      // of a launch: its lanes have to stay below 2^32
-
 // Memories in registers: result t of 2 KS has rows 32 (t / 2) + 8 q + 4 (t % 2) on with lane (column, q)
 template <int KS>
 __device__ __forceinline__ void load_memory(const float *from, uint32_t Dk, uint32_t Dv, bool in, uint32_t r8, f32x4 (&S)[2 * KS])
@@ -230,16 +238,55 @@ __device__ __forceinline__ void store_memory(float *to, uint32_t Dk, uint32_t Dv
         }
 }
 
-// A lane's eight tokens of a chunk in one column of rows [N, ld], 0 where there is no token
+// A lane's eight tokens of a chunk in one column of rows [N, ld]: one address for the workgroup, 32-bit distances from it for lanes and tokens
+// (32 rows of at most 2^24 values).
+struct Column {
+    uint64_t row;                       // lowest of the chunk
+    uint32_t count, from, step;         // tokens of the chunk; distance of the lane's first token, and from one to the next
+    __device__ __forceinline__ Column(const Span &s, uint32_t t0, uint32_t r8, uint64_t ld)
+    {
+        count = s.len - t0 < kChunk ? s.len - t0 : kChunk;
+        row = s.turn ? s.begin + (s.len - t0 - count) : s.begin + t0;
+        from = (s.turn ? count - 1 - r8 : r8) * (uint32_t)ld;
+        step = s.turn ? 0u - (uint32_t)ld : (uint32_t)ld;
+    }
+};
+
+// another token's value where there is none, which `held` clears: not before it is used, so that nothing waits for the load
 template <class T>
-__device__ __forceinline__ void load_column(const T *p, uint64_t ld, const Span &span, uint32_t t0, bool in, T (&out)[8])
+__device__ __forceinline__ void load_column(const T *p, uint64_t ld, uint32_t lane_column, const Span &span, uint32_t t0, uint32_t r8, T (&out)[8])
+{
+    if (t0 >= span.len) return;
+    const Column c(span, t0, r8, ld);
+    const T *base = p + c.row * ld;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) out[x] = base[(r8 + x < c.count ? c.from + x * c.step : 0u) + lane_column];
+}
+
+template <class T>
+__device__ __forceinline__ float held(T value, const Span &span, uint32_t t, bool in) { return in && t < span.len ? (float)value : 0.0f; }
+
+template <class T>
+__device__ __forceinline__ void store_column(T *p, uint64_t ld, uint32_t lane_column, const Span &span, uint32_t t0, uint32_t r8, bool in, const float (&v)[8])
+{
+    const Column c(span, t0, r8, ld);
+    T *base = p + c.row * ld;
+    if (!in) return;
+    if (c.count == kChunk)
+#pragma unroll
+        for (int x = 0; x < 8; ++x) base[c.from + x * c.step + lane_column] = (T)v[x];
+    else
+#pragma unroll
+        for (int x = 0; x < 8; ++x)
+            if (r8 + x < c.count) base[c.from + x * c.step + lane_column] = (T)v[x];
+}
+
+// Left operands: tile h or t of a matrix in LDS, all pieces.  They are read ahead of the products, so that these do not wait for one after the other.
+template <int n, int rows, int pitch>
+__device__ __forceinline__ void lefts(const uint16_t (&m)[n][rows][pitch], uint32_t row, uint32_t col, bf16x8 (&out)[n])
 {
 #pragma unroll
-    for (int x = 0; x < 8; ++x) {
-        const bool here = in && t0 + x < span.len;
-        const T value = p[span.row(here ? t0 + x : 0) * ld];
-        out[x] = here ? value : (T)0.0f;
-    }
+    for (int p = 0; p < n; ++p) out[p] = left(&m[p][row][col]);
 }
 
 }  // namespace dg_delta

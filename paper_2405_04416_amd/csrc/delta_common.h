@@ -2,8 +2,8 @@
 //
 // Per head, with a memory S [Dk, Dv]:  S <- e^g S;  S <- S + beta k (v - S^T k)^T;  o = scale S^T q.
 // Over a chunk of tokens, S the memory before it, G the sums of g from its start on, D[i, j] = e^(G[i] - G[j]):
-//   A[i, j] = beta[i] D[i, j] k[i] k[j]  (j < i),   T = (1 + A)^-1,   P[i, j] = scale D[i, j] q[i] k[j]  (j <= i),
-//   U = T beta (V - e^G K S)  (what the tokens write),   O = scale e^G Q S + P U,   S' = e^G[last] S + K^T (e^(G[last] - G) U).
+//   A[i, j] = D[i, j] k[i] k[j] beta[j]  (j < i),   T = (1 + A)^-1,   P[i, j] = scale D[i, j] q[i] k[j]  (j <= i),
+//   Y = T (V - e^G K S)  (what the tokens miss),   U = beta Y  (what they write),   O = scale e^G Q S + P U,   S' = e^G[last] S + K^T (e^(G[last] - G) U).
 //
 // Products are taken on the matrix units in bf16, of values that are cut into pieces of 8 bits: one for a bf16 value, two for fp16, three for
 // fp32, which lose nothing; of the products of pieces those below 2^-24 are left out.  So everything is as exact as in fp32, at several times
@@ -23,6 +23,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kMark = 64;               // tokens between memories that the forward pass leaves for the backward pass
 constexpr int kMaxD = 128;
+constexpr uint64_t kMostLaunched = 1 << 22;     // workgroups of a launch: its lanes have to stay below 2^32
 // e^-104 is 0 in fp32: below that a gate is shut.  Logarithms are cut off here so that their differences stay numbers.
 constexpr float kShut = -200.0f;
 
@@ -38,7 +39,7 @@ struct Delta {
     uint64_t ldo, lddo;
     float *s_last, *ds0;
     float *marks, *dmarks;              // [slots][H][Dk][Dv]: memories before each 64 tokens, gradients of those after
-    float *u, *dr;                      // [N][H][Dv]
+    float *y, *dr;                      // [N][H][Dv]: what tokens miss, v - S^T k, and the gradient of what they write, beta times that
     void *dq, *dk, *dv;
     uint64_t lddq, lddk, lddv;
     float *dg, *dbeta;
@@ -49,7 +50,7 @@ struct Delta {
     uint64_t N;
     uint32_t n_seq, Hk, H, Dk, Dv, reverse, slots;
     float scale;
-    uint32_t vec_q, vec_k, vec_v, vec_o;        // whether 8 values of a head's row can be loaded at once
+    uint32_t vec_q, vec_k, vec_v, vec_o, vec_dv, vec_dqk;       // whether a head's rows lie in whole 16 bytes
 };
 
 template <class T>
@@ -60,8 +61,10 @@ struct Pieces<bf16> { static constexpr int n = 1; };
 // ------------------------------------------------------------------------------ sequences
 struct Span {
     uint64_t begin;
-    uint32_t len, reverse;
-    __device__ __forceinline__ uint64_t row(uint32_t i) const { return reverse ? begin + len - 1 - i : begin + i; }
+    uint32_t len;
+    int32_t turn;                       // -1: from the last row to the first, else 0
+    // row of token i; without a branch, which would keep loads apart
+    __device__ __forceinline__ uint64_t row(uint32_t i) const { return begin + (turn & (len - 1)) + (int64_t)(((int32_t)i ^ turn) - turn); }
 };
 
 // no row from N on, whatever the offsets say
@@ -69,10 +72,10 @@ __device__ __forceinline__ Span span_of(const Delta &d, uint32_t seq)
 {
     if (!d.first) {
         const uint64_t len = d.N / d.n_seq;
-        return {seq * len, (uint32_t)len, d.reverse};
+        return {seq * len, (uint32_t)len, d.reverse ? -1 : 0};
     }
     const uint64_t b = d.first[seq], e = d.first[seq + 1], begin = b < d.N ? b : d.N, end = e < d.N ? e : d.N;
-    return {begin, end > begin ? (uint32_t)(end - begin) : 0u, d.reverse};
+    return {begin, end > begin ? (uint32_t)(end - begin) : 0u, d.reverse ? -1 : 0};
 }
 
 // Where the memories of a sequence are left: every sequence begins one slot after floor(begin / 64) more than the one before, which leaves room for all
@@ -172,6 +175,8 @@ size_t weight_bytes(uint64_t N, uint32_t n_seq, uint32_t H);
 size_t chunk_bytes(uint64_t N, uint32_t n_seq);
 void launch_weights(const Delta &d, uint32_t dtype, bool backward, hipStream_t st);
 void launch_forward(const Delta &d, uint32_t dtype, hipStream_t st);
+void launch_small(const Delta &d, uint32_t dtype, bool back, hipStream_t st);        // heads of up to 32 x 32
+void launch_slots(const Delta &d, hipStream_t st);
 void launch_tokens(const Delta &d, uint32_t dtype, hipStream_t st);
 void launch_backward(const Delta &d, uint32_t dtype, hipStream_t st);
 void launch_gradients(const Delta &d, uint32_t dtype, hipStream_t st);

@@ -19,17 +19,40 @@ delta_fwd_kernel(Delta d, uint32_t with, uint32_t groups, uint64_t from)
     const uint64_t memory = ((uint64_t)seq * d.H + head) * d.Dk * d.Dv + col;
     f32x4 S[kTiles];
     load_memory<KS>(d.s0 ? d.s0 + memory : nullptr, d.Dk, d.Dv, in, r8, S);
-    const T *values = (const T *)d.v + head * d.Dv + (in ? col : 0);
+    const T *values = (const T *)d.v + head * d.Dv;
+    const uint32_t at = in ? col : 0;
     T next[8];
-    if (span.len) load_column<T>(values, d.ldv, span, r8, in, next);
+    float out[8], missed[8];            // of the chunk before: stored when the next one's loads are on their way, so that none waits for a store
+    auto store = [&](uint32_t t0) {
+        store_column<T>((T *)d.o + head * d.Dv, d.ldo, at, span, t0, r8, in, out);
+        if (d.y) store_column<float>(d.y + head * d.Dv, (uint64_t)d.H * d.Dv, at, span, t0, r8, in, missed);
+    };
+    load_column<T>(values, d.ldv, at, span, 0, r8, next);
     along<T, KS, false>(d, span, seq, head, room, wave, waves, [&](const Operands<T, KS, false> &o, uint32_t c) {
         if (wave >= with) return;
+        const uint32_t t0 = c * kChunk;
         if (d.marks && c % (kMark / kChunk) == 0)
             store_memory<KS>(d.marks + ((uint64_t)(first_slot(span, seq) + c / (kMark / kChunk)) * d.H + head) * d.Dk * d.Dv + col, d.Dk, d.Dv, in, r8, S);
+        if (c) store(t0 - kChunk);
         float value[8];
 #pragma unroll
-        for (int x = 0; x < 8; ++x) value[x] = (float)next[x];
-        load_column<T>(values, d.ldv, span, (c + 1) * kChunk + r8, in, next);
+        for (int x = 0; x < 8; ++x) value[x] = held(next[x], span, t0 + r8 + x, in);
+        load_column<T>(values, d.ldv, at, span, t0 + kChunk, r8, next);
+
+        bf16x8 keys[KS][2][n], queries[KS][2][n], inverse[2][3], pull[2][3];
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                lefts(o.key.K, h * 16 + c16, s * 32 + r8, keys[s][h]);
+                lefts(o.key.Q, h * 16 + c16, s * 32 + r8, queries[s][h]);
+            }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            lefts(o.weight.inverse, h * 16 + c16, r8, inverse[h]);
+            lefts(o.weight.P, h * 16 + c16, r8, pull[h]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
         f32x4 ks[2] = {}, qs[2] = {};
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
@@ -37,59 +60,47 @@ delta_fwd_kernel(Delta d, uint32_t with, uint32_t groups, uint64_t from)
             split_rows<3>(S[2 * s], S[2 * s + 1], sp);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                bf16x8 a[n];
-#pragma unroll
-                for (int p = 0; p < n; ++p) a[p] = left(&o.key.K[p][h * 16 + c16][s * 32 + r8]);
-                ks[h] = multiply<n, 3>(a, sp, ks[h]);
-#pragma unroll
-                for (int p = 0; p < n; ++p) a[p] = left(&o.key.Q[p][h * 16 + c16][s * 32 + r8]);
-                qs[h] = multiply<n, 3>(a, sp, qs[h]);
+                ks[h] = multiply<n, 3>(keys[s][h], sp, ks[h]);
+                qs[h] = multiply<n, 3>(queries[s][h], sp, qs[h]);
             }
         }
-        f32x4 r[2], u[2], until[2];
+        bf16x8 turned[kTiles][n];
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) lefts(o.key.KT, t * 16 + c16, r8, turned[t]);
+        __builtin_amdgcn_sched_barrier(0);
+        f32x4 r[2], u[2], beta[2], until[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const f32x4 beta = *reinterpret_cast<const f32x4 *>(&o.weight.beta[r8 + h * 4]), read = *reinterpret_cast<const f32x4 *>(&o.weight.read[r8 + h * 4]);
+            const f32x4 read = *reinterpret_cast<const f32x4 *>(&o.weight.read[r8 + h * 4]);
+            beta[h] = *reinterpret_cast<const f32x4 *>(&o.weight.beta[r8 + h * 4]);
             until[h] = *reinterpret_cast<const f32x4 *>(&o.weight.until[r8 + h * 4]);
 #pragma unroll
-            for (int x = 0; x < 4; ++x) r[h][x] = beta[x] * value[h * 4 + x] - read[x] * ks[h][x];
+            for (int x = 0; x < 4; ++x) r[h][x] = value[h * 4 + x] - read[x] * ks[h][x];
         }
         bf16x8 right[3];
         split_rows<3>(r[0], r[1], right);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            bf16x8 a[3];
+            const f32x4 y = multiply<3, 3>(inverse[h], right, (f32x4){});
 #pragma unroll
-            for (int p = 0; p < 3; ++p) a[p] = left(&o.weight.inverse[p][h * 16 + c16][r8]);
-            u[h] = multiply<3, 3>(a, right, (f32x4){});
+            for (int x = 0; x < 4; ++x) missed[h * 4 + x] = y[x];
+            u[h] = y * beta[h];
         }
+        bf16x8 written[3];
+        split_rows<3>(u[0] * until[0], u[1] * until[1], written);
+        const float whole = o.weight.whole;
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) S[t] = multiply<n, 3>(turned[t], written, S[t] * whole);
         split_rows<3>(u[0], u[1], right);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const f32x4 query = *reinterpret_cast<const f32x4 *>(&o.weight.query[r8 + h * 4]);
-            bf16x8 a[3];
+            const f32x4 sum = multiply<3, 3>(pull[h], right, query * qs[h]);
 #pragma unroll
-            for (int p = 0; p < 3; ++p) a[p] = left(&o.weight.P[p][h * 16 + c16][r8]);
-            const f32x4 out = multiply<3, 3>(a, right, query * qs[h]);
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const uint32_t t = c * kChunk + r8 + h * 4 + x;
-                if (!in || t >= span.len) continue;
-                const uint64_t row = span.row(t);
-                ((T *)d.o)[row * d.ldo + head * d.Dv + col] = (T)out[x];
-                if (d.u) d.u[(row * d.H + head) * d.Dv + col] = u[h][x];
-            }
-        }
-        split_rows<3>(u[0] * until[0], u[1] * until[1], right);
-        const float whole = o.weight.whole;
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-            bf16x8 a[n];
-#pragma unroll
-            for (int p = 0; p < n; ++p) a[p] = left(&o.key.KT[p][t * 16 + c16][r8]);
-            S[t] = multiply<n, 3>(a, right, S[t] * whole);
+            for (int x = 0; x < 4; ++x) out[h * 4 + x] = sum[x];
         }
     });
+    if (span.len && wave < with) store((span.len - 1) / kChunk * kChunk);
     if (d.s_last) store_memory<KS>(d.s_last + memory, d.Dk, d.Dv, in, r8, S);
 }
 
@@ -98,8 +109,8 @@ void launch_type(const Delta &d, hipStream_t st)
 {
     const Columns c = columns_of(d);
     const uint64_t units = (uint64_t)d.n_seq * d.H * c.groups;
-    for (uint64_t from = 0; from < units; from += kMostGroups) {
-        const uint32_t grid = (uint32_t)(units - from < kMostGroups ? units - from : kMostGroups), threads = c.waves * 64;
+    for (uint64_t from = 0; from < units; from += kMostLaunched) {
+        const uint32_t grid = (uint32_t)(units - from < kMostLaunched ? units - from : kMostLaunched), threads = c.waves * 64;
         if (d.Dk <= 32) delta_fwd_kernel<T, 1><<<grid, threads, 0, st>>>(d, c.with, c.groups, from);
         else if (d.Dk <= 64) delta_fwd_kernel<T, 2><<<grid, threads, 0, st>>>(d, c.with, c.groups, from);
         else delta_fwd_kernel<T, 4><<<grid, threads, 0, st>>>(d, c.with, c.groups, from);

@@ -1,12 +1,14 @@
 // The gated delta rule: T and P of all chunks of 32 tokens (delta_chunk.h), a workgroup of two wavefronts for each chunk and head, one for T, one for P.
 //   T = (1 + A)^-1 of 32 rows: the two diagonal blocks of 16 by substitution, row by row in the lanes' registers, the block below as -T22 A21 T11.
+// Forward A has beta of its columns (T gives what tokens miss, Y), backward of its rows (T^T gives dR): so neither divides by a rate, which may be 0.
+// Operands come straight from memory and results go straight to the workspace; only the small blocks pass through LDS.
 #include "delta_chunk.h"
 
 namespace {
 
 using namespace dg_delta;
 
-// four values side by side, in pieces
+// four values side by side, in pieces, to the workspace
 __device__ __forceinline__ void put4(const float (&v)[4], uint16_t (*rows)[kChunk][kPitch], uint32_t row, uint32_t col)
 {
     uint32_t w[3][2];
@@ -15,30 +17,36 @@ __device__ __forceinline__ void put4(const float (&v)[4], uint16_t (*rows)[kChun
     for (int p = 0; p < 3; ++p) *reinterpret_cast<u32x2 *>(&rows[p][line(row)][col]) = (u32x2){w[p][0], w[p][1]};
 }
 
-template <class T, int KS>
 struct Shared {
-    Weights weight;
-    uint16_t K[Pieces<T>::n][kChunk][32 * KS + 8], Q[Pieces<T>::n][kChunk][32 * KS + 8];
-    double G[kChunk];
+    double G[2][kChunk];
+    float beta[kChunk];
     float A[2][16][20], inverse[2][16][20];     // A^T and T of the diagonal blocks
 };
 
-// the product of two 16-row blocks of K or Q
-template <int n, int KS>
-__device__ __forceinline__ f32x4 rows_product(const uint16_t (*a)[kChunk][32 * KS + 8], uint32_t ra, const uint16_t (*b)[kChunk][32 * KS + 8], uint32_t rb, uint32_t lane)
+// 16 rows of K or Q as an operand, in pieces
+template <class T, int KS>
+struct Block {
+    static constexpr int n = Pieces<T>::n;
+    bf16x8 v[KS][n];
+    __device__ __forceinline__ Block(const T *p, uint64_t ld, const Span &span, uint32_t t0, uint32_t t, uint32_t c8, uint32_t D, bool vec)
+    {
+        const bool in = t0 + t < span.len;
+        const T *row = p + span.row(in ? t0 + t : t0) * ld;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            float x[8];
+            eight<T>(row, s * 32 + c8, D, in, vec, x);
+            split8<n>(x, v[s]);
+        }
+    }
+};
+
+template <class T, int KS>
+__device__ __forceinline__ f32x4 product(const Block<T, KS> &a, const Block<T, KS> &b)
 {
     f32x4 acc = {};
-    const uint32_t la = line(ra + lane % 16), lb = line(rb + lane % 16), c = lane / 16 * 8;
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-        bf16x8 x[n], y[n];
-#pragma unroll
-        for (int p = 0; p < n; ++p) {
-            x[p] = left(&a[p][la][s * 32 + c]);
-            y[p] = left(&b[p][lb][s * 32 + c]);
-        }
-        acc = multiply<n, n>(x, y, acc);
-    }
+    for (int s = 0; s < KS; ++s) acc = multiply(a.v[s], b.v[s], acc);
     return acc;
 }
 
@@ -46,8 +54,7 @@ template <class T, int KS, bool kBackward>
 __global__ void __launch_bounds__(128)
 delta_weights_kernel(Delta d, uint64_t from)
 {
-    __shared__ Shared<T, KS> lds;
-    constexpr int n = Pieces<T>::n;
+    __shared__ Shared lds;
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c16 = lane % 16, r4 = lane / 16 * 4;
     const uint64_t unit = from + blockIdx.x;
     const uint32_t head = (uint32_t)(unit % d.H), group = d.H / d.Hk, hk = head / group;
@@ -67,82 +74,76 @@ delta_weights_kernel(Delta d, uint64_t from)
     const uint32_t t0 = c * kChunk;
     if (t0 >= span.len) return;
 
-    // wavefront 0: K; wavefront 1: Q
-    {
-        const T *rows = wave ? (const T *)d.q + hk * d.Dk : (const T *)d.k + hk * d.Dk;
-        const uint64_t ld = wave ? d.ldq : d.ldk;
-        const bool vec = wave ? d.vec_q : d.vec_k;
-        const uint32_t col = lane % (4 * KS) * 8;
-#pragma unroll
-        for (int it = 0; it < 2 * KS; ++it) {
-            const uint32_t t = it * (16 / KS) + lane / (4 * KS);
-            const bool in = t0 + t < span.len;
-            float v[8];
-            eight<T>(rows + span.row(in ? t0 + t : t0) * ld, col, d.Dk, in, vec, v);
-            put<n, KS>(v, t, col, wave ? lds.Q : lds.K, nullptr);
-        }
-    }
+    Weights &out = d.weights[slot * d.H + head];
     const uint32_t mine = lane % kChunk;
     const bool held = t0 + mine < span.len;
     const uint64_t row = span.row(held ? t0 + mine : t0);
-    const float beta = held ? d.beta[row * d.ldb + head] : 0.0f;
-    double G = held ? (double)fmaxf(d.g[row * d.ldg + head], kShut) : 0.0;
+    const float gate = d.g[row * d.ldg + head], rate = d.beta[row * d.ldb + head];
+    const T *keys = (const T *)d.k + hk * d.Dk, *queries = (const T *)d.q + hk * d.Dk;
+    const Block<T, KS> k0(keys, d.ldk, span, t0, c16, r4 * 2, d.Dk, d.vec_k), k1(keys, d.ldk, span, t0, 16 + c16, r4 * 2, d.Dk, d.vec_k);
+    const float beta = held ? rate : 0.0f;
+    double sum = held ? (double)fmaxf(gate, kShut) : 0.0;
 #pragma unroll
     for (int s = 1; s < kChunk; s *= 2) {
-        const double before = __shfl_up(G, s, kChunk);
-        if (mine >= (uint32_t)s) G += before;
+        const double before = __shfl_up(sum, s, kChunk);
+        if (mine >= (uint32_t)s) sum += before;
     }
-    const double last = __shfl(G, kChunk - 1, kChunk);
-    if (wave == 0 && lane < kChunk) {
-        const float since = expf((float)G);
-        lds.G[lane] = G;
-        lds.weight.beta[lane] = beta;
-        lds.weight.read[lane] = beta * since;
-        lds.weight.query[lane] = d.scale * since;
-        lds.weight.until[lane] = expf((float)(last - G));
-        if (lane == 0) lds.weight.whole = expf((float)last);
+    const double last = __shfl(sum, kChunk - 1, kChunk);
+    double *G = lds.G[wave];                    // each wavefront has its own, so that none waits for the other
+    if (lane < kChunk) {
+        G[lane] = sum;
+        if (wave == 0) {
+            const float since = expf((float)sum);
+            lds.beta[lane] = beta;
+            out.beta[lane] = beta;
+            out.read[lane] = kBackward ? beta * since : since;
+            out.query[lane] = d.scale * since;
+            out.until[lane] = expf((float)(last - sum));
+            if (lane == 0) out.whole = expf((float)last);
+        }
     }
-    __syncthreads();
-    const auto &K = lds.K, &Q = lds.Q;
+    wave_fence();
     const float none[4] = {};
     if (wave == 1) {
         // P; forward rows i, backward rows j
+        const Block<T, KS> q0(queries, d.ldq, span, t0, c16, r4 * 2, d.Dk, d.vec_q), q1(queries, d.ldq, span, t0, 16 + c16, r4 * 2, d.Dk, d.vec_q);
 #pragma unroll
         for (int b = 0; b < 3; ++b) {           // blocks (tokens i, tokens j): (0, 0), (1, 0), (1, 1)
             const uint32_t bi = b ? 16 : 0, bj = b == 2 ? 16 : 0;
-            const f32x4 acc = kBackward ? rows_product<n, KS>(Q, bi, K, bj, lane) : rows_product<n, KS>(K, bj, Q, bi, lane);
+            const Block<T, KS> &q = b ? q1 : q0, &k = b == 2 ? k1 : k0;
+            const f32x4 acc = kBackward ? product(q, k) : product(k, q);
             float v[4];
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
                 const uint32_t i = bi + (kBackward ? r4 + x : c16), j = bj + (kBackward ? c16 : r4 + x);
-                v[x] = i >= j ? d.scale * acc[x] * expf((float)(lds.G[i] - lds.G[j])) : 0.0f;
+                v[x] = i >= j ? d.scale * acc[x] * expf((float)(G[i] - G[j])) : 0.0f;
             }
-            if (kBackward) put4(v, lds.weight.P, bj + c16, bi + r4);
-            else put4(v, lds.weight.P, bi + c16, bj + r4);
+            if (kBackward) put4(v, out.P, bj + c16, bi + r4);
+            else put4(v, out.P, bi + c16, bj + r4);
         }
-        put4(none, lds.weight.P, kBackward ? 16 + c16 : c16, kBackward ? r4 : 16 + r4);
+        put4(none, out.P, kBackward ? 16 + c16 : c16, kBackward ? r4 : 16 + r4);
     } else {
-        put4(none, lds.weight.inverse, kBackward ? 16 + c16 : c16, kBackward ? r4 : 16 + r4);
+        put4(none, out.inverse, kBackward ? 16 + c16 : c16, kBackward ? r4 : 16 + r4);
         // A: the diagonal blocks to LDS, the other stays as an operand
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            const f32x4 acc = rows_product<n, KS>(K, b * 16, K, b * 16, lane);
+            const f32x4 acc = b ? product(k1, k1) : product(k0, k0);
             f32x4 v;
 #pragma unroll
             for (int x = 0; x < 4; ++x) {       // A[r4 + x, c16]
                 const uint32_t i = b * 16 + r4 + x, j = b * 16 + c16;
-                v[x] = i > j ? lds.weight.beta[i] * acc[x] * expf((float)(lds.G[i] - lds.G[j])) : 0.0f;
+                v[x] = i > j ? lds.beta[kBackward ? i : j] * acc[x] * expf((float)(G[i] - G[j])) : 0.0f;
             }
             *reinterpret_cast<f32x4 *>(&lds.A[b][c16][r4]) = v;
         }
         f32x4 a21;
         {
             // forward: rows i, columns j; backward: rows j, columns i
-            const f32x4 acc = kBackward ? rows_product<n, KS>(K, 0, K, 16, lane) : rows_product<n, KS>(K, 16, K, 0, lane);
+            const f32x4 acc = kBackward ? product(k0, k1) : product(k1, k0);
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
                 const uint32_t i = 16 + (kBackward ? c16 : r4 + x), j = kBackward ? r4 + x : c16;
-                a21[x] = lds.weight.beta[i] * acc[x] * expf((float)(lds.G[i] - lds.G[j]));
+                a21[x] = lds.beta[kBackward ? i : j] * acc[x] * expf((float)(G[i] - G[j]));
             }
         }
         wave_fence();
@@ -166,14 +167,14 @@ delta_weights_kernel(Delta d, uint64_t from)
             for (int j = 0; j < 16; j += 4) {
                 const float v[4] = {t[j], t[j + 1], t[j + 2], t[j + 3]};
                 *reinterpret_cast<f32x4 *>(&lds.inverse[block][c16][j]) = (f32x4){v[0], v[1], v[2], v[3]};
-                if (!kBackward) put4(v, lds.weight.inverse, block * 16 + c16, block * 16 + j);
+                if (!kBackward) put4(v, out.inverse, block * 16 + c16, block * 16 + j);
             }
         wave_fence();
         if (kBackward && lane < 32)             // rows of T^T
 #pragma unroll
             for (int j = 0; j < 16; j += 4) {
                 const float v[4] = {lds.inverse[block][j][c16], lds.inverse[block][j + 1][c16], lds.inverse[block][j + 2][c16], lds.inverse[block][j + 3][c16]};
-                put4(v, lds.weight.inverse, block * 16 + c16, block * 16 + j);
+                put4(v, out.inverse, block * 16 + c16, block * 16 + j);
             }
         // the block below the diagonal in fp32: forward as its transpose (A21^T T22^T, then T11^T times that), so that a lane has four values of a row
         // of what is stored in either case
@@ -188,20 +189,17 @@ delta_weights_kernel(Delta d, uint64_t from)
         for (int s = 0; s < 4; ++s) x = __builtin_amdgcn_mfma_f32_16x16x4f32(kBackward ? t22[s] : t11[s], w[s], x, 0, 0, 0);
         const float v[4] = {-x[0], -x[1], -x[2], -x[3]};
         // forward: lane i, values j; backward: lane j, values i
-        if (kBackward) put4(v, lds.weight.inverse, c16, 16 + r4);
-        else put4(v, lds.weight.inverse, 16 + c16, r4);
+        if (kBackward) put4(v, out.inverse, c16, 16 + r4);
+        else put4(v, out.inverse, 16 + c16, r4);
     }
-    __syncthreads();
-    uint8_t *to = (uint8_t *)(d.weights + slot * d.H + head);
-    for (uint32_t at = threadIdx.x * 16; at < sizeof(Weights); at += 128 * 16) *reinterpret_cast<u32x4 *>(to + at) = *reinterpret_cast<const u32x4 *>((const uint8_t *)&lds.weight + at);
 }
 
 template <class T, int KS, bool kBackward>
 void launch_size(const Delta &d, hipStream_t st)
 {
     const uint64_t slots = d.first ? chunk_slots(d.N, d.n_seq) : d.n_seq * ((d.N / d.n_seq + kChunk - 1) / kChunk), units = slots * d.H;
-    for (uint64_t from = 0; from < units; from += kMostGroups) {
-        const uint32_t grid = (uint32_t)(units - from < kMostGroups ? units - from : kMostGroups);
+    for (uint64_t from = 0; from < units; from += kMostLaunched) {
+        const uint32_t grid = (uint32_t)(units - from < kMostLaunched ? units - from : kMostLaunched);
         delta_weights_kernel<T, KS, kBackward><<<grid, 128, 0, st>>>(d, from);
     }
 }
