@@ -87,7 +87,7 @@ extern "C" int dg_delta_rule_fwd(const void *q, uint64_t ldq, const void *k, uin
     d.q = q, d.k = k, d.v = v, d.g = g, d.beta = beta, d.ldq = ldq, d.ldk = ldk, d.ldv = ldv, d.ldg = ldg, d.ldb = ldbeta, d.s0 = s0, d.o = o, d.ldo = ldo, d.s_last = s_last;
     d.first = first, d.N = N, d.n_seq = n_seq, d.Hk = Hk, d.H = H, d.Dk = Dk, d.Dv = Dv, d.reverse = reverse, d.scale = scale;
     if (saved) d.marks = (float *)saved, d.y = (float *)((char *)saved + padded(marks_bytes(N, n_seq, H, Dk, Dv)));
-    d.vec_q = wide_rows(q, ldq, Dk, dtype), d.vec_k = wide_rows(k, ldk, Dk, dtype), d.vec_v = wide_rows(v, ldv, Dv, dtype);
+    d.vec_q = wide_rows(q, ldq, Dk, dtype), d.vec_k = wide_rows(k, ldk, Dk, dtype), d.vec_v = wide_rows(v, ldv, Dv, dtype), d.vec_o = wide_rows(o, ldo, Dv, dtype);
     if (takes_small(n_seq, H, Dk, Dv)) launch_small(d, dtype, false, (hipStream_t)stream);
     else if (!saved && N <= kFewTokens * n_seq) launch_tokens(d, dtype, (hipStream_t)stream);
     else {

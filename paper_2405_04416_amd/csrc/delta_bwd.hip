@@ -7,106 +7,145 @@ namespace {
 
 using namespace dg_delta;
 
+// A chunk for a wavefront with 16 columns of the gradient, S.  dout: that of o of the lane's eight tokens; gradient: that of what they write.
 template <class T, int KS>
+__device__ __forceinline__ void take_chunk(const Operands<T, KS, true> &o, uint32_t c16, uint32_t r8, const float (&dout)[8], f32x4 (&S)[2 * KS], float (&gradient)[8])
+{
+    constexpr int n = Pieces<T>::n, kTiles = 2 * KS;
+    bf16x8 keys[KS][2][n], inverse[2][3], pull[2][3];
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) lefts(o.key.K, h * 16 + c16, s * 32 + r8, keys[s][h]);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        lefts(o.weight.P, h * 16 + c16, r8, pull[h]);
+        lefts(o.weight.inverse, h * 16 + c16, r8, inverse[h]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    f32x4 ks[2] = {};
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+        bf16x8 sp[3];
+        split_rows<3>(S[2 * s], S[2 * s + 1], sp);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) ks[h] = multiply<n, 3>(keys[s][h], sp, ks[h]);
+    }
+    bf16x8 turned[kTiles][n], queries[kTiles][n];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        lefts(o.key.KT, t * 16 + c16, r8, turned[t]);
+        lefts(o.key.Q, t * 16 + c16, r8, queries[t]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    bf16x8 exact[n], right[3], right_q[3];
+    split8<n>(dout, exact);
+    f32x4 du[2], dr[2], back[2];
+    float queried[8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const f32x4 until = *reinterpret_cast<const f32x4 *>(&o.weight.until[r8 + h * 4]), query = *reinterpret_cast<const f32x4 *>(&o.weight.query[r8 + h * 4]);
+        du[h] = multiply<3, n>(pull[h], exact, until * ks[h]);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) queried[h * 4 + x] = dout[h * 4 + x] * query[x];
+    }
+    split_rows<3>(du[0], du[1], right);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        dr[h] = multiply<3, 3>(inverse[h], right, (f32x4){});
+        back[h] = -dr[h] * *reinterpret_cast<const f32x4 *>(&o.weight.read[r8 + h * 4]);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) gradient[h * 4 + x] = dr[h][x];
+    }
+    split8<3>(queried, right_q);
+    split_rows<3>(back[0], back[1], right);
+    const float whole = o.weight.whole;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        S[t] = multiply<n, 3>(queries[t], right_q, S[t] * whole);
+        S[t] = multiply<n, 3>(turned[t], right, S[t]);
+    }
+}
+
+template <class T, int KS, bool kHelped>
+struct Lds { using type = Room<T, KS, true>; };
+template <class T, int KS>
+struct Lds<T, KS, true> { using type = Helped<T, KS, true>; };
+
+template <class T, int KS, bool kHelped>
 __global__ void __launch_bounds__(kMostWaves * 64)
 delta_bwd_kernel(Delta d, uint32_t with, uint32_t groups, uint64_t from)
 {
-    __shared__ alignas(16) Room<T, KS, true> room;
-    constexpr int n = Pieces<T>::n, kTiles = 2 * KS;
+    __shared__ typename Lds<T, KS, kHelped>::type room;
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = blockDim.x / 64, c16 = lane % 16, r8 = lane / 16 * 8;
     const uint64_t unit = from + blockIdx.x;
-    const uint32_t head = (uint32_t)(unit / groups % d.H), seq = (uint32_t)(unit / groups / d.H), col = ((uint32_t)(unit % groups) * with + wave) * 16 + c16;
+    const uint32_t head = (uint32_t)(unit / groups % d.H), seq = (uint32_t)(unit / groups / d.H), column0 = (uint32_t)(unit % groups) * with * 16, col = column0 + wave * 16 + c16;
     const Span span = span_of(d, seq);
     const bool in = wave < with && col < d.Dv;
     const uint64_t memory = ((uint64_t)seq * d.H + head) * d.Dk * d.Dv + col;
-    f32x4 S[kTiles];
+    const uint32_t last = span.len ? (span.len - 1) / kChunk : 0;
+    f32x4 S[2 * KS];
     load_memory<KS>(d.ds_last ? d.ds_last + memory : nullptr, d.Dk, d.Dv, in, r8, S);
-    const T *gradients = (const T *)d.dout + head * d.Dv;
-    const uint32_t at = in ? col : 0, last = span.len ? (span.len - 1) / kChunk : 0;
-    T next[8];
-    float gradient[8];                  // of the chunk before: stored when the next one's loads are on their way
-    auto store = [&](uint32_t t0) { store_column<float>(d.dr + head * d.Dv, (uint64_t)d.H * d.Dv, at, span, t0, r8, in, gradient); };
-    load_column<T>(gradients, d.lddo, at, span, last * kChunk, r8, next);
-    along<T, KS, true>(d, span, seq, head, room, wave, waves, [&](const Operands<T, KS, true> &o, uint32_t c) {
-        if (wave >= with) return;
-        const uint32_t t0 = c * kChunk;
+    auto mark = [&](uint32_t c) {
         if (c == last || c % (kMark / kChunk) == kMark / kChunk - 1)
             store_memory<KS>(d.dmarks + ((uint64_t)(first_slot(span, seq) + c / (kMark / kChunk)) * d.H + head) * d.Dk * d.Dv + col, d.Dk, d.Dv, in, r8, S);
-        if (c != last) store(t0 + kChunk);
-        float dout[8];
+    };
+    float dout[8], gradient[8];
+    if constexpr (kHelped) {
+        along_helped<T, KS, true>(d, span, seq, head, column0, room, wave, with, waves, [&](const Operands<T, KS, true> &o, uint32_t c, Tiles<T, true> &tile) {
+            mark(c);
+            const uint32_t at = wave * 16 + c16;
 #pragma unroll
-        for (int x = 0; x < 8; ++x) dout[x] = held(next[x], span, t0 + r8 + x, in);
-        load_column<T>(gradients, d.lddo, at, span, c ? t0 - kChunk : 0, r8, next);
-
-        bf16x8 keys[KS][2][n], inverse[2][3], pull[2][3];
+            for (int x = 0; x < 8; ++x) dout[x] = (float)tile.in[r8 + x][at];
+            take_chunk<T, KS>(o, c16, r8, dout, S, gradient);
 #pragma unroll
-        for (int s = 0; s < KS; ++s)
+            for (int x = 0; x < 8; ++x) tile.wide[r8 + x][at] = gradient[x];
+        });
+    } else {
+        const T *gradients = (const T *)d.dout + head * d.Dv;
+        const uint32_t at = in ? col : 0;
+        T next[8];
+        // of the chunk before: stored when the next one's loads are on their way
+        auto store = [&](uint32_t t0) { store_column<float>(d.dr + head * d.Dv, (uint64_t)d.H * d.Dv, at, span, t0, r8, in, gradient); };
+        load_column<T>(gradients, d.lddo, at, span, last * kChunk, r8, next);
+        along<T, KS, true>(d, span, seq, head, room, wave, waves, [&](const Operands<T, KS, true> &o, uint32_t c) {
+            if (wave >= with) return;
+            const uint32_t t0 = c * kChunk;
+            mark(c);
+            if (c != last) store(t0 + kChunk);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) lefts(o.key.K, h * 16 + c16, s * 32 + r8, keys[s][h]);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            lefts(o.weight.P, h * 16 + c16, r8, pull[h]);
-            lefts(o.weight.inverse, h * 16 + c16, r8, inverse[h]);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        f32x4 ks[2] = {};
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            bf16x8 sp[3];
-            split_rows<3>(S[2 * s], S[2 * s + 1], sp);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) ks[h] = multiply<n, 3>(keys[s][h], sp, ks[h]);
-        }
-        bf16x8 turned[kTiles][n], queries[kTiles][n];
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-            lefts(o.key.KT, t * 16 + c16, r8, turned[t]);
-            lefts(o.key.Q, t * 16 + c16, r8, queries[t]);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        bf16x8 exact[n], right[3], right_q[3];
-        split8<n>(dout, exact);
-        f32x4 du[2], dr[2], back[2];
-        float queried[8];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const f32x4 until = *reinterpret_cast<const f32x4 *>(&o.weight.until[r8 + h * 4]), query = *reinterpret_cast<const f32x4 *>(&o.weight.query[r8 + h * 4]);
-            du[h] = multiply<3, n>(pull[h], exact, until * ks[h]);
-#pragma unroll
-            for (int x = 0; x < 4; ++x) queried[h * 4 + x] = dout[h * 4 + x] * query[x];
-        }
-        split_rows<3>(du[0], du[1], right);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            dr[h] = multiply<3, 3>(inverse[h], right, (f32x4){});
-            back[h] = -dr[h] * *reinterpret_cast<const f32x4 *>(&o.weight.read[r8 + h * 4]);
-#pragma unroll
-            for (int x = 0; x < 4; ++x) gradient[h * 4 + x] = dr[h][x];
-        }
-        split8<3>(queried, right_q);
-        split_rows<3>(back[0], back[1], right);
-        const float whole = o.weight.whole;
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-            S[t] = multiply<n, 3>(queries[t], right_q, S[t] * whole);
-            S[t] = multiply<n, 3>(turned[t], right, S[t]);
-        }
-    });
-    if (span.len && wave < with) store(0);
+            for (int x = 0; x < 8; ++x) dout[x] = held(next[x], span, t0 + r8 + x, in);
+            load_column<T>(gradients, d.lddo, at, span, c ? t0 - kChunk : 0, r8, next);
+            take_chunk<T, KS>(o, c16, r8, dout, S, gradient);
+        });
+        if (span.len && wave < with) store(0);
+    }
     if (d.ds0) store_memory<KS>(d.ds0 + memory, d.Dk, d.Dv, in, r8, S);
+}
+
+template <class T, int KS>
+void launch_size(const Delta &d, hipStream_t st)
+{
+    constexpr bool kRoom = sizeof(Helped<T, KS, true>) <= 160 * 1024;
+    const Columns c = columns_of(d, kRoom);
+    const uint64_t units = (uint64_t)d.n_seq * d.H * c.groups;
+    for (uint64_t from = 0; from < units; from += kMostLaunched) {
+        const uint32_t grid = (uint32_t)(units - from < kMostLaunched ? units - from : kMostLaunched);
+        if constexpr (kRoom)
+            if (c.helped) {
+                delta_bwd_kernel<T, KS, true><<<grid, c.waves * 64, 0, st>>>(d, c.with, c.groups, from);
+                continue;
+            }
+        delta_bwd_kernel<T, KS, false><<<grid, c.waves * 64, 0, st>>>(d, c.with, c.groups, from);
+    }
 }
 
 template <class T>
 void launch_type(const Delta &d, hipStream_t st)
 {
-    const Columns c = columns_of(d);
-    const uint64_t units = (uint64_t)d.n_seq * d.H * c.groups;
-    for (uint64_t from = 0; from < units; from += kMostLaunched) {
-        const uint32_t grid = (uint32_t)(units - from < kMostLaunched ? units - from : kMostLaunched), threads = c.waves * 64;
-        if (d.Dk <= 32) delta_bwd_kernel<T, 1><<<grid, threads, 0, st>>>(d, c.with, c.groups, from);
-        else if (d.Dk <= 64) delta_bwd_kernel<T, 2><<<grid, threads, 0, st>>>(d, c.with, c.groups, from);
-        else delta_bwd_kernel<T, 4><<<grid, threads, 0, st>>>(d, c.with, c.groups, from);
-    }
+    if (d.Dk <= 32) launch_size<T, 1>(d, st);
+    else if (d.Dk <= 64) launch_size<T, 2>(d, st);
+    else launch_size<T, 4>(d, st);
 }
 
 }  // namespace

@@ -26,11 +26,13 @@ struct alignas(16) Keys {
     uint16_t Q[n][kBackward ? DK : kChunk][kBackward ? kPitch : DK + 8];       // backward: Q^T
 };
 
-struct alignas(kPage) Weights {
+struct alignas(16) Weights {
     uint16_t inverse[3][kChunk][kPitch], P[3][kChunk][kPitch];                 // T and P; backward: T^T and P^T
     float beta[kChunk], read[kChunk], query[kChunk], until[kChunk];            // beta, e^G (backward: beta e^G), scale e^G, e^(G[last] - G)
     float whole;                                                               // e^G[last]
+    float rest[127];                                                           // of a page
 };
+static_assert(sizeof(Weights) % kPage == 0, "fetched by pages");
 
 // In the workspace: a chunk's slot has those of its heads.  A sequence's first slot is floor(begin / 32) + its number, which leaves room for all.
 inline uint64_t chunk_slots(uint64_t N, uint32_t n_seq) { return N / kChunk + n_seq; }
@@ -87,6 +89,15 @@ struct Room {
     Operands<T, KS, kBackward> ops[kBuffers];
 };
 
+// Where some wavefronts have columns and the others bring what these need and take away what they leave: up to 32 columns of a chunk's tokens
+constexpr int kTileColumns = 32;
+template <class T, bool kBackward>
+struct alignas(16) Tiles {
+    T in[kChunk][kTileColumns + 8];                             // v, or gradients of o
+    T out[kBackward ? 1 : kChunk][kTileColumns + 8];            // o
+    float wide[kChunk][kTileColumns + 4];                       // what tokens miss, or gradients of what they write
+};
+
 // eight values of a token: as they lie in its row, and each into its column's row
 template <int n, int KS>
 __device__ __forceinline__ void put(const float (&v)[8], uint32_t t, uint32_t col, uint16_t (*rows)[kChunk][32 * KS + 8], uint16_t (*columns)[32 * KS][kPitch])
@@ -102,8 +113,8 @@ __device__ __forceinline__ void put(const float (&v)[8], uint32_t t, uint32_t co
     }
 }
 
-// K and Q of a chunk on their way to LDS: a workgroup has at least KS wavefronts, so that two vectors of each are enough for a lane
-template <class T, int KS, bool kBackward>
+// K and Q of a chunk on their way to LDS, kEach vectors of each for a lane: a workgroup has wavefronts enough for that
+template <class T, int KS, bool kBackward, int kEach>
 struct Rows {
     static constexpr int n = Pieces<T>::n;
     const T *q, *k;
@@ -111,7 +122,7 @@ struct Rows {
     uint32_t Dk, wave, waves, lane;
     bool vec;
     Span span;
-    dg_rows::Pack<T, 8> qs[2], ks[2];
+    dg_rows::Pack<T, 8> qs[kEach], ks[kEach];
 
     __device__ __forceinline__ uint32_t token(int i) const { return (i * waves + wave) * (16 / KS) + lane / (4 * KS); }
     __device__ __forceinline__ uint32_t column() const { return lane % (4 * KS) * 8; }
@@ -122,7 +133,7 @@ struct Rows {
         if (!vec) return;
         constexpr int m = 16 / sizeof(T);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kEach; ++i) {
             const uint32_t t = c * kChunk + token(i);
             const uint64_t row = span.row(token(i) < kChunk && t < span.len ? t : c * kChunk);
 #pragma unroll
@@ -141,7 +152,7 @@ struct Rows {
     __device__ __forceinline__ void store(uint32_t c, Keys<T, KS, kBackward> &to)
     {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kEach; ++i) {
             const uint32_t t = token(i);
             if (t >= kChunk) continue;
             float x[8], y[8];
@@ -174,7 +185,7 @@ __device__ __forceinline__ void along(const Delta &d, const Span &span, uint32_t
     if (chunks == 0) return;
     const uint64_t slot0 = first_chunk(span, seq);
     auto chunk = [&](uint32_t i) { return kBackward ? chunks - 1 - i : i; };
-    Rows<T, KS, kBackward> rows = {(const T *)d.q + hk * d.Dk, (const T *)d.k + hk * d.Dk, d.ldq, d.ldk, d.Dk, wave, waves, threadIdx.x % 64, d.vec_q && d.vec_k, span, {}, {}};
+    Rows<T, KS, kBackward, 2> rows = {(const T *)d.q + hk * d.Dk, (const T *)d.k + hk * d.Dk, d.ldq, d.ldk, d.Dk, wave, waves, threadIdx.x % 64, d.vec_q && d.vec_k, span, {}, {}};
     auto weights = [&](uint32_t i) {
         const uint8_t *from = (const uint8_t *)(d.weights + (slot0 + chunk(i)) * d.H + head) + threadIdx.x % 64 * 16;
         uint8_t *to = (uint8_t *)&room.ops[i % kBuffers].weight;
@@ -201,16 +212,155 @@ __device__ __forceinline__ void along(const Delta &d, const Span &span, uint32_t
     }
 }
 
-// How many wavefronts of a workgroup have columns, how many there are (those that fetch K and Q alone among them), and how many workgroups a head has
-struct Columns { uint32_t with, waves, groups; };
+// The same with wavefronts `with` on bringing and taking away.  use(operands, chunk, tile) for those that have columns; in, out, wide: columns of the workgroup in
+// rows of tokens.  What is brought is fetched two chunks ahead.
+template <class T, int KS, bool kBackward>
+struct Helped {
+    static constexpr int kWeights = 8;          // of 16 bytes to a lane: all of them with two wavefronts
+    static_assert(sizeof(Weights) <= kWeights * 128 * 16, "two wavefronts bring the weights");
+    Operands<T, KS, kBackward> ops[2];
+    Tiles<T, kBackward> tiles[2];
+};
 
-inline Columns columns_of(const Delta &d)
+template <class T, int KS, bool kBackward>
+struct Helper {
+    static constexpr int kWeights = Helped<T, KS, kBackward>::kWeights;
+    const Delta &d;
+    const Span &span;
+    uint64_t slot0;
+    uint32_t head, lanes, self, columns, column0;       // lanes that help, this one among them
+    Rows<T, KS, kBackward, 4> rows;
+    u32x4 weights[kWeights];
+    dg_rows::Pack<T, 8> in;
+
+    __device__ __forceinline__ uint32_t token() const { return self * 8 / columns; }
+    __device__ __forceinline__ uint32_t column() const { return self * 8 % columns; }
+    // row of a token of chunk c, another where it is none
+    __device__ __forceinline__ uint64_t row_of(uint32_t c, uint32_t t) const { return span.row(c * kChunk + t < span.len ? c * kChunk + t : c * kChunk); }
+
+    __device__ __forceinline__ void fetch(uint32_t c)
+    {
+        rows.fetch(c);
+        const u32x4 *from = (const u32x4 *)(d.weights + (slot0 + c) * d.H + head);
+#pragma unroll
+        for (int i = 0; i < kWeights; ++i) {
+            const uint32_t at = i * lanes + self;
+            weights[i] = from[at < sizeof(Weights) / 16 ? at : 0];
+        }
+        if (self * 8 >= kChunk * columns) return;
+        const T *p = kBackward ? (const T *)d.dout + row_of(c, token()) * d.lddo : (const T *)d.v + row_of(c, token()) * d.ldv;
+        const uint32_t first = column0 + column();
+        p += head * d.Dv;
+        if (kBackward ? d.vec_o : d.vec_v) {
+            constexpr int m = 16 / sizeof(T);
+#pragma unroll
+            for (int h = 0; h < 8 / m; ++h) {
+                const dg_rows::Pack<T, m> x = *reinterpret_cast<const dg_rows::Pack<T, m> *>(p + (first + h * m < d.Dv ? first + h * m : 0));
+#pragma unroll
+                for (int j = 0; j < m; ++j) in.v[h * m + j] = x.v[j];
+            }
+        } else
+#pragma unroll
+            for (int j = 0; j < 8; ++j) in.v[j] = p[first + j < d.Dv ? first + j : 0];
+    }
+
+    __device__ __forceinline__ void put(uint32_t c, Operands<T, KS, kBackward> &ops, Tiles<T, kBackward> &tile)
+    {
+        u32x4 *to = (u32x4 *)&ops.weight;
+#pragma unroll
+        for (int i = 0; i < kWeights; ++i) {
+            const uint32_t at = i * lanes + self;
+            if (at < sizeof(Weights) / 16) to[at] = weights[i];
+        }
+        rows.store(c, ops.key);
+        if (self * 8 >= kChunk * columns) return;
+        const bool there = c * kChunk + token() < span.len;
+        dg_rows::Pack<T, 8> x;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x.v[j] = there && column0 + column() + j < d.Dv ? in.v[j] : (T)0.0f;
+        constexpr int m = 16 / sizeof(T);
+#pragma unroll
+        for (int h = 0; h < 8 / m; ++h) {
+            dg_rows::Pack<T, m> part;
+#pragma unroll
+            for (int j = 0; j < m; ++j) part.v[j] = x.v[h * m + j];
+            *reinterpret_cast<dg_rows::Pack<T, m> *>(&tile.in[token()][column() + h * m]) = part;
+        }
+    }
+
+    template <class E, int pitch>
+    __device__ __forceinline__ void take(const E (&tile)[kChunk][pitch], E *p, bool vec) const
+    {
+        constexpr int m = 16 / sizeof(E);
+        const uint32_t first = column0 + column();
+#pragma unroll
+        for (int h = 0; h < 8 / m; ++h) {
+            const dg_rows::Pack<E, m> x = *reinterpret_cast<const dg_rows::Pack<E, m> *>(&tile[token()][column() + h * m]);
+            if (vec && first + h * m < d.Dv) *reinterpret_cast<dg_rows::Pack<E, m> *>(p + first + h * m) = x;
+            else
+#pragma unroll
+                for (int j = 0; j < m; ++j)
+                    if (first + h * m + j < d.Dv) p[first + h * m + j] = x.v[j];
+        }
+    }
+
+    __device__ __forceinline__ void take_away(uint32_t c, const Tiles<T, kBackward> &tile) const
+    {
+        if (self * 8 >= kChunk * columns || c * kChunk + token() >= span.len) return;
+        const uint64_t row = row_of(c, token());
+        if constexpr (!kBackward) take(tile.out, (T *)d.o + row * d.ldo + head * d.Dv, d.vec_o);
+        float *wide = kBackward ? d.dr : d.y;
+        if (wide) take(tile.wide, wide + (row * d.H + head) * d.Dv, d.Dv % 4 == 0);
+    }
+};
+
+template <class T, int KS, bool kBackward, class Use>
+__device__ __forceinline__ void along_helped(const Delta &d, const Span &span, uint32_t seq, uint32_t head, uint32_t column0, Helped<T, KS, kBackward> &room, uint32_t wave, uint32_t with,
+                                             uint32_t waves, Use use)
+{
+    const uint32_t chunks = (span.len + kChunk - 1) / kChunk, hk = head / (d.H / d.Hk);
+    if (chunks == 0) return;
+    auto chunk = [&](uint32_t i) { return kBackward ? chunks - 1 - i : i; };
+    if (wave < with) {
+        for (uint32_t i = 0; i < chunks; ++i) {
+            __syncthreads();
+            use(room.ops[i % 2], chunk(i), room.tiles[i % 2]);
+        }
+        __syncthreads();
+        return;
+    }
+    const uint32_t helpers = waves - with;
+    Helper<T, KS, kBackward> h = {d, span, first_chunk(span, seq), head, helpers * 64, threadIdx.x - with * 64, with * 16, column0,
+                                  {(const T *)d.q + hk * d.Dk, (const T *)d.k + hk * d.Dk, d.ldq, d.ldk, d.Dk, wave - with, helpers, threadIdx.x % 64, d.vec_q && d.vec_k, span, {}, {}}, {}, {}};
+    h.fetch(chunk(0));
+    h.put(chunk(0), room.ops[0], room.tiles[0]);
+    if (chunks > 1) h.fetch(chunk(1));
+    for (uint32_t i = 0; i < chunks; ++i) {
+        __syncthreads();
+        if (i + 1 < chunks) h.put(chunk(i + 1), room.ops[(i + 1) % 2], room.tiles[(i + 1) % 2]);
+        if (i + 2 < chunks) h.fetch(chunk(i + 2));
+        if (i) h.take_away(chunk(i - 1), room.tiles[(i - 1) % 2]);
+    }
+    __syncthreads();
+    h.take_away(chunk(chunks - 1), room.tiles[(chunks - 1) % 2]);
+}
+
+// How many wavefronts of a workgroup have columns, how many there are (those that help among them), and how many workgroups a head has
+struct Columns { uint32_t with, waves, groups; bool helped; };
+
+// With fewer heads than the chip has room for, one or two wavefronts of a workgroup have columns and the others help; otherwise as many as possible have
+// columns and all help.  room: whether there is any for two buffers and the tiles.
+inline Columns columns_of(const Delta &d, bool room)
 {
     const uint32_t all = (d.Dv + 15) / 16, least = d.Dk <= 32 ? 1 : d.Dk <= 64 ? 2 : 4;
     const uint64_t units = (uint64_t)d.n_seq * d.H;
+    if (room && units * all <= 512) {
+        const uint32_t with = units * all <= 256 || all == 1 ? 1 : 2;
+        return {with, 4, (all + with - 1) / with, true};
+    }
     uint32_t with = all < (uint32_t)kMostWaves ? all : kMostWaves;
     while (with > 1 && units * ((all + with - 1) / with) < 256) with = (with + 1) / 2;        // few heads: as many workgroups as there are compute units
-    return {with, with < least ? least : with, (all + with - 1) / with};
+    return {with, with < least ? least : with, (all + with - 1) / with, false};
 }
 
 // Memories in registers: result t of 2 KS has rows 32 (t / 2) + 8 q + 4 (t % 2) on with lane (column, q)

@@ -5,116 +5,157 @@ namespace {
 
 using namespace dg_delta;
 
+// A chunk for a wavefront with 16 columns of the memory, S.  value: v of the lane's eight tokens; out, missed: o and what they miss.
 template <class T, int KS>
+__device__ __forceinline__ void take_chunk(const Operands<T, KS, false> &o, uint32_t c16, uint32_t r8, const float (&value)[8], f32x4 (&S)[2 * KS], float (&out)[8], float (&missed)[8])
+{
+    constexpr int n = Pieces<T>::n, kTiles = 2 * KS;
+    bf16x8 keys[KS][2][n], queries[KS][2][n], inverse[2][3], pull[2][3];
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            lefts(o.key.K, h * 16 + c16, s * 32 + r8, keys[s][h]);
+            lefts(o.key.Q, h * 16 + c16, s * 32 + r8, queries[s][h]);
+        }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        lefts(o.weight.inverse, h * 16 + c16, r8, inverse[h]);
+        lefts(o.weight.P, h * 16 + c16, r8, pull[h]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    f32x4 ks[2] = {}, qs[2] = {};
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+        bf16x8 sp[3];
+        split_rows<3>(S[2 * s], S[2 * s + 1], sp);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            ks[h] = multiply<n, 3>(keys[s][h], sp, ks[h]);
+            qs[h] = multiply<n, 3>(queries[s][h], sp, qs[h]);
+        }
+    }
+    bf16x8 turned[kTiles][n];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) lefts(o.key.KT, t * 16 + c16, r8, turned[t]);
+    __builtin_amdgcn_sched_barrier(0);
+    f32x4 r[2], u[2], beta[2], until[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const f32x4 read = *reinterpret_cast<const f32x4 *>(&o.weight.read[r8 + h * 4]);
+        beta[h] = *reinterpret_cast<const f32x4 *>(&o.weight.beta[r8 + h * 4]);
+        until[h] = *reinterpret_cast<const f32x4 *>(&o.weight.until[r8 + h * 4]);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) r[h][x] = value[h * 4 + x] - read[x] * ks[h][x];
+    }
+    bf16x8 right[3];
+    split_rows<3>(r[0], r[1], right);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const f32x4 y = multiply<3, 3>(inverse[h], right, (f32x4){});
+#pragma unroll
+        for (int x = 0; x < 4; ++x) missed[h * 4 + x] = y[x];
+        u[h] = y * beta[h];
+    }
+    bf16x8 written[3];
+    split_rows<3>(u[0] * until[0], u[1] * until[1], written);
+    const float whole = o.weight.whole;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) S[t] = multiply<n, 3>(turned[t], written, S[t] * whole);
+    split_rows<3>(u[0], u[1], right);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const f32x4 query = *reinterpret_cast<const f32x4 *>(&o.weight.query[r8 + h * 4]);
+        const f32x4 sum = multiply<3, 3>(pull[h], right, query * qs[h]);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) out[h * 4 + x] = sum[x];
+    }
+}
+
+template <class T, int KS, bool kHelped>
+struct Lds { using type = Room<T, KS, false>; };
+template <class T, int KS>
+struct Lds<T, KS, true> { using type = Helped<T, KS, false>; };
+
+template <class T, int KS, bool kHelped>
 __global__ void __launch_bounds__(kMostWaves * 64)
 delta_fwd_kernel(Delta d, uint32_t with, uint32_t groups, uint64_t from)
 {
-    __shared__ alignas(16) Room<T, KS, false> room;
-    constexpr int n = Pieces<T>::n, kTiles = 2 * KS;
+    __shared__ typename Lds<T, KS, kHelped>::type room;
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = blockDim.x / 64, c16 = lane % 16, r8 = lane / 16 * 8;
     const uint64_t unit = from + blockIdx.x;
-    const uint32_t head = (uint32_t)(unit / groups % d.H), seq = (uint32_t)(unit / groups / d.H), col = ((uint32_t)(unit % groups) * with + wave) * 16 + c16;
+    const uint32_t head = (uint32_t)(unit / groups % d.H), seq = (uint32_t)(unit / groups / d.H), column0 = (uint32_t)(unit % groups) * with * 16, col = column0 + wave * 16 + c16;
     const Span span = span_of(d, seq);
     const bool in = wave < with && col < d.Dv;
     const uint64_t memory = ((uint64_t)seq * d.H + head) * d.Dk * d.Dv + col;
-    f32x4 S[kTiles];
+    f32x4 S[2 * KS];
     load_memory<KS>(d.s0 ? d.s0 + memory : nullptr, d.Dk, d.Dv, in, r8, S);
-    const T *values = (const T *)d.v + head * d.Dv;
-    const uint32_t at = in ? col : 0;
-    T next[8];
-    float out[8], missed[8];            // of the chunk before: stored when the next one's loads are on their way, so that none waits for a store
-    auto store = [&](uint32_t t0) {
-        store_column<T>((T *)d.o + head * d.Dv, d.ldo, at, span, t0, r8, in, out);
-        if (d.y) store_column<float>(d.y + head * d.Dv, (uint64_t)d.H * d.Dv, at, span, t0, r8, in, missed);
-    };
-    load_column<T>(values, d.ldv, at, span, 0, r8, next);
-    along<T, KS, false>(d, span, seq, head, room, wave, waves, [&](const Operands<T, KS, false> &o, uint32_t c) {
-        if (wave >= with) return;
-        const uint32_t t0 = c * kChunk;
+    auto mark = [&](uint32_t c) {
         if (d.marks && c % (kMark / kChunk) == 0)
             store_memory<KS>(d.marks + ((uint64_t)(first_slot(span, seq) + c / (kMark / kChunk)) * d.H + head) * d.Dk * d.Dv + col, d.Dk, d.Dv, in, r8, S);
-        if (c) store(t0 - kChunk);
-        float value[8];
+    };
+    float value[8], out[8], missed[8];
+    if constexpr (kHelped) {
+        along_helped<T, KS, false>(d, span, seq, head, column0, room, wave, with, waves, [&](const Operands<T, KS, false> &o, uint32_t c, Tiles<T, false> &tile) {
+            mark(c);
+            const uint32_t at = wave * 16 + c16;
 #pragma unroll
-        for (int x = 0; x < 8; ++x) value[x] = held(next[x], span, t0 + r8 + x, in);
-        load_column<T>(values, d.ldv, at, span, t0 + kChunk, r8, next);
-
-        bf16x8 keys[KS][2][n], queries[KS][2][n], inverse[2][3], pull[2][3];
+            for (int x = 0; x < 8; ++x) value[x] = (float)tile.in[r8 + x][at];
+            take_chunk<T, KS>(o, c16, r8, value, S, out, missed);
 #pragma unroll
-        for (int s = 0; s < KS; ++s)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                lefts(o.key.K, h * 16 + c16, s * 32 + r8, keys[s][h]);
-                lefts(o.key.Q, h * 16 + c16, s * 32 + r8, queries[s][h]);
+            for (int x = 0; x < 8; ++x) {
+                tile.out[r8 + x][at] = (T)out[x];
+                if (d.y) tile.wide[r8 + x][at] = missed[x];
             }
+        });
+    } else {
+        const T *values = (const T *)d.v + head * d.Dv;
+        const uint32_t at = in ? col : 0;
+        T next[8];
+        // of the chunk before: stored when the next one's loads are on their way, so that none waits for a store
+        auto store = [&](uint32_t t0) {
+            store_column<T>((T *)d.o + head * d.Dv, d.ldo, at, span, t0, r8, in, out);
+            if (d.y) store_column<float>(d.y + head * d.Dv, (uint64_t)d.H * d.Dv, at, span, t0, r8, in, missed);
+        };
+        load_column<T>(values, d.ldv, at, span, 0, r8, next);
+        along<T, KS, false>(d, span, seq, head, room, wave, waves, [&](const Operands<T, KS, false> &o, uint32_t c) {
+            if (wave >= with) return;
+            const uint32_t t0 = c * kChunk;
+            mark(c);
+            if (c) store(t0 - kChunk);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            lefts(o.weight.inverse, h * 16 + c16, r8, inverse[h]);
-            lefts(o.weight.P, h * 16 + c16, r8, pull[h]);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        f32x4 ks[2] = {}, qs[2] = {};
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            bf16x8 sp[3];
-            split_rows<3>(S[2 * s], S[2 * s + 1], sp);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                ks[h] = multiply<n, 3>(keys[s][h], sp, ks[h]);
-                qs[h] = multiply<n, 3>(queries[s][h], sp, qs[h]);
-            }
-        }
-        bf16x8 turned[kTiles][n];
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) lefts(o.key.KT, t * 16 + c16, r8, turned[t]);
-        __builtin_amdgcn_sched_barrier(0);
-        f32x4 r[2], u[2], beta[2], until[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const f32x4 read = *reinterpret_cast<const f32x4 *>(&o.weight.read[r8 + h * 4]);
-            beta[h] = *reinterpret_cast<const f32x4 *>(&o.weight.beta[r8 + h * 4]);
-            until[h] = *reinterpret_cast<const f32x4 *>(&o.weight.until[r8 + h * 4]);
-#pragma unroll
-            for (int x = 0; x < 4; ++x) r[h][x] = value[h * 4 + x] - read[x] * ks[h][x];
-        }
-        bf16x8 right[3];
-        split_rows<3>(r[0], r[1], right);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const f32x4 y = multiply<3, 3>(inverse[h], right, (f32x4){});
-#pragma unroll
-            for (int x = 0; x < 4; ++x) missed[h * 4 + x] = y[x];
-            u[h] = y * beta[h];
-        }
-        bf16x8 written[3];
-        split_rows<3>(u[0] * until[0], u[1] * until[1], written);
-        const float whole = o.weight.whole;
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) S[t] = multiply<n, 3>(turned[t], written, S[t] * whole);
-        split_rows<3>(u[0], u[1], right);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const f32x4 query = *reinterpret_cast<const f32x4 *>(&o.weight.query[r8 + h * 4]);
-            const f32x4 sum = multiply<3, 3>(pull[h], right, query * qs[h]);
-#pragma unroll
-            for (int x = 0; x < 4; ++x) out[h * 4 + x] = sum[x];
-        }
-    });
-    if (span.len && wave < with) store((span.len - 1) / kChunk * kChunk);
+            for (int x = 0; x < 8; ++x) value[x] = held(next[x], span, t0 + r8 + x, in);
+            load_column<T>(values, d.ldv, at, span, t0 + kChunk, r8, next);
+            take_chunk<T, KS>(o, c16, r8, value, S, out, missed);
+        });
+        if (span.len && wave < with) store((span.len - 1) / kChunk * kChunk);
+    }
     if (d.s_last) store_memory<KS>(d.s_last + memory, d.Dk, d.Dv, in, r8, S);
+}
+
+template <class T, int KS>
+void launch_size(const Delta &d, hipStream_t st)
+{
+    constexpr bool kRoom = sizeof(Helped<T, KS, false>) <= 160 * 1024;
+    const Columns c = columns_of(d, kRoom);
+    const uint64_t units = (uint64_t)d.n_seq * d.H * c.groups;
+    for (uint64_t from = 0; from < units; from += kMostLaunched) {
+        const uint32_t grid = (uint32_t)(units - from < kMostLaunched ? units - from : kMostLaunched);
+        if constexpr (kRoom)
+            if (c.helped) {
+                delta_fwd_kernel<T, KS, true><<<grid, c.waves * 64, 0, st>>>(d, c.with, c.groups, from);
+                continue;
+            }
+        delta_fwd_kernel<T, KS, false><<<grid, c.waves * 64, 0, st>>>(d, c.with, c.groups, from);
+    }
 }
 
 template <class T>
 void launch_type(const Delta &d, hipStream_t st)
 {
-    const Columns c = columns_of(d);
-    const uint64_t units = (uint64_t)d.n_seq * d.H * c.groups;
-    for (uint64_t from = 0; from < units; from += kMostLaunched) {
-        const uint32_t grid = (uint32_t)(units - from < kMostLaunched ? units - from : kMostLaunched), threads = c.waves * 64;
-        if (d.Dk <= 32) delta_fwd_kernel<T, 1><<<grid, threads, 0, st>>>(d, c.with, c.groups, from);
-        else if (d.Dk <= 64) delta_fwd_kernel<T, 2><<<grid, threads, 0, st>>>(d, c.with, c.groups, from);
-        else delta_fwd_kernel<T, 4><<<grid, threads, 0, st>>>(d, c.with, c.groups, from);
-    }
+    if (d.Dk <= 32) launch_size<T, 1>(d, st);
+    else if (d.Dk <= 64) launch_size<T, 2>(d, st);
+    else launch_size<T, 4>(d, st);
 }
 
 }  // namespace
