@@ -56,10 +56,10 @@ __device__ __forceinline__ void load8_aligned(const T *row, uint32_t c, uint32_t
 }
 
 // eight values of a row of D from column c on, 0 from D on and without a row
-template <class T>
-__device__ __forceinline__ void eight(const T *row, uint32_t c, uint32_t D, bool in, bool vec, float (&out)[8])
+template <class T, bool kVec>
+__device__ __forceinline__ void eight(const T *row, uint32_t c, uint32_t D, bool in, float (&out)[8])
 {
-    if (vec) {
+    if constexpr (kVec) {
         dg_rows::Pack<T, 8> p;
         load8_aligned<T>(row, c, D, in, p);
 #pragma unroll
@@ -114,13 +114,12 @@ __device__ __forceinline__ void put(const float (&v)[8], uint32_t t, uint32_t co
 }
 
 // K and Q of a chunk on their way to LDS, kEach vectors of each for a lane: a workgroup has wavefronts enough for that
-template <class T, int KS, bool kBackward, int kEach>
+template <class T, int KS, bool kBackward, int kEach, bool kVec>
 struct Rows {
     static constexpr int n = Pieces<T>::n;
     const T *q, *k;
     uint64_t ldq, ldk;
     uint32_t Dk, wave, waves, lane;
-    bool vec;
     Span span;
     dg_rows::Pack<T, 8> qs[kEach], ks[kEach];
 
@@ -130,7 +129,7 @@ struct Rows {
     // a vector where there is one, otherwise another, which store() clears
     __device__ __forceinline__ void fetch(uint32_t c)
     {
-        if (!vec) return;
+        if (!kVec) return;
         constexpr int m = 16 / sizeof(T);
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
@@ -157,7 +156,7 @@ struct Rows {
             if (t >= kChunk) continue;
             float x[8], y[8];
             const bool in = c * kChunk + t < span.len;
-            if (vec) {
+            if constexpr (kVec) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const bool here = in && column() + j < Dk;
@@ -166,8 +165,8 @@ struct Rows {
                 }
             } else {
                 const uint64_t row = span.row(in ? c * kChunk + t : c * kChunk);
-                eight<T>(k + row * ldk, column(), Dk, in, false, x);
-                eight<T>(q + row * ldq, column(), Dk, in, false, y);
+                eight<T, false>(k + row * ldk, column(), Dk, in, x);
+                eight<T, false>(q + row * ldq, column(), Dk, in, y);
             }
             put<n, KS>(x, t, column(), to.K, to.KT);
             if constexpr (kBackward) put<n, KS>(y, t, column(), nullptr, to.Q);
@@ -177,7 +176,7 @@ struct Rows {
 };
 
 // use(operands, chunk) for a sequence's chunks in turn, backward from the last one on
-template <class T, int KS, bool kBackward, class Use>
+template <class T, int KS, bool kBackward, bool kVec, class Use>
 __device__ __forceinline__ void along(const Delta &d, const Span &span, uint32_t seq, uint32_t head, Room<T, KS, kBackward> &room, uint32_t wave, uint32_t waves, Use use)
 {
     constexpr int kBuffers = Room<T, KS, kBackward>::kBuffers;
@@ -185,7 +184,7 @@ __device__ __forceinline__ void along(const Delta &d, const Span &span, uint32_t
     if (chunks == 0) return;
     const uint64_t slot0 = first_chunk(span, seq);
     auto chunk = [&](uint32_t i) { return kBackward ? chunks - 1 - i : i; };
-    Rows<T, KS, kBackward, 2> rows = {(const T *)d.q + hk * d.Dk, (const T *)d.k + hk * d.Dk, d.ldq, d.ldk, d.Dk, wave, waves, threadIdx.x % 64, d.vec_q && d.vec_k, span, {}, {}};
+    Rows<T, KS, kBackward, 2, kVec> rows = {(const T *)d.q + hk * d.Dk, (const T *)d.k + hk * d.Dk, d.ldq, d.ldk, d.Dk, wave, waves, threadIdx.x % 64, span, {}, {}};
     auto weights = [&](uint32_t i) {
         const uint8_t *from = (const uint8_t *)(d.weights + (slot0 + chunk(i)) * d.H + head) + threadIdx.x % 64 * 16;
         uint8_t *to = (uint8_t *)&room.ops[i % kBuffers].weight;
@@ -212,7 +211,7 @@ __device__ __forceinline__ void along(const Delta &d, const Span &span, uint32_t
     }
 }
 
-// The same with wavefronts `with` on bringing and taking away.  use(operands, chunk, tile) for those that have columns; in, out, wide: columns of the workgroup in
+// The same with wavefronts `with` on bringing and taking away, of rows in whole 16 bytes.  use(operands, chunk, tile) for those that have columns; in, out, wide: columns of the workgroup in
 // rows of tokens.  What is brought is fetched two chunks ahead.
 template <class T, int KS, bool kBackward>
 struct Helped {
@@ -229,7 +228,7 @@ struct Helper {
     const Span &span;
     uint64_t slot0;
     uint32_t head, lanes, self, columns, column0;       // lanes that help, this one among them
-    Rows<T, KS, kBackward, 4> rows;
+    Rows<T, KS, kBackward, 4, true> rows;
     u32x4 weights[kWeights];
     dg_rows::Pack<T, 8> in;
 
@@ -251,17 +250,13 @@ struct Helper {
         const T *p = kBackward ? (const T *)d.dout + row_of(c, token()) * d.lddo : (const T *)d.v + row_of(c, token()) * d.ldv;
         const uint32_t first = column0 + column();
         p += head * d.Dv;
-        if (kBackward ? d.vec_o : d.vec_v) {
-            constexpr int m = 16 / sizeof(T);
+        constexpr int m = 16 / sizeof(T);
 #pragma unroll
-            for (int h = 0; h < 8 / m; ++h) {
-                const dg_rows::Pack<T, m> x = *reinterpret_cast<const dg_rows::Pack<T, m> *>(p + (first + h * m < d.Dv ? first + h * m : 0));
+        for (int h = 0; h < 8 / m; ++h) {
+            const dg_rows::Pack<T, m> x = *reinterpret_cast<const dg_rows::Pack<T, m> *>(p + (first + h * m < d.Dv ? first + h * m : 0));
 #pragma unroll
-                for (int j = 0; j < m; ++j) in.v[h * m + j] = x.v[j];
-            }
-        } else
-#pragma unroll
-            for (int j = 0; j < 8; ++j) in.v[j] = p[first + j < d.Dv ? first + j : 0];
+            for (int j = 0; j < m; ++j) in.v[h * m + j] = x.v[j];
+        }
     }
 
     __device__ __forceinline__ void put(uint32_t c, Operands<T, KS, kBackward> &ops, Tiles<T, kBackward> &tile)
@@ -289,28 +284,22 @@ struct Helper {
     }
 
     template <class E, int pitch>
-    __device__ __forceinline__ void take(const E (&tile)[kChunk][pitch], E *p, bool vec) const
+    __device__ __forceinline__ void take(const E (&tile)[kChunk][pitch], E *p) const
     {
         constexpr int m = 16 / sizeof(E);
         const uint32_t first = column0 + column();
 #pragma unroll
-        for (int h = 0; h < 8 / m; ++h) {
-            const dg_rows::Pack<E, m> x = *reinterpret_cast<const dg_rows::Pack<E, m> *>(&tile[token()][column() + h * m]);
-            if (vec && first + h * m < d.Dv) *reinterpret_cast<dg_rows::Pack<E, m> *>(p + first + h * m) = x;
-            else
-#pragma unroll
-                for (int j = 0; j < m; ++j)
-                    if (first + h * m + j < d.Dv) p[first + h * m + j] = x.v[j];
-        }
+        for (int h = 0; h < 8 / m; ++h)
+            if (first + h * m < d.Dv) *reinterpret_cast<dg_rows::Pack<E, m> *>(p + first + h * m) = *reinterpret_cast<const dg_rows::Pack<E, m> *>(&tile[token()][column() + h * m]);
     }
 
     __device__ __forceinline__ void take_away(uint32_t c, const Tiles<T, kBackward> &tile) const
     {
         if (self * 8 >= kChunk * columns || c * kChunk + token() >= span.len) return;
         const uint64_t row = row_of(c, token());
-        if constexpr (!kBackward) take(tile.out, (T *)d.o + row * d.ldo + head * d.Dv, d.vec_o);
+        if constexpr (!kBackward) take(tile.out, (T *)d.o + row * d.ldo + head * d.Dv);
         float *wide = kBackward ? d.dr : d.y;
-        if (wide) take(tile.wide, wide + (row * d.H + head) * d.Dv, d.Dv % 4 == 0);
+        if (wide) take(tile.wide, wide + (row * d.H + head) * d.Dv);
     }
 };
 
@@ -331,7 +320,7 @@ __device__ __forceinline__ void along_helped(const Delta &d, const Span &span, u
     }
     const uint32_t helpers = waves - with;
     Helper<T, KS, kBackward> h = {d, span, first_chunk(span, seq), head, helpers * 64, threadIdx.x - with * 64, with * 16, column0,
-                                  {(const T *)d.q + hk * d.Dk, (const T *)d.k + hk * d.Dk, d.ldq, d.ldk, d.Dk, wave - with, helpers, threadIdx.x % 64, d.vec_q && d.vec_k, span, {}, {}}, {}, {}};
+                                  {(const T *)d.q + hk * d.Dk, (const T *)d.k + hk * d.Dk, d.ldq, d.ldk, d.Dk, wave - with, helpers, threadIdx.x % 64, span, {}, {}}, {}, {}};
     h.fetch(chunk(0));
     h.put(chunk(0), room.ops[0], room.tiles[0]);
     if (chunks > 1) h.fetch(chunk(1));

@@ -50,7 +50,9 @@ struct Delta {
     uint64_t N;
     uint32_t n_seq, Hk, H, Dk, Dv, reverse, slots;
     float scale;
-    uint32_t vec_q, vec_k, vec_v, vec_o, vec_dv, vec_dqk;       // whether a head's rows lie in whole 16 bytes
+    // Whether heads' rows lie in whole 16 bytes: q and k; q, k, v and o or its gradient, and with them rows of fp32 values; dv, dq and dk too.  Kernels take it as a template
+    // argument: of a branch between loads of 16 bytes and single ones the compiler makes single ones for both.
+    bool vec_keys, vec_all, vec_out;
 };
 
 template <class T>
@@ -140,24 +142,6 @@ __device__ __forceinline__ f32x4 multiply(const bf16x8 (&a)[na], const bf16x8 (&
 }
 
 // ------------------------------------------------------------------------------ memory
-// eight values of a row of D from column c on, 0 from D on (and without a row)
-template <class T>
-__device__ __forceinline__ void load8(const T *row, uint32_t c, uint32_t D, bool vec, float (&out)[8])
-{
-    if (row && vec && c + 8 <= D) {
-#pragma unroll
-        for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
-            constexpr int n = 16 / sizeof(T);
-            const dg_rows::Pack<T, n> p = *reinterpret_cast<const dg_rows::Pack<T, n> *>(row + c + h * n);
-#pragma unroll
-            for (int i = 0; i < n; ++i) out[h * n + i] = (float)p.v[i];
-        }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) out[i] = row && c + i < D ? (float)row[c + i] : 0.0f;
-}
-
 __device__ __forceinline__ void wave_fence()
 {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

@@ -77,7 +77,7 @@ struct Lds { using type = Room<T, KS, false>; };
 template <class T, int KS>
 struct Lds<T, KS, true> { using type = Helped<T, KS, false>; };
 
-template <class T, int KS, bool kHelped>
+template <class T, int KS, bool kHelped, bool kVec>
 __global__ void __launch_bounds__(kMostWaves * 64)
 delta_fwd_kernel(Delta d, uint32_t with, uint32_t groups, uint64_t from)
 {
@@ -118,7 +118,7 @@ delta_fwd_kernel(Delta d, uint32_t with, uint32_t groups, uint64_t from)
             if (d.y) store_column<float>(d.y + head * d.Dv, (uint64_t)d.H * d.Dv, at, span, t0, r8, in, missed);
         };
         load_column<T>(values, d.ldv, at, span, 0, r8, next);
-        along<T, KS, false>(d, span, seq, head, room, wave, waves, [&](const Operands<T, KS, false> &o, uint32_t c) {
+        along<T, KS, false, kVec>(d, span, seq, head, room, wave, waves, [&](const Operands<T, KS, false> &o, uint32_t c) {
             if (wave >= with) return;
             const uint32_t t0 = c * kChunk;
             mark(c);
@@ -137,16 +137,17 @@ template <class T, int KS>
 void launch_size(const Delta &d, hipStream_t st)
 {
     constexpr bool kRoom = sizeof(Helped<T, KS, false>) <= 160 * 1024;
-    const Columns c = columns_of(d, kRoom);
+    const Columns c = columns_of(d, kRoom && d.vec_all);
     const uint64_t units = (uint64_t)d.n_seq * d.H * c.groups;
     for (uint64_t from = 0; from < units; from += kMostLaunched) {
         const uint32_t grid = (uint32_t)(units - from < kMostLaunched ? units - from : kMostLaunched);
         if constexpr (kRoom)
             if (c.helped) {
-                delta_fwd_kernel<T, KS, true><<<grid, c.waves * 64, 0, st>>>(d, c.with, c.groups, from);
+                delta_fwd_kernel<T, KS, true, true><<<grid, c.waves * 64, 0, st>>>(d, c.with, c.groups, from);
                 continue;
             }
-        delta_fwd_kernel<T, KS, false><<<grid, c.waves * 64, 0, st>>>(d, c.with, c.groups, from);
+        if (d.vec_keys) delta_fwd_kernel<T, KS, false, true><<<grid, c.waves * 64, 0, st>>>(d, c.with, c.groups, from);
+        else delta_fwd_kernel<T, KS, false, false><<<grid, c.waves * 64, 0, st>>>(d, c.with, c.groups, from);
     }
 }
 

@@ -40,11 +40,11 @@ __device__ __forceinline__ float of_token(float v)
 }
 
 // Eight values of a row from column c on, or others where there are none: `cleared` tells them apart when they are used, so that nothing waits for the load
-template <class T>
-__device__ __forceinline__ void ahead(const T *row, uint32_t c, uint32_t D, bool vec, dg_rows::Pack<T, 8> &out)
+template <class T, bool kVec>
+__device__ __forceinline__ void ahead(const T *row, uint32_t c, uint32_t D, dg_rows::Pack<T, 8> &out)
 {
     constexpr int m = 16 / sizeof(T);
-    if (vec) {
+    if constexpr (kVec) {
 #pragma unroll
         for (int h = 0; h < 8 / m; ++h) {
             const dg_rows::Pack<T, m> p = *reinterpret_cast<const dg_rows::Pack<T, m> *>(row + (c + h * m < D ? c + h * m : 0));
@@ -72,7 +72,7 @@ __device__ __forceinline__ void put8(const float (&v)[8], uint16_t (&to)[n][rows
     for (int p = 0; p < n; ++p) *reinterpret_cast<u32x4 *>(&to[p][row][col]) = (u32x4){w[p][0], w[p][1], w[p][2], w[p][3]};
 }
 
-template <class T, int KS>
+template <class T, int KS, bool kVec>
 __global__ void __launch_bounds__(256, 1)
 delta_grad_kernel(Delta d, uint64_t from)
 {
@@ -104,7 +104,6 @@ delta_grad_kernel(Delta d, uint64_t from)
     const uint32_t brought = threadIdx.x / 4, c8 = threadIdx.x % 4 * 8;         // the token, or row of the memory, of which a thread brings eight columns
     const bool there = brought < count;
     const uint64_t brought_row = row_of(brought);
-    const bool vec_f = d.Dv % 4 == 0;
     f32x4 dq[kTiles] = {}, dk[kTiles] = {};
 
     for (uint32_t h = 0; h < group; ++h) {
@@ -117,13 +116,13 @@ delta_grad_kernel(Delta d, uint64_t from)
 #pragma unroll
             for (int i = 0; i < kMemoryRows; ++i) {
                 const uint64_t r = brought + i * 64 < d.Dk ? brought + i * 64 : 0;
-                ahead<float>(S + r * d.Dv, c, d.Dv, vec_f, next_s[i]);
-                ahead<float>(dS + r * d.Dv, c, d.Dv, vec_f, next_ds[i]);
+                ahead<float, kVec>(S + r * d.Dv, c, d.Dv, next_s[i]);
+                ahead<float, kVec>(dS + r * d.Dv, c, d.Dv, next_ds[i]);
             }
-            ahead<float>(d.y + at, c, d.Dv, vec_f, next_y);
-            ahead<float>(d.dr + at, c, d.Dv, vec_f, next_r);
-            ahead<T>((const T *)d.dout + brought_row * d.lddo + head * d.Dv, c, d.Dv, d.vec_o, next_o);
-            ahead<T>((const T *)d.v + brought_row * d.ldv + head * d.Dv, c, d.Dv, d.vec_v, next_v);
+            ahead<float, kVec>(d.y + at, c, d.Dv, next_y);
+            ahead<float, kVec>(d.dr + at, c, d.Dv, next_r);
+            ahead<T, kVec>((const T *)d.dout + brought_row * d.lddo + head * d.Dv, c, d.Dv, next_o);
+            ahead<T, kVec>((const T *)d.v + brought_row * d.ldv + head * d.Dv, c, d.Dv, next_v);
         };
         fetch(c8);
         const float beta_brought = there ? d.beta[brought_row * d.ldb + head] : 0.0f;
@@ -165,7 +164,6 @@ delta_grad_kernel(Delta d, uint64_t from)
                 cleared<float>(next_y, c, d.Dv, there, y);
                 cleared<T>(next_v, c, d.Dv, there, x);
                 T *dv = (T *)d.dv + brought_row * d.lddv + head * d.Dv + c;
-                const bool vectors = d.vec_dv && c + 8 <= d.Dv && there;
                 float out[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -173,16 +171,16 @@ delta_grad_kernel(Delta d, uint64_t from)
                     y[j] *= beta_brought;
                     out[j] = beta_brought * r[j];
                     values = fmaf(out[j], x[j], values);
-                    if (!vectors && there && c + j < d.Dv) dv[j] = (T)out[j];
+                    if (!kVec && there && c + j < d.Dv) dv[j] = (T)out[j];
                 }
-                if (vectors) {
+                if (kVec && there) {
                     constexpr int m = 16 / sizeof(T);
 #pragma unroll
                     for (int j = 0; j < 8; j += m) {
                         float part[m];
 #pragma unroll
                         for (int i = 0; i < m; ++i) part[i] = out[j + i];
-                        dg_rows::store<T, m>(dv + j, part);
+                        if (c + j < d.Dv) dg_rows::store<T, m>(dv + j, part);
                     }
                 }
                 put8(y, lds.U, brought, c8);
@@ -241,8 +239,8 @@ delta_grad_kernel(Delta d, uint64_t from)
         for (uint32_t item = threadIdx.x; item < kTokens * 4 * KS; item += 256) {
             const uint32_t t = item / (4 * KS), col = item % (4 * KS) * 8;
             dg_rows::Pack<T, 8> k8, q8;
-            ahead<T>(K + row_of(t) * d.ldk, col, d.Dk, d.vec_k, k8);
-            ahead<T>(Q + row_of(t) * d.ldq, col, d.Dk, d.vec_q, q8);
+            ahead<T, kVec>(K + row_of(t) * d.ldk, col, d.Dk, k8);
+            ahead<T, kVec>(Q + row_of(t) * d.ldq, col, d.Dk, q8);
             float v[8];
             uint32_t w[n][4];
             cleared<T>(k8, col, d.Dk, t < count, v);
@@ -351,7 +349,8 @@ delta_grad_kernel(Delta d, uint64_t from)
     for (int t = 0; t < kTiles; ++t) {
         const uint32_t c = t * 16 + r4;
         T *to_q = (T *)d.dq + row * d.lddq + hk * d.Dk + c, *to_k = (T *)d.dk + row * d.lddk + hk * d.Dk + c;
-        if (d.vec_dqk && c + 4 <= d.Dk) {
+        if constexpr (kVec) {
+            if (c >= d.Dk) continue;
             const float a[4] = {dq[t][0], dq[t][1], dq[t][2], dq[t][3]}, b[4] = {dk[t][0], dk[t][1], dk[t][2], dk[t][3]};
             dg_rows::store<T, 4>(to_q, a);
             dg_rows::store<T, 4>(to_k, b);
@@ -382,16 +381,23 @@ delta_slots_kernel(Delta d, uint32_t *slot_seq)
     slot_seq[slot] = begin <= slot && (uint64_t)(slot - begin) * kTokens < span.len ? low : ~0u;
 }
 
-template <class T>
-void launch_type(const Delta &d, hipStream_t st)
+template <class T, int KS>
+void launch_size(const Delta &d, hipStream_t st)
 {
     const uint64_t slots = d.first ? d.slots : d.n_seq * ((d.N / d.n_seq + kTokens - 1) / kTokens), units = slots * d.Hk;
     for (uint64_t from = 0; from < units; from += kMostLaunched) {
         const uint32_t grid = (uint32_t)(units - from < kMostLaunched ? units - from : kMostLaunched);
-        if (d.Dk <= 32) delta_grad_kernel<T, 1><<<grid, 256, 0, st>>>(d, from);
-        else if (d.Dk <= 64) delta_grad_kernel<T, 2><<<grid, 256, 0, st>>>(d, from);
-        else delta_grad_kernel<T, 4><<<grid, 256, 0, st>>>(d, from);
+        if (d.vec_all && d.vec_out) delta_grad_kernel<T, KS, true><<<grid, 256, 0, st>>>(d, from);
+        else delta_grad_kernel<T, KS, false><<<grid, 256, 0, st>>>(d, from);
     }
+}
+
+template <class T>
+void launch_type(const Delta &d, hipStream_t st)
+{
+    if (d.Dk <= 32) launch_size<T, 1>(d, st);
+    else if (d.Dk <= 64) launch_size<T, 2>(d, st);
+    else launch_size<T, 4>(d, st);
 }
 
 }  // namespace

@@ -12,13 +12,13 @@ namespace {
 using namespace dg_delta;
 
 // P values of a row of D that all lanes of a head read; D is P if kFull
-template <class T, int P, bool kFull>
+template <class T, int P, bool kFull, bool kVec>
 struct Vector {
     T v[P];
-    __device__ __forceinline__ void load(const T *row, uint32_t D, bool vec)
+    __device__ __forceinline__ void load(const T *row, uint32_t D)
     {
         constexpr int m = 16 / sizeof(T);
-        if (vec) {
+        if constexpr (kVec) {
 #pragma unroll
             for (int i = 0; i < P; i += m) {
                 const dg_rows::Pack<T, m> p = *reinterpret_cast<const dg_rows::Pack<T, m> *>(row + (kFull || i < (int)D ? i : 0));
@@ -34,8 +34,8 @@ struct Vector {
 };
 
 // sum of products, in four parts
-template <class T, int P, bool kFull>
-__device__ __forceinline__ float dot(const float (&a)[P], const Vector<T, P, kFull> &b, uint32_t D)
+template <class T, int P, bool kFull, bool kVec>
+__device__ __forceinline__ float dot(const float (&a)[P], const Vector<T, P, kFull, kVec> &b, uint32_t D)
 {
     float part[4] = {};
 #pragma unroll
@@ -44,16 +44,16 @@ __device__ __forceinline__ float dot(const float (&a)[P], const Vector<T, P, kFu
 }
 
 // a <- a f + b s
-template <class T, int P, bool kFull>
-__device__ __forceinline__ void step(float (&a)[P], float f, const Vector<T, P, kFull> &b, float s, uint32_t D)
+template <class T, int P, bool kFull, bool kVec>
+__device__ __forceinline__ void step(float (&a)[P], float f, const Vector<T, P, kFull, kVec> &b, float s, uint32_t D)
 {
 #pragma unroll
     for (int i = 0; i < P; ++i) a[i] = fmaf(b.at(i, D), s, a[i] * f);
 }
 
 // a <- a + b s
-template <class T, int P, bool kFull>
-__device__ __forceinline__ void add(float (&a)[P], const Vector<T, P, kFull> &b, float s, uint32_t D)
+template <class T, int P, bool kFull, bool kVec>
+__device__ __forceinline__ void add(float (&a)[P], const Vector<T, P, kFull, kVec> &b, float s, uint32_t D)
 {
 #pragma unroll
     for (int i = 0; i < P; ++i) a[i] = fmaf(b.at(i, D), s, a[i]);
@@ -81,7 +81,7 @@ struct Place {
     }
 };
 
-template <class T, int PK, int PV, bool kFull>
+template <class T, int PK, int PV, bool kFull, bool kVec>
 __global__ void __launch_bounds__(64)
 delta_small_fwd_kernel(Delta d, uint64_t from)
 {
@@ -100,9 +100,9 @@ delta_small_fwd_kernel(Delta d, uint64_t from)
         Walk<T> O((T *)d.o + at.head * d.Dv + c, d.ldo, span, 0, false);
         Walk<float> Y(d.y + at.head * d.Dv + c, ldy, span, 0, false);
         float *mark = d.marks + ((uint64_t)first_slot(span, at.seq) * d.H + at.head) * d.Dk * d.Dv + c;
-        Vector<T, PK, kFull> k, q, next_k, next_q;
-        next_k.load(K.p, d.Dk, d.vec_k);
-        next_q.load(Q.p, d.Dk, d.vec_q);
+        Vector<T, PK, kFull, kVec> k, q, next_k, next_q;
+        next_k.load(K.p, d.Dk);
+        next_q.load(Q.p, d.Dk);
         T next_v = *V.p;
         float next_g = *G.p, next_beta = *B.p;
         for (uint32_t t = 0; t < len; ++t) {
@@ -111,8 +111,8 @@ delta_small_fwd_kernel(Delta d, uint64_t from)
             const float a = expf(next_g), beta = next_beta;
             if (t + 1 < len) {
                 K.next(), Q.next(), V.next(), G.next(), B.next();
-                next_k.load(K.p, d.Dk, d.vec_k);
-                next_q.load(Q.p, d.Dk, d.vec_q);
+                next_k.load(K.p, d.Dk);
+                next_q.load(Q.p, d.Dk);
                 next_v = *V.p, next_g = *G.p, next_beta = *B.p;
             }
             if (d.marks && t % kMark == 0) {
@@ -139,7 +139,7 @@ delta_small_fwd_kernel(Delta d, uint64_t from)
 }
 
 // dS of a token: + scale q do^T;  dR = dS^T k;  - k (beta dR)^T;  e^g dS goes to the token before.  dg gets v dv, for what follows.
-template <class T, int PK, int PV, bool kFull>
+template <class T, int PK, int PV, bool kFull, bool kVec>
 __global__ void __launch_bounds__(64)
 delta_small_bwd_kernel(Delta d, uint64_t from)
 {
@@ -159,9 +159,9 @@ delta_small_bwd_kernel(Delta d, uint64_t from)
         Walk<T> dV((T *)d.dv + at.head * d.Dv + c, d.lddv, span, last, true);
         Walk<float> R(d.dr + at.head * d.Dv + c, ldy, span, last, true), dB(d.dbeta + at.head, d.lddb, span, last, true), dG(d.dg + at.head, d.lddg, span, last, true);
         float *mark = d.dmarks + ((uint64_t)(first_slot(span, at.seq) + last / kMark) * d.H + at.head) * d.Dk * d.Dv + c;
-        Vector<T, PK, kFull> k, q, next_k, next_q;
-        next_k.load(K.p, d.Dk, d.vec_k);
-        next_q.load(Q.p, d.Dk, d.vec_q);
+        Vector<T, PK, kFull, kVec> k, q, next_k, next_q;
+        next_k.load(K.p, d.Dk);
+        next_q.load(Q.p, d.Dk);
         T next_v = *V.p, next_o = *O.p;
         float next_g = *G.p, next_beta = *B.p, next_y = *Y.p;
         for (uint32_t t = last;; --t) {
@@ -170,8 +170,8 @@ delta_small_bwd_kernel(Delta d, uint64_t from)
             const float a = expf(next_g), beta = next_beta, y = next_y;
             if (t) {
                 K.next(), Q.next(), V.next(), O.next(), G.next(), B.next(), Y.next();
-                next_k.load(K.p, d.Dk, d.vec_k);
-                next_q.load(Q.p, d.Dk, d.vec_q);
+                next_k.load(K.p, d.Dk);
+                next_q.load(Q.p, d.Dk);
                 next_v = *V.p, next_o = *O.p, next_g = *G.p, next_beta = *B.p, next_y = *Y.p;
             }
             if (t % kMark == kMark - 1 || t == last) {
@@ -205,7 +205,7 @@ delta_small_bwd_kernel(Delta d, uint64_t from)
 }
 
 // Rows: 64 tokens of a key head, one of its value heads after the other
-template <class T, int PK, int PV, bool kShared, bool kFull>
+template <class T, int PK, int PV, bool kShared, bool kFull, bool kVec>
 __global__ void __launch_bounds__(64)
 delta_small_grad_kernel(Delta d, uint64_t from)
 {
@@ -234,13 +234,12 @@ delta_small_grad_kernel(Delta d, uint64_t from)
     const uint32_t count = !there ? 0 : span.len - t0 < kMark ? span.len - t0 : kMark;
     const bool in = there && lane % PK < d.Dk;
     if (!there) return;
-    const bool vec_f = d.Dv % 4 == 0;
     const uint32_t last = t0 + count - 1, ldy = d.H * d.Dv;
     for (uint32_t h = 0; h < group; ++h) {
         const uint32_t head = hk * group + h;
         const uint64_t memory = ((slot * d.H + head) * d.Dk + r) * d.Dv;
-        Vector<float, PV, kFull> w, next_y, next_r, y, dr;
-        Vector<T, PV, kFull> next_o, o;
+        Vector<float, PV, kFull, kVec> w, next_y, next_r, y, dr;
+        Vector<T, PV, kFull, kVec> next_o, o;
         T next_k, next_q;
         float next_g, next_beta, S[PV], end = 0.0f;
         struct Rows {
@@ -252,15 +251,15 @@ delta_small_grad_kernel(Delta d, uint64_t from)
             __device__ __forceinline__ void next() { Y.next(), R.next(), G.next(), B.next(), O.next(), K.next(), Q.next(); }
         };
         auto fetch = [&](const Rows &at) {
-            next_y.load(at.Y.p, d.Dv, vec_f);
-            next_r.load(at.R.p, d.Dv, vec_f);
-            next_o.load(at.O.p, d.Dv, d.vec_o);
+            next_y.load(at.Y.p, d.Dv);
+            next_r.load(at.R.p, d.Dv);
+            next_o.load(at.O.p, d.Dv);
             next_k = *at.K.p, next_q = *at.Q.p, next_g = *at.G.p, next_beta = *at.B.p;
         };
         {
             Rows at(d, span, t0, false, head, hk * d.Dk + r, ldy);
             Walk<T> dQ((T *)d.dq + hk * d.Dk + r, d.lddq, span, t0, false);
-            w.load(d.marks + memory, d.Dv, vec_f);
+            w.load(d.marks + memory, d.Dv);
             fetch(at);
 #pragma unroll
             for (int i = 0; i < PV; ++i) S[i] = in ? w.at(i, d.Dv) : 0.0f;
@@ -285,7 +284,7 @@ delta_small_grad_kernel(Delta d, uint64_t from)
         Rows at(d, span, last, true, head, hk * d.Dk + r, ldy);
         Walk<T> dK((T *)d.dk + hk * d.Dk + r, d.lddk, span, last, true);
         Walk<float> dG(d.dg + head, d.lddg, span, last, true);
-        w.load(d.dmarks + memory, d.Dv, vec_f);
+        w.load(d.dmarks + memory, d.Dv);
         fetch(at);
         float dS[PV];
 #pragma unroll
@@ -323,25 +322,26 @@ void in_turns(uint64_t all, Go go)
     for (uint64_t from = 0; from < all; from += kMostLaunched) go((uint32_t)(all - from < kMostLaunched ? all - from : kMostLaunched), from);
 }
 
-template <class T, int PK, int PV, bool kFull>
+template <class T, int PK, int PV, bool kFull, bool kVec>
 void launch_size(const Delta &d, bool back, hipStream_t st)
 {
     const uint64_t along = ((uint64_t)d.n_seq * d.H + 64 / PV - 1) / (64 / PV);
-    if (!back) return in_turns(along, [&](uint32_t grid, uint64_t from) { delta_small_fwd_kernel<T, PK, PV, kFull><<<grid, 64, 0, st>>>(d, from); });
-    in_turns(along, [&](uint32_t grid, uint64_t from) { delta_small_bwd_kernel<T, PK, PV, kFull><<<grid, 64, 0, st>>>(d, from); });
+    if (!back) return in_turns(along, [&](uint32_t grid, uint64_t from) { delta_small_fwd_kernel<T, PK, PV, kFull, kVec><<<grid, 64, 0, st>>>(d, from); });
+    in_turns(along, [&](uint32_t grid, uint64_t from) { delta_small_bwd_kernel<T, PK, PV, kFull, kVec><<<grid, 64, 0, st>>>(d, from); });
     if (d.N == 0) return;
     const uint64_t slots = d.first ? d.slots : (uint64_t)d.n_seq * ((d.N / d.n_seq + kMark - 1) / kMark);
     in_turns((slots * d.Hk + 64 / PK - 1) / (64 / PK), [&](uint32_t grid, uint64_t from) {
-        if (d.H == d.Hk) delta_small_grad_kernel<T, PK, PV, false, kFull><<<grid, 64, 0, st>>>(d, from);
-        else delta_small_grad_kernel<T, PK, PV, true, kFull><<<grid, 64, 0, st>>>(d, from);
+        if (d.H == d.Hk) delta_small_grad_kernel<T, PK, PV, false, kFull, kVec><<<grid, 64, 0, st>>>(d, from);
+        else delta_small_grad_kernel<T, PK, PV, true, kFull, kVec><<<grid, 64, 0, st>>>(d, from);
     });
 }
 
 template <class T, int PK, int PV>
 void launch_padded(const Delta &d, bool back, hipStream_t st)
 {
-    if (d.Dk == PK && d.Dv == PV) launch_size<T, PK, PV, true>(d, back, st);
-    else launch_size<T, PK, PV, false>(d, back, st);
+    if (d.Dk == PK && d.Dv == PV && d.vec_all) launch_size<T, PK, PV, true, true>(d, back, st);
+    else if (d.vec_all) launch_size<T, PK, PV, false, true>(d, back, st);
+    else launch_size<T, PK, PV, false, false>(d, back, st);
 }
 
 template <class T>

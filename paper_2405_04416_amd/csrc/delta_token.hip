@@ -2,7 +2,7 @@
 //
 // Bound by memory: the memories go in and out once, 8 Dk Dv bytes per head and sequence.  A wavefront has 32 columns of a memory in registers, lane
 // (r, c) rows 16 r to 16 r + 15 of columns 4 c to 4 c + 3; S^T k and S^T q are summed over r at once, as S'^T q = e^g S^T q + (k q) u.
-#include "delta_common.h"
+#include "delta_chunk.h"
 
 namespace {
 
@@ -17,24 +17,23 @@ __device__ __forceinline__ float over_rows(float v)
     return v + __shfl_xor(v, 32);
 }
 
-template <class T>
-__device__ __forceinline__ void load_rows(const T *p, uint32_t from, uint32_t D, bool vec, float (&out)[kRows])
+template <class T, bool kVec>
+__device__ __forceinline__ void load_rows(const T *p, uint32_t from, uint32_t D, float (&out)[kRows])
 {
     float half[8];
 #pragma unroll
     for (int h = 0; h < kRows / 8; ++h) {
-        load8<T>(p, from + h * 8, D, vec, half);
+        eight<T, kVec>(p, from + h * 8, D, true, half);
 #pragma unroll
         for (int i = 0; i < 8; ++i) out[h * 8 + i] = half[i];
     }
 }
 
-template <class T>
+template <class T, bool kVec>
 __global__ void __launch_bounds__(256)
 delta_token_kernel(Delta d, uint32_t groups, uint64_t units)
 {
     const uint32_t lane = threadIdx.x % 64, r = lane / 8 * kRows;
-    const bool wide = d.Dv % 4 == 0 && reinterpret_cast<uintptr_t>(d.s0) % 16 == 0 && reinterpret_cast<uintptr_t>(d.s_last) % 16 == 0;
     for (uint64_t unit = (uint64_t)blockIdx.x * 4 + threadIdx.x / 64; unit < units; unit += (uint64_t)gridDim.x * 4) {
         const uint32_t c = (uint32_t)(unit % groups) * 32 + lane % 8 * 4, head = (uint32_t)(unit / groups % d.H), seq = (uint32_t)(unit / groups / d.H);
         const uint32_t hk = head / (d.H / d.Hk);
@@ -45,8 +44,9 @@ delta_token_kernel(Delta d, uint32_t groups, uint64_t units)
         for (int i = 0; i < kRows; ++i) {
             const float *row = d.s0 + memory + (uint64_t)(r + i) * d.Dv + c;
             const bool in = d.s0 && r + i < d.Dk;
-            if (in && wide && c < d.Dv) {
-                const f32x4 v = *reinterpret_cast<const f32x4 *>(row);
+            if constexpr (kVec) {
+                f32x4 v = {};
+                if (in && c < d.Dv) v = *reinterpret_cast<const f32x4 *>(row);
 #pragma unroll
                 for (int x = 0; x < 4; ++x) S[i][x] = v[x];
             } else
@@ -56,8 +56,8 @@ delta_token_kernel(Delta d, uint32_t groups, uint64_t units)
         for (uint32_t t = 0; t < span.len; ++t) {
             const uint64_t row = span.row(t);
             float k[kRows], q[kRows];
-            load_rows<T>((const T *)d.k + row * d.ldk + hk * d.Dk, r, d.Dk, d.vec_k, k);
-            load_rows<T>((const T *)d.q + row * d.ldq + hk * d.Dk, r, d.Dk, d.vec_q, q);
+            load_rows<T, kVec>((const T *)d.k + row * d.ldk + hk * d.Dk, r, d.Dk, k);
+            load_rows<T, kVec>((const T *)d.q + row * d.ldq + hk * d.Dk, r, d.Dk, q);
             const float a = expf(d.g[row * d.ldg + head]), beta = d.beta[row * d.ldb + head];
             float sk[4] = {}, sq[4] = {}, kq = 0.0f;
 #pragma unroll
@@ -86,8 +86,9 @@ delta_token_kernel(Delta d, uint32_t groups, uint64_t units)
         for (int i = 0; i < kRows; ++i) {
             float *row = d.s_last + memory + (uint64_t)(r + i) * d.Dv + c;
             if (r + i >= d.Dk) continue;
-            if (wide && c < d.Dv) *reinterpret_cast<f32x4 *>(row) = (f32x4){S[i][0], S[i][1], S[i][2], S[i][3]};
-            else
+            if constexpr (kVec) {
+                if (c < d.Dv) *reinterpret_cast<f32x4 *>(row) = (f32x4){S[i][0], S[i][1], S[i][2], S[i][3]};
+            } else
 #pragma unroll
                 for (int x = 0; x < 4; ++x)
                     if (c + x < d.Dv) row[x] = S[i][x];
@@ -95,14 +96,21 @@ delta_token_kernel(Delta d, uint32_t groups, uint64_t units)
     }
 }
 
-}  // namespace
-
-void dg_delta::launch_tokens(const Delta &d, uint32_t dtype, hipStream_t st)
+template <class T>
+void launch_type(const Delta &d, hipStream_t st)
 {
     const uint32_t groups = (d.Dv + 31) / 32;
     const uint64_t units = (uint64_t)d.n_seq * d.H * groups, all = (units + 3) / 4;
     const uint32_t grid = (uint32_t)(all < 1u << 20 ? all : 1u << 20);
-    if (dtype == DG_F32) delta_token_kernel<float><<<grid, 256, 0, st>>>(d, groups, units);
-    else if (dtype == DG_F16) delta_token_kernel<f16><<<grid, 256, 0, st>>>(d, groups, units);
-    else delta_token_kernel<bf16><<<grid, 256, 0, st>>>(d, groups, units);
+    if (d.vec_all && dg::aligned(d.s0, 16) && dg::aligned(d.s_last, 16)) delta_token_kernel<T, true><<<grid, 256, 0, st>>>(d, groups, units);
+    else delta_token_kernel<T, false><<<grid, 256, 0, st>>>(d, groups, units);
+}
+
+}  // namespace
+
+void dg_delta::launch_tokens(const Delta &d, uint32_t dtype, hipStream_t st)
+{
+    if (dtype == DG_F32) launch_type<float>(d, st);
+    else if (dtype == DG_F16) launch_type<f16>(d, st);
+    else launch_type<bf16>(d, st);
 }

@@ -24,25 +24,25 @@ struct Shared {
 };
 
 // 16 rows of K or Q as an operand, in pieces
-template <class T, int KS>
+template <class T, int KS, bool kVec>
 struct Block {
     static constexpr int n = Pieces<T>::n;
     bf16x8 v[KS][n];
-    __device__ __forceinline__ Block(const T *p, uint64_t ld, const Span &span, uint32_t t0, uint32_t t, uint32_t c8, uint32_t D, bool vec)
+    __device__ __forceinline__ Block(const T *p, uint64_t ld, const Span &span, uint32_t t0, uint32_t t, uint32_t c8, uint32_t D)
     {
         const bool in = t0 + t < span.len;
         const T *row = p + span.row(in ? t0 + t : t0) * ld;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             float x[8];
-            eight<T>(row, s * 32 + c8, D, in, vec, x);
+            eight<T, kVec>(row, s * 32 + c8, D, in, x);
             split8<n>(x, v[s]);
         }
     }
 };
 
-template <class T, int KS>
-__device__ __forceinline__ f32x4 product(const Block<T, KS> &a, const Block<T, KS> &b)
+template <class T, int KS, bool kVec>
+__device__ __forceinline__ f32x4 product(const Block<T, KS, kVec> &a, const Block<T, KS, kVec> &b)
 {
     f32x4 acc = {};
 #pragma unroll
@@ -50,7 +50,7 @@ __device__ __forceinline__ f32x4 product(const Block<T, KS> &a, const Block<T, K
     return acc;
 }
 
-template <class T, int KS, bool kBackward>
+template <class T, int KS, bool kBackward, bool kVec>
 __global__ void __launch_bounds__(128)
 delta_weights_kernel(Delta d, uint64_t from)
 {
@@ -80,7 +80,7 @@ delta_weights_kernel(Delta d, uint64_t from)
     const uint64_t row = span.row(held ? t0 + mine : t0);
     const float gate = d.g[row * d.ldg + head], rate = d.beta[row * d.ldb + head];
     const T *keys = (const T *)d.k + hk * d.Dk, *queries = (const T *)d.q + hk * d.Dk;
-    const Block<T, KS> k0(keys, d.ldk, span, t0, c16, r4 * 2, d.Dk, d.vec_k), k1(keys, d.ldk, span, t0, 16 + c16, r4 * 2, d.Dk, d.vec_k);
+    const Block<T, KS, kVec> k0(keys, d.ldk, span, t0, c16, r4 * 2, d.Dk), k1(keys, d.ldk, span, t0, 16 + c16, r4 * 2, d.Dk);
     const float beta = held ? rate : 0.0f;
     double sum = held ? (double)fmaxf(gate, kShut) : 0.0;
 #pragma unroll
@@ -106,11 +106,11 @@ delta_weights_kernel(Delta d, uint64_t from)
     const float none[4] = {};
     if (wave == 1) {
         // P; forward rows i, backward rows j
-        const Block<T, KS> q0(queries, d.ldq, span, t0, c16, r4 * 2, d.Dk, d.vec_q), q1(queries, d.ldq, span, t0, 16 + c16, r4 * 2, d.Dk, d.vec_q);
+        const Block<T, KS, kVec> q0(queries, d.ldq, span, t0, c16, r4 * 2, d.Dk), q1(queries, d.ldq, span, t0, 16 + c16, r4 * 2, d.Dk);
 #pragma unroll
         for (int b = 0; b < 3; ++b) {           // blocks (tokens i, tokens j): (0, 0), (1, 0), (1, 1)
             const uint32_t bi = b ? 16 : 0, bj = b == 2 ? 16 : 0;
-            const Block<T, KS> &q = b ? q1 : q0, &k = b == 2 ? k1 : k0;
+            const Block<T, KS, kVec> &q = b ? q1 : q0, &k = b == 2 ? k1 : k0;
             const f32x4 acc = kBackward ? product(q, k) : product(k, q);
             float v[4];
 #pragma unroll
@@ -200,7 +200,8 @@ void launch_size(const Delta &d, hipStream_t st)
     const uint64_t slots = d.first ? chunk_slots(d.N, d.n_seq) : d.n_seq * ((d.N / d.n_seq + kChunk - 1) / kChunk), units = slots * d.H;
     for (uint64_t from = 0; from < units; from += kMostLaunched) {
         const uint32_t grid = (uint32_t)(units - from < kMostLaunched ? units - from : kMostLaunched);
-        delta_weights_kernel<T, KS, kBackward><<<grid, 128, 0, st>>>(d, from);
+        if (d.vec_keys) delta_weights_kernel<T, KS, kBackward, true><<<grid, 128, 0, st>>>(d, from);
+        else delta_weights_kernel<T, KS, kBackward, false><<<grid, 128, 0, st>>>(d, from);
     }
 }
 
