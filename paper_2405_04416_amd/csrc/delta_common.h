@@ -142,6 +142,14 @@ __device__ __forceinline__ f32x4 multiply(const bf16x8 (&a)[na], const bf16x8 (&
 }
 
 // ------------------------------------------------------------------------------ memory
+// The same number, of which the compiler does not know that it is: what follows from it is computed where it is needed, in place of being kept in registers (and
+// beyond them in memory) all along a loop.
+__device__ __forceinline__ uint32_t again(uint32_t x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 __device__ __forceinline__ void wave_fence()
 {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

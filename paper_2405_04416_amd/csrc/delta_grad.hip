@@ -5,32 +5,51 @@
 // behind, e^G[last] S + K^T e^(G[last] - G) U, with dS';  dg[t] = sum of dG from t on.
 //
 // A workgroup takes 64 tokens of a key head, one value head after the other, 32 columns of values at a time through LDS (in pieces, cut once for all), a wavefront
-// 16 tokens: a lane has a token, of which everything above is a column of a product, so that what X and Z become are right operands of the next product where
-// they are.  X and Z are made twice, by rows and by columns.
+// 16 tokens and half of the columns of keys: a lane has a token, of which everything above is a column of a product.  X and Z are made once, block by block,
+// and go through LDS by rows and by columns.
 #include "delta_chunk.h"
+#include "rows_vectors.h"
 
 namespace {
 
 using namespace dg_delta;
 
-constexpr int kTokens = kMark, kTokenPitch = kTokens + 8, kColumns = 32, kColumnPitch = kColumns + 8;
+constexpr int kTokens = kMark, kTokenPitch = kTokens + 8, kColumns = 32, kColumnPitch = kColumns + 8, kWaves = 8, kThreads = kWaves * 64;
 
+// 32 columns of values at a time
 template <class T, int KS>
-struct Shared {
-    static constexpr int n = Pieces<T>::n;
-    union {
-        struct {                        // 32 columns of values at a time
-            uint16_t S[3][32 * KS][kColumnPitch], dS[3][32 * KS][kColumnPitch], U[3][kTokens][kColumnPitch], R[3][kTokens][kColumnPitch], O[n][kTokens][kColumnPitch];
-        };
-        struct { uint16_t KT[n][32 * KS][kTokenPitch], QT[n][32 * KS][kTokenPitch]; };
-    };
-    double G[kTokens];
-    float beta[kTokens], dG[kTokens], values[kTokens], end[4];
+struct Values {
+    uint16_t S[3][32 * KS][kColumnPitch], dS[3][32 * KS][kColumnPitch], U[3][kTokens][kColumnPitch], R[3][kTokens][kColumnPitch], O[Pieces<T>::n][kTokens][kColumnPitch];
 };
 
-// A lane has rows 4 q to 4 q + 3 of two results of 16, which become places 8 q to 8 q + 7 of the next sum over tokens: where token t stands among the columns
-// of its left operands.
-__device__ __forceinline__ uint32_t place(uint32_t t) { return (t & ~31u) | (t >> 2 & 3) << 3 | (t >> 4 & 1) << 2 | (t & 3); }
+// X and Z by rows (row i, columns j) and Z, later X, by columns (row j, columns i)
+struct Pulls { uint16_t X[3][kTokens][kTokenPitch], Z[3][kTokens][kTokenPitch], ZT[3][kTokens][kTokenPitch]; };
+
+// columns of K, or of Q, as rows
+template <class T, int KS>
+struct Turned { uint16_t rows[Pieces<T>::n][32 * KS][kTokenPitch]; };
+
+struct Tokens {
+    double G[kTokens];
+    float beta[kTokens], dG[2][kTokens], values[kTokens], end[kWaves];
+};
+
+// K and Q both stay if there is room; otherwise they come one after the other for every head
+template <class T, int KS>
+constexpr bool kTogether = (sizeof(Values<T, KS>) > sizeof(Pulls) ? sizeof(Values<T, KS>) : sizeof(Pulls)) + 2 * sizeof(Turned<T, KS>) + sizeof(Tokens) <= 160 * 1024;
+
+template <class T, int KS, bool kBoth>
+struct Shared : Tokens {
+    union {
+        Values<T, KS> value;
+        struct { Pulls pull; Turned<T, KS> turned[1]; };
+    };
+};
+template <class T, int KS>
+struct Shared<T, KS, true> : Tokens {
+    union { Values<T, KS> value; Pulls pull; };
+    Turned<T, KS> turned[2];
+};
 
 // sum over the four lanes that have a token
 __device__ __forceinline__ float of_token(float v)
@@ -39,46 +58,85 @@ __device__ __forceinline__ float of_token(float v)
     return v + __shfl_xor(v, 32);
 }
 
-// Eight values of a row from column c on, or others where there are none: `cleared` tells them apart when they are used, so that nothing waits for the load
-template <class T, bool kVec>
-__device__ __forceinline__ void ahead(const T *row, uint32_t c, uint32_t D, dg_rows::Pack<T, 8> &out)
+// W values from an address on that the workgroup shares and a lane's distance in bytes; `left` of them are a row's, the others are whatever comes instead: `cleared`
+// tells them apart when they are used, so that nothing waits for the load.
+template <class T, int W, bool kVec>
+__device__ __forceinline__ void ahead(const T *base, uint32_t bytes, int left, dg_rows::Pack<T, W> &out)
 {
-    constexpr int m = 16 / sizeof(T);
+    constexpr int m = 16 / sizeof(T) < W ? 16 / sizeof(T) : W;
     if constexpr (kVec) {
 #pragma unroll
-        for (int h = 0; h < 8 / m; ++h) {
-            const dg_rows::Pack<T, m> p = *reinterpret_cast<const dg_rows::Pack<T, m> *>(row + (c + h * m < D ? c + h * m : 0));
+        for (int h = 0; h < W / m; ++h) {
+            const dg_rows::Pack<T, m> p = *reinterpret_cast<const dg_rows::Pack<T, m> *>((const char *)base + (h * m < left ? bytes + h * m * (uint32_t)sizeof(T) : 0u));
 #pragma unroll
             for (int i = 0; i < m; ++i) out.v[h * m + i] = p.v[i];
         }
     } else
 #pragma unroll
-        for (int i = 0; i < 8; ++i) out.v[i] = row[c + i < D ? c + i : 0];
+        for (int i = 0; i < W; ++i) out.v[i] = *reinterpret_cast<const T *>((const char *)base + (i < left ? bytes + i * (uint32_t)sizeof(T) : 0u));
 }
 
-template <class T>
-__device__ __forceinline__ void cleared(const dg_rows::Pack<T, 8> &p, uint32_t c, uint32_t D, bool in, float (&out)[8])
+template <class T, int W>
+__device__ __forceinline__ void cleared(const dg_rows::Pack<T, W> &p, uint32_t c, uint32_t D, bool in, float (&out)[W])
 {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) out[i] = in && c + i < D ? (float)p.v[i] : 0.0f;
+    for (int i = 0; i < W; ++i) out[i] = in && c + i < D ? (float)p.v[i] : 0.0f;
 }
 
 template <int n, int rows, int pitch>
-__device__ __forceinline__ void put8(const float (&v)[8], uint16_t (&to)[n][rows][pitch], uint32_t row, uint32_t col)
+__device__ __forceinline__ void put4(const float (&v)[4], uint16_t (&to)[n][rows][pitch], uint32_t row, uint32_t col)
 {
-    uint32_t w[n][4];
-    split<n, 8>(v, w);
+    uint32_t w[n][2];
+    split<n, 4>(v, w);
 #pragma unroll
-    for (int p = 0; p < n; ++p) *reinterpret_cast<u32x4 *>(&to[p][row][col]) = (u32x4){w[p][0], w[p][1], w[p][2], w[p][3]};
+    for (int p = 0; p < n; ++p) *reinterpret_cast<u32x2 *>(&to[p][row][col]) = (u32x2){w[p][0], w[p][1]};
+}
+
+// K or Q from the block's lowest row on; at(t): how many rows behind it token t is
+template <class T, int KS, bool kVec, class At>
+__device__ __forceinline__ void turn(const T *K, uint32_t ld, uint32_t Dk, uint32_t count, At at, Turned<T, KS> &to)
+{
+    constexpr int n = Pieces<T>::n, kEach = KS > 2 ? KS / 2 : 1;        // of a thread, if it has any
+    // rows are loaded as they lie
+    auto token = [](int i) { return (i * kThreads + threadIdx.x) / (4 * KS); };
+    const uint32_t col = threadIdx.x % (4 * KS) * 8;
+    if (token(0) >= kTokens) return;
+    dg_rows::Pack<T, 8> x[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) ahead<T, 8, kVec>(K, (at(token(i)) * ld + col) * (uint32_t)sizeof(T), (int)Dk - (int)col, x[i]);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const uint32_t t = token(i);
+        float v[8];
+        uint32_t w[n][4];
+        cleared<T, 8>(x[i], col, Dk, t < count, v);
+        split<n, 8>(v, w);
+#pragma unroll
+        for (int p = 0; p < n; ++p)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) to.rows[p][col + j][t] = (uint16_t)(w[p][j / 2] >> (j % 2 * 16));
+    }
+}
+
+// four values of a row side by side, or of a column one below the other
+__device__ __forceinline__ void put_across(const float (&v)[4], uint16_t (&to)[3][kTokens][kTokenPitch], uint32_t row, uint32_t col) { put4(v, to, row, col); }
+__device__ __forceinline__ void put_down(const float (&v)[4], uint16_t (&to)[3][kTokens][kTokenPitch], uint32_t row, uint32_t col)
+{
+    uint32_t w[3][2];
+    split<3, 4>(v, w);
+#pragma unroll
+    for (int p = 0; p < 3; ++p)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to[p][row + i][col] = (uint16_t)(w[p][i / 2] >> (i % 2 * 16));
 }
 
 template <class T, int KS, bool kVec>
-__global__ void __launch_bounds__(256, 1)
+__global__ void __launch_bounds__(kThreads)
 delta_grad_kernel(Delta d, uint64_t from)
 {
-    __shared__ alignas(16) Shared<T, KS> lds;
-    constexpr int n = Pieces<T>::n, kTiles = 2 * KS, kMemoryRows = KS == 4 ? 2 : 1;     // rows of the memory that a thread brings
-    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c16 = lane % 16, r4 = lane / 16 * 4, r8 = lane / 16 * 8;
+    __shared__ alignas(16) Shared<T, KS, kTogether<T, KS>> lds;
+    constexpr int n = Pieces<T>::n, kTiles = KS, kMemoryRows = KS > 2 ? KS / 2 : 1;     // results of 16 columns of keys of a wavefront; rows of the memory of a thread, if it has any
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64 % 4), half = __builtin_amdgcn_readfirstlane(threadIdx.x / 256), key0 = half * 16 * KS;
     const uint64_t unit = from + blockIdx.x;
     const uint32_t hk = (uint32_t)(unit % d.Hk), group = d.H / d.Hk;
     uint32_t slot = (uint32_t)(unit / d.Hk), seq, block;
@@ -95,39 +153,59 @@ delta_grad_kernel(Delta d, uint64_t from)
     else slot = first_slot(span, seq) + block;
     if ((uint64_t)block * kTokens >= span.len) return;
     const uint32_t t0 = block * kTokens, count = span.len - t0 < kTokens ? span.len - t0 : kTokens;
-    const T *K = (const T *)d.k + hk * d.Dk, *Q = (const T *)d.q + hk * d.Dk;
-    auto row_of = [&](uint32_t t) { return span.row(t0 + (t < count ? t : 0)); };
+    // rows as distances from the lowest of the block: up to 63 rows of less than 2^24 values
+    const uint64_t lowest = span.turn ? span.begin + (span.len - t0 - count) : span.begin + t0;
+    auto behind = [&](uint32_t t) { return t >= count ? 0u : span.turn ? count - 1 - t : t; };
+    auto row_of = [&](uint32_t t) { return lowest + behind(t); };
+    const T *K = (const T *)d.k + lowest * d.ldk + hk * d.Dk, *Q = (const T *)d.q + lowest * d.ldq + hk * d.Dk;
 
-    const uint32_t mine = wave * 16 + c16;              // the token that a lane has as a column
-    const bool in = mine < count;
-    const uint64_t row = row_of(mine);
-    const uint32_t brought = threadIdx.x / 4, c8 = threadIdx.x % 4 * 8;         // the token, or row of the memory, of which a thread brings eight columns
-    const bool there = brought < count;
-    const uint64_t brought_row = row_of(brought);
+    constexpr bool kBoth = kTogether<T, KS>;
+    if constexpr (kBoth) {
+        turn<T, KS, kVec>(K, (uint32_t)d.ldk, d.Dk, count, behind, lds.turned[0]);
+        turn<T, KS, kVec>(Q, (uint32_t)d.ldq, d.Dk, count, behind, lds.turned[1]);
+    }
+    // X and Z are made of ten blocks of 16 x 16 on and below the diagonal: one for each wavefront, another for the first two
+    const uint32_t blocks = threadIdx.x < 128 ? 2 : 1;
+    const uint32_t all_waves = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    auto block_row = [&](uint32_t i) -> uint32_t { return all_waves + 8 * i < 1 ? 0 : all_waves + 8 * i < 3 ? 1 : all_waves + 8 * i < 6 ? 2 : 3; };
+    auto block_column = [&](uint32_t i) -> uint32_t { return all_waves + 8 * i - block_row(i) * (block_row(i) + 1) / 2; };
+    const uint32_t bi[2] = {block_row(0), block_row(1)}, bj[2] = {block_column(0), block_column(1)};
     f32x4 dq[kTiles] = {}, dk[kTiles] = {};
 
     for (uint32_t h = 0; h < group; ++h) {
         const uint32_t head = hk * group + h;
+        const uint32_t thread = again(threadIdx.x), lane = thread % 64, c16 = lane % 16, r4 = lane / 16 * 4, r8 = lane / 16 * 8;
+        const uint32_t mine = wave * 16 + c16;              // the token that a lane has as a column
+        // A thread brings four columns of rows b, b + 64 of the memory and its gradient, and of token b: eight threads a line
+        const uint32_t b = thread / 8, c4 = thread % 8 * 4;
+        const uint64_t brought_row = row_of(b);
+        const bool there = b < count;
+        const uint32_t ldf = d.H * d.Dv;
+        uint32_t at_s[kMemoryRows];
+#pragma unroll
+        for (int i = 0; i < kMemoryRows; ++i) at_s[i] = ((b + i * 64 < d.Dk ? b + i * 64 : 0) * d.Dv + c4) * 4;
+        const uint32_t at_f = (behind(b) * ldf + c4) * 4, at_o = (behind(b) * (uint32_t)d.lddo + c4) * (uint32_t)sizeof(T), at_v = (behind(b) * (uint32_t)d.ldv + c4) * (uint32_t)sizeof(T);
         const float *S = d.marks + ((uint64_t)slot * d.H + head) * d.Dk * d.Dv, *dS = d.dmarks + ((uint64_t)slot * d.H + head) * d.Dk * d.Dv;
-        const uint64_t at = (brought_row * d.H + head) * d.Dv;
-        dg_rows::Pack<float, 8> next_s[kMemoryRows], next_ds[kMemoryRows], next_y, next_r;
-        dg_rows::Pack<T, 8> next_o, next_v;
-        auto fetch = [&](uint32_t c) {
+        dg_rows::Pack<float, 4> next_s[kMemoryRows], next_ds[kMemoryRows], next_y, next_r;
+        dg_rows::Pack<T, 4> next_o, next_v;
+        const float *Y = d.y + lowest * ldf + head * d.Dv, *R = d.dr + lowest * ldf + head * d.Dv;
+        const T *O = (const T *)d.dout + lowest * d.lddo + head * d.Dv, *V = (const T *)d.v + lowest * d.ldv + head * d.Dv;
+        auto fetch = [&](uint32_t c0) {
+            const int left = (int)d.Dv - (int)(c0 + c4);
 #pragma unroll
             for (int i = 0; i < kMemoryRows; ++i) {
-                const uint64_t r = brought + i * 64 < d.Dk ? brought + i * 64 : 0;
-                ahead<float, kVec>(S + r * d.Dv, c, d.Dv, next_s[i]);
-                ahead<float, kVec>(dS + r * d.Dv, c, d.Dv, next_ds[i]);
+                ahead<float, 4, kVec>(S + c0, at_s[i], left, next_s[i]);
+                ahead<float, 4, kVec>(dS + c0, at_s[i], left, next_ds[i]);
             }
-            ahead<float, kVec>(d.y + at, c, d.Dv, next_y);
-            ahead<float, kVec>(d.dr + at, c, d.Dv, next_r);
-            ahead<T, kVec>((const T *)d.dout + brought_row * d.lddo + head * d.Dv, c, d.Dv, next_o);
-            ahead<T, kVec>((const T *)d.v + brought_row * d.ldv + head * d.Dv, c, d.Dv, next_v);
+            ahead<float, 4, kVec>(Y + c0, at_f, left, next_y);
+            ahead<float, 4, kVec>(R + c0, at_f, left, next_r);
+            ahead<T, 4, kVec>(O + c0, at_o, left, next_o);
+            ahead<T, 4, kVec>(V + c0, at_v, left, next_v);
         };
-        fetch(c8);
-        const float beta_brought = there ? d.beta[brought_row * d.ldb + head] : 0.0f;
+        fetch(0);
+        const float rate = there ? d.beta[brought_row * d.ldb + head] : 0.0f;
         __syncthreads();                                // what the last head left in LDS has been read
-        if (wave == 0) {
+        if (thread < 64) {
             const bool held = lane < count;
             const uint64_t r = row_of(lane);
             const float value = d.g[r * d.ldg + head], b = d.beta[r * d.ldb + head];
@@ -141,67 +219,57 @@ delta_grad_kernel(Delta d, uint64_t from)
             lds.beta[lane] = held ? b : 0.0f;
         }
         f32x4 from_q[kTiles] = {}, from_k[kTiles] = {}, to_k[kTiles] = {};          // dO S^T, dR S^T, U dS'^T
-        f32x4 m1[4] = {}, e1[4] = {}, m2[4] = {}, e2[4] = {};                       // dO U^T, dR U^T of the lane's row and of its column
-        float dbeta = 0.0f, dot = 0.0f, values = 0.0f;
+        f32x4 m[2] = {}, e[2] = {};                                                 // dO U^T, dR U^T of the wavefront's blocks: lane i, rows j
+        float dbeta = 0.0f, values = 0.0f, dot = 0.0f;
 #pragma unroll 1
         for (uint32_t c0 = 0; c0 < d.Dv; c0 += kColumns) {
             {
-                const uint32_t c = c0 + c8;
-                float x[8], y[8], r[8];
+                const uint32_t c = c0 + c4;
+                float x[4], y[4], r[4], out[4];
 #pragma unroll
                 for (int i = 0; i < kMemoryRows; ++i) {
-                    const uint32_t to = brought + i * 64;
+                    const uint32_t to = b + i * 64;
                     if (to >= 32 * KS) continue;
-                    cleared<float>(next_s[i], c, d.Dv, to < d.Dk, x);
-                    put8(x, lds.S, to, c8);
-                    cleared<float>(next_ds[i], c, d.Dv, to < d.Dk, y);
-                    put8(y, lds.dS, to, c8);
+                    cleared<float, 4>(next_s[i], c, d.Dv, to < d.Dk, x);
+                    put4(x, lds.value.S, to, c4);
+                    cleared<float, 4>(next_ds[i], c, d.Dv, to < d.Dk, y);
+                    put4(y, lds.value.dS, to, c4);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) dot = fmaf(x[j], y[j], dot);
+                    for (int j = 0; j < 4; ++j) dot = fmaf(x[j], y[j], dot);
                 }
-                cleared<float>(next_r, c, d.Dv, there, r);
-                put8(r, lds.R, brought, c8);
-                cleared<float>(next_y, c, d.Dv, there, y);
-                cleared<T>(next_v, c, d.Dv, there, x);
+                cleared<float, 4>(next_r, c, d.Dv, there, r);
+                put4(r, lds.value.R, b, c4);
+                cleared<float, 4>(next_y, c, d.Dv, there, y);
+                cleared<T, 4>(next_v, c, d.Dv, there, x);
                 T *dv = (T *)d.dv + brought_row * d.lddv + head * d.Dv + c;
-                float out[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
+                for (int j = 0; j < 4; ++j) {
                     dbeta = fmaf(r[j], y[j], dbeta);
-                    y[j] *= beta_brought;
-                    out[j] = beta_brought * r[j];
+                    y[j] *= rate;
+                    out[j] = rate * r[j];
                     values = fmaf(out[j], x[j], values);
                     if (!kVec && there && c + j < d.Dv) dv[j] = (T)out[j];
                 }
-                if (kVec && there) {
-                    constexpr int m = 16 / sizeof(T);
-#pragma unroll
-                    for (int j = 0; j < 8; j += m) {
-                        float part[m];
-#pragma unroll
-                        for (int i = 0; i < m; ++i) part[i] = out[j + i];
-                        if (c + j < d.Dv) dg_rows::store<T, m>(dv + j, part);
-                    }
-                }
-                put8(y, lds.U, brought, c8);
-                cleared<T>(next_o, c, d.Dv, there, x);
-                put8(x, lds.O, brought, c8);
+                if (kVec && there && c < d.Dv) dg_rows::store<T, 4>(dv, out);
+                put4(y, lds.value.U, b, c4);
+                cleared<T, 4>(next_o, c, d.Dv, there, x);
+                put4(x, lds.value.O, b, c4);
             }
             __syncthreads();
-            if (c0 + kColumns < d.Dv) fetch(c0 + kColumns + c8);
-            bf16x8 o[n], r[3], u[3], a[3], b[n];
-            lefts(lds.O, mine, r8, o);
-            lefts(lds.R, mine, r8, r);
-            lefts(lds.U, mine, r8, u);
+            if (c0 + kColumns < d.Dv) fetch(c0 + kColumns);
+            bf16x8 o[n], r[3], u[3], a[3];
+            lefts(lds.value.O, mine, r8, o);
+            lefts(lds.value.R, mine, r8, r);
+            lefts(lds.value.U, mine, r8, u);
             // one tile's operands on their way while another's are multiplied, and no more, for which there would not be registers
             bf16x8 s2[2][3], ds2[2][3];
-            lefts(lds.S, c16, r8, s2[0]);
-            lefts(lds.dS, c16, r8, ds2[0]);
+            lefts(lds.value.S, key0 + c16, r8, s2[0]);
+            lefts(lds.value.dS, key0 + c16, r8, ds2[0]);
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
                 if (t + 1 < kTiles) {
-                    lefts(lds.S, (t + 1) * 16 + c16, r8, s2[(t + 1) % 2]);
-                    lefts(lds.dS, (t + 1) * 16 + c16, r8, ds2[(t + 1) % 2]);
+                    lefts(lds.value.S, key0 + (t + 1) * 16 + c16, r8, s2[(t + 1) % 2]);
+                    lefts(lds.value.dS, key0 + (t + 1) * 16 + c16, r8, ds2[(t + 1) % 2]);
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 from_q[t] = multiply<3, n>(s2[t % 2], o, from_q[t]);
@@ -209,70 +277,52 @@ delta_grad_kernel(Delta d, uint64_t from)
                 to_k[t] = multiply<3, 3>(ds2[t % 2], u, to_k[t]);
             }
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
+            for (int i = 0; i < 2; ++i) {
                 __builtin_amdgcn_sched_barrier(0);
-                if (t <= (int)wave) {                   // tokens j: up to the lane's
-                    lefts(lds.U, t * 16 + c16, r8, a);
-                    m1[t] = multiply<3, n>(a, o, m1[t]);
-                    e1[t] = multiply<3, 3>(a, r, e1[t]);
-                }
-                if (t >= (int)wave) {                   // tokens i: from the lane's on
-                    lefts(lds.O, t * 16 + c16, r8, b);
-                    m2[t] = multiply<n, 3>(b, u, m2[t]);
-                    lefts(lds.R, t * 16 + c16, r8, a);
-                    e2[t] = multiply<3, 3>(a, u, e2[t]);
-                }
+                if (i >= (int)blocks) continue;
+                lefts(lds.value.U, bj[i] * 16 + c16, r8, a);
+                lefts(lds.value.O, bi[i] * 16 + c16, r8, o);
+                lefts(lds.value.R, bi[i] * 16 + c16, r8, r);
+                m[i] = multiply<3, n>(a, o, m[i]);
+                e[i] = multiply<3, 3>(a, r, e[i]);
             }
             __syncthreads();
         }
-        dbeta += __shfl_xor(dbeta, 1);
-        dbeta += __shfl_xor(dbeta, 2);
-        values += __shfl_xor(values, 1);
-        values += __shfl_xor(values, 2);
-        if (threadIdx.x % 4 == 0) {
-            lds.values[brought] = values;
+        dbeta = dg_rows::group_sum<8>(dbeta);
+        values = dg_rows::group_sum<8>(values);
+        if (thread % 8 == 0) {
+            lds.values[b] = values;
             if (there) d.dbeta[brought_row * d.lddb + head] = dbeta;
         }
         const double G = lds.G[mine], last = lds.G[kTokens - 1];
         const float since = expf((float)G), until = expf((float)(last - G)), beta = lds.beta[mine];
-        // columns of K and Q as rows, where the columns of values have been
-        for (uint32_t item = threadIdx.x; item < kTokens * 4 * KS; item += 256) {
-            const uint32_t t = item / (4 * KS), col = item % (4 * KS) * 8;
-            dg_rows::Pack<T, 8> k8, q8;
-            ahead<T, kVec>(K + row_of(t) * d.ldk, col, d.Dk, k8);
-            ahead<T, kVec>(Q + row_of(t) * d.ldq, col, d.Dk, q8);
-            float v[8];
-            uint32_t w[n][4];
-            cleared<T>(k8, col, d.Dk, t < count, v);
-            split<n, 8>(v, w);
-    #pragma unroll
-            for (int p = 0; p < n; ++p)
-    #pragma unroll
-                for (int i = 0; i < 8; ++i) lds.KT[p][col + i][place(t)] = (uint16_t)(w[p][i / 2] >> (i % 2 * 16));
-            cleared<T>(q8, col, d.Dk, t < count, v);
-            split<n, 8>(v, w);
-    #pragma unroll
-            for (int p = 0; p < n; ++p)
-    #pragma unroll
-                for (int i = 0; i < 8; ++i) lds.QT[p][col + i][place(t)] = (uint16_t)(w[p][i / 2] >> (i % 2 * 16));
-        }
-        // X and Z, of the lane's row and of its column
+        if constexpr (!kBoth) turn<T, KS, kVec>(K, (uint32_t)d.ldk, d.Dk, count, behind, lds.turned[0]);
+        // X and Z
+        float x[2][4];
+        const float none[4] = {};
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int k = 0; k < 2; ++k) {
+            if (k >= (int)blocks) continue;
+            const uint32_t i = bi[k] * 16 + c16, j0 = bj[k] * 16 + r4;
+            const double Gi = lds.G[i];
+            const float rate_i = lds.beta[i];
+            float z[4];
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const uint32_t j = t * 16 + r4 + x;
-                if (t <= (int)wave) {
-                    const float fade = j <= mine ? expf((float)(G - lds.G[j])) : 0.0f;
-                    m1[t][x] *= d.scale * fade;
-                    e1[t][x] = j < mine ? -beta * fade * e1[t][x] : 0.0f;
-                }
-                if (t >= (int)wave) {                   // j is the later token here
-                    const float fade = j >= mine ? expf((float)(lds.G[j] - G)) : 0.0f;
-                    m2[t][x] *= d.scale * fade;
-                    e2[t][x] = j > mine ? -lds.beta[j] * fade * e2[t][x] : 0.0f;
-                }
+            for (int y = 0; y < 4; ++y) {
+                const float fade = j0 + y <= i ? expf((float)(Gi - lds.G[j0 + y])) : 0.0f;
+                x[k][y] = d.scale * fade * m[k][y];
+                z[y] = j0 + y < i ? -rate_i * fade * e[k][y] : 0.0f;
             }
+            put_across(x[k], lds.pull.X, i, j0);
+            put_across(z, lds.pull.Z, i, j0);
+            put_down(z, lds.pull.ZT, j0, i);
+        }
+        // the blocks behind the diagonal that are multiplied with
+        if (half == 1 && wave < 2) {
+            put_across(none, lds.pull.X, wave * 32 + c16, wave * 32 + 16 + r4);
+            put_across(none, lds.pull.Z, wave * 32 + c16, wave * 32 + 16 + r4);
+            put_across(none, lds.pull.ZT, wave * 32 + 16 + c16, wave * 32 + r4);
+        }
         // what the memory before gives and the one behind takes, and what the tokens of the block tell each other
         float at_end = 0.0f, dG = 0.0f;
         f32x4 here[kTiles];
@@ -285,57 +335,73 @@ delta_grad_kernel(Delta d, uint64_t from)
         __syncthreads();
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            bf16x8 x1[3], y1[3], x2[3], y2[3];
+            bf16x8 x1[3], z1[3], z2[3], a[2][n];
             const bool before = 2 * s <= (int)wave, after = 2 * s + 1 >= (int)wave;
-            split_rows<3>(m1[2 * s], m1[2 * s + 1], x1);
-            split_rows<3>(e1[2 * s], e1[2 * s + 1], y1);
-            split_rows<3>(m2[2 * s], m2[2 * s + 1], x2);
-            split_rows<3>(e2[2 * s], e2[2 * s + 1], y2);
-            bf16x8 a[2][n], b[2][n];
-            lefts(lds.KT, c16, s * 32 + r8, a[0]);
-            lefts(lds.QT, c16, s * 32 + r8, b[0]);
+            lefts(lds.pull.X, mine, s * 32 + r8, x1);
+            lefts(lds.pull.Z, mine, s * 32 + r8, z1);
+            lefts(lds.pull.ZT, mine, s * 32 + r8, z2);
+            lefts(lds.turned[0].rows, key0 + c16, s * 32 + r8, a[0]);
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
-                if (t + 1 < kTiles) {
-                    lefts(lds.KT, (t + 1) * 16 + c16, s * 32 + r8, a[(t + 1) % 2]);
-                    lefts(lds.QT, (t + 1) * 16 + c16, s * 32 + r8, b[(t + 1) % 2]);
-                }
+                if (t + 1 < kTiles) lefts(lds.turned[0].rows, key0 + (t + 1) * 16 + c16, s * 32 + r8, a[(t + 1) % 2]);
                 __builtin_amdgcn_sched_barrier(0);
                 if (before) {
                     here[t] = multiply<n, 3>(a[t % 2], x1, here[t]);
-                    dk[t] = multiply<n, 3>(a[t % 2], y1, dk[t]);
+                    dk[t] = multiply<n, 3>(a[t % 2], z1, dk[t]);
                 }
-                if (after) {
-                    dk[t] = multiply<n, 3>(b[t % 2], x2, dk[t]);
-                    dk[t] = multiply<n, 3>(a[t % 2], y2, dk[t]);
-                }
+                if (after) dk[t] = multiply<n, 3>(a[t % 2], z2, dk[t]);
             }
         }
+        auto dot_tokens = [&](const uint16_t (&rows)[n][32 * KS][kTokenPitch], const f32x4 (&with)[kTiles]) {
+            float sum = 0.0f;
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-            dq[t] += here[t];
+            for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const uint32_t c = t * 16 + r4 + x;
-                float q = 0.0f, k = 0.0f;       // from their pieces, 0 where there is no token or column
+                for (int y = 0; y < 4; ++y) {
+                    float value = 0.0f;             // from its pieces, 0 where there is no token or column
 #pragma unroll
-                for (int p = 0; p < n; ++p) {
-                    q += __uint_as_float((uint32_t)lds.QT[p][c][place(mine)] << 16);
-                    k += __uint_as_float((uint32_t)lds.KT[p][c][place(mine)] << 16);
+                    for (int p = 0; p < n; ++p) value += __uint_as_float((uint32_t)rows[p][key0 + t * 16 + r4 + y][mine] << 16);
+                    sum = fmaf(value, with[t][y], sum);
                 }
-                dG = fmaf(q, here[t][x], dG);
-                at_end = fmaf(k, to_k[t][x], at_end);
+            return sum;
+        };
+        at_end = dot_tokens(lds.turned[0].rows, to_k);
+        __syncthreads();
+        if constexpr (!kBoth) turn<T, KS, kVec>(Q, (uint32_t)d.ldq, d.Dk, count, behind, lds.turned[0]);
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            if (k < (int)blocks) put_down(x[k], lds.pull.X, bj[k] * 16 + r4, bi[k] * 16 + c16);
+        if (half == 1 && wave < 2) put_across(none, lds.pull.X, wave * 32 + 16 + c16, wave * 32 + r4);
+        __syncthreads();
+        auto &queries = lds.turned[kBoth ? 1 : 0].rows;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            bf16x8 x2[3], a[2][n];
+            const bool after = 2 * s + 1 >= (int)wave;
+            lefts(lds.pull.X, mine, s * 32 + r8, x2);
+            lefts(queries, key0 + c16, s * 32 + r8, a[0]);
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+                if (t + 1 < kTiles) lefts(queries, key0 + (t + 1) * 16 + c16, s * 32 + r8, a[(t + 1) % 2]);
+                __builtin_amdgcn_sched_barrier(0);
+                if (after) dk[t] = multiply<n, 3>(a[t % 2], x2, dk[t]);
             }
         }
+        dG = dot_tokens(queries, here);
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) dq[t] += here[t];
         dG = of_token(dG);
-        if (lane < 16) lds.dG[mine] = dG;
+        if (lane < 16) lds.dG[half][mine] = dG;
         float end = fmaf(expf((float)last), dot, at_end);
 #pragma unroll
         for (int s = 1; s < 64; s *= 2) end += __shfl_xor(end, s);
-        if (lane == 0) lds.end[wave] = end;
+        if (lane == 0) lds.end[thread / 64] = end;
         __syncthreads();
-        if (wave == 0) {
-            float sum = lds.dG[lane] - lds.values[lane] + (lane == 63 ? lds.end[0] + lds.end[1] + lds.end[2] + lds.end[3] : 0.0f);
+        if (thread < 64) {
+            float sum = lds.dG[0][lane] + lds.dG[1][lane] - lds.values[lane];
+            if (lane == 63)
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) sum += lds.end[w];
 #pragma unroll
             for (int s = 1; s < 64; s *= 2) {
                 const float after = __shfl_down(sum, s);
@@ -344,10 +410,12 @@ delta_grad_kernel(Delta d, uint64_t from)
             if (lane < count) d.dg[row_of(lane) * d.lddg + head] = sum;
         }
     }
-    if (!in) return;
+    const uint32_t mine = wave * 16 + threadIdx.x % 16, r4 = threadIdx.x % 64 / 16 * 4;
+    const uint64_t row = row_of(mine);
+    if (mine >= count) return;
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-        const uint32_t c = t * 16 + r4;
+        const uint32_t c = key0 + t * 16 + r4;
         T *to_q = (T *)d.dq + row * d.lddq + hk * d.Dk + c, *to_k = (T *)d.dk + row * d.lddk + hk * d.Dk + c;
         if constexpr (kVec) {
             if (c >= d.Dk) continue;
@@ -387,8 +455,8 @@ void launch_size(const Delta &d, hipStream_t st)
     const uint64_t slots = d.first ? d.slots : d.n_seq * ((d.N / d.n_seq + kTokens - 1) / kTokens), units = slots * d.Hk;
     for (uint64_t from = 0; from < units; from += kMostLaunched) {
         const uint32_t grid = (uint32_t)(units - from < kMostLaunched ? units - from : kMostLaunched);
-        if (d.vec_all && d.vec_out) delta_grad_kernel<T, KS, true><<<grid, 256, 0, st>>>(d, from);
-        else delta_grad_kernel<T, KS, false><<<grid, 256, 0, st>>>(d, from);
+        if (d.vec_all && d.vec_out) delta_grad_kernel<T, KS, true><<<grid, kThreads, 0, st>>>(d, from);
+        else delta_grad_kernel<T, KS, false><<<grid, kThreads, 0, st>>>(d, from);
     }
 }
 
