@@ -9,8 +9,14 @@ using namespace dg_delta;
 // Up to so many tokens a sequence, on average, they are taken one by one.
 constexpr uint64_t kFewTokens = 4;
 
+// From so many heads of all sequences on small ones are taken token by token, several to a wavefront.
+constexpr uint64_t kManyHeads = 512;
+
 // Whether a lane takes a column or row of the memory along a sequence, instead of wavefronts chunks of it
-bool takes_small(uint32_t n_seq, uint32_t H, uint32_t Dk, uint32_t Dv) { return Dk <= 32 && Dv <= 32 && (uint64_t)n_seq * H >= 1; }
+bool takes_small(uint64_t N, uint32_t n_seq, uint32_t H, uint32_t Dk, uint32_t Dv)
+{
+    return Dk <= 32 && Dv <= 32 && ((uint64_t)n_seq * H >= kManyHeads || N <= kFewTokens * n_seq);
+}
 
 uint64_t slots_of(uint64_t N, uint32_t n_seq) { return N / kMark + n_seq; }
 
@@ -94,7 +100,7 @@ extern "C" int dg_delta_rule_fwd(const void *q, uint64_t ldq, const void *k, uin
     d.first = first, d.N = N, d.n_seq = n_seq, d.Hk = Hk, d.H = H, d.Dk = Dk, d.Dv = Dv, d.reverse = reverse, d.scale = scale;
     if (saved) d.marks = (float *)saved, d.y = (float *)((char *)saved + padded(marks_bytes(N, n_seq, H, Dk, Dv)));
     use_vectors(d, o, ldo, dtype);
-    if (takes_small(n_seq, H, Dk, Dv)) launch_small(d, dtype, false, (hipStream_t)stream);
+    if (takes_small(N, n_seq, H, Dk, Dv)) launch_small(d, dtype, false, (hipStream_t)stream);
     else if (!saved && N <= kFewTokens * n_seq) launch_tokens(d, dtype, (hipStream_t)stream);
     else {
         const size_t bytes = forward_bytes(N, n_seq, H);
@@ -139,7 +145,7 @@ extern "C" int dg_delta_rule_bwd(const void *q, uint64_t ldq, const void *k, uin
     use_vectors(d, do_, lddo, dtype);
     d.vec_out = wide_rows(dv, lddv, Dv, dtype) && wide_rows(dq, lddq, Dk, dtype) && wide_rows(dk, lddk, Dk, dtype);
     if (N) launch_slots(d, (hipStream_t)stream);
-    if (takes_small(n_seq, H, Dk, Dv)) launch_small(d, dtype, true, (hipStream_t)stream);
+    if (takes_small(N, n_seq, H, Dk, Dv)) launch_small(d, dtype, true, (hipStream_t)stream);
     else {
         if (N) launch_weights(d, dtype, true, (hipStream_t)stream);
         launch_backward(d, dtype, (hipStream_t)stream);

@@ -35,12 +35,21 @@ struct Product {
     uint32_t tiles_m, tiles_n;
 };
 
-// 16 values of a row from column c on, 0 from K on; where the row ends within them they are fetched one by one, so that nothing behind it is read
-__device__ __forceinline__ u32x4 sixteen(const uint8_t *row, uint32_t c, uint32_t K)
+// 16 values of a row from column c on, 0 from K on.  Where the row ends within them, what lies behind it is cleared; behind the last row nothing may lie, so that there
+// they are fetched one by one.
+__device__ __forceinline__ u32x4 sixteen(const uint8_t *row, uint32_t c, uint32_t K, bool last)
 {
-    if (c + 16 <= K) return *reinterpret_cast<const u32x4 *>(row + c);
     u32x4 v = {0, 0, 0, 0};
-    for (uint32_t i = 0; c + i < K && i < 16; ++i) v[i / 4] |= (uint32_t)row[c + i] << (8 * (i % 4));
+    if (c >= K) return v;
+    if (c + 16 <= K || !last) v = *reinterpret_cast<const u32x4 *>(row + c);
+    else
+        for (uint32_t i = 0; c + i < K; ++i) v[i / 4] |= (uint32_t)row[c + i] << (8 * (i % 4));
+    const uint32_t here = K - c;
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) {
+        const uint32_t bytes = here > 4 * i ? here - 4 * i : 0;
+        v[i] = bytes >= 4 ? v[i] : v[i] & ((1u << 8 * bytes) - 1);
+    }
     return v;
 }
 
@@ -62,10 +71,12 @@ few_rows_kernel(Product p)
     const uint32_t n = n0 + lane % 16 < p.b.rows ? n0 + lane % 16 : p.b.rows - 1;
     const uint8_t *b = p.b.q + n * p.b.ld, *sb = p.b.scales + n * p.b.lds;
     const uint8_t *a[MT], *sa[MT];
+    bool last[MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
         const uint32_t m = t * 16 + lane % 16 < p.a.rows ? t * 16 + lane % 16 : p.a.rows - 1;
         a[t] = p.a.q + m * p.a.ld;
+        last[t] = m + 1 == p.a.rows;
         sa[t] = p.a.scales + m * p.a.lds;
     }
     f32x4 acc[MT] = {};
@@ -100,10 +111,11 @@ few_rows_kernel(Product p)
         for (; kb < full; kb += kFewWaves) blocks(kb, std::integral_constant<int, 1>());
     if (full < p.blocks && wave == full % kFewWaves) {
         const uint32_t c = full * kBlockK + part;
-        const i32x8 vb = both(sixteen(b, c, p.K), sixteen(b, c + 16, p.K));
+        const bool last_b = n + 1 == p.b.rows;
+        const i32x8 vb = both(sixteen(b, c, p.K, last_b), sixteen(b, c + 16, p.K, last_b));
 #pragma unroll
         for (int t = 0; t < MT; ++t)
-            acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(vb, both(sixteen(a[t], c, p.K), sixteen(a[t], c + 16, p.K)), acc[t], 0, 0, 0,
+            acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(vb, both(sixteen(a[t], c, p.K, last[t]), sixteen(a[t], c + 16, p.K, last[t])), acc[t], 0, 0, 0,
                                                                       (int)sb[full], 0, (int)sa[t][full]);
     }
 #pragma unroll
@@ -122,31 +134,59 @@ few_rows_kernel(Product p)
 }
 
 // ------------------------------------------------------------------------------ tiles
-// A workgroup of four wavefronts has a square tile, a wavefront a quarter of it: WT x WT products of 32 x 32.  In LDS a row of 128 bytes lies in
+// A workgroup has a tile, PM x PN wavefronts side by side in it, each of WM x WN products of 32 x 32.  In LDS a row of 128 bytes lies in
 // eight pieces of 16, piece c of row r at place c ^ key(r): the 16 lanes that read together then meet all banks once.
 __device__ __forceinline__ uint32_t key(uint32_t r) { return (r & 7) ^ (r >> 3 & 1); }
 
-template <int WT>
+// kBuffers blocks of columns are in LDS or on their way.
+template <int WM, int WN, int PM, int PN, int buffers>
 struct Tile {
-    static constexpr uint32_t kRows = 64 * WT;
-    static constexpr uint32_t kBytes = kRows * kBlockK;
+    static constexpr int kWM = WM, kWN = WN;
+    static constexpr uint32_t kWaves = PM * PN, kThreads = 64 * kWaves, kRowsA = 32 * WM * PM, kRowsB = 32 * WN * PN, kPM = PM, kPN = PN, kBuffers = buffers;
+};
+using Large = Tile<4, 4, 2, 2, 2>;      // 256 x 256
+using Middle = Tile<2, 2, 2, 2, 2>;     // 128 x 128
+using Small = Tile<1, 1, 2, 2, 2>;      // 64 x 64
+
+// Whole blocks of columns of a side's rows into LDS.  Loads that write to LDS put lane i's 16 bytes at place i, so lanes choose what they fetch: at one address for
+// the workgroup and 32-bit distances from it (255 rows of less than 2^24 bytes).
+template <uint32_t kRows, uint32_t kWaves>
+struct Stage {
+    static constexpr uint32_t kEach = kRows / 8 / kWaves;
+    const uint8_t *base;
+    uint32_t at[kEach], wave;
+    __device__ __forceinline__ Stage(const Side &s, uint32_t row0) : base(s.q + row0 * s.ld), wave(__builtin_amdgcn_readfirstlane(threadIdx.x / 64))
+    {
+        const uint32_t lane = threadIdx.x % 64, last = s.rows - 1 - row0;
+#pragma unroll
+        for (uint32_t i = 0; i < kEach; ++i) {
+            const uint32_t r = (i * kWaves + wave) * 8 + lane / 8;
+            at[i] = (r < last ? r : last) * (uint32_t)s.ld + ((lane % 8) ^ key(r)) * 16;
+        }
+    }
+    __device__ __forceinline__ void fetch(uint32_t kb, uint8_t *to) const
+    {
+        const uint8_t *from = base + kb * kBlockK;
+#pragma unroll
+        for (uint32_t i = 0; i < kEach; ++i)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)(from + at[i]),
+                                             (__attribute__((address_space(3))) uint32_t *)(to + (i * kWaves + wave) * 8 * kBlockK), 16, 0, 0);
+    }
 };
 
-// One block of columns of a side's rows into LDS.  Loads that write to LDS put lane i's 16 bytes at place i, so lanes choose what they fetch.
-template <int WT>
-__device__ __forceinline__ void stage(const Side &s, uint32_t row0, uint32_t kb, uint32_t K, uint8_t *to)
+// The block in which the rows end
+template <uint32_t kRows, uint32_t kWaves>
+__device__ __forceinline__ void stage_last(const Side &s, uint32_t row0, uint32_t kb, uint32_t K, uint8_t *to)
 {
-    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const bool whole = (kb + 1) * kBlockK <= K;
+    constexpr uint32_t kEach = kRows / 8 / kWaves;
+    u32x4 v[kEach];
 #pragma unroll
-    for (int i = 0; i < 2 * WT; ++i) {
-        const uint32_t first = (i * 4 + wave) * 8, r = first + lane / 8, c = kb * kBlockK + ((lane % 8) ^ key(r)) * 16;
-        const uint8_t *row = s.q + (uint64_t)(row0 + r < s.rows ? row0 + r : s.rows - 1) * s.ld;
-        if (whole)
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)(row + c), (__attribute__((address_space(3))) uint32_t *)(to + first * kBlockK), 16, 0,
-                                             0);
-        else *reinterpret_cast<u32x4 *>(to + first * kBlockK + lane * 16) = sixteen(row, c, K);
+    for (uint32_t e = 0; e < kEach; ++e) {
+        const uint32_t i = e * kWaves * 64 + threadIdx.x, r = i / 8, c = kb * kBlockK + ((i % 8) ^ key(r)) * 16, at = row0 + r < s.rows ? row0 + r : s.rows - 1;
+        v[e] = sixteen(s.q + at * s.ld, c, K, at + 1 == s.rows);
     }
+#pragma unroll
+    for (uint32_t e = 0; e < kEach; ++e) *reinterpret_cast<u32x4 *>(to + (e * kWaves * 64 + threadIdx.x) * 16) = v[e];
 }
 
 // Four blocks' exponents of a row, as many as there are
@@ -159,32 +199,41 @@ __device__ __forceinline__ int exponents(const uint8_t *scales, uint32_t kb, uin
     return (int)e;
 }
 
-template <int WT, int kByte>
-__device__ __forceinline__ void multiply(const uint8_t *la, const uint8_t *lb, uint32_t lane, const int (&ea)[WT], const int (&eb)[WT], f32x16 (&acc)[WT][WT])
-{
+// Operands of half a block of columns, and their products
+template <int WM, int WN>
+struct Half {
+    i32x8 a[WM], b[WN];
+    __device__ __forceinline__ void read(const uint8_t *la, const uint8_t *lb, uint32_t lane, uint32_t half)
+    {
+        const uint32_t k = key(lane % 32), c = 4 * half + lane / 32 * 2;
+        auto operand = [&](const uint8_t *tile, int t) {
+            const uint8_t *row = tile + (t * 32 + lane % 32) * kBlockK;
+            return both(*reinterpret_cast<const u32x4 *>(row + (c ^ k) * 16), *reinterpret_cast<const u32x4 *>(row + ((c + 1) ^ k) * 16));
+        };
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-        i32x8 a[WT], b[WT];
-        const uint32_t c = 4 * s + lane / 32 * 2, k = key(lane % 32);
+        for (int t = 0; t < WN; ++t) b[t] = operand(lb, t);
 #pragma unroll
-        for (int t = 0; t < WT; ++t) {
-            const uint8_t *row = la + (t * 32 + lane % 32) * kBlockK;
-            a[t] = both(*reinterpret_cast<const u32x4 *>(row + (c ^ k) * 16), *reinterpret_cast<const u32x4 *>(row + ((c + 1) ^ k) * 16));
-            row = lb + (t * 32 + lane % 32) * kBlockK;
-            b[t] = both(*reinterpret_cast<const u32x4 *>(row + (c ^ k) * 16), *reinterpret_cast<const u32x4 *>(row + ((c + 1) ^ k) * 16));
-        }
-#pragma unroll
-        for (int i = 0; i < WT; ++i)
-#pragma unroll
-            for (int j = 0; j < WT; ++j)
-                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b[j], a[i], acc[i][j], 0, 0, kByte, eb[j], kByte, ea[i]);
+        for (int t = 0; t < WM; ++t) a[t] = operand(la, t);
     }
-}
+    __device__ __forceinline__ void multiply(const int (&ea)[WM], const int (&eb)[WN], f32x16 (&acc)[WM][WN]) const
+    {
+#pragma unroll
+        for (int i = 0; i < WM; ++i)
+#pragma unroll
+            for (int j = 0; j < WN; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b[j], a[i], acc[i][j], 0, 0, 0, eb[j], 0, ea[i]);
+    }
+};
 
+// Of all wavefronts: reads of LDS, and loads but for the `later` newest (they come in order).  Not __syncthreads(), which would wait for all loads.
+template <uint32_t later>
 __device__ __forceinline__ void loads_done()
 {
-    __builtin_amdgcn_s_waitcnt(0x0f70);         // all loads, those that write to LDS among them
-    __syncthreads();
+    static_assert(later < 64, "as the instruction takes it");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070 | later % 16 | later / 16 << 14);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
 }
 
 __device__ __forceinline__ void wave_fence()
@@ -193,13 +242,15 @@ __device__ __forceinline__ void wave_fence()
     __builtin_amdgcn_wave_barrier();
 }
 
-template <class T, int WT>
-__global__ void __launch_bounds__(256)
+template <class T, class Tile>
+__global__ void __launch_bounds__(Tile::kThreads)
 tile_kernel(Product p)
 {
-    constexpr uint32_t kRows = Tile<WT>::kRows, kBytes = Tile<WT>::kBytes, kHalf = kRows / 2;
-    __shared__ alignas(16) uint8_t lds[2][2][kBytes];
-    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, tiles = p.tiles_m * p.tiles_n;
+    constexpr int WM = Tile::kWM, WN = Tile::kWN;
+    constexpr uint32_t kRowsA = Tile::kRowsA, kRowsB = Tile::kRowsB, kBytes = (kRowsA + kRowsB) * kBlockK;
+    constexpr uint32_t kBuffers = Tile::kBuffers;
+    __shared__ alignas(16) uint8_t lds[kBuffers][kBytes];       // blocks of columns: rows of a, then of b
+    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), tiles = p.tiles_m * p.tiles_n;
     // Workgroups go to the eight chiplets in turn: each gets a run of neighbouring tiles, in columns of eight, so that its cache serves them
     uint32_t id = blockIdx.x;
     const uint32_t all = tiles * p.splits, per = all / 8, more = all % 8, chiplet = id % 8;
@@ -207,62 +258,94 @@ tile_kernel(Product p)
     const uint32_t split = id / tiles;
     id %= tiles;
     const uint32_t column = id / (8 * p.tiles_n), high = p.tiles_m - column * 8 < 8 ? p.tiles_m - column * 8 : 8, within = id % (8 * p.tiles_n);
-    const uint32_t m0 = (column * 8 + within % high) * kRows, n0 = within / high * kRows;
+    const uint32_t m0 = (column * 8 + within % high) * kRowsA, n0 = within / high * kRowsB;
     const uint32_t begin = (uint64_t)p.blocks * split / p.splits, end = (uint64_t)p.blocks * (split + 1) / p.splits;
-    const uint32_t wm = wave / 2 * kHalf, wn = wave % 2 * kHalf;
-    const uint8_t *sa[WT], *sb[WT];
+    const uint32_t wm = wave / Tile::kPN * 32 * WM, wn = wave % Tile::kPN * 32 * WN;
+    const uint8_t *sa[WM], *sb[WN];
 #pragma unroll
-    for (int t = 0; t < WT; ++t) {
-        const uint32_t m = m0 + wm + t * 32 + lane % 32, n = n0 + wn + t * 32 + lane % 32;
+    for (int t = 0; t < WM; ++t) {
+        const uint32_t m = m0 + wm + t * 32 + lane % 32;
         sa[t] = p.a.scales + (uint64_t)(m < p.a.rows ? m : p.a.rows - 1) * p.a.lds;
+    }
+#pragma unroll
+    for (int t = 0; t < WN; ++t) {
+        const uint32_t n = n0 + wn + t * 32 + lane % 32;
         sb[t] = p.b.scales + (uint64_t)(n < p.b.rows ? n : p.b.rows - 1) * p.b.lds;
     }
-    f32x16 acc[WT][WT] = {};
-    int ea[WT], eb[WT], next_a[WT], next_b[WT];
+    f32x16 acc[WM][WN] = {};
+    int ea[WM], eb[WN], next_a[WM], next_b[WN];     // a block's exponents lie in the lowest byte
+    auto fetch_exponents = [&](uint32_t kb) {
 #pragma unroll
-    for (int t = 0; t < WT; ++t) {
-        next_a[t] = exponents(sa[t], begin, end);
-        next_b[t] = exponents(sb[t], begin, end);
-    }
-    if (begin < end) {
-        stage<WT>(p.a, m0, begin, p.K, lds[0][0]);
-        stage<WT>(p.b, n0, begin, p.K, lds[0][1]);
-    }
-    for (uint32_t kb0 = begin; kb0 < end; kb0 += 4) {
+        for (int t = 0; t < WM; ++t) next_a[t] = exponents(sa[t], kb, p.blocks);
 #pragma unroll
-        for (int t = 0; t < WT; ++t) {
-            ea[t] = next_a[t];
-            eb[t] = next_b[t];
+        for (int t = 0; t < WN; ++t) next_b[t] = exponents(sb[t], kb, p.blocks);
+    };
+    const Stage<kRowsA, Tile::kWaves> stage_a(p.a, m0);
+    const Stage<kRowsB, Tile::kWaves> stage_b(p.b, n0);
+    auto fetch = [&](uint32_t kb, uint32_t half) {
+        stage_a.fetch(kb, lds[half]);
+        stage_b.fetch(kb, lds[half] + kRowsA * kBlockK);
+    };
+    const uint32_t whole = end * kBlockK <= p.K ? end : end - 1;       // blocks before this one are whole
+    const uint32_t at_a = wm * kBlockK, at_b = (kRowsA + wn) * kBlockK;
+    constexpr uint32_t kLater = (kBuffers - 2) * (kRowsA + kRowsB) / 8 / Tile::kWaves;      // loads of a wavefront for the blocks behind the next one
+    Half<WM, WN> first, second;
+    // behind the last block: something that is there, and is not used, so that as many loads as ever are on their way
+    auto fetch_ahead = [&](uint32_t kb) { fetch(kb < whole ? kb : whole - 1, (kb - begin) % kBuffers); };
+    if (begin < whole) {
+        fetch_exponents(begin);
+        fetch(begin, 0);
+#pragma unroll
+        for (uint32_t i = 1; i < kBuffers; ++i) fetch_ahead(begin + i);
+        loads_done<kLater + (kRowsA + kRowsB) / 8 / Tile::kWaves>();
+        first.read(lds[0] + at_a, lds[0] + at_b, lane, 0);
+    }
+    // Half a block is multiplied while the next half's operands come from LDS, of the next block too: between the halves a block's operands are all in registers,
+    // so that its place can be loaded again.
+    for (uint32_t kb = begin; kb < whole; ++kb) {
+        const uint32_t i = kb - begin;
+        if (i % 4 == 0) {
+#pragma unroll
+            for (int t = 0; t < WM; ++t) ea[t] = next_a[t];
+#pragma unroll
+            for (int t = 0; t < WN; ++t) eb[t] = next_b[t];
         }
-        auto step = [&](auto byte) {
-            constexpr int i = decltype(byte)::value;
-            const uint32_t kb = kb0 + i;
-            if (kb >= end) return;
-            loads_done();                       // this block has come, and the other half of LDS has been read by all
-            if (kb + 1 < end) {
-                stage<WT>(p.a, m0, kb + 1, p.K, lds[(i + 1) % 2][0]);
-                stage<WT>(p.b, n0, kb + 1, p.K, lds[(i + 1) % 2][1]);
-            }
-            if (i == 0 && kb + 4 < end)
+        second.read(lds[i % kBuffers] + at_a, lds[i % kBuffers] + at_b, lane, 1);
+        first.multiply(ea, eb, acc);
+        __builtin_amdgcn_sched_barrier(0);
+        loads_done<kLater>();
+        if (i % 4 == 0 && kb + 4 < whole) fetch_exponents(kb + 4);
+        fetch_ahead(kb + kBuffers);
+        first.read(lds[(i + 1) % kBuffers] + at_a, lds[(i + 1) % kBuffers] + at_b, lane, 0);
+        second.multiply(ea, eb, acc);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int t = 0; t < WT; ++t) {
-                    next_a[t] = exponents(sa[t], kb + 4, end);
-                    next_b[t] = exponents(sb[t], kb + 4, end);
-                }
-            multiply<WT, i>(lds[i % 2][0] + wm * kBlockK, lds[i % 2][1] + wn * kBlockK, lane, ea, eb, acc);
-        };
-        step(std::integral_constant<int, 0>());
-        step(std::integral_constant<int, 1>());
-        step(std::integral_constant<int, 2>());
-        step(std::integral_constant<int, 3>());
+        for (int t = 0; t < WM; ++t) ea[t] = (int)((uint32_t)ea[t] >> 8);
+#pragma unroll
+        for (int t = 0; t < WN; ++t) eb[t] = (int)((uint32_t)eb[t] >> 8);
+    }
+    if (begin < whole) loads_done<0>();
+    if (whole < end) {
+        stage_last<kRowsA, Tile::kWaves>(p.a, m0, whole, p.K, lds[0]);
+        stage_last<kRowsB, Tile::kWaves>(p.b, n0, whole, p.K, lds[0] + kRowsA * kBlockK);
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < WM; ++t) ea[t] = sa[t][whole];
+#pragma unroll
+        for (int t = 0; t < WN; ++t) eb[t] = sb[t][whole];
+#pragma unroll
+        for (uint32_t h = 0; h < 2; ++h) {
+            first.read(lds[0] + at_a, lds[0] + at_b, lane, h);
+            first.multiply(ea, eb, acc);
+        }
     }
     // Lane l has row l % 32 of a, and of b rows 8 g + 4 (l / 32) to 3 on, g = 0 to 3
     if (p.part) {
         float *part = p.part + (uint64_t)split * p.a.rows * p.b.rows;
 #pragma unroll
-        for (int i = 0; i < WT; ++i)
+        for (int i = 0; i < WM; ++i)
 #pragma unroll
-            for (int j = 0; j < WT; ++j)
+            for (int j = 0; j < WN; ++j)
 #pragma unroll
                 for (int g = 0; g < 16; ++g) {
                     const uint32_t m = m0 + wm + i * 32 + lane % 32, n = n0 + wn + j * 32 + g / 4 * 8 + lane / 32 * 4 + g % 4;
@@ -271,35 +354,35 @@ tile_kernel(Product p)
         return;
     }
     // 32 rows at a time through LDS, so that a row's stores lie next to each other
-    constexpr uint32_t kStride = WT * 32 + 8;
+    constexpr uint32_t kStride = WN * 32 + 8;
     __syncthreads();
-    T *mine = reinterpret_cast<T *>(&lds[0][0][0]) + wave * 32 * kStride;
-    static_assert(4 * 32 * kStride * sizeof(T) <= sizeof(lds), "room for the results");
+    T *mine = reinterpret_cast<T *>(&lds[0][0]) + wave * 32 * kStride;
+    static_assert(Tile::kWaves * 32 * kStride * sizeof(T) <= sizeof(lds), "room for the results");
     const bool vectors = p.b.rows % 8 == 0 && p.ldy % 8 == 0 && reinterpret_cast<uintptr_t>(p.y) % 16 == 0;
 #pragma unroll
-    for (int i = 0; i < WT; ++i) {
+    for (int i = 0; i < WM; ++i) {
         wave_fence();
 #pragma unroll
-        for (int j = 0; j < WT; ++j)
+        for (int j = 0; j < WN; ++j)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const float v[4] = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
                 dg_rows::store<T, 4>(mine + lane % 32 * kStride + j * 32 + g * 8 + lane / 32 * 4, v);
             }
         wave_fence();
-        constexpr uint32_t kVectors = WT * 4;       // of a row
+        if (vectors) {
+            constexpr uint32_t kVectors = WN * 4;       // of a row
 #pragma unroll
-        for (uint32_t e = 0; e < 32 * kVectors; e += 64) {
-            const uint32_t r = (e + lane) / kVectors, c = (e + lane) % kVectors * 8, m = m0 + wm + i * 32 + r, n = n0 + wn + c;
-            if (m >= p.a.rows || n >= p.b.rows) continue;
-            const dg_rows::Pack<T, 8> v = *reinterpret_cast<const dg_rows::Pack<T, 8> *>(mine + r * kStride + c);
-            T *to = (T *)p.y + m * p.ldy + n;
-            if (vectors) *reinterpret_cast<dg_rows::Pack<T, 8> *>(to) = v;
-            else
-#pragma unroll
-                for (int x = 0; x < 8; ++x)
-                    if (n + x < p.b.rows) to[x] = v.v[x];
-        }
+            for (uint32_t e = 0; e < 32 * kVectors; e += 64) {
+                const uint32_t r = (e + lane) / kVectors, c = (e + lane) % kVectors * 8, m = m0 + wm + i * 32 + r, n = n0 + wn + c;
+                if (m < p.a.rows && n < p.b.rows) *reinterpret_cast<dg_rows::Pack<T, 8> *>((T *)p.y + m * p.ldy + n) = *reinterpret_cast<const dg_rows::Pack<T, 8> *>(mine + r * kStride + c);
+            }
+        } else
+#pragma unroll 8
+            for (uint32_t e = 0; e < 32 * 32 * WN; e += 64) {
+                const uint32_t r = (e + lane) / (32 * WN), c = (e + lane) % (32 * WN), m = m0 + wm + i * 32 + r, n = n0 + wn + c;
+                if (m < p.a.rows && n < p.b.rows) ((T *)p.y)[m * p.ldy + n] = mine[r * kStride + c];
+            }
     }
 }
 
@@ -344,9 +427,9 @@ void launch(const Product &p, const Plan &plan, hipStream_t st)
         return;
     }
     const uint32_t grid = plan.tiles_m * plan.tiles_n * plan.splits;
-    if (plan.tile == 256) tile_kernel<T, 4><<<grid, 256, 0, st>>>(p);
-    else if (plan.tile == 128) tile_kernel<T, 2><<<grid, 256, 0, st>>>(p);
-    else tile_kernel<T, 1><<<grid, 256, 0, st>>>(p);
+    if (plan.tile == 256) tile_kernel<T, Large><<<grid, Large::kThreads, 0, st>>>(p);
+    else if (plan.tile == 128) tile_kernel<T, Middle><<<grid, Middle::kThreads, 0, st>>>(p);
+    else tile_kernel<T, Small><<<grid, Small::kThreads, 0, st>>>(p);
     if (p.part) {
         const uint64_t blocks = ((uint64_t)p.a.rows * p.b.rows + 255) / 256;
         join_kernel<T><<<(uint32_t)(blocks < 4096 ? blocks : 4096), 256, 0, st>>>(p);
@@ -356,11 +439,12 @@ void launch(const Product &p, const Plan &plan, hipStream_t st)
 int check_side(const char *who, const char *name, const Side &s, uint32_t K, uint32_t blocks)
 {
     DG_REQUIRE(s.q && s.scales && dg::aligned(s.q, 16) && s.ld % 16 == 0, DG_ERR_ARG, "%s: null pointer, or rows of %s that do not begin at multiples of 16 bytes", who, name);
-    DG_REQUIRE(s.ld >= K && s.lds >= blocks && s.ld <= 1ull << 40 && s.lds <= 1ull << 40, DG_ERR_ARG, "%s: rows of %s overlap", who, name);
+    DG_REQUIRE(s.ld >= K && s.lds >= blocks && s.lds <= 1ull << 40, DG_ERR_ARG, "%s: rows of %s overlap", who, name);
+    DG_REQUIRE(s.ld < 1ull << 24, DG_ERR_UNSUPPORTED, "%s: rows of %s 2^24 values or more apart", who, name);
     return DG_OK;
 }
 
-bool in_range(uint64_t M, uint64_t N, uint32_t K) { return M <= 1ull << 24 && N <= 1ull << 24 && M * N <= 1ull << 40 && K >= 1 && K <= 1u << 24; }
+bool in_range(uint64_t M, uint64_t N, uint32_t K) { return M <= 1ull << 24 && N <= 1ull << 24 && M * N <= 1ull << 40 && K >= 1 && K < 1u << 24; }
 
 }  // namespace
 
