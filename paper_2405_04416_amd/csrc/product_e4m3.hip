@@ -399,7 +399,10 @@ join_kernel(Product p)
 }
 
 // ------------------------------------------------------------------------------ launch
-constexpr uint32_t kFew = 64;           // rows of a up to which b's bytes are what counts
+// Rows of a up to which b's bytes are what counts, and up to which a launch of their own for sums of split columns costs more than that a's rows come from the caches for
+// every 16 of b.  Few rows / tiles in us: 64 x 1024 x 1024 8.6 / 11.7, 24 x 4096 x 1024 8.7 / 11.4, 40 x 4096 x 4096 13.7 / 13.2, 32 x 8192 x 4096 18.3 / 13.7,
+// 64 x 8192 x 4096 29.3 / 17.4.
+constexpr uint32_t kFew = 16, kFewShort = 64, kShort = 2048;
 
 struct Plan { uint32_t tile, tiles_m, tiles_n, splits; };      // tile 0: few rows
 
@@ -407,7 +410,7 @@ struct Plan { uint32_t tile, tiles_m, tiles_n, splits; };      // tile 0: few ro
 Plan plan_of(uint32_t M, uint32_t N, uint32_t K)
 {
     const uint32_t blocks = (K + kBlockK - 1) / kBlockK;
-    if (M <= kFew) return {0, 0, 0, 1};
+    if (M <= kFew || (M <= kFewShort && K <= kShort)) return {0, 0, 0, 1};
     uint32_t tile = 256;
     while (tile > 64 && (uint64_t)((M + tile - 1) / tile) * ((N + tile - 1) / tile) < 256) tile /= 2;
     const uint32_t tm = (M + tile - 1) / tile, tn = (N + tile - 1) / tile;
