@@ -623,7 +623,7 @@ int dg_e4m3_rows(const void *x, uint64_t ldx, uint64_t N, uint32_t W, uint32_t d
  * are not there are not read.  y must not overlap an input.
  * ws: dg_e4m3_product_workspace_bytes(M, N, K) bytes (NULL where that is 0), 16-byte aligned.
  * Errors: DG_ERR_ARG for K == 0, sides that are not 16-byte aligned or whose ld is no multiple of 16, another dtype;
- * DG_ERR_UNSUPPORTED for more than 2^24 rows or columns, rows 2^24 values or more apart, or more than 2^40 results. */
+ * DG_ERR_UNSUPPORTED for more than 2^24 rows or columns, rows 2^24 values or more apart, or more than 2^39 results. */
 size_t dg_e4m3_product_workspace_bytes(uint64_t M, uint64_t N, uint32_t K);
 int dg_e4m3_product(const void *a, uint64_t lda, const uint8_t *a_scales, uint64_t ldsa, const void *b, uint64_t ldb,
                     const uint8_t *b_scales, uint64_t ldsb, uint64_t M, uint64_t N, uint32_t K, uint32_t dtype,

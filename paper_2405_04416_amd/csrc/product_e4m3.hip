@@ -447,7 +447,8 @@ int check_side(const char *who, const char *name, const Side &s, uint32_t K, uin
     return DG_OK;
 }
 
-bool in_range(uint64_t M, uint64_t N, uint32_t K) { return M <= 1ull << 24 && N <= 1ull << 24 && M * N <= 1ull << 40 && K >= 1 && K < 1u << 24; }
+// 2^39 results are 2^23 tiles of 256 lanes: a launch has fewer than 2^32 lanes.
+bool in_range(uint64_t M, uint64_t N, uint32_t K) { return M <= 1ull << 24 && N <= 1ull << 24 && M * N <= 1ull << 39 && K >= 1 && K < 1u << 24; }
 
 }  // namespace
 
@@ -464,7 +465,7 @@ extern "C" int dg_e4m3_product(const void *a, uint64_t lda, const uint8_t *a_sca
     const char *who = "dg_e4m3_product";
     DG_REQUIRE(dtype == DG_F16 || dtype == DG_BF16, DG_ERR_ARG, "%s: the result is fp16 or bf16", who);
     DG_REQUIRE(K >= 1, DG_ERR_ARG, "%s: K must be positive", who);
-    DG_REQUIRE(in_range(M, N, K), DG_ERR_UNSUPPORTED, "%s: more than 2^24 rows or columns, or 2^40 results", who);
+    DG_REQUIRE(in_range(M, N, K), DG_ERR_UNSUPPORTED, "%s: more than 2^24 rows or columns, or 2^39 results", who);
     if (M == 0 || N == 0) return DG_OK;
     const uint32_t blocks = (K + kBlockK - 1) / kBlockK;
     Product p = {};
