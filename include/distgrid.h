@@ -618,8 +618,8 @@ int dg_rms_norm_e4m3_fwd(const void *x, uint64_t ldx, const void *residual, uint
 int dg_e4m3_rows(const void *x, uint64_t ldx, uint64_t N, uint32_t W, uint32_t dtype, void *q, uint64_t ldq,
                  uint8_t *scales, uint64_t lds, void *stream);
 /* Product of rows in 8 bits: y[m, n] = sum over k of a[m, k] b[n, k], what they stand for; a [M, K], b [N, K] (a projection's
- * weights, a row for each output), scales [M or N, ceil(K / 128)].  y [M, N] of type dtype, DG_F16 or DG_BF16: the matrix instruction
- * aligns a sum's terms to the largest, so that sums are off by some 1e-5 of it, which fp32 would show.  Columns from K on and rows that
+ * weights, a row for each output), scales [M or N, ceil(K / 128)].  y [M, N] of type dtype, DG_F16 or DG_BF16: of eight neighbouring
+ * products the matrix instruction cuts off what is below 2^-13 of the largest, so that sums are off by some 1e-5, which fp32 would show.  Columns from K on and rows that
  * are not there are not read.  y must not overlap an input.
  * ws: dg_e4m3_product_workspace_bytes(M, N, K) bytes (NULL where that is 0), 16-byte aligned.
  * Errors: DG_ERR_ARG for K == 0, sides that are not 16-byte aligned or whose ld is no multiple of 16, another dtype;
@@ -632,7 +632,7 @@ int dg_e4m3_product(const void *a, uint64_t lda, const uint8_t *a_scales, uint64
 /* Gated delta rule: H heads, each with a memory S [Dk, Dv], along n_seq sequences of rows, N rows in all.  For a token
  *   S <- e^g S;   S <- S + beta k (v - S^T k)^T;   o = scale S^T q,      S before the first token: s0, or 0 if NULL.
  * q, k [N, Hk Dk], v, o [N, H Dv], heads next to each other in a row; H is a multiple of Hk, head h takes key head h / (H / Hk).
- * g (logarithm of the decay, <= 0; -infinity, and anything below -104, forgets all) and beta (rate) [N, H] fp32, rows ldg and ldbeta apart.
+ * g (logarithm of the decay, <= 0; -infinity, and anything below -104, forgets all that is finite) and beta (rate) [N, H] fp32, rows ldg and ldbeta apart.
  * s0, s_last [n_seq, H, Dk, Dv] fp32, either may be NULL; s_last receives the memories after the last tokens (s0 for a sequence without
  * one) and may be s0, unless a backward pass is to follow.  Keys of length one (dg_rms_norm_fwd over rows of Dk with gamma = Dk^-1/2) and rates up to 1 keep memories bounded.
  * first, reverse: as for dg_recurrence_fwd.  One token per sequence (N == n_seq), or a few, is the step of a program that gets its tokens one after the other.

@@ -491,3 +491,56 @@ def dropout_mask(seed, offset, n, p):
     f.restype = C.c_double
     factor = f(C.c_uint64(seed), C.c_uint64(offset), C.c_uint64(n), C.c_double(p), _p(keep))
     return keep.astype(bool), factor
+
+
+# ------------------------------------------------------------------ root-mean-square norm, rows in 8 bits, gated delta rule
+def rms_norm_fwd(x, gamma, eps):
+    x, gamma = _f64(x), _f64(gamma)
+    y = np.zeros_like(x)
+    lib().dgo_rms_norm_fwd(_p(x), _p(gamma), C.c_uint64(x.shape[0]), C.c_uint32(x.shape[1]), C.c_double(eps), _p(y))
+    return y
+
+
+def rms_norm_bwd(x, gamma, dy, eps):
+    """(dx, dgamma)"""
+    x, gamma, dy = _f64(x), _f64(gamma), _f64(dy)
+    dx, dgamma = np.zeros_like(x), np.zeros(x.shape[1])
+    lib().dgo_rms_norm_bwd(_p(x), _p(gamma), _p(dy), C.c_uint64(x.shape[0]), C.c_uint32(x.shape[1]), C.c_double(eps), _p(dx), _p(dgamma))
+    return dx, dgamma
+
+
+def e4m3_rows(x):
+    """(q, the values of 8 bits; scales, the bytes [N, ceil(W / 128)])"""
+    x = _f64(x)
+    q, scales = np.zeros_like(x), np.zeros((x.shape[0], -(-x.shape[1] // 128)), np.uint8)
+    lib().dgo_e4m3_rows(_p(x), C.c_uint64(x.shape[0]), C.c_uint32(x.shape[1]), _p(q), _p(scales))
+    return q, scales
+
+
+def _delta(q, k, v, g, beta, first, s0):
+    """64-bit arrays q, k [N, Hk, Dk], v [N, H, Dv], and the sizes"""
+    q, k, v, g, beta, s0, first = _f64(q), _f64(k), _f64(v), _f64(g), _f64(beta), _f64(s0), _arr(first, np.uint32)
+    (_, Hk, Dk), (_, H, Dv) = q.shape, v.shape
+    return q, k, v, g, beta, first, s0, (Hk, H, Dk, Dv)
+
+
+def delta_rule_fwd(q, k, v, g, beta, first, scale=1.0, reverse=False, s0=None):
+    """q, k [N, Hk, Dk], v [N, H, Dv], g, beta [N, H] -> (o, s_last [n_seq, H, Dk, Dv]); rows of no sequence are NaN."""
+    q, k, v, g, beta, first, s0, (Hk, H, Dk, Dv) = _delta(q, k, v, g, beta, first, s0)
+    o, s_last = np.full_like(v, np.nan), np.zeros((first.size - 1, H, Dk, Dv))
+    u = C.c_uint32
+    lib().dgo_delta_rule_fwd(_p(q), _p(k), _p(v), _p(g), _p(beta), u(first.size - 1), _p(first), u(Hk), u(H), u(Dk), u(Dv), C.c_int(reverse), C.c_double(scale), _p(s0),
+                             _p(o), _p(s_last))
+    return o, s_last
+
+
+def delta_rule_bwd(q, k, v, g, beta, first, do, scale=1.0, reverse=False, s0=None, ds_last=None):
+    """(dq, dk, dv, dg, dbeta, ds0); rows of no sequence are 0 in dq, dk, NaN in the others."""
+    q, k, v, g, beta, first, s0, (Hk, H, Dk, Dv) = _delta(q, k, v, g, beta, first, s0)
+    do, ds_last = _f64(do), _f64(ds_last)
+    dq, dk, dv, dg, dbeta = np.zeros_like(q), np.zeros_like(k), np.full_like(v, np.nan), np.full_like(g, np.nan), np.full_like(g, np.nan)
+    ds0 = np.zeros((first.size - 1, H, Dk, Dv))
+    u = C.c_uint32
+    lib().dgo_delta_rule_bwd(_p(q), _p(k), _p(v), _p(g), _p(beta), u(first.size - 1), _p(first), u(Hk), u(H), u(Dk), u(Dv), C.c_int(reverse), C.c_double(scale), _p(s0),
+                             _p(do), _p(ds_last), _p(dq), _p(dk), _p(dv), _p(dg), _p(dbeta), _p(ds0))
+    return dq, dk, dv, dg, dbeta, ds0

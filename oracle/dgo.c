@@ -925,3 +925,152 @@ double dgo_dropout_mask(uint64_t seed, uint64_t offset, uint64_t n, double p, ui
     for (uint64_t i = 0; i < n; ++i) keep[i] = ((dgo_rand64(seed, offset + i / 4) >> (16 * (i % 4))) & 0xffffu) >= below;
     return below == 65536u ? 0.0 : 65536.0 / (65536u - below);
 }
+
+/* ------------------------------------------------------------------ */
+/* Root-mean-square norm, rows in 8 bits, gated delta rule             */
+/* ------------------------------------------------------------------ */
+
+static double row_size(const double *x, uint32_t W, double eps)
+{
+    double s = 0.0;
+    for (uint32_t c = 0; c < W; ++c) s += x[c] * x[c];
+    return sqrt(s / W + eps);
+}
+
+void dgo_rms_norm_fwd(const double *x, const double *gamma, uint64_t N, uint32_t W, double eps, double *y)
+{
+    for (uint64_t r = 0; r < N; ++r, x += W, y += W) {
+        double d = row_size(x, W, eps);
+        for (uint32_t c = 0; c < W; ++c) y[c] = x[c] / d * (gamma ? gamma[c] : 1.0);
+    }
+}
+
+void dgo_rms_norm_bwd(const double *x, const double *gamma, const double *dy, uint64_t N, uint32_t W, double eps, double *dx, double *dgamma)
+{
+    for (uint32_t c = 0; c < W; ++c) dgamma[c] = 0.0;
+    for (uint64_t r = 0; r < N; ++r, x += W, dy += W, dx += W) {
+        double d = row_size(x, W, eps);
+        for (uint32_t c = 0; c < W; ++c) dgamma[c] += dy[c] * x[c] / d;
+        /* d (x_i / d) / d x_c = delta_ic / d - x_i x_c / (W d^3) */
+        for (uint32_t c = 0; c < W; ++c) {
+            double sum = 0.0;
+            for (uint32_t i = 0; i < W; ++i) sum += dy[i] * (gamma ? gamma[i] : 1.0) * ((i == c) / d - x[i] * x[c] / (W * d * d * d));
+            dx[c] = sum;
+        }
+    }
+}
+
+void dgo_e4m3_rows(const double *x, uint64_t N, uint32_t W, double *q, uint8_t *scales)
+{
+    for (uint64_t r = 0; r < N; ++r, x += W, q += W)
+        for (uint32_t c0 = 0; c0 < W; c0 += 128) {
+            uint32_t c1 = c0 + 128 < W ? c0 + 128 : W;
+            double most = 0.0;
+            int e = -127;
+            for (uint32_t c = c0; c < c1; ++c)
+                if (isfinite(x[c]) && fabs(x[c]) > most) most = fabs(x[c]);
+            while (most > ldexp(448.0, e)) ++e;
+            *scales++ = (uint8_t)(e + 127);
+            for (uint32_t c = c0; c < c1; ++c) {
+                double v = ldexp(x[c], -e);
+                int order;
+                if (!isfinite(v)) {
+                    q[c] = NAN;
+                    continue;
+                }
+                frexp(v, &order);                       /* |v| in [2^(order - 1), 2^order) */
+                if (v == 0.0 || order < -5) order = -5;
+                q[c] = ldexp(nearbyint(ldexp(v, 4 - order)), order - 4);
+            }
+        }
+}
+
+static double kept(double g) { return g < -104.0 ? 0.0 : exp(g); }
+
+/* One token: S to what it is after it, y = v - e^g S^T k */
+static void delta_token(double *S, const double *k, const double *v, double a, double beta, uint32_t Dk, uint32_t Dv, double *y)
+{
+    for (uint32_t c = 0; c < Dv; ++c) y[c] = v[c];
+    for (uint32_t r = 0; r < Dk; ++r)
+        for (uint32_t c = 0; c < Dv; ++c) {
+            S[r * Dv + c] = a == 0.0 ? 0.0 : a * S[r * Dv + c];
+            y[c] -= S[r * Dv + c] * k[r];
+        }
+    for (uint32_t r = 0; r < Dk; ++r)
+        for (uint32_t c = 0; c < Dv; ++c) S[r * Dv + c] += beta * k[r] * y[c];
+}
+
+void dgo_delta_rule_fwd(const double *q, const double *k, const double *v, const double *g, const double *beta, uint32_t n_seq, const uint32_t *first,
+                        uint32_t Hk, uint32_t H, uint32_t Dk, uint32_t Dv, int reverse, double scale, const double *s0, double *o, double *s_last)
+{
+    double *y = malloc(Dv * sizeof *y);
+    for (uint32_t j = 0; j < n_seq; ++j)
+        for (uint32_t h = 0; h < H; ++h) {
+            const uint64_t memory = ((uint64_t)j * H + h) * Dk * Dv;
+            double *S = s_last + memory;
+            for (uint32_t i = 0; i < Dk * Dv; ++i) S[i] = s0 ? s0[memory + i] : 0.0;
+            for (uint32_t n = 0; n < first[j + 1] - first[j]; ++n) {
+                const uint64_t i = reverse ? first[j + 1] - 1 - n : first[j] + n, key = (i * Hk + h / (H / Hk)) * Dk;
+                delta_token(S, k + key, v + (i * H + h) * Dv, kept(g[i * H + h]), beta[i * H + h], Dk, Dv, y);
+                for (uint32_t c = 0; c < Dv; ++c) {
+                    double sum = 0.0;
+                    for (uint32_t r = 0; r < Dk; ++r) sum += S[r * Dv + c] * q[key + r];
+                    o[(i * H + h) * Dv + c] = scale * sum;
+                }
+            }
+        }
+    free(y);
+}
+
+void dgo_delta_rule_bwd(const double *q, const double *k, const double *v, const double *g, const double *beta, uint32_t n_seq, const uint32_t *first,
+                        uint32_t Hk, uint32_t H, uint32_t Dk, uint32_t Dv, int reverse, double scale, const double *s0, const double *dout,
+                        const double *ds_last, double *dq, double *dk, double *dv, double *dg, double *dbeta, double *ds0)
+{
+    const uint64_t D = (uint64_t)Dk * Dv;
+    double *dS = malloc(D * sizeof *dS);
+    for (uint32_t j = 0; j < n_seq; ++j)
+        for (uint32_t h = 0; h < H; ++h) {
+            const uint64_t memory = ((uint64_t)j * H + h) * D;
+            const uint32_t len = first[j + 1] - first[j];
+            /* the memories before all tokens and after the last, and what tokens miss */
+            double *all = malloc((len + 1) * D * sizeof *all), *y = malloc(((uint64_t)len * Dv + 1) * sizeof *y);
+            for (uint64_t i = 0; i < D; ++i) {
+                all[i] = s0 ? s0[memory + i] : 0.0;
+                dS[i] = ds_last ? ds_last[memory + i] : 0.0;
+            }
+            for (uint32_t n = 0; n < len; ++n) {
+                const uint64_t i = reverse ? first[j + 1] - 1 - n : first[j] + n, key = (i * Hk + h / (H / Hk)) * Dk;
+                memcpy(all + (n + 1) * D, all + n * D, D * sizeof *all);
+                delta_token(all + (n + 1) * D, k + key, v + (i * H + h) * Dv, kept(g[i * H + h]), beta[i * H + h], Dk, Dv, y + (uint64_t)n * Dv);
+            }
+            for (uint32_t n = len; n-- > 0;) {
+                const uint64_t i = reverse ? first[j + 1] - 1 - n : first[j] + n, key = (i * Hk + h / (H / Hk)) * Dk, value = (i * H + h) * Dv;
+                const double a = kept(g[i * H + h]), b = beta[i * H + h], *before = all + n * D, *S = before + D, *miss = y + (uint64_t)n * Dv;
+                double rate = 0.0, decay = 0.0;
+                for (uint32_t c = 0; c < Dv; ++c) {
+                    double sum = 0.0;
+                    for (uint32_t r = 0; r < Dk; ++r) {
+                        dq[key + r] += scale * S[r * Dv + c] * dout[value + c];
+                        dS[r * Dv + c] += scale * q[key + r] * dout[value + c];
+                        sum += dS[r * Dv + c] * k[key + r];
+                    }
+                    rate += sum * miss[c];
+                    dv[value + c] = b * sum;
+                }
+                for (uint32_t r = 0; r < Dk; ++r)
+                    for (uint32_t c = 0; c < Dv; ++c) {
+                        const double was = a == 0.0 ? 0.0 : a * before[r * Dv + c];
+                        dk[key + r] += b * dS[r * Dv + c] * miss[c] - was * dv[value + c];
+                        dS[r * Dv + c] -= k[key + r] * dv[value + c];
+                        decay += dS[r * Dv + c] * was;
+                        dS[r * Dv + c] = a == 0.0 ? 0.0 : a * dS[r * Dv + c];
+                    }
+                dbeta[i * H + h] = rate;
+                dg[i * H + h] = decay;
+            }
+            memcpy(ds0 + memory, dS, D * sizeof *dS);
+            free(all);
+            free(y);
+        }
+    free(dS);
+}

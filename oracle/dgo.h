@@ -209,6 +209,25 @@ void dgo_recurrence_bwd(const double *z, const double *u, uint32_t n_seq, const 
  * floor(65536 p + 1/2); returns the factor of the kept ones */
 double dgo_dropout_mask(uint64_t seed, uint64_t offset, uint64_t n, double p, uint8_t *keep);
 
+/* ------------------------------------------------------------------------------------------------
+ * Block with an associative memory: root-mean-square norm, rows in 8 bits, gated delta rule.
+ * ---------------------------------------------------------------------------------------------- */
+/* y = x / sqrt(mean(x^2) + eps) * gamma, row by row; gamma may be NULL */
+void dgo_rms_norm_fwd(const double *x, const double *gamma, uint64_t N, uint32_t W, double eps, double *y);
+/* gradients of sum(dy * y); the Jacobian of a row is applied as it stands, W x W */
+void dgo_rms_norm_bwd(const double *x, const double *gamma, const double *dy, uint64_t N, uint32_t W, double eps, double *dx, double *dgamma);
+/* x stands for q 2^(scales - 127), a scale for each 128 columns: the smallest one, from 2^-127 on, with which finite values are within 448; q: values
+ * of three bits behind the leading one, exponents from -6 on, to the nearest even; what is not finite is NaN */
+void dgo_e4m3_rows(const double *x, uint64_t N, uint32_t W, double *q, uint8_t *scales);
+/* S <- e^g S;  S <- S + beta k (v - S^T k)^T;  o = scale S^T q along rows [first[j], first[j+1]) of sequence j, or from the last to the first (reverse); e^g is 0
+ * for g < -104.  q, k [N][Hk][Dk], v, o [N][H][Dv], g, beta [N][H], s0, s_last [n_seq][H][Dk][Dv]; s0 may be NULL.  Rows of no sequence are left alone. */
+void dgo_delta_rule_fwd(const double *q, const double *k, const double *v, const double *g, const double *beta, uint32_t n_seq, const uint32_t *first,
+                        uint32_t Hk, uint32_t H, uint32_t Dk, uint32_t Dv, int reverse, double scale, const double *s0, double *o, double *s_last);
+/* gradients of sum(dout * o) + sum(ds_last * s_last); ds_last may be NULL.  dq, dk are added to. */
+void dgo_delta_rule_bwd(const double *q, const double *k, const double *v, const double *g, const double *beta, uint32_t n_seq, const uint32_t *first,
+                        uint32_t Hk, uint32_t H, uint32_t Dk, uint32_t Dv, int reverse, double scale, const double *s0, const double *dout,
+                        const double *ds_last, double *dq, double *dk, double *dv, double *dg, double *dbeta, double *ds0);
+
 #ifdef __cplusplus
 }
 #endif

@@ -26,6 +26,7 @@ constexpr int kMaxD = 128;
 constexpr uint64_t kMostLaunched = 1 << 22;     // workgroups of a launch: its lanes have to stay below 2^32
 // e^-104 is 0 in fp32: below that a gate is shut.  Logarithms are cut off here so that their differences stay numbers.
 constexpr float kShut = -200.0f;
+__device__ __forceinline__ float cut_off(float g) { return g < kShut ? kShut : g; }     // NaN stays NaN
 
 struct Weights;
 

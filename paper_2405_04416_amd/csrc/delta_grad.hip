@@ -209,7 +209,7 @@ delta_grad_kernel(Delta d, uint64_t from)
             const bool held = lane < count;
             const uint64_t r = row_of(lane);
             const float value = d.g[r * d.ldg + head], b = d.beta[r * d.ldb + head];
-            double G = held ? (double)fmaxf(value, kShut) : 0.0;
+            double G = held ? (double)cut_off(value) : 0.0;
 #pragma unroll
             for (int s = 1; s < 64; s *= 2) {
                 const double before = __shfl_up(G, s);

@@ -82,7 +82,7 @@ delta_weights_kernel(Delta d, uint64_t from)
     const T *keys = (const T *)d.k + hk * d.Dk, *queries = (const T *)d.q + hk * d.Dk;
     const Block<T, KS, kVec> k0(keys, d.ldk, span, t0, c16, r4 * 2, d.Dk), k1(keys, d.ldk, span, t0, 16 + c16, r4 * 2, d.Dk);
     const float beta = held ? rate : 0.0f;
-    double sum = held ? (double)fmaxf(gate, kShut) : 0.0;
+    double sum = held ? (double)cut_off(gate) : 0.0;
 #pragma unroll
     for (int s = 1; s < kChunk; s *= 2) {
         const double before = __shfl_up(sum, s, kChunk);
