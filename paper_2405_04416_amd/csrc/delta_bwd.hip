@@ -9,7 +9,7 @@ using namespace dg_delta;
 
 // A chunk for a wavefront with 16 columns of the gradient, S.  dout: that of o of the lane's eight tokens; gradient: that of what they write.
 template <class T, int KS>
-__device__ __forceinline__ void take_chunk(const Operands<T, KS, true> &o, uint32_t c16, uint32_t r8, const float (&dout)[8], f32x4 (&S)[2 * KS], float (&gradient)[8])
+__device__ __forceinline__ void take_chunk(const Operands<T, KS> &o, uint32_t c16, uint32_t r8, const float (&dout)[8], f32x4 (&S)[2 * KS], float (&gradient)[8])
 {
     constexpr int n = Pieces<T>::n, kTiles = 2 * KS;
     bf16x8 keys[KS][2][n], inverse[2][3], pull[2][3];
@@ -34,8 +34,8 @@ __device__ __forceinline__ void take_chunk(const Operands<T, KS, true> &o, uint3
     bf16x8 turned[kTiles][n], queries[kTiles][n];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-        lefts(o.key.KT, t * 16 + c16, r8, turned[t]);
-        lefts(o.key.Q, t * 16 + c16, r8, queries[t]);
+        lefts_turned(o.key.K, t / 2, t % 2, c16 + r8 * 2, turned[t]);
+        lefts_turned(o.key.Q, t / 2, t % 2, c16 + r8 * 2, queries[t]);
     }
     __builtin_amdgcn_sched_barrier(0);
     bf16x8 exact[n], right[3], right_q[3];
@@ -67,77 +67,180 @@ __device__ __forceinline__ void take_chunk(const Operands<T, KS, true> &o, uint3
     }
 }
 
-template <class T, int KS, bool kHelped>
-struct Lds { using type = Room<T, KS, true>; };
+// The same shared by KS wavefronts, rows 32 wave on each.
 template <class T, int KS>
-struct Lds<T, KS, true> { using type = Helped<T, KS, true>; };
+struct Share {
+    static constexpr int n = Pieces<T>::n;
+    f32x4 S[2];
+    bf16x8 inverse[2][3], turned[2][n], queries[2][n];
+    f32x4 read[2], until[2];
+    float whole;
 
-template <class T, int KS, bool kHelped, bool kVec>
+    // up to the sum K S; all that comes after it is read meanwhile
+    __device__ __forceinline__ void before(const Operands<T, KS> &o, Shares<KS, true> &to, uint32_t wave, uint32_t lane)
+    {
+        const uint32_t c16 = lane % 16, r8 = lane / 16 * 8;
+        bf16x8 keys[2][n], sp[3];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) lefts(o.key.K, h * 16 + c16, wave * 32 + r8, keys[h]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            until[h] = *reinterpret_cast<const f32x4 *>(&o.weight.until[r8 + h * 4]);
+            lefts(o.weight.inverse, h * 16 + c16, r8, inverse[h]);
+            read[h] = *reinterpret_cast<const f32x4 *>(&o.weight.read[r8 + h * 4]);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            lefts_turned(o.key.Q, wave, h, lane, queries[h]);
+            lefts_turned(o.key.K, wave, h, lane, turned[h]);
+        }
+        whole = o.weight.whole;
+        __builtin_amdgcn_sched_barrier(0);
+        split_rows<3>(S[0], S[1], sp);
+        f32x4 sum[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) sum[h] = multiply<n, 3>(keys[h], sp, (f32x4){});
+#pragma unroll
+        for (int h = 0; h < 2; ++h) to.keys[wave][h][lane] = sum[h];
+    }
+
+    __device__ __forceinline__ void after(Shares<KS, true> &shares, uint32_t parity, uint32_t wave, uint32_t lane)
+    {
+        f32x4 du[2], dr[2], back[2];
+        bf16x8 right[3], queried[3];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) du[h] = shares.ahead[h][lane] + until[h] * shares.sum(shares.keys, h, lane);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) queried[p] = operand(shares.queried[p][lane]);
+        split_rows<3>(du[0], du[1], right);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) dr[h] = multiply<3, 3>(inverse[h], right, (f32x4){});
+#pragma unroll
+        for (int h = 0; h < 2; ++h) S[h] = multiply<n, 3>(queries[h], queried, S[h] * whole);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) back[h] = -dr[h] * read[h];
+        split_rows<3>(back[0], back[1], right);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) S[h] = multiply<n, 3>(turned[h], right, S[h]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (wave == h % KS) shares.left[parity][h][lane] = dr[h];
+    }
+};
+
+// what does not wait for S: one wavefront makes P^T dO, the other scale e^G dO in pieces
+template <class T, int KS>
+__device__ __forceinline__ void make_ahead(const Operands<T, KS> &o, const Tile<T> &tile, Shares<KS, true> &to, uint32_t which, uint32_t lane)
+{
+    constexpr int n = Pieces<T>::n;
+    const uint32_t c16 = lane % 16, r8 = lane / 16 * 8;
+    float dout[8];
+    tile.read(lane, dout);
+    if (which == 0) {
+        bf16x8 pull[2][3], exact[n];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) lefts(o.weight.P, h * 16 + c16, r8, pull[h]);
+        split8<n>(dout, exact);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) to.ahead[h][lane] = multiply<3, n>(pull[h], exact, (f32x4){});
+    } else {
+        bf16x8 pieces[3];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const f32x4 query = *reinterpret_cast<const f32x4 *>(&o.weight.query[r8 + h * 4]);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) dout[h * 4 + x] *= query[x];
+        }
+        split8<3>(dout, pieces);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) to.queried[p][lane] = __builtin_bit_cast(u32x4, pieces[p]);
+    }
+}
+
+template <class T, int KS>
+__global__ void __launch_bounds__(kSharedWaves<KS> * 64)
+delta_bwd_shared_kernel(Delta d, uint32_t groups, uint64_t from)
+{
+    __shared__ Helped<T, KS, true> room;
+    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c16 = lane % 16, r8 = lane / 16 * 8;
+    const uint64_t unit = from + blockIdx.x;
+    const uint32_t head = (uint32_t)(unit / groups % d.H), seq = (uint32_t)(unit / groups / d.H), column0 = (uint32_t)(unit % groups) * kShared, col = column0 + c16;
+    const Span span = span_of(d, seq);
+    const uint32_t row0 = wave * 32, rows = d.Dk > row0 ? d.Dk - row0 : 0, chunks = (span.len + kChunk - 1) / kChunk;
+    const bool column = col < d.Dv, in = wave < KS && column;
+    const uint64_t memory = (((uint64_t)seq * d.H + head) * d.Dk + row0) * d.Dv + col;
+    Share<T, KS> share;
+    f32x4 gradient;
+    load_memory<1>(d.ds_last ? d.ds_last + memory : nullptr, rows, d.Dv, in, r8, share.S);
+    along_helped<T, KS, true>(d, span, seq, head, column0, room, wave,
+        [&](uint32_t i) {
+            const uint32_t c = chunks - 1 - i;
+            share.before(room.ops[i % 2], room.shares, wave, lane);
+            if (i == 0 || c % (kMark / kChunk) == kMark / kChunk - 1)
+                store_memory<1>(d.dmarks + (((uint64_t)(first_slot(span, seq) + c / (kMark / kChunk)) * d.H + head) * d.Dk + row0) * d.Dv + col, rows, d.Dv, in, r8, share.S);
+        },
+        [&](uint32_t i) { share.after(room.shares, i % 2, wave, lane); },
+        [&](uint32_t i) {
+            if (i < chunks) make_ahead<T, KS>(room.ops[i % 2], room.tiles[i % 2], room.shares, wave - KS, lane);
+            gradient = room.shares.left[(i + 1) % 2][wave - KS][lane];
+        },
+        [&](uint32_t i) {
+            if (i) store_four<float>(d.dr + head * d.Dv, (uint64_t)d.H * d.Dv, col, span, (chunks - i) * kChunk, r8, (wave - KS) * 4, column, gradient);
+        });
+    if (d.ds0) store_memory<1>(d.ds0 + memory, rows, d.Dv, in, r8, share.S);
+}
+
+template <class T, int KS, bool kVec>
 __global__ void __launch_bounds__(kMostWaves * 64)
 delta_bwd_kernel(Delta d, uint32_t with, uint32_t groups, uint64_t from)
 {
-    __shared__ typename Lds<T, KS, kHelped>::type room;
+    __shared__ Room<T, KS> room;
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = blockDim.x / 64, c16 = lane % 16, r8 = lane / 16 * 8;
     const uint64_t unit = from + blockIdx.x;
-    const uint32_t head = (uint32_t)(unit / groups % d.H), seq = (uint32_t)(unit / groups / d.H), column0 = (uint32_t)(unit % groups) * with * 16, col = column0 + wave * 16 + c16;
+    const uint32_t head = (uint32_t)(unit / groups % d.H), seq = (uint32_t)(unit / groups / d.H), col = (uint32_t)(unit % groups) * with * 16 + wave * 16 + c16;
     const Span span = span_of(d, seq);
     const bool in = wave < with && col < d.Dv;
     const uint64_t memory = ((uint64_t)seq * d.H + head) * d.Dk * d.Dv + col;
     const uint32_t last = span.len ? (span.len - 1) / kChunk : 0;
     f32x4 S[2 * KS];
     load_memory<KS>(d.ds_last ? d.ds_last + memory : nullptr, d.Dk, d.Dv, in, r8, S);
-    auto mark = [&](uint32_t c) {
+    float dout[8], gradient[8];
+    const T *gradients = (const T *)d.dout + head * d.Dv;
+    const uint32_t at = in ? col : 0;
+    T next[8];
+    // of the chunk before: stored when the next one's loads are on their way
+    auto store = [&](uint32_t t0) { store_column<float>(d.dr + head * d.Dv, (uint64_t)d.H * d.Dv, at, span, t0, r8, in, gradient); };
+    load_column<T>(gradients, d.lddo, at, span, last * kChunk, r8, next);
+    along<T, KS, true, kVec>(d, span, seq, head, room, wave, waves, [&](const Operands<T, KS> &o, uint32_t c) {
+        if (wave >= with) return;
+        const uint32_t t0 = c * kChunk;
         if (c == last || c % (kMark / kChunk) == kMark / kChunk - 1)
             store_memory<KS>(d.dmarks + ((uint64_t)(first_slot(span, seq) + c / (kMark / kChunk)) * d.H + head) * d.Dk * d.Dv + col, d.Dk, d.Dv, in, r8, S);
-    };
-    float dout[8], gradient[8];
-    if constexpr (kHelped) {
-        along_helped<T, KS, true>(d, span, seq, head, column0, room, wave, with, waves, [&](const Operands<T, KS, true> &o, uint32_t c, Tiles<T, true> &tile) {
-            mark(c);
-            const uint32_t at = wave * 16 + c16;
+        if (c != last) store(t0 + kChunk);
 #pragma unroll
-            for (int x = 0; x < 8; ++x) dout[x] = (float)tile.in[r8 + x][at];
-            take_chunk<T, KS>(o, c16, r8, dout, S, gradient);
-#pragma unroll
-            for (int x = 0; x < 8; ++x) tile.wide[r8 + x][at] = gradient[x];
-        });
-    } else {
-        const T *gradients = (const T *)d.dout + head * d.Dv;
-        const uint32_t at = in ? col : 0;
-        T next[8];
-        // of the chunk before: stored when the next one's loads are on their way
-        auto store = [&](uint32_t t0) { store_column<float>(d.dr + head * d.Dv, (uint64_t)d.H * d.Dv, at, span, t0, r8, in, gradient); };
-        load_column<T>(gradients, d.lddo, at, span, last * kChunk, r8, next);
-        along<T, KS, true, kVec>(d, span, seq, head, room, wave, waves, [&](const Operands<T, KS, true> &o, uint32_t c) {
-            if (wave >= with) return;
-            const uint32_t t0 = c * kChunk;
-            mark(c);
-            if (c != last) store(t0 + kChunk);
-#pragma unroll
-            for (int x = 0; x < 8; ++x) dout[x] = held(next[x], span, t0 + r8 + x, in);
-            load_column<T>(gradients, d.lddo, at, span, c ? t0 - kChunk : 0, r8, next);
-            take_chunk<T, KS>(o, c16, r8, dout, S, gradient);
-        });
-        if (span.len && wave < with) store(0);
-    }
+        for (int x = 0; x < 8; ++x) dout[x] = held(next[x], span, t0 + r8 + x, in);
+        load_column<T>(gradients, d.lddo, at, span, c ? t0 - kChunk : 0, r8, next);
+        take_chunk<T, KS>(o, c16, r8, dout, S, gradient);
+    });
+    if (span.len && wave < with) store(0);
     if (d.ds0) store_memory<KS>(d.ds0 + memory, d.Dk, d.Dv, in, r8, S);
 }
 
 template <class T, int KS>
 void launch_size(const Delta &d, hipStream_t st)
 {
-    constexpr bool kRoom = sizeof(Helped<T, KS, true>) <= 160 * 1024;
-    const Columns c = columns_of(d, kRoom && d.vec_all);
+    constexpr bool kRoom = kHasRoom<T, KS, true>;
+    const Columns c = columns_of(d, kRoom);
     const uint64_t units = (uint64_t)d.n_seq * d.H * c.groups;
     for (uint64_t from = 0; from < units; from += kMostLaunched) {
         const uint32_t grid = (uint32_t)(units - from < kMostLaunched ? units - from : kMostLaunched);
         if constexpr (kRoom)
             if (c.helped) {
-                delta_bwd_kernel<T, KS, true, true><<<grid, c.waves * 64, 0, st>>>(d, c.with, c.groups, from);
+                delta_bwd_shared_kernel<T, KS><<<grid, kSharedWaves<KS> * 64, 0, st>>>(d, c.groups, from);
                 continue;
             }
-        if (d.vec_keys) delta_bwd_kernel<T, KS, false, true><<<grid, c.waves * 64, 0, st>>>(d, c.with, c.groups, from);
-        else delta_bwd_kernel<T, KS, false, false><<<grid, c.waves * 64, 0, st>>>(d, c.with, c.groups, from);
+        if (d.vec_keys) delta_bwd_kernel<T, KS, true><<<grid, c.waves * 64, 0, st>>>(d, c.with, c.groups, from);
+        else delta_bwd_kernel<T, KS, false><<<grid, c.waves * 64, 0, st>>>(d, c.with, c.groups, from);
     }
 }
 

@@ -1,9 +1,9 @@
 // The gated delta rule in chunks of 32 tokens, along the sequences.  Internal.
 //
-// A wavefront has all rows of 16 columns of the memory in its registers, so that a chunk needs no exchange between wavefronts: results of the matrix unit
+// A wavefront has all rows of 16 columns of the memory in its registers (or, where heads are few, 32 rows of them), so that a chunk needs no exchange between wavefronts: results of the matrix unit
 // are the right operands of the next product (split_rows).  Left operands are the same for all columns and lie in LDS.  Those that depend on q, k, g and beta
 // alone (T and P) are made by a launch of its own (delta_weights.hip), for all chunks at once, in the workspace, as they are to lie in LDS, and come by loads that write there;
-// K and Q come through registers, which cut them into pieces and turn them.
+// K and Q come through registers, which cut them into pieces; reads that transpose turn them.
 #pragma once
 #include "delta_common.h"
 
@@ -18,12 +18,10 @@ constexpr int kPage = 1024;             // what a wavefront fetches at once
 // Rows of left operands lie by result: number i at `line(i)`.
 __host__ __device__ constexpr uint32_t line(uint32_t i) { return (i & ~31u) | (i >> 2 & 1) << 4 | (i >> 3 & 3) << 2 | (i & 3); }
 
-template <class T, int KS, bool kBackward>
+template <class T, int KS>
 struct alignas(16) Keys {
     static constexpr int n = Pieces<T>::n, DK = 32 * KS;
-    uint16_t K[n][kChunk][DK + 8];
-    uint16_t KT[n][DK][kPitch];
-    uint16_t Q[n][kBackward ? DK : kChunk][kBackward ? kPitch : DK + 8];       // backward: Q^T
+    uint16_t K[n][kChunk][DK + 8], Q[n][kChunk][DK + 8];
 };
 
 struct alignas(16) Weights {
@@ -38,6 +36,9 @@ static_assert(sizeof(Weights) % kPage == 0, "fetched by pages");
 inline uint64_t chunk_slots(uint64_t N, uint32_t n_seq) { return N / kChunk + n_seq; }
 
 __device__ __forceinline__ uint64_t first_chunk(const Span &s, uint32_t seq) { return s.begin / kChunk + seq; }
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 s16x4_in_lds;
 
 __device__ __forceinline__ bf16x8 left(const uint16_t *row) { return operand(*reinterpret_cast<const u32x4 *>(row)); }
 
@@ -75,131 +76,147 @@ __device__ __forceinline__ void eight(const T *row, uint32_t c, uint32_t D, bool
 
 // ------------------------------------------------------------------------------ along a sequence
 constexpr int kMostWaves = 4;           // in a workgroup
+constexpr uint64_t kFewColumns = 512;   // groups of 16
 
-template <class T, int KS, bool kBackward>
+template <class T, int KS>
 struct Operands {
     Weights weight;
-    Keys<T, KS, kBackward> key;
+    Keys<T, KS> key;
 };
 
 // Buffers: two if they fit, so that a chunk's operands come while the one before is worked on
-template <class T, int KS, bool kBackward>
+template <class T, int KS>
 struct Room {
-    static constexpr int kBuffers = 2 * sizeof(Operands<T, KS, kBackward>) <= 160 * 1024 ? 2 : 1;
-    Operands<T, KS, kBackward> ops[kBuffers];
+    static constexpr int kBuffers = 2 * sizeof(Operands<T, KS>) <= 160 * 1024 ? 2 : 1;
+    Operands<T, KS> ops[kBuffers];
 };
 
-// Where some wavefronts have columns and the others bring what these need and take away what they leave: up to 32 columns of a chunk's tokens
-constexpr int kTileColumns = 32;
-template <class T, bool kBackward>
-struct alignas(16) Tiles {
-    T in[kChunk][kTileColumns + 8];                             // v, or gradients of o
-    T out[kBackward ? 1 : kChunk][kTileColumns + 8];            // o
-    float wide[kChunk][kTileColumns + 4];                       // what tokens miss, or gradients of what they write
-};
-
-// eight values of a token: as they lie in its row, and each into its column's row
+// eight values of a token
 template <int n, int KS>
-__device__ __forceinline__ void put(const float (&v)[8], uint32_t t, uint32_t col, uint16_t (*rows)[kChunk][32 * KS + 8], uint16_t (*columns)[32 * KS][kPitch])
+__device__ __forceinline__ void put(const float (&v)[8], uint32_t t, uint32_t col, uint16_t (&rows)[n][kChunk][32 * KS + 8])
 {
     uint32_t w[n][4];
     split<n, 8>(v, w);
 #pragma unroll
-    for (int p = 0; p < n; ++p) {
-        if (rows) *reinterpret_cast<u32x4 *>(&rows[p][line(t)][col]) = (u32x4){w[p][0], w[p][1], w[p][2], w[p][3]};
-        if (columns)
+    for (int p = 0; p < n; ++p) *reinterpret_cast<u32x4 *>(&rows[p][line(t)][col]) = (u32x4){w[p][0], w[p][1], w[p][2], w[p][3]};
+}
+
+// The same of eight that came as they lie, halves of them behind D as 0
+template <class T, int KS>
+__device__ __forceinline__ void put_raw(const u32x4 (&v)[sizeof(T) / 2], bool in, uint32_t col, uint32_t D, uint32_t t, uint16_t (&rows)[Pieces<T>::n][kChunk][32 * KS + 8])
+{
+    constexpr int m = 16 / sizeof(T);
+    u32x4 clear[sizeof(T) / 2];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) columns[p][line(col + i)][t] = (uint16_t)(w[p][i / 2] >> (i % 2 * 16));
+    for (int h = 0; h < 8 / m; ++h)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) clear[h][x] = in && col + h * m < D ? v[h][x] : 0u;
+    if constexpr (Pieces<T>::n == 1) *reinterpret_cast<u32x4 *>(&rows[0][line(t)][col]) = clear[0];
+    else {
+        const dg_rows::Pack<T, 8> p = __builtin_bit_cast(dg_rows::Pack<T, 8>, clear);
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = (float)p.v[i];
+        put<Pieces<T>::n, KS>(x, t, col, rows);
     }
 }
 
+// Where a chunk's tokens lie: lowest row, and how many rows behind it a token is (the lowest's place for tokens that are not there)
+struct Place {
+    uint64_t row;
+    uint32_t count;
+    int32_t turn;
+    __device__ __forceinline__ Place(const Span &s, uint32_t t0) : count(s.len - t0 < kChunk ? s.len - t0 : kChunk), turn(s.turn)
+    {
+        row = s.turn ? s.begin + (s.len - t0 - count) : s.begin + t0;
+    }
+    __device__ __forceinline__ uint32_t behind(uint32_t t) const { return t >= count ? 0u : turn ? count - 1 - t : t; }
+};
+
 // K and Q of a chunk on their way to LDS, kEach vectors of each for a lane: a workgroup has wavefronts enough for that
-template <class T, int KS, bool kBackward, int kEach, bool kVec>
+template <class T, int KS, int kEach>
+struct Fetched {
+    u32x4 qs[kEach][sizeof(T) / 2], ks[kEach][sizeof(T) / 2];
+};
+
+template <class T, int KS, int kEach, bool kVec>
 struct Rows {
     static constexpr int n = Pieces<T>::n;
     const T *q, *k;
     uint64_t ldq, ldk;
     uint32_t Dk, wave, waves, lane;
     Span span;
-    dg_rows::Pack<T, 8> qs[kEach], ks[kEach];
 
     __device__ __forceinline__ uint32_t token(int i) const { return (i * waves + wave) * (16 / KS) + lane / (4 * KS); }
     __device__ __forceinline__ uint32_t column() const { return lane % (4 * KS) * 8; }
 
-    // a vector where there is one, otherwise another, which store() clears
-    __device__ __forceinline__ void fetch(uint32_t c)
+    // a vector where there is one, otherwise another, which store() clears; one address for the workgroup, 32-bit distances from it (32 rows of at most 2^24 values)
+    __device__ __forceinline__ void fetch(uint32_t c, Fetched<T, KS, kEach> &to) const
     {
         if (!kVec) return;
         constexpr int m = 16 / sizeof(T);
+        const Place at(span, c * kChunk);
+        const uint8_t *const k0 = (const uint8_t *)(k + at.row * ldk), *const q0 = (const uint8_t *)(q + at.row * ldq);
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const uint32_t t = c * kChunk + token(i);
-            const uint64_t row = span.row(token(i) < kChunk && t < span.len ? t : c * kChunk);
+            const uint32_t row = at.behind(token(i)), to_k = row * (uint32_t)ldk * sizeof(T), to_q = row * (uint32_t)ldq * sizeof(T);
 #pragma unroll
             for (int h = 0; h < 8 / m; ++h) {
-                const uint32_t col = column() + h * m < Dk ? column() + h * m : 0;
-                const dg_rows::Pack<T, m> x = *reinterpret_cast<const dg_rows::Pack<T, m> *>(k + row * ldk + col), y = *reinterpret_cast<const dg_rows::Pack<T, m> *>(q + row * ldq + col);
-#pragma unroll
-                for (int j = 0; j < m; ++j) {
-                    ks[i].v[h * m + j] = x.v[j];
-                    qs[i].v[h * m + j] = y.v[j];
-                }
+                const uint32_t col = (column() + h * m < Dk ? column() + h * m : 0) * sizeof(T);
+                to.ks[i][h] = *reinterpret_cast<const u32x4 *>(k0 + (to_k + col));
+                to.qs[i][h] = *reinterpret_cast<const u32x4 *>(q0 + (to_q + col));
             }
         }
     }
 
-    __device__ __forceinline__ void store(uint32_t c, Keys<T, KS, kBackward> &to)
+    __device__ __forceinline__ void store(uint32_t c, const Fetched<T, KS, kEach> &from, Keys<T, KS> &to) const
     {
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const uint32_t t = token(i);
             if (t >= kChunk) continue;
-            float x[8], y[8];
             const bool in = c * kChunk + t < span.len;
             if constexpr (kVec) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const bool here = in && column() + j < Dk;
-                    x[j] = here ? (float)ks[i].v[j] : 0.0f;
-                    y[j] = here ? (float)qs[i].v[j] : 0.0f;
-                }
+                put_raw<T, KS>(from.ks[i], in, column(), Dk, t, to.K);
+                put_raw<T, KS>(from.qs[i], in, column(), Dk, t, to.Q);
             } else {
+                float x[8], y[8];
                 const uint64_t row = span.row(in ? c * kChunk + t : c * kChunk);
                 eight<T, false>(k + row * ldk, column(), Dk, in, x);
                 eight<T, false>(q + row * ldq, column(), Dk, in, y);
+                put<n, KS>(x, t, column(), to.K);
+                put<n, KS>(y, t, column(), to.Q);
             }
-            put<n, KS>(x, t, column(), to.K, to.KT);
-            if constexpr (kBackward) put<n, KS>(y, t, column(), nullptr, to.Q);
-            else put<n, KS>(y, t, column(), to.Q, nullptr);
         }
     }
 };
 
 // use(operands, chunk) for a sequence's chunks in turn, backward from the last one on
 template <class T, int KS, bool kBackward, bool kVec, class Use>
-__device__ __forceinline__ void along(const Delta &d, const Span &span, uint32_t seq, uint32_t head, Room<T, KS, kBackward> &room, uint32_t wave, uint32_t waves, Use use)
+__device__ __forceinline__ void along(const Delta &d, const Span &span, uint32_t seq, uint32_t head, Room<T, KS> &room, uint32_t wave, uint32_t waves, Use use)
 {
-    constexpr int kBuffers = Room<T, KS, kBackward>::kBuffers;
+    constexpr int kBuffers = Room<T, KS>::kBuffers;
     const uint32_t chunks = (span.len + kChunk - 1) / kChunk, hk = head / (d.H / d.Hk);
     if (chunks == 0) return;
     const uint64_t slot0 = first_chunk(span, seq);
     auto chunk = [&](uint32_t i) { return kBackward ? chunks - 1 - i : i; };
-    Rows<T, KS, kBackward, 2, kVec> rows = {(const T *)d.q + hk * d.Dk, (const T *)d.k + hk * d.Dk, d.ldq, d.ldk, d.Dk, wave, waves, threadIdx.x % 64, span, {}, {}};
+    Rows<T, KS, 2, kVec> rows = {(const T *)d.q + hk * d.Dk, (const T *)d.k + hk * d.Dk, d.ldq, d.ldk, d.Dk, wave, waves, threadIdx.x % 64, span};
+    Fetched<T, KS, 2> fetched;
     auto weights = [&](uint32_t i) {
         const uint8_t *from = (const uint8_t *)(d.weights + (slot0 + chunk(i)) * d.H + head) + threadIdx.x % 64 * 16;
         uint8_t *to = (uint8_t *)&room.ops[i % kBuffers].weight;
         for (uint32_t at = wave * kPage; at < sizeof(Weights); at += waves * kPage)
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)(from + at), (__attribute__((address_space(3))) uint32_t *)(to + at), 16, 0, 0);
     };
-    rows.fetch(chunk(0));
+    rows.fetch(chunk(0), fetched);
     weights(0);
-    rows.store(chunk(0), room.ops[0].key);
+    rows.store(chunk(0), fetched, room.ops[0].key);
     for (uint32_t i = 0; i < chunks; ++i) {
         __builtin_amdgcn_s_waitcnt(0x0f70);         // all loads, those that write to LDS among them
         __syncthreads();
         const bool more = i + 1 < chunks;
         if (more) {
-            rows.fetch(chunk(i + 1));
+            rows.fetch(chunk(i + 1), fetched);
             if (kBuffers == 2) weights(i + 1);
         }
         use(room.ops[i % kBuffers], chunk(i));
@@ -207,146 +224,200 @@ __device__ __forceinline__ void along(const Delta &d, const Span &span, uint32_t
             __syncthreads();
             if (more) weights(i + 1);
         }
-        if (more) rows.store(chunk(i + 1), room.ops[(i + 1) % kBuffers].key);
+        if (more) rows.store(chunk(i + 1), fetched, room.ops[(i + 1) % kBuffers].key);
     }
 }
 
-// The same with wavefronts `with` on bringing and taking away, of rows in whole 16 bytes.  use(operands, chunk, tile) for those that have columns; in, out, wide: columns of the workgroup in
-// rows of tokens.  What is brought is fetched two chunks ahead.
+// ------------------------------------------------------------------------------ along a sequence, few heads
+// With fewer columns than the chip has room for, what bounds is how long a chunk takes a wavefront: so KS of them share 16 columns, with 32 rows of the memory each.  K S is then a sum
+// over the wavefronts, which goes through LDS (Shares): a chunk has two halves, between barriers, what goes before the sum and what comes after.  All that the next chunk does not wait for
+// is done by others: two for what is made of a chunk's tokens (o, the gradients' part that does not depend on S), some that bring what all need, of rows in whole 16 bytes.
+constexpr int kShared = 16;             // columns
+constexpr int kAside = 2;
+
+template <int KS>
+constexpr int kHelpers = KS == 1 ? 2 : KS;
+template <int KS>
+constexpr int kSharedWaves = KS + kAside + kHelpers<KS>;
+
+template <class T>
+struct alignas(16) Tile {
+    T in[kChunk][kShared + 8];          // v, or gradients of o
+    // a lane's eight tokens of a column
+    __device__ __forceinline__ void read(uint32_t lane, float (&out)[8]) const
+    {
+        const uint32_t c16 = lane % 16, r8 = lane / 16 * 8;
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4_in_lds *)&in[r8 + h * 4 + c16 / 4][c16 % 4 * 4]);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const short bits = v[x];
+                    out[h * 4 + x] = (float)__builtin_bit_cast(T, bits);
+                }
+            }
+        } else
+#pragma unroll
+            for (int x = 0; x < 8; ++x) out[x] = (float)in[r8 + x][c16];
+    }
+};
+
+// What wavefronts hand each other; for those aside two buffers, since they are a chunk behind
+template <int KS, bool kBackward>
+struct alignas(16) Shares {
+    f32x4 keys[KS][2][64];                                      // K S
+    f32x4 queries[kBackward ? 1 : 2][kBackward ? 1 : KS][2][64];
+    f32x4 left[2][kBackward ? 2 : 4][64];                       // what tokens miss (backward: gradients of what they write), what they write
+    f32x4 ahead[kBackward ? 2 : 1][64];                         // backward: P^T dO
+    u32x4 queried[kBackward ? 3 : 1][64];                       // scale e^G dO, in pieces
+
+    // all wavefronts' sum
+    __device__ __forceinline__ static f32x4 sum(const f32x4 (&of)[KS][2][64], int h, uint32_t lane)
+    {
+        f32x4 v[KS];
+#pragma unroll
+        for (int s = 0; s < KS; ++s) v[s] = of[s][h][lane];
+        if constexpr (KS == 4) return (v[0] + v[1]) + (v[2] + v[3]);
+        else if constexpr (KS == 2) return v[0] + v[1];
+        else return v[0];
+    }
+};
+
 template <class T, int KS, bool kBackward>
 struct Helped {
-    static constexpr int kWeights = 8;          // of 16 bytes to a lane: all of them with two wavefronts
-    static_assert(sizeof(Weights) <= kWeights * 128 * 16, "two wavefronts bring the weights");
-    Operands<T, KS, kBackward> ops[2];
-    Tiles<T, kBackward> tiles[2];
+    Operands<T, KS> ops[2];
+    Tile<T> tiles[2];
+    Shares<KS, kBackward> shares;
 };
+template <class T, int KS, bool kBackward>
+constexpr bool kHasRoom = sizeof(Helped<T, KS, kBackward>) <= 160 * 1024;
 
 template <class T, int KS, bool kBackward>
 struct Helper {
-    static constexpr int kWeights = Helped<T, KS, kBackward>::kWeights;
+    static constexpr int kLanes = kHelpers<KS> * 64, kEach = (2 * KS + kHelpers<KS> - 1) / kHelpers<KS>, kWeights = (int)(sizeof(Weights) / 16 + kLanes - 1) / kLanes;
+    static_assert(kLanes * 8 >= kChunk * kShared, "a lane has eight values of the tile at most");
+    static_assert(sizeof(Weights) / 16 % kLanes == 0, "all lanes fetch weights");
     const Delta &d;
     const Span &span;
     uint64_t slot0;
-    uint32_t head, lanes, self, columns, column0;       // lanes that help, this one among them
-    Rows<T, KS, kBackward, 4, true> rows;
-    u32x4 weights[kWeights];
-    dg_rows::Pack<T, 8> in;
+    uint32_t head, self, column0;
+    Rows<T, KS, kEach, true> rows;
+    struct Chunk {
+        Fetched<T, KS, kEach> rows;
+        u32x4 weights[kWeights], in[sizeof(T) / 2];
+    };
 
-    __device__ __forceinline__ uint32_t token() const { return self * 8 / columns; }
-    __device__ __forceinline__ uint32_t column() const { return self * 8 % columns; }
-    // row of a token of chunk c, another where it is none
-    __device__ __forceinline__ uint64_t row_of(uint32_t c, uint32_t t) const { return span.row(c * kChunk + t < span.len ? c * kChunk + t : c * kChunk); }
+    __device__ __forceinline__ uint32_t token() const { return self * 8 / kShared % kChunk; }
+    __device__ __forceinline__ uint32_t column() const { return self * 8 % kShared; }
 
-    __device__ __forceinline__ void fetch(uint32_t c)
+    __device__ __forceinline__ void fetch(uint32_t c, Chunk &to) const
     {
-        rows.fetch(c);
+        constexpr int m = 16 / sizeof(T);
+        rows.fetch(c, to.rows);
         const u32x4 *from = (const u32x4 *)(d.weights + (slot0 + c) * d.H + head);
 #pragma unroll
-        for (int i = 0; i < kWeights; ++i) {
-            const uint32_t at = i * lanes + self;
-            weights[i] = from[at < sizeof(Weights) / 16 ? at : 0];
-        }
-        if (self * 8 >= kChunk * columns) return;
-        const T *p = kBackward ? (const T *)d.dout + row_of(c, token()) * d.lddo : (const T *)d.v + row_of(c, token()) * d.ldv;
-        const uint32_t first = column0 + column();
-        p += head * d.Dv;
+        for (int i = 0; i < kWeights; ++i) to.weights[i] = from[i * kLanes + self];
+        const Place at(span, c * kChunk);
+        const uint64_t ld = kBackward ? d.lddo : d.ldv;
+        const uint8_t *p = (const uint8_t *)((const T *)(kBackward ? d.dout : d.v) + at.row * ld + head * d.Dv);
+        const uint32_t row = at.behind(token()) * (uint32_t)ld, first = column0 + column();
+#pragma unroll
+        for (int h = 0; h < 8 / m; ++h) to.in[h] = *reinterpret_cast<const u32x4 *>(p + (row + (first + h * m < d.Dv ? first + h * m : 0)) * (uint32_t)sizeof(T));
+    }
+
+    __device__ __forceinline__ void put_tile(uint32_t c, const Chunk &from, Tile<T> &tile) const
+    {
+        if (self * 8 >= kChunk * kShared) return;
+        const bool there = c * kChunk + token() < span.len;
         constexpr int m = 16 / sizeof(T);
 #pragma unroll
         for (int h = 0; h < 8 / m; ++h) {
-            const dg_rows::Pack<T, m> x = *reinterpret_cast<const dg_rows::Pack<T, m> *>(p + (first + h * m < d.Dv ? first + h * m : 0));
+            u32x4 part;
 #pragma unroll
-            for (int j = 0; j < m; ++j) in.v[h * m + j] = x.v[j];
+            for (int x = 0; x < 4; ++x) part[x] = there && column0 + column() + h * m < d.Dv ? from.in[h][x] : 0u;
+            *reinterpret_cast<u32x4 *>(&tile.in[token()][column() + h * m]) = part;
         }
     }
 
-    __device__ __forceinline__ void put(uint32_t c, Operands<T, KS, kBackward> &ops, Tiles<T, kBackward> &tile)
+    __device__ __forceinline__ void put_operands(uint32_t c, const Chunk &from, Operands<T, KS> &ops) const
     {
         u32x4 *to = (u32x4 *)&ops.weight;
 #pragma unroll
-        for (int i = 0; i < kWeights; ++i) {
-            const uint32_t at = i * lanes + self;
-            if (at < sizeof(Weights) / 16) to[at] = weights[i];
-        }
-        rows.store(c, ops.key);
-        if (self * 8 >= kChunk * columns) return;
-        const bool there = c * kChunk + token() < span.len;
-        dg_rows::Pack<T, 8> x;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x.v[j] = there && column0 + column() + j < d.Dv ? in.v[j] : (T)0.0f;
-        constexpr int m = 16 / sizeof(T);
-#pragma unroll
-        for (int h = 0; h < 8 / m; ++h) {
-            dg_rows::Pack<T, m> part;
-#pragma unroll
-            for (int j = 0; j < m; ++j) part.v[j] = x.v[h * m + j];
-            *reinterpret_cast<dg_rows::Pack<T, m> *>(&tile.in[token()][column() + h * m]) = part;
-        }
-    }
-
-    template <class E, int pitch>
-    __device__ __forceinline__ void take(const E (&tile)[kChunk][pitch], E *p) const
-    {
-        constexpr int m = 16 / sizeof(E);
-        const uint32_t first = column0 + column();
-#pragma unroll
-        for (int h = 0; h < 8 / m; ++h)
-            if (first + h * m < d.Dv) *reinterpret_cast<dg_rows::Pack<E, m> *>(p + first + h * m) = *reinterpret_cast<const dg_rows::Pack<E, m> *>(&tile[token()][column() + h * m]);
-    }
-
-    __device__ __forceinline__ void take_away(uint32_t c, const Tiles<T, kBackward> &tile) const
-    {
-        if (self * 8 >= kChunk * columns || c * kChunk + token() >= span.len) return;
-        const uint64_t row = row_of(c, token());
-        if constexpr (!kBackward) take(tile.out, (T *)d.o + row * d.ldo + head * d.Dv);
-        float *wide = kBackward ? d.dr : d.y;
-        if (wide) take(tile.wide, wide + (row * d.H + head) * d.Dv);
+        for (int i = 0; i < kWeights; ++i) to[i * kLanes + self] = from.weights[i];
+        rows.store(c, from.rows, ops.key);
     }
 };
 
-template <class T, int KS, bool kBackward, class Use>
-__device__ __forceinline__ void along_helped(const Delta &d, const Span &span, uint32_t seq, uint32_t head, uint32_t column0, Helped<T, KS, kBackward> &room, uint32_t wave, uint32_t with,
-                                             uint32_t waves, Use use)
+// before(i), after(i) in the wavefronts that have columns, early(i), late(i) in those aside, i counting chunks (backward from the last one): all but early go with the two buffers i % 2; early(i)
+// may read what after(i - 1) left, and both early(i) and late(i) run up to i = number of chunks.  The others have a chunk's time for what they bring for the next one.
+template <class T, int KS, bool kBackward, class Before, class After, class Early, class Late>
+__device__ __forceinline__ void along_helped(const Delta &d, const Span &span, uint32_t seq, uint32_t head, uint32_t column0, Helped<T, KS, kBackward> &room, uint32_t wave, Before before,
+                                             After after, Early early, Late late)
 {
     const uint32_t chunks = (span.len + kChunk - 1) / kChunk, hk = head / (d.H / d.Hk);
     if (chunks == 0) return;
-    auto chunk = [&](uint32_t i) { return kBackward ? chunks - 1 - i : i; };
-    if (wave < with) {
+    if (wave < KS) {
+        __builtin_amdgcn_s_setprio(3);          // the others are to wait for these
         for (uint32_t i = 0; i < chunks; ++i) {
             __syncthreads();
-            use(room.ops[i % 2], chunk(i), room.tiles[i % 2]);
+            before(i);
+            __syncthreads();
+            after(i);
         }
         __syncthreads();
         return;
     }
-    const uint32_t helpers = waves - with;
-    Helper<T, KS, kBackward> h = {d, span, first_chunk(span, seq), head, helpers * 64, threadIdx.x - with * 64, with * 16, column0,
-                                  {(const T *)d.q + hk * d.Dk, (const T *)d.k + hk * d.Dk, d.ldq, d.ldk, d.Dk, wave - with, helpers, threadIdx.x % 64, span, {}, {}}, {}, {}};
-    h.fetch(chunk(0));
-    h.put(chunk(0), room.ops[0], room.tiles[0]);
-    if (chunks > 1) h.fetch(chunk(1));
-    for (uint32_t i = 0; i < chunks; ++i) {
+    if (wave < KS + kAside) {
+        for (uint32_t i = 0; i < chunks; ++i) {
+            __syncthreads();
+            early(i);
+            __syncthreads();
+            late(i);
+        }
         __syncthreads();
-        if (i + 1 < chunks) h.put(chunk(i + 1), room.ops[(i + 1) % 2], room.tiles[(i + 1) % 2]);
-        if (i + 2 < chunks) h.fetch(chunk(i + 2));
-        if (i) h.take_away(chunk(i - 1), room.tiles[(i - 1) % 2]);
+        early(chunks);
+        late(chunks);
+        return;
+    }
+    using Help = Helper<T, KS, kBackward>;
+    constexpr uint32_t kFirst = KS + kAside;
+    const Help h = {d, span, first_chunk(span, seq), head, threadIdx.x - kFirst * 64, column0,
+                    {(const T *)d.q + hk * d.Dk, (const T *)d.k + hk * d.Dk, d.ldq, d.ldk, d.Dk, wave - kFirst, kHelpers<KS>, threadIdx.x % 64, span}};
+    // A chunk is fetched two before it is put; `coming` holds the next one.  Without a branch about a load (behind the last chunk it comes again), so that a wait is for the oldest loads only.
+    typename Help::Chunk held[2];
+    auto chunk = [&](uint32_t i) {
+        const uint32_t c = i < chunks ? i : chunks - 1;
+        return kBackward ? chunks - 1 - c : c;
+    };
+    auto turn = [&](uint32_t i, typename Help::Chunk &coming) {
+        __syncthreads();
+        h.put_tile(chunk(i + 1), coming, room.tiles[(i + 1) % 2]);
+        __syncthreads();
+        h.put_operands(chunk(i + 1), coming, room.ops[(i + 1) % 2]);
+        h.fetch(chunk(i + 3), coming);
+    };
+    h.fetch(chunk(0), held[0]);
+    h.fetch(chunk(1), held[1]);
+    h.put_tile(chunk(0), held[0], room.tiles[0]);
+    h.put_operands(chunk(0), held[0], room.ops[0]);
+    h.fetch(chunk(2), held[0]);
+    for (uint32_t i = 0; i < chunks; i += 2) {
+        turn(i, held[1]);
+        if (i + 1 < chunks) turn(i + 1, held[0]);
     }
     __syncthreads();
-    h.take_away(chunk(chunks - 1), room.tiles[(chunks - 1) % 2]);
 }
 
 // How many wavefronts of a workgroup have columns, how many there are (those that help among them), and how many workgroups a head has
 struct Columns { uint32_t with, waves, groups; bool helped; };
 
-// With fewer heads than the chip has room for, one or two wavefronts of a workgroup have columns and the others help; otherwise as many as possible have
-// columns and all help.  room: whether there is any for two buffers and the tiles.
+// With fewer heads than the chip has room for, wavefronts share columns; otherwise each has 16 of its own, as many as possible to a workgroup, and all bring operands.
 inline Columns columns_of(const Delta &d, bool room)
 {
     const uint32_t all = (d.Dv + 15) / 16, least = d.Dk <= 32 ? 1 : d.Dk <= 64 ? 2 : 4;
     const uint64_t units = (uint64_t)d.n_seq * d.H;
-    if (room && units * all <= 512) {
-        const uint32_t with = units * all <= 256 || all == 1 ? 1 : 2;
-        return {with, 4, (all + with - 1) / with, true};
-    }
+    if (room && d.vec_all && units * all <= kFewColumns) return {1, 0, all, true};
     uint32_t with = all < (uint32_t)kMostWaves ? all : kMostWaves;
     while (with > 1 && units * ((all + with - 1) / with) < 256) with = (with + 1) / 2;        // few heads: as many workgroups as there are compute units
     return {with, with < least ? least : with, (all + with - 1) / with, false};
@@ -420,12 +491,36 @@ __device__ __forceinline__ void store_column(T *p, uint64_t ld, uint32_t lane_co
             if (r8 + x < c.count) base[c.from + x * c.step + lane_column] = (T)v[x];
 }
 
+// four tokens from `first` of the lane's eight on
+template <class T>
+__device__ __forceinline__ void store_four(T *p, uint64_t ld, uint32_t lane_column, const Span &span, uint32_t t0, uint32_t r8, uint32_t first, bool in, const f32x4 &v)
+{
+    const Column c(span, t0, r8 + first, ld);
+    T *base = p + c.row * ld;
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+        if (in && r8 + first + x < c.count) base[c.from + x * c.step + lane_column] = (T)v[x];
+}
+
 // Left operands: tile h or t of a matrix in LDS, all pieces.  They are read ahead of the products, so that these do not wait for one after the other.
 template <int n, int rows, int pitch>
 __device__ __forceinline__ void lefts(const uint16_t (&m)[n][rows][pitch], uint32_t row, uint32_t col, bf16x8 (&out)[n])
 {
 #pragma unroll
     for (int p = 0; p < n; ++p) out[p] = left(&m[p][row][col]);
+}
+
+// Columns of K or Q as left operands of a sum over tokens: tile 2 s + h of the memory's rows.  16 lanes read 16 columns of 4 rows and get a column each: of rows of four tokens,
+// 4 lanes each, what lane l reads is columns 8 (l % 4) + 4 h on, so that column r is that of the memory's row with number r of result h.
+template <int n, int pitch>
+__device__ __forceinline__ void lefts_turned(const uint16_t (&m)[n][kChunk][pitch], uint32_t s, uint32_t h, uint32_t lane, bf16x8 (&out)[n])
+{
+#pragma unroll
+    for (int p = 0; p < n; ++p) {
+        const uint16_t *at = &m[p][lane / 4][s * 32 + h * 4 + lane % 4 * 8];            // tokens 8 (lane / 16) on lie in rows 4 (lane / 16) on, and 16 rows on
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4_in_lds *)at), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4_in_lds *)(at + 16 * pitch));
+        out[p] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
 }
 
 }  // namespace dg_delta

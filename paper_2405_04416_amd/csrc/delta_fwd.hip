@@ -7,7 +7,7 @@ using namespace dg_delta;
 
 // A chunk for a wavefront with 16 columns of the memory, S.  value: v of the lane's eight tokens; out, missed: o and what they miss.
 template <class T, int KS>
-__device__ __forceinline__ void take_chunk(const Operands<T, KS, false> &o, uint32_t c16, uint32_t r8, const float (&value)[8], f32x4 (&S)[2 * KS], float (&out)[8], float (&missed)[8])
+__device__ __forceinline__ void take_chunk(const Operands<T, KS> &o, uint32_t c16, uint32_t r8, const float (&value)[8], f32x4 (&S)[2 * KS], float (&out)[8], float (&missed)[8])
 {
     constexpr int n = Pieces<T>::n, kTiles = 2 * KS;
     bf16x8 keys[KS][2][n], queries[KS][2][n], inverse[2][3], pull[2][3];
@@ -37,7 +37,7 @@ __device__ __forceinline__ void take_chunk(const Operands<T, KS, false> &o, uint
     }
     bf16x8 turned[kTiles][n];
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) lefts(o.key.KT, t * 16 + c16, r8, turned[t]);
+    for (int t = 0; t < kTiles; ++t) lefts_turned(o.key.K, t / 2, t % 2, c16 + r8 * 2, turned[t]);
     __builtin_amdgcn_sched_barrier(0);
     f32x4 r[2], u[2], beta[2], until[2];
 #pragma unroll
@@ -72,82 +72,184 @@ __device__ __forceinline__ void take_chunk(const Operands<T, KS, false> &o, uint
     }
 }
 
-template <class T, int KS, bool kHelped>
-struct Lds { using type = Room<T, KS, false>; };
+// The same shared by KS wavefronts, rows 32 wave on each.
 template <class T, int KS>
-struct Lds<T, KS, true> { using type = Helped<T, KS, false>; };
+struct Share {
+    static constexpr int n = Pieces<T>::n;
+    f32x4 S[2];
+    bf16x8 inverse[2][3], turned[2][n];
+    f32x4 read[2], beta[2], until[2];
+    float value[8], whole;
 
-template <class T, int KS, bool kHelped, bool kVec>
+    // up to the sums K S and Q S; all that comes after them is read meanwhile
+    __device__ __forceinline__ void before(const Operands<T, KS> &o, const Tile<T> &tile, Shares<KS, false> &to, uint32_t parity, uint32_t wave, uint32_t lane)
+    {
+        const uint32_t c16 = lane % 16, r8 = lane / 16 * 8;
+        bf16x8 keys[2][n], queries[2][n], sp[3];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) lefts(o.key.K, h * 16 + c16, wave * 32 + r8, keys[h]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) lefts(o.key.Q, h * 16 + c16, wave * 32 + r8, queries[h]);
+        tile.read(lane, value);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            read[h] = *reinterpret_cast<const f32x4 *>(&o.weight.read[r8 + h * 4]);
+            lefts(o.weight.inverse, h * 16 + c16, r8, inverse[h]);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            beta[h] = *reinterpret_cast<const f32x4 *>(&o.weight.beta[r8 + h * 4]);
+            until[h] = *reinterpret_cast<const f32x4 *>(&o.weight.until[r8 + h * 4]);
+            lefts_turned(o.key.K, wave, h, lane, turned[h]);
+        }
+        whole = o.weight.whole;
+        __builtin_amdgcn_sched_barrier(0);
+        split_rows<3>(S[0], S[1], sp);
+        f32x4 sum[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) sum[h] = multiply<n, 3>(keys[h], sp, (f32x4){});
+#pragma unroll
+        for (int h = 0; h < 2; ++h) to.keys[wave][h][lane] = sum[h];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) sum[h] = multiply<n, 3>(queries[h], sp, (f32x4){});
+#pragma unroll
+        for (int h = 0; h < 2; ++h) to.queries[parity][wave][h][lane] = sum[h];
+    }
+
+    __device__ __forceinline__ void after(Shares<KS, false> &shares, uint32_t parity, uint32_t wave, uint32_t lane)
+    {
+        f32x4 r[2], u[2], y[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const f32x4 ks = shares.sum(shares.keys, h, lane);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) r[h][x] = value[h * 4 + x] - read[h][x] * ks[x];
+        }
+        bf16x8 right[3], written[3];
+        split_rows<3>(r[0], r[1], right);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) y[h] = multiply<3, 3>(inverse[h], right, (f32x4){});
+#pragma unroll
+        for (int h = 0; h < 2; ++h) u[h] = y[h] * beta[h];
+        split_rows<3>(u[0] * until[0], u[1] * until[1], written);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) S[h] = multiply<n, 3>(turned[h], written, S[h] * whole);
+        // for those aside, from each wavefront a part
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (wave == (KS == 4 ? 2 + h : h % KS)) shares.left[parity][h][lane] = y[h];
+            if (wave == h % KS) shares.left[parity][2 + h][lane] = u[h];
+        }
+    }
+};
+
+// o of 16 of a chunk's tokens, and what they miss
+template <class T, int KS>
+struct Outputs {
+    bf16x8 pull[3];
+    f32x4 u[2], y, query, qs;
+
+    __device__ __forceinline__ void read(const Operands<T, KS> &o, const Shares<KS, false> &shares, uint32_t parity, uint32_t h, uint32_t lane)
+    {
+        const uint32_t c16 = lane % 16, r8 = lane / 16 * 8;
+        lefts(o.weight.P, h * 16 + c16, r8, pull);
+        query = *reinterpret_cast<const f32x4 *>(&o.weight.query[r8 + h * 4]);
+        u[0] = shares.left[parity][2][lane], u[1] = shares.left[parity][3][lane], y = shares.left[parity][h][lane];
+        qs = shares.sum(shares.queries[parity], h, lane);
+    }
+    __device__ __forceinline__ f32x4 make() const
+    {
+        bf16x8 right[3];
+        split_rows<3>(u[0], u[1], right);
+        return multiply<3, 3>(pull, right, query * qs);
+    }
+};
+
+template <class T, int KS>
+__global__ void __launch_bounds__(kSharedWaves<KS> * 64)
+delta_fwd_shared_kernel(Delta d, uint32_t groups, uint64_t from)
+{
+    __shared__ Helped<T, KS, false> room;
+    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c16 = lane % 16, r8 = lane / 16 * 8;
+    const uint64_t unit = from + blockIdx.x;
+    const uint32_t head = (uint32_t)(unit / groups % d.H), seq = (uint32_t)(unit / groups / d.H), column0 = (uint32_t)(unit % groups) * kShared, col = column0 + c16;
+    const Span span = span_of(d, seq);
+    const uint32_t row0 = wave * 32, rows = d.Dk > row0 ? d.Dk - row0 : 0;
+    const bool column = col < d.Dv, in = wave < KS && column;
+    const uint64_t memory = (((uint64_t)seq * d.H + head) * d.Dk + row0) * d.Dv + col;
+    Share<T, KS> share;
+    Outputs<T, KS> outputs;
+    load_memory<1>(d.s0 ? d.s0 + memory : nullptr, rows, d.Dv, in, r8, share.S);
+    along_helped<T, KS, false>(d, span, seq, head, column0, room, wave,
+        [&](uint32_t c) {
+            share.before(room.ops[c % 2], room.tiles[c % 2], room.shares, c % 2, wave, lane);
+            if (d.marks && c % (kMark / kChunk) == 0)
+                store_memory<1>(d.marks + (((uint64_t)(first_slot(span, seq) + c / (kMark / kChunk)) * d.H + head) * d.Dk + row0) * d.Dv + col, rows, d.Dv, in, r8, share.S);
+        },
+        [&](uint32_t c) { share.after(room.shares, c % 2, wave, lane); },
+        [&](uint32_t c) { outputs.read(room.ops[(c + 1) % 2], room.shares, (c + 1) % 2, wave - KS, lane); },
+        [&](uint32_t c) {
+            if (c == 0) return;
+            const uint32_t t0 = (c - 1) * kChunk, h = wave - KS;
+            store_four<T>((T *)d.o + head * d.Dv, d.ldo, col, span, t0, r8, h * 4, column, outputs.make());
+            if (d.y) store_four<float>(d.y + head * d.Dv, (uint64_t)d.H * d.Dv, col, span, t0, r8, h * 4, column, outputs.y);
+        });
+    if (d.s_last) store_memory<1>(d.s_last + memory, rows, d.Dv, in, r8, share.S);
+}
+
+template <class T, int KS, bool kVec>
 __global__ void __launch_bounds__(kMostWaves * 64)
 delta_fwd_kernel(Delta d, uint32_t with, uint32_t groups, uint64_t from)
 {
-    __shared__ typename Lds<T, KS, kHelped>::type room;
+    __shared__ Room<T, KS> room;
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = blockDim.x / 64, c16 = lane % 16, r8 = lane / 16 * 8;
     const uint64_t unit = from + blockIdx.x;
-    const uint32_t head = (uint32_t)(unit / groups % d.H), seq = (uint32_t)(unit / groups / d.H), column0 = (uint32_t)(unit % groups) * with * 16, col = column0 + wave * 16 + c16;
+    const uint32_t head = (uint32_t)(unit / groups % d.H), seq = (uint32_t)(unit / groups / d.H), col = (uint32_t)(unit % groups) * with * 16 + wave * 16 + c16;
     const Span span = span_of(d, seq);
     const bool in = wave < with && col < d.Dv;
     const uint64_t memory = ((uint64_t)seq * d.H + head) * d.Dk * d.Dv + col;
     f32x4 S[2 * KS];
     load_memory<KS>(d.s0 ? d.s0 + memory : nullptr, d.Dk, d.Dv, in, r8, S);
-    auto mark = [&](uint32_t c) {
+    float value[8], out[8], missed[8];
+    const T *values = (const T *)d.v + head * d.Dv;
+    const uint32_t at = in ? col : 0;
+    T next[8];
+    // of the chunk before: stored when the next one's loads are on their way, so that none waits for a store
+    auto store = [&](uint32_t t0) {
+        store_column<T>((T *)d.o + head * d.Dv, d.ldo, at, span, t0, r8, in, out);
+        if (d.y) store_column<float>(d.y + head * d.Dv, (uint64_t)d.H * d.Dv, at, span, t0, r8, in, missed);
+    };
+    load_column<T>(values, d.ldv, at, span, 0, r8, next);
+    along<T, KS, false, kVec>(d, span, seq, head, room, wave, waves, [&](const Operands<T, KS> &o, uint32_t c) {
+        if (wave >= with) return;
+        const uint32_t t0 = c * kChunk;
         if (d.marks && c % (kMark / kChunk) == 0)
             store_memory<KS>(d.marks + ((uint64_t)(first_slot(span, seq) + c / (kMark / kChunk)) * d.H + head) * d.Dk * d.Dv + col, d.Dk, d.Dv, in, r8, S);
-    };
-    float value[8], out[8], missed[8];
-    if constexpr (kHelped) {
-        along_helped<T, KS, false>(d, span, seq, head, column0, room, wave, with, waves, [&](const Operands<T, KS, false> &o, uint32_t c, Tiles<T, false> &tile) {
-            mark(c);
-            const uint32_t at = wave * 16 + c16;
+        if (c) store(t0 - kChunk);
 #pragma unroll
-            for (int x = 0; x < 8; ++x) value[x] = (float)tile.in[r8 + x][at];
-            take_chunk<T, KS>(o, c16, r8, value, S, out, missed);
-#pragma unroll
-            for (int x = 0; x < 8; ++x) {
-                tile.out[r8 + x][at] = (T)out[x];
-                if (d.y) tile.wide[r8 + x][at] = missed[x];
-            }
-        });
-    } else {
-        const T *values = (const T *)d.v + head * d.Dv;
-        const uint32_t at = in ? col : 0;
-        T next[8];
-        // of the chunk before: stored when the next one's loads are on their way, so that none waits for a store
-        auto store = [&](uint32_t t0) {
-            store_column<T>((T *)d.o + head * d.Dv, d.ldo, at, span, t0, r8, in, out);
-            if (d.y) store_column<float>(d.y + head * d.Dv, (uint64_t)d.H * d.Dv, at, span, t0, r8, in, missed);
-        };
-        load_column<T>(values, d.ldv, at, span, 0, r8, next);
-        along<T, KS, false, kVec>(d, span, seq, head, room, wave, waves, [&](const Operands<T, KS, false> &o, uint32_t c) {
-            if (wave >= with) return;
-            const uint32_t t0 = c * kChunk;
-            mark(c);
-            if (c) store(t0 - kChunk);
-#pragma unroll
-            for (int x = 0; x < 8; ++x) value[x] = held(next[x], span, t0 + r8 + x, in);
-            load_column<T>(values, d.ldv, at, span, t0 + kChunk, r8, next);
-            take_chunk<T, KS>(o, c16, r8, value, S, out, missed);
-        });
-        if (span.len && wave < with) store((span.len - 1) / kChunk * kChunk);
-    }
+        for (int x = 0; x < 8; ++x) value[x] = held(next[x], span, t0 + r8 + x, in);
+        load_column<T>(values, d.ldv, at, span, t0 + kChunk, r8, next);
+        take_chunk<T, KS>(o, c16, r8, value, S, out, missed);
+    });
+    if (span.len && wave < with) store((span.len - 1) / kChunk * kChunk);
     if (d.s_last) store_memory<KS>(d.s_last + memory, d.Dk, d.Dv, in, r8, S);
 }
 
 template <class T, int KS>
 void launch_size(const Delta &d, hipStream_t st)
 {
-    constexpr bool kRoom = sizeof(Helped<T, KS, false>) <= 160 * 1024;
-    const Columns c = columns_of(d, kRoom && d.vec_all);
+    constexpr bool kRoom = kHasRoom<T, KS, false>;
+    const Columns c = columns_of(d, kRoom);
     const uint64_t units = (uint64_t)d.n_seq * d.H * c.groups;
     for (uint64_t from = 0; from < units; from += kMostLaunched) {
         const uint32_t grid = (uint32_t)(units - from < kMostLaunched ? units - from : kMostLaunched);
         if constexpr (kRoom)
             if (c.helped) {
-                delta_fwd_kernel<T, KS, true, true><<<grid, c.waves * 64, 0, st>>>(d, c.with, c.groups, from);
+                delta_fwd_shared_kernel<T, KS><<<grid, kSharedWaves<KS> * 64, 0, st>>>(d, c.groups, from);
                 continue;
             }
-        if (d.vec_keys) delta_fwd_kernel<T, KS, false, true><<<grid, c.waves * 64, 0, st>>>(d, c.with, c.groups, from);
-        else delta_fwd_kernel<T, KS, false, false><<<grid, c.waves * 64, 0, st>>>(d, c.with, c.groups, from);
+        if (d.vec_keys) delta_fwd_kernel<T, KS, true><<<grid, c.waves * 64, 0, st>>>(d, c.with, c.groups, from);
+        else delta_fwd_kernel<T, KS, false><<<grid, c.waves * 64, 0, st>>>(d, c.with, c.groups, from);
     }
 }
 
