@@ -67,41 +67,50 @@ __device__ __forceinline__ void take_chunk(const Operands<T, KS> &o, uint32_t c1
     }
 }
 
-// The same shared by KS wavefronts, rows 32 wave on each.
+// The same shared by wavefronts, rows 32 kOwn wave on each.
 template <class T, int KS>
 struct Share {
-    static constexpr int n = Pieces<T>::n;
-    f32x4 S[2];
-    bf16x8 inverse[2][3], turned[2][n], queries[2][n];
+    static constexpr int n = Pieces<T>::n, kOwn = KS / kSharers<KS>;
+    f32x4 S[2 * kOwn];
+    bf16x8 inverse[2][3], turned[2 * kOwn][n], queries[2 * kOwn][n];
     f32x4 read[2], until[2];
     float whole;
 
-    // up to the sum K S; all that comes after it is read meanwhile
+    // up to the sum K S; then all that comes after it is read
     __device__ __forceinline__ void before(const Operands<T, KS> &o, Shares<KS, true> &to, uint32_t wave, uint32_t lane)
     {
         const uint32_t c16 = lane % 16, r8 = lane / 16 * 8;
-        bf16x8 keys[2][n], sp[3];
+        bf16x8 keys[kOwn][2][n], sp[3];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) lefts(o.key.K, h * 16 + c16, wave * 32 + r8, keys[h]);
+        for (int s = 0; s < kOwn; ++s)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) lefts(o.key.K, h * 16 + c16, (wave * kOwn + s) * 32 + r8, keys[s][h]);
+        __builtin_amdgcn_sched_barrier(0);
+        f32x4 sum[kOwn][2];
+#pragma unroll
+        for (int s = 0; s < kOwn; ++s) {
+            split_rows<3>(S[2 * s], S[2 * s + 1], sp);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) sum[s][h] = multiply<n, 3>(keys[s][h], sp, (f32x4){});
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if constexpr (kOwn == 2) sum[0][h] += sum[1][h];
+            to.keys[wave][h][lane] = sum[0][h];
+        }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             until[h] = *reinterpret_cast<const f32x4 *>(&o.weight.until[r8 + h * 4]);
             lefts(o.weight.inverse, h * 16 + c16, r8, inverse[h]);
-            read[h] = *reinterpret_cast<const f32x4 *>(&o.weight.read[r8 + h * 4]);
         }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            lefts_turned(o.key.Q, wave, h, lane, queries[h]);
-            lefts_turned(o.key.K, wave, h, lane, turned[h]);
-        }
+        for (int t = 0; t < 2 * kOwn; ++t) lefts_turned(o.key.Q, wave * kOwn + t / 2, t % 2, lane, queries[t]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) read[h] = *reinterpret_cast<const f32x4 *>(&o.weight.read[r8 + h * 4]);
+#pragma unroll
+        for (int t = 0; t < 2 * kOwn; ++t) lefts_turned(o.key.K, wave * kOwn + t / 2, t % 2, lane, turned[t]);
         whole = o.weight.whole;
-        __builtin_amdgcn_sched_barrier(0);
-        split_rows<3>(S[0], S[1], sp);
-        f32x4 sum[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) sum[h] = multiply<n, 3>(keys[h], sp, (f32x4){});
-#pragma unroll
-        for (int h = 0; h < 2; ++h) to.keys[wave][h][lane] = sum[h];
     }
 
     __device__ __forceinline__ void after(Shares<KS, true> &shares, uint32_t parity, uint32_t wave, uint32_t lane)
@@ -114,17 +123,18 @@ struct Share {
         for (int p = 0; p < 3; ++p) queried[p] = operand(shares.queried[p][lane]);
         split_rows<3>(du[0], du[1], right);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) dr[h] = multiply<3, 3>(inverse[h], right, (f32x4){});
+        for (int h = 0; h < 2; ++h) dr[h] = multiply_soon<3, 3>(inverse[h], right, (f32x4){});
+        // while that is on its way
 #pragma unroll
-        for (int h = 0; h < 2; ++h) S[h] = multiply<n, 3>(queries[h], queried, S[h] * whole);
+        for (int t = 0; t < 2 * kOwn; ++t) S[t] = multiply<n, 3>(queries[t], queried, S[t] * whole);
 #pragma unroll
         for (int h = 0; h < 2; ++h) back[h] = -dr[h] * read[h];
         split_rows<3>(back[0], back[1], right);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) S[h] = multiply<n, 3>(turned[h], right, S[h]);
+        for (int t = 0; t < 2 * kOwn; ++t) S[t] = multiply<n, 3>(turned[t], right, S[t]);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-            if (wave == h % KS) shares.left[parity][h][lane] = dr[h];
+            if (wave == h % kSharers<KS>) shares.left[parity][h][lane] = dr[h];
     }
 };
 
@@ -163,31 +173,31 @@ delta_bwd_shared_kernel(Delta d, uint32_t groups, uint64_t from)
 {
     __shared__ Helped<T, KS, true> room;
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c16 = lane % 16, r8 = lane / 16 * 8;
-    const uint64_t unit = from + blockIdx.x;
-    const uint32_t head = (uint32_t)(unit / groups % d.H), seq = (uint32_t)(unit / groups / d.H), column0 = (uint32_t)(unit % groups) * kShared, col = column0 + c16;
+    const Unit unit(d, groups, from);
+    const uint32_t head = unit.head, seq = unit.seq, column0 = unit.group * kShared, col = column0 + c16;
     const Span span = span_of(d, seq);
-    const uint32_t row0 = wave * 32, rows = d.Dk > row0 ? d.Dk - row0 : 0, chunks = (span.len + kChunk - 1) / kChunk;
-    const bool column = col < d.Dv, in = wave < KS && column;
+    const uint32_t row0 = wave * (Share<T, KS>::kOwn * 32), rows = d.Dk > row0 ? d.Dk - row0 : 0, chunks = (span.len + kChunk - 1) / kChunk;
+    const bool column = col < d.Dv, in = wave < kSharers<KS> && column;
     const uint64_t memory = (((uint64_t)seq * d.H + head) * d.Dk + row0) * d.Dv + col;
     Share<T, KS> share;
     f32x4 gradient;
-    load_memory<1>(d.ds_last ? d.ds_last + memory : nullptr, rows, d.Dv, in, r8, share.S);
+    load_memory<Share<T, KS>::kOwn>(d.ds_last ? d.ds_last + memory : nullptr, rows, d.Dv, in, r8, share.S);
     along_helped<T, KS, true>(d, span, seq, head, column0, room, wave,
         [&](uint32_t i) {
             const uint32_t c = chunks - 1 - i;
             share.before(room.ops[i % 2], room.shares, wave, lane);
             if (i == 0 || c % (kMark / kChunk) == kMark / kChunk - 1)
-                store_memory<1>(d.dmarks + (((uint64_t)(first_slot(span, seq) + c / (kMark / kChunk)) * d.H + head) * d.Dk + row0) * d.Dv + col, rows, d.Dv, in, r8, share.S);
+                store_memory<Share<T, KS>::kOwn>(d.dmarks + (((uint64_t)(first_slot(span, seq) + c / (kMark / kChunk)) * d.H + head) * d.Dk + row0) * d.Dv + col, rows, d.Dv, in, r8, share.S);
         },
         [&](uint32_t i) { share.after(room.shares, i % 2, wave, lane); },
         [&](uint32_t i) {
-            if (i < chunks) make_ahead<T, KS>(room.ops[i % 2], room.tiles[i % 2], room.shares, wave - KS, lane);
-            gradient = room.shares.left[(i + 1) % 2][wave - KS][lane];
+            if (i < chunks) make_ahead<T, KS>(room.ops[i % 2], room.tiles[i % 2], room.shares, wave - kSharers<KS>, lane);
+            gradient = room.shares.left[(i + 1) % 2][wave - kSharers<KS>][lane];
         },
         [&](uint32_t i) {
-            if (i) store_four<float>(d.dr + head * d.Dv, (uint64_t)d.H * d.Dv, col, span, (chunks - i) * kChunk, r8, (wave - KS) * 4, column, gradient);
+            if (i) store_four<float>(d.dr + head * d.Dv, (uint64_t)d.H * d.Dv, col, span, (chunks - i) * kChunk, r8, (wave - kSharers<KS>) * 4, column, gradient);
         });
-    if (d.ds0) store_memory<1>(d.ds0 + memory, rows, d.Dv, in, r8, share.S);
+    if (d.ds0) store_memory<Share<T, KS>::kOwn>(d.ds0 + memory, rows, d.Dv, in, r8, share.S);
 }
 
 template <class T, int KS, bool kVec>
@@ -196,8 +206,8 @@ delta_bwd_kernel(Delta d, uint32_t with, uint32_t groups, uint64_t from)
 {
     __shared__ Room<T, KS> room;
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = blockDim.x / 64, c16 = lane % 16, r8 = lane / 16 * 8;
-    const uint64_t unit = from + blockIdx.x;
-    const uint32_t head = (uint32_t)(unit / groups % d.H), seq = (uint32_t)(unit / groups / d.H), col = (uint32_t)(unit % groups) * with * 16 + wave * 16 + c16;
+    const Unit unit(d, groups, from);
+    const uint32_t head = unit.head, seq = unit.seq, col = unit.group * with * 16 + wave * 16 + c16;
     const Span span = span_of(d, seq);
     const bool in = wave < with && col < d.Dv;
     const uint64_t memory = ((uint64_t)seq * d.H + head) * d.Dk * d.Dv + col;

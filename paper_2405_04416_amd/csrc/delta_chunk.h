@@ -229,16 +229,18 @@ __device__ __forceinline__ void along(const Delta &d, const Span &span, uint32_t
 }
 
 // ------------------------------------------------------------------------------ along a sequence, few heads
-// With fewer columns than the chip has room for, what bounds is how long a chunk takes a wavefront: so KS of them share 16 columns, with 32 rows of the memory each.  K S is then a sum
+// With fewer columns than the chip has room for, what bounds is how long a chunk takes a wavefront: so two of them share 16 columns, with up to 64 rows of the memory each.  K S is then a sum
 // over the wavefronts, which goes through LDS (Shares): a chunk has two halves, between barriers, what goes before the sum and what comes after.  All that the next chunk does not wait for
 // is done by others: two for what is made of a chunk's tokens (o, the gradients' part that does not depend on S), some that bring what all need, of rows in whole 16 bytes.
 constexpr int kShared = 16;             // columns
 constexpr int kAside = 2;
 
 template <int KS>
-constexpr int kHelpers = KS == 1 ? 2 : KS;
+constexpr int kSharers = KS == 1 ? 1 : 2;
 template <int KS>
-constexpr int kSharedWaves = KS + kAside + kHelpers<KS>;
+constexpr int kHelpers = KS == 4 ? 4 : 2;
+template <int KS>
+constexpr int kSharedWaves = kSharers<KS> + kAside + kHelpers<KS>;
 
 template <class T>
 struct alignas(16) Tile {
@@ -266,21 +268,16 @@ struct alignas(16) Tile {
 // What wavefronts hand each other; for those aside two buffers, since they are a chunk behind
 template <int KS, bool kBackward>
 struct alignas(16) Shares {
-    f32x4 keys[KS][2][64];                                      // K S
-    f32x4 queries[kBackward ? 1 : 2][kBackward ? 1 : KS][2][64];
+    f32x4 keys[kSharers<KS>][2][64];                            // K S
+    f32x4 queries[kBackward ? 1 : 2][kBackward ? 1 : kSharers<KS>][2][64];
     f32x4 left[2][kBackward ? 2 : 4][64];                       // what tokens miss (backward: gradients of what they write), what they write
     f32x4 ahead[kBackward ? 2 : 1][64];                         // backward: P^T dO
     u32x4 queried[kBackward ? 3 : 1][64];                       // scale e^G dO, in pieces
 
-    // all wavefronts' sum
-    __device__ __forceinline__ static f32x4 sum(const f32x4 (&of)[KS][2][64], int h, uint32_t lane)
+    __device__ __forceinline__ static f32x4 sum(const f32x4 (&of)[kSharers<KS>][2][64], int h, uint32_t lane)
     {
-        f32x4 v[KS];
-#pragma unroll
-        for (int s = 0; s < KS; ++s) v[s] = of[s][h][lane];
-        if constexpr (KS == 4) return (v[0] + v[1]) + (v[2] + v[3]);
-        else if constexpr (KS == 2) return v[0] + v[1];
-        else return v[0];
+        if constexpr (kSharers<KS> == 2) return of[0][h][lane] + of[1][h][lane];
+        else return of[0][h][lane];
     }
 };
 
@@ -357,7 +354,8 @@ __device__ __forceinline__ void along_helped(const Delta &d, const Span &span, u
 {
     const uint32_t chunks = (span.len + kChunk - 1) / kChunk, hk = head / (d.H / d.Hk);
     if (chunks == 0) return;
-    if (wave < KS) {
+    constexpr uint32_t kSharing = kSharers<KS>, kFirst = kSharing + kAside;
+    if (wave < kSharing) {
         __builtin_amdgcn_s_setprio(3);          // the others are to wait for these
         for (uint32_t i = 0; i < chunks; ++i) {
             __syncthreads();
@@ -368,7 +366,7 @@ __device__ __forceinline__ void along_helped(const Delta &d, const Span &span, u
         __syncthreads();
         return;
     }
-    if (wave < KS + kAside) {
+    if (wave < kFirst) {
         for (uint32_t i = 0; i < chunks; ++i) {
             __syncthreads();
             early(i);
@@ -381,7 +379,6 @@ __device__ __forceinline__ void along_helped(const Delta &d, const Span &span, u
         return;
     }
     using Help = Helper<T, KS, kBackward>;
-    constexpr uint32_t kFirst = KS + kAside;
     const Help h = {d, span, first_chunk(span, seq), head, threadIdx.x - kFirst * 64, column0,
                     {(const T *)d.q + hk * d.Dk, (const T *)d.k + hk * d.Dk, d.ldq, d.ldk, d.Dk, wave - kFirst, kHelpers<KS>, threadIdx.x % 64, span}};
     // A chunk is fetched two before it is put; `coming` holds the next one.  Without a branch about a load (behind the last chunk it comes again), so that a wait is for the oldest loads only.
@@ -408,6 +405,24 @@ __device__ __forceinline__ void along_helped(const Delta &d, const Span &span, u
     }
     __syncthreads();
 }
+
+// Which head (of all sequences) and group of columns a workgroup has.  Those of a head read the same operands: they get numbers that differ by 8, and so the same of the eight L2 caches.
+struct Unit {
+    uint32_t seq, head, group;
+    __device__ __forceinline__ Unit(const Delta &d, uint32_t groups, uint64_t from)
+    {
+        const uint64_t unit = from + blockIdx.x, heads = (uint64_t)d.n_seq * d.H, eights = heads / 8 * 8 * groups;
+        uint64_t of;
+        if (unit < eights) {
+            of = unit / (8 * groups) * 8 + unit % 8;
+            group = (uint32_t)(unit / 8 % groups);
+        } else {
+            of = unit / groups;
+            group = (uint32_t)(unit % groups);
+        }
+        seq = (uint32_t)(of / d.H), head = (uint32_t)(of % d.H);
+    }
+};
 
 // How many wavefronts of a workgroup have columns, how many there are (those that help among them), and how many workgroups a head has
 struct Columns { uint32_t with, waves, groups; bool helped; };

@@ -142,6 +142,23 @@ __device__ __forceinline__ f32x4 multiply(const bf16x8 (&a)[na], const bf16x8 (&
     return c;
 }
 
+// The same in two sums side by side, for where what bounds is how long one product waits for the one before
+template <int na, int nb>
+__device__ __forceinline__ f32x4 multiply_soon(const bf16x8 (&a)[na], const bf16x8 (&b)[nb], f32x4 c)
+{
+    f32x4 other = {};
+    int turn = 0;
+#pragma unroll
+    for (int i = 0; i < na; ++i)
+#pragma unroll
+        for (int j = 0; j < nb; ++j)
+            if (i + j < 3) {
+                if (turn++ % 2) other = mfma(a[i], b[j], other);
+                else c = mfma(a[i], b[j], c);
+            }
+    return c + other;
+}
+
 // ------------------------------------------------------------------------------ memory
 // The same number, of which the compiler does not know that it is: what follows from it is computed where it is needed, in place of being kept in registers (and
 // beyond them in memory) all along a loop.

@@ -72,53 +72,60 @@ __device__ __forceinline__ void take_chunk(const Operands<T, KS> &o, uint32_t c1
     }
 }
 
-// The same shared by KS wavefronts, rows 32 wave on each.
+// The same shared by wavefronts, rows 32 kOwn wave on each.
 template <class T, int KS>
 struct Share {
-    static constexpr int n = Pieces<T>::n;
-    f32x4 S[2];
-    bf16x8 inverse[2][3], turned[2][n];
+    static constexpr int n = Pieces<T>::n, kOwn = KS / kSharers<KS>;
+    f32x4 S[2 * kOwn];
+    bf16x8 queries[kOwn][2][n], sp[kOwn][3], inverse[2][3], turned[2 * kOwn][n];
     f32x4 read[2], beta[2], until[2];
     float value[8], whole;
 
-    // up to the sums K S and Q S; all that comes after them is read meanwhile
-    __device__ __forceinline__ void before(const Operands<T, KS> &o, const Tile<T> &tile, Shares<KS, false> &to, uint32_t parity, uint32_t wave, uint32_t lane)
+    // up to the sum K S; then all that comes after it is read
+    __device__ __forceinline__ void before(const Operands<T, KS> &o, const Tile<T> &tile, Shares<KS, false> &to, uint32_t wave, uint32_t lane)
     {
         const uint32_t c16 = lane % 16, r8 = lane / 16 * 8;
-        bf16x8 keys[2][n], queries[2][n], sp[3];
+        bf16x8 keys[kOwn][2][n];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) lefts(o.key.K, h * 16 + c16, wave * 32 + r8, keys[h]);
+        for (int s = 0; s < kOwn; ++s)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) lefts(o.key.Q, h * 16 + c16, wave * 32 + r8, queries[h]);
-        tile.read(lane, value);
+            for (int h = 0; h < 2; ++h) lefts(o.key.K, h * 16 + c16, (wave * kOwn + s) * 32 + r8, keys[s][h]);
+        __builtin_amdgcn_sched_barrier(0);
+        f32x4 sum[kOwn][2];
+#pragma unroll
+        for (int s = 0; s < kOwn; ++s) {
+            split_rows<3>(S[2 * s], S[2 * s + 1], sp[s]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) sum[s][h] = multiply<n, 3>(keys[s][h], sp[s], (f32x4){});
+        }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            read[h] = *reinterpret_cast<const f32x4 *>(&o.weight.read[r8 + h * 4]);
-            lefts(o.weight.inverse, h * 16 + c16, r8, inverse[h]);
+            if constexpr (kOwn == 2) sum[0][h] += sum[1][h];
+            to.keys[wave][h][lane] = sum[0][h];
         }
+        __builtin_amdgcn_sched_barrier(0);
+        tile.read(lane, value);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) read[h] = *reinterpret_cast<const f32x4 *>(&o.weight.read[r8 + h * 4]);
+#pragma unroll
+        for (int s = 0; s < kOwn; ++s)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) lefts(o.key.Q, h * 16 + c16, (wave * kOwn + s) * 32 + r8, queries[s][h]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) lefts(o.weight.inverse, h * 16 + c16, r8, inverse[h]);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             beta[h] = *reinterpret_cast<const f32x4 *>(&o.weight.beta[r8 + h * 4]);
             until[h] = *reinterpret_cast<const f32x4 *>(&o.weight.until[r8 + h * 4]);
-            lefts_turned(o.key.K, wave, h, lane, turned[h]);
         }
+#pragma unroll
+        for (int t = 0; t < 2 * kOwn; ++t) lefts_turned(o.key.K, wave * kOwn + t / 2, t % 2, lane, turned[t]);
         whole = o.weight.whole;
-        __builtin_amdgcn_sched_barrier(0);
-        split_rows<3>(S[0], S[1], sp);
-        f32x4 sum[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) sum[h] = multiply<n, 3>(keys[h], sp, (f32x4){});
-#pragma unroll
-        for (int h = 0; h < 2; ++h) to.keys[wave][h][lane] = sum[h];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) sum[h] = multiply<n, 3>(queries[h], sp, (f32x4){});
-#pragma unroll
-        for (int h = 0; h < 2; ++h) to.queries[parity][wave][h][lane] = sum[h];
     }
 
     __device__ __forceinline__ void after(Shares<KS, false> &shares, uint32_t parity, uint32_t wave, uint32_t lane)
     {
-        f32x4 r[2], u[2], y[2];
+        f32x4 r[2], u[2], y[2], qs[2] = {};
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const f32x4 ks = shares.sum(shares.keys, h, lane);
@@ -128,17 +135,25 @@ struct Share {
         bf16x8 right[3], written[3];
         split_rows<3>(r[0], r[1], right);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) y[h] = multiply<3, 3>(inverse[h], right, (f32x4){});
+        for (int h = 0; h < 2; ++h) y[h] = multiply_soon<3, 3>(inverse[h], right, (f32x4){});
+        // while that is on its way
+#pragma unroll
+        for (int s = 0; s < kOwn; ++s)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) qs[h] = multiply<n, 3>(queries[s][h], sp[s], qs[h]);
 #pragma unroll
         for (int h = 0; h < 2; ++h) u[h] = y[h] * beta[h];
         split_rows<3>(u[0] * until[0], u[1] * until[1], written);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) S[h] = multiply<n, 3>(turned[h], written, S[h] * whole);
-        // for those aside, from each wavefront a part
+        for (int t = 0; t < 2 * kOwn; ++t) S[t] = multiply<n, 3>(turned[t], written, S[t] * whole);
+        // for those aside
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            if (wave == (KS == 4 ? 2 + h : h % KS)) shares.left[parity][h][lane] = y[h];
-            if (wave == h % KS) shares.left[parity][2 + h][lane] = u[h];
+            shares.queries[parity][wave][h][lane] = qs[h];
+            if (wave == h % kSharers<KS>) {
+                shares.left[parity][h][lane] = y[h];
+                shares.left[parity][2 + h][lane] = u[h];
+            }
         }
     }
 };
@@ -171,30 +186,30 @@ delta_fwd_shared_kernel(Delta d, uint32_t groups, uint64_t from)
 {
     __shared__ Helped<T, KS, false> room;
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c16 = lane % 16, r8 = lane / 16 * 8;
-    const uint64_t unit = from + blockIdx.x;
-    const uint32_t head = (uint32_t)(unit / groups % d.H), seq = (uint32_t)(unit / groups / d.H), column0 = (uint32_t)(unit % groups) * kShared, col = column0 + c16;
+    const Unit unit(d, groups, from);
+    const uint32_t head = unit.head, seq = unit.seq, column0 = unit.group * kShared, col = column0 + c16;
     const Span span = span_of(d, seq);
-    const uint32_t row0 = wave * 32, rows = d.Dk > row0 ? d.Dk - row0 : 0;
-    const bool column = col < d.Dv, in = wave < KS && column;
+    const uint32_t row0 = wave * (Share<T, KS>::kOwn * 32), rows = d.Dk > row0 ? d.Dk - row0 : 0;
+    const bool column = col < d.Dv, in = wave < kSharers<KS> && column;
     const uint64_t memory = (((uint64_t)seq * d.H + head) * d.Dk + row0) * d.Dv + col;
     Share<T, KS> share;
     Outputs<T, KS> outputs;
-    load_memory<1>(d.s0 ? d.s0 + memory : nullptr, rows, d.Dv, in, r8, share.S);
+    load_memory<Share<T, KS>::kOwn>(d.s0 ? d.s0 + memory : nullptr, rows, d.Dv, in, r8, share.S);
     along_helped<T, KS, false>(d, span, seq, head, column0, room, wave,
         [&](uint32_t c) {
-            share.before(room.ops[c % 2], room.tiles[c % 2], room.shares, c % 2, wave, lane);
+            share.before(room.ops[c % 2], room.tiles[c % 2], room.shares, wave, lane);
             if (d.marks && c % (kMark / kChunk) == 0)
-                store_memory<1>(d.marks + (((uint64_t)(first_slot(span, seq) + c / (kMark / kChunk)) * d.H + head) * d.Dk + row0) * d.Dv + col, rows, d.Dv, in, r8, share.S);
+                store_memory<Share<T, KS>::kOwn>(d.marks + (((uint64_t)(first_slot(span, seq) + c / (kMark / kChunk)) * d.H + head) * d.Dk + row0) * d.Dv + col, rows, d.Dv, in, r8, share.S);
         },
         [&](uint32_t c) { share.after(room.shares, c % 2, wave, lane); },
-        [&](uint32_t c) { outputs.read(room.ops[(c + 1) % 2], room.shares, (c + 1) % 2, wave - KS, lane); },
+        [&](uint32_t c) { outputs.read(room.ops[(c + 1) % 2], room.shares, (c + 1) % 2, wave - kSharers<KS>, lane); },
         [&](uint32_t c) {
             if (c == 0) return;
-            const uint32_t t0 = (c - 1) * kChunk, h = wave - KS;
+            const uint32_t t0 = (c - 1) * kChunk, h = wave - kSharers<KS>;
             store_four<T>((T *)d.o + head * d.Dv, d.ldo, col, span, t0, r8, h * 4, column, outputs.make());
             if (d.y) store_four<float>(d.y + head * d.Dv, (uint64_t)d.H * d.Dv, col, span, t0, r8, h * 4, column, outputs.y);
         });
-    if (d.s_last) store_memory<1>(d.s_last + memory, rows, d.Dv, in, r8, share.S);
+    if (d.s_last) store_memory<Share<T, KS>::kOwn>(d.s_last + memory, rows, d.Dv, in, r8, share.S);
 }
 
 template <class T, int KS, bool kVec>
@@ -203,8 +218,8 @@ delta_fwd_kernel(Delta d, uint32_t with, uint32_t groups, uint64_t from)
 {
     __shared__ Room<T, KS> room;
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = blockDim.x / 64, c16 = lane % 16, r8 = lane / 16 * 8;
-    const uint64_t unit = from + blockIdx.x;
-    const uint32_t head = (uint32_t)(unit / groups % d.H), seq = (uint32_t)(unit / groups / d.H), col = (uint32_t)(unit % groups) * with * 16 + wave * 16 + c16;
+    const Unit unit(d, groups, from);
+    const uint32_t head = unit.head, seq = unit.seq, col = unit.group * with * 16 + wave * 16 + c16;
     const Span span = span_of(d, seq);
     const bool in = wave < with && col < d.Dv;
     const uint64_t memory = ((uint64_t)seq * d.H + head) * d.Dk * d.Dv + col;
