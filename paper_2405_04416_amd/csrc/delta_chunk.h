@@ -269,7 +269,7 @@ struct alignas(16) Tile {
 template <int KS, bool kBackward>
 struct alignas(16) Shares {
     f32x4 keys[kSharers<KS>][2][64];                            // K S
-    f32x4 queries[kBackward ? 1 : 2][kBackward ? 1 : kSharers<KS>][2][64];
+    u32x4 memory[kBackward ? 1 : KS][kBackward ? 1 : 3][64];    // forward: S in pieces
     f32x4 left[2][kBackward ? 2 : 4][64];                       // what tokens miss (backward: gradients of what they write), what they write
     f32x4 ahead[kBackward ? 2 : 1][64];                         // backward: P^T dO
     u32x4 queried[kBackward ? 3 : 1][64];                       // scale e^G dO, in pieces
@@ -392,17 +392,20 @@ __device__ __forceinline__ void along_helped(const Delta &d, const Span &span, u
         h.put_tile(chunk(i + 1), coming, room.tiles[(i + 1) % 2]);
         __syncthreads();
         h.put_operands(chunk(i + 1), coming, room.ops[(i + 1) % 2]);
+        __builtin_amdgcn_sched_barrier(0);          // loads ahead of the stores would go to other registers, which would be copied, and waited for, at once
         h.fetch(chunk(i + 3), coming);
+        __builtin_amdgcn_sched_barrier(0);
     };
     h.fetch(chunk(0), held[0]);
     h.fetch(chunk(1), held[1]);
     h.put_tile(chunk(0), held[0], room.tiles[0]);
     h.put_operands(chunk(0), held[0], room.ops[0]);
     h.fetch(chunk(2), held[0]);
-    for (uint32_t i = 0; i < chunks; i += 2) {
+    for (uint32_t i = 0; i + 1 < chunks; i += 2) {
         turn(i, held[1]);
-        if (i + 1 < chunks) turn(i + 1, held[0]);
+        turn(i + 1, held[0]);
     }
+    if (chunks % 2) turn(chunks - 1, held[1]);
     __syncthreads();
 }
 

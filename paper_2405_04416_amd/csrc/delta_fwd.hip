@@ -77,7 +77,7 @@ template <class T, int KS>
 struct Share {
     static constexpr int n = Pieces<T>::n, kOwn = KS / kSharers<KS>;
     f32x4 S[2 * kOwn];
-    bf16x8 queries[kOwn][2][n], sp[kOwn][3], inverse[2][3], turned[2 * kOwn][n];
+    bf16x8 inverse[2][3], turned[2 * kOwn][n];
     f32x4 read[2], beta[2], until[2];
     float value[8], whole;
 
@@ -85,7 +85,7 @@ struct Share {
     __device__ __forceinline__ void before(const Operands<T, KS> &o, const Tile<T> &tile, Shares<KS, false> &to, uint32_t wave, uint32_t lane)
     {
         const uint32_t c16 = lane % 16, r8 = lane / 16 * 8;
-        bf16x8 keys[kOwn][2][n];
+        bf16x8 keys[kOwn][2][n], sp[kOwn][3];
 #pragma unroll
         for (int s = 0; s < kOwn; ++s)
 #pragma unroll
@@ -103,14 +103,14 @@ struct Share {
             if constexpr (kOwn == 2) sum[0][h] += sum[1][h];
             to.keys[wave][h][lane] = sum[0][h];
         }
+#pragma unroll
+        for (int s = 0; s < kOwn; ++s)
+#pragma unroll
+            for (int p = 0; p < 3; ++p) to.memory[wave * kOwn + s][p][lane] = __builtin_bit_cast(u32x4, sp[s][p]);
         __builtin_amdgcn_sched_barrier(0);
         tile.read(lane, value);
 #pragma unroll
         for (int h = 0; h < 2; ++h) read[h] = *reinterpret_cast<const f32x4 *>(&o.weight.read[r8 + h * 4]);
-#pragma unroll
-        for (int s = 0; s < kOwn; ++s)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) lefts(o.key.Q, h * 16 + c16, (wave * kOwn + s) * 32 + r8, queries[s][h]);
 #pragma unroll
         for (int h = 0; h < 2; ++h) lefts(o.weight.inverse, h * 16 + c16, r8, inverse[h]);
 #pragma unroll
@@ -125,7 +125,7 @@ struct Share {
 
     __device__ __forceinline__ void after(Shares<KS, false> &shares, uint32_t parity, uint32_t wave, uint32_t lane)
     {
-        f32x4 r[2], u[2], y[2], qs[2] = {};
+        f32x4 r[2], u[2], y[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const f32x4 ks = shares.sum(shares.keys, h, lane);
@@ -136,11 +136,6 @@ struct Share {
         split_rows<3>(r[0], r[1], right);
 #pragma unroll
         for (int h = 0; h < 2; ++h) y[h] = multiply_soon<3, 3>(inverse[h], right, (f32x4){});
-        // while that is on its way
-#pragma unroll
-        for (int s = 0; s < kOwn; ++s)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) qs[h] = multiply<n, 3>(queries[s][h], sp[s], qs[h]);
 #pragma unroll
         for (int h = 0; h < 2; ++h) u[h] = y[h] * beta[h];
         split_rows<3>(u[0] * until[0], u[1] * until[1], written);
@@ -148,35 +143,45 @@ struct Share {
         for (int t = 0; t < 2 * kOwn; ++t) S[t] = multiply<n, 3>(turned[t], written, S[t] * whole);
         // for those aside
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            shares.queries[parity][wave][h][lane] = qs[h];
+        for (int h = 0; h < 2; ++h)
             if (wave == h % kSharers<KS>) {
                 shares.left[parity][h][lane] = y[h];
                 shares.left[parity][2 + h][lane] = u[h];
             }
-        }
     }
 };
 
-// o of 16 of a chunk's tokens, and what they miss
+// o of 16 of a chunk's tokens, and what they miss: Q S while the chunk is under way, the rest when it is done
 template <class T, int KS>
 struct Outputs {
+    static constexpr int n = Pieces<T>::n;
     bf16x8 pull[3];
-    f32x4 u[2], y, query, qs;
+    f32x4 u[2], y, qs;
 
-    __device__ __forceinline__ void read(const Operands<T, KS> &o, const Shares<KS, false> &shares, uint32_t parity, uint32_t h, uint32_t lane)
+    __device__ __forceinline__ void query(const Operands<T, KS> &o, const Shares<KS, false> &shares, uint32_t h, uint32_t lane)
     {
         const uint32_t c16 = lane % 16, r8 = lane / 16 * 8;
-        lefts(o.weight.P, h * 16 + c16, r8, pull);
-        query = *reinterpret_cast<const f32x4 *>(&o.weight.query[r8 + h * 4]);
+        f32x4 sum[2] = {};
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            bf16x8 queries[n], sp[3];
+            lefts(o.key.Q, h * 16 + c16, s * 32 + r8, queries);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) sp[p] = operand(shares.memory[s][p][lane]);
+            sum[s % 2] = multiply<n, 3>(queries, sp, sum[s % 2]);
+        }
+        qs = (sum[0] + sum[1]) * *reinterpret_cast<const f32x4 *>(&o.weight.query[r8 + h * 4]);
+    }
+    __device__ __forceinline__ void read(const Operands<T, KS> &o, const Shares<KS, false> &shares, uint32_t parity, uint32_t h, uint32_t lane)
+    {
+        lefts(o.weight.P, h * 16 + lane % 16, lane / 16 * 8, pull);
         u[0] = shares.left[parity][2][lane], u[1] = shares.left[parity][3][lane], y = shares.left[parity][h][lane];
-        qs = shares.sum(shares.queries[parity], h, lane);
     }
     __device__ __forceinline__ f32x4 make() const
     {
         bf16x8 right[3];
         split_rows<3>(u[0], u[1], right);
-        return multiply<3, 3>(pull, right, query * qs);
+        return multiply_soon<3, 3>(pull, right, qs);
     }
 };
 
@@ -189,7 +194,7 @@ delta_fwd_shared_kernel(Delta d, uint32_t groups, uint64_t from)
     const Unit unit(d, groups, from);
     const uint32_t head = unit.head, seq = unit.seq, column0 = unit.group * kShared, col = column0 + c16;
     const Span span = span_of(d, seq);
-    const uint32_t row0 = wave * (Share<T, KS>::kOwn * 32), rows = d.Dk > row0 ? d.Dk - row0 : 0;
+    const uint32_t row0 = wave * (Share<T, KS>::kOwn * 32), rows = d.Dk > row0 ? d.Dk - row0 : 0, chunks = (span.len + kChunk - 1) / kChunk;
     const bool column = col < d.Dv, in = wave < kSharers<KS> && column;
     const uint64_t memory = (((uint64_t)seq * d.H + head) * d.Dk + row0) * d.Dv + col;
     Share<T, KS> share;
@@ -204,10 +209,12 @@ delta_fwd_shared_kernel(Delta d, uint32_t groups, uint64_t from)
         [&](uint32_t c) { share.after(room.shares, c % 2, wave, lane); },
         [&](uint32_t c) { outputs.read(room.ops[(c + 1) % 2], room.shares, (c + 1) % 2, wave - kSharers<KS>, lane); },
         [&](uint32_t c) {
-            if (c == 0) return;
             const uint32_t t0 = (c - 1) * kChunk, h = wave - kSharers<KS>;
-            store_four<T>((T *)d.o + head * d.Dv, d.ldo, col, span, t0, r8, h * 4, column, outputs.make());
-            if (d.y) store_four<float>(d.y + head * d.Dv, (uint64_t)d.H * d.Dv, col, span, t0, r8, h * 4, column, outputs.y);
+            if (c) {
+                store_four<T>((T *)d.o + head * d.Dv, d.ldo, col, span, t0, r8, h * 4, column, outputs.make());
+                if (d.y) store_four<float>(d.y + head * d.Dv, (uint64_t)d.H * d.Dv, col, span, t0, r8, h * 4, column, outputs.y);
+            }
+            if (c < chunks) outputs.query(room.ops[c % 2], room.shares, h, lane);
         });
     if (d.s_last) store_memory<Share<T, KS>::kOwn>(d.s_last + memory, rows, d.Dv, in, r8, share.S);
 }
