@@ -3,7 +3,9 @@
 //
 // Forward, and backward along the sequences (dR of what tokens write, with it dv, dbeta): columns.  Then, with what tokens write and its gradient known,
 // 64 tokens at a time: rows, once forward (dq, and what dk owes to the memory that was read), once backward (what dk owes to the memory that is written).
-// Bound by the vector units: four operations per value of the memory and token in each of the four sweeps.
+// Bound by the vector units: four operations per value of the memory and token in each of the four sweeps.  Vectors that all lanes of a head need lie over 16 lanes, from which
+// the multiplication takes each value itself (when every lane loaded all of them, the first-level cache was what bounded).
+#include <utility>
 #include "delta_common.h"
 #include "rows_vectors.h"
 
@@ -11,52 +13,65 @@ namespace {
 
 using namespace dg_delta;
 
-// P values of a row of D that all lanes of a head read; D is P if kFull
-template <class T, int P, bool kFull, bool kVec>
+constexpr int kAhead = 4;               // tokens that are loaded before they are needed
+
+template <class F, int... I>
+__device__ __forceinline__ void each(std::integer_sequence<int, I...>, F f) { (f(std::integral_constant<int, I>{}), ...); }
+template <int n, class F>
+__device__ __forceinline__ void each(F f) { each(std::make_integer_sequence<int, n>{}, f); }
+
+// P values that all lanes of a head need: lane l of 16 has l, l + 16, ...; 0 from D on
+template <class T, int P>
 struct Vector {
-    T v[P];
+    T v[P / 16];
     __device__ __forceinline__ void load(const T *row, uint32_t D)
     {
-        constexpr int m = 16 / sizeof(T);
-        if constexpr (kVec) {
 #pragma unroll
-            for (int i = 0; i < P; i += m) {
-                const dg_rows::Pack<T, m> p = *reinterpret_cast<const dg_rows::Pack<T, m> *>(row + (kFull || i < (int)D ? i : 0));
-#pragma unroll
-                for (int j = 0; j < m; ++j) v[i + j] = p.v[j];
-            }
-        } else
-#pragma unroll
-            for (int i = 0; i < P; ++i) v[i] = row[kFull || i < (int)D ? i : 0];
+        for (int i = 0; i < P / 16; ++i) {
+            const uint32_t c = i * 16 + threadIdx.x % 16;
+            v[i] = row[c < D ? c : 0];
+        }
     }
-    // behind D something else was loaded, so that nothing waits for the load
-    __device__ __forceinline__ float at(int i, uint32_t D) const { return kFull || i < (int)D ? (float)v[i] : 0.0f; }
+};
+
+// the same in fp32, cleared from D on
+template <int P>
+struct Spread {
+    float v[P / 16];
+    template <class T>
+    __device__ __forceinline__ Spread(const Vector<T, P> &from, uint32_t D)
+    {
+#pragma unroll
+        for (int i = 0; i < P / 16; ++i) v[i] = i * 16 + threadIdx.x % 16 < D ? (float)from.v[i] : 0.0f;
+    }
+    template <int i>
+    __device__ __forceinline__ float at() const
+    {
+        return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v[i / 16]), 0x150 + i % 16, 0xf, 0xf, true));       // value i % 16 of the row's lanes
+    }
 };
 
 // sum of products, in four parts
-template <class T, int P, bool kFull, bool kVec>
-__device__ __forceinline__ float dot(const float (&a)[P], const Vector<T, P, kFull, kVec> &b, uint32_t D)
+template <int P>
+__device__ __forceinline__ float dot(const float (&a)[P], const Spread<P> &b)
 {
     float part[4] = {};
-#pragma unroll
-    for (int i = 0; i < P; ++i) part[i % 4] = fmaf(a[i], b.at(i, D), part[i % 4]);
+    each<P>([&](auto i) { part[i % 4] = fmaf(b.template at<i>(), a[i], part[i % 4]); });
     return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
 // a <- a f + b s
-template <class T, int P, bool kFull, bool kVec>
-__device__ __forceinline__ void step(float (&a)[P], float f, const Vector<T, P, kFull, kVec> &b, float s, uint32_t D)
+template <int P>
+__device__ __forceinline__ void step(float (&a)[P], float f, const Spread<P> &b, float s)
 {
-#pragma unroll
-    for (int i = 0; i < P; ++i) a[i] = fmaf(b.at(i, D), s, a[i] * f);
+    each<P>([&](auto i) { a[i] = fmaf(b.template at<i>(), s, a[i] * f); });
 }
 
 // a <- a + b s
-template <class T, int P, bool kFull, bool kVec>
-__device__ __forceinline__ void add(float (&a)[P], const Vector<T, P, kFull, kVec> &b, float s, uint32_t D)
+template <int P>
+__device__ __forceinline__ void add(float (&a)[P], const Spread<P> &b, float s)
 {
-#pragma unroll
-    for (int i = 0; i < P; ++i) a[i] = fmaf(b.at(i, D), s, a[i]);
+    each<P>([&](auto i) { a[i] = fmaf(b.template at<i>(), s, a[i]); });
 }
 
 // a place in rows that goes from token to token
@@ -67,6 +82,32 @@ struct Walk {
     __device__ __forceinline__ Walk(T *base, uint64_t ld, const Span &span, uint32_t t, bool back) : p(base + span.row(t) * ld), step((span.turn < 0) != back ? -(int64_t)ld : (int64_t)ld) {}
     __device__ __forceinline__ void next() { p += step; }
 };
+
+// use(token) for count tokens, each fetched kAhead before: fetch() loads what the places point at, go() moves these on.  No branch about a load (behind the last token it comes again), so that
+// a wait is for the oldest loads only.
+template <class Token, class Fetch, class Go, class Use>
+__device__ __forceinline__ void along_tokens(uint32_t count, Fetch fetch, Go go, Use use)
+{
+    Token ahead[kAhead];
+    uint32_t at = 0;                    // of the token that is fetched next
+    auto get = [&](Token &to) {
+        fetch(to);
+        if (++at < count) go();
+    };
+    each<kAhead>([&](auto i) { get(ahead[i]); });
+    uint32_t t = 0;
+    for (; t + kAhead <= count; t += kAhead)
+        each<kAhead>([&](auto i) {
+            const Token now = ahead[i];
+            __builtin_amdgcn_sched_barrier(0);
+            get(ahead[i]);
+            __builtin_amdgcn_sched_barrier(0);
+            use(t + i, now);
+        });
+    each<kAhead - 1>([&](auto i) {
+        if (t + i < count) use(t + i, ahead[i]);
+    });
+}
 
 // A lane's place among the heads of all sequences: sequence, head, column
 struct Place {
@@ -81,77 +122,76 @@ struct Place {
     }
 };
 
-template <class T, int PK, int PV, bool kFull, bool kVec>
+template <class T, int PK, int PV>
 __global__ void __launch_bounds__(64)
 delta_small_fwd_kernel(Delta d, uint64_t from)
 {
     const Place at = Place::of<PV>(d, from);
     const Span span = span_of(d, at.seq);
-    const uint32_t hk = at.head / (d.H / d.Hk), c = kFull || at.column < d.Dv ? at.column : 0, ldy = d.H * d.Dv;
-    const bool in = at.in && (kFull || at.column < d.Dv);
+    const uint32_t hk = at.head / (d.H / d.Hk), c = at.column < d.Dv ? at.column : 0, ldy = d.H * d.Dv;
+    const bool in = at.in && at.column < d.Dv;
     const uint32_t len = at.in ? span.len : 0;
     const uint64_t memory = ((uint64_t)at.seq * d.H + at.head) * d.Dk * d.Dv + c;
     float S[PK];
 #pragma unroll
-    for (int r = 0; r < PK; ++r) S[r] = d.s0 && in && (kFull || r < (int)d.Dk) ? d.s0[memory + (uint64_t)r * d.Dv] : 0.0f;
+    for (int r = 0; r < PK; ++r) S[r] = d.s0 && in && r < (int)d.Dk ? d.s0[memory + (uint64_t)r * d.Dv] : 0.0f;
     if (len) {
         Walk<const T> K((const T *)d.k + hk * d.Dk, d.ldk, span, 0, false), Q((const T *)d.q + hk * d.Dk, d.ldq, span, 0, false), V((const T *)d.v + at.head * d.Dv + c, d.ldv, span, 0, false);
         Walk<const float> G(d.g + at.head, d.ldg, span, 0, false), B(d.beta + at.head, d.ldb, span, 0, false);
         Walk<T> O((T *)d.o + at.head * d.Dv + c, d.ldo, span, 0, false);
         Walk<float> Y(d.y + at.head * d.Dv + c, ldy, span, 0, false);
         float *mark = d.marks + ((uint64_t)first_slot(span, at.seq) * d.H + at.head) * d.Dk * d.Dv + c;
-        Vector<T, PK, kFull, kVec> k, q, next_k, next_q;
-        next_k.load(K.p, d.Dk);
-        next_q.load(Q.p, d.Dk);
-        T next_v = *V.p;
-        float next_g = *G.p, next_beta = *B.p;
-        for (uint32_t t = 0; t < len; ++t) {
-            k = next_k, q = next_q;
-            const T v = next_v;
-            const float a = expf(next_g), beta = next_beta;
-            if (t + 1 < len) {
-                K.next(), Q.next(), V.next(), G.next(), B.next();
-                next_k.load(K.p, d.Dk);
-                next_q.load(Q.p, d.Dk);
-                next_v = *V.p, next_g = *G.p, next_beta = *B.p;
-            }
-            if (d.marks && t % kMark == 0) {
-                if (in)
+        struct Token {
+            Vector<T, PK> k, q;
+            T v;
+            float g, beta;
+        };
+        along_tokens<Token>(len,
+            [&](Token &to) {
+                to.k.load(K.p, d.Dk);
+                to.q.load(Q.p, d.Dk);
+                to.v = *V.p, to.g = *G.p, to.beta = *B.p;
+            },
+            [&] { K.next(), Q.next(), V.next(), G.next(), B.next(); },
+            [&](uint32_t t, const Token &now) {
+                if (d.marks && t % kMark == 0) {
+                    if (in)
 #pragma unroll
-                    for (int r = 0; r < PK; ++r)
-                        if (kFull || r < (int)d.Dk) mark[(uint64_t)r * d.Dv] = S[r];
-                mark += (uint64_t)d.H * d.Dk * d.Dv;
-            }
-            const float y = (float)v - a * dot(S, k, d.Dk);
-            step(S, a, k, beta * y, d.Dk);
-            const float o = d.scale * dot(S, q, d.Dk);
-            if (in) {
-                *O.p = (T)o;
-                if (d.y) *Y.p = y;
-            }
-            O.next(), Y.next();
-        }
+                        for (int r = 0; r < PK; ++r)
+                            if (r < (int)d.Dk) mark[(uint64_t)r * d.Dv] = S[r];
+                    mark += (uint64_t)d.H * d.Dk * d.Dv;
+                }
+                const Spread<PK> k(now.k, d.Dk), q(now.q, d.Dk);
+                const float a = expf(now.g), y = (float)now.v - a * dot(S, k);
+                step(S, a, k, now.beta * y);
+                const float o = d.scale * dot(S, q);
+                if (in) {
+                    *O.p = (T)o;
+                    if (d.y) *Y.p = y;
+                }
+                O.next(), Y.next();
+            });
     }
     if (d.s_last && in)
 #pragma unroll
         for (int r = 0; r < PK; ++r)
-            if (kFull || r < (int)d.Dk) d.s_last[memory + (uint64_t)r * d.Dv] = S[r];
+            if (r < (int)d.Dk) d.s_last[memory + (uint64_t)r * d.Dv] = S[r];
 }
 
 // dS of a token: + scale q do^T;  dR = dS^T k;  - k (beta dR)^T;  e^g dS goes to the token before.  dg gets v dv, for what follows.
-template <class T, int PK, int PV, bool kFull, bool kVec>
+template <class T, int PK, int PV>
 __global__ void __launch_bounds__(64)
 delta_small_bwd_kernel(Delta d, uint64_t from)
 {
     const Place at = Place::of<PV>(d, from);
     const Span span = span_of(d, at.seq);
-    const uint32_t hk = at.head / (d.H / d.Hk), c = kFull || at.column < d.Dv ? at.column : 0, ldy = d.H * d.Dv;
-    const bool in = at.in && (kFull || at.column < d.Dv);
+    const uint32_t hk = at.head / (d.H / d.Hk), c = at.column < d.Dv ? at.column : 0, ldy = d.H * d.Dv;
+    const bool in = at.in && at.column < d.Dv;
     const uint32_t len = at.in ? span.len : 0, last = len ? len - 1 : 0;
     const uint64_t memory = ((uint64_t)at.seq * d.H + at.head) * d.Dk * d.Dv + c;
     float S[PK];
 #pragma unroll
-    for (int r = 0; r < PK; ++r) S[r] = d.ds_last && in && (kFull || r < (int)d.Dk) ? d.ds_last[memory + (uint64_t)r * d.Dv] : 0.0f;
+    for (int r = 0; r < PK; ++r) S[r] = d.ds_last && in && r < (int)d.Dk ? d.ds_last[memory + (uint64_t)r * d.Dv] : 0.0f;
     if (len) {
         Walk<const T> K((const T *)d.k + hk * d.Dk, d.ldk, span, last, true), Q((const T *)d.q + hk * d.Dk, d.ldq, span, last, true);
         Walk<const T> V((const T *)d.v + at.head * d.Dv + c, d.ldv, span, last, true), O((const T *)d.dout + at.head * d.Dv + c, d.lddo, span, last, true);
@@ -159,53 +199,52 @@ delta_small_bwd_kernel(Delta d, uint64_t from)
         Walk<T> dV((T *)d.dv + at.head * d.Dv + c, d.lddv, span, last, true);
         Walk<float> R(d.dr + at.head * d.Dv + c, ldy, span, last, true), dB(d.dbeta + at.head, d.lddb, span, last, true), dG(d.dg + at.head, d.lddg, span, last, true);
         float *mark = d.dmarks + ((uint64_t)(first_slot(span, at.seq) + last / kMark) * d.H + at.head) * d.Dk * d.Dv + c;
-        Vector<T, PK, kFull, kVec> k, q, next_k, next_q;
-        next_k.load(K.p, d.Dk);
-        next_q.load(Q.p, d.Dk);
-        T next_v = *V.p, next_o = *O.p;
-        float next_g = *G.p, next_beta = *B.p, next_y = *Y.p;
-        for (uint32_t t = last;; --t) {
-            k = next_k, q = next_q;
-            const T v = next_v, o = next_o;
-            const float a = expf(next_g), beta = next_beta, y = next_y;
-            if (t) {
-                K.next(), Q.next(), V.next(), O.next(), G.next(), B.next(), Y.next();
-                next_k.load(K.p, d.Dk);
-                next_q.load(Q.p, d.Dk);
-                next_v = *V.p, next_o = *O.p, next_g = *G.p, next_beta = *B.p, next_y = *Y.p;
-            }
-            if (t % kMark == kMark - 1 || t == last) {
-                if (in)
+        struct Token {
+            Vector<T, PK> k, q;
+            T v, o;
+            float g, beta, y;
+        };
+        along_tokens<Token>(len,
+            [&](Token &to) {
+                to.k.load(K.p, d.Dk);
+                to.q.load(Q.p, d.Dk);
+                to.v = *V.p, to.o = *O.p, to.g = *G.p, to.beta = *B.p, to.y = *Y.p;
+            },
+            [&] { K.next(), Q.next(), V.next(), O.next(), G.next(), B.next(), Y.next(); },
+            [&](uint32_t i, const Token &now) {
+                const uint32_t t = last - i;
+                if (t % kMark == kMark - 1 || i == 0) {
+                    if (in)
 #pragma unroll
-                    for (int r = 0; r < PK; ++r)
-                        if (kFull || r < (int)d.Dk) mark[(uint64_t)r * d.Dv] = S[r];
-                mark -= (uint64_t)d.H * d.Dk * d.Dv;
-            }
-            add(S, q, d.scale * (in ? (float)o : 0.0f), d.Dk);
-            const float dr = dot(S, k, d.Dk), dv = beta * dr;
-            step(S, a, k, -a * dv, d.Dk);
-            // the lanes of a head go through the same tokens: all of them are here
-            const float dbeta = dg_rows::group_sum<PV>(in ? dr * y : 0.0f), values = dg_rows::group_sum<PV>(in ? dv * (float)v : 0.0f);
-            if (in) {
-                *R.p = dr;
-                *dV.p = (T)dv;
-                if (at.column == 0) {
-                    *dB.p = dbeta;
-                    *dG.p = values;
+                        for (int r = 0; r < PK; ++r)
+                            if (r < (int)d.Dk) mark[(uint64_t)r * d.Dv] = S[r];
+                    mark -= (uint64_t)d.H * d.Dk * d.Dv;
                 }
-            }
-            R.next(), dV.next(), dB.next(), dG.next();
-            if (t == 0) break;
-        }
+                const Spread<PK> k(now.k, d.Dk), q(now.q, d.Dk);
+                add(S, q, d.scale * (in ? (float)now.o : 0.0f));
+                const float a = expf(now.g), dr = dot(S, k), dv = now.beta * dr;
+                step(S, a, k, -a * dv);
+                // the lanes of a head go through the same tokens: all of them are here
+                const float dbeta = dg_rows::group_sum<PV>(in ? dr * now.y : 0.0f), values = dg_rows::group_sum<PV>(in ? dv * (float)now.v : 0.0f);
+                if (in) {
+                    *R.p = dr;
+                    *dV.p = (T)dv;
+                    if (at.column == 0) {
+                        *dB.p = dbeta;
+                        *dG.p = values;
+                    }
+                }
+                R.next(), dV.next(), dB.next(), dG.next();
+            });
     }
     if (d.ds0 && in)
 #pragma unroll
         for (int r = 0; r < PK; ++r)
-            if (kFull || r < (int)d.Dk) d.ds0[memory + (uint64_t)r * d.Dv] = S[r];
+            if (r < (int)d.Dk) d.ds0[memory + (uint64_t)r * d.Dv] = S[r];
 }
 
 // Rows: 64 tokens of a key head, one of its value heads after the other
-template <class T, int PK, int PV, bool kShared, bool kFull, bool kVec>
+template <class T, int PK, int PV, bool kShared>
 __global__ void __launch_bounds__(64)
 delta_small_grad_kernel(Delta d, uint64_t from)
 {
@@ -238,10 +277,13 @@ delta_small_grad_kernel(Delta d, uint64_t from)
     for (uint32_t h = 0; h < group; ++h) {
         const uint32_t head = hk * group + h;
         const uint64_t memory = ((slot * d.H + head) * d.Dk + r) * d.Dv;
-        Vector<float, PV, kFull, kVec> w, next_y, next_r, y, dr;
-        Vector<T, PV, kFull, kVec> next_o, o;
-        T next_k, next_q;
-        float next_g, next_beta, S[PV], end = 0.0f;
+        float S[PV], end = 0.0f;
+        struct Token {
+            Vector<float, PV> y, dr;
+            Vector<T, PV> o;
+            T k, q;
+            float g, beta;
+        };
         struct Rows {
             Walk<const float> Y, R, G, B;
             Walk<const T> O, K, Q;
@@ -249,60 +291,50 @@ delta_small_grad_kernel(Delta d, uint64_t from)
                 : Y(d.y + head * d.Dv, ldy, span, t, back), R(d.dr + head * d.Dv, ldy, span, t, back), G(d.g + head, d.ldg, span, t, back), B(d.beta + head, d.ldb, span, t, back),
                   O((const T *)d.dout + head * d.Dv, d.lddo, span, t, back), K((const T *)d.k + column, d.ldk, span, t, back), Q((const T *)d.q + column, d.ldq, span, t, back) {}
             __device__ __forceinline__ void next() { Y.next(), R.next(), G.next(), B.next(), O.next(), K.next(), Q.next(); }
-        };
-        auto fetch = [&](const Rows &at) {
-            next_y.load(at.Y.p, d.Dv);
-            next_r.load(at.R.p, d.Dv);
-            next_o.load(at.O.p, d.Dv);
-            next_k = *at.K.p, next_q = *at.Q.p, next_g = *at.G.p, next_beta = *at.B.p;
+            __device__ __forceinline__ void fetch(Token &to, uint32_t Dv) const
+            {
+                to.y.load(Y.p, Dv);
+                to.dr.load(R.p, Dv);
+                to.o.load(O.p, Dv);
+                to.k = *K.p, to.q = *Q.p, to.g = *G.p, to.beta = *B.p;
+            }
         };
         {
             Rows at(d, span, t0, false, head, hk * d.Dk + r, ldy);
             Walk<T> dQ((T *)d.dq + hk * d.Dk + r, d.lddq, span, t0, false);
-            w.load(d.marks + memory, d.Dv);
-            fetch(at);
 #pragma unroll
-            for (int i = 0; i < PV; ++i) S[i] = in ? w.at(i, d.Dv) : 0.0f;
-            for (uint32_t t = 0; t < count; ++t) {
-                const float k = in ? (float)next_k : 0.0f, q = in ? (float)next_q : 0.0f, beta = next_beta, a = expf(next_g);
-                y = next_y, dr = next_r, o = next_o;
-                if (t + 1 < count) {
-                    at.next();
-                    fetch(at);
-                }
-                const float read = -beta * a * dot(S, dr, d.Dv);
-                step(S, a, y, k * beta, d.Dv);
-                float dq = d.scale * dot(S, o, d.Dv);
+            for (int i = 0; i < PV; ++i) S[i] = in && i < (int)d.Dv ? d.marks[memory + i] : 0.0f;
+            along_tokens<Token>(count, [&](Token &to) { at.fetch(to, d.Dv); }, [&] { at.next(); }, [&](uint32_t t, const Token &now) {
+                const float k = in ? (float)now.k : 0.0f, q = in ? (float)now.q : 0.0f, a = expf(now.g);
+                const Spread<PV> y(now.y, d.Dv), dr(now.dr, d.Dv), o(now.o, d.Dv);
+                const float read = -now.beta * a * dot(S, dr);
+                step(S, a, y, k * now.beta);
+                float dq = d.scale * dot(S, o);
                 const float all = dg_rows::group_sum<PK>(q * dq);
                 if (lane % PK == 0) lds_end[t][lane / PK] = all;
                 lds_k[t][lane] = kShared && h ? lds_k[t][lane] + read : read;
                 if (kShared) lds_q[t][lane] = dq = h ? lds_q[t][lane] + dq : dq;
                 if (h + 1 == group && in) *dQ.p = (T)dq;
                 dQ.next();
-            }
+            });
         }
         Rows at(d, span, last, true, head, hk * d.Dk + r, ldy);
         Walk<T> dK((T *)d.dk + hk * d.Dk + r, d.lddk, span, last, true);
         Walk<float> dG(d.dg + head, d.lddg, span, last, true);
-        w.load(d.dmarks + memory, d.Dv);
-        fetch(at);
         float dS[PV];
 #pragma unroll
         for (int i = 0; i < PV; ++i) {
-            dS[i] = in ? w.at(i, d.Dv) : 0.0f;
+            dS[i] = in && i < (int)d.Dv ? d.dmarks[memory + i] : 0.0f;
             end = fmaf(S[i], dS[i], end);
         }
         end = dg_rows::group_sum<PK>(end);
-        for (uint32_t t = count - 1;; --t) {
-            const float k = in ? (float)next_k : 0.0f, q = in ? (float)next_q : 0.0f, beta = next_beta, a = expf(next_g);
-            y = next_y, dr = next_r, o = next_o;
-            if (t) {
-                at.next();
-                fetch(at);
-            }
-            add(dS, o, d.scale * q, d.Dv);
-            const float dk = fmaf(beta, dot(dS, y, d.Dv), lds_k[t][lane]);
-            step(dS, a, dr, -a * beta * k, d.Dv);
+        along_tokens<Token>(count, [&](Token &to) { at.fetch(to, d.Dv); }, [&] { at.next(); }, [&](uint32_t i, const Token &now) {
+            const uint32_t t = count - 1 - i;
+            const float k = in ? (float)now.k : 0.0f, q = in ? (float)now.q : 0.0f, a = expf(now.g);
+            const Spread<PV> y(now.y, d.Dv), dr(now.dr, d.Dv), o(now.o, d.Dv);
+            add(dS, o, d.scale * q);
+            const float dk = fmaf(now.beta, dot(dS, y), lds_k[t][lane]);
+            step(dS, a, dr, -a * now.beta * k);
             if (lane % PK == 0) {               // values of v dv lie where dg comes
                 end += lds_end[t][lane / PK] - *dG.p;
                 *dG.p = end;
@@ -310,8 +342,7 @@ delta_small_grad_kernel(Delta d, uint64_t from)
             if (h + 1 < group) lds_k[t][lane] = dk;
             else if (in) *dK.p = (T)dk;
             dK.next(), dG.next();
-            if (t == 0) break;
-        }
+        });
     }
 }
 
@@ -322,33 +353,25 @@ void in_turns(uint64_t all, Go go)
     for (uint64_t from = 0; from < all; from += kMostLaunched) go((uint32_t)(all - from < kMostLaunched ? all - from : kMostLaunched), from);
 }
 
-template <class T, int PK, int PV, bool kFull, bool kVec>
+template <class T, int PK, int PV>
 void launch_size(const Delta &d, bool back, hipStream_t st)
 {
     const uint64_t along = ((uint64_t)d.n_seq * d.H + 64 / PV - 1) / (64 / PV);
-    if (!back) return in_turns(along, [&](uint32_t grid, uint64_t from) { delta_small_fwd_kernel<T, PK, PV, kFull, kVec><<<grid, 64, 0, st>>>(d, from); });
-    in_turns(along, [&](uint32_t grid, uint64_t from) { delta_small_bwd_kernel<T, PK, PV, kFull, kVec><<<grid, 64, 0, st>>>(d, from); });
+    if (!back) return in_turns(along, [&](uint32_t grid, uint64_t from) { delta_small_fwd_kernel<T, PK, PV><<<grid, 64, 0, st>>>(d, from); });
+    in_turns(along, [&](uint32_t grid, uint64_t from) { delta_small_bwd_kernel<T, PK, PV><<<grid, 64, 0, st>>>(d, from); });
     if (d.N == 0) return;
     const uint64_t slots = d.first ? d.slots : (uint64_t)d.n_seq * ((d.N / d.n_seq + kMark - 1) / kMark);
     in_turns((slots * d.Hk + 64 / PK - 1) / (64 / PK), [&](uint32_t grid, uint64_t from) {
-        if (d.H == d.Hk) delta_small_grad_kernel<T, PK, PV, false, kFull, kVec><<<grid, 64, 0, st>>>(d, from);
-        else delta_small_grad_kernel<T, PK, PV, true, kFull, kVec><<<grid, 64, 0, st>>>(d, from);
+        if (d.H == d.Hk) delta_small_grad_kernel<T, PK, PV, false><<<grid, 64, 0, st>>>(d, from);
+        else delta_small_grad_kernel<T, PK, PV, true><<<grid, 64, 0, st>>>(d, from);
     });
-}
-
-template <class T, int PK, int PV>
-void launch_padded(const Delta &d, bool back, hipStream_t st)
-{
-    if (d.Dk == PK && d.Dv == PV && d.vec_all) launch_size<T, PK, PV, true, true>(d, back, st);
-    else if (d.vec_all) launch_size<T, PK, PV, false, true>(d, back, st);
-    else launch_size<T, PK, PV, false, false>(d, back, st);
 }
 
 template <class T>
 void launch_type(const Delta &d, bool back, hipStream_t st)
 {
-    if (d.Dk <= 16) d.Dv <= 16 ? launch_padded<T, 16, 16>(d, back, st) : launch_padded<T, 16, 32>(d, back, st);
-    else d.Dv <= 16 ? launch_padded<T, 32, 16>(d, back, st) : launch_padded<T, 32, 32>(d, back, st);
+    if (d.Dk <= 16) d.Dv <= 16 ? launch_size<T, 16, 16>(d, back, st) : launch_size<T, 16, 32>(d, back, st);
+    else d.Dv <= 16 ? launch_size<T, 32, 16>(d, back, st) : launch_size<T, 32, 32>(d, back, st);
 }
 
 }  // namespace
