@@ -13,7 +13,7 @@ PEAKS_PATH = os.path.join(HERE, "libdgpeaks.so")     # yardstick kernels of the 
 
 SOURCES = ["host.hip", "segments.hip", "encode.hip", "encode_bwd_binned.hip", "encode_bwd_fill.hip", "order.hip", "encode_ordered.hip", "mlp.hip", "mlp_mfma.hip", "mlp_small.hip", "render.hip", "optim.hip", "occupancy.hip",
            "norm.hip", "recurrence.hip", "dropout.hip", "rms_norm.hip", "rows_e4m3.hip", "product_e4m3.hip",
-           "delta.hip", "delta_token.hip", "delta_small.hip", "delta_weights.hip", "delta_fwd.hip", "delta_bwd.hip", "delta_grad.hip"]
+           "delta.hip", "delta_token.hip", "delta_small.hip", "delta_weights.hip", "delta_fwd.hip", "delta_bwd.hip", "delta_join.hip", "delta_grad.hip"]
 COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
           # packed fp32 instructions are kept out of every kernel of this library
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

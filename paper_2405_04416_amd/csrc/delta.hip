@@ -25,13 +25,18 @@ size_t rows_bytes(uint64_t N, uint32_t H, uint32_t Dv) { return (size_t)(N * H *
 size_t padded(size_t n) { return (n + 15) / 16 * 16; }
 size_t slot_bytes(uint64_t N, uint32_t n_seq) { return padded(slots_of(N, n_seq) * 4); }
 
-// The workspace: T and P of the chunks and whose the chunks are, for either pass; then what the backward pass hands on.
-size_t forward_bytes(uint64_t N, uint32_t n_seq, uint32_t H) { return weight_bytes(N, n_seq, H) + chunk_bytes(N, n_seq); }
+// The workspace: T and P of the chunks, whose the chunks are, and what parts of sequences leave, for either pass; then what the backward pass hands on.
+size_t forward_bytes(uint64_t N, uint32_t n_seq, uint32_t H) { return weight_bytes(N, n_seq, H) + chunk_bytes(N, n_seq) + parts_bytes(N, n_seq, H); }
 
 void use_workspace(Delta &d, void *ws)
 {
     d.weights = (Weights *)ws;
     d.chunk_seq = (const uint32_t *)((char *)ws + weight_bytes(d.N, d.n_seq, d.H));
+    d.parts = 1;
+    if (const size_t bytes = parts_bytes(d.N, d.n_seq, d.H)) {
+        d.ends = (float *)((char *)d.chunk_seq + chunk_bytes(d.N, d.n_seq));
+        d.starts = d.ends + bytes / sizeof(float) / 3 * 2;
+    }
 }
 
 void use_vectors(Delta &d, const void *o, uint64_t ldo, uint32_t dtype)

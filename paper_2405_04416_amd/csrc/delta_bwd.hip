@@ -68,7 +68,7 @@ __device__ __forceinline__ void take_chunk(const Operands<T, KS> &o, uint32_t c1
 }
 
 // The same shared by wavefronts, rows 32 kOwn wave on each.
-template <class T, int KS>
+template <class T, int KS, bool kEnds>
 struct Share {
     static constexpr int n = Pieces<T>::n, kOwn = KS / kSharers<KS>;
     f32x4 S[2 * kOwn];
@@ -77,7 +77,7 @@ struct Share {
     float whole;
 
     // up to the sum K S; then all that comes after it is read
-    __device__ __forceinline__ void before(const Operands<T, KS> &o, Shares<KS, true> &to, uint32_t wave, uint32_t lane)
+    __device__ __forceinline__ void before(const Operands<T, KS> &o, Shares<KS, true, kEnds> &to, uint32_t wave, uint32_t lane)
     {
         const uint32_t c16 = lane % 16, r8 = lane / 16 * 8;
         bf16x8 keys[kOwn][2][n], sp[3];
@@ -113,7 +113,7 @@ struct Share {
         whole = o.weight.whole;
     }
 
-    __device__ __forceinline__ void after(Shares<KS, true> &shares, uint32_t parity, uint32_t wave, uint32_t lane)
+    __device__ __forceinline__ void after(Shares<KS, true, kEnds> &shares, uint32_t parity, uint32_t wave, uint32_t lane)
     {
         f32x4 du[2], dr[2], back[2];
         bf16x8 right[3], queried[3];
@@ -132,6 +132,7 @@ struct Share {
         split_rows<3>(back[0], back[1], right);
 #pragma unroll
         for (int t = 0; t < 2 * kOwn; ++t) S[t] = multiply<n, 3>(turned[t], right, S[t]);
+        if constexpr (!kEnds)
 #pragma unroll
         for (int h = 0; h < 2; ++h)
             if (wave == h % kSharers<KS>) shares.left[parity][h][lane] = dr[h];
@@ -139,8 +140,8 @@ struct Share {
 };
 
 // what does not wait for S: one wavefront makes P^T dO, the other scale e^G dO in pieces
-template <class T, int KS>
-__device__ __forceinline__ void make_ahead(const Operands<T, KS> &o, const Tile<T> &tile, Shares<KS, true> &to, uint32_t which, uint32_t lane)
+template <class T, int KS, bool kEnds>
+__device__ __forceinline__ void make_ahead(const Operands<T, KS> &o, const Tile<T> &tile, Shares<KS, true, kEnds> &to, uint32_t which, uint32_t lane)
 {
     constexpr int n = Pieces<T>::n;
     const uint32_t c16 = lane % 16, r8 = lane / 16 * 8;
@@ -167,37 +168,43 @@ __device__ __forceinline__ void make_ahead(const Operands<T, KS> &o, const Tile<
     }
 }
 
-template <class T, int KS>
+template <class T, int KS, bool kEnds>
 __global__ void __launch_bounds__(kSharedWaves<KS> * 64)
 delta_bwd_shared_kernel(Delta d, uint32_t groups, uint64_t from)
 {
-    __shared__ Helped<T, KS, true> room;
+    using Mine = Share<T, KS, kEnds>;
+    __shared__ Helped<T, KS, true, kEnds> room;
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c16 = lane % 16, r8 = lane / 16 * 8;
-    const Unit unit(d, groups, from);
-    const uint32_t head = unit.head, seq = unit.seq, column0 = unit.group * kShared, col = column0 + c16;
-    const Span span = span_of(d, seq);
-    const uint32_t row0 = wave * (Share<T, KS>::kOwn * 32), rows = d.Dk > row0 ? d.Dk - row0 : 0, chunks = (span.len + kChunk - 1) / kChunk;
-    const bool column = col < d.Dv, in = wave < kSharers<KS> && column;
-    const uint64_t memory = (((uint64_t)seq * d.H + head) * d.Dk + row0) * d.Dv + col;
-    Share<T, KS> share;
+    const Unit unit(d, kEnds ? d.parts - 1 : d.parts, groups, from);
+    const uint32_t head = unit.head, seq = unit.seq, column0 = unit.group * kShared, col = column0 + c16, one = (d.Dv + 15) / 16 * 16;
+    if (kEnds && unit.part == 0 && column0 >= one) return;
+    const Place0 place = Place0::of<true>(d, unit);
+    const Span &span = place.span;
+    const uint32_t row0 = wave * (Mine::kOwn * 32), rows = d.Dk > row0 ? d.Dk - row0 : 0, chunks = (span.len + kChunk - 1) / kChunk;
+    const bool column = col < d.Dv, in = wave < kSharers<KS> && column, mine = wave < kSharers<KS>;
+    const uint64_t first = ((uint64_t)seq * d.H + head) * d.Dk + row0, later = (((uint64_t)seq * d.parts + unit.part) * d.H + head) * d.Dk + row0;
+    Mine share;
+    if (kEnds && column0 >= one) unit_memory<Mine::kOwn>(col - one, row0, r8, share.S);
+    else if (unit.part == 0) load_memory<Mine::kOwn>(d.ds_last ? d.ds_last + first * d.Dv + col : nullptr, rows, d.Dv, in, r8, share.S);
+    else load_memory<Mine::kOwn>(kEnds ? nullptr : d.starts + later * d.Dv + col, rows, d.Dv, in, r8, share.S);
     f32x4 gradient;
-    load_memory<Share<T, KS>::kOwn>(d.ds_last ? d.ds_last + memory : nullptr, rows, d.Dv, in, r8, share.S);
-    along_helped<T, KS, true>(d, span, seq, head, column0, room, wave,
+    along_helped<T, KS, true, kEnds>(d, span, place.slot, head, column0, room, wave,
         [&](uint32_t i) {
             const uint32_t c = chunks - 1 - i;
             share.before(room.ops[i % 2], room.shares, wave, lane);
-            if (i == 0 || c % (kMark / kChunk) == kMark / kChunk - 1)
-                store_memory<Share<T, KS>::kOwn>(d.dmarks + (((uint64_t)(first_slot(span, seq) + c / (kMark / kChunk)) * d.H + head) * d.Dk + row0) * d.Dv + col, rows, d.Dv, in, r8, share.S);
+            if (!kEnds && (i == 0 || c % (kMark / kChunk) == kMark / kChunk - 1))
+                store_memory<Mine::kOwn>(d.dmarks + (((uint64_t)(place.mark + c / (kMark / kChunk)) * d.H + head) * d.Dk + row0) * d.Dv + col, rows, d.Dv, in, r8, share.S);
         },
         [&](uint32_t i) { share.after(room.shares, i % 2, wave, lane); },
         [&](uint32_t i) {
-            if (i < chunks) make_ahead<T, KS>(room.ops[i % 2], room.tiles[i % 2], room.shares, wave - kSharers<KS>, lane);
-            gradient = room.shares.left[(i + 1) % 2][wave - kSharers<KS>][lane];
+            if (i < chunks) make_ahead<T, KS, kEnds>(room.ops[i % 2], room.tiles[i % 2], room.shares, wave - kSharers<KS>, lane);
+            if constexpr (!kEnds) gradient = room.shares.left[(i + 1) % 2][wave - kSharers<KS>][lane];
         },
         [&](uint32_t i) {
-            if (i) store_four<float>(d.dr + head * d.Dv, (uint64_t)d.H * d.Dv, col, span, (chunks - i) * kChunk, r8, (wave - kSharers<KS>) * 4, column, gradient);
+            if (!kEnds && i) store_four<float>(d.dr + head * d.Dv, (uint64_t)d.H * d.Dv, col, span, (chunks - i) * kChunk, r8, (wave - kSharers<KS>) * 4, column, gradient);
         });
-    if (d.ds0) store_memory<Share<T, KS>::kOwn>(d.ds0 + memory, rows, d.Dv, in, r8, share.S);
+    if (kEnds) store_memory<Mine::kOwn>(d.ends + later * d.ends_width() + col, rows, d.ends_width(), mine, r8, share.S);
+    else if (d.ds0 && unit.part == d.parts - 1) store_memory<Mine::kOwn>(d.ds0 + first * d.Dv + col, rows, d.Dv, in, r8, share.S);
 }
 
 template <class T, int KS, bool kVec>
@@ -206,7 +213,7 @@ delta_bwd_kernel(Delta d, uint32_t with, uint32_t groups, uint64_t from)
 {
     __shared__ Room<T, KS> room;
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = blockDim.x / 64, c16 = lane % 16, r8 = lane / 16 * 8;
-    const Unit unit(d, groups, from);
+    const Unit unit(d, 1, groups, from);
     const uint32_t head = unit.head, seq = unit.seq, col = unit.group * with * 16 + wave * 16 + c16;
     const Span span = span_of(d, seq);
     const bool in = wave < with && col < d.Dv;
@@ -237,18 +244,24 @@ delta_bwd_kernel(Delta d, uint32_t with, uint32_t groups, uint64_t from)
 }
 
 template <class T, int KS>
-void launch_size(const Delta &d, hipStream_t st)
+void launch_size(Delta d, hipStream_t st)
 {
     constexpr bool kRoom = kHasRoom<T, KS, true>;
     const Columns c = columns_of(d, kRoom);
+    if constexpr (kRoom)
+        if (c.helped) {
+            cut(d, 160 * 1024 / sizeof(Helped<T, KS, true, true>), 160 * 1024 / sizeof(Helped<T, KS, true>));
+            if (d.parts > 1) {
+                const uint32_t groups = d.ends_width() / kShared;
+                delta_bwd_shared_kernel<T, KS, true><<<d.n_seq * d.H * (d.parts - 1) * groups, kSharedWaves<KS> * 64, 0, st>>>(d, groups, 0);
+                launch_join(d, st);
+            }
+            delta_bwd_shared_kernel<T, KS, false><<<d.n_seq * d.H * d.parts * c.groups, kSharedWaves<KS> * 64, 0, st>>>(d, c.groups, 0);
+            return;
+        }
     const uint64_t units = (uint64_t)d.n_seq * d.H * c.groups;
     for (uint64_t from = 0; from < units; from += kMostLaunched) {
         const uint32_t grid = (uint32_t)(units - from < kMostLaunched ? units - from : kMostLaunched);
-        if constexpr (kRoom)
-            if (c.helped) {
-                delta_bwd_shared_kernel<T, KS><<<grid, kSharedWaves<KS> * 64, 0, st>>>(d, c.groups, from);
-                continue;
-            }
         if (d.vec_keys) delta_bwd_kernel<T, KS, true><<<grid, c.waves * 64, 0, st>>>(d, c.with, c.groups, from);
         else delta_bwd_kernel<T, KS, false><<<grid, c.waves * 64, 0, st>>>(d, c.with, c.groups, from);
     }

@@ -18,10 +18,10 @@ constexpr int kPage = 1024;             // what a wavefront fetches at once
 // Rows of left operands lie by result: number i at `line(i)`.
 __host__ __device__ constexpr uint32_t line(uint32_t i) { return (i & ~31u) | (i >> 2 & 1) << 4 | (i >> 3 & 3) << 2 | (i & 3); }
 
-template <class T, int KS>
+template <class T, int KS, bool kQ = true>
 struct alignas(16) Keys {
     static constexpr int n = Pieces<T>::n, DK = 32 * KS;
-    uint16_t K[n][kChunk][DK + 8], Q[n][kChunk][DK + 8];
+    uint16_t K[n][kChunk][DK + 8], Q[kQ ? n : 1][kQ ? kChunk : 1][DK + 8];
 };
 
 struct alignas(16) Weights {
@@ -78,10 +78,10 @@ __device__ __forceinline__ void eight(const T *row, uint32_t c, uint32_t D, bool
 constexpr int kMostWaves = 4;           // in a workgroup
 constexpr uint64_t kFewColumns = 512;   // groups of 16
 
-template <class T, int KS>
+template <class T, int KS, bool kQ = true>
 struct Operands {
     Weights weight;
-    Keys<T, KS> key;
+    Keys<T, KS, kQ> key;
 };
 
 // Buffers: two if they fit, so that a chunk's operands come while the one before is worked on
@@ -169,7 +169,8 @@ struct Rows {
         }
     }
 
-    __device__ __forceinline__ void store(uint32_t c, const Fetched<T, KS, kEach> &from, Keys<T, KS> &to) const
+    template <bool kQ>
+    __device__ __forceinline__ void store(uint32_t c, const Fetched<T, KS, kEach> &from, Keys<T, KS, kQ> &to) const
     {
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
@@ -178,14 +179,14 @@ struct Rows {
             const bool in = c * kChunk + t < span.len;
             if constexpr (kVec) {
                 put_raw<T, KS>(from.ks[i], in, column(), Dk, t, to.K);
-                put_raw<T, KS>(from.qs[i], in, column(), Dk, t, to.Q);
+                if constexpr (kQ) put_raw<T, KS>(from.qs[i], in, column(), Dk, t, to.Q);
             } else {
                 float x[8], y[8];
                 const uint64_t row = span.row(in ? c * kChunk + t : c * kChunk);
                 eight<T, false>(k + row * ldk, column(), Dk, in, x);
                 eight<T, false>(q + row * ldq, column(), Dk, in, y);
                 put<n, KS>(x, t, column(), to.K);
-                put<n, KS>(y, t, column(), to.Q);
+                if constexpr (kQ) put<n, KS>(y, t, column(), to.Q);
             }
         }
     }
@@ -266,11 +267,11 @@ struct alignas(16) Tile {
 };
 
 // What wavefronts hand each other; for those aside two buffers, since they are a chunk behind
-template <int KS, bool kBackward>
+template <int KS, bool kBackward, bool kEnds = false>
 struct alignas(16) Shares {
     f32x4 keys[kSharers<KS>][2][64];                            // K S
-    u32x4 memory[kBackward ? 1 : KS][kBackward ? 1 : 3][64];    // forward: S in pieces
-    f32x4 left[2][kBackward ? 2 : 4][64];                       // what tokens miss (backward: gradients of what they write), what they write
+    u32x4 memory[kBackward || kEnds ? 1 : KS][kBackward || kEnds ? 1 : 3][64];    // forward: S in pieces
+    f32x4 left[kEnds ? 1 : 2][kEnds ? 1 : kBackward ? 2 : 4][64];                       // what tokens miss (backward: gradients of what they write), what they write
     f32x4 ahead[kBackward ? 2 : 1][64];                         // backward: P^T dO
     u32x4 queried[kBackward ? 3 : 1][64];                       // scale e^G dO, in pieces
 
@@ -281,11 +282,14 @@ struct alignas(16) Shares {
     }
 };
 
-template <class T, int KS, bool kBackward>
+// kEnds: for the memory at the end alone
+template <class T, int KS, bool kBackward, bool kEnds = false>
 struct Helped {
-    Operands<T, KS> ops[2];
+    static constexpr bool kQ = kBackward || !kEnds;
+    using Ops = Operands<T, KS, kQ>;
+    Ops ops[2];
     Tile<T> tiles[2];
-    Shares<KS, kBackward> shares;
+    Shares<KS, kBackward, kEnds> shares;
 };
 template <class T, int KS, bool kBackward>
 constexpr bool kHasRoom = sizeof(Helped<T, KS, kBackward>) <= 160 * 1024;
@@ -337,7 +341,8 @@ struct Helper {
         }
     }
 
-    __device__ __forceinline__ void put_operands(uint32_t c, const Chunk &from, Operands<T, KS> &ops) const
+    template <bool kQ>
+    __device__ __forceinline__ void put_operands(uint32_t c, const Chunk &from, Operands<T, KS, kQ> &ops) const
     {
         u32x4 *to = (u32x4 *)&ops.weight;
 #pragma unroll
@@ -348,9 +353,9 @@ struct Helper {
 
 // before(i), after(i) in the wavefronts that have columns, early(i), late(i) in those aside, i counting chunks (backward from the last one): all but early go with the two buffers i % 2; early(i)
 // may read what after(i - 1) left, and both early(i) and late(i) run up to i = number of chunks.  The others have a chunk's time for what they bring for the next one.
-template <class T, int KS, bool kBackward, class Before, class After, class Early, class Late>
-__device__ __forceinline__ void along_helped(const Delta &d, const Span &span, uint32_t seq, uint32_t head, uint32_t column0, Helped<T, KS, kBackward> &room, uint32_t wave, Before before,
-                                             After after, Early early, Late late)
+template <class T, int KS, bool kBackward, bool kEnds, class Before, class After, class Early, class Late>
+__device__ __forceinline__ void along_helped(const Delta &d, const Span &span, uint64_t slot0, uint32_t head, uint32_t column0, Helped<T, KS, kBackward, kEnds> &room, uint32_t wave,
+                                             Before before, After after, Early early, Late late)
 {
     const uint32_t chunks = (span.len + kChunk - 1) / kChunk, hk = head / (d.H / d.Hk);
     if (chunks == 0) return;
@@ -379,7 +384,7 @@ __device__ __forceinline__ void along_helped(const Delta &d, const Span &span, u
         return;
     }
     using Help = Helper<T, KS, kBackward>;
-    const Help h = {d, span, first_chunk(span, seq), head, threadIdx.x - kFirst * 64, column0,
+    const Help h = {d, span, slot0, head, threadIdx.x - kFirst * 64, column0,
                     {(const T *)d.q + hk * d.Dk, (const T *)d.k + hk * d.Dk, d.ldq, d.ldk, d.Dk, wave - kFirst, kHelpers<KS>, threadIdx.x % 64, span}};
     // A chunk is fetched two before it is put; `coming` holds the next one.  Without a branch about a load (behind the last chunk it comes again), so that a wait is for the oldest loads only.
     typename Help::Chunk held[2];
@@ -409,12 +414,13 @@ __device__ __forceinline__ void along_helped(const Delta &d, const Span &span, u
     __syncthreads();
 }
 
-// Which head (of all sequences) and group of columns a workgroup has.  Those of a head read the same operands: they get numbers that differ by 8, and so the same of the eight L2 caches.
+// Which head (of all sequences), part and group of columns a workgroup has.  Those of a head and part read the same operands: they get numbers that differ by 8, and so the same of the eight
+// L2 caches.
 struct Unit {
-    uint32_t seq, head, group;
-    __device__ __forceinline__ Unit(const Delta &d, uint32_t groups, uint64_t from)
+    uint32_t seq, head, part, group;
+    __device__ __forceinline__ Unit(const Delta &d, uint32_t parts, uint32_t groups, uint64_t from)
     {
-        const uint64_t unit = from + blockIdx.x, heads = (uint64_t)d.n_seq * d.H, eights = heads / 8 * 8 * groups;
+        const uint64_t unit = from + blockIdx.x, all = (uint64_t)d.n_seq * d.H * parts, eights = all / 8 * 8 * groups;
         uint64_t of;
         if (unit < eights) {
             of = unit / (8 * groups) * 8 + unit % 8;
@@ -423,9 +429,61 @@ struct Unit {
             of = unit / groups;
             group = (uint32_t)(unit % groups);
         }
+        part = (uint32_t)(of % parts);
+        of /= parts;
         seq = (uint32_t)(of / d.H), head = (uint32_t)(of % d.H);
     }
 };
+
+// ------------------------------------------------------------------------------ parts
+// A sequence of few heads is cut in parts where that fills the chip.  A part turns the memory before it into the one behind it by S' = M S + E: a first launch makes E (from no memory; the first part
+// from s0) and M (from the unit matrix, its columns as further columns whose values are 0) of all parts but the last, delta_join.hip goes from part to part, a second launch does the whole work with
+// known beginnings.  Backward the same from the other end.  `part` counts in the order of the run.
+struct Place0 {
+    Span span;
+    uint64_t slot;
+    uint32_t mark;
+    template <bool kBackward>
+    __device__ __forceinline__ static Place0 of(const Delta &d, const Unit &unit)
+    {
+        const Span whole = span_of(d, unit.seq);
+        const uint64_t slot = first_chunk(whole, unit.seq);
+        const uint32_t mark = first_slot(whole, unit.seq);
+        if (d.parts == 1) return {whole, slot, mark};
+        const uint32_t part = kBackward ? d.parts - 1 - unit.part : unit.part;
+        return {part_of(whole, part, d.stretch), slot + part * (d.stretch / kChunk), mark + part * (d.stretch / kMark)};
+    }
+};
+
+// a lane's part of the unit matrix: column `one`
+template <int KS>
+__device__ __forceinline__ void unit_memory(uint32_t one, uint32_t row0, uint32_t r8, f32x4 (&S)[2 * KS])
+{
+#pragma unroll
+    for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) S[t][x] = row0 + t / 2 * 32 + r8 + t % 2 * 4 + x == one ? 1.0f : 0.0f;
+}
+
+constexpr uint32_t kUnits = 256;        // compute units
+constexpr uint32_t kMostParts = 16, kLeastStretch = 512;
+
+// Number of parts for the least time by rounds of workgroups: per_first, per_second of the two launches' run on a compute unit at once (the first, which has less to do, counts 0.8).
+inline void cut(Delta &d, uint32_t per_first, uint32_t per_second)
+{
+    d.parts = 1;
+    if (d.first || !d.ends || d.N / d.n_seq > 0xffffffffu) return;
+    const uint32_t len = (uint32_t)(d.N / d.n_seq), all = (d.Dv + 15) / 16, keys = (d.Dk + 15) / 16;
+    const uint64_t heads = (uint64_t)d.n_seq * d.H;
+    auto rounds = [](uint64_t groups, uint32_t per) { return (double)((groups + kUnits - 1) / kUnits <= per ? 1 + 0.25 * ((groups - 1) / kUnits) : (double)((groups + kUnits * per - 1) / (kUnits * per)) * (0.75 + 0.25 * per)); };
+    double best = 0.8 * rounds(heads * all, per_second);
+    for (uint32_t p = 3; p <= kMostParts && heads * p <= kUnits && len / p >= kLeastStretch; ++p) {
+        const uint32_t stretch = (len / p + kMark - 1) / kMark * kMark;
+        if ((uint64_t)stretch * (p - 1) >= len || (uint64_t)stretch * p < len) continue;
+        const double cost = (0.8 * rounds(heads * ((p - 1) * all + (p - 2) * keys), per_first) + rounds(heads * all * p, per_second)) / p;
+        if (cost < best) best = cost, d.parts = p, d.stretch = stretch;
+    }
+}
 
 // How many wavefronts of a workgroup have columns, how many there are (those that help among them), and how many workgroups a head has
 struct Columns { uint32_t with, waves, groups; bool helped; };

@@ -50,6 +50,10 @@ struct Delta {
     Weights *weights;                           // [chunk slots][H]
     uint64_t N;
     uint32_t n_seq, Hk, H, Dk, Dv, reverse, slots;
+    // Sequences cut in parts of `stretch` tokens (1: whole): what a part makes of no memory and of every column of the unit matrix, [n_seq][parts][H][Dk][ends_width()], and memories before them
+    uint32_t parts, stretch;
+    float *ends, *starts;
+    __host__ __device__ uint32_t ends_width() const { return (Dv + 15) / 16 * 16 + (Dk + 15) / 16 * 16; }
     float scale;
     // Whether heads' rows lie in whole 16 bytes: q and k; q, k, v and o or its gradient, and with them rows of fp32 values; dv, dq and dk too.  Kernels take it as a template
     // argument: of a branch between loads of 16 bytes and single ones the compiler makes single ones for both.
@@ -79,6 +83,13 @@ __device__ __forceinline__ Span span_of(const Delta &d, uint32_t seq)
     }
     const uint64_t b = d.first[seq], e = d.first[seq + 1], begin = b < d.N ? b : d.N, end = e < d.N ? e : d.N;
     return {begin, end > begin ? (uint32_t)(end - begin) : 0u, d.reverse ? -1 : 0};
+}
+
+// a part of a sequence
+__device__ __forceinline__ Span part_of(const Span &s, uint32_t part, uint32_t stretch)
+{
+    const uint32_t t0 = part * stretch, len = s.len - t0 < stretch ? s.len - t0 : stretch;
+    return {s.turn ? s.begin + (s.len - t0 - len) : s.begin + t0, len, s.turn};
 }
 
 // Where the memories of a sequence are left: every sequence begins one slot after floor(begin / 64) more than the one before, which leaves room for all
@@ -187,6 +198,8 @@ void launch_weights(const Delta &d, uint32_t dtype, bool backward, hipStream_t s
 void launch_forward(const Delta &d, uint32_t dtype, hipStream_t st);
 void launch_small(const Delta &d, uint32_t dtype, bool back, hipStream_t st);        // heads of up to 32 x 32
 void launch_slots(const Delta &d, hipStream_t st);
+size_t parts_bytes(uint64_t N, uint32_t n_seq, uint32_t H);
+void launch_join(const Delta &d, hipStream_t st);
 void launch_tokens(const Delta &d, uint32_t dtype, hipStream_t st);
 void launch_backward(const Delta &d, uint32_t dtype, hipStream_t st);
 void launch_gradients(const Delta &d, uint32_t dtype, hipStream_t st);

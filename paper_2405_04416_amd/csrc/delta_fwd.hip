@@ -73,7 +73,7 @@ __device__ __forceinline__ void take_chunk(const Operands<T, KS> &o, uint32_t c1
 }
 
 // The same shared by wavefronts, rows 32 kOwn wave on each.
-template <class T, int KS>
+template <class T, int KS, bool kEnds>
 struct Share {
     static constexpr int n = Pieces<T>::n, kOwn = KS / kSharers<KS>;
     f32x4 S[2 * kOwn];
@@ -82,7 +82,7 @@ struct Share {
     float value[8], whole;
 
     // up to the sum K S; then all that comes after it is read
-    __device__ __forceinline__ void before(const Operands<T, KS> &o, const Tile<T> &tile, Shares<KS, false> &to, uint32_t wave, uint32_t lane)
+    __device__ __forceinline__ void before(const Operands<T, KS, !kEnds> &o, const Tile<T> &tile, Shares<KS, false, kEnds> &to, uint32_t wave, uint32_t lane)
     {
         const uint32_t c16 = lane % 16, r8 = lane / 16 * 8;
         bf16x8 keys[kOwn][2][n], sp[kOwn][3];
@@ -103,6 +103,7 @@ struct Share {
             if constexpr (kOwn == 2) sum[0][h] += sum[1][h];
             to.keys[wave][h][lane] = sum[0][h];
         }
+        if constexpr (!kEnds)
 #pragma unroll
         for (int s = 0; s < kOwn; ++s)
 #pragma unroll
@@ -123,7 +124,7 @@ struct Share {
         whole = o.weight.whole;
     }
 
-    __device__ __forceinline__ void after(Shares<KS, false> &shares, uint32_t parity, uint32_t wave, uint32_t lane)
+    __device__ __forceinline__ void after(Shares<KS, false, kEnds> &shares, uint32_t parity, uint32_t wave, uint32_t lane)
     {
         f32x4 r[2], u[2], y[2];
 #pragma unroll
@@ -142,6 +143,7 @@ struct Share {
 #pragma unroll
         for (int t = 0; t < 2 * kOwn; ++t) S[t] = multiply<n, 3>(turned[t], written, S[t] * whole);
         // for those aside
+        if constexpr (!kEnds)
 #pragma unroll
         for (int h = 0; h < 2; ++h)
             if (wave == h % kSharers<KS>) {
@@ -185,38 +187,48 @@ struct Outputs {
     }
 };
 
-template <class T, int KS>
+template <class T, int KS, bool kEnds>
 __global__ void __launch_bounds__(kSharedWaves<KS> * 64)
 delta_fwd_shared_kernel(Delta d, uint32_t groups, uint64_t from)
 {
-    __shared__ Helped<T, KS, false> room;
+    using Mine = Share<T, KS, kEnds>;
+    __shared__ Helped<T, KS, false, kEnds> room;
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c16 = lane % 16, r8 = lane / 16 * 8;
-    const Unit unit(d, groups, from);
-    const uint32_t head = unit.head, seq = unit.seq, column0 = unit.group * kShared, col = column0 + c16;
-    const Span span = span_of(d, seq);
-    const uint32_t row0 = wave * (Share<T, KS>::kOwn * 32), rows = d.Dk > row0 ? d.Dk - row0 : 0, chunks = (span.len + kChunk - 1) / kChunk;
-    const bool column = col < d.Dv, in = wave < kSharers<KS> && column;
-    const uint64_t memory = (((uint64_t)seq * d.H + head) * d.Dk + row0) * d.Dv + col;
-    Share<T, KS> share;
+    const Unit unit(d, kEnds ? d.parts - 1 : d.parts, groups, from);
+    const uint32_t head = unit.head, seq = unit.seq, column0 = unit.group * kShared, col = column0 + c16, one = (d.Dv + 15) / 16 * 16;
+    if (kEnds && unit.part == 0 && column0 >= one) return;
+    const Place0 place = Place0::of<false>(d, unit);
+    const Span &span = place.span;
+    const uint32_t row0 = wave * (Mine::kOwn * 32), rows = d.Dk > row0 ? d.Dk - row0 : 0, chunks = (span.len + kChunk - 1) / kChunk;
+    const bool column = col < d.Dv, in = wave < kSharers<KS> && column, mine = wave < kSharers<KS>;
+    const uint64_t first = ((uint64_t)seq * d.H + head) * d.Dk + row0, later = (((uint64_t)seq * d.parts + unit.part) * d.H + head) * d.Dk + row0;
+    Mine share;
+    if (kEnds && column0 >= one) unit_memory<Mine::kOwn>(col - one, row0, r8, share.S);
+    else if (unit.part == 0) load_memory<Mine::kOwn>(d.s0 ? d.s0 + first * d.Dv + col : nullptr, rows, d.Dv, in, r8, share.S);
+    else load_memory<Mine::kOwn>(kEnds ? nullptr : d.starts + later * d.Dv + col, rows, d.Dv, in, r8, share.S);
     Outputs<T, KS> outputs;
-    load_memory<Share<T, KS>::kOwn>(d.s0 ? d.s0 + memory : nullptr, rows, d.Dv, in, r8, share.S);
-    along_helped<T, KS, false>(d, span, seq, head, column0, room, wave,
+    along_helped<T, KS, false, kEnds>(d, span, place.slot, head, column0, room, wave,
         [&](uint32_t c) {
             share.before(room.ops[c % 2], room.tiles[c % 2], room.shares, wave, lane);
-            if (d.marks && c % (kMark / kChunk) == 0)
-                store_memory<Share<T, KS>::kOwn>(d.marks + (((uint64_t)(first_slot(span, seq) + c / (kMark / kChunk)) * d.H + head) * d.Dk + row0) * d.Dv + col, rows, d.Dv, in, r8, share.S);
+            if (!kEnds && d.marks && c % (kMark / kChunk) == 0)
+                store_memory<Mine::kOwn>(d.marks + (((uint64_t)(place.mark + c / (kMark / kChunk)) * d.H + head) * d.Dk + row0) * d.Dv + col, rows, d.Dv, in, r8, share.S);
         },
         [&](uint32_t c) { share.after(room.shares, c % 2, wave, lane); },
-        [&](uint32_t c) { outputs.read(room.ops[(c + 1) % 2], room.shares, (c + 1) % 2, wave - kSharers<KS>, lane); },
         [&](uint32_t c) {
-            const uint32_t t0 = (c - 1) * kChunk, h = wave - kSharers<KS>;
-            if (c) {
-                store_four<T>((T *)d.o + head * d.Dv, d.ldo, col, span, t0, r8, h * 4, column, outputs.make());
-                if (d.y) store_four<float>(d.y + head * d.Dv, (uint64_t)d.H * d.Dv, col, span, t0, r8, h * 4, column, outputs.y);
+            if constexpr (!kEnds) outputs.read(room.ops[(c + 1) % 2], room.shares, (c + 1) % 2, wave - kSharers<KS>, lane);
+        },
+        [&](uint32_t c) {
+            if constexpr (!kEnds) {
+                const uint32_t t0 = (c - 1) * kChunk, h = wave - kSharers<KS>;
+                if (c) {
+                    store_four<T>((T *)d.o + head * d.Dv, d.ldo, col, span, t0, r8, h * 4, column, outputs.make());
+                    if (d.y) store_four<float>(d.y + head * d.Dv, (uint64_t)d.H * d.Dv, col, span, t0, r8, h * 4, column, outputs.y);
+                }
+                if (c < chunks) outputs.query(room.ops[c % 2], room.shares, h, lane);
             }
-            if (c < chunks) outputs.query(room.ops[c % 2], room.shares, h, lane);
         });
-    if (d.s_last) store_memory<Share<T, KS>::kOwn>(d.s_last + memory, rows, d.Dv, in, r8, share.S);
+    if (kEnds) store_memory<Mine::kOwn>(d.ends + later * d.ends_width() + col, rows, d.ends_width(), mine, r8, share.S);
+    else if (d.s_last && unit.part == d.parts - 1) store_memory<Mine::kOwn>(d.s_last + first * d.Dv + col, rows, d.Dv, in, r8, share.S);
 }
 
 template <class T, int KS, bool kVec>
@@ -225,7 +237,7 @@ delta_fwd_kernel(Delta d, uint32_t with, uint32_t groups, uint64_t from)
 {
     __shared__ Room<T, KS> room;
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = blockDim.x / 64, c16 = lane % 16, r8 = lane / 16 * 8;
-    const Unit unit(d, groups, from);
+    const Unit unit(d, 1, groups, from);
     const uint32_t head = unit.head, seq = unit.seq, col = unit.group * with * 16 + wave * 16 + c16;
     const Span span = span_of(d, seq);
     const bool in = wave < with && col < d.Dv;
@@ -258,18 +270,24 @@ delta_fwd_kernel(Delta d, uint32_t with, uint32_t groups, uint64_t from)
 }
 
 template <class T, int KS>
-void launch_size(const Delta &d, hipStream_t st)
+void launch_size(Delta d, hipStream_t st)
 {
     constexpr bool kRoom = kHasRoom<T, KS, false>;
     const Columns c = columns_of(d, kRoom);
+    if constexpr (kRoom)
+        if (c.helped) {
+            cut(d, 160 * 1024 / sizeof(Helped<T, KS, false, true>), 160 * 1024 / sizeof(Helped<T, KS, false>));
+            if (d.parts > 1) {
+                const uint32_t groups = d.ends_width() / kShared;
+                delta_fwd_shared_kernel<T, KS, true><<<d.n_seq * d.H * (d.parts - 1) * groups, kSharedWaves<KS> * 64, 0, st>>>(d, groups, 0);
+                launch_join(d, st);
+            }
+            delta_fwd_shared_kernel<T, KS, false><<<d.n_seq * d.H * d.parts * c.groups, kSharedWaves<KS> * 64, 0, st>>>(d, c.groups, 0);
+            return;
+        }
     const uint64_t units = (uint64_t)d.n_seq * d.H * c.groups;
     for (uint64_t from = 0; from < units; from += kMostLaunched) {
         const uint32_t grid = (uint32_t)(units - from < kMostLaunched ? units - from : kMostLaunched);
-        if constexpr (kRoom)
-            if (c.helped) {
-                delta_fwd_shared_kernel<T, KS><<<grid, kSharedWaves<KS> * 64, 0, st>>>(d, c.groups, from);
-                continue;
-            }
         if (d.vec_keys) delta_fwd_kernel<T, KS, true><<<grid, c.waves * 64, 0, st>>>(d, c.with, c.groups, from);
         else delta_fwd_kernel<T, KS, false><<<grid, c.waves * 64, 0, st>>>(d, c.with, c.groups, from);
     }

@@ -1,0 +1,57 @@
+// The gated delta rule, sequences in parts: from part to part.  S before the first part but one is what the first one leaves, E; then S' = M S + E.
+// A workgroup has 16 columns of a head's memory, in LDS; M and E come from memory once.  Some microseconds a part, next to what the parts themselves take.
+#include "delta_chunk.h"
+
+namespace {
+
+using namespace dg_delta;
+
+constexpr int kThreads = 256, kColumns = 16;
+
+__global__ void __launch_bounds__(kThreads)
+delta_join_kernel(Delta d, uint32_t groups)
+{
+    __shared__ f32x4 lds[2][kMaxD][kColumns / 4];
+    const uint32_t group = blockIdx.x % groups, head = blockIdx.x / groups % d.H, seq = blockIdx.x / groups / d.H, row = threadIdx.x / 4, four = threadIdx.x % 4;
+    const uint32_t width = d.ends_width(), one = (d.Dv + 15) / 16 * 16, col = group * kColumns + four * 4;
+    for (uint32_t p = 0; p + 1 < d.parts; ++p) {
+        const uint64_t at = (((uint64_t)seq * d.parts + p) * d.H + head) * d.Dk;
+        const float *ends = d.ends + at * width;
+        float *next = d.starts + (at + (uint64_t)d.H * d.Dk) * d.Dv;
+        for (uint32_t r = row; r < d.Dk; r += kThreads / 4) {
+            f32x4 sum = *reinterpret_cast<const f32x4 *>(ends + (uint64_t)r * width + col);
+            if (p) {
+                const float *m = ends + (uint64_t)r * width + one;
+                f32x4 part[4] = {};
+                for (uint32_t k = 0; k < d.Dk; k += 4) {
+                    const f32x4 v = *reinterpret_cast<const f32x4 *>(m + k);            // behind Dk the unit matrix has no columns: rows of 0 and results of 0
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        if (k + x < d.Dk) part[x] += v[x] * lds[(p + 1) % 2][k + x][four];
+                }
+                sum += (part[0] + part[1]) + (part[2] + part[3]);
+            }
+            lds[p % 2][r][four] = sum;
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+                if (col + x < d.Dv) next[(uint64_t)r * d.Dv + col + x] = sum[x];
+        }
+        __syncthreads();
+    }
+}
+
+}  // namespace
+
+size_t dg_delta::parts_bytes(uint64_t N, uint32_t n_seq, uint32_t H)
+{
+    const uint64_t heads = (uint64_t)n_seq * H;
+    if (n_seq == 0 || heads * 3 > kUnits || N / n_seq < 3 * kLeastStretch) return 0;
+    const uint64_t most = heads * kMostParts < kUnits ? heads * kMostParts : kUnits;
+    return (size_t)most * kMaxD * 3 * kMaxD * sizeof(float);
+}
+
+void dg_delta::launch_join(const Delta &d, hipStream_t st)
+{
+    const uint32_t groups = (d.Dv + kColumns - 1) / kColumns;
+    delta_join_kernel<<<d.n_seq * d.H * groups, kThreads, 0, st>>>(d, groups);
+}

@@ -618,18 +618,18 @@ def test_delta_rule_strides(n_seq, S, Hk, H, Dk, Dv, pad, shift, dtype):
 
 
 @pytest.mark.parametrize("reverse", [False, True])
-@pytest.mark.parametrize("S,H,Dk,Dv,dtype", [(5000, 1, 64, 32, "fp32"), (4097, 2, 32, 16, "bf16"), (3001, 1, 128, 128, "fp16"), (9000, 1, 16, 16, "fp32")])
+@pytest.mark.parametrize("S,H,Dk,Dv,dtype", [(5000, 1, 64, 32, "fp32"), (4097, 2, 32, 16, "bf16"), (3001, 1, 128, 128, "fp16"), (9000, 1, 16, 16, "fp32"), (1537, 3, 50, 20, "fp16"),
+                                               (2111, 1, 100, 7, "fp32"), (6000, 1, 128, 128, "bf16")])
 def test_delta_rule_of_long_sequences(S, H, Dk, Dv, dtype, reverse):
     say("delta rule long", S, H, Dk, Dv, dtype, reverse)
     a = delta_inputs(np.random.default_rng(S), S, 1, H, Dk, Dv, 1, TYPES[dtype], decay=0.3)
     check_delta(a, 1, None, TYPES[dtype], reverse)
 
 
-@pytest.mark.parametrize("n_seq,H,Dk,Dv", [(1, 1, 64, 64), (2, 2, 128, 128), (600, 1, 16, 16)])
-def test_delta_rule_that_remembers_long(n_seq, H, Dk, Dv):
-    """Nothing is forgotten, small rates: what was written lives on from block to block."""
-    say("delta rule memory", n_seq, H, Dk, Dv)
-    S = 700 if n_seq < 9 else 130
+@pytest.mark.parametrize("n_seq,S,H,Dk,Dv", [(1, 700, 1, 64, 64), (2, 700, 2, 128, 128), (600, 130, 1, 16, 16), (1, 2600, 1, 64, 32), (2, 1700, 1, 128, 128)])
+def test_delta_rule_that_remembers_long(n_seq, S, H, Dk, Dv):
+    """Nothing is forgotten, small rates: what was written lives on from block to block, and from part to part."""
+    say("delta rule memory", n_seq, S, H, Dk, Dv)
     a = delta_inputs(np.random.default_rng(8), n_seq * S, 1, H, Dk, Dv, n_seq, torch.float32, decay=0.0, rate=0.05)
     check_delta(a, n_seq, None, torch.float32)
 
