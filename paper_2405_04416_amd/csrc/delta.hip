@@ -6,16 +6,17 @@ namespace {
 
 using namespace dg_delta;
 
-// Up to so many tokens a sequence, on average, they are taken one by one.
+// Up to so many tokens a sequence, on average, they are taken one by one.  Heads of 128 x 128, one by one / in chunks, in us: 64 sequences of 16 heads 53 / 98 with 4 tokens each, 127 / 102
+// with 16; 4 sequences of 8 heads 14 / 16 with 4, 38 / 15 with 16.
 constexpr uint64_t kFewTokens = 4;
 
-// From so many heads of all sequences on small ones are taken token by token, several to a wavefront.
-constexpr uint64_t kManyHeads = 512;
-
-// Whether a lane takes a column or row of the memory along a sequence, instead of wavefronts chunks of it
+// Small heads are taken token by token where those of all sequences fill the chip, or where tokens are few.  Training,
+// token by token / in chunks, in us: 768 heads of 16 x 16 270 / 265, 1536 of them 185 / 258; of 16 x 32 1024 223 / 197, 2048 239 / 355; of 32 x 32 2048 847 / 793, 4096 759 / 795.
 bool takes_small(uint64_t N, uint32_t n_seq, uint32_t H, uint32_t Dk, uint32_t Dv)
 {
-    return Dk <= 32 && Dv <= 32 && ((uint64_t)n_seq * H >= kManyHeads || N <= kFewTokens * n_seq);
+    if (Dk > 32 || Dv > 32) return false;
+    const uint64_t padded = (Dk <= 16 ? 16 : 32) * (Dv <= 16 ? 16 : 32);
+    return (uint64_t)n_seq * H * 2 >= 5 * padded || N <= kFewTokens * n_seq;
 }
 
 uint64_t slots_of(uint64_t N, uint32_t n_seq) { return N / kMark + n_seq; }

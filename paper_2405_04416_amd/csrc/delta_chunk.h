@@ -76,7 +76,9 @@ __device__ __forceinline__ void eight(const T *row, uint32_t c, uint32_t D, bool
 
 // ------------------------------------------------------------------------------ along a sequence
 constexpr int kMostWaves = 4;           // in a workgroup
-constexpr uint64_t kFewColumns = 512;   // groups of 16
+// Groups of 16 columns up to which wavefronts share them.  Training of heads of 128 x 128, shared / each its own, in us: 384 groups of 2048 tokens 583 / 1007, 512 683 / 747, 768 of 1024 tokens
+// 520 / 664, 1024 695 / 597.
+constexpr uint64_t kFewColumns = 768;
 
 template <class T, int KS, bool kQ = true>
 struct Operands {
@@ -439,12 +441,12 @@ struct Unit {
 // A sequence of few heads is cut in parts where that fills the chip.  A part turns the memory before it into the one behind it by S' = M S + E: a first launch makes E (from no memory; the first part
 // from s0) and M (from the unit matrix, its columns as further columns whose values are 0) of all parts but the last, delta_join.hip goes from part to part, a second launch does the whole work with
 // known beginnings.  Backward the same from the other end.  `part` counts in the order of the run.
-struct Place0 {
+struct PartPlace {
     Span span;
     uint64_t slot;
     uint32_t mark;
     template <bool kBackward>
-    __device__ __forceinline__ static Place0 of(const Delta &d, const Unit &unit)
+    __device__ __forceinline__ static PartPlace of(const Delta &d, const Unit &unit)
     {
         const Span whole = span_of(d, unit.seq);
         const uint64_t slot = first_chunk(whole, unit.seq);

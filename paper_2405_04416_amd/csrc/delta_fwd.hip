@@ -197,7 +197,7 @@ delta_fwd_shared_kernel(Delta d, uint32_t groups, uint64_t from)
     const Unit unit(d, kEnds ? d.parts - 1 : d.parts, groups, from);
     const uint32_t head = unit.head, seq = unit.seq, column0 = unit.group * kShared, col = column0 + c16, one = (d.Dv + 15) / 16 * 16;
     if (kEnds && unit.part == 0 && column0 >= one) return;
-    const Place0 place = Place0::of<false>(d, unit);
+    const PartPlace place = PartPlace::of<false>(d, unit);
     const Span &span = place.span;
     const uint32_t row0 = wave * (Mine::kOwn * 32), rows = d.Dk > row0 ? d.Dk - row0 : 0, chunks = (span.len + kChunk - 1) / kChunk;
     const bool column = col < d.Dv, in = wave < kSharers<KS> && column, mine = wave < kSharers<KS>;
