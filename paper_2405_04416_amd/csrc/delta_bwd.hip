@@ -168,7 +168,7 @@ __device__ __forceinline__ void make_ahead(const Operands<T, KS> &o, const Tile<
     }
 }
 
-template <class T, int KS, bool kEnds>
+template <class T, int KS, bool kEnds, bool kVec>
 __global__ void __launch_bounds__(kSharedWaves<KS> * 64)
 delta_bwd_shared_kernel(Delta d, uint32_t groups, uint64_t from)
 {
@@ -188,7 +188,7 @@ delta_bwd_shared_kernel(Delta d, uint32_t groups, uint64_t from)
     else if (unit.part == 0) load_memory<Mine::kOwn>(d.ds_last ? d.ds_last + first * d.Dv + col : nullptr, rows, d.Dv, in, r8, share.S);
     else load_memory<Mine::kOwn>(kEnds ? nullptr : d.starts + later * d.Dv + col, rows, d.Dv, in, r8, share.S);
     f32x4 gradient;
-    along_helped<T, KS, true, kEnds>(d, span, place.slot, head, column0, room, wave,
+    along_helped<T, KS, true, kEnds, kVec>(d, span, place.slot, head, column0, room, wave,
         [&](uint32_t i) {
             const uint32_t c = chunks - 1 - i;
             share.before(room.ops[i % 2], room.shares, wave, lane);
@@ -251,12 +251,14 @@ void launch_size(Delta d, hipStream_t st)
     if constexpr (kRoom)
         if (c.helped) {
             cut(d, 160 * 1024 / sizeof(Helped<T, KS, true, true>), 160 * 1024 / sizeof(Helped<T, KS, true>));
+            const uint32_t groups = d.ends_width() / kShared, first = d.n_seq * d.H * (d.parts - 1) * groups, all = d.n_seq * d.H * d.parts * c.groups, threads = kSharedWaves<KS> * 64;
             if (d.parts > 1) {
-                const uint32_t groups = d.ends_width() / kShared;
-                delta_bwd_shared_kernel<T, KS, true><<<d.n_seq * d.H * (d.parts - 1) * groups, kSharedWaves<KS> * 64, 0, st>>>(d, groups, 0);
+                if (d.vec_all) delta_bwd_shared_kernel<T, KS, true, true><<<first, threads, 0, st>>>(d, groups, 0);
+                else delta_bwd_shared_kernel<T, KS, true, false><<<first, threads, 0, st>>>(d, groups, 0);
                 launch_join(d, st);
             }
-            delta_bwd_shared_kernel<T, KS, false><<<d.n_seq * d.H * d.parts * c.groups, kSharedWaves<KS> * 64, 0, st>>>(d, c.groups, 0);
+            if (d.vec_all) delta_bwd_shared_kernel<T, KS, false, true><<<all, threads, 0, st>>>(d, c.groups, 0);
+            else delta_bwd_shared_kernel<T, KS, false, false><<<all, threads, 0, st>>>(d, c.groups, 0);
             return;
         }
     const uint64_t units = (uint64_t)d.n_seq * d.H * c.groups;

@@ -5,6 +5,7 @@
 // alone (T and P) are made by a launch of its own (delta_weights.hip), for all chunks at once, in the workspace, as they are to lie in LDS, and come by loads that write there;
 // K and Q come through registers, which cut them into pieces; reads that transpose turn them.
 #pragma once
+#include <type_traits>
 #include "delta_common.h"
 
 namespace dg_delta {
@@ -76,9 +77,10 @@ __device__ __forceinline__ void eight(const T *row, uint32_t c, uint32_t D, bool
 
 // ------------------------------------------------------------------------------ along a sequence
 constexpr int kMostWaves = 4;           // in a workgroup
-// Groups of 16 columns up to which wavefronts share them.  Training of heads of 128 x 128, shared / each its own, in us: 384 groups of 2048 tokens 583 / 1007, 512 683 / 747, 768 of 1024 tokens
-// 520 / 664, 1024 695 / 597.
-constexpr uint64_t kFewColumns = 768;
+// Groups of 16 columns up to which wavefronts share them.  Training, shared / each its own, in us: heads of 128 x 128 384 groups of 2048 tokens 583 / 1007, 512 683 / 747, 768 of 1024 tokens
+// 520 / 664, 1024 695 / 597;  of 127 x 128, value by value, 400 groups 801 / 998, 720 (fp32) 1651 / 1571;  of 64 columns of keys 300 groups 636 / 641, 600 746 / 694;  of 32 300 groups 480 / 508,
+// 600 561 / 529.
+constexpr uint64_t kFewColumns = 512, kFewLargeColumns = 768;
 
 template <class T, int KS, bool kQ = true>
 struct Operands {
@@ -103,19 +105,47 @@ __device__ __forceinline__ void put(const float (&v)[8], uint32_t t, uint32_t co
     for (int p = 0; p < n; ++p) *reinterpret_cast<u32x4 *>(&rows[p][line(t)][col]) = (u32x4){w[p][0], w[p][1], w[p][2], w[p][3]};
 }
 
-// The same of eight that came as they lie, halves of them behind D as 0
+// Eight values on their way, as they lie: in whole 16 bytes (kVec) or one by one
+template <class T, bool kVec>
+struct Eight {
+    static constexpr int m = 16 / sizeof(T);
+    u32x4 w[kVec ? 8 / m : 1];
+    T v[kVec ? 1 : 8];
+
+    // of the row that lies `row` bytes behind, from column c on; another column's from D on, which is cleared where they are used: not before, so that nothing waits for the load
+    __device__ __forceinline__ void load(const uint8_t *base, uint32_t row, uint32_t c, uint32_t D)
+    {
+        if constexpr (kVec) {
+#pragma unroll
+            for (int h = 0; h < 8 / m; ++h) w[h] = *reinterpret_cast<const u32x4 *>(base + (row + (c + h * m < D ? c + h * m : 0) * (uint32_t)sizeof(T)));
+        } else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const T *>(base + (row + (c + i < D ? c + i : 0) * (uint32_t)sizeof(T)));
+    }
+
+    __device__ __forceinline__ dg_rows::Pack<T, 8> values(bool in, uint32_t c, uint32_t D) const
+    {
+        dg_rows::Pack<T, 8> p;
+        if constexpr (kVec) {
+            u32x4 clear[8 / m];
+#pragma unroll
+            for (int h = 0; h < 8 / m; ++h)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) clear[h][x] = in && c + h * m < D ? w[h][x] : 0u;
+            p = __builtin_bit_cast(dg_rows::Pack<T, 8>, clear);
+        } else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p.v[i] = in && c + i < D ? v[i] : (T)0.0f;
+        return p;
+    }
+};
+
+// eight of a token, in pieces
 template <class T, int KS>
-__device__ __forceinline__ void put_raw(const u32x4 (&v)[sizeof(T) / 2], bool in, uint32_t col, uint32_t D, uint32_t t, uint16_t (&rows)[Pieces<T>::n][kChunk][32 * KS + 8])
+__device__ __forceinline__ void put_eight(const dg_rows::Pack<T, 8> &p, uint32_t t, uint32_t col, uint16_t (&rows)[Pieces<T>::n][kChunk][32 * KS + 8])
 {
-    constexpr int m = 16 / sizeof(T);
-    u32x4 clear[sizeof(T) / 2];
-#pragma unroll
-    for (int h = 0; h < 8 / m; ++h)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) clear[h][x] = in && col + h * m < D ? v[h][x] : 0u;
-    if constexpr (Pieces<T>::n == 1) *reinterpret_cast<u32x4 *>(&rows[0][line(t)][col]) = clear[0];
+    if constexpr (Pieces<T>::n == 1) *reinterpret_cast<u32x4 *>(&rows[0][line(t)][col]) = __builtin_bit_cast(u32x4, p);
     else {
-        const dg_rows::Pack<T, 8> p = __builtin_bit_cast(dg_rows::Pack<T, 8>, clear);
         float x[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = (float)p.v[i];
@@ -136,9 +166,9 @@ struct Place {
 };
 
 // K and Q of a chunk on their way to LDS, kEach vectors of each for a lane: a workgroup has wavefronts enough for that
-template <class T, int KS, int kEach>
+template <class T, int kEach, bool kVec>
 struct Fetched {
-    u32x4 qs[kEach][sizeof(T) / 2], ks[kEach][sizeof(T) / 2];
+    Eight<T, kVec> qs[kEach], ks[kEach];
 };
 
 template <class T, int KS, int kEach, bool kVec>
@@ -153,43 +183,28 @@ struct Rows {
     __device__ __forceinline__ uint32_t column() const { return lane % (4 * KS) * 8; }
 
     // a vector where there is one, otherwise another, which store() clears; one address for the workgroup, 32-bit distances from it (32 rows of at most 2^24 values)
-    __device__ __forceinline__ void fetch(uint32_t c, Fetched<T, KS, kEach> &to) const
+    __device__ __forceinline__ void fetch(uint32_t c, Fetched<T, kEach, kVec> &to) const
     {
-        if (!kVec) return;
-        constexpr int m = 16 / sizeof(T);
         const Place at(span, c * kChunk);
         const uint8_t *const k0 = (const uint8_t *)(k + at.row * ldk), *const q0 = (const uint8_t *)(q + at.row * ldq);
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const uint32_t row = at.behind(token(i)), to_k = row * (uint32_t)ldk * sizeof(T), to_q = row * (uint32_t)ldq * sizeof(T);
-#pragma unroll
-            for (int h = 0; h < 8 / m; ++h) {
-                const uint32_t col = (column() + h * m < Dk ? column() + h * m : 0) * sizeof(T);
-                to.ks[i][h] = *reinterpret_cast<const u32x4 *>(k0 + (to_k + col));
-                to.qs[i][h] = *reinterpret_cast<const u32x4 *>(q0 + (to_q + col));
-            }
+            const uint32_t row = at.behind(token(i));
+            to.ks[i].load(k0, row * (uint32_t)ldk * sizeof(T), column(), Dk);
+            to.qs[i].load(q0, row * (uint32_t)ldq * sizeof(T), column(), Dk);
         }
     }
 
     template <bool kQ>
-    __device__ __forceinline__ void store(uint32_t c, const Fetched<T, KS, kEach> &from, Keys<T, KS, kQ> &to) const
+    __device__ __forceinline__ void store(uint32_t c, const Fetched<T, kEach, kVec> &from, Keys<T, KS, kQ> &to) const
     {
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const uint32_t t = token(i);
             if (t >= kChunk) continue;
             const bool in = c * kChunk + t < span.len;
-            if constexpr (kVec) {
-                put_raw<T, KS>(from.ks[i], in, column(), Dk, t, to.K);
-                if constexpr (kQ) put_raw<T, KS>(from.qs[i], in, column(), Dk, t, to.Q);
-            } else {
-                float x[8], y[8];
-                const uint64_t row = span.row(in ? c * kChunk + t : c * kChunk);
-                eight<T, false>(k + row * ldk, column(), Dk, in, x);
-                eight<T, false>(q + row * ldq, column(), Dk, in, y);
-                put<n, KS>(x, t, column(), to.K);
-                if constexpr (kQ) put<n, KS>(y, t, column(), to.Q);
-            }
+            put_eight<T, KS>(from.ks[i].values(in, column(), Dk), t, column(), to.K);
+            if constexpr (kQ) put_eight<T, KS>(from.qs[i].values(in, column(), Dk), t, column(), to.Q);
         }
     }
 };
@@ -204,7 +219,7 @@ __device__ __forceinline__ void along(const Delta &d, const Span &span, uint32_t
     const uint64_t slot0 = first_chunk(span, seq);
     auto chunk = [&](uint32_t i) { return kBackward ? chunks - 1 - i : i; };
     Rows<T, KS, 2, kVec> rows = {(const T *)d.q + hk * d.Dk, (const T *)d.k + hk * d.Dk, d.ldq, d.ldk, d.Dk, wave, waves, threadIdx.x % 64, span};
-    Fetched<T, KS, 2> fetched;
+    Fetched<T, 2, kVec> fetched;
     auto weights = [&](uint32_t i) {
         const uint8_t *from = (const uint8_t *)(d.weights + (slot0 + chunk(i)) * d.H + head) + threadIdx.x % 64 * 16;
         uint8_t *to = (uint8_t *)&room.ops[i % kBuffers].weight;
@@ -234,7 +249,7 @@ __device__ __forceinline__ void along(const Delta &d, const Span &span, uint32_t
 // ------------------------------------------------------------------------------ along a sequence, few heads
 // With fewer columns than the chip has room for, what bounds is how long a chunk takes a wavefront: so two of them share 16 columns, with up to 64 rows of the memory each.  K S is then a sum
 // over the wavefronts, which goes through LDS (Shares): a chunk has two halves, between barriers, what goes before the sum and what comes after.  All that the next chunk does not wait for
-// is done by others: two for what is made of a chunk's tokens (o, the gradients' part that does not depend on S), some that bring what all need, of rows in whole 16 bytes.
+// is done by others: two for what is made of a chunk's tokens (o, the gradients' part that does not depend on S), some that bring what all need.
 constexpr int kShared = 16;             // columns
 constexpr int kAside = 2;
 
@@ -247,7 +262,7 @@ constexpr int kSharedWaves = kSharers<KS> + kAside + kHelpers<KS>;
 
 template <class T>
 struct alignas(16) Tile {
-    T in[kChunk][kShared + 8];          // v, or gradients of o
+    T in[kChunk][kShared + 16 / sizeof(T)];     // v, or gradients of o
     // a lane's eight tokens of a column
     __device__ __forceinline__ void read(uint32_t lane, float (&out)[8]) const
     {
@@ -269,14 +284,24 @@ struct alignas(16) Tile {
 };
 
 // What wavefronts hand each other; for those aside two buffers, since they are a chunk behind
-template <int KS, bool kBackward, bool kEnds = false>
-struct alignas(16) Shares {
-    f32x4 keys[kSharers<KS>][2][64];                            // K S
-    u32x4 memory[kBackward || kEnds ? 1 : KS][kBackward || kEnds ? 1 : 3][64];    // forward: S in pieces
-    f32x4 left[kEnds ? 1 : 2][kEnds ? 1 : kBackward ? 2 : 4][64];                       // what tokens miss (backward: gradients of what they write), what they write
-    f32x4 ahead[kBackward ? 2 : 1][64];                         // backward: P^T dO
-    u32x4 queried[kBackward ? 3 : 1][64];                       // scale e^G dO, in pieces
+struct Nothing {};
+template <int KS>
+struct Forward {
+    f32x4 left[2][2][64];               // what tokens miss
+    u32x4 memory[KS][3][64];            // S in pieces
+};
+template <bool kEnds>
+struct Backward {
+    f32x4 left[kEnds ? 1 : 2][2][64];   // gradients of what tokens write
+    f32x4 ahead[2][64];                 // P^T dO
+    u32x4 queried[3][64];               // scale e^G dO, in pieces
+};
 
+template <int KS, bool kBackward, bool kEnds = false>
+struct alignas(16) Shares : std::conditional_t<kBackward, Backward<kEnds>, std::conditional_t<kEnds, Nothing, Forward<KS>>> {
+    f32x4 keys[kSharers<KS>][2][64];    // K S
+
+    // all wavefronts' sum
     __device__ __forceinline__ static f32x4 sum(const f32x4 (&of)[kSharers<KS>][2][64], int h, uint32_t lane)
     {
         if constexpr (kSharers<KS> == 2) return of[0][h][lane] + of[1][h][lane];
@@ -296,7 +321,7 @@ struct Helped {
 template <class T, int KS, bool kBackward>
 constexpr bool kHasRoom = sizeof(Helped<T, KS, kBackward>) <= 160 * 1024;
 
-template <class T, int KS, bool kBackward>
+template <class T, int KS, bool kBackward, bool kVec>
 struct Helper {
     static constexpr int kLanes = kHelpers<KS> * 64, kEach = (2 * KS + kHelpers<KS> - 1) / kHelpers<KS>, kWeights = (int)(sizeof(Weights) / 16 + kLanes - 1) / kLanes;
     static_assert(kLanes * 8 >= kChunk * kShared, "a lane has eight values of the tile at most");
@@ -305,10 +330,11 @@ struct Helper {
     const Span &span;
     uint64_t slot0;
     uint32_t head, self, column0;
-    Rows<T, KS, kEach, true> rows;
+    Rows<T, KS, kEach, kVec> rows;
     struct Chunk {
-        Fetched<T, KS, kEach> rows;
-        u32x4 weights[kWeights], in[sizeof(T) / 2];
+        Fetched<T, kEach, kVec> rows;
+        Eight<T, kVec> in;
+        u32x4 weights[kWeights];
     };
 
     __device__ __forceinline__ uint32_t token() const { return self * 8 / kShared % kChunk; }
@@ -316,7 +342,6 @@ struct Helper {
 
     __device__ __forceinline__ void fetch(uint32_t c, Chunk &to) const
     {
-        constexpr int m = 16 / sizeof(T);
         rows.fetch(c, to.rows);
         const u32x4 *from = (const u32x4 *)(d.weights + (slot0 + c) * d.H + head);
 #pragma unroll
@@ -324,23 +349,17 @@ struct Helper {
         const Place at(span, c * kChunk);
         const uint64_t ld = kBackward ? d.lddo : d.ldv;
         const uint8_t *p = (const uint8_t *)((const T *)(kBackward ? d.dout : d.v) + at.row * ld + head * d.Dv);
-        const uint32_t row = at.behind(token()) * (uint32_t)ld, first = column0 + column();
-#pragma unroll
-        for (int h = 0; h < 8 / m; ++h) to.in[h] = *reinterpret_cast<const u32x4 *>(p + (row + (first + h * m < d.Dv ? first + h * m : 0)) * (uint32_t)sizeof(T));
+        to.in.load(p, at.behind(token()) * (uint32_t)ld * sizeof(T), column0 + column(), d.Dv);
     }
 
     __device__ __forceinline__ void put_tile(uint32_t c, const Chunk &from, Tile<T> &tile) const
     {
         if (self * 8 >= kChunk * kShared) return;
-        const bool there = c * kChunk + token() < span.len;
-        constexpr int m = 16 / sizeof(T);
+        const dg_rows::Pack<T, 8> p = from.in.values(c * kChunk + token() < span.len, column0 + column(), d.Dv);
+        struct Halves { u32x4 w[sizeof(T) / 2]; };
+        const Halves h = __builtin_bit_cast(Halves, p);
 #pragma unroll
-        for (int h = 0; h < 8 / m; ++h) {
-            u32x4 part;
-#pragma unroll
-            for (int x = 0; x < 4; ++x) part[x] = there && column0 + column() + h * m < d.Dv ? from.in[h][x] : 0u;
-            *reinterpret_cast<u32x4 *>(&tile.in[token()][column() + h * m]) = part;
-        }
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) *reinterpret_cast<u32x4 *>(&tile.in[token()][column() + i * (16 / (int)sizeof(T))]) = h.w[i];
     }
 
     template <bool kQ>
@@ -355,7 +374,7 @@ struct Helper {
 
 // before(i), after(i) in the wavefronts that have columns, early(i), late(i) in those aside, i counting chunks (backward from the last one): all but early go with the two buffers i % 2; early(i)
 // may read what after(i - 1) left, and both early(i) and late(i) run up to i = number of chunks.  The others have a chunk's time for what they bring for the next one.
-template <class T, int KS, bool kBackward, bool kEnds, class Before, class After, class Early, class Late>
+template <class T, int KS, bool kBackward, bool kEnds, bool kVec, class Before, class After, class Early, class Late>
 __device__ __forceinline__ void along_helped(const Delta &d, const Span &span, uint64_t slot0, uint32_t head, uint32_t column0, Helped<T, KS, kBackward, kEnds> &room, uint32_t wave,
                                              Before before, After after, Early early, Late late)
 {
@@ -385,7 +404,7 @@ __device__ __forceinline__ void along_helped(const Delta &d, const Span &span, u
         late(chunks);
         return;
     }
-    using Help = Helper<T, KS, kBackward>;
+    using Help = Helper<T, KS, kBackward, kVec>;
     const Help h = {d, span, slot0, head, threadIdx.x - kFirst * 64, column0,
                     {(const T *)d.q + hk * d.Dk, (const T *)d.k + hk * d.Dk, d.ldq, d.ldk, d.Dk, wave - kFirst, kHelpers<KS>, threadIdx.x % 64, span}};
     // A chunk is fetched two before it is put; `coming` holds the next one.  Without a branch about a load (behind the last chunk it comes again), so that a wait is for the oldest loads only.
@@ -495,7 +514,7 @@ inline Columns columns_of(const Delta &d, bool room)
 {
     const uint32_t all = (d.Dv + 15) / 16, least = d.Dk <= 32 ? 1 : d.Dk <= 64 ? 2 : 4;
     const uint64_t units = (uint64_t)d.n_seq * d.H;
-    if (room && d.vec_all && units * all <= kFewColumns) return {1, 0, all, true};
+    if (room && units * all <= (d.Dk > 64 && d.vec_all ? kFewLargeColumns : kFewColumns)) return {1, 0, all, true};
     uint32_t with = all < (uint32_t)kMostWaves ? all : kMostWaves;
     while (with > 1 && units * ((all + with - 1) / with) < 256) with = (with + 1) / 2;        // few heads: as many workgroups as there are compute units
     return {with, with < least ? least : with, (all + with - 1) / with, false};

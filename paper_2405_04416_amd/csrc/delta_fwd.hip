@@ -78,7 +78,7 @@ struct Share {
     static constexpr int n = Pieces<T>::n, kOwn = KS / kSharers<KS>;
     f32x4 S[2 * kOwn];
     bf16x8 inverse[2][3], turned[2 * kOwn][n];
-    f32x4 read[2], beta[2], until[2];
+    f32x4 read[2], written[2];          // of what tokens miss, what the memory gets: beta e^(G[last] - G)
     float value[8], whole;
 
     // up to the sum K S; then all that comes after it is read
@@ -116,8 +116,7 @@ struct Share {
         for (int h = 0; h < 2; ++h) lefts(o.weight.inverse, h * 16 + c16, r8, inverse[h]);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            beta[h] = *reinterpret_cast<const f32x4 *>(&o.weight.beta[r8 + h * 4]);
-            until[h] = *reinterpret_cast<const f32x4 *>(&o.weight.until[r8 + h * 4]);
+            written[h] = *reinterpret_cast<const f32x4 *>(&o.weight.beta[r8 + h * 4]) * *reinterpret_cast<const f32x4 *>(&o.weight.until[r8 + h * 4]);
         }
 #pragma unroll
         for (int t = 0; t < 2 * kOwn; ++t) lefts_turned(o.key.K, wave * kOwn + t / 2, t % 2, lane, turned[t]);
@@ -126,30 +125,25 @@ struct Share {
 
     __device__ __forceinline__ void after(Shares<KS, false, kEnds> &shares, uint32_t parity, uint32_t wave, uint32_t lane)
     {
-        f32x4 r[2], u[2], y[2];
+        f32x4 r[2], y[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const f32x4 ks = shares.sum(shares.keys, h, lane);
 #pragma unroll
             for (int x = 0; x < 4; ++x) r[h][x] = value[h * 4 + x] - read[h][x] * ks[x];
         }
-        bf16x8 right[3], written[3];
+        bf16x8 right[3];
         split_rows<3>(r[0], r[1], right);
 #pragma unroll
         for (int h = 0; h < 2; ++h) y[h] = multiply_soon<3, 3>(inverse[h], right, (f32x4){});
+        split_rows<3>(y[0] * written[0], y[1] * written[1], right);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) u[h] = y[h] * beta[h];
-        split_rows<3>(u[0] * until[0], u[1] * until[1], written);
-#pragma unroll
-        for (int t = 0; t < 2 * kOwn; ++t) S[t] = multiply<n, 3>(turned[t], written, S[t] * whole);
+        for (int t = 0; t < 2 * kOwn; ++t) S[t] = multiply<n, 3>(turned[t], right, S[t] * whole);
         // for those aside
         if constexpr (!kEnds)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-            if (wave == h % kSharers<KS>) {
-                shares.left[parity][h][lane] = y[h];
-                shares.left[parity][2 + h][lane] = u[h];
-            }
+            for (int h = 0; h < 2; ++h)
+                if (wave == h % kSharers<KS>) shares.left[parity][h][lane] = y[h];
     }
 };
 
@@ -176,8 +170,14 @@ struct Outputs {
     }
     __device__ __forceinline__ void read(const Operands<T, KS> &o, const Shares<KS, false> &shares, uint32_t parity, uint32_t h, uint32_t lane)
     {
-        lefts(o.weight.P, h * 16 + lane % 16, lane / 16 * 8, pull);
-        u[0] = shares.left[parity][2][lane], u[1] = shares.left[parity][3][lane], y = shares.left[parity][h][lane];
+        const uint32_t r8 = lane / 16 * 8;
+        lefts(o.weight.P, h * 16 + lane % 16, r8, pull);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const f32x4 v = shares.left[parity][i][lane];
+            u[i] = v * *reinterpret_cast<const f32x4 *>(&o.weight.beta[r8 + i * 4]);
+            if (i == (int)h) y = v;
+        }
     }
     __device__ __forceinline__ f32x4 make() const
     {
@@ -187,7 +187,7 @@ struct Outputs {
     }
 };
 
-template <class T, int KS, bool kEnds>
+template <class T, int KS, bool kEnds, bool kVec>
 __global__ void __launch_bounds__(kSharedWaves<KS> * 64)
 delta_fwd_shared_kernel(Delta d, uint32_t groups, uint64_t from)
 {
@@ -207,7 +207,7 @@ delta_fwd_shared_kernel(Delta d, uint32_t groups, uint64_t from)
     else if (unit.part == 0) load_memory<Mine::kOwn>(d.s0 ? d.s0 + first * d.Dv + col : nullptr, rows, d.Dv, in, r8, share.S);
     else load_memory<Mine::kOwn>(kEnds ? nullptr : d.starts + later * d.Dv + col, rows, d.Dv, in, r8, share.S);
     Outputs<T, KS> outputs;
-    along_helped<T, KS, false, kEnds>(d, span, place.slot, head, column0, room, wave,
+    along_helped<T, KS, false, kEnds, kVec>(d, span, place.slot, head, column0, room, wave,
         [&](uint32_t c) {
             share.before(room.ops[c % 2], room.tiles[c % 2], room.shares, wave, lane);
             if (!kEnds && d.marks && c % (kMark / kChunk) == 0)
@@ -277,12 +277,14 @@ void launch_size(Delta d, hipStream_t st)
     if constexpr (kRoom)
         if (c.helped) {
             cut(d, 160 * 1024 / sizeof(Helped<T, KS, false, true>), 160 * 1024 / sizeof(Helped<T, KS, false>));
+            const uint32_t groups = d.ends_width() / kShared, first = d.n_seq * d.H * (d.parts - 1) * groups, all = d.n_seq * d.H * d.parts * c.groups, threads = kSharedWaves<KS> * 64;
             if (d.parts > 1) {
-                const uint32_t groups = d.ends_width() / kShared;
-                delta_fwd_shared_kernel<T, KS, true><<<d.n_seq * d.H * (d.parts - 1) * groups, kSharedWaves<KS> * 64, 0, st>>>(d, groups, 0);
+                if (d.vec_all) delta_fwd_shared_kernel<T, KS, true, true><<<first, threads, 0, st>>>(d, groups, 0);
+                else delta_fwd_shared_kernel<T, KS, true, false><<<first, threads, 0, st>>>(d, groups, 0);
                 launch_join(d, st);
             }
-            delta_fwd_shared_kernel<T, KS, false><<<d.n_seq * d.H * d.parts * c.groups, kSharedWaves<KS> * 64, 0, st>>>(d, c.groups, 0);
+            if (d.vec_all) delta_fwd_shared_kernel<T, KS, false, true><<<all, threads, 0, st>>>(d, c.groups, 0);
+            else delta_fwd_shared_kernel<T, KS, false, false><<<all, threads, 0, st>>>(d, c.groups, 0);
             return;
         }
     const uint64_t units = (uint64_t)d.n_seq * d.H * c.groups;
