@@ -75,6 +75,62 @@ __device__ __forceinline__ float group_max(float v)
     return v;
 }
 
+// What is rounded to 8 bits is known to some 2^-40 before: fp32 arithmetic would leave one value in half a million on the other side of a step of e4m3, a sixteenth of it away.  Sums of squares
+// are taken in 64 bits, the scale and its products in two parts of 32.  All of it hides behind the loads.
+template <int C>
+__device__ __forceinline__ double exchanged2(double v)
+{
+    struct Halves { float lo, hi; };
+    Halves h = __builtin_bit_cast(Halves, v);
+    h.lo = exchanged<C>(h.lo), h.hi = exchanged<C>(h.hi);
+    return __builtin_bit_cast(double, h);
+}
+
+template <int G>
+__device__ __forceinline__ double group_sum2(double v)
+{
+    if (G >= 2) v += exchanged2<0xb1>(v);
+    if (G >= 4) v += exchanged2<0x4e>(v);
+    if (G >= 8) v += exchanged2<0x141>(v);
+    if (G >= 16) v += exchanged2<0x140>(v);
+    if (G >= 32) v += __shfl_xor(v, 16);
+    if (G >= 64) v += __shfl_xor(v, 32);
+    return v;
+}
+
+template <int G, int kThreads>
+__device__ __forceinline__ double row_sum2(double v, double *red)
+{
+    v = group_sum2<(G < dg::kWave ? G : dg::kWave)>(v);
+    if (G <= dg::kWave) return v;
+    __syncthreads();                                // the last use of red is over
+    if (threadIdx.x % dg::kWave == 0) red[threadIdx.x / dg::kWave] = v;
+    __syncthreads();
+    v = 0.0;
+#pragma unroll
+    for (int w = 0; w < kThreads / dg::kWave; ++w) v += red[w];
+    return v;
+}
+
+struct Scale {
+    float s, rest;
+    // 1 / sqrt(squares / W + eps): fp32, then a step of Newton's
+    __device__ __forceinline__ Scale(double squares, uint32_t W, float eps)
+    {
+        const double m = squares / W + eps;
+        const float s0 = 1.0f / sqrtf((float)m);
+        const double off = fma(-m * s0, (double)s0, 1.0), exact = fma(0.5 * s0, off, (double)s0);
+        s = off == off ? (float)exact : s0;         // of infinities and NaN as in fp32
+        rest = off == off ? (float)(exact - s) : 0.0f;
+    }
+    __device__ __forceinline__ float times(float x, float gamma) const
+    {
+#pragma clang fp contract(off)
+        const float p = x * s, p_off = fmaf(x, rest, fmaf(x, s, -p)), y = p * gamma;
+        return y + fmaf(p_off, gamma, fmaf(p, gamma, -y));
+    }
+};
+
 // A row in registers to 8 bits.  A vector's lane stores it at its own place; of a row's last vector, where it begins early, only what is its own.
 template <int V, int G, int K, bool kLoose>
 __device__ __forceinline__ void store8(const float (&y)[K][V], const Rms &a, uint64_t row, bool held, uint32_t lane)
@@ -122,6 +178,7 @@ rms_fwd_kernel(Rms a)
     constexpr int R = kThreads / G;
     constexpr bool kAhead = K > 1;
     __shared__ float red[kThreads / dg::kWave][1];
+    __shared__ double red2[kMade == kNormed8 ? kThreads / dg::kWave : 1];
     const uint32_t lane = threadIdx.x % G;
     float gamma[K][V];
     if (kMade != kPlain8) weights<V, G, K, kLoose>(a.gamma, 1.0f, a, lane, gamma);
@@ -150,7 +207,20 @@ rms_fwd_kernel(Rms a)
         row += (uint64_t)gridDim.x * R;
         if (kAhead) fetch();
         uint32_t c;
-        if (kMade != kPlain8) {
+        if (kMade == kNormed8) {
+            double sum = 0.0;
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int from = skipped<V, kLoose>(a.W, (k * G + lane) * V);
+#pragma unroll
+                for (int v = 0; v < V; ++v) sum = kLoose && v < from ? sum : fma((double)x[k][v], (double)x[k][v], sum);
+            }
+            const Scale s(row_sum2<G, kThreads>(sum, red2), a.W, a.eps);
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int v = 0; v < V; ++v) x[k][v] = s.times(x[k][v], gamma[k][v]);
+        } else if (kMade != kPlain8) {
             float sum[1] = {0.0f};
 #pragma unroll
             for (int k = 0; k < K; ++k) {
@@ -200,16 +270,31 @@ __device__ __forceinline__ float wide_scale(const T *x, const T *r, const Rms &a
     return 1.0f / sqrtf(sum[0] / (float)a.W + a.eps);
 }
 
+template <class T>
+__device__ __forceinline__ Scale wide_scale2(const T *x, const T *r, const Rms &a, double *red)
+{
+    double sum = 0.0;
+    for (uint32_t c = threadIdx.x; c < a.W; c += kWide) {
+        const double t = r ? (double)(float)(T)((float)x[c] + (float)r[c]) : (double)(float)x[c];
+        sum = fma(t, t, sum);
+    }
+    return Scale(row_sum2<kWide, kWide>(sum, red), a.W, a.eps);
+}
+
 template <class T, Made kMade>
 __global__ void __launch_bounds__(kWide)
 rms_fwd_wide_kernel(Rms a)
 {
     __shared__ float red[kWide / dg::kWave][1];
+    __shared__ double red2[kMade == kNormed8 ? kWide / dg::kWave : 1];
     const uint32_t wave = threadIdx.x / dg::kWave, lane = threadIdx.x % dg::kWave;
     for (uint64_t row = blockIdx.x; row < a.N; row += gridDim.x) {
         const T *x = (const T *)a.x + row * a.ldx, *r = a.r ? (const T *)a.r + row * a.ldr : nullptr;
         T *t = a.t ? (T *)a.t + row * a.ldt : nullptr;
-        const float s = kMade == kPlain8 ? 1.0f : wide_scale<T>(x, r, a, red);
+        float s = 1.0f;
+        Scale exact(1.0, 1, 0.0f);
+        if (kMade == kNormed) s = wide_scale<T>(x, r, a, red);
+        if (kMade == kNormed8) exact = wide_scale2<T>(x, r, a, red2);
         // a wavefront takes a block of columns, two to a lane; a lane reads the places that it stores to, and no others
         for (uint32_t c0 = wave * kScaled; c0 < a.W; c0 += kWide / dg::kWave * kScaled) {
             float y[2];
@@ -221,7 +306,8 @@ rms_fwd_wide_kernel(Rms a)
                 if (c >= a.W) continue;
                 const T sum = r ? (T)((float)x[c] + (float)r[c]) : x[c];
                 y[i] = (float)sum;
-                if (kMade != kPlain8) y[i] = y[i] * s * (a.gamma ? a.gamma[c] : 1.0f);
+                if (kMade == kNormed) y[i] = y[i] * s * (a.gamma ? a.gamma[c] : 1.0f);
+                if (kMade == kNormed8) y[i] = exact.times(y[i], a.gamma ? a.gamma[c] : 1.0f);
                 if (t) t[c] = sum;
                 if (kMade == kNormed) ((T *)a.out + row * a.ldo)[c] = (T)y[i];
                 largest = fmaxf(largest, finite_size(y[i]));
