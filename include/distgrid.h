@@ -638,7 +638,7 @@ int dg_e4m3_product(const void *a, uint64_t lda, const uint8_t *a_scales, uint64
  * first, reverse: as for dg_recurrence_fwd.  One token per sequence (N == n_seq), or a few, is the step of a program that gets its tokens one after the other.
  * saved: NULL, or dg_delta_rule_saved_bytes(N, n_seq, H, Dk, Dv) bytes for the backward pass, 16-byte aligned (what tokens write, and the memories before every
  * 64th).  ws: dg_delta_rule_fwd_workspace_bytes(N, n_seq, H) bytes, 16-byte aligned; not needed without `saved` for up to four tokens a sequence (N <= 4 n_seq).
- * dg_delta_rule_workspace_bytes(N, n_seq, Hk, H, Dk, Dv) are enough for either pass; no call needs what another left there.
+ * dg_delta_rule_workspace_bytes(N, n_seq, Hk, H, Dk, Dv) are enough for either pass; no call needs what another left there.  Long sequences of one length and few heads are worked on in parts.
  * Everything is as exact as in fp32, and the same call gives the same bits.  Tokens are taken 32 or 64 at a time: an infinity or NaN in a token's row may show in
  * the results of up to 63 tokens before it.  o must not overlap an input.
  * Errors: DG_ERR_ARG for heads or sizes of 0, H that Hk does not divide, N that n_seq does not divide (first NULL), a scale that is not finite;

@@ -38,6 +38,12 @@ inline uint64_t chunk_slots(uint64_t N, uint32_t n_seq) { return N / kChunk + n_
 
 __device__ __forceinline__ uint64_t first_chunk(const Span &s, uint32_t seq) { return s.begin / kChunk + seq; }
 
+__device__ __forceinline__ void wave_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 s16x4_in_lds;
 
@@ -268,6 +274,7 @@ struct alignas(16) Tile {
     {
         const uint32_t c16 = lane % 16, r8 = lane / 16 * 8;
         if constexpr (sizeof(T) == 2) {
+            wave_fence();               // what others have stored is read, of which the compiler sees nothing
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4_in_lds *)&in[r8 + h * 4 + c16 / 4][c16 % 4 * 4]);
@@ -277,6 +284,7 @@ struct alignas(16) Tile {
                     out[h * 4 + x] = (float)__builtin_bit_cast(T, bits);
                 }
             }
+            wave_fence();
         } else
 #pragma unroll
             for (int x = 0; x < 8; ++x) out[x] = (float)in[r8 + x][c16];
@@ -612,12 +620,14 @@ __device__ __forceinline__ void lefts(const uint16_t (&m)[n][rows][pitch], uint3
 template <int n, int pitch>
 __device__ __forceinline__ void lefts_turned(const uint16_t (&m)[n][kChunk][pitch], uint32_t s, uint32_t h, uint32_t lane, bf16x8 (&out)[n])
 {
+    wave_fence();                       // what others have stored is read, of which the compiler sees nothing
 #pragma unroll
     for (int p = 0; p < n; ++p) {
         const uint16_t *at = &m[p][lane / 4][s * 32 + h * 4 + lane % 4 * 8];            // tokens 8 (lane / 16) on lie in rows 4 (lane / 16) on, and 16 rows on
         const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4_in_lds *)at), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4_in_lds *)(at + 16 * pitch));
         out[p] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
     }
+    wave_fence();
 }
 
 }  // namespace dg_delta

@@ -179,12 +179,6 @@ __device__ __forceinline__ uint32_t again(uint32_t x)
     return x;
 }
 
-__device__ __forceinline__ void wave_fence()
-{
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
 inline bool wide_rows(const void *p, uint64_t ld, uint32_t D, uint32_t dtype)
 {
     return dg_rows::rows_aligned(p, ld, dtype, 16) && D * dg_rows::item_bytes(dtype) % 16 == 0;

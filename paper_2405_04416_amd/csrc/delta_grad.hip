@@ -7,6 +7,8 @@
 // A workgroup takes 64 tokens of a key head, one value head after the other, 32 columns of values at a time through LDS (in pieces, cut once for all), a wavefront
 // 16 tokens and half of the columns of keys: a lane has a token, of which everything above is a column of a product.  X and Z are made once, block by block,
 // and go through LDS by rows and by columns.
+// Bound by cutting into pieces and by LDS: 2 x 8192 tokens x 16 heads of 128 x 128, bf16, 0.40 ms, five times what its matrix instructions alone would take; 2003 ragged sequences x 3 heads of
+// 24 x 40, fp32, 0.36 ms.
 #include "delta_chunk.h"
 #include "rows_vectors.h"
 

