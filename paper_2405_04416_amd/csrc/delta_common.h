@@ -193,7 +193,7 @@ void launch_forward(const Delta &d, uint32_t dtype, hipStream_t st);
 void launch_small(const Delta &d, uint32_t dtype, bool back, hipStream_t st);        // heads of up to 32 x 32
 void launch_slots(const Delta &d, hipStream_t st);
 size_t parts_bytes(uint64_t N, uint32_t n_seq, uint32_t H);
-void launch_join(const Delta &d, hipStream_t st);
+void launch_join(const Delta &d, const float *before, hipStream_t st);        // before: memories before the first parts, or NULL
 void launch_tokens(const Delta &d, uint32_t dtype, hipStream_t st);
 void launch_backward(const Delta &d, uint32_t dtype, hipStream_t st);
 void launch_gradients(const Delta &d, uint32_t dtype, hipStream_t st);

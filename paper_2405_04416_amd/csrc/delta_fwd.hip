@@ -208,7 +208,7 @@ delta_fwd_shared_kernel(Delta d, uint32_t groups, uint64_t from)
     const uint64_t first = ((uint64_t)seq * d.H + head) * d.Dk + row0, later = (((uint64_t)seq * d.parts + unit.part) * d.H + head) * d.Dk + row0;
     Mine share;
     if (kEnds && column0 >= one) unit_memory<Mine::kOwn>(col - one, row0, r8, share.S);
-    else if (unit.part == 0) load_memory<Mine::kOwn>(d.s0 ? d.s0 + first * d.Dv + col : nullptr, rows, d.Dv, in, r8, share.S);
+    else if (unit.part == 0 && (kEnds || d.parts == 1)) load_memory<Mine::kOwn>(d.s0 ? d.s0 + first * d.Dv + col : nullptr, rows, d.Dv, in, r8, share.S);
     else load_memory<Mine::kOwn>(kEnds ? nullptr : d.starts + later * d.Dv + col, rows, d.Dv, in, r8, share.S);
     Outputs<T, KS> outputs;
     along_helped<T, KS, false, kEnds, kVec>(d, span, place.slot, head, column0, room, wave,
@@ -285,7 +285,7 @@ void launch_size(Delta d, hipStream_t st)
             if (d.parts > 1) {
                 if (d.vec_all) delta_fwd_shared_kernel<T, KS, true, true><<<first, threads, 0, st>>>(d, groups, 0);
                 else delta_fwd_shared_kernel<T, KS, true, false><<<first, threads, 0, st>>>(d, groups, 0);
-                launch_join(d, st);
+                launch_join(d, d.s0, st);
             }
             if (d.vec_all) delta_fwd_shared_kernel<T, KS, false, true><<<all, threads, 0, st>>>(d, c.groups, 0);
             else delta_fwd_shared_kernel<T, KS, false, false><<<all, threads, 0, st>>>(d, c.groups, 0);

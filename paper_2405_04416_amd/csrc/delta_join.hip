@@ -9,11 +9,19 @@ using namespace dg_delta;
 constexpr int kThreads = 256, kColumns = 16;
 
 __global__ void __launch_bounds__(kThreads)
-delta_join_kernel(Delta d, uint32_t groups)
+delta_join_kernel(Delta d, uint32_t groups, const float *before)
 {
     __shared__ f32x4 lds[2][kMaxD][kColumns / 4];
     const uint32_t group = blockIdx.x % groups, head = blockIdx.x / groups % d.H, seq = blockIdx.x / groups / d.H, row = threadIdx.x / 4, four = threadIdx.x % 4;
     const uint32_t width = d.ends_width(), one = (d.Dv + 15) / 16 * 16, col = group * kColumns + four * 4;
+    // The first part's beginning with the others': what the last one leaves may lie in its place
+    for (uint32_t r = row; r < d.Dk; r += kThreads / 4)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+            if (col + x < d.Dv) {
+                const uint64_t at = (((uint64_t)seq * d.H + head) * d.Dk + r) * d.Dv + col + x;
+                d.starts[((((uint64_t)seq * d.parts) * d.H + head) * d.Dk + r) * d.Dv + col + x] = before ? before[at] : 0.0f;
+            }
     for (uint32_t p = 0; p + 1 < d.parts; ++p) {
         const uint64_t at = (((uint64_t)seq * d.parts + p) * d.H + head) * d.Dk;
         const float *ends = d.ends + at * width;
@@ -50,8 +58,8 @@ size_t dg_delta::parts_bytes(uint64_t N, uint32_t n_seq, uint32_t H)
     return (size_t)most * kMaxD * 3 * kMaxD * sizeof(float);
 }
 
-void dg_delta::launch_join(const Delta &d, hipStream_t st)
+void dg_delta::launch_join(const Delta &d, const float *before, hipStream_t st)
 {
     const uint32_t groups = (d.Dv + kColumns - 1) / kColumns;
-    delta_join_kernel<<<d.n_seq * d.H * groups, kThreads, 0, st>>>(d, groups);
+    delta_join_kernel<<<d.n_seq * d.H * groups, kThreads, 0, st>>>(d, groups, before);
 }

@@ -508,6 +508,9 @@ def alike(what, value, want, plain, terms, dtype):
     """Off by no more, in root mean square, than eight times what the formulas in fp32 are (and a few roundings of the values, where those happen to be exact), besides the
     rounding to the type; sums of terms that cancel by that much of the terms."""
     err, limit = rms(got(value).reshape(want.shape) - want), 8 * rms(plain - want) + (8 * U + T_OF[dtype]) * rms(want) + 16 * U * rms(terms) + LEAST[dtype]
+    # Of a few numbers the formulas' own error may be next to nothing by chance.  They are sums of terms of about one, which cancel: each token rounds some four times to half a unit of one, and
+    # with half of the memory forgotten at each token three or so count: 12 U, 16 with what is cut off.
+    if want.size < 16: limit += 16 * U
     assert err <= limit, "%s: off by %.3g of %.3g, %.3g allowed" % (what, err, rms(want), limit)
 
 
@@ -729,7 +732,7 @@ def test_delta_rule_heads_in_one_row():
 def test_delta_rule_memory_in_place():
     """s_last in s0's place, and ds0 in ds_last's: the same bits."""
     say("delta rule in place")
-    for n_seq, S, H, D in ((2, 70, 2, 64), (800, 20, 1, 16)):
+    for n_seq, S, H, D in ((2, 70, 2, 64), (800, 20, 1, 16), (1, 1700, 2, 64), (2, 3000, 1, 32)):
         a = delta_inputs(np.random.default_rng(7), n_seq * S, H, H, D, D, n_seq, torch.float16)
         want = run_delta(a, n_seq, None, torch.float16)
         t = {n: torch.from_numpy(a[n].reshape(n_seq * S, -1)).to(DEV, torch.float16) for n in ("q", "k", "v", "do")}
@@ -854,3 +857,20 @@ def test_calls_in_a_graph():
         other[-1]["y"].float().sum()
         torch.cuda.synchronize()
         for n in RESULTS: assert torch.equal(args[-1][n], other[-1][n]), (i, n)
+
+
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("n_seq,S,Hk,H,Dk,Dv,dtype", [(1, 2000, 2, 4, 64, 33, "bf16"), (2, 1600, 1, 3, 31, 20, "fp16"), (1, 1700, 1, 1, 128, 128, "fp32"), (1, 1540, 1, 1, 1, 1, "fp32")])
+def test_delta_rule_in_parts_without_memories(n_seq, S, Hk, H, Dk, Dv, dtype, reverse):
+    """Long sequences of few heads from no memory, shared keys, rows of any size; the gradient of the last memory is 0."""
+    say("delta rule parts", n_seq, S, Hk, H, Dk, Dv, dtype, reverse)
+    a = delta_inputs(np.random.default_rng(S), n_seq * S, Hk, H, Dk, Dv, n_seq, TYPES[dtype], carry=False)
+    check_delta(a, n_seq, None, TYPES[dtype], reverse, pad=1 if Dv % 8 else 0)
+
+
+def test_delta_rule_in_parts_forgets():
+    """Gates that are shut in the middle of a part, and at its edges."""
+    say("delta rule parts shut")
+    a = delta_inputs(np.random.default_rng(3), 3000, 1, 2, 64, 64, 1, torch.float16)
+    for t in (0, 511, 512, 700, 1023, 1024, 1500, 2047, 2048, 2999): a["g"][t] = -np.inf
+    check_delta(a, 1, None, torch.float16)
