@@ -768,18 +768,73 @@ def test_delta_rule_gradient_against_differences():
         assert abs((f[0] - f[1]) / (2 * h) - d) <= noise / h + 30 * h * h * size, n
 
 
-def test_delta_rule_of_nothing():
-    say("delta rule empty")
-    x, g = torch.zeros(0, 64, device=DEV), torch.zeros(0, 2, device=DEV)
-    s0 = torch.randn(3, 2, 32, 32, device=DEV)
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_delta_rule_of_nothing(D):
+    say("delta rule empty", D)
+    x, g = torch.zeros(0, 2 * D, device=DEV), torch.zeros(0, 2, device=DEV)
+    s0 = torch.randn(3, 2, D, D, device=DEV)
     room = lambda n: torch.empty(max(n, 16), dtype=torch.uint8, device=DEV)
     for first in (None, torch.zeros(4, dtype=torch.int32, device=DEV)):
-        s_last, ds0 = torch.zeros_like(s0), torch.zeros_like(s0)
-        B.dg_delta_rule_fwd(x, x, x, g, g, 2, 3, first, False, 1.0, s0, x, s_last, room(B.dg_delta_rule_saved_bytes(0, 3, 2, 32, 32)), room(B.dg_delta_rule_fwd_workspace_bytes(0, 3, 2)))
-        B.dg_delta_rule_bwd(x, x, x, g, g, 2, 3, first, False, 1.0, room(B.dg_delta_rule_saved_bytes(0, 3, 2, 32, 32)), x, s0, x, x, x, g, g, ds0,
-                            room(B.dg_delta_rule_workspace_bytes(0, 3, 2, 2, 32, 32)))
-        assert torch.equal(s_last, s0) and torch.equal(ds0, s0)
+        s_last, ds0, alone = torch.zeros_like(s0), torch.zeros_like(s0), torch.zeros_like(s0)
+        saved = room(B.dg_delta_rule_saved_bytes(0, 3, 2, D, D))
+        B.dg_delta_rule_fwd(x, x, x, g, g, 2, 3, first, False, 1.0, s0, x, s_last, saved, room(B.dg_delta_rule_fwd_workspace_bytes(0, 3, 2)))
+        B.dg_delta_rule_bwd(x, x, x, g, g, 2, 3, first, False, 1.0, saved, x, s0, x, x, x, g, g, ds0, room(B.dg_delta_rule_workspace_bytes(0, 3, 2, 2, D, D)))
+        B.dg_delta_rule_fwd(x, x, x, g, g, 2, 3, first, False, 1.0, s0, x, alone)
+        assert torch.equal(s_last, s0) and torch.equal(ds0, s0) and torch.equal(alone, s0)
     B.dg_delta_rule_fwd(x, x, x, g, g, 2, 0, None, False, 1.0, None, x, None)
+
+
+# ------------------------------------------------------------------ rows far apart
+def far(t, ld):
+    """The same values in rows `ld` apart, of storage that is not filled."""
+    view = torch.empty(t.shape[0] * ld, dtype=t.dtype, device=DEV).view(t.shape[0], ld)[:, :t.shape[1]]
+    return view.copy_(t)
+
+
+@pytest.mark.parametrize("n_seq,S,H,D", [(1, 520, 2, 64), (130, 4, 2, 64), (520, 1, 5, 16), (1, 520, 1, 128)])
+def test_delta_rule_of_rows_far_apart(n_seq, S, H, D):
+    """Rows 2^22 values apart, 4 GiB and more from the first to the last: the bits of rows side by side."""
+    say("delta rule far", n_seq, S, H, D)
+    N, ld = n_seq * S, 1 << 22
+    a = delta_inputs(np.random.default_rng(S), N, H, H, D, D, n_seq, torch.float16)
+    want = run_delta(a, n_seq, None, torch.float16)
+    storage = torch.empty(N * ld, dtype=torch.float16, device=DEV).view(N, ld)
+    W, at = H * D, iter(range(0, ld, 4096))
+    place = lambda: storage[:, (lambda c: slice(c, c + W))(next(at))]
+    rows = {n: place().copy_(torch.from_numpy(a[n].reshape(N, -1))) for n in ("q", "k", "v", "do")}
+    outs = {n: place() for n in ("o", "dq", "dk", "dv")}
+    g, beta, s0, ds = (f32(a[n]) for n in ("g", "beta", "s0", "ds_last"))
+    dg, dbeta, s_last, ds0 = torch.zeros_like(g), torch.zeros_like(g), torch.zeros_like(s0), torch.zeros_like(s0)
+    room = lambda n: torch.empty(max(n, 16), dtype=torch.uint8, device=DEV)
+    saved, ws = room(B.dg_delta_rule_saved_bytes(N, n_seq, H, D, D)), room(B.dg_delta_rule_workspace_bytes(N, n_seq, H, H, D, D))
+    B.dg_delta_rule_fwd(rows["q"], rows["k"], rows["v"], g, beta, H, n_seq, None, False, 1.0, s0, outs["o"], s_last, saved, ws)
+    B.dg_delta_rule_bwd(rows["q"], rows["k"], rows["v"], g, beta, H, n_seq, None, False, 1.0, saved, rows["do"], ds, outs["dq"], outs["dk"], outs["dv"], dg, dbeta, ds0, ws)
+    for n, x in dict(outs, dg=dg, dbeta=dbeta, s_last=s_last, ds0=ds0).items(): assert torch.equal(x, want[n]), n
+
+
+@pytest.mark.parametrize("M,N,K", [(600, 70, 130), (10, 600, 256), (700, 800, 128)])
+def test_product_and_norm_of_rows_far_apart(M, N, K):
+    say("product far", M, N, K)
+    ld = (1 << 23) - 16
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(M)
+    x, w = torch.randn(M, K, device=DEV, generator=gen).half(), torch.randn(N, K, device=DEV, generator=gen).half()
+    (_, _, a, sa), (_, _, b, sb) = put8(M, K), put8(N, K)
+    far8 = lambda rows: torch.empty(rows * ld, dtype=torch.uint8, device=DEV).view(rows, ld).view(torch.float8_e4m3fn)[:, :K]
+    a2, b2, sa2, sb2 = far8(M), far8(N), torch.zeros_like(sa), torch.zeros_like(sb)
+    B.dg_rms_norm_e4m3_fwd(x, None, None, 1e-5, None, a, sa)
+    B.dg_rms_norm_e4m3_fwd(far(x, ld // 2), None, None, 1e-5, None, a2, sa2)
+    B.dg_e4m3_rows(w, b, sb)
+    B.dg_e4m3_rows(far(w, ld // 2), b2, sb2)
+    bytes_of = lambda t: t.view(torch.uint8)
+    assert torch.equal(bytes_of(sa), bytes_of(sa2)) and torch.equal(bytes_of(sb), bytes_of(sb2))
+    assert torch.equal(a.float(), a2.float()) and torch.equal(b.float(), b2.float())
+    n = B.dg_e4m3_product_workspace_bytes(M, N, K)
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV) if n else None
+    y, y2 = torch.zeros(M, N, dtype=torch.float16, device=DEV), far(torch.zeros(M, N, dtype=torch.float16, device=DEV), ld // 2)
+    B.dg_e4m3_product(a, sa, b, sb, y, ws)
+    B.dg_e4m3_product(a2, sa2, b2, sb2, y2, ws)
+    assert torch.equal(y, y2)
 
 
 # ------------------------------------------------------------------ streams, graphs
