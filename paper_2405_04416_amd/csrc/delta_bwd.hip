@@ -251,7 +251,7 @@ void launch_size(Delta d, hipStream_t st)
     const Columns c = columns_of(d, kRoom);
     if constexpr (kRoom)
         if (c.helped) {
-            cut(d, 160 * 1024 / sizeof(Helped<T, KS, true, true>), 160 * 1024 / sizeof(Helped<T, KS, true>));
+            cut(d, side_by_side(sizeof(Helped<T, KS, true, true>)), side_by_side(sizeof(Helped<T, KS, true>)));
             const uint32_t groups = d.ends_width() / kShared, first = d.n_seq * d.H * (d.parts - 1) * groups, all = d.n_seq * d.H * d.parts * c.groups, threads = kSharedWaves<KS> * 64;
             if (d.parts > 1) {
                 if (d.vec_all) delta_bwd_shared_kernel<T, KS, true, true><<<first, threads, 0, st>>>(d, groups, 0);

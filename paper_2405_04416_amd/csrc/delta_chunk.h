@@ -25,12 +25,18 @@ struct alignas(16) Keys {
     uint16_t K[n][kChunk][DK + 8], Q[kQ ? n : 1][kQ ? kChunk : 1][DK + 8];
 };
 
-struct alignas(16) Weights {
-    uint16_t inverse[3][kChunk][kPitch], P[3][kChunk][kPitch];                 // T and P; backward: T^T and P^T
+struct Nothing {};
+struct Inverse { uint16_t inverse[3][kChunk][kPitch]; };                      // T; backward: T^T
+struct Pull { uint16_t P[3][kChunk][kPitch]; };                               // P; backward: P^T
+struct Fades {
     float beta[kChunk], read[kChunk], query[kChunk], until[kChunk];            // beta, e^G (backward: beta e^G), scale e^G, e^(G[last] - G)
     float whole;                                                               // e^G[last]
     float rest[127];                                                           // of a page
 };
+template <bool kP>
+struct alignas(16) WeightsOf : Inverse, std::conditional_t<kP, Pull, Nothing>, Fades {};
+struct Weights : WeightsOf<true> {};
+static_assert(sizeof(Weights) == sizeof(Inverse) + sizeof(Pull) + sizeof(Fades) && sizeof(WeightsOf<false>) == sizeof(Inverse) + sizeof(Fades), "one behind the other");
 static_assert(sizeof(Weights) % kPage == 0, "fetched by pages");
 
 // In the workspace: a chunk's slot has those of its heads.  A sequence's first slot is floor(begin / 32) + its number, which leaves room for all.
@@ -90,7 +96,7 @@ constexpr uint64_t kFewColumns = 512, kFewLargeColumns = 768;
 
 template <class T, int KS, bool kQ = true>
 struct Operands {
-    Weights weight;
+    WeightsOf<kQ> weight;
     Keys<T, KS, kQ> key;
 };
 
@@ -292,7 +298,6 @@ struct alignas(16) Tile {
 };
 
 // What wavefronts hand each other; for those aside two buffers, since they are a chunk behind
-struct Nothing {};
 template <int KS>
 struct Forward {
     f32x4 left[2][2][64];               // what tokens miss
@@ -329,11 +334,11 @@ struct Helped {
 template <class T, int KS, bool kBackward>
 constexpr bool kHasRoom = sizeof(Helped<T, KS, kBackward>) <= 160 * 1024;
 
-template <class T, int KS, bool kBackward, bool kVec>
+template <class T, int KS, bool kBackward, bool kQ, bool kVec>
 struct Helper {
-    static constexpr int kLanes = kHelpers<KS> * 64, kEach = (2 * KS + kHelpers<KS> - 1) / kHelpers<KS>, kWeights = (int)(sizeof(Weights) / 16 + kLanes - 1) / kLanes;
+    static constexpr uint32_t kUnits16 = sizeof(WeightsOf<kQ>) / 16, kBehind = sizeof(Inverse) / 16, kSkipped = (sizeof(Weights) - sizeof(WeightsOf<kQ>)) / 16;      // 16 bytes each; P, where nothing needs it
+    static constexpr int kLanes = kHelpers<KS> * 64, kEach = (2 * KS + kHelpers<KS> - 1) / kHelpers<KS>, kWeights = (int)(kUnits16 + kLanes - 1) / kLanes;
     static_assert(kLanes * 8 >= kChunk * kShared, "a lane has eight values of the tile at most");
-    static_assert(sizeof(Weights) / 16 % kLanes == 0, "all lanes fetch weights");
     const Delta &d;
     const Span &span;
     uint64_t slot0;
@@ -353,7 +358,10 @@ struct Helper {
         rows.fetch(c, to.rows);
         const u32x4 *from = (const u32x4 *)(d.weights + (slot0 + c) * d.H + head);
 #pragma unroll
-        for (int i = 0; i < kWeights; ++i) to.weights[i] = from[i * kLanes + self];
+        for (int i = 0; i < kWeights; ++i) {
+            const uint32_t at = i * kLanes + self;
+            to.weights[i] = from[at < kBehind ? at : at < kUnits16 ? at + kSkipped : 0];
+        }
         const Place at(span, c * kChunk);
         const uint64_t ld = kBackward ? d.lddo : d.ldv;
         const uint8_t *p = (const uint8_t *)((const T *)(kBackward ? d.dout : d.v) + at.row * ld + head * d.Dv);
@@ -370,12 +378,12 @@ struct Helper {
         for (int i = 0; i < (int)sizeof(T) / 2; ++i) *reinterpret_cast<u32x4 *>(&tile.in[token()][column() + i * (16 / (int)sizeof(T))]) = h.w[i];
     }
 
-    template <bool kQ>
     __device__ __forceinline__ void put_operands(uint32_t c, const Chunk &from, Operands<T, KS, kQ> &ops) const
     {
         u32x4 *to = (u32x4 *)&ops.weight;
 #pragma unroll
-        for (int i = 0; i < kWeights; ++i) to[i * kLanes + self] = from.weights[i];
+        for (int i = 0; i < kWeights; ++i)
+            if (kUnits16 % kLanes == 0 || i * kLanes + self < kUnits16) to[i * kLanes + self] = from.weights[i];
         rows.store(c, from.rows, ops.key);
     }
 };
@@ -412,7 +420,7 @@ __device__ __forceinline__ void along_helped(const Delta &d, const Span &span, u
         late(chunks);
         return;
     }
-    using Help = Helper<T, KS, kBackward, kVec>;
+    using Help = Helper<T, KS, kBackward, Helped<T, KS, kBackward, kEnds>::kQ, kVec>;
     const Help h = {d, span, slot0, head, threadIdx.x - kFirst * 64, column0,
                     {(const T *)d.q + hk * d.Dk, (const T *)d.k + hk * d.Dk, d.ldq, d.ldk, d.Dk, wave - kFirst, kHelpers<KS>, threadIdx.x % 64, span}};
     // A chunk is fetched two before it is put; `coming` holds the next one.  Without a branch about a load (behind the last chunk it comes again), so that a wait is for the oldest loads only.
@@ -496,6 +504,8 @@ __device__ __forceinline__ void unit_memory(uint32_t one, uint32_t row0, uint32_
 
 constexpr uint32_t kUnits = 256;        // compute units
 constexpr uint32_t kMostParts = 16, kLeastStretch = 512;
+// Workgroups that a unit runs at once, by the bytes of LDS each has.  Of 160 KB two of 52 KB do, two of 56 KB one after the other (measured; 264 workgroups of 320 lanes take as long as 256, or twice).
+constexpr uint32_t side_by_side(size_t bytes) { return bytes <= 52 * 1024 ? (uint32_t)(104 * 1024 / bytes) : 1; }
 
 // Number of parts for the least time by rounds of workgroups: per_first, per_second of the two launches' run on a compute unit at once (the first, which has less to do, counts 0.8).
 inline void cut(Delta &d, uint32_t per_first, uint32_t per_second)

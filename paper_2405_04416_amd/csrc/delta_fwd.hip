@@ -2,7 +2,7 @@
 //
 // Bound by how long a chunk takes after the one before, not by memory or the matrix instructions: cutting S, what tokens miss and what they write into pieces takes 5.5 operations a value, and a
 // wavefront issues one in some 6 cycles.  A wavefront with all 128 rows of its columns: 4400 cycles a chunk; two that share them, with o made by others: 2500 (1.05 us).  65536 tokens x 8 heads of
-// 128 x 128, bf16: 2.27 ms whole, in four parts 0.74 (ends) + 0.04 (joined) + 0.61; 2 x 8192 tokens x 16 heads 0.39.
+// 128 x 128, bf16: 2.27 ms whole, in four parts 0.71 (ends) + 0.02 (joined) + 0.62; 2 x 8192 tokens x 16 heads 0.39.
 #include "delta_chunk.h"
 
 namespace {
@@ -280,7 +280,7 @@ void launch_size(Delta d, hipStream_t st)
     const Columns c = columns_of(d, kRoom);
     if constexpr (kRoom)
         if (c.helped) {
-            cut(d, 160 * 1024 / sizeof(Helped<T, KS, false, true>), 160 * 1024 / sizeof(Helped<T, KS, false>));
+            cut(d, side_by_side(sizeof(Helped<T, KS, false, true>)), side_by_side(sizeof(Helped<T, KS, false>)));
             const uint32_t groups = d.ends_width() / kShared, first = d.n_seq * d.H * (d.parts - 1) * groups, all = d.n_seq * d.H * d.parts * c.groups, threads = kSharedWaves<KS> * 64;
             if (d.parts > 1) {
                 if (d.vec_all) delta_fwd_shared_kernel<T, KS, true, true><<<first, threads, 0, st>>>(d, groups, 0);

