@@ -40,10 +40,10 @@ void use_workspace(Delta &d, void *ws)
     }
 }
 
-void use_vectors(Delta &d, const void *o, uint64_t ldo, uint32_t dtype)
+void use_vectors(Delta &d, uint32_t dtype)
 {
     d.vec_keys = wide_rows(d.q, d.ldq, d.Dk, dtype) && wide_rows(d.k, d.ldk, d.Dk, dtype);
-    d.vec_all = d.vec_keys && wide_rows(d.v, d.ldv, d.Dv, dtype) && wide_rows(o, ldo, d.Dv, dtype);
+    d.vec_all = d.vec_keys && wide_rows(d.v, d.ldv, d.Dv, dtype) && (!d.dout || wide_rows(d.dout, d.lddo, d.Dv, dtype));
 }
 
 int check_sizes(const char *who, uint64_t N, uint32_t n_seq, const uint32_t *first, uint32_t Hk, uint32_t H, uint32_t Dk, uint32_t Dv, uint32_t dtype)
@@ -105,7 +105,7 @@ extern "C" int dg_delta_rule_fwd(const void *q, uint64_t ldq, const void *k, uin
     d.q = q, d.k = k, d.v = v, d.g = g, d.beta = beta, d.ldq = ldq, d.ldk = ldk, d.ldv = ldv, d.ldg = ldg, d.ldb = ldbeta, d.s0 = s0, d.o = o, d.ldo = ldo, d.s_last = s_last;
     d.first = first, d.N = N, d.n_seq = n_seq, d.Hk = Hk, d.H = H, d.Dk = Dk, d.Dv = Dv, d.reverse = reverse, d.scale = scale;
     if (saved) d.marks = (float *)saved, d.y = (float *)((char *)saved + padded(marks_bytes(N, n_seq, H, Dk, Dv)));
-    use_vectors(d, o, ldo, dtype);
+    use_vectors(d, dtype);
     if (takes_small(N, n_seq, H, Dk, Dv)) launch_small(d, dtype, false, (hipStream_t)stream);
     else if (!saved && N <= kFewTokens * n_seq) launch_tokens(d, dtype, (hipStream_t)stream);
     else {
@@ -148,7 +148,7 @@ extern "C" int dg_delta_rule_bwd(const void *q, uint64_t ldq, const void *k, uin
     use_workspace(d, ws);
     char *const rest = (char *)ws + forward_bytes(N, n_seq, H);
     d.dmarks = (float *)rest, d.dr = (float *)(rest + marks), d.slot_seq = (const uint32_t *)(rest + marks + rows_bytes(N, H, Dv));
-    use_vectors(d, do_, lddo, dtype);
+    use_vectors(d, dtype);
     d.vec_out = wide_rows(dv, lddv, Dv, dtype) && wide_rows(dq, lddq, Dk, dtype) && wide_rows(dk, lddk, Dk, dtype);
     if (N) launch_slots(d, (hipStream_t)stream);
     if (takes_small(N, n_seq, H, Dk, Dv)) launch_small(d, dtype, true, (hipStream_t)stream);

@@ -55,7 +55,7 @@ struct Delta {
     float *ends, *starts;
     __host__ __device__ uint32_t ends_width() const { return (Dv + 15) / 16 * 16 + (Dk + 15) / 16 * 16; }
     float scale;
-    // Whether heads' rows lie in whole 16 bytes: q and k; q, k, v and o or its gradient, and with them rows of fp32 values; dv, dq and dk too.  Kernels take it as a template
+    // Whether heads' rows lie in whole 16 bytes: q and k; q, k, v and, backward, the gradient of o, and with them rows of fp32 values; dv, dq and dk too.  Kernels take it as a template
     // argument: of a branch between loads of 16 bytes and single ones the compiler makes single ones for both.
     bool vec_keys, vec_all, vec_out;
 };
