@@ -640,4 +640,18 @@ __device__ __forceinline__ void lefts_turned(const uint16_t (&m)[n][kChunk][pitc
     wave_fence();
 }
 
+// A lane's column of 16 as an operand: column col + lane % 16, eight rows from row + 8 (lane / 16) on.  16 lanes read 16 columns of four rows, 4 values each, and get a column each.
+template <int n, int rows, int pitch>
+__device__ __forceinline__ void columns(const uint16_t (&m)[n][rows][pitch], uint32_t row, uint32_t col, uint32_t lane, bf16x8 (&out)[n])
+{
+    wave_fence();                       // what others have stored is read, of which the compiler sees nothing
+#pragma unroll
+    for (int p = 0; p < n; ++p) {
+        const uint16_t *at = &m[p][row + lane / 16 * 8 + lane % 16 / 4][col + lane % 4 * 4];
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4_in_lds *)at), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4_in_lds *)(at + 4 * pitch));
+        out[p] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+    wave_fence();
+}
+
 }  // namespace dg_delta

@@ -6,9 +6,9 @@
 //
 // A workgroup takes 64 tokens of a key head, one value head after the other, 32 columns of values at a time through LDS (in pieces, cut once for all), a wavefront
 // 16 tokens and half of the columns of keys: a lane has a token, of which everything above is a column of a product.  X and Z are made once, block by block,
-// and go through LDS by rows and by columns.
-// Bound by cutting into pieces and by LDS: 2 x 8192 tokens x 16 heads of 128 x 128, bf16, 0.40 ms, five times what its matrix instructions alone would take; 2003 ragged sequences x 3 heads of
-// 24 x 40, fp32, 0.36 ms.
+// and go through LDS, from which reads that transpose take them, K and Q by columns too.
+// Bound by cutting into pieces and by LDS: 2 x 8192 tokens x 16 heads of 128 x 128, bf16, 0.38 ms, five times what its matrix instructions alone would take; 2003 ragged sequences x 3 heads of
+// 24 x 40, fp32, 0.34 ms.
 #include "delta_chunk.h"
 #include "rows_vectors.h"
 
@@ -24,12 +24,12 @@ struct Values {
     uint16_t S[3][32 * KS][kColumnPitch], dS[3][32 * KS][kColumnPitch], U[3][kTokens][kColumnPitch], R[3][kTokens][kColumnPitch], O[Pieces<T>::n][kTokens][kColumnPitch];
 };
 
-// X and Z by rows (row i, columns j) and Z, later X, by columns (row j, columns i)
-struct Pulls { uint16_t X[3][kTokens][kTokenPitch], Z[3][kTokens][kTokenPitch], ZT[3][kTokens][kTokenPitch]; };
+// X and Z: row i, columns j
+struct Pulls { uint16_t X[3][kTokens][kTokenPitch], Z[3][kTokens][kTokenPitch]; };
 
-// columns of K, or of Q, as rows
+// K or Q
 template <class T, int KS>
-struct Turned { uint16_t rows[Pieces<T>::n][32 * KS][kTokenPitch]; };
+struct Turned { uint16_t rows[Pieces<T>::n][kTokens][32 * KS + 8]; };
 
 struct Tokens {
     double G[kTokens];
@@ -114,23 +114,12 @@ __device__ __forceinline__ void turn(const T *K, uint32_t ld, uint32_t Dk, uint3
         cleared<T, 8>(x[i], col, Dk, t < count, v);
         split<n, 8>(v, w);
 #pragma unroll
-        for (int p = 0; p < n; ++p)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) to.rows[p][col + j][t] = (uint16_t)(w[p][j / 2] >> (j % 2 * 16));
+        for (int p = 0; p < n; ++p) *reinterpret_cast<u32x4 *>(&to.rows[p][t][col]) = (u32x4){w[p][0], w[p][1], w[p][2], w[p][3]};
     }
 }
 
-// four values of a row side by side, or of a column one below the other
+// four values of a row side by side
 __device__ __forceinline__ void put_across(const float (&v)[4], uint16_t (&to)[3][kTokens][kTokenPitch], uint32_t row, uint32_t col) { put4(v, to, row, col); }
-__device__ __forceinline__ void put_down(const float (&v)[4], uint16_t (&to)[3][kTokens][kTokenPitch], uint32_t row, uint32_t col)
-{
-    uint32_t w[3][2];
-    split<3, 4>(v, w);
-#pragma unroll
-    for (int p = 0; p < 3; ++p)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) to[p][row + i][col] = (uint16_t)(w[p][i / 2] >> (i % 2 * 16));
-}
 
 template <class T, int KS, bool kVec>
 __global__ void __launch_bounds__(kThreads)
@@ -317,13 +306,11 @@ delta_grad_kernel(Delta d, uint64_t from)
             }
             put_across(x[k], lds.pull.X, i, j0);
             put_across(z, lds.pull.Z, i, j0);
-            put_down(z, lds.pull.ZT, j0, i);
         }
         // the blocks behind the diagonal that are multiplied with
         if (half == 1 && wave < 2) {
             put_across(none, lds.pull.X, wave * 32 + c16, wave * 32 + 16 + r4);
             put_across(none, lds.pull.Z, wave * 32 + c16, wave * 32 + 16 + r4);
-            put_across(none, lds.pull.ZT, wave * 32 + 16 + c16, wave * 32 + r4);
         }
         // what the memory before gives and the one behind takes, and what the tokens of the block tell each other
         float at_end = 0.0f, dG = 0.0f;
@@ -341,11 +328,11 @@ delta_grad_kernel(Delta d, uint64_t from)
             const bool before = 2 * s <= (int)wave, after = 2 * s + 1 >= (int)wave;
             lefts(lds.pull.X, mine, s * 32 + r8, x1);
             lefts(lds.pull.Z, mine, s * 32 + r8, z1);
-            lefts(lds.pull.ZT, mine, s * 32 + r8, z2);
-            lefts(lds.turned[0].rows, key0 + c16, s * 32 + r8, a[0]);
+            columns(lds.pull.Z, s * 32, wave * 16, lane, z2);
+            columns(lds.turned[0].rows, s * 32, key0, lane, a[0]);
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
-                if (t + 1 < kTiles) lefts(lds.turned[0].rows, key0 + (t + 1) * 16 + c16, s * 32 + r8, a[(t + 1) % 2]);
+                if (t + 1 < kTiles) columns(lds.turned[0].rows, s * 32, key0 + (t + 1) * 16, lane, a[(t + 1) % 2]);
                 __builtin_amdgcn_sched_barrier(0);
                 if (before) {
                     here[t] = multiply<n, 3>(a[t % 2], x1, here[t]);
@@ -354,37 +341,38 @@ delta_grad_kernel(Delta d, uint64_t from)
                 if (after) dk[t] = multiply<n, 3>(a[t % 2], z2, dk[t]);
             }
         }
-        auto dot_tokens = [&](const uint16_t (&rows)[n][32 * KS][kTokenPitch], const f32x4 (&with)[kTiles]) {
+        auto dot_tokens = [&](const uint16_t (&rows)[n][kTokens][32 * KS + 8], const f32x4 (&with)[kTiles]) {
             float sum = 0.0f;
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t)
+            for (int t = 0; t < kTiles; ++t) {
+                float value[4] = {};                // from its pieces, 0 where there is no token or column
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    float value = 0.0f;             // from its pieces, 0 where there is no token or column
+                for (int p = 0; p < n; ++p) {
+                    const u32x2 w = *reinterpret_cast<const u32x2 *>(&rows[p][mine][key0 + t * 16 + r4]);
 #pragma unroll
-                    for (int p = 0; p < n; ++p) value += __uint_as_float((uint32_t)rows[p][key0 + t * 16 + r4 + y][mine] << 16);
-                    sum = fmaf(value, with[t][y], sum);
+                    for (int y = 0; y < 4; ++y) value[y] += __uint_as_float(y % 2 ? w[y / 2] & 0xffff0000u : w[y / 2] << 16);
                 }
+#pragma unroll
+                for (int y = 0; y < 4; ++y) sum = fmaf(value[y], with[t][y], sum);
+            }
             return sum;
         };
         at_end = dot_tokens(lds.turned[0].rows, to_k);
-        __syncthreads();
-        if constexpr (!kBoth) turn<T, KS, kVec>(Q, (uint32_t)d.ldq, d.Dk, count, behind, lds.turned[0]);
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-            if (k < (int)blocks) put_down(x[k], lds.pull.X, bj[k] * 16 + r4, bi[k] * 16 + c16);
-        if (half == 1 && wave < 2) put_across(none, lds.pull.X, wave * 32 + 16 + c16, wave * 32 + r4);
-        __syncthreads();
+        if constexpr (!kBoth) {
+            __syncthreads();
+            turn<T, KS, kVec>(Q, (uint32_t)d.ldq, d.Dk, count, behind, lds.turned[0]);
+            __syncthreads();
+        }
         auto &queries = lds.turned[kBoth ? 1 : 0].rows;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             bf16x8 x2[3], a[2][n];
             const bool after = 2 * s + 1 >= (int)wave;
-            lefts(lds.pull.X, mine, s * 32 + r8, x2);
-            lefts(queries, key0 + c16, s * 32 + r8, a[0]);
+            columns(lds.pull.X, s * 32, wave * 16, lane, x2);
+            columns(queries, s * 32, key0, lane, a[0]);
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
-                if (t + 1 < kTiles) lefts(queries, key0 + (t + 1) * 16 + c16, s * 32 + r8, a[(t + 1) % 2]);
+                if (t + 1 < kTiles) columns(queries, s * 32, key0 + (t + 1) * 16, lane, a[(t + 1) % 2]);
                 __builtin_amdgcn_sched_barrier(0);
                 if (after) dk[t] = multiply<n, 3>(a[t % 2], x2, dk[t]);
             }
