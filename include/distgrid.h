@@ -609,7 +609,7 @@ int dg_rms_norm_bwd(const void *total, uint64_t ldt, const float *gamma, const v
 
 /* Rows in 8 bits: value c of row i stands for q[i, c] 2^(scales[i, c / 128] - 127), q in e4m3 (bias 7, largest 448, no
  * infinity).  A block of 128 columns has the smallest scale >= 2^-127 for which none of its finite values is beyond 448 times it; infinities and NaN
- * become NaN.  Values are rounded once, from fp32, to the nearest even one.  q: 16-byte aligned, ldq (in values) a multiple of 16;
+ * become NaN.  Values are rounded once, to the nearest even one (the norm's from some 2^-40, not from fp32).  q: 16-byte aligned, ldq (in values) a multiple of 16;
  * scales [N, ceil(W / 128)] bytes, rows lds apart; what lies between rows stays as it is.  q, scales and total must not overlap, nor q and scales inputs.
  * dg_rms_norm_e4m3_fwd: what dg_rms_norm_fwd gives, in 8 bits.  dg_e4m3_rows: the rows themselves (weights). */
 int dg_rms_norm_e4m3_fwd(const void *x, uint64_t ldx, const void *residual, uint64_t ldr, const float *gamma,

@@ -2,7 +2,7 @@
 //   t = x + r, rounded to the rows' type (what the next block adds to);  y = t s gamma,  s = 1 / sqrt(mean(t^2) + eps).
 //
 // Bound by memory: a row is read once into registers and summed there, as in layer norm, and everything that depends on it is stored from there.
-// 8192 rows of 4096 bf16 values with the residual: 47 us, 5.7 TB/s of what goes in and out; 16384 of 2048 into 8 bits 48 us, 4.9 TB/s.  1024 rows of 32: 2.9 us, a launch.
+// 8192 rows of 4096 bf16 values with the residual: 47 us, 5.7 TB/s of what goes in and out; 16384 of 2048 into 8 bits 49 us, 4.8 TB/s.  1024 rows of 32: 2.9 us, a launch.
 #pragma once
 #include "rows_vectors.h"
 
@@ -77,7 +77,9 @@ __device__ __forceinline__ float group_max(float v)
 }
 
 // What is rounded to 8 bits is known to some 2^-40 before: fp32 arithmetic would leave one value in half a million on the other side of a step of e4m3, a sixteenth of it away.  Sums of squares
-// are taken in 64 bits, the scale and its products in two parts of 32.  All of it hides behind the loads.
+// are taken in 64 bits, the scale and its products in two parts of 32.  The nearest fp32 number to the sum of the two serves as long as it is no border itself: halfway between two of e4m3, or 448 times
+// a power of two, where the scale changes.  Borders end in 19 zeros.  There (and at 0) it is rounded to odd, which leaves it on the border's side that the sum is on.  (All of this of values from
+// 2^-100 on, below which fp32 has no room for the second part.)  16384 rows of 2048: 49.1 us; with every value rounded to odd 51.1, with none 48.4, but then one in two million falls on the wrong side.
 template <int C>
 __device__ __forceinline__ double exchanged2(double v)
 {
@@ -113,6 +115,15 @@ __device__ __forceinline__ double row_sum2(double v, double *red)
     return v;
 }
 
+// a + b, |b| <= |a|, towards 0 and then to the odd one if that is not all of it
+__device__ __forceinline__ float odd_sum(float a, float b)
+{
+#pragma clang fp contract(off)
+    const float sum = a + b, left = b - (sum - a);
+    const uint32_t bits = __float_as_uint(sum), beyond = (bits ^ __float_as_uint(left)) >> 31;
+    return left != 0.0f ? __uint_as_float((bits - beyond) | 1u) : sum;
+}
+
 struct Scale {
     float s, rest;
     // 1 / sqrt(squares / W + eps): fp32, then a step of Newton's
@@ -124,11 +135,30 @@ struct Scale {
         s = off == off ? (float)exact : s0;         // of infinities and NaN as in fp32
         rest = off == off ? (float)(exact - s) : 0.0f;
     }
+    template <bool kOdd>
     __device__ __forceinline__ float times(float x, float gamma) const
     {
 #pragma clang fp contract(off)
-        const float p = x * s, p_off = fmaf(x, rest, fmaf(x, s, -p)), y = p * gamma;
-        return y + fmaf(p_off, gamma, fmaf(p, gamma, -y));
+        const float p = x * s, p_off = fmaf(x, rest, fmaf(x, s, -p)), y = p * gamma, y_off = fmaf(p_off, gamma, fmaf(p, gamma, -y));
+        return kOdd ? odd_sum(y, y_off) : y + y_off;
+    }
+    // x <- what is to be rounded to 8 bits
+    template <int V>
+    __device__ __forceinline__ void apply(float (&x)[V], const float (&gamma)[V]) const
+    {
+        float y[V];
+        uint32_t least = ~0u;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            y[v] = times<false>(x[v], gamma[v]);
+            const uint32_t end = __float_as_uint(y[v]) & 0x7ffff;
+            least = end < least ? end : least;
+        }
+        if (least == 0)
+#pragma unroll
+            for (int v = 0; v < V; ++v) y[v] = times<true>(x[v], gamma[v]);
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] = y[v];
     }
 };
 
@@ -218,9 +248,7 @@ rms_fwd_kernel(Rms a)
             }
             const Scale s(row_sum2<G, kThreads>(sum, red2), a.W, a.eps);
 #pragma unroll
-            for (int k = 0; k < K; ++k)
-#pragma unroll
-                for (int v = 0; v < V; ++v) x[k][v] = s.times(x[k][v], gamma[k][v]);
+            for (int k = 0; k < K; ++k) s.apply(x[k], gamma[k]);
         } else if (kMade != kPlain8) {
             float sum[1] = {0.0f};
 #pragma unroll
@@ -308,7 +336,7 @@ rms_fwd_wide_kernel(Rms a)
                 const T sum = r ? (T)((float)x[c] + (float)r[c]) : x[c];
                 y[i] = (float)sum;
                 if (kMade == kNormed) y[i] = y[i] * s * (a.gamma ? a.gamma[c] : 1.0f);
-                if (kMade == kNormed8) y[i] = exact.times(y[i], a.gamma ? a.gamma[c] : 1.0f);
+                if (kMade == kNormed8) y[i] = exact.times<true>(y[i], a.gamma ? a.gamma[c] : 1.0f);
                 if (t) t[c] = sum;
                 if (kMade == kNormed) ((T *)a.out + row * a.ldo)[c] = (T)y[i];
                 largest = fmaxf(largest, finite_size(y[i]));

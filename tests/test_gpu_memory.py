@@ -267,6 +267,43 @@ def test_norm_in_8_bits(N, W, pad, shift, dtype):
         kept_between(qb, sb, W)
 
 
+def next_to_borders(rng, t, W, eps):
+    """Weights with which the norm of a row t has values next to what lies halfway between two of e4m3, and blocks whose largest is next to 448 times a power of two: at a distance
+    between 2^-36 and 2^-23, so that the nearest fp32 number is the border itself for many."""
+    t = t.astype(np.longdouble)
+    th = t / np.sqrt((t * t).mean() + eps)
+    order = rng.integers(-9, 9, W)                                      # of the values; the steps are 2^(order - 3), 2^-9 at least
+    step = np.exp2(np.maximum(order, -6) - 3.0)
+    border = (np.maximum(np.floor(np.exp2(order + rng.random(W)) / step), 0) + 0.5) * step
+    border = np.where(border < 448.0, border, 432.0)
+    border[::128] = np.where(np.arange(-(-W // 128)) % 3 < 2, 448.0, 416.0)
+    border *= np.exp2(np.repeat(rng.integers(-20, 20, -(-W // 128)), 128)[:W].astype(np.float64))
+    gamma = (border / th).astype(np.float32)
+    up = np.nextafter(gamma, np.where(rng.random(W) < 0.5, np.float32(np.inf), np.float32(-np.inf)).astype(np.float32))
+    return np.where(np.abs(gamma * th / border - 1) < 2.0 ** -36, up, gamma), border
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("W", [5, 32, 100, 128, 513, 1000, 1024, 4096, 8192, 9001])
+def test_norm_in_8_bits_rounds_once(W, dtype):
+    """Values that are known to 2^-40 and lie 2^-36 or more from a border of e4m3 are the 64 bits' own, scales too."""
+    say("norm in 8 bits, borders", W, dtype)
+    eps = float(np.float32(1e-5))
+    on_border = 0
+    for seed in range(8):
+        rng = np.random.default_rng(1000 * W + seed)
+        x, x64 = rounded(rng.choice([-1.0, 1.0], (1, W)) * (0.5 + rng.random((1, W))), TYPES[dtype])
+        gamma, border = next_to_borders(rng, x64[0], W, eps)
+        want = oracle.rms_norm_fwd(x64, gamma, eps)
+        on_border += int((np.abs(want[0]).astype(np.float32) == np.abs(border)).sum())
+        _, _, q, s = put8(1, W)
+        B.dg_rms_norm_e4m3_fwd(put(x)[0], None, f32(gamma), 1e-5, None, q, s)
+        wq, ws = oracle.e4m3_rows(want)
+        np.testing.assert_array_equal(s.view(torch.uint8).cpu().numpy(), ws)
+        np.testing.assert_array_equal(q.float().double().cpu().numpy(), wq)
+    assert on_border >= W
+
+
 # ------------------------------------------------------------------ product of rows in 8 bits
 def product_bound(a, b):
     """Errors of a b^T before its rounding.  Of eight neighbouring products the matrix instruction cuts off what is below 2^-13 of the largest (2 to the sum of its factors' exponents),
