@@ -80,7 +80,7 @@ class DeltaMixer:
         return t
 
     def _part_with(self, *inputs):
-        """A result of this block that goes in again is needed until its gradient has been taken: other buffers take its place."""
+        """A result of this block that goes in again is needed until its gradient has been taken, and is a result again where there is no residual: other buffers take its place."""
         for name in ("t", "out", "dx"):
             t = self.buffers.get(name)
             if t is not None and any(x is not None and x.untyped_storage().data_ptr() == t.untyped_storage().data_ptr() for x in inputs):
@@ -97,6 +97,8 @@ class DeltaMixer:
 
     def _mix(self, x, r, g, beta, n_seq, first, s0, s_last, saved):
         self.saved = None               # what a backward pass would need is overwritten
+        if r is None:
+            self._part_with(x)          # x is the first result
         N = x.shape[0]
         t, n8 = (x if r is None else self._buffer("t", x.shape)), self._room8("n8", N, self.width)
         B.dg_rms_norm_e4m3_fwd(x, r, self.gamma, EPS, None if r is None else t, *n8)
@@ -114,7 +116,7 @@ class DeltaMixer:
     def forward(self, x, r, g, beta, n_seq, first=None, s0=None, s_last=None, training=True):
         """x, r [N, width] (r may be None) -> (t, out) for the next block.  g, beta [N, heads] fp32; n_seq segments of N / n_seq samples each, or of the rows that `first`
         gives them (of rows of none `out` is 0).  s0, s_last [n_seq, heads, d_key, d_value] fp32 or None: memories in and out (s_last may be s0 outside training).
-        The results are buffers that the next pass overwrites, unless that is a training pass on them (t is x without r).  backward reads x, g, beta, first and s0 again: they
+        The results are buffers that the next pass overwrites, unless that is a training pass on them, or one without r (where t is x).  backward reads x, g, beta, first and s0 again: they
         have to stay as they are until then."""
         N = x.shape[0]
         saved = None

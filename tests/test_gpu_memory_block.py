@@ -139,6 +139,30 @@ def test_blocks_in_a_stack_and_a_graph():
         for a, b in zip(results, want): assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("way", ["forward", "training", "advance"])
+def test_own_results_go_in_again_without_a_residual(way):
+    """t is x: the pass must not write its other result there."""
+    say("memory block again", way)
+    rng = np.random.default_rng(7)
+    n_seq, S = (5, 1) if way == "advance" else (3, 20)
+    block, other = (DeltaMixer(dtype=torch.float16, seed=2, **SHAPES[0]) for _ in range(2))
+    rows, _, g, beta, s0, _ = make(rng, n_seq * S, n_seq, block, "fp16")
+    g, beta, memories = f32(g), f32(beta), [f32(s0), f32(s0)]
+
+    def go(b, x, memory):
+        if way == "advance": return b.advance(x, None, g, beta, memory)
+        return b.forward(x, None, g, beta, n_seq, training=way == "training")
+
+    x, y = rows["x"], rows["x"].clone()
+    for i in range(4):
+        was = x.clone()
+        t, x = go(block, x, memories[0])
+        assert torch.equal(t, was) and x.data_ptr() != t.data_ptr()
+        ty, out = go(other, y, memories[1])                 # the same with a copy
+        assert torch.equal(t, ty) and torch.equal(x, out)
+        y = out.clone()
+
+
 def test_refusals():
     with pytest.raises(DistGridError):
         DeltaMixer(32, 2, weights=[torch.zeros(4, 4)] * 3, device=DEV)
