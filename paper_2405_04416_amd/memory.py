@@ -18,7 +18,7 @@ which another one ended, as partitions do along a ray.  Every arithmetic step ha
 import torch
 
 from . import binding as B
-from .mixer import _overlap
+from .mixer import _overlap, keep_captured
 
 EPS = 1e-5
 KEY_EPS = 1e-6
@@ -61,7 +61,7 @@ class DeltaMixer:
         self.scale = d_key ** -0.5
         self.opt = None
         self.saved = None
-        self.buffers = {}
+        self.buffers, self.captured = {}, []
 
     def _buffer(self, name, shape, dtype=None):
         """A buffer that this block keeps from pass to pass, replaced when a pass needs another size."""
@@ -111,6 +111,7 @@ class DeltaMixer:
         B.dg_delta_rule_fwd(qv[:, :self.wq], k, qv[:, self.wq:], g, beta, self.Hk, n_seq, first, self.reverse, self.scale, s0, o, s_last, saved,
                             self._workspace("ws_delta", B.dg_delta_rule_fwd_workspace_bytes(N, n_seq, self.H)))
         self._product(self._rows8("o8", o), self.forth[2], out)
+        keep_captured(self.captured, self.buffers)
         return t, out
 
     def forward(self, x, r, g, beta, n_seq, first=None, s0=None, s_last=None, training=True):
@@ -151,6 +152,7 @@ class DeltaMixer:
         self._product(self._rows8("dk8", draw.view(N, self.wq)), self.back[1], dn)
         B.dg_dropout_fwd(part, dn, 0.0, 0, 0, dn)           # without dropping: the sum
         B.dg_rms_norm_bwd(t, self.gamma, dn, dt, EPS, dx, self.dgamma, self._workspace("ws_norm", B.dg_rms_norm_bwd_workspace_bytes(N, self.width)))
+        keep_captured(self.captured, self.buffers)
         return dx, dg, dbeta
 
     def advance(self, x, r, g, beta, memory):

@@ -30,6 +30,12 @@ def _overlap(a, b):
     return begin(a) < end(b) and begin(b) < end(a)
 
 
+def keep_captured(kept, buffers):
+    """A graph replays with the addresses that it was captured with: buffers of a pass that is being captured stay, whatever sizes later passes need."""
+    if torch.cuda.is_current_stream_capturing():
+        kept.append(list(buffers.values()))
+
+
 class RayMixer:
     def __init__(self, width, dtype=torch.float16, p=0.1, reverse=False, seed=0, device="cuda:0"):
         """width: features per sample; p: share that dropout takes during training; reverse: back to front; seed: of dropout, not
@@ -43,7 +49,7 @@ class RayMixer:
         self.opt = None
         self.drawn = 0              # words of the generator that earlier passes have used
         self.saved = None
-        self.buffers = {}
+        self.buffers, self.captured = {}, []
 
     def _buffer(self, name, shape, dtype):
         """A buffer that this block keeps from pass to pass, replaced when a pass needs another size."""
@@ -90,6 +96,7 @@ class RayMixer:
         if training:
             self.saved = (x, n_seq, first, h0, states, p, self.drawn)
             self.drawn += -(-x.numel() // 4)
+        keep_captured(self.captured, self.buffers)
         return y
 
     def backward(self, dy, dh_last=None, dh0=None):
@@ -109,12 +116,14 @@ class RayMixer:
         B.dg_dropout_fwd(part, dy, 0.0, 0, 0, dx)
         B.dg_layer_norm_bwd(x, self.gamma_u, du, EPS, part, g[2], g[3], ws)
         B.dg_dropout_fwd(part, dx, 0.0, 0, 0, dx)
+        keep_captured(self.captured, self.buffers)
         return dx
 
     def advance(self, x, h):
         """One more sample for every segment, x [n_seq, width]; the states h [n_seq, width] fp32 are updated in place."""
         m, y = self._recur(x, x.shape[0], None, h, h, None), self._rows("y", x)
         B.dg_dropout_fwd(m, x, 0.0, 0, 0, y)
+        keep_captured(self.captured, self.buffers)
         return y
 
     def optimiser_step(self, iteration, lr):

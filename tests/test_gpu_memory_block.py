@@ -163,6 +163,39 @@ def test_own_results_go_in_again_without_a_residual(way):
         y = out.clone()
 
 
+def test_a_graph_outlives_passes_of_other_sizes():
+    """What a captured pass works in is not given back when passes of other sizes need other buffers."""
+    say("memory block, sizes between replays")
+    rng = np.random.default_rng(11)
+    N, n_seq = 1536, 4
+    block, twin = (DeltaMixer(dtype=torch.bfloat16, seed=3, **SHAPES[0]) for _ in range(2))
+    rows, _, g, beta, s0, _ = make(rng, N, n_seq, block, "bf16")
+    g, beta, s0 = f32(g), f32(beta), f32(s0)
+
+    def step(b):
+        t, out = b.forward(rows["x"], rows["r"], g, beta, n_seq, None, s0)
+        return [t, out, *b.backward(rows["dt"], rows["dout"]), b.dgamma]
+
+    step(block)                                     # its buffers are there before the graph is
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        results = step(block)
+    for n in (800, 12, 2400):
+        x = rows["x"][:1].expand(n, -1).contiguous()
+        block.forward(x, x, g[:1].expand(n, -1).contiguous(), beta[:1].expand(n, -1).contiguous(), n_seq)
+        block.backward(x, x)
+        block.advance(rows["x"][:n_seq], rows["r"][:n_seq], g[:n_seq].contiguous(), beta[:n_seq].contiguous(), s0.clone())
+    others = [torch.full((size,), 7, dtype=torch.uint8, device=DEV) for size in [1 << 10, 1 << 14, 1 << 17, 1 << 19, 1 << 21, 1 << 23] for _ in range(40)]
+    for _ in range(3):
+        for z in (rows["x"], rows["dout"]): z.copy_(torch.randn(z.shape, device=DEV))
+        for z in results: z.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(results, step(twin)): assert torch.equal(a, b)
+        for z in others: assert bool((z == 7).all())
+
+
 def test_refusals():
     with pytest.raises(DistGridError):
         DeltaMixer(32, 2, weights=[torch.zeros(4, 4)] * 3, device=DEV)

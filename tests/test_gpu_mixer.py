@@ -139,6 +139,34 @@ def test_block_gradient_is_of_the_pass_that_was():
     assert all(torch.equal(a, b) for a, b in zip(*out))
 
 
+def test_a_graph_outlives_passes_of_other_sizes():
+    """What a captured pass works in is not given back when passes of other sizes need other buffers."""
+    say("block, sizes between replays")
+    torch.manual_seed(5)
+    n_seq, S, W = 6, 200, 48
+    x, dy = torch.randn(n_seq * S, W, device=DEV), torch.randn(n_seq * S, W, device=DEV)
+    block, twin = (RayMixer(W, torch.float32, p=0.0, device=DEV) for _ in range(2))
+    step = lambda b: [b.forward(x, n_seq), b.backward(dy), b.grads]
+    step(block)                                     # its buffers are there before the graph is
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        results = step(block)
+    for n in (600, 12, 2400):
+        z = torch.randn(n, W, device=DEV)
+        block.forward(z, n_seq)
+        block.backward(z)
+        block.advance(z[:n_seq], torch.zeros(n_seq, W, device=DEV))
+    others = [torch.full((size,), 7, dtype=torch.uint8, device=DEV) for size in [1 << 10, 1 << 14, 1 << 17, 1 << 18, 1 << 19, 1 << 21] for _ in range(40)]
+    for _ in range(3):
+        for z in (x, dy): z.copy_(torch.randn(z.shape, device=DEV))
+        for z in results: z.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(results, step(twin)): assert torch.equal(a, b)
+        for z in others: assert bool((z == 7).all())
+
+
 def test_block_refuses_states_in_place_in_training():
     """The gradient needs the state that went in."""
     say("block h0")
