@@ -637,14 +637,17 @@ int dg_e4m3_product(const void *a, uint64_t lda, const uint8_t *a_scales, uint64
  * one) and may be s0, unless a backward pass is to follow.  Keys of length one (dg_rms_norm_fwd over rows of Dk with gamma = Dk^-1/2) and rates up to 1 keep memories bounded.
  * first, reverse: as for dg_recurrence_fwd.  One token per sequence (N == n_seq), or a few, is the step of a program that gets its tokens one after the other.
  * saved: NULL, or dg_delta_rule_saved_bytes(N, n_seq, H, Dk, Dv) bytes for the backward pass, 16-byte aligned (what tokens write, and the memories before every
- * 64th).  ws: dg_delta_rule_fwd_workspace_bytes(N, n_seq, H) bytes, 16-byte aligned; not needed without `saved` for up to four tokens a sequence (N <= 4 n_seq).
- * dg_delta_rule_workspace_bytes(N, n_seq, Hk, H, Dk, Dv) are enough for either pass; no call needs what another left there.  Long sequences of one length and few heads are worked on in parts.
+ * 64th).  ws: dg_delta_rule_fwd_workspace_bytes(N, n_seq, H) bytes, 16-byte aligned, are enough for heads of any size; a call needs no more than
+ * dg_delta_rule_fwd_least_workspace_bytes(N, n_seq, H, Dk, Dv, saves) (saves: whether `saved` is given), which is 0 (ws may be NULL) for many small heads, and without `saved` for up to four tokens a
+ * sequence (N <= 4 n_seq).  dg_delta_rule_workspace_bytes(N, n_seq, Hk, H, Dk, Dv) are enough for either pass; no call needs what another left there.  Long sequences of one length and few heads are worked on in parts.
  * Everything is as exact as in fp32, and the same call gives the same bits.  Tokens are taken 32 or 64 at a time: an infinity or NaN in a token's row may show in
  * the results of up to 63 tokens before it.  o must not overlap an input.
  * Errors: DG_ERR_ARG for heads or sizes of 0, H that Hk does not divide, N that n_seq does not divide (first NULL), a scale that is not finite;
  * DG_ERR_UNSUPPORTED for Dk or Dv above 128, rows 2^24 values or more apart, N >= 2^32, n_seq >= 2^31, H > 2^16, N H > 2^36, n_seq H > 2^32. */
 size_t dg_delta_rule_saved_bytes(uint64_t N, uint32_t n_seq, uint32_t H, uint32_t Dk, uint32_t Dv);
 size_t dg_delta_rule_fwd_workspace_bytes(uint64_t N, uint32_t n_seq, uint32_t H);
+size_t dg_delta_rule_fwd_least_workspace_bytes(uint64_t N, uint32_t n_seq, uint32_t H, uint32_t Dk, uint32_t Dv,
+                                               uint32_t saves);
 size_t dg_delta_rule_workspace_bytes(uint64_t N, uint32_t n_seq, uint32_t Hk, uint32_t H, uint32_t Dk, uint32_t Dv);
 int dg_delta_rule_fwd(const void *q, uint64_t ldq, const void *k, uint64_t ldk, const void *v, uint64_t ldv,
                       const float *g, uint64_t ldg, const float *beta, uint64_t ldbeta, uint64_t N, uint32_t n_seq,

@@ -176,6 +176,7 @@ _SIGNATURES = {
                                   C.c_void_p]),
     "dg_delta_rule_saved_bytes": (C.c_size_t, [C.c_uint64] + [C.c_uint32] * 4),
     "dg_delta_rule_fwd_workspace_bytes": (C.c_size_t, [C.c_uint64, C.c_uint32, C.c_uint32]),
+    "dg_delta_rule_fwd_least_workspace_bytes": (C.c_size_t, [C.c_uint64] + [C.c_uint32] * 5),
     "dg_delta_rule_workspace_bytes": (C.c_size_t, [C.c_uint64] + [C.c_uint32] * 5),
     "dg_delta_rule_fwd": (C.c_int, [C.c_void_p, C.c_uint64] * 5 + [C.c_uint64, C.c_uint32, C.c_void_p] + [C.c_uint32] * 5 + [C.c_float, C.c_uint32, C.c_void_p, C.c_void_p,
                                     C.c_uint64, C.c_void_p] + [C.c_void_p, C.c_size_t] * 2 + [C.c_void_p]),
@@ -864,6 +865,10 @@ def dg_delta_rule_saved_bytes(N, n_seq, H, Dk, Dv):
 
 def dg_delta_rule_fwd_workspace_bytes(N, n_seq, H):
     return int(lib().dg_delta_rule_fwd_workspace_bytes(N, n_seq, H))
+
+
+def dg_delta_rule_fwd_least_workspace_bytes(N, n_seq, H, Dk, Dv, saves):
+    return int(lib().dg_delta_rule_fwd_least_workspace_bytes(N, n_seq, H, Dk, Dv, saves))
 
 
 def dg_delta_rule_workspace_bytes(N, n_seq, Hk, H, Dk, Dv):

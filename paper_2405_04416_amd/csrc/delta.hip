@@ -29,6 +29,9 @@ size_t slot_bytes(uint64_t N, uint32_t n_seq) { return padded(slots_of(N, n_seq)
 // The workspace: T and P of the chunks, whose the chunks are, and what parts of sequences leave, for either pass; then what the backward pass hands on.
 size_t forward_bytes(uint64_t N, uint32_t n_seq, uint32_t H) { return weight_bytes(N, n_seq, H) + chunk_bytes(N, n_seq) + parts_bytes(N, n_seq, H); }
 
+// The first of these, of which heads that are taken token by token need nothing: it is most of it, 16 KB for 32 tokens of a head, and for 2^20 rays of 64 samples and 2 heads of 16 x 16 96 GiB.
+size_t chunks_bytes(uint64_t N, uint32_t n_seq, uint32_t H, uint32_t Dk, uint32_t Dv) { return takes_small(N, n_seq, H, Dk, Dv) ? 0 : forward_bytes(N, n_seq, H); }
+
 void use_workspace(Delta &d, void *ws)
 {
     d.weights = (Weights *)ws;
@@ -77,9 +80,14 @@ extern "C" size_t dg_delta_rule_saved_bytes(uint64_t N, uint32_t n_seq, uint32_t
 
 extern "C" size_t dg_delta_rule_fwd_workspace_bytes(uint64_t N, uint32_t n_seq, uint32_t H) { return forward_bytes(N, n_seq, H); }
 
+extern "C" size_t dg_delta_rule_fwd_least_workspace_bytes(uint64_t N, uint32_t n_seq, uint32_t H, uint32_t Dk, uint32_t Dv, uint32_t saves)
+{
+    return !saves && N <= kFewTokens * n_seq ? 0 : chunks_bytes(N, n_seq, H, Dk, Dv);
+}
+
 extern "C" size_t dg_delta_rule_workspace_bytes(uint64_t N, uint32_t n_seq, uint32_t Hk, uint32_t H, uint32_t Dk, uint32_t Dv)
 {
-    return forward_bytes(N, n_seq, H) + padded(marks_bytes(N, n_seq, H, Dk, Dv)) + rows_bytes(N, H, Dv) + slot_bytes(N, n_seq);
+    return chunks_bytes(N, n_seq, H, Dk, Dv) + padded(marks_bytes(N, n_seq, H, Dk, Dv)) + rows_bytes(N, H, Dv) + slot_bytes(N, n_seq);
 }
 
 extern "C" int dg_delta_rule_fwd(const void *q, uint64_t ldq, const void *k, uint64_t ldk, const void *v, uint64_t ldv, const float *g, uint64_t ldg,
@@ -145,13 +153,14 @@ extern "C" int dg_delta_rule_bwd(const void *q, uint64_t ldq, const void *k, uin
     d.dout = do_, d.lddo = lddo, d.dq = dq, d.dk = dk, d.dv = dv, d.lddq = lddq, d.lddk = lddk, d.lddv = lddv, d.dg = dg, d.dbeta = dbeta, d.lddg = lddg, d.lddb = lddbeta;
     d.first = first, d.N = N, d.n_seq = n_seq, d.Hk = Hk, d.H = H, d.Dk = Dk, d.Dv = Dv, d.reverse = reverse, d.scale = scale, d.slots = (uint32_t)slots_of(N, n_seq);
     d.marks = (float *)const_cast<void *>(saved), d.y = (float *)((char *)const_cast<void *>(saved) + marks);
-    use_workspace(d, ws);
-    char *const rest = (char *)ws + forward_bytes(N, n_seq, H);
+    const bool small = takes_small(N, n_seq, H, Dk, Dv);
+    if (!small) use_workspace(d, ws);
+    char *const rest = (char *)ws + chunks_bytes(N, n_seq, H, Dk, Dv);
     d.dmarks = (float *)rest, d.dr = (float *)(rest + marks), d.slot_seq = (const uint32_t *)(rest + marks + rows_bytes(N, H, Dv));
     use_vectors(d, dtype);
     d.vec_out = wide_rows(dv, lddv, Dv, dtype) && wide_rows(dq, lddq, Dk, dtype) && wide_rows(dk, lddk, Dk, dtype);
     if (N) launch_slots(d, (hipStream_t)stream);
-    if (takes_small(N, n_seq, H, Dk, Dv)) launch_small(d, dtype, true, (hipStream_t)stream);
+    if (small) launch_small(d, dtype, true, (hipStream_t)stream);
     else {
         if (N) launch_weights(d, dtype, true, (hipStream_t)stream);
         launch_backward(d, dtype, (hipStream_t)stream);

@@ -109,7 +109,7 @@ class DeltaMixer:
         o, out = self._buffer("o", [N, self.wv]), self._buffer("out", [N, self.width])
         if first is not None: o.zero_()         # rows of no segment are left as they are, and read by the projection
         B.dg_delta_rule_fwd(qv[:, :self.wq], k, qv[:, self.wq:], g, beta, self.Hk, n_seq, first, self.reverse, self.scale, s0, o, s_last, saved,
-                            self._workspace("ws_delta", B.dg_delta_rule_fwd_workspace_bytes(N, n_seq, self.H)))
+                            self._workspace("ws_delta", B.dg_delta_rule_fwd_least_workspace_bytes(N, n_seq, self.H, self.Dk, self.Dv, saved is not None)))
         self._product(self._rows8("o8", o), self.forth[2], out)
         keep_captured(self.captured, self.buffers)
         return t, out

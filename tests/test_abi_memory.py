@@ -135,6 +135,20 @@ def test_sizes_of_what_is_kept():
     assert one < two < 2.1 * one
 
 
+def test_small_heads_need_no_room_for_chunks():
+    """Heads that are taken token by token: what the gradient hands on (as much as is kept, and a number for each 64 tokens), and for the forward pass nothing."""
+    for N, n_seq, Hk, H, D in ((65536 * 64, 65536, 2, 2, 16), ((1 << 20) * 64, 1 << 20, 2, 2, 16), (5000 * 30, 5000, 1, 3, 32), (3000, 1000, 2, 2, 8)):
+        kept = B.dg_delta_rule_saved_bytes(N, n_seq, H, D, D)
+        assert B.dg_delta_rule_workspace_bytes(N, n_seq, Hk, H, D, D) <= kept + (N // 64 + n_seq) * 4 + 64
+        assert all(B.dg_delta_rule_fwd_least_workspace_bytes(N, n_seq, H, D, D, saves) == 0 for saves in (False, True))
+        assert B.dg_delta_rule_fwd_workspace_bytes(N, n_seq, H) > 0                     # for any heads
+    N, n_seq, H = 4000, 1000, 16                                                        # a few tokens
+    assert B.dg_delta_rule_fwd_least_workspace_bytes(N, n_seq, H, 128, 128, False) == 0
+    for shape in ((N, n_seq, H, 128, 128, True), (N + n_seq, n_seq, H, 128, 128, False), (64, 2, 2, 16, 16, False)):
+        least = B.dg_delta_rule_fwd_least_workspace_bytes(*shape)
+        assert 0 < least <= B.dg_delta_rule_fwd_workspace_bytes(*shape[:3]) and least < B.dg_delta_rule_workspace_bytes(*shape[:2], shape[2], *shape[2:5])
+
+
 @pytest.mark.parametrize("call", [
     lambda x: B.dg_rms_norm_fwd(x, x[:, :4], None, 1e-5, None, x),
     lambda x: B.dg_rms_norm_fwd(x, None, None, 1e-5, None, x.half()),

@@ -966,3 +966,30 @@ def test_delta_rule_in_parts_forgets():
     a = delta_inputs(np.random.default_rng(3), 3000, 1, 2, 64, 64, 1, torch.float16)
     for t in (0, 511, 512, 700, 1023, 1024, 1500, 2047, 2048, 2999): a["g"][t] = -np.inf
     check_delta(a, 1, None, torch.float16)
+
+
+@pytest.mark.parametrize("first", [False, True], ids=["even", "ragged"])
+@pytest.mark.parametrize("n_seq,S,Hk,H,D", [(700, 9, 2, 2, 16), (40, 3, 1, 3, 24), (1300, 70, 2, 4, 32), (9, 40, 2, 2, 64), (2, 300, 1, 3, 100)])
+def test_workspaces_of_exactly_what_is_asked_for(n_seq, S, Hk, H, D, first):
+    """What lies behind them stays as it is, and what lies in them does not matter."""
+    say("delta workspaces", n_seq, S, Hk, H, D, first)
+    rng = np.random.default_rng(n_seq)
+    N = n_seq * S
+    offsets = np.sort(np.concatenate([[0, N], rng.integers(0, N + 1, n_seq - 1)])) if first else None
+    a = delta_inputs(rng, N, Hk, H, D, D, n_seq, torch.float32)
+    want = run_delta(a, n_seq, offsets, torch.float32)
+    q, k, v, do, g, beta, s0, ds = (f32(a[n].reshape(N, -1)) if len(a[n]) == N else f32(a[n]) for n in ("q", "k", "v", "do", "g", "beta", "s0", "ds_last"))
+    fd = torch.from_numpy(offsets.astype(np.int32)).to(DEV) if first else None
+    sizes = dict(saved=B.dg_delta_rule_saved_bytes(N, n_seq, H, D, D), fwd=B.dg_delta_rule_fwd_least_workspace_bytes(N, n_seq, H, D, D, True),
+                 alone=B.dg_delta_rule_fwd_least_workspace_bytes(N, n_seq, H, D, D, False), bwd=B.dg_delta_rule_workspace_bytes(N, n_seq, Hk, H, D, D))
+    rooms = {n: torch.full((size + 4096,), 119, dtype=torch.uint8, device=DEV) for n, size in sizes.items()}
+    use = {n: rooms[n][:size] if size else None for n, size in sizes.items()}
+    o, alone, s_last, ds0 = torch.full_like(v, 5.0), torch.full_like(v, 5.0), torch.zeros_like(s0), torch.zeros_like(s0)
+    outs = {n: torch.full_like(x, 5.0) for n, x in zip(NAMES, (q, k, v, g, beta))}
+    B.dg_delta_rule_fwd(q, k, v, g, beta, Hk, n_seq, fd, False, 1.0, s0, o, s_last, use["saved"], use["fwd"])
+    B.dg_delta_rule_bwd(q, k, v, g, beta, Hk, n_seq, fd, False, 1.0, use["saved"], do, ds, *outs.values(), ds0, use["bwd"])
+    B.dg_delta_rule_fwd(q, k, v, g, beta, Hk, n_seq, fd, False, 1.0, s0, alone, None, None, use["alone"])
+    torch.cuda.synchronize()
+    for n, x in dict(outs, o=o, s_last=s_last, ds0=ds0).items(): assert torch.equal(x, want[n]), n
+    assert torch.equal(alone, o)
+    for n, size in sizes.items(): assert bool((rooms[n][size:] == 119).all()), n
