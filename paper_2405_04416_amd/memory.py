@@ -22,6 +22,7 @@ from .mixer import _overlap, keep_captured
 
 EPS = 1e-5
 KEY_EPS = 1e-6
+MOST_ROWS = 1 << 24     # of a product
 
 
 def rows_in_8_bits(x):
@@ -88,6 +89,9 @@ class DeltaMixer:
 
     def _product(self, a, b, y):
         M, N, K = a[0].shape[0], b[0].shape[0], a[0].shape[1]
+        for i in range(MOST_ROWS, M, MOST_ROWS):            # more rows than a product takes, some after the others
+            self._product([z[i:i + MOST_ROWS] for z in a], b, y[i:i + MOST_ROWS])
+        if M > MOST_ROWS: M, a, y = MOST_ROWS, [z[:MOST_ROWS] for z in a], y[:MOST_ROWS]
         B.dg_e4m3_product(*a, *b, y, self._workspace("ws_product", B.dg_e4m3_product_workspace_bytes(M, N, K)))
 
     def _rows8(self, name, x):

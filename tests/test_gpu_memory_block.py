@@ -196,6 +196,25 @@ def test_a_graph_outlives_passes_of_other_sizes():
         for z in others: assert bool((z == 7).all())
 
 
+def test_more_samples_than_a_product_takes():
+    """Segments do not know of each other: those around row 2^24, where products are cut, and the last ones give what they give alone."""
+    say("memory block of 2^24 samples and more")
+    S, n_seq, some = 37, 453600, 300
+    N = S * n_seq
+    assert N > (1 << 24) + 1000
+    block, alone = (DeltaMixer(16, 1, d_key=8, d_value=8, seed=4) for _ in range(2))
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(1)
+    x, dout = (torch.randn(N, 16, device=DEV, generator=gen).half() for _ in range(2))
+    g, beta = -torch.rand(N, 1, device=DEV, generator=gen), torch.rand(N, 1, device=DEV, generator=gen)
+    t, out = block.forward(x, None, g, beta, n_seq)
+    dx, dg, dbeta = block.backward(None, dout)
+    for seq in ((1 << 24) // S - some // 2, n_seq - some):
+        rows = slice(seq * S, (seq + some) * S)
+        _, out1 = alone.forward(x[rows].contiguous(), None, g[rows].contiguous(), beta[rows].contiguous(), some)
+        for name, a, b in zip(("out", "dx", "dg", "dbeta"), (out1, *alone.backward(None, dout[rows].contiguous())), (out, dx, dg, dbeta)): close(name, a, got(b[rows]), "fp16")
+
+
 def test_refusals():
     with pytest.raises(DistGridError):
         DeltaMixer(32, 2, weights=[torch.zeros(4, 4)] * 3, device=DEV)
