@@ -68,6 +68,7 @@ class DeltaMixer:
         """A buffer that this block keeps from pass to pass, replaced when a pass needs another size."""
         t, shape, dtype = self.buffers.get(name), torch.Size(shape), dtype or self.dtype
         if t is None or t.shape != shape or t.dtype != dtype:
+            keep_captured(self.captured, [t])           # products of other sizes have other workspaces within a pass
             t = self.buffers[name] = torch.empty(shape, dtype=dtype, device=self.dev)
         return t
 
@@ -77,6 +78,7 @@ class DeltaMixer:
     def _room8(self, name, N, W):
         t = self.buffers.get(name)
         if t is None or t[0].shape != (N, W):
+            keep_captured(self.captured, [t])
             t = self.buffers[name] = room_in_8_bits(N, W, self.dev)
         return t
 
@@ -115,7 +117,7 @@ class DeltaMixer:
         B.dg_delta_rule_fwd(qv[:, :self.wq], k, qv[:, self.wq:], g, beta, self.Hk, n_seq, first, self.reverse, self.scale, s0, o, s_last, saved,
                             self._workspace("ws_delta", B.dg_delta_rule_fwd_least_workspace_bytes(N, n_seq, self.H, self.Dk, self.Dv, saved is not None)))
         self._product(self._rows8("o8", o), self.forth[2], out)
-        keep_captured(self.captured, self.buffers)
+        keep_captured(self.captured, self.buffers.values())
         return t, out
 
     def forward(self, x, r, g, beta, n_seq, first=None, s0=None, s_last=None, training=True):
@@ -156,7 +158,7 @@ class DeltaMixer:
         self._product(self._rows8("dk8", draw.view(N, self.wq)), self.back[1], dn)
         B.dg_dropout_fwd(part, dn, 0.0, 0, 0, dn)           # without dropping: the sum
         B.dg_rms_norm_bwd(t, self.gamma, dn, dt, EPS, dx, self.dgamma, self._workspace("ws_norm", B.dg_rms_norm_bwd_workspace_bytes(N, self.width)))
-        keep_captured(self.captured, self.buffers)
+        keep_captured(self.captured, self.buffers.values())
         return dx, dg, dbeta
 
     def advance(self, x, r, g, beta, memory):

@@ -31,9 +31,9 @@ def _overlap(a, b):
 
 
 def keep_captured(kept, buffers):
-    """A graph replays with the addresses that it was captured with: buffers of a pass that is being captured stay, whatever sizes later passes need."""
+    """A graph replays with the addresses that it was captured with: the buffers of a pass that is being captured stay, whatever sizes what follows needs."""
     if torch.cuda.is_current_stream_capturing():
-        kept.append(list(buffers.values()))
+        kept.extend(buffers)
 
 
 class RayMixer:
@@ -55,6 +55,7 @@ class RayMixer:
         """A buffer that this block keeps from pass to pass, replaced when a pass needs another size."""
         t = self.buffers.get(name)
         if t is None or t.shape != shape or t.dtype != dtype:
+            keep_captured(self.captured, [t])
             t = self.buffers[name] = torch.empty(shape, dtype=dtype, device=self.dev)
         return t
 
@@ -96,7 +97,7 @@ class RayMixer:
         if training:
             self.saved = (x, n_seq, first, h0, states, p, self.drawn)
             self.drawn += -(-x.numel() // 4)
-        keep_captured(self.captured, self.buffers)
+        keep_captured(self.captured, self.buffers.values())
         return y
 
     def backward(self, dy, dh_last=None, dh0=None):
@@ -116,14 +117,14 @@ class RayMixer:
         B.dg_dropout_fwd(part, dy, 0.0, 0, 0, dx)
         B.dg_layer_norm_bwd(x, self.gamma_u, du, EPS, part, g[2], g[3], ws)
         B.dg_dropout_fwd(part, dx, 0.0, 0, 0, dx)
-        keep_captured(self.captured, self.buffers)
+        keep_captured(self.captured, self.buffers.values())
         return dx
 
     def advance(self, x, h):
         """One more sample for every segment, x [n_seq, width]; the states h [n_seq, width] fp32 are updated in place."""
         m, y = self._recur(x, x.shape[0], None, h, h, None), self._rows("y", x)
         B.dg_dropout_fwd(m, x, 0.0, 0, 0, y)
-        keep_captured(self.captured, self.buffers)
+        keep_captured(self.captured, self.buffers.values())
         return y
 
     def optimiser_step(self, iteration, lr):

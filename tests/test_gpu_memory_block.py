@@ -163,12 +163,13 @@ def test_own_results_go_in_again_without_a_residual(way):
         y = out.clone()
 
 
-def test_a_graph_outlives_passes_of_other_sizes():
-    """What a captured pass works in is not given back when passes of other sizes need other buffers."""
-    say("memory block, sizes between replays")
+@pytest.mark.parametrize("shape,N", [(SHAPES[0], 1536), (dict(width=1024, heads=1, d_key=64, d_value=64), 160)], ids=["rows", "products in parts"])
+def test_a_graph_outlives_passes_of_other_sizes(shape, N):
+    """What a captured pass works in is not given back when others, or this one, need buffers of other sizes."""
+    say("memory block, sizes between replays", N)
     rng = np.random.default_rng(11)
-    N, n_seq = 1536, 4
-    block, twin = (DeltaMixer(dtype=torch.bfloat16, seed=3, **SHAPES[0]) for _ in range(2))
+    n_seq = 4
+    block, twin = (DeltaMixer(dtype=torch.bfloat16, seed=3, **shape) for _ in range(2))
     rows, _, g, beta, s0, _ = make(rng, N, n_seq, block, "bf16")
     g, beta, s0 = f32(g), f32(beta), f32(s0)
 
