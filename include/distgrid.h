@@ -643,7 +643,7 @@ int dg_e4m3_product(const void *a, uint64_t lda, const uint8_t *a_scales, uint64
  * Everything is as exact as in fp32, and the same call gives the same bits.  Tokens are taken 32 or 64 at a time: an infinity or NaN in a token's row may show in
  * the results of up to 63 tokens before it.  o must not overlap an input.
  * Errors: DG_ERR_ARG for heads or sizes of 0, H that Hk does not divide, N that n_seq does not divide (first NULL), a scale that is not finite;
- * DG_ERR_UNSUPPORTED for Dk or Dv above 128, rows 2^24 values or more apart, N >= 2^32, n_seq >= 2^31, H > 2^16, N H > 2^36, n_seq H > 2^32. */
+ * DG_ERR_UNSUPPORTED for Dk or Dv above 128, rows 2^24 values or more apart, N > 2^32 - 64, n_seq >= 2^31, H > 2^16, N H > 2^36, n_seq H > 2^32. */
 size_t dg_delta_rule_saved_bytes(uint64_t N, uint32_t n_seq, uint32_t H, uint32_t Dk, uint32_t Dv);
 size_t dg_delta_rule_fwd_workspace_bytes(uint64_t N, uint32_t n_seq, uint32_t H);
 size_t dg_delta_rule_fwd_least_workspace_bytes(uint64_t N, uint32_t n_seq, uint32_t H, uint32_t Dk, uint32_t Dv,

@@ -54,8 +54,9 @@ int check_sizes(const char *who, uint64_t N, uint32_t n_seq, const uint32_t *fir
     DG_REQUIRE(dg_rows::known_type(dtype), DG_ERR_ARG, "%s: unknown element type %u", who, dtype);
     DG_REQUIRE(Hk >= 1 && H >= 1 && H % Hk == 0 && Dk >= 1 && Dv >= 1, DG_ERR_ARG, "%s: heads and their sizes must be positive, and H a multiple of Hk", who);
     DG_REQUIRE(Dk <= kMaxD && Dv <= kMaxD, DG_ERR_UNSUPPORTED, "%s: heads of more than %d values", who, kMaxD);
-    DG_REQUIRE(N < 1ull << 32 && H <= 1u << 16 && n_seq < 1u << 31 && N * H <= 1ull << 36 && (uint64_t)n_seq * H <= 1ull << 32, DG_ERR_UNSUPPORTED,
-               "%s: more than 2^32 rows, 2^31 sequences, 2^16 heads, 2^36 rows of heads or 2^32 memories", who);
+    // tokens of a sequence are counted in steps of up to 64, in 32 bits
+    DG_REQUIRE(N <= (1ull << 32) - kMark && H <= 1u << 16 && n_seq < 1u << 31 && N * H <= 1ull << 36 && (uint64_t)n_seq * H <= 1ull << 32, DG_ERR_UNSUPPORTED,
+               "%s: more than 2^32 - 64 rows, 2^31 sequences, 2^16 heads, 2^36 rows of heads or 2^32 memories", who);
     DG_REQUIRE(n_seq >= 1 || N == 0, DG_ERR_ARG, "%s: rows without a sequence", who);
     DG_REQUIRE(first || n_seq == 0 || N % n_seq == 0, DG_ERR_ARG, "%s: %llu rows in %u sequences of one length", who, (unsigned long long)N, n_seq);
     DG_REQUIRE(dg::aligned(first, 4), DG_ERR_ARG, "%s: misaligned offsets", who);

@@ -70,8 +70,8 @@ struct Span {
     uint64_t begin;
     uint32_t len;
     int32_t turn;                       // -1: from the last row to the first, else 0
-    // row of token i; without a branch, which would keep loads apart
-    __device__ __forceinline__ uint64_t row(uint32_t i) const { return begin + (turn & (len - 1)) + (int64_t)(((int32_t)i ^ turn) - turn); }
+    // row of token i < len, of which there may be 2^31 and more: all in 32 bits without a sign, then added.  Without a branch, which would keep loads apart
+    __host__ __device__ __forceinline__ uint64_t row(uint32_t i) const { return begin + ((i ^ (uint32_t)turn) + ((uint32_t)turn & len)); }
 };
 
 // no row from N on, whatever the offsets say

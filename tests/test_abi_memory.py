@@ -135,6 +135,14 @@ def test_sizes_of_what_is_kept():
     assert one < two < 2.1 * one
 
 
+def test_the_most_rows():
+    """Tokens are counted in steps of up to 64, in 32 bits.  (The last call lacks a workspace.)"""
+    long = dict(n_seq=1, H=1, Hk=1)
+    for N in ((1 << 32) - 1, (1 << 32) - 63):
+        assert delta(N=N, **long) == -2 and delta_bwd(N=N, **long) == -2
+    assert delta(N=(1 << 32) - 64, **long) == -3 and delta_bwd(N=(1 << 32) - 64, **long) == -3
+
+
 def test_small_heads_need_no_room_for_chunks():
     """Heads that are taken token by token: what the gradient hands on (as much as is kept, and a number for each 64 tokens), and for the forward pass nothing."""
     for N, n_seq, Hk, H, D in ((65536 * 64, 65536, 2, 2, 16), ((1 << 20) * 64, 1 << 20, 2, 2, 16), (5000 * 30, 5000, 1, 3, 32), (3000, 1000, 2, 2, 8)):
