@@ -28,7 +28,7 @@ __device__ __forceinline__ void take_chunk(const Operands<T, KS> &o, uint32_t c1
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
         bf16x8 sp[3];
-        split_rows<3>(S[2 * s], S[2 * s + 1], sp);
+        split_rows<3, (n > 1)>(S[2 * s], S[2 * s + 1], sp);
 #pragma unroll
         for (int h = 0; h < 2; ++h) ks[h] = multiply<n, 3>(keys[s][h], sp, ks[h]);
     }
@@ -58,8 +58,8 @@ __device__ __forceinline__ void take_chunk(const Operands<T, KS> &o, uint32_t c1
 #pragma unroll
         for (int x = 0; x < 4; ++x) gradient[h * 4 + x] = dr[h][x];
     }
-    split8<3>(queried, right_q);
-    split_rows<3>(back[0], back[1], right);
+    split8<3, (n > 1)>(queried, right_q);
+    split_rows<3, (n > 1)>(back[0], back[1], right);
     const float whole = o.weight.whole;
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
@@ -90,7 +90,7 @@ struct Share {
         f32x4 sum[kOwn][2];
 #pragma unroll
         for (int s = 0; s < kOwn; ++s) {
-            split_rows<3>(S[2 * s], S[2 * s + 1], sp);
+            split_rows<3, (n > 1)>(S[2 * s], S[2 * s + 1], sp);
 #pragma unroll
             for (int h = 0; h < 2; ++h) sum[s][h] = multiply<n, 3>(keys[s][h], sp, (f32x4){});
         }
@@ -130,7 +130,7 @@ struct Share {
         for (int t = 0; t < 2 * kOwn; ++t) S[t] = multiply<n, 3>(queries[t], queried, S[t] * whole);
 #pragma unroll
         for (int h = 0; h < 2; ++h) back[h] = -dr[h] * read[h];
-        split_rows<3>(back[0], back[1], right);
+        split_rows<3, (n > 1)>(back[0], back[1], right);
 #pragma unroll
         for (int t = 0; t < 2 * kOwn; ++t) S[t] = multiply<n, 3>(turned[t], right, S[t]);
         if constexpr (!kEnds)
@@ -163,7 +163,7 @@ __device__ __forceinline__ void make_ahead(const Operands<T, KS> &o, const Tile<
 #pragma unroll
             for (int x = 0; x < 4; ++x) dout[h * 4 + x] *= query[x];
         }
-        split8<3>(dout, pieces);
+        split8<3, (n > 1)>(dout, pieces);
 #pragma unroll
         for (int p = 0; p < 3; ++p) to.queried[p][lane] = __builtin_bit_cast(u32x4, pieces[p]);
     }

@@ -6,8 +6,9 @@
 //   Y = T (V - e^G K S)  (what the tokens miss),   U = beta Y  (what they write),   O = scale e^G Q S + P U,   S' = e^G[last] S + K^T (e^(G[last] - G) U).
 //
 // Products are taken on the matrix units in bf16, of values that are cut into pieces of 8 bits: one for a bf16 value, two for fp16, three for
-// fp32, which lose nothing; of the products of pieces those below 2^-24 are left out.  So everything is as exact as in fp32, at several times
-// the rate of the fp32 matrix instruction (139 TFLOP/s measured; three bf16 products 445).
+// fp32, which lose nothing.  Of the products of pieces the smallest three of nine are left out: at most 2^-22 of the product of two values, of either sign (second pieces are rounded: cut off they would leave
+// up to 2^-21, always of the product's sign).  A single product is off by 0.7 U in root mean square, U = 2^-24, where fp32 has 0.4; a sum by its roundings, as in fp32.  All of it at several times the rate
+// of the fp32 matrix instruction (139 TFLOP/s measured; three bf16 products 445).
 #pragma once
 #include "rows_common.h"
 
@@ -102,8 +103,9 @@ __device__ __forceinline__ float top(float x) { return __uint_as_float(__float_a
 // the upper halves of two words, a's below b's
 __device__ __forceinline__ uint32_t upper(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302); }
 
-// x = sum of n pieces, each the leading 8 bits of what the ones before leave
-template <int n, int count>
+// x = sum of n pieces of 8 bits.  Of three the first is cut off, so that no finite value has an infinite one, and with kNear the second is rounded, so that what it leaves has either sign; otherwise it
+// is cut off, too: for a product with a single piece, of which nothing is left out.
+template <int n, int count, bool kNear = true>
 __device__ __forceinline__ void split(const float (&x)[count], uint32_t (&out)[n][count / 2])
 {
 #pragma unroll
@@ -111,6 +113,13 @@ __device__ __forceinline__ void split(const float (&x)[count], uint32_t (&out)[n
         float a = x[i], b = x[i + 1];
 #pragma unroll
         for (int p = 0; p < n; ++p) {
+            if (kNear && n == 3 && p == 1) {            // a conversion to bf16 takes longer than the addition (65536 tokens x 8 heads 1.47 ms, 1.43)
+                const float ra = __uint_as_float(__float_as_uint(a) + 0x8000u), rb = __uint_as_float(__float_as_uint(b) + 0x8000u);
+                out[p][i / 2] = upper(ra, rb);
+                a -= top(ra);
+                b -= top(rb);
+                continue;
+            }
             out[p][i / 2] = upper(a, b);
             if (p + 1 < n) {
                 a -= top(a);
@@ -122,34 +131,34 @@ __device__ __forceinline__ void split(const float (&x)[count], uint32_t (&out)[n
 
 __device__ __forceinline__ bf16x8 operand(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
 
-template <int n>
+template <int n, bool kNear = true>
 __device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&out)[n])
 {
     uint32_t w[n][4];
-    split<n, 8>(x, w);
+    split<n, 8, kNear>(x, w);
 #pragma unroll
     for (int p = 0; p < n; ++p) out[p] = operand((u32x4){w[p][0], w[p][1], w[p][2], w[p][3]});
 }
 
 // Two 16-row results of the matrix unit as the right operand of a product that sums over their rows
-template <int n>
+template <int n, bool kNear = true>
 __device__ __forceinline__ void split_rows(const f32x4 &a, const f32x4 &b, bf16x8 (&out)[n])
 {
     const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-    split8<n>(x, out);
+    split8<n, kNear>(x, out);
 }
 
 __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
-// Sum of the products of pieces whose orders add up to less than three
+// Sum of the products of pieces whose orders add up to less than three, the smallest first, which are rounded least while the sum is small
 template <int na, int nb>
 __device__ __forceinline__ f32x4 multiply(const bf16x8 (&a)[na], const bf16x8 (&b)[nb], f32x4 c)
 {
 #pragma unroll
-    for (int i = 0; i < na; ++i)
+    for (int order = na + nb - 2 < 2 ? na + nb - 2 : 2; order >= 0; --order)
 #pragma unroll
-        for (int j = 0; j < nb; ++j)
-            if (i + j < 3) c = mfma(a[i], b[j], c);
+        for (int i = 0; i < na; ++i)
+            if (order >= i && order - i < nb) c = mfma(a[i], b[order - i], c);
     return c;
 }
 
@@ -160,12 +169,12 @@ __device__ __forceinline__ f32x4 multiply_soon(const bf16x8 (&a)[na], const bf16
     f32x4 other = {};
     int turn = 0;
 #pragma unroll
-    for (int i = 0; i < na; ++i)
+    for (int order = na + nb - 2 < 2 ? na + nb - 2 : 2; order >= 0; --order)
 #pragma unroll
-        for (int j = 0; j < nb; ++j)
-            if (i + j < 3) {
-                if (turn++ % 2) other = mfma(a[i], b[j], other);
-                else c = mfma(a[i], b[j], c);
+        for (int i = 0; i < na; ++i)
+            if (order >= i && order - i < nb) {
+                if (turn++ % 2) other = mfma(a[i], b[order - i], other);
+                else c = mfma(a[i], b[order - i], c);
             }
     return c + other;
 }

@@ -32,7 +32,7 @@ __device__ __forceinline__ void take_chunk(const Operands<T, KS> &o, uint32_t c1
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
         bf16x8 sp[3];
-        split_rows<3>(S[2 * s], S[2 * s + 1], sp);
+        split_rows<3, (n > 1)>(S[2 * s], S[2 * s + 1], sp);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             ks[h] = multiply<n, 3>(keys[s][h], sp, ks[h]);
@@ -62,7 +62,7 @@ __device__ __forceinline__ void take_chunk(const Operands<T, KS> &o, uint32_t c1
         u[h] = y * beta[h];
     }
     bf16x8 written[3];
-    split_rows<3>(u[0] * until[0], u[1] * until[1], written);
+    split_rows<3, (n > 1)>(u[0] * until[0], u[1] * until[1], written);
     const float whole = o.weight.whole;
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) S[t] = multiply<n, 3>(turned[t], written, S[t] * whole);
@@ -98,7 +98,7 @@ struct Share {
         f32x4 sum[kOwn][2];
 #pragma unroll
         for (int s = 0; s < kOwn; ++s) {
-            split_rows<3>(S[2 * s], S[2 * s + 1], sp[s]);
+            split_rows<3, (n > 1)>(S[2 * s], S[2 * s + 1], sp[s]);
 #pragma unroll
             for (int h = 0; h < 2; ++h) sum[s][h] = multiply<n, 3>(keys[s][h], sp[s], (f32x4){});
         }
@@ -140,7 +140,7 @@ struct Share {
         split_rows<3>(r[0], r[1], right);
 #pragma unroll
         for (int h = 0; h < 2; ++h) y[h] = multiply_soon<3, 3>(inverse[h], right, (f32x4){});
-        split_rows<3>(y[0] * written[0], y[1] * written[1], right);
+        split_rows<3, (n > 1)>(y[0] * written[0], y[1] * written[1], right);
 #pragma unroll
         for (int t = 0; t < 2 * kOwn; ++t) S[t] = multiply<n, 3>(turned[t], right, S[t] * whole);
         // for those aside

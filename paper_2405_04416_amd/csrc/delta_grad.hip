@@ -85,11 +85,11 @@ __device__ __forceinline__ void cleared(const dg_rows::Pack<T, W> &p, uint32_t c
     for (int i = 0; i < W; ++i) out[i] = in && c + i < D ? (float)p.v[i] : 0.0f;
 }
 
-template <int n, int rows, int pitch>
+template <bool kNear = true, int n, int rows, int pitch>
 __device__ __forceinline__ void put4(const float (&v)[4], uint16_t (&to)[n][rows][pitch], uint32_t row, uint32_t col)
 {
     uint32_t w[n][2];
-    split<n, 4>(v, w);
+    split<n, 4, kNear>(v, w);
 #pragma unroll
     for (int p = 0; p < n; ++p) *reinterpret_cast<u32x2 *>(&to[p][row][col]) = (u32x2){w[p][0], w[p][1]};
 }
@@ -117,9 +117,6 @@ __device__ __forceinline__ void turn(const T *K, uint32_t ld, uint32_t Dk, uint3
         for (int p = 0; p < n; ++p) *reinterpret_cast<u32x4 *>(&to.rows[p][t][col]) = (u32x4){w[p][0], w[p][1], w[p][2], w[p][3]};
     }
 }
-
-// four values of a row side by side
-__device__ __forceinline__ void put_across(const float (&v)[4], uint16_t (&to)[3][kTokens][kTokenPitch], uint32_t row, uint32_t col) { put4(v, to, row, col); }
 
 template <class T, int KS, bool kVec>
 __global__ void __launch_bounds__(kThreads)
@@ -304,13 +301,13 @@ delta_grad_kernel(Delta d, uint64_t from)
                 x[k][y] = d.scale * fade * m[k][y];
                 z[y] = j0 + y < i ? -rate_i * fade * e[k][y] : 0.0f;
             }
-            put_across(x[k], lds.pull.X, i, j0);
-            put_across(z, lds.pull.Z, i, j0);
+            put4<(n > 1)>(x[k], lds.pull.X, i, j0);
+            put4<(n > 1)>(z, lds.pull.Z, i, j0);
         }
         // the blocks behind the diagonal that are multiplied with
         if (half == 1 && wave < 2) {
-            put_across(none, lds.pull.X, wave * 32 + c16, wave * 32 + 16 + r4);
-            put_across(none, lds.pull.Z, wave * 32 + c16, wave * 32 + 16 + r4);
+            put4<(n > 1)>(none, lds.pull.X, wave * 32 + c16, wave * 32 + 16 + r4);
+            put4<(n > 1)>(none, lds.pull.Z, wave * 32 + c16, wave * 32 + 16 + r4);
         }
         // what the memory before gives and the one behind takes, and what the tokens of the block tell each other
         float at_end = 0.0f, dG = 0.0f;

@@ -968,6 +968,27 @@ def test_delta_rule_in_parts_forgets():
     check_delta(a, 1, None, torch.float16)
 
 
+@pytest.mark.parametrize("n_seq,S,H,D", [(2, 160, 8, 128), (16, 8, 64, 64), (2, 160, 16, 33), (64, 16, 32, 100)])
+def test_single_products_are_off_to_either_side(n_seq, S, H, D):
+    """o and dq of one product each, of fp32 values: queries, and gradients of o, of one value each, and nothing is written.  With leading bits of 1, pieces of 8 bits each leave less than 2^-7 behind the first
+    and 2^-16 behind the second, which is rounded; what is left out is 2 (2^-7 + 2^-16) 2^-16 < 4.1 U of the product then, and the last of the sums 2 U at most, the ones before, of what is 2^-6 and less, a tenth:
+    6.2 U.  Errors of either sign have a mean of 6.2 U sqrt(2 ln(2 / 1e-9) / n) = 0.26 U at most, but for one time in 1e9, over n = 25 000 and more."""
+    say("delta single products", n_seq, S, H, D)
+    rng = np.random.default_rng(D)
+    N, f = n_seq * S, lambda *shape: (rng.uniform(1, 2, shape) * rng.choice([-1.0, 1.0], shape)).astype(np.float32)
+    s0, value, dvalue = f(n_seq, H, D, D), f(N, H), f(N, H)
+    at, seq, t, h = rng.integers(0, D, (N, H)), np.repeat(np.arange(n_seq), S)[:, None], np.arange(N)[:, None], np.arange(H)[None]
+    a = {n: np.zeros((N, H, D)) for n in ("q", "k", "v", "do")}
+    a["q"][t, h, at], a["do"][t, h, at] = value, dvalue
+    a.update(g=np.zeros((N, H)), beta=np.zeros((N, H)), s0=s0, ds_last=None)
+    res = run_delta(a, n_seq, None, torch.float32)
+    for n, x, v, S0 in (("o", res["o"], value, s0[seq, h, at]), ("dq", res["dq"], dvalue, s0[seq, h, :, at])):
+        want = v[:, :, None].astype(np.float64) * S0
+        off = (got(x).reshape(want.shape) - want) / want
+        assert off.size >= 25000 and np.abs(off).max() <= 6.2 * U, (n, np.abs(off).max() / U)
+        assert abs(off.mean()) <= 0.26 * U, (n, off.mean() / U)
+
+
 @pytest.mark.parametrize("first", [False, True], ids=["even", "ragged"])
 @pytest.mark.parametrize("n_seq,S,Hk,H,D", [(700, 9, 2, 2, 16), (40, 3, 1, 3, 24), (1300, 70, 2, 4, 32), (9, 40, 2, 2, 64), (2, 300, 1, 3, 100)])
 def test_workspaces_of_exactly_what_is_asked_for(n_seq, S, Hk, H, D, first):
