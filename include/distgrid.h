@@ -634,7 +634,7 @@ int dg_e4m3_product(const void *a, uint64_t lda, const uint8_t *a_scales, uint64
  * q, k [N, Hk Dk], v, o [N, H Dv], heads next to each other in a row; H is a multiple of Hk, head h takes key head h / (H / Hk).
  * g (logarithm of the decay, <= 0; -infinity, and anything below -104, forgets all that is finite) and beta (rate) [N, H] fp32, rows ldg and ldbeta apart.
  * s0, s_last [n_seq, H, Dk, Dv] fp32, either may be NULL; s_last receives the memories after the last tokens (s0 for a sequence without
- * one) and may be s0, unless a backward pass is to follow.  Keys of length one (dg_rms_norm_fwd over rows of Dk with gamma = Dk^-1/2) and rates up to 1 keep memories bounded.
+ * one) and may be s0, which the backward pass does not read.  Keys of length one (dg_rms_norm_fwd over rows of Dk with gamma = Dk^-1/2) and rates up to 1 keep memories bounded.
  * first, reverse: as for dg_recurrence_fwd.  One token per sequence (N == n_seq), or a few, is the step of a program that gets its tokens one after the other.
  * saved: NULL, or dg_delta_rule_saved_bytes(N, n_seq, H, Dk, Dv) bytes for the backward pass, 16-byte aligned (what tokens write, and the memories before every
  * 64th).  ws: dg_delta_rule_fwd_workspace_bytes(N, n_seq, H) bytes, 16-byte aligned, are enough for heads of any size; a call needs no more than

@@ -143,7 +143,7 @@ few_rows_kernel(Product p)
 // eight pieces of 16, piece c of row r at place c ^ key(r): the 16 lanes that read together then meet all banks once.
 __device__ __forceinline__ uint32_t key(uint32_t r) { return (r & 7) ^ (r >> 3 & 1); }
 
-// kBuffers blocks of columns are in LDS or on their way.
+// Two blocks of columns are in LDS or on their way.
 template <int WM, int WN, int PM, int PN, int buffers>
 struct Tile {
     static constexpr int kWM = WM, kWN = WN;

@@ -123,13 +123,13 @@ class DeltaMixer:
     def forward(self, x, r, g, beta, n_seq, first=None, s0=None, s_last=None, training=True):
         """x, r [N, width] (r may be None) -> (t, out) for the next block.  g, beta [N, heads] fp32; n_seq segments of N / n_seq samples each, or of the rows that `first`
         gives them (of rows of none `out` is 0).  s0, s_last [n_seq, heads, d_key, d_value] fp32 or None: memories in and out (s_last may be s0 outside training).
-        The results are buffers that the next pass overwrites, unless that is a training pass on them, or one without r (where t is x).  backward reads x, g, beta, first and s0 again: they
+        The results are buffers that the next pass overwrites, unless that is a training pass on them, or one without r (where t is x).  backward reads x, g, beta and first again: they
         have to stay as they are until then."""
         N = x.shape[0]
         saved = None
         if training:
             if s0 is not None and s_last is not None and _overlap(s0, s_last):
-                raise B.DistGridError("the gradient needs s0: s_last must not lie in its memory")
+                raise B.DistGridError("s_last must not lie in the memory of s0, of which ds0 is the gradient")
             self._part_with(x, r)
             saved = self._workspace("saved", max(B.dg_delta_rule_saved_bytes(N, n_seq, self.H, self.Dk, self.Dv), 16))
         t, out = self._mix(x, r, g, beta, n_seq, first, s0, s_last, saved)

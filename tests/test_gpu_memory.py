@@ -968,6 +968,25 @@ def test_delta_rule_in_parts_forgets():
     check_delta(a, 1, None, torch.float16)
 
 
+@pytest.mark.parametrize("n_seq,S,H,D", [(2, 70, 2, 64), (800, 20, 1, 16), (5, 4, 3, 40), (300, 40, 8, 64), (1, 1700, 2, 64), (2, 3000, 1, 32)])
+def test_memories_in_place_in_training(n_seq, S, H, D):
+    """The gradient does not read s0: s_last may lie there."""
+    say("delta rule in place, training", n_seq, S, H, D)
+    N = n_seq * S
+    a = delta_inputs(np.random.default_rng(8), N, H, H, D, D, n_seq, torch.bfloat16)
+    want = run_delta(a, n_seq, None, torch.bfloat16)
+    t = {n: torch.from_numpy(a[n].reshape(N, -1)).to(DEV, torch.bfloat16) for n in ("q", "k", "v", "do")}
+    g, beta, memory, ds = f32(a["g"].reshape(N, -1)), f32(a["beta"].reshape(N, -1)), f32(a["s0"]), f32(a["ds_last"])
+    room = lambda n: torch.full((n,), 255, dtype=torch.uint8, device=DEV)
+    saved, ws = room(B.dg_delta_rule_saved_bytes(N, n_seq, H, D, D)), room(B.dg_delta_rule_workspace_bytes(N, n_seq, H, H, D, D))
+    o, grads = torch.zeros_like(t["v"]), [torch.zeros_like(t[n]) for n in ("q", "k", "v")] + [torch.zeros_like(g) for _ in range(2)]
+    B.dg_delta_rule_fwd(t["q"], t["k"], t["v"], g, beta, H, n_seq, None, False, 1.0, memory, o, memory, saved, ws)
+    assert torch.equal(memory, want["s_last"]) and torch.equal(o, want["o"])
+    memory.fill_(float("nan"))
+    B.dg_delta_rule_bwd(t["q"], t["k"], t["v"], g, beta, H, n_seq, None, False, 1.0, saved, t["do"], ds, *grads, ds, ws)
+    for n, x in zip(NAMES, grads + [ds]): assert torch.equal(x, want[n]), n
+
+
 @pytest.mark.parametrize("n_seq,S,H,D", [(2, 160, 8, 128), (16, 8, 64, 64), (2, 160, 16, 33), (64, 16, 32, 100)])
 def test_single_products_are_off_to_either_side(n_seq, S, H, D):
     """o and dq of one product each, of fp32 values: queries, and gradients of o, of one value each, and nothing is written.  With leading bits of 1, pieces of 8 bits each leave less than 2^-7 behind the first
