@@ -144,14 +144,14 @@ few_rows_kernel(Product p)
 __device__ __forceinline__ uint32_t key(uint32_t r) { return (r & 7) ^ (r >> 3 & 1); }
 
 // Two blocks of columns are in LDS or on their way.
-template <int WM, int WN, int PM, int PN, int buffers>
+template <int WM, int WN, int PM, int PN>
 struct Tile {
     static constexpr int kWM = WM, kWN = WN;
-    static constexpr uint32_t kWaves = PM * PN, kThreads = 64 * kWaves, kRowsA = 32 * WM * PM, kRowsB = 32 * WN * PN, kPM = PM, kPN = PN, kBuffers = buffers;
+    static constexpr uint32_t kWaves = PM * PN, kThreads = 64 * kWaves, kRowsA = 32 * WM * PM, kRowsB = 32 * WN * PN, kPM = PM, kPN = PN;
 };
-using Large = Tile<4, 4, 2, 2, 2>;      // 256 x 256
-using Middle = Tile<2, 2, 2, 2, 2>;     // 128 x 128
-using Small = Tile<1, 1, 2, 2, 2>;      // 64 x 64
+using Large = Tile<4, 4, 2, 2>;         // 256 x 256
+using Middle = Tile<2, 2, 2, 2>;        // 128 x 128
+using Small = Tile<1, 1, 2, 2>;         // 64 x 64
 
 // Whole blocks of columns of a side's rows into LDS.  Loads that write to LDS put lane i's 16 bytes at place i, so lanes choose what they fetch: at one address for
 // the workgroup and 32-bit distances from it (255 rows of less than 2^24 bytes).
@@ -253,8 +253,7 @@ tile_kernel(Product p)
 {
     constexpr int WM = Tile::kWM, WN = Tile::kWN;
     constexpr uint32_t kRowsA = Tile::kRowsA, kRowsB = Tile::kRowsB, kBytes = (kRowsA + kRowsB) * kBlockK;
-    constexpr uint32_t kBuffers = Tile::kBuffers;
-    __shared__ alignas(16) uint8_t lds[kBuffers][kBytes];       // blocks of columns: rows of a, then of b
+    __shared__ alignas(16) uint8_t lds[2][kBytes];       // blocks of columns: rows of a, then of b
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), tiles = p.tiles_m * p.tiles_n;
     // Workgroups go to the eight chiplets in turn: each gets a run of neighbouring tiles, in columns of eight, so that its cache serves them
     uint32_t id = blockIdx.x;
@@ -293,16 +292,14 @@ tile_kernel(Product p)
     };
     const uint32_t whole = end * kBlockK <= p.K ? end : end - 1;       // blocks before this one are whole
     const uint32_t at_a = wm * kBlockK, at_b = (kRowsA + wn) * kBlockK;
-    constexpr uint32_t kLater = (kBuffers - 2) * (kRowsA + kRowsB) / 8 / Tile::kWaves;      // loads of a wavefront for the blocks behind the next one
     Half<WM, WN> first, second;
     // behind the last block: something that is there, and is not used, so that as many loads as ever are on their way
-    auto fetch_ahead = [&](uint32_t kb) { fetch(kb < whole ? kb : whole - 1, (kb - begin) % kBuffers); };
+    auto fetch_ahead = [&](uint32_t kb) { fetch(kb < whole ? kb : whole - 1, (kb - begin) % 2); };
     if (begin < whole) {
         fetch_exponents(begin);
         fetch(begin, 0);
-#pragma unroll
-        for (uint32_t i = 1; i < kBuffers; ++i) fetch_ahead(begin + i);
-        loads_done<kLater + (kRowsA + kRowsB) / 8 / Tile::kWaves>();
+        fetch_ahead(begin + 1);
+        loads_done<(kRowsA + kRowsB) / 8 / Tile::kWaves>();
         first.read(lds[0] + at_a, lds[0] + at_b, lane, 0);
     }
     // Half a block is multiplied while the next half's operands come from LDS, of the next block too: between the halves a block's operands are all in registers,
@@ -315,13 +312,13 @@ tile_kernel(Product p)
 #pragma unroll
             for (int t = 0; t < WN; ++t) eb[t] = next_b[t];
         }
-        second.read(lds[i % kBuffers] + at_a, lds[i % kBuffers] + at_b, lane, 1);
+        second.read(lds[i % 2] + at_a, lds[i % 2] + at_b, lane, 1);
         first.multiply(ea, eb, acc);
         __builtin_amdgcn_sched_barrier(0);
-        loads_done<kLater>();
+        loads_done<0>();
         if (i % 4 == 0 && kb + 4 < whole) fetch_exponents(kb + 4);
-        fetch_ahead(kb + kBuffers);
-        first.read(lds[(i + 1) % kBuffers] + at_a, lds[(i + 1) % kBuffers] + at_b, lane, 0);
+        fetch_ahead(kb + 2);
+        first.read(lds[(i + 1) % 2] + at_a, lds[(i + 1) % 2] + at_b, lane, 0);
         second.multiply(ea, eb, acc);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
