@@ -968,6 +968,36 @@ def test_delta_rule_in_parts_forgets():
     check_delta(a, 1, None, torch.float16)
 
 
+@pytest.mark.parametrize("n_seq,S,H,Dk,Dv", [((1 << 24) + 5000, 1, 1, 4, 4), (65600, 5, 64, 1, 33)], ids=["token by token", "in chunks"])
+def test_more_workgroups_than_a_launch_has(n_seq, S, H, Dk, Dv):
+    """More than 2^22, which launches take one after the other: sequences around there, and the last ones, give what they give alone, bit for bit."""
+    say("delta rule in several launches", n_seq, S, H, Dk, Dv)
+    assert n_seq * H > (1 << 22) * (4 if Dv <= 16 else 1)
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(9)
+    normal = lambda n, w: torch.randn(n, w, device=DEV, generator=gen)
+
+    def both(n, q, k, v, do, g, beta):
+        room = lambda size: torch.empty(size, dtype=torch.uint8, device=DEV)
+        saved, ws = room(B.dg_delta_rule_saved_bytes(n * S, n, H, Dk, Dv)), room(B.dg_delta_rule_workspace_bytes(n * S, n, H, H, Dk, Dv))
+        o, outs, ds0 = torch.zeros_like(v), [torch.zeros_like(x) for x in (q, k, v, g, beta)], torch.zeros(n, H, Dk, Dv, device=DEV)
+        B.dg_delta_rule_fwd(q, k, v, g, beta, H, n, None, True, 0.5, None, o, None, saved, ws)
+        B.dg_delta_rule_bwd(q, k, v, g, beta, H, n, None, True, 0.5, saved, do, None, *outs, ds0, ws)
+        return [o, *outs, ds0.view(n, -1)]
+
+    N = n_seq * S
+    rows = [normal(N, H * Dk), normal(N, H * Dk), normal(N, H * Dv), normal(N, H * Dv), -torch.rand(N, H, device=DEV, generator=gen), torch.rand(N, H, device=DEV, generator=gen)]
+    rows[1] /= Dk ** 0.5 * 4
+    whole = both(n_seq, *rows)
+    some = 3000 if H == 1 else 50
+    for seq in ((1 << 22) * (4 if Dv <= 16 else 1) // H - some // 2, n_seq - some):
+        at = slice(seq * S, (seq + some) * S)
+        alone = both(some, *(x[at].contiguous() for x in rows))
+        for name, a, b in zip(("o", "dq", "dk", "dv", "dg", "dbeta", "ds0"), alone, whole): assert torch.equal(a, b[seq:seq + some] if name == "ds0" else b[at]), name
+    del whole, alone
+    torch.cuda.empty_cache()
+
+
 @pytest.mark.parametrize("n_seq,S,H,D", [(2, 70, 2, 64), (800, 20, 1, 16), (5, 4, 3, 40), (300, 40, 8, 64), (1, 1700, 2, 64), (2, 3000, 1, 32)])
 def test_memories_in_place_in_training(n_seq, S, H, D):
     """The gradient does not read s0: s_last may lie there."""
