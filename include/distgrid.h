@@ -657,7 +657,9 @@ int dg_delta_rule_fwd(const void *q, uint64_t ldq, const void *k, uint64_t ldk, 
                       size_t saved_bytes, void *ws, size_t ws_bytes, void *stream);
 /* Its backward pass; arguments of the forward pass as they were then, saved as it left it, do_ the gradient of o, ds_last that of s_last (0 if NULL).
  * dq, dk [N, Hk Dk], dv [N, H Dv], dg, dbeta [N, H] and ds0 [n_seq, H, Dk, Dv] (NULL: not wanted; it may be ds_last) are overwritten; rows that no
- * sequence has are left as they are.  Gradients of a key head are summed over the heads that share it.  They must not overlap inputs. */
+ * sequence has are left as they are.  Gradients of a key head are summed over the heads that share it.  They must not overlap inputs.
+ * dg is a sum over the token and up to 63 after it, up to the next that forgets all (where it is 0), of which all but the token's own part cancels: it is off by roundings of
+ * what is added, also where the token's own part is small. */
 int dg_delta_rule_bwd(const void *q, uint64_t ldq, const void *k, uint64_t ldk, const void *v, uint64_t ldv,
                       const float *g, uint64_t ldg, const float *beta, uint64_t ldbeta, uint64_t N, uint32_t n_seq,
                       const uint32_t *first, uint32_t Hk, uint32_t H, uint32_t Dk, uint32_t Dv, uint32_t reverse,

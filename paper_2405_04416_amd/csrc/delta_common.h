@@ -28,6 +28,8 @@ constexpr uint64_t kMostLaunched = 1 << 22;     // workgroups of a launch: its l
 // e^-104 is 0 in fp32: below that a gate is shut.  Logarithms are cut off here so that their differences stay numbers.
 constexpr float kShut = -200.0f;
 __device__ __forceinline__ float cut_off(float g) { return g < kShut ? kShut : g; }     // NaN stays NaN
+// A gate that keeps nothing at all: what comes after it has no part in gradients before it.  That of the gates, a sum of what comes after them of which all but their own part cancels, ends there.
+__device__ __forceinline__ bool keeps_nothing(float g) { return g < -104.0f; }
 
 struct Weights;
 

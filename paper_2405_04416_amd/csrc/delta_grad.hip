@@ -2,7 +2,7 @@
 // and the gradient dR of what they write (U = beta Y): with X = scale D (dO U^T) up to the diagonal, Z = -beta D (dR U^T) below it, D and G of the 64 tokens,
 //   dq = scale e^G dO S^T + X K,    dk = -beta e^G dR S^T + e^(G[last] - G) U dS'^T + X^T Q + Z K + Z^T K,    dv = beta dR,   dbeta = dR Y.
 // With e^-G S for a memory the rule has no decay, values e^-G v and results e^G o: so dG = o do - v dv = q dq - v dv, and dG[last] also the product of the memory
-// behind, e^G[last] S + K^T e^(G[last] - G) U, with dS';  dg[t] = sum of dG from t on.
+// behind, e^G[last] S + K^T e^(G[last] - G) U, with dS';  dg[t] = sum of dG from t on, up to the next gate that keeps nothing.
 //
 // A workgroup takes 64 tokens of a key head, one value head after the other, 32 columns of values at a time through LDS (in pieces, cut once for all), a wavefront
 // 16 tokens and half of the columns of keys: a lane has a token, of which everything above is a column of a product.  X and Z are made once, block by block,
@@ -192,12 +192,14 @@ delta_grad_kernel(Delta d, uint64_t from)
         };
         fetch(0);
         const float rate = there ? d.beta[brought_row * d.ldb + head] : 0.0f;
+        uint64_t shut = 0;                              // tokens whose gates keep nothing
         __syncthreads();                                // what the last head left in LDS has been read
         if (thread < 64) {
             const bool held = lane < count;
             const uint64_t r = row_of(lane);
             const float value = d.g[r * d.ldg + head], b = d.beta[r * d.ldb + head];
             double G = held ? (double)cut_off(value) : 0.0;
+            shut = __ballot(held && keeps_nothing(value));
 #pragma unroll
             for (int s = 1; s < 64; s *= 2) {
                 const double before = __shfl_up(G, s);
@@ -389,12 +391,15 @@ delta_grad_kernel(Delta d, uint64_t from)
             if (lane == 63)
 #pragma unroll
                 for (int w = 0; w < kWaves; ++w) sum += lds.end[w];
+            // up to the next gate that keeps nothing
+            const uint64_t later = lane < 63 ? shut >> (lane + 1) : 0;
+            const uint32_t end = later ? lane + 1 + __builtin_ctzll(later) : 64;
 #pragma unroll
             for (int s = 1; s < 64; s *= 2) {
                 const float after = __shfl_down(sum, s);
-                if (lane + s < 64) sum += after;
+                if (lane + s < end) sum += after;
             }
-            if (lane < count) d.dg[row_of(lane) * d.lddg + head] = sum;
+            if (lane < count) d.dg[row_of(lane) * d.lddg + head] = shut >> lane & 1 ? 0.0f : sum;
         }
     }
     const uint32_t mine = wave * 16 + threadIdx.x % 16, r4 = threadIdx.x % 64 / 16 * 4;

@@ -338,6 +338,7 @@ delta_small_grad_kernel(Delta d, uint64_t from)
             step(dS, a, dr, -a * now.beta * k);
             if (lane % PK == 0) {               // values of v dv lie where dg comes
                 end += lds_end[t][lane / PK] - *dG.p;
+                if (keeps_nothing(now.g)) end = 0.0f;
                 *dG.p = end;
             }
             if (h + 1 < group) lds_k[t][lane] = dk;

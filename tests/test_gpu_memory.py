@@ -1038,6 +1038,31 @@ def test_single_products_are_off_to_either_side(n_seq, S, H, D):
         assert abs(off.mean()) <= 0.26 * U, (n, off.mean() / U)
 
 
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("n_seq,S,Hk,H,D", [(2, 100, 1, 2, 64), (2, 100, 1, 2, 24), (400, 100, 2, 4, 16), (3, 200, 3, 3, 128)])
+def test_gradients_stop_where_all_is_forgotten(n_seq, S, Hk, H, D, reverse):
+    """What comes after a token that keeps nothing has no part in the gradients of the tokens before it: the same bits, whatever it is, and the token's own gate has none."""
+    say("delta rule, gradients before a gate that is shut", n_seq, S, Hk, H, D, reverse)
+    rng = np.random.default_rng(S)
+    N = n_seq * S
+    a = delta_inputs(rng, N, Hk, H, D, D, n_seq, torch.float32, decay=0.05)
+    place = np.arange(S)[::-1] if reverse else np.arange(S)                 # token t of a sequence lies at row place[t]
+    order = lambda x: x.reshape(n_seq, S, -1)[:, place]
+    for t, gate in ((20, -np.inf), (50, -150.0), (90, -104.5)): a["g"].reshape(n_seq, S, H)[:, place[t]] = gate
+    a["ds_last"] *= 1e5
+    for n in ("v", "do"): a[n].reshape(n_seq, S, -1)[:, place[50:]] *= 1e5
+    first = run_delta(a, n_seq, None, torch.float32, reverse=reverse)
+    other = {n: None if x is None else x.copy() for n, x in a.items()}
+    for n in ("q", "k", "v", "do"): other[n].reshape(n_seq, S, -1)[:, place[50:]] = order(a[n])[:, 50:][:, ::-1]
+    other["ds_last"] = other["ds_last"][:, :, ::-1].copy()
+    second = run_delta(other, n_seq, None, torch.float32, reverse=reverse)
+    for n in NAMES[:-1]:
+        x, y = (order(got(r[n])) for r in (first, second))
+        np.testing.assert_array_equal(x[:, :50], y[:, :50], err_msg=n)
+        assert not np.array_equal(x[:, 50:], y[:, 50:])
+    for t in (20, 50, 90): assert not order(got(first["dg"]))[:, t].any()
+
+
 @pytest.mark.parametrize("first", [False, True], ids=["even", "ragged"])
 @pytest.mark.parametrize("n_seq,S,Hk,H,D", [(700, 9, 2, 2, 16), (40, 3, 1, 3, 24), (1300, 70, 2, 4, 32), (9, 40, 2, 2, 64), (2, 300, 1, 3, 100)])
 def test_workspaces_of_exactly_what_is_asked_for(n_seq, S, Hk, H, D, first):
