@@ -592,6 +592,7 @@ int dg_dropout_bwd(const void *dy, uint64_t n, double p, uint64_t seed, uint64_t
 
 /* Root-mean-square norm of N rows of W values after the residual's addition:
  *   t = x + r, rounded to dtype;   y = t s gamma,  s = 1 / sqrt(mean(t^2) + eps).
+ * Squares are added in fp32: a row of values beyond some 1e19, whose sum that leaves, has y = 0.
  * residual NULL: t = x, and total has to be NULL.  total (t) may be NULL, and may be x or residual; y may be x or residual, but not where
  * total is.  gamma [W] fp32; NULL: 1.  Other overlaps of outputs with each other or with inputs are not allowed.
  * Errors: as dg_layer_norm_fwd. */

@@ -3,11 +3,13 @@ import numpy as np
 import pytest
 import torch
 
+import dg_inputs as di
 import oracle
+from paper_2405_04416_amd import binding as B
 from paper_2405_04416_amd.binding import DistGridError
 from paper_2405_04416_amd.memory import EPS, KEY_EPS, DeltaMixer, train_example
 
-from gpu_util import DEV
+from gpu_util import DEV, dev, host, rel_err
 from test_gpu_memory import worth
 from test_gpu_sequence import TYPES, f32, got, rounded, say
 
@@ -214,6 +216,54 @@ def test_more_samples_than_a_product_takes():
         rows = slice(seq * S, (seq + some) * S)
         _, out1 = alone.forward(x[rows].contiguous(), None, g[rows].contiguous(), beta[rows].contiguous(), some)
         for name, a, b in zip(("out", "dx", "dg", "dbeta"), (out1, *alone.backward(None, dout[rows].contiguous())), (out, dx, dg, dbeta)): close(name, a, got(b[rows]), "fp16")
+
+
+def test_block_between_the_encode_and_the_networks():
+    """Features of a hash grid, the samples of a segment one after the other, through the block to the field networks and back to the table: every hand-over against the oracle on
+    what the stage before it gave.  A stage of the field rounds to fp16 some eight times, 2^-11 of values up to twice its result's: 0.01 of it."""
+    say("memory block in the field")
+    rng = np.random.default_rng(6)
+    n_seg, S, field = 41, 32, 0.01
+    N = n_seg * S
+    u = di.make_unit_coords(N, seed=7)
+    growth = B.dg_growth_factor(16, 512, 16)
+    grid, ref_grid = B.dg_grid_desc_init(16, 2, 14, 16, growth, [1.0, 1.0, 1.0]), oracle.grid_init(16, 2, 14, 16, growth, [1.0, 1.0, 1.0])
+    table = di.make_table(ref_grid.n_entries, 2, 1.0, seed=8)
+    order = B.dg_order_desc_init(grid, N)
+    ordered, pieces = torch.zeros(N, 4, device=DEV), torch.zeros(B.dg_order_pieces_words(order, N), dtype=torch.int32, device=DEV)
+    B.dg_order_samples(order, dev(u), N, ordered, pieces, torch.zeros(B.dg_order_workspace_bytes(order) // 4, dtype=torch.int32, device=DEV))
+    feat = torch.empty(N, 32, dtype=torch.float16, device=DEV)
+    B.dg_hashgrid_encode_fwd_ordered(grid, dev(table), ordered, N, feat)
+    block = DeltaMixer(32, 2, d_key=16, d_value=16, dtype=torch.float16, seed=3)
+    block.gamma.copy_(f32(1.0 + 0.3 * rng.standard_normal(32)))
+    length = rng.exponential(size=(N, 1))                           # of steps: what is stored fades with the way
+    g, beta = (-0.2 * np.repeat(length, 2, 1)).astype(np.float32), rng.random((N, 2)).astype(np.float32)
+    t, out = block.forward(feat, None, f32(g), f32(beta), n_seg)
+    y = torch.empty_like(out)
+    B.dg_dropout_fwd(out, t, 0.0, 0, 0, y)                          # the residual's addition
+    zeros = lambda *shape: np.zeros(shape)
+    x64, offsets = got(feat), np.arange(n_seg + 1) * S
+    want = lambda dt, dout: the_oracles(block, x64, zeros(N, 32), g.astype(np.float64), beta.astype(np.float64), offsets, None, dt, dout, None)
+    close("y", y, x64 + want(zeros(N, 32), zeros(N, 32))[1], "fp16")
+    mlp, ref_mlp = B.dg_mlp_desc(32, 64, 16, 16, 64, 2, 1), oracle.mlp_desc(32, 64, 16, 16, 64, 2, 1)
+    weights, dirs = (rng.standard_normal(9408) * 0.2).astype(np.float16), rng.standard_normal((n_seg, 16)).astype(np.float16)
+    dsigma, drgb = rng.standard_normal(N).astype(np.float32) * 0.01, rng.standard_normal((N, 3)).astype(np.float32) * 0.01
+    sigma, rgb, dfeat = torch.zeros(N, device=DEV), torch.zeros(N, 3, device=DEV), torch.zeros(N, 32, device=DEV)
+    dW, largest = torch.zeros(9408, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.dg_mlp_fwd_rows(mlp, dev(weights), y, dev(dirs), None, S, N, sigma, rgb)
+    B.dg_mlp_bwd_rows(mlp, dev(weights), y, dev(dirs), None, S, N, dev(dsigma), dev(drgb), 256.0, 16, dfeat, largest, dW,
+                      torch.zeros(B.dg_mlp_bwd_app_workspace_bytes(mlp, N, S) // 4 + 64, device=DEV))
+    y64, scale = got(y), 64.0
+    w_sigma, w_rgb = oracle.mlp_fwd(ref_mlp, weights, y64, dirs, S)
+    assert rel_err(host(sigma), w_sigma) <= field and rel_err(host(rgb), w_rgb) <= field
+    assert rel_err(host(dfeat), oracle.mlp_bwd(ref_mlp, weights, y64, dirs, S, dsigma, drgb, 256.0)[0]) <= field
+    dy = (dfeat * scale).half()                                     # the networks give their gradient in fp32
+    dx, dg, dbeta = block.backward(dy, dy)
+    _, _, _, w_dx, w_dgamma, w_dg, w_dbeta, _ = want(got(dy), got(dy))
+    for name, value, w in zip(("dx", "dgamma", "dg", "dbeta"), (dx, block.dgamma, dg, dbeta), (w_dx, w_dgamma, w_dg, w_dbeta)): close(name, value, w, "fp16")
+    dtable, ws = torch.zeros(ref_grid.n_entries, 2, device=DEV), torch.zeros(B.dg_hashgrid_encode_bwd_workspace_bytes(grid, N) // 4 + 64, device=DEV)
+    B.dg_hashgrid_encode_bwd(grid, dev(u), (dx.float() / scale).view(N, 16, 2).transpose(0, 1).contiguous(), N, dtable, ws)     # and it is read in planes
+    assert rel_err(host(dtable), oracle.encode_bwd(ref_grid, u, got(dx) / scale)) <= field
 
 
 def test_refusals():
