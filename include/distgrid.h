@@ -620,7 +620,7 @@ int dg_e4m3_rows(const void *x, uint64_t ldx, uint64_t N, uint32_t W, uint32_t d
                  uint8_t *scales, uint64_t lds, void *stream);
 /* Product of rows in 8 bits: y[m, n] = sum over k of a[m, k] b[n, k], what they stand for; a [M, K], b [N, K] (a projection's
  * weights, a row for each output), scales [M or N, ceil(K / 128)].  y [M, N] of type dtype, DG_F16 or DG_BF16: of eight neighbouring
- * products the matrix instruction cuts off what is below 2^-13 of the largest, so that sums are off by some 1e-5, which fp32 would show.  Columns from K on and rows that
+ * products the matrix instruction cuts off what is below 2^-13 of the largest, so that sums are off by some 6e-5 of their size, which fp32 would show.  Columns from K on and rows that
  * are not there are not read.  y must not overlap an input.
  * ws: dg_e4m3_product_workspace_bytes(M, N, K) bytes (NULL where that is 0), 16-byte aligned.
  * Errors: DG_ERR_ARG for K == 0, sides that are not 16-byte aligned or whose ld is no multiple of 16, another dtype;
@@ -640,7 +640,7 @@ int dg_e4m3_product(const void *a, uint64_t lda, const uint8_t *a_scales, uint64
  * saved: NULL, or dg_delta_rule_saved_bytes(N, n_seq, H, Dk, Dv) bytes for the backward pass, 16-byte aligned (what tokens write, and the memories before every
  * 64th).  ws: dg_delta_rule_fwd_workspace_bytes(N, n_seq, H) bytes, 16-byte aligned, are enough for heads of any size; a call needs no more than
  * dg_delta_rule_fwd_least_workspace_bytes(N, n_seq, H, Dk, Dv, saves) (saves: whether `saved` is given), which is 0 (ws may be NULL) for many small heads, and without `saved` for up to four tokens a
- * sequence (N <= 4 n_seq).  dg_delta_rule_workspace_bytes(N, n_seq, Hk, H, Dk, Dv) are enough for either pass; no call needs what another left there.  Long sequences of one length and few heads are worked on in parts.
+ * sequence (N <= 4 n_seq, by the mean: a long one among many short ones goes token by token as well, which takes long).  dg_delta_rule_workspace_bytes(N, n_seq, Hk, H, Dk, Dv) are enough for either pass; no call needs what another left there.  Long sequences of one length and few heads are worked on in parts.
  * Sums and memories are fp32; of a product of two values up to 2^-22 is left out, on either side, before its sum is
  * rounded.  The same call gives the same bits.  Tokens are taken 32 or 64 at a time: an infinity or NaN in a token's row may show in
  * the results of up to 63 tokens before it.  o must not overlap an input.

@@ -1,8 +1,8 @@
 // The gated delta rule: T and P of all chunks of 32 tokens (delta_chunk.h), a workgroup of two wavefronts for each chunk and head, one for T, one for P.
 //   T = (1 + A)^-1 of 32 rows: the two diagonal blocks of 16 by substitution, row by row in the lanes' registers, the block below as -T22 A21 T11.
 // Forward A has beta of its columns (T gives what tokens miss, Y), backward of its rows (T^T gives dR): so neither divides by a rate, which may be 0.
-// Operands come straight from memory and results go straight to the workspace; only the small blocks pass through LDS.  Bound by the substitution, 16 rows that wait for each other, and by the
-// 16 KB that every chunk and head leaves: 65536 tokens x 8 heads of 128 150 us (1.8 TB/s written).
+// Operands come straight from memory and results go straight to the workspace; only the small blocks pass through LDS.  Bound by the substitution, 16 rows that wait for each other, and by
+// memory, 16 KB that every chunk and head leaves and as much that it reads: 65536 tokens x 8 heads of 128 150 us (3.8 TB/s).
 #include "delta_chunk.h"
 
 namespace {
