@@ -12,6 +12,7 @@ distances of samples, and of which it gets the gradients.
 
 Rows are samples, segment after segment: all of one length, or with the offsets `first` that dg_march_segments writes.  A segment can start from the memory in
 which another one ended, as partitions do along a ray.  Every arithmetic step happens inside libdistgrid; this file allocates, slices and calls.
+As RayMixer, the block stands between the encode and the networks in a program of its own: fp16 rows of features go in as they are, and t + out goes to the networks.
 
     python -m paper_2405_04416_amd.memory       trains a block to give back, at the end of each ray, what its samples stored
 """

@@ -31,7 +31,8 @@ def _overlap(a, b):
 
 
 def keep_captured(kept, buffers):
-    """A graph replays with the addresses that it was captured with: the buffers of a pass that is being captured stay, whatever sizes what follows needs."""
+    """A graph replays with the addresses that it was captured with: the buffers of a pass that is being captured stay, whatever sizes what follows needs.
+    A program that parts with its graphs may clear the block's list `captured`."""
     if torch.cuda.is_current_stream_capturing():
         kept.extend(buffers)
 
