@@ -642,7 +642,7 @@ int dg_e4m3_product(const void *a, uint64_t lda, const uint8_t *a_scales, uint64
  * dg_delta_rule_fwd_least_workspace_bytes(N, n_seq, H, Dk, Dv, saves) (saves: whether `saved` is given), which is 0 (ws may be NULL) for many small heads, and without `saved` for up to four tokens a
  * sequence (N <= 4 n_seq, by the mean: a long one among many short ones goes token by token as well, which takes long).  dg_delta_rule_workspace_bytes(N, n_seq, Hk, H, Dk, Dv) are enough for either pass; no call needs what another left there.  Long sequences of one length and few heads are worked on in parts.
  * Sums and memories are fp32; of a product of two values up to 2^-22 is left out, on either side, before its sum is
- * rounded.  The same call gives the same bits.  Tokens are taken 32 or 64 at a time: an infinity or NaN in a token's row may show in
+ * rounded, and what is below 2^-126 (of fp32 values their last eight bits below 2^-110) counts as 0.  The same call gives the same bits.  Tokens are taken 32 or 64 at a time: an infinity or NaN in a token's row may show in
  * the results of up to 63 tokens before it.  o must not overlap an input.
  * Errors: DG_ERR_ARG for heads or sizes of 0, H that Hk does not divide, N that n_seq does not divide (first NULL), a scale that is not finite;
  * DG_ERR_UNSUPPORTED for Dk or Dv above 128, rows 2^24 values or more apart, N > 2^32 - 64, n_seq >= 2^31, H > 2^16, N H > 2^36, n_seq H > 2^32. */
