@@ -247,21 +247,19 @@ delta_bwd_kernel(Delta d, uint32_t with, uint32_t groups, uint64_t from)
 template <class T, int KS>
 void launch_size(Delta d, hipStream_t st)
 {
-    constexpr bool kRoom = kHasRoom<T, KS, true>;
-    const Columns c = columns_of(d, kRoom);
-    if constexpr (kRoom)
-        if (c.helped) {
-            cut(d, side_by_side(sizeof(Helped<T, KS, true, true>)), side_by_side(sizeof(Helped<T, KS, true>)));
-            const uint32_t groups = d.ends_width() / kShared, first = d.n_seq * d.H * (d.parts - 1) * groups, all = d.n_seq * d.H * d.parts * c.groups, threads = kSharedWaves<KS> * 64;
-            if (d.parts > 1) {
-                if (d.vec_all) delta_bwd_shared_kernel<T, KS, true, true><<<first, threads, 0, st>>>(d, groups, 0);
-                else delta_bwd_shared_kernel<T, KS, true, false><<<first, threads, 0, st>>>(d, groups, 0);
-                launch_join(d, d.ds_last, st);
-            }
-            if (d.vec_all) delta_bwd_shared_kernel<T, KS, false, true><<<all, threads, 0, st>>>(d, c.groups, 0);
-            else delta_bwd_shared_kernel<T, KS, false, false><<<all, threads, 0, st>>>(d, c.groups, 0);
-            return;
+    const Columns c = columns_of(d);
+    if (c.helped) {
+        cut(d, side_by_side(sizeof(Helped<T, KS, true, true>)), side_by_side(sizeof(Helped<T, KS, true>)));
+        const uint32_t groups = d.ends_width() / kShared, first = d.n_seq * d.H * (d.parts - 1) * groups, all = d.n_seq * d.H * d.parts * c.groups, threads = kSharedWaves<KS> * 64;
+        if (d.parts > 1) {
+            if (d.vec_all) delta_bwd_shared_kernel<T, KS, true, true><<<first, threads, 0, st>>>(d, groups, 0);
+            else delta_bwd_shared_kernel<T, KS, true, false><<<first, threads, 0, st>>>(d, groups, 0);
+            launch_join(d, d.ds_last, st);
         }
+        if (d.vec_all) delta_bwd_shared_kernel<T, KS, false, true><<<all, threads, 0, st>>>(d, c.groups, 0);
+        else delta_bwd_shared_kernel<T, KS, false, false><<<all, threads, 0, st>>>(d, c.groups, 0);
+        return;
+    }
     const uint64_t units = (uint64_t)d.n_seq * d.H * c.groups;
     for (uint64_t from = 0; from < units; from += kMostLaunched) {
         const uint32_t grid = (uint32_t)(units - from < kMostLaunched ? units - from : kMostLaunched);

@@ -100,12 +100,12 @@ struct Operands {
     Keys<T, KS, kQ> key;
 };
 
-// Buffers: two if they fit, so that a chunk's operands come while the one before is worked on
+// Two buffers, so that a chunk's operands come while the one before is worked on
 template <class T, int KS>
 struct Room {
-    static constexpr int kBuffers = 2 * sizeof(Operands<T, KS>) <= 160 * 1024 ? 2 : 1;
-    Operands<T, KS> ops[kBuffers];
+    Operands<T, KS> ops[2];
 };
+static_assert(sizeof(Room<float, 4>) <= 160 * 1024, "the largest has room");
 
 // eight values of a token
 template <int n, int KS>
@@ -225,7 +225,6 @@ struct Rows {
 template <class T, int KS, bool kBackward, bool kVec, class Use>
 __device__ __forceinline__ void along(const Delta &d, const Span &span, uint32_t seq, uint32_t head, Room<T, KS> &room, uint32_t wave, uint32_t waves, Use use)
 {
-    constexpr int kBuffers = Room<T, KS>::kBuffers;
     const uint32_t chunks = (span.len + kChunk - 1) / kChunk, hk = head / (d.H / d.Hk);
     if (chunks == 0) return;
     const uint64_t slot0 = first_chunk(span, seq);
@@ -234,7 +233,7 @@ __device__ __forceinline__ void along(const Delta &d, const Span &span, uint32_t
     Fetched<T, 2, kVec> fetched;
     auto weights = [&](uint32_t i) {
         const uint8_t *from = (const uint8_t *)(d.weights + (slot0 + chunk(i)) * d.H + head) + threadIdx.x % 64 * 16;
-        uint8_t *to = (uint8_t *)&room.ops[i % kBuffers].weight;
+        uint8_t *to = (uint8_t *)&room.ops[i % 2].weight;
         for (uint32_t at = wave * kPage; at < sizeof(Weights); at += waves * kPage)
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)(from + at), (__attribute__((address_space(3))) uint32_t *)(to + at), 16, 0, 0);
     };
@@ -247,14 +246,10 @@ __device__ __forceinline__ void along(const Delta &d, const Span &span, uint32_t
         const bool more = i + 1 < chunks;
         if (more) {
             rows.fetch(chunk(i + 1), fetched);
-            if (kBuffers == 2) weights(i + 1);
+            weights(i + 1);
         }
-        use(room.ops[i % kBuffers], chunk(i));
-        if (kBuffers == 1) {
-            __syncthreads();
-            if (more) weights(i + 1);
-        }
-        if (more) rows.store(chunk(i + 1), fetched, room.ops[(i + 1) % kBuffers].key);
+        use(room.ops[i % 2], chunk(i));
+        if (more) rows.store(chunk(i + 1), fetched, room.ops[(i + 1) % 2].key);
     }
 }
 
@@ -331,8 +326,7 @@ struct Helped {
     Tile<T> tiles[2];
     Shares<KS, kBackward, kEnds> shares;
 };
-template <class T, int KS, bool kBackward>
-constexpr bool kHasRoom = sizeof(Helped<T, KS, kBackward>) <= 160 * 1024;
+static_assert(sizeof(Helped<float, 4, false>) <= 160 * 1024 && sizeof(Helped<float, 4, true>) <= 160 * 1024, "the largest has room");
 
 template <class T, int KS, bool kBackward, bool kQ, bool kVec>
 struct Helper {
@@ -528,11 +522,11 @@ inline void cut(Delta &d, uint32_t per_first, uint32_t per_second)
 struct Columns { uint32_t with, waves, groups; bool helped; };
 
 // With fewer heads than the chip has room for, wavefronts share columns; otherwise each has 16 of its own, as many as possible to a workgroup, and all bring operands.
-inline Columns columns_of(const Delta &d, bool room)
+inline Columns columns_of(const Delta &d)
 {
     const uint32_t all = (d.Dv + 15) / 16, least = d.Dk <= 32 ? 1 : d.Dk <= 64 ? 2 : 4;
     const uint64_t units = (uint64_t)d.n_seq * d.H;
-    if (room && units * all <= (d.Dk > 64 && d.vec_all ? kFewLargeColumns : kFewColumns)) return {1, 0, all, true};
+    if (units * all <= (d.Dk > 64 && d.vec_all ? kFewLargeColumns : kFewColumns)) return {1, 0, all, true};
     uint32_t with = all < (uint32_t)kMostWaves ? all : kMostWaves;
     while (with > 1 && units * ((all + with - 1) / with) < 256) with = (with + 1) / 2;        // few heads: as many workgroups as there are compute units
     return {with, with < least ? least : with, (all + with - 1) / with, false};
